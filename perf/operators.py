@@ -425,7 +425,7 @@ def run(state):
     out = [r.logprob, r.entropy, r.lse]
     if kind == "logprobs":
         return out + ([r.top_ids, r.top_logprobs] if state["top"] else [])
-    return out + [logprobs.token_logprobs_grad(state["logits"], state["target"], r.lse, r.entropy, state["g_logprob"],
+    return out + [logprobs.token_logprobs_grad(state["logits"], state["target"], r.row_stats, r.entropy, state["g_logprob"],
                                                state["g_entropy"], scale=state["scale"])]
 
 
