@@ -26,7 +26,9 @@ EXPORTS = [
     "jf_save_weights", "jf_get_weights", "jf_prefill", "jf_truncate", "jf_seq_len", "jf_jacobi_step",
     "jf_forward_logits", "jf_generate", "jf_generate_device", "jf_set_profiling", "jf_kernel_time",
     "jf_op_gemm_workspace_bytes", "jf_op_gemm", "jf_op_gemm_noalloc", "jf_tl_enable", "jf_trajectory_noisy_blocks",
-    "jf_set_wait_limit", "jf_wait_limit_probe",
+    "jf_set_wait_limit", "jf_wait_limit_probe", "jf_op_kv8_append", "jf_op_kv8_read",
+    "jf_op_kv8_attention_workspace_bytes", "jf_op_kv8_attention", "jf_op_token_logprobs_workspace_bytes",
+    "jf_op_token_logprobs", "jf_op_token_logprobs_grad",
 ]
 JF_OP_GEMM_NOALLOC_SCRATCH_BYTES = 8 << 20
 
@@ -69,6 +71,16 @@ class GenStats(C.Structure):
                 ("traj_cap", C.c_int), ("traj_rows", C.c_int), ("traj_iters", C.c_int)]
 
 
+class Kv8Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("page_table", C.c_void_p), ("n_seqs", C.c_int), ("n_pages", C.c_int), ("pages_per_seq", C.c_int),
+                ("n_kv_heads", C.c_int), ("head_dim", C.c_int)]
+
+
+class Kv8Rows(C.Structure):
+    _fields_ = [("row_start", C.c_void_p), ("len", C.c_void_p), ("n_rows", C.c_int), ("max_rows", C.c_int)]
+
+
 _lib = None
 
 
@@ -108,6 +120,15 @@ def load():
     L.jf_trajectory_noisy_blocks.argtypes = [vp, i32, i32, i32, vp, i32, i32, i32, i32, vp, vp, vp]
     L.jf_set_wait_limit.argtypes = [vp, C.c_uint64]
     L.jf_wait_limit_probe.argtypes = [vp, P(C.c_uint64)]
+    ll, f32 = C.c_longlong, C.c_float
+    kc, kr = P(Kv8Cache), P(Kv8Rows)
+    L.jf_op_kv8_append.argtypes = [kc, kr, i32, vp, ll, vp, ll, vp, ll, i32, vp, vp, i32, i32, vp, vp, vp]
+    L.jf_op_kv8_read.argtypes = [kc, kr, i32, vp, vp, vp, vp]
+    L.jf_op_kv8_attention_workspace_bytes.argtypes = [kc, kr, i32, i32, P(C.c_size_t)]
+    L.jf_op_kv8_attention.argtypes = [kc, kr, i32, vp, ll, i32, f32, vp, i32, vp, vp, vp, C.c_size_t, vp, vp]
+    L.jf_op_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, P(C.c_size_t)]
+    L.jf_op_token_logprobs.argtypes = [i32, vp, ll, i32, i32, f32, vp, vp, vp, vp, vp, i32, vp, vp, vp, C.c_size_t, vp, vp]
+    L.jf_op_token_logprobs_grad.argtypes = [i32, vp, ll, i32, i32, f32, vp, vp, vp, vp, vp, vp, ll, vp, vp]
     for name in EXPORTS:
         f = getattr(L, name)
         if name not in ("jf_destroy", "jf_last_error"):

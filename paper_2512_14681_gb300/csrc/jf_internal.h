@@ -16,6 +16,7 @@ enum DeviceError : int {
   JF_DERR_BOUNDS = 4,        // a page-table / token / position index was out of range
   JF_DERR_STATE = 5,         // inconsistent decode state detected on the device
   JF_DERR_TIMEOUT_PROBE = 6, // the wait-limit probe's wait ran out (its intended outcome)
+  JF_DERR_NONFINITE = 7,     // a value appended to an 8-bit cache was infinite or not a number
 };
 
 // Default limit of every bounded device wait: far beyond any legitimate wait. A context's limit

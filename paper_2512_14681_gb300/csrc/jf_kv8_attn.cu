@@ -1,0 +1,647 @@
+// Attention of a batch's new rows over the 8-bit paged cache (jf_ops.h: jf_op_kv8_attention).
+//
+// With q scaled by a power of two per row so that its largest magnitude lies in [2^14, 2^15), codes c_k, c_v and
+// block exponents e_k, e_v, a key's score in the log2 domain is s = (q . c_k) 2^(e_k) f, f the row's factor (the
+// scaling undone, the softmax scale, log2 e), and
+//   out = sum_j 2^(s_j - m) 2^(e_v_j) c_v_j / sum_j 2^(s_j - m).
+// Codes are exact in fp16, so both products run on fp16 operands with fp32 sums. The values' exponents go into
+// the probabilities: p' = 2^(s - m) 2^(e_v - E) in fp16, against a running reference E in whose unit the output
+// accumulates; E follows e_v only when the difference leaves a range in which fp16 keeps p' as well as it keeps p.
+//
+// Work is split evenly whatever the batch: a unit is (sequence, KV head, tile of (token, head) query rows), a
+// chunk a run of keys of one unit, and CTA i of N takes chunks [T i / N, T (i + 1) / N) of all T. A unit that
+// one CTA holds entirely is finished there; of the others each CTA leaves a partial state (m, l, O) in the
+// workspace, at most two a CTA, and k_kv8_combine joins a row's states in CTA order.
+#include "../../include/jf_ops.h"
+#include "jf_kv8.cuh"
+#include "jf_once.h"
+
+namespace jf {
+namespace {
+
+struct Kv8AttnParams {
+  jf_kv8_cache c;
+  jf_kv8_rows r;
+  const void* q;
+  long long ld_q;
+  int n_heads;
+  float scale_log2;  // softmax scale * log2 e
+  const uint32_t* mask;
+  int mask_words;
+  void* out;
+  float* lse;
+  long long* plan;   // [n_seqs + 1]: chunks of the sequences before b
+  float* states;     // [2 N][tile rows x hd O, then m, then l]
+  int* err;
+};
+
+// 2^x by the MUFU ex2 instruction (flushes results below 2^-126 to zero; 2^-inf = 0).
+JF_DEV float ex2_ftz(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+JF_DEV uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+JF_DEV float2 unpack_f16(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+
+// ---------------------------------------------------------------------------------------------
+// The plan: which chunks there are. TR: query rows of a tile, CH: keys of a chunk.
+// ---------------------------------------------------------------------------------------------
+template <int TR, int CH>
+struct Plan {
+  // Chunks of one tile of a sequence's rows.
+  static JF_DEV int chunks(const Kv8AttnParams& a, const Kv8Seq& s, int G, int tile) {
+    const int last = a.mask ? s.n - 1 : min(s.n - 1, ((tile + 1) * TR - 1) / G);  // a masked row may see any new row
+    return (s.len + last + CH) / CH;
+  }
+  static JF_DEV int tiles(const Kv8Seq& s, int G) { return (int)(((long long)s.n * G + TR - 1) / TR); }
+  // Chunks of a sequence's units, per KV head.
+  static JF_DEV long long per_head(const Kv8AttnParams& a, const Kv8Seq& s, int G) {
+    const int n = tiles(s, G);
+    if (a.mask) return n > 0 ? (long long)n * chunks(a, s, G, 0) : 0;
+    long long sum = 0;
+    for (int t = 0; t < n; ++t) sum += chunks(a, s, G, t);
+    return sum;
+  }
+  // pre[b] = chunks of the sequences before b, pre[n_seqs] = T; by the whole CTA (ends with a barrier).
+  static JF_DEV void build(const Kv8AttnParams& a, int G, long long* pre) {
+    for (int b = threadIdx.x; b < a.c.n_seqs; b += blockDim.x)
+      pre[b + 1] = per_head(a, kv8_seq(a.c, a.r, b, a.err), G) * a.c.n_kv_heads;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+      const int lane = threadIdx.x;
+      long long base = 0;
+      if (lane == 0) pre[0] = 0;
+      for (int b0 = 0; b0 < a.c.n_seqs; b0 += 32) {
+        const int b = b0 + lane;
+        long long v = b < a.c.n_seqs ? pre[b + 1] : 0;
+#pragma unroll
+        for (int sh = 1; sh < 32; sh <<= 1) {
+          const long long u = __shfl_up_sync(0xffffffffu, v, sh);
+          if (lane >= sh) v += u;
+        }
+        if (b < a.c.n_seqs) pre[b + 1] = base + v;
+        base += __shfl_sync(0xffffffffu, v, 31);
+      }
+    }
+    __syncthreads();
+  }
+};
+
+JF_DEV long long share_begin(long long total, int i, int n) { return total * i / n; }
+// The CTA that holds chunk x of `total`: the last i with share_begin(i) <= x.
+JF_DEV int share_of(long long total, long long x, int n) {
+  int i = (int)((x * n + n - 1) / total);
+  while (i > 0 && share_begin(total, i, n) > x) --i;
+  while (i + 1 < n && share_begin(total, i + 1, n) <= x) ++i;
+  return i;
+}
+// Where CTA i leaves its part of a unit whose chunks begin at `first`: a CTA has at most one unit that began
+// before its share and one that goes on after it.
+JF_DEV int state_slot(long long total, long long first, int i, int n) { return 2 * i + (share_begin(total, i, n) > first ? 0 : 1); }
+
+// A CTA's walk over the units of its share. Uniform over the CTA.
+template <int TR, int CH>
+struct Walk {
+  long long at, end, first;  // chunks of the whole batch: the next one, the end of the share, the unit's first
+  int b, kvh, tile, n_chunks;
+  Kv8Seq s;
+
+  JF_DEV void start(const Kv8AttnParams& a, const long long* pre, int G, long long at_, long long end_) {
+    at = at_;
+    end = end_;
+    int lo = 0, hi = a.c.n_seqs;  // the last b with pre[b] <= at (then pre[b + 1] > at)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (pre[mid] <= at) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    s = kv8_seq(a.c, a.r, b, a.err);
+    const long long head = (pre[b + 1] - pre[b]) / a.c.n_kv_heads, off = at - pre[b];
+    kvh = (int)(off / head);
+    long long rest = off - kvh * head;
+    tile = 0;
+    while (rest >= (n_chunks = Plan<TR, CH>::chunks(a, s, G, tile))) {
+      rest -= n_chunks;
+      ++tile;
+    }
+    first = at - rest;
+  }
+  // To the unit that begins where this one ends (at == first + n_chunks < end).
+  JF_DEV void next(const Kv8AttnParams& a, int G) {
+    first = at;
+    if (++tile == Plan<TR, CH>::tiles(s, G)) {
+      tile = 0;
+      if (++kvh == a.c.n_kv_heads) {
+        kvh = 0;
+        do s = kv8_seq(a.c, a.r, ++b, a.err);
+        while (s.n == 0);
+      }
+    }
+    n_chunks = Plan<TR, CH>::chunks(a, s, G, tile);
+  }
+};
+
+// Whether new row i of the sequence sees slot kp (>= len).
+JF_DEV bool sees_new(const Kv8AttnParams& a, const Kv8Seq& s, int i, int kp) {
+  const int j = kp - s.len;
+  if (!a.mask) return j <= i;
+  return j < s.n && (a.mask[(long long)(s.row0 + i) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
+}
+
+template <typename T>
+JF_DEV float load_q(const T* p) { return act_to_f32(*p); }
+
+JF_DEV void store2(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
+JF_DEV void store2(bf16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
+
+// Power of two that brings a row's largest magnitude into [2^14, 2^15), as an exponent (0 for a row of zeros or
+// one that holds an infinity).
+JF_DEV int query_shift(float amax) {
+  const int x = __float_as_int(amax) >> 23;
+  return x == 0 || x == 255 ? (x == 0 && amax > 0.f ? 126 : 0) : min(14 - (x - 127), 126);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Few query rows per KV head (single-token serving; fp32 at any row count): warp-level products.
+//
+// A CTA's four warps share a tile of 16 query rows; each takes one page (16 keys) of a 64-key chunk at a time and
+// keeps its own softmax state; the four states are joined when the unit's share ends. A warp streams its pages
+// through a ring of its own in shared memory (cp.async, 16-byte pieces swizzled so that both fragment loads are
+// free of bank conflicts), so no barrier stands between loads and products.
+//
+// m16n8k16 fragments, lane = 4 g + t. S = Q K^T contracts over dims, whose order is free as long as Q's follows
+// it: lane t's four values of each k-step are four consecutive dims (one 32-bit word of codes) of the 16-byte
+// pieces PK t .. PK t + PK - 1 of keys g and g + 8. O = P V: lane (g, t) holds keys 2t, 2t + 1, 2t + 8, 2t + 9 of P
+// as it held their scores, and needs these keys' codes at dims NT g + j, j = 0 .. NT - 1, of the n-tiles j.
+// NS: fp16 terms of queries and probabilities (1 for bf16 models, 2 for fp32).
+// ---------------------------------------------------------------------------------------------
+constexpr int W_WARPS = 4, W_TR = 16, W_CH = W_WARPS * kPage;
+constexpr int W_STAGES = 4;
+constexpr float W_LAG = 4.f;             // a row's reference maximum follows its scores when they exceed it by more
+constexpr int W_EV_SET = 5, W_EV_MAX = 10;  // e_v - E: where E is set, largest (p' <= 2^14); smallest 0
+
+template <int HD>
+constexpr int w_smem() {
+  const int ring = W_WARPS * W_STAGES * 2 * kPage * HD, join = W_WARPS * W_TR * (HD + 4) * 4;
+  return ring > join ? ring : join;
+}
+
+JF_DEV void cp_async16_zfill(uint32_t dst, const void* src, bool valid) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+}
+
+// Byte offset of 16-byte piece c of row r of a page in a warp's ring.
+template <int HD>
+JF_DEV int w_piece(int r, int c) {
+  return HD == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ (r >> 1 & 3)) << 4);
+}
+
+JF_DEV void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <typename T, int HD, int NS>
+__global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows(const Kv8AttnParams a) {
+  constexpr int KS = HD / 16;   // k-steps of S
+  constexpr int NT = HD / 8;    // n-tiles of O
+  constexpr int PK = HD / 64;   // 16-byte pieces of a key that a lane reads
+  constexpr int PAGE_BYTES = kPage * HD;
+  extern __shared__ __align__(128) uint8_t sm[];
+  __shared__ long long pre[kKv8MaxSeqs + 1];
+  __shared__ float s_ml[W_WARPS][W_TR][3];  // m, l, E as 2^E's exponent
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int G = a.n_heads / a.c.n_kv_heads, Hkv = a.c.n_kv_heads;
+  pdl_launch_dependents();
+  pdl_wait();
+  using P = Plan<W_TR, W_CH>;
+  P::build(a, G, pre);
+  const long long total = pre[a.c.n_seqs];
+  if (blockIdx.x == 0)
+    for (int b = tid; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
+  Walk<W_TR, W_CH> w;
+  {
+    const long long lo = share_begin(total, blockIdx.x, gridDim.x), hi = share_begin(total, blockIdx.x + 1, gridDim.x);
+    if (lo >= hi) return;
+    w.start(a, pre, G, lo, hi);
+  }
+  const uint32_t ring = smem_u32(sm) + warp * (W_STAGES * 2 * PAGE_BYTES);
+  const uint8_t *Kc = reinterpret_cast<const uint8_t*>(a.c.k), *Vc = reinterpret_cast<const uint8_t*>(a.c.v);
+
+  while (true) {
+    const Kv8Seq s = w.s;
+    const int c0 = (int)(w.at - w.first), c1 = (int)min((long long)w.n_chunks, w.end - w.first);
+    const int keys = s.len + s.n;  // slots that hold a token
+    const int rows = s.n * G, r0 = w.tile * W_TR;
+    // ---- queries: fragments of this lane's rows g, g + 8, scaled
+    uint32_t qf[NS][KS][4];
+    float f[2];
+    {
+      const T* Q = reinterpret_cast<const T*>(a.q);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int row = r0 + g + 8 * i;
+        const bool live = row < rows;
+        const T* src = Q + (long long)(s.row0 + (live ? row / G : 0)) * a.ld_q + (long long)(w.kvh * G + (live ? row % G : 0)) * HD + PK * 16 * t;
+        float x[4 * KS];
+        float amax = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4 * KS; ++j) {
+          x[j] = live ? load_q(src + j) : 0.f;
+          amax = fmaxf(amax, fabsf(x[j]));
+        }
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+        const int sh = query_shift(amax);
+        const float up = pow2i(sh);
+        f[i] = pow2i(-sh) * a.scale_log2;
+#pragma unroll
+        for (int j = 0; j < KS; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float lo = x[4 * j + 2 * h] * up, hi = x[4 * j + 2 * h + 1] * up;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+              qf[n][j][2 * h + i] = pack_f16(lo, hi);
+              const float2 got = unpack_f16(qf[n][j][2 * h + i]);
+              lo -= got.x;
+              hi -= got.y;
+            }
+          }
+      }
+    }
+    float o[NT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    int E = 0;  // o is in units of 2^E; set by the first page
+    bool have_E = false;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
+    const int tok[2] = {min(r0 + g, rows - 1) / G, min(r0 + g + 8, rows - 1) / G};  // of the lane's rows
+
+    // ---- this warp's pages: page index W_WARPS c + warp of each chunk c, up to the last one that holds a token
+    const int p_first = c0 * W_WARPS + warp;
+    const int p_end = min(c1 * W_WARPS, (keys + kPage - 1) / kPage);
+    const int n_pages = p_end > p_first ? (p_end - p_first + W_WARPS - 1) / W_WARPS : 0;
+    int id_l = -1, e_l = 0, e_cur = 0;  // lane j: page 32 i + j: id, exponents of K and V packed; of the pages in use
+    auto fetch_ids = [&](int i0) {      // 32 pages from the warp's i0'th on
+      id_l = -1;
+      e_l = 0;
+      const int i = i0 + lane;
+      if (i < n_pages) {
+        id_l = kv8_page(a.c, w.b, p_first + i * W_WARPS, a.err);
+        if (id_l >= 0) {
+          const long long blk = (long long)id_l * Hkv + w.kvh;
+          e_l = (int)(uint8_t)a.c.k_exp[blk] | (int)(uint8_t)a.c.v_exp[blk] << 8;
+        }
+      }
+    };
+    auto issue = [&](int i) {  // loads of the warp's i'th page (zeros for slots without a token)
+      if (i < n_pages) {
+        if ((i & 31) == 0) fetch_ids(i);
+        const int id = __shfl_sync(0xffffffffu, id_l, i & 31);
+        const int slot0 = (p_first + i * W_WARPS) * kPage;
+        const long long off = ((long long)max(id, 0) * Hkv + w.kvh) * PAGE_BYTES;
+        const uint32_t dst = ring + (i % W_STAGES) * (2 * PAGE_BYTES);
+#pragma unroll
+        for (int j = 0; j < PAGE_BYTES / 512; ++j) {
+          const int piece = j * 32 + lane, r = piece / (HD / 16), c = piece % (HD / 16);
+          const bool in = id >= 0 && slot0 + r < keys;
+          cp_async16_zfill(dst + w_piece<HD>(r, c), Kc + off + piece * 16, in);
+          cp_async16_zfill(dst + PAGE_BYTES + w_piece<HD>(r, c), Vc + off + piece * 16, in);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int i = 0; i < W_STAGES - 1; ++i) issue(i);
+    for (int i = 0; i < n_pages; ++i) {
+      if ((i & 31) == 0) e_cur = e_l;  // (the next 32 pages' are fetched later in this group)
+      asm volatile("cp.async.wait_group %0;" ::"n"(W_STAGES - 2) : "memory");
+      __syncwarp();  // every lane's pieces of page i; and every lane is done with the stage that is loaded next
+      issue(i + W_STAGES - 1);
+      const int e2 = __shfl_sync(0xffffffffu, e_cur, i & 31);
+      const int ek = (int)(int8_t)(e2 & 0xff), ev = (int)(int8_t)(e2 >> 8);
+      const uint32_t sk = ring + (i % W_STAGES) * (2 * PAGE_BYTES), sv = sk + PAGE_BYTES;
+      // ---- S: two n-tiles of 8 keys
+      float sc[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[n][k] = 0.f;
+#pragma unroll
+        for (int pc = 0; pc < PK; ++pc) {
+          uint32_t wd[4];
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3])
+                       : "r"(sk + w_piece<HD>(g + 8 * n, PK * t + pc))
+                       : "memory");
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t b0 = e4m3x2_to_f16x2(wd[k]), b1 = e4m3x2_to_f16x2(wd[k] >> 16);
+#pragma unroll
+            for (int x = 0; x < NS; ++x) mma_f16(sc[n], qf[x][pc * 4 + k], b0, b1);
+          }
+        }
+      }
+      const float fu[2] = {pow2i(ek) * f[0], pow2i(ek) * f[1]};
+      const int kp0 = (p_first + i * W_WARPS) * kPage;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[n][k] *= fu[k >> 1];
+      if (kp0 + kPage > s.len) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int kp = kp0 + 8 * n + 2 * t + (k & 1);
+            if (kp >= s.len && !(kp < keys && sees_new(a, s, tok[k >> 1], kp))) sc[n][k] = -INFINITY;
+          }
+      }
+      // ---- reference maxima (rows g, g + 8) and the reference exponent, raised for the whole warp together
+      const float mx[2] = {fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1])),
+                           fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]))};
+      const bool far_E = !have_E || ev - E > W_EV_MAX || ev < E;
+      if (__any_sync(0xffffffffu, mx[0] > m[0] + W_LAG || mx[1] > m[1] + W_LAG) || far_E) {
+        float al[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float x = fmaxf(mx[k], __shfl_xor_sync(0xffffffffu, mx[k], 1));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+          const float mn = fmaxf(m[k], x);
+          al[k] = m[k] == -INFINITY ? 0.f : ex2_ftz(m[k] - mn);
+          m[k] = mn;
+          l[k] *= al[k];
+        }
+        if (far_E) {
+          const int E2 = ev - W_EV_SET;
+          // (a step beyond 2^+-126: what was summed is out of the new unit's reach one way or the other)
+          const float step = have_E ? pow2i(max(-126, min(126, E - E2))) : 0.f;
+          al[0] *= step;
+          al[1] *= step;
+          E = E2;
+          have_E = true;
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[j][k] *= al[k >> 1];
+      }
+      // ---- P, then O += P V
+      const float nb[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
+      const float up = pow2i(ev - E);
+      uint32_t pf[NS][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float p0 = ex2_ftz(sc[n][2 * k] + nb[k]), p1 = ex2_ftz(sc[n][2 * k + 1] + nb[k]);
+          l[k] += p0 + p1;
+          float lo = p0 * up, hi = p1 * up;
+#pragma unroll
+          for (int x = 0; x < NS; ++x) {
+            pf[x][2 * n + k] = pack_f16(lo, hi);
+            const float2 got = unpack_f16(pf[x][2 * n + k]);
+            lo -= got.x;
+            hi -= got.y;
+          }
+        }
+      // codes of the lane's four keys at NT consecutive dims, as pairs of keys
+      uint32_t vw[4][NT / 4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int key = 2 * t + (k & 1) + 8 * (k >> 1);
+        if constexpr (HD == 128)
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                       : "=r"(vw[k][0]), "=r"(vw[k][1]), "=r"(vw[k][2]), "=r"(vw[k][3])
+                       : "r"(sv + w_piece<HD>(key, g))
+                       : "memory");
+        else
+          asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];"
+                       : "=r"(vw[k][0]), "=r"(vw[k][1])
+                       : "r"(sv + w_piece<HD>(key, g >> 1) + (g & 1) * 8)
+                       : "memory");
+      }
+#pragma unroll
+      for (int q = 0; q < NT / 4; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t sel = h ? 0x7362u : 0x5140u;
+          const uint32_t c0w = __byte_perm(vw[0][q], vw[1][q], sel), c1w = __byte_perm(vw[2][q], vw[3][q], sel);
+#pragma unroll
+          for (int x = 0; x < NS; ++x) {
+            mma_f16(o[4 * q + 2 * h], pf[x], e4m3x2_to_f16x2(c0w), e4m3x2_to_f16x2(c1w));
+            mma_f16(o[4 * q + 2 * h + 1], pf[x], e4m3x2_to_f16x2(c0w >> 16), e4m3x2_to_f16x2(c1w >> 16));
+          }
+        }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    // ---- join the four warps' states
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
+      l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
+    }
+    __syncthreads();  // every warp is done with its ring
+    float* so = reinterpret_cast<float*>(sm) + warp * (W_TR * (HD + 4));
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) so[(g + 8 * (k >> 1)) * (HD + 4) + NT * ((2 * t + (k & 1))) + j] = o[j][k];
+    if (t == 0) {
+      s_ml[warp][g][0] = m[0], s_ml[warp][g][1] = l[0], s_ml[warp][g][2] = (float)E;
+      s_ml[warp][g + 8][0] = m[1], s_ml[warp][g + 8][1] = l[1], s_ml[warp][g + 8][2] = (float)E;
+    }
+    __syncthreads();
+    const bool whole = c0 == 0 && c1 == w.n_chunks;
+    float* st = a.states + (long long)state_slot(total, w.first, blockIdx.x, gridDim.x) * (W_TR * (HD + 2));
+    for (int i = tid; i < W_TR * (HD / 2); i += 32 * W_WARPS) {
+      const int r = i / (HD / 2), d = i % (HD / 2) * 2, row = r0 + r;
+      if (row >= rows) break;
+      float M = -INFINITY;
+#pragma unroll
+      for (int q = 0; q < W_WARPS; ++q) M = fmaxf(M, s_ml[q][r][0]);
+      float L = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+      for (int q = 0; q < W_WARPS; ++q) {
+        const float wt = s_ml[q][r][0] == -INFINITY ? 0.f : exp2f(s_ml[q][r][0] - M);
+        L = fmaf(wt, s_ml[q][r][1], L);
+        const float wo = wt * pow2i((int)s_ml[q][r][2]);
+        const float* src = reinterpret_cast<float*>(sm) + q * (W_TR * (HD + 4)) + r * (HD + 4) + d;
+        if (wt != 0.f) x = fmaf(wo, src[0], x), y = fmaf(wo, src[1], y);
+      }
+      if (whole) {
+        const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+        const long long at = (long long)(s.row0 + row / G) * a.n_heads + w.kvh * G + row % G;
+        store2(reinterpret_cast<T*>(a.out) + at * HD + d, x * il, y * il);
+        if (a.lse && d == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+      } else {
+        store2(st + r * HD + d, x, y);
+        if (d == 0) st[W_TR * HD + r] = M, st[W_TR * (HD + 1) + r] = L;
+      }
+    }
+    w.at = w.first + c1;
+    if (w.at >= w.end) return;
+    __syncthreads();
+    w.next(a, G);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Joins the partial states of the units that several CTAs share: one warp per (row, query head). n: CTAs of the
+// kernel that left them.
+// ---------------------------------------------------------------------------------------------
+template <typename T, int HD, int TR, int CH>
+__global__ void __launch_bounds__(256) k_kv8_combine(const Kv8AttnParams a, int n) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int G = a.n_heads / a.c.n_kv_heads;
+  if (i >= (long long)a.r.n_rows * a.n_heads) return;
+  const int row = (int)(i / a.n_heads), head = (int)(i % a.n_heads);
+  // the sequence of the row
+  int lo = 0, m = a.c.n_seqs;
+  while (m > 1) {
+    const int step = (m + 31) / 32, b = lo + lane * step;
+    const unsigned hits = __ballot_sync(0xffffffffu, lane * step < m && a.r.row_start[b] <= row);
+    const int k = hits ? 31 - __clz(hits) : 0;
+    lo += k * step;
+    m = min(step, m - k * step);
+  }
+  const Kv8Seq s = kv8_seq(a.c, a.r, lo, a.err);
+  if (row < s.row0 || row >= s.row0 + s.n) return;
+  const int tr = (row - s.row0) * G + head % G, tile = tr / TR, r = tr % TR;
+  const long long total = a.plan[a.c.n_seqs], base = a.plan[lo], per_head = (a.plan[lo + 1] - base) / a.c.n_kv_heads;
+  using P = Plan<TR, CH>;
+  long long before = 0;
+  for (int t = lane; t < tile; t += 32) before += P::chunks(a, s, G, t);
+#pragma unroll
+  for (int sh = 16; sh > 0; sh >>= 1) before += __shfl_xor_sync(0xffffffffu, before, sh);
+  const long long first = base + head / G * per_head + before, end = first + P::chunks(a, s, G, tile);
+  const int i0 = share_of(total, first, n), i1 = share_of(total, end - 1, n);
+  if (i0 == i1) return;  // finished by the one CTA that held it
+  constexpr int D = HD / 32;
+  float M = -INFINITY, L = 0.f, o[D];
+#pragma unroll
+  for (int j = 0; j < D; ++j) o[j] = 0.f;
+  // (CTAs without a chunk lie between others only when there are fewer chunks than CTAs: they left nothing)
+  for (int c = i0; c <= i1; ++c) {
+    if (share_begin(total, c, n) == share_begin(total, c + 1, n)) continue;
+    const float* st = a.states + (long long)state_slot(total, first, c, n) * (TR * (HD + 2));
+    const float mc = st[TR * HD + r], lc = st[TR * (HD + 1) + r];
+    const float mn = fmaxf(M, mc);
+    const float wa = M == -INFINITY ? 0.f : exp2f(M - mn), wb = mc == -INFINITY ? 0.f : exp2f(mc - mn);
+    L = wa * L + wb * lc;
+#pragma unroll
+    for (int j = 0; j < D; ++j) o[j] = wa * o[j] + wb * st[r * HD + D * lane + j];
+    M = mn;
+  }
+  const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+  T* dst = reinterpret_cast<T*>(a.out) + i * HD + D * lane;
+#pragma unroll
+  for (int j = 0; j < D; j += 2) store2(dst + j, o[j] * il, o[j + 1] * il);
+  if (a.lse && lane == 0) a.lse[i] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+}
+
+struct DeviceInfo {
+  int sms, rows_ctas[4];  // resident CTAs of k_kv8_attn_rows per SM: bf16 64 / 128, fp32 64 / 128
+};
+PerDeviceOnce g_once;
+DeviceInfo g_info[PerDeviceOnce::kMaxDevices];
+
+template <typename T, int HD, int NS>
+cudaError_t prepare_rows(int* per_sm) {
+  cudaError_t e = cudaFuncSetAttribute(k_kv8_attn_rows<T, HD, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, w_smem<HD>());
+  if (e != cudaSuccess) return e;
+  e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(per_sm, k_kv8_attn_rows<T, HD, NS>, 32 * W_WARPS, w_smem<HD>());
+  return e == cudaSuccess && *per_sm < 1 ? cudaErrorInvalidConfiguration : e;
+}
+
+// Kernel attributes and sizes of the current device (set once per device).
+const DeviceInfo* device_info() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  const int rc = g_once.run(dev, [&]() -> int {
+    DeviceInfo& d = g_info[dev];
+    cudaError_t e = cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = prepare_rows<bf16, 64, 1>(&d.rows_ctas[0]);
+    if (e == cudaSuccess) e = prepare_rows<bf16, 128, 1>(&d.rows_ctas[1]);
+    if (e == cudaSuccess) e = prepare_rows<float, 64, 2>(&d.rows_ctas[2]);
+    if (e == cudaSuccess) e = prepare_rows<float, 128, 2>(&d.rows_ctas[3]);
+    return (int)e;
+  });
+  return rc == 0 ? &g_info[dev] : nullptr;
+}
+
+struct Form {
+  int ctas, tile_rows;
+};
+Form choose(const DeviceInfo& d, const jf_kv8_cache& c, const jf_kv8_rows& r, int dtype, int n_heads) {
+  return {d.sms * d.rows_ctas[(dtype == JF_F32 ? 2 : 0) + (c.head_dim == 128 ? 1 : 0)], W_TR};
+}
+size_t plan_bytes(const jf_kv8_cache& c) { return ((size_t)(c.n_seqs + 1) * 8 + 255) / 256 * 256; }
+
+template <typename T, int HD, int NS>
+cudaError_t launch_rows(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
+  cudaError_t e = kv8_launch(k_kv8_attn_rows<T, HD, NS>, dim3(ctas), dim3(32 * W_WARPS), w_smem<HD>(), st, a);
+  if (e != cudaSuccess) return e;
+  const long long warps = (long long)a.r.n_rows * a.n_heads;
+  return kv8_launch(k_kv8_combine<T, HD, W_TR, W_CH>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a, ctas);
+}
+
+}  // namespace
+}  // namespace jf
+
+using namespace jf;
+
+extern "C" jf_status jf_op_kv8_attention_workspace_bytes(const jf_kv8_cache* cache, const jf_kv8_rows* rows, int dtype,
+                                                         int n_heads, size_t* out_bytes) {
+  const jf_status s = kv8_check(cache, rows);
+  if (s != JF_OK) return s;
+  if (!out_bytes || (dtype != JF_F32 && dtype != JF_BF16) || n_heads < 1 || n_heads % cache->n_kv_heads) return JF_EINVAL;
+  const DeviceInfo* d = device_info();
+  if (!d) return JF_ECUDA;
+  const Form f = choose(*d, *cache, *rows, dtype, n_heads);
+  *out_bytes = plan_bytes(*cache) + (size_t)2 * f.ctas * f.tile_rows * (cache->head_dim + 2) * 4;
+  return JF_OK;
+}
+
+extern "C" jf_status jf_op_kv8_attention(const jf_kv8_cache* cache, const jf_kv8_rows* rows, int dtype, const void* q,
+                                         long long ld_q, int n_heads, float scale, const uint32_t* mask, int mask_words,
+                                         void* out, float* lse, void* workspace, size_t workspace_bytes, int* err_word,
+                                         void* cuda_stream) {
+  jf_status s = kv8_check(cache, rows);
+  if (s != JF_OK) return s;
+  if ((dtype != JF_F32 && dtype != JF_BF16) || !err_word || n_heads < 1 || n_heads % cache->n_kv_heads) return JF_EINVAL;
+  if (ld_q < (long long)n_heads * cache->head_dim || !(scale == scale)) return JF_EINVAL;
+  if (rows->n_rows == 0) return JF_OK;
+  const uintptr_t type_mask = dtype == JF_BF16 ? 1 : 3;
+  if (!q || !out || ((uintptr_t)q & type_mask) || ((uintptr_t)out & (2 * type_mask + 1)) || ((uintptr_t)workspace & 15)) return JF_EINVAL;
+  if (mask && (mask_words < 1 || (long long)mask_words * 32 < rows->max_rows)) return JF_EINVAL;
+  if ((long long)rows->n_rows * n_heads > (1ll << 33)) return JF_EUNSUPPORTED;  // the combine's grid
+  size_t need = 0;
+  s = jf_op_kv8_attention_workspace_bytes(cache, rows, dtype, n_heads, &need);
+  if (s != JF_OK) return s;
+  if (!workspace || workspace_bytes < need) return JF_ENOMEM;
+  const DeviceInfo* d = device_info();
+  if (!d) return JF_ECUDA;
+  const Form f = choose(*d, *cache, *rows, dtype, n_heads);
+  Kv8AttnParams a = {*cache, *rows, q, ld_q, n_heads, scale * 1.4426950408889634f, mask, mask_words, out, lse,
+                     reinterpret_cast<long long*>(workspace),
+                     reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + plan_bytes(*cache)), err_word};
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e;
+  if (dtype == JF_BF16)
+    e = cache->head_dim == 128 ? launch_rows<bf16, 128, 1>(a, f.ctas, st) : launch_rows<bf16, 64, 1>(a, f.ctas, st);
+  else
+    e = cache->head_dim == 128 ? launch_rows<float, 128, 2>(a, f.ctas, st) : launch_rows<float, 64, 2>(a, f.ctas, st);
+  return e == cudaSuccess ? JF_OK : JF_ECUDA;
+}

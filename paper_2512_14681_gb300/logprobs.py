@@ -1,0 +1,115 @@
+"""Log probabilities of given tokens with entropy and top alternatives, and their gradient (jf_op_token_logprobs*
+of include/jf_ops.h), on the current stream or the one given as stream=: scores of a draft's or a trajectory's tokens, and the loss of training on them.
+
+    r = token_logprobs(logits, targets, top=5)                                    # r.logprob, r.entropy, r.top_ids, ...
+    d = token_logprobs_grad(logits, targets, r.row_stats, r.entropy, -1 / n)      # of the mean negative log likelihood
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import NamedTuple
+
+import torch
+
+from . import _lib as J
+from .kv8 import _checked, _dtype, _on_stream, _want
+
+_err = {}        # error word by device
+_workspaces = {}  # by (device, stream): calls on different streams may overlap
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: torch.Tensor        # [rows] log probability of the target (0 where it is negative)
+    entropy: torch.Tensor        # [rows]
+    lse: torch.Tensor            # [rows] log sum exp of the scaled logits
+    row_stats: torch.Tensor      # [rows][2], for the gradient
+    top_ids: torch.Tensor | None       # int32 [rows][top], 0x7fffffff past the tokens that can occur
+    top_logprobs: torch.Tensor | None  # [rows][top]
+
+
+def _error_word(device):
+    if device not in _err:
+        _err[device] = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.current_stream(device).synchronize()  # zero for every stream
+    return _err[device]
+
+
+def check(device=None):
+    """Raise what the device has reported since the last check (synchronises), and clear it: a target beyond the
+    vocabulary."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    word = _err.get(device)
+    if word is not None and int(word.item()):
+        word.zero_()
+        raise J.JfError(J.JF_EDEVICE, "a target was beyond the vocabulary")
+
+
+def _logits(t, name="logits"):
+    _want(t.is_cuda and t.dim() == 2 and t.shape[1] >= 1 and (t.stride(1) == 1 or t.shape[1] == 1),
+          f"{name}: CUDA [rows][vocab] with contiguous rows is wanted")
+    return max(t.stride(0), t.shape[1])
+
+
+def _vector(t, rows, dtype, device, name):
+    _want(t.device == device and t.dtype == dtype and t.is_contiguous() and t.numel() == rows,
+          f"{name}: a contiguous {dtype} tensor of {rows} elements on {device} is wanted")
+    return t.data_ptr()
+
+
+@_on_stream
+def token_logprobs(logits, targets, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
+    """logits: CUDA [rows][vocab] (float32 or bfloat16, any row stride); targets: int32 [rows]; scale: inverse
+    temperature; top: alternatives listed per row (at most 64)."""
+    lib = J.load()
+    ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
+    dtype = _dtype(logits.dtype)
+    tp = _vector(targets, rows, torch.int32, dev, "targets")
+    st = torch.cuda.current_stream(dev).cuda_stream
+    out = torch.empty(5, rows, dtype=torch.float32, device=dev)
+    logprob, entropy, lse, stats = out[0], out[1], out[2], out[3:].view(rows, 2)
+    ids = torch.empty(rows, top, dtype=torch.int32, device=dev) if top else None
+    lps = torch.empty(rows, top, dtype=torch.float32, device=dev) if top else None
+    need = C.c_size_t()
+    _checked(lib.jf_op_token_logprobs_workspace_bytes(rows, vocab, top, C.byref(need)), "jf_op_token_logprobs_workspace_bytes")
+    ws = None
+    if need.value:
+        ws = _workspaces.get((dev, st))
+        if ws is None or ws.numel() < need.value:
+            ws = _workspaces[dev, st] = torch.empty(need.value, dtype=torch.uint8, device=dev)
+    _checked(lib.jf_op_token_logprobs(dtype, logits.data_ptr(), ld, rows, vocab, scale, tp, logprob.data_ptr(), entropy.data_ptr(),
+                                      lse.data_ptr(), stats.data_ptr(), top, ids.data_ptr() if top else None,
+                                      lps.data_ptr() if top else None, ws.data_ptr() if ws is not None else None,
+                                      ws.numel() if ws is not None else 0, _error_word(dev).data_ptr(), st),
+             "jf_op_token_logprobs")
+    return TokenLogprobs(logprob, entropy, lse, stats, ids, lps)
+
+
+@_on_stream
+def token_logprobs_grad(logits, targets, row_stats, entropy, grad_logprob, grad_entropy=None, scale: float = 1.0,
+                        out=None):
+    """Gradient of sum(grad_logprob * logprob + grad_entropy * entropy) by the logits, in their type. grad_logprob,
+    grad_entropy: float32 [rows], a number, or None (0). out: where it goes (it may be `logits`)."""
+    lib = J.load()
+    ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
+    dtype = _dtype(logits.dtype)
+    if out is None:
+        out = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)
+    ld_out = _logits(out, "out")
+    _want(out.dtype == logits.dtype and out.device == dev and out.shape == logits.shape, "out: like logits is wanted")
+
+    def share(g, name):
+        if g is None:
+            return None, None
+        if not isinstance(g, torch.Tensor):
+            g = torch.full((rows,), float(g), dtype=torch.float32, device=dev)
+        return g, _vector(g, rows, torch.float32, dev, name)
+
+    gl, gl_p = share(grad_logprob, "grad_logprob")
+    ge, ge_p = share(grad_entropy, "grad_entropy")
+    ep = _vector(entropy, rows, torch.float32, dev, "entropy") if ge is not None else None
+    _checked(lib.jf_op_token_logprobs_grad(dtype, logits.data_ptr(), ld, rows, vocab, scale,
+                                           _vector(targets, rows, torch.int32, dev, "targets"),
+                                           _vector(row_stats, 2 * rows, torch.float32, dev, "row_stats"), ep, gl_p, ge_p,
+                                           out.data_ptr(), ld_out, _error_word(dev).data_ptr(), torch.cuda.current_stream(dev).cuda_stream),
+             "jf_op_token_logprobs_grad")
+    return out
