@@ -30,8 +30,8 @@ struct Kv8AttnParams {
   int mask_words;
   void* out;
   float* lse;
-  long long* plan;   // [n_seqs + 1]: chunks of the sequences before b
-  float* states;     // [2 N][tile rows x hd O, then m, then l]
+  int* plan;         // [n_seqs + 1]: chunks of the sequences before b
+  float* states;     // [2 N][tile rows x hd normalised O, then m, then l]
   int* err;
 };
 
@@ -57,30 +57,30 @@ struct Plan {
     const int last = a.mask ? s.n - 1 : min(s.n - 1, ((tile + 1) * TR - 1) / G);  // a masked row may see any new row
     return (s.len + last + CH) / CH;
   }
-  static JF_DEV int tiles(const Kv8Seq& s, int G) { return (int)(((long long)s.n * G + TR - 1) / TR); }
+  static JF_DEV int tiles(const Kv8Seq& s, int G) { return (s.n * G + TR - 1) / TR; }
   // Chunks of a sequence's units, per KV head.
-  static JF_DEV long long per_head(const Kv8AttnParams& a, const Kv8Seq& s, int G) {
+  static JF_DEV int per_head(const Kv8AttnParams& a, const Kv8Seq& s, int G) {
     const int n = tiles(s, G);
-    if (a.mask) return n > 0 ? (long long)n * chunks(a, s, G, 0) : 0;
-    long long sum = 0;
+    if (a.mask) return n > 0 ? n * chunks(a, s, G, 0) : 0;
+    int sum = 0;
     for (int t = 0; t < n; ++t) sum += chunks(a, s, G, t);
     return sum;
   }
   // pre[b] = chunks of the sequences before b, pre[n_seqs] = T; by the whole CTA (ends with a barrier).
-  static JF_DEV void build(const Kv8AttnParams& a, int G, long long* pre) {
+  static JF_DEV void build(const Kv8AttnParams& a, int G, int* pre) {
     for (int b = threadIdx.x; b < a.c.n_seqs; b += blockDim.x)
       pre[b + 1] = per_head(a, kv8_seq(a.c, a.r, b, a.err), G) * a.c.n_kv_heads;
     __syncthreads();
     if (threadIdx.x < 32) {
       const int lane = threadIdx.x;
-      long long base = 0;
+      int base = 0;
       if (lane == 0) pre[0] = 0;
       for (int b0 = 0; b0 < a.c.n_seqs; b0 += 32) {
         const int b = b0 + lane;
-        long long v = b < a.c.n_seqs ? pre[b + 1] : 0;
+        int v = b < a.c.n_seqs ? pre[b + 1] : 0;
 #pragma unroll
         for (int sh = 1; sh < 32; sh <<= 1) {
-          const long long u = __shfl_up_sync(0xffffffffu, v, sh);
+          const int u = __shfl_up_sync(0xffffffffu, v, sh);
           if (lane >= sh) v += u;
         }
         if (b < a.c.n_seqs) pre[b + 1] = base + v;
@@ -91,26 +91,30 @@ struct Plan {
   }
 };
 
-JF_DEV long long share_begin(long long total, int i, int n) { return total * i / n; }
-// The CTA that holds chunk x of `total`: the last i with share_begin(i) <= x.
-JF_DEV int share_of(long long total, long long x, int n) {
-  int i = (int)((x * n + n - 1) / total);
-  while (i > 0 && share_begin(total, i, n) > x) --i;
-  while (i + 1 < n && share_begin(total, i + 1, n) <= x) ++i;
-  return i;
-}
-// Where CTA i leaves its part of a unit whose chunks begin at `first`: a CTA has at most one unit that began
-// before its share and one that goes on after it.
-JF_DEV int state_slot(long long total, long long first, int i, int n) { return 2 * i + (share_begin(total, i, n) > first ? 0 : 1); }
+// The chunks of the batch in n shares, the first `more` of them one chunk longer.
+struct Shares {
+  int each, more;
+  JF_DEV Shares(int total, int n) : each(total / n), more(total - total / n * n) {}
+  JF_DEV int begin(int i) const { return i * each + min(i, more); }
+  JF_DEV int size(int i) const { return each + (i < more ? 1 : 0); }
+  // The CTA that holds chunk x.
+  JF_DEV int of(int x) const {
+    const int cut = more * (each + 1);
+    return x < cut ? x / (each + 1) : more + (x - cut) / each;
+  }
+  // Where CTA i leaves its part of a unit whose chunks begin at `first`: a CTA has at most one unit that began
+  // before its share and one that goes on after it.
+  JF_DEV int slot(int first, int i) const { return 2 * i + (begin(i) > first ? 0 : 1); }
+};
 
 // A CTA's walk over the units of its share. Uniform over the CTA.
 template <int TR, int CH>
 struct Walk {
-  long long at, end, first;  // chunks of the whole batch: the next one, the end of the share, the unit's first
+  int at, end, first;  // chunks of the whole batch: the next one, the end of the share, the unit's first
   int b, kvh, tile, n_chunks;
   Kv8Seq s;
 
-  JF_DEV void start(const Kv8AttnParams& a, const long long* pre, int G, long long at_, long long end_) {
+  JF_DEV void start(const Kv8AttnParams& a, const int* pre, int G, int at_, int end_) {
     at = at_;
     end = end_;
     int lo = 0, hi = a.c.n_seqs;  // the last b with pre[b] <= at (then pre[b + 1] > at)
@@ -121,9 +125,9 @@ struct Walk {
     }
     b = lo;
     s = kv8_seq(a.c, a.r, b, a.err);
-    const long long head = (pre[b + 1] - pre[b]) / a.c.n_kv_heads, off = at - pre[b];
-    kvh = (int)(off / head);
-    long long rest = off - kvh * head;
+    const int head = (pre[b + 1] - pre[b]) / a.c.n_kv_heads, off = at - pre[b];
+    kvh = off / head;
+    int rest = off - kvh * head;
     tile = 0;
     while (rest >= (n_chunks = Plan<TR, CH>::chunks(a, s, G, tile))) {
       rest -= n_chunks;
@@ -153,8 +157,38 @@ JF_DEV bool sees_new(const Kv8AttnParams& a, const Kv8Seq& s, int i, int kp) {
   return j < s.n && (a.mask[(long long)(s.row0 + i) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
 }
 
-template <typename T>
-JF_DEV float load_q(const T* p) { return act_to_f32(*p); }
+// N consecutive values as fp32 (zeros unless live); by 16-byte loads where the caller's rows allow it.
+template <int N>
+JF_DEV void load_run(const float* p, bool live, bool by16, float (&x)[N]) {
+  if (by16 && live) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(p + i);
+      x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = live ? p[i] : 0.f;
+  }
+}
+template <int N>
+JF_DEV void load_run(const bf16* p, bool live, bool by16, float (&x)[N]) {
+  if (by16 && live) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p + i);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[i + 2 * j] = __uint_as_float(w[j] << 16);
+        x[i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = live ? __bfloat162float(p[i]) : 0.f;
+  }
+}
 
 JF_DEV void store2(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
 JF_DEV void store2(bf16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
@@ -215,7 +249,7 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
   constexpr int PK = HD / 64;   // 16-byte pieces of a key that a lane reads
   constexpr int PAGE_BYTES = kPage * HD;
   extern __shared__ __align__(128) uint8_t sm[];
-  __shared__ long long pre[kKv8MaxSeqs + 1];
+  __shared__ int pre[kKv8MaxSeqs + 1];
   __shared__ float s_ml[W_WARPS][W_TR][3];  // m, l, E as 2^E's exponent
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int G = a.n_heads / a.c.n_kv_heads, Hkv = a.c.n_kv_heads;
@@ -223,21 +257,22 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
   pdl_wait();
   using P = Plan<W_TR, W_CH>;
   P::build(a, G, pre);
-  const long long total = pre[a.c.n_seqs];
+  const Shares shares(pre[a.c.n_seqs], gridDim.x);
   if (blockIdx.x == 0)
     for (int b = tid; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
   Walk<W_TR, W_CH> w;
   {
-    const long long lo = share_begin(total, blockIdx.x, gridDim.x), hi = share_begin(total, blockIdx.x + 1, gridDim.x);
-    if (lo >= hi) return;
-    w.start(a, pre, G, lo, hi);
+    const int n = shares.size(blockIdx.x);
+    if (n == 0) return;
+    w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + n);
   }
   const uint32_t ring = smem_u32(sm) + warp * (W_STAGES * 2 * PAGE_BYTES);
+  const bool q16 = ((uintptr_t)a.q & 15) == 0 && a.ld_q * sizeof(T) % 16 == 0;
   const uint8_t *Kc = reinterpret_cast<const uint8_t*>(a.c.k), *Vc = reinterpret_cast<const uint8_t*>(a.c.v);
 
   while (true) {
     const Kv8Seq s = w.s;
-    const int c0 = (int)(w.at - w.first), c1 = (int)min((long long)w.n_chunks, w.end - w.first);
+    const int c0 = w.at - w.first, c1 = min(w.n_chunks, w.end - w.first);
     const int keys = s.len + s.n;  // slots that hold a token
     const int rows = s.n * G, r0 = w.tile * W_TR;
     // ---- queries: fragments of this lane's rows g, g + 8, scaled
@@ -252,11 +287,9 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
         const T* src = Q + (long long)(s.row0 + (live ? row / G : 0)) * a.ld_q + (long long)(w.kvh * G + (live ? row % G : 0)) * HD + PK * 16 * t;
         float x[4 * KS];
         float amax = 0.f;
+        load_run<4 * KS>(src, live, q16, x);
 #pragma unroll
-        for (int j = 0; j < 4 * KS; ++j) {
-          x[j] = live ? load_q(src + j) : 0.f;
-          amax = fmaxf(amax, fabsf(x[j]));
-        }
+        for (int j = 0; j < 4 * KS; ++j) amax = fmaxf(amax, fabsf(x[j]));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
         const int sh = query_shift(amax);
@@ -461,26 +494,32 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
     }
     __syncthreads();
     const bool whole = c0 == 0 && c1 == w.n_chunks;
-    float* st = a.states + (long long)state_slot(total, w.first, blockIdx.x, gridDim.x) * (W_TR * (HD + 2));
+    float* st = a.states + (long long)shares.slot(w.first, blockIdx.x) * (W_TR * (HD + 2));
     for (int i = tid; i < W_TR * (HD / 2); i += 32 * W_WARPS) {
       const int r = i / (HD / 2), d = i % (HD / 2) * 2, row = r0 + r;
       if (row >= rows) break;
-      float M = -INFINITY;
+      float M = -INFINITY, Ew = -126.f;
 #pragma unroll
-      for (int q = 0; q < W_WARPS; ++q) M = fmaxf(M, s_ml[q][r][0]);
-      float L = 0.f, x = 0.f, y = 0.f;
+      for (int q = 0; q < W_WARPS; ++q) {
+        M = fmaxf(M, s_ml[q][r][0]);
+        if (s_ml[q][r][0] != -INFINITY) Ew = fmaxf(Ew, s_ml[q][r][2]);
+      }
+      float L = 0.f, x = 0.f, y = 0.f;  // x, y in units of 2^Ew
 #pragma unroll
       for (int q = 0; q < W_WARPS; ++q) {
         const float wt = s_ml[q][r][0] == -INFINITY ? 0.f : exp2f(s_ml[q][r][0] - M);
         L = fmaf(wt, s_ml[q][r][1], L);
-        const float wo = wt * pow2i((int)s_ml[q][r][2]);
+        const float wo = wt * pow2i((int)fmaxf(s_ml[q][r][2] - Ew, -126.f));
         const float* src = reinterpret_cast<float*>(sm) + q * (W_TR * (HD + 4)) + r * (HD + 4) + d;
         if (wt != 0.f) x = fmaf(wo, src[0], x), y = fmaf(wo, src[1], y);
       }
+      // normalised here: the sums themselves may be out of fp32's range where the values are near its end
+      const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L), unit = pow2i((int)Ew);
+      x = x * il * unit;
+      y = y * il * unit;
       if (whole) {
-        const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
         const long long at = (long long)(s.row0 + row / G) * a.n_heads + w.kvh * G + row % G;
-        store2(reinterpret_cast<T*>(a.out) + at * HD + d, x * il, y * il);
+        store2(reinterpret_cast<T*>(a.out) + at * HD + d, x, y);
         if (a.lse && d == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
       } else {
         store2(st + r * HD + d, x, y);
@@ -519,35 +558,58 @@ __global__ void __launch_bounds__(256) k_kv8_combine(const Kv8AttnParams a, int 
   const Kv8Seq s = kv8_seq(a.c, a.r, lo, a.err);
   if (row < s.row0 || row >= s.row0 + s.n) return;
   const int tr = (row - s.row0) * G + head % G, tile = tr / TR, r = tr % TR;
-  const long long total = a.plan[a.c.n_seqs], base = a.plan[lo], per_head = (a.plan[lo + 1] - base) / a.c.n_kv_heads;
+  const int base = a.plan[lo], per_head = (a.plan[lo + 1] - base) / a.c.n_kv_heads;
+  const Shares shares(a.plan[a.c.n_seqs], n);
   using P = Plan<TR, CH>;
-  long long before = 0;
+  int before = 0;
   for (int t = lane; t < tile; t += 32) before += P::chunks(a, s, G, t);
 #pragma unroll
   for (int sh = 16; sh > 0; sh >>= 1) before += __shfl_xor_sync(0xffffffffu, before, sh);
-  const long long first = base + head / G * per_head + before, end = first + P::chunks(a, s, G, tile);
-  const int i0 = share_of(total, first, n), i1 = share_of(total, end - 1, n);
+  const int first = base + head / G * per_head + before, end = first + P::chunks(a, s, G, tile);
+  const int i0 = shares.of(first), i1 = shares.of(end - 1);
   if (i0 == i1) return;  // finished by the one CTA that held it
+  auto state = [&](int c) { return c > i1 ? nullptr : a.states + (long long)shares.slot(first, c) * (TR * (HD + 2)); };
+  // each lane: the statistics of every 32nd CTA
+  float M = -INFINITY;
+  for (int c = i0 + lane; c <= i1; c += 32)
+    if (const float* st = state(c)) M = fmaxf(M, st[TR * HD + r]);
+#pragma unroll
+  for (int sh = 16; sh > 0; sh >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, sh));
+  float L = 0.f;
+  for (int c = i0 + lane; c <= i1; c += 32)
+    if (const float* st = state(c)) {
+      const float mc = st[TR * HD + r], lc = st[TR * (HD + 1) + r];
+      L += mc == -INFINITY ? lc : exp2f(mc - M) * lc;  // (nothing seen: 0, or NaN)
+    }
+#pragma unroll
+  for (int sh = 16; sh > 0; sh >>= 1) L += __shfl_xor_sync(0xffffffffu, L, sh);
+  const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
   constexpr int D = HD / 32;
-  float M = -INFINITY, L = 0.f, o[D];
+  float o[D];
 #pragma unroll
   for (int j = 0; j < D; ++j) o[j] = 0.f;
-  // (CTAs without a chunk lie between others only when there are fewer chunks than CTAs: they left nothing)
-  for (int c = i0; c <= i1; ++c) {
-    if (share_begin(total, c, n) == share_begin(total, c + 1, n)) continue;
-    const float* st = a.states + (long long)state_slot(total, first, c, n) * (TR * (HD + 2));
-    const float mc = st[TR * HD + r], lc = st[TR * (HD + 1) + r];
-    const float mn = fmaxf(M, mc);
-    const float wa = M == -INFINITY ? 0.f : exp2f(M - mn), wb = mc == -INFINITY ? 0.f : exp2f(mc - mn);
-    L = wa * L + wb * lc;
+  for (int c0 = i0; c0 <= i1; c0 += 32) {
+    const float* st = state(c0 + lane);
+    float wt = 0.f;
+    if (st) {
+      const float mc = st[TR * HD + r];
+      wt = mc == -INFINITY ? 0.f : exp2f(mc - M) * st[TR * (HD + 1) + r] * il;
+    }
+    for (int k = 0; k < 32 && c0 + k <= i1; ++k) {
+      const unsigned long long pk = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(st), k);
+      const float wk = __shfl_sync(0xffffffffu, wt, k);
+      if (!pk || wk == 0.f) continue;
+      const float* sk = reinterpret_cast<const float*>(pk) + r * HD + D * lane;
 #pragma unroll
-    for (int j = 0; j < D; ++j) o[j] = wa * o[j] + wb * st[r * HD + D * lane + j];
-    M = mn;
+      for (int j = 0; j < D; ++j) o[j] = fmaf(wk, sk[j], o[j]);
+    }
   }
-  const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+  if (!(L >= 0.f))  // NaN scores only
+#pragma unroll
+    for (int j = 0; j < D; ++j) o[j] = L;
   T* dst = reinterpret_cast<T*>(a.out) + i * HD + D * lane;
 #pragma unroll
-  for (int j = 0; j < D; j += 2) store2(dst + j, o[j] * il, o[j + 1] * il);
+  for (int j = 0; j < D; j += 2) store2(dst + j, o[j], o[j + 1]);
   if (a.lse && lane == 0) a.lse[i] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
@@ -587,7 +649,7 @@ struct Form {
 Form choose(const DeviceInfo& d, const jf_kv8_cache& c, const jf_kv8_rows& r, int dtype, int n_heads) {
   return {d.sms * d.rows_ctas[(dtype == JF_F32 ? 2 : 0) + (c.head_dim == 128 ? 1 : 0)], W_TR};
 }
-size_t plan_bytes(const jf_kv8_cache& c) { return ((size_t)(c.n_seqs + 1) * 8 + 255) / 256 * 256; }
+size_t plan_bytes(const jf_kv8_cache& c) { return ((size_t)(c.n_seqs + 1) * 4 + 255) / 256 * 256; }
 
 template <typename T, int HD, int NS>
 cudaError_t launch_rows(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
@@ -626,7 +688,12 @@ extern "C" jf_status jf_op_kv8_attention(const jf_kv8_cache* cache, const jf_kv8
   const uintptr_t type_mask = dtype == JF_BF16 ? 1 : 3;
   if (!q || !out || ((uintptr_t)q & type_mask) || ((uintptr_t)out & (2 * type_mask + 1)) || ((uintptr_t)workspace & 15)) return JF_EINVAL;
   if (mask && (mask_words < 1 || (long long)mask_words * 32 < rows->max_rows)) return JF_EINVAL;
-  if ((long long)rows->n_rows * n_heads > (1ll << 33)) return JF_EUNSUPPORTED;  // the combine's grid
+  {  // chunks and rows are counted in 32 bits
+    const long long group_rows = (long long)rows->n_rows * (n_heads / cache->n_kv_heads);
+    const long long units = (group_rows / W_TR + cache->n_seqs) * cache->n_kv_heads;
+    const long long chunks = (long long)cache->pages_per_seq * kPage / W_CH + 1;
+    if (group_rows * cache->n_kv_heads > 0x3fffffffll || units > 0x7fffffffll / chunks) return JF_EUNSUPPORTED;
+  }
   size_t need = 0;
   s = jf_op_kv8_attention_workspace_bytes(cache, rows, dtype, n_heads, &need);
   if (s != JF_OK) return s;
@@ -635,7 +702,7 @@ extern "C" jf_status jf_op_kv8_attention(const jf_kv8_cache* cache, const jf_kv8
   if (!d) return JF_ECUDA;
   const Form f = choose(*d, *cache, *rows, dtype, n_heads);
   Kv8AttnParams a = {*cache, *rows, q, ld_q, n_heads, scale * 1.4426950408889634f, mask, mask_words, out, lse,
-                     reinterpret_cast<long long*>(workspace),
+                     reinterpret_cast<int*>(workspace),
                      reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + plan_bytes(*cache)), err_word};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;

@@ -39,9 +39,14 @@ def _checked(status: int, what: str):
         raise J.JfError(status, what)
 
 
-def _want(ok, what: str):
+def _want(ok, what: str, *values):
+    """A refusal, its message written only then."""
     if not ok:
-        raise J.JfError(J.JF_EINVAL, what)
+        raise J.JfError(J.JF_EINVAL, what.format(*values))
+
+
+def _raw_stream(device):
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _on_stream(call):
@@ -57,7 +62,7 @@ def _on_stream(call):
 
 def _device_i32(t, n, name):
     _want(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n,
-          f"{name}: a contiguous int32 CUDA tensor of {n} elements is wanted")
+          "{}: a contiguous int32 CUDA tensor of {} elements is wanted", name, n)
 
 
 def rope_table(n: int, head_dim: int, theta: float, device="cuda"):
@@ -99,10 +104,10 @@ class Kv8Cache:
     def __init__(self, k, v, k_exp, v_exp, page_table):
         for name, t in (("k", k), ("v", v)):
             _want(t.is_cuda and t.is_contiguous() and t.dim() == 4 and t.element_size() == 1 and t.shape[2] == PAGE,
-                  f"{name}: contiguous 8-bit codes [pages][heads][16][head_dim] are wanted")
+                  "{}: contiguous 8-bit codes [pages][heads][16][head_dim] are wanted", name)
         for name, t in (("k_exp", k_exp), ("v_exp", v_exp)):
             _want(t.is_cuda and t.is_contiguous() and t.dtype == torch.int8 and t.shape == k.shape[:2],
-                  f"{name}: contiguous int8 [pages][heads] is wanted")
+                  "{}: contiguous int8 [pages][heads] is wanted", name)
         _want(k.shape == v.shape, "k and v differ in shape")
         _want(page_table.dim() == 2, "page_table: [sequences][pages] is wanted")
         _device_i32(page_table, page_table.numel(), "page_table")
@@ -115,6 +120,7 @@ class Kv8Cache:
         self.err = torch.zeros(1, dtype=torch.int32, device=k.device)
         torch.cuda.current_stream(k.device).synchronize()  # zero for every stream
         self._workspaces = {}  # by stream: calls on different streams may overlap
+        self._need = {}
 
     @classmethod
     def empty(cls, n_seqs: int, max_ctx: int, n_kv_heads: int, head_dim: int, device="cuda"):
@@ -126,9 +132,6 @@ class Kv8Cache:
         return cls(codes(), codes(), exps(), exps(),
                    torch.arange(pages, dtype=torch.int32, device=device).view(n_seqs, per_seq))
 
-    def _stream(self):
-        return torch.cuda.current_stream(self.device).cuda_stream
-
     def _rows_of(self, t, heads, rows, name):
         """Row stride of [n_rows][heads * head_dim] (or [n_rows][heads][head_dim]) values."""
         width = heads * self.head_dim
@@ -137,7 +140,7 @@ class Kv8Cache:
         else:
             ok = t.dim() == 2 and t.shape[1] == width and t.stride(1) == 1
         _want(ok and t.shape[0] == rows.n_rows and t.device == self.device,
-              f"{name}: [{rows.n_rows}][{heads} x {self.head_dim}] with contiguous heads on {self.device} is wanted")
+              "{}: [{}][{} x {}] with contiguous heads on {} is wanted", name, rows.n_rows, heads, self.head_dim, self.device)
         return max(t.stride(0), width)  # (one row's stride may be anything)
 
     def _batch(self, rows):
@@ -170,7 +173,7 @@ class Kv8Cache:
         ptr = lambda t: t.data_ptr() if t is not None else None
         _checked(self.lib.jf_op_kv8_append(
             C.byref(self.c), C.byref(rows.c), _dtype(k.dtype), ptr(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, heads,
-            ptr(positions), ptr(rope), rope_len, _dtype(out_dtype), ptr(q_out), self.err.data_ptr(), self._stream()),
+            ptr(positions), ptr(rope), rope_len, _dtype(out_dtype), ptr(q_out), self.err.data_ptr(), _raw_stream(self.device)),
             "jf_op_kv8_append")
         return q_out
 
@@ -181,7 +184,7 @@ class Kv8Cache:
         shape = (rows.n_rows, self.n_kv_heads, self.head_dim)
         k, v = (torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
         _checked(self.lib.jf_op_kv8_read(C.byref(self.c), C.byref(rows.c), _dtype(dtype), k.data_ptr(), v.data_ptr(),
-                                         self.err.data_ptr(), self._stream()), "jf_op_kv8_read")
+                                         self.err.data_ptr(), _raw_stream(self.device)), "jf_op_kv8_read")
         return k, v
 
     @_on_stream
@@ -199,13 +202,17 @@ class Kv8Cache:
             _want(mask.dim() == 2, "mask: [rows][words] is wanted")
             words = mask.shape[1]
             _device_i32(mask, rows.n_rows * words, "mask")
-        st = self._stream()
-        need = C.c_size_t()
-        _checked(self.lib.jf_op_kv8_attention_workspace_bytes(C.byref(self.c), C.byref(rows.c), dtype, heads, C.byref(need)),
-                 "jf_op_kv8_attention_workspace_bytes")
+        st = _raw_stream(self.device)
+        key = (dtype, heads, rows.n_rows, rows.max_rows)
+        need = self._need.get(key)
+        if need is None:
+            n = C.c_size_t()
+            _checked(self.lib.jf_op_kv8_attention_workspace_bytes(C.byref(self.c), C.byref(rows.c), dtype, heads, C.byref(n)),
+                     "jf_op_kv8_attention_workspace_bytes")
+            need = self._need[key] = n.value
         ws = self._workspaces.get(st)
-        if ws is None or ws.numel() < need.value:
-            ws = self._workspaces[st] = torch.empty(max(need.value, 16), dtype=torch.uint8, device=self.device)
+        if ws is None or ws.numel() < need:
+            ws = self._workspaces[st] = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
         out = torch.empty(rows.n_rows, heads, self.head_dim, dtype=q.dtype, device=self.device)
         lse = torch.empty(rows.n_rows, heads, dtype=torch.float32, device=self.device) if want_lse else None
         _checked(self.lib.jf_op_kv8_attention(

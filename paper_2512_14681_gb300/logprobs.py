@@ -7,12 +7,13 @@ of include/jf_ops.h), on the current stream or the one given as stream=: scores 
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import NamedTuple
 
 import torch
 
 from . import _lib as J
-from .kv8 import _checked, _dtype, _on_stream, _want
+from .kv8 import _checked, _dtype, _on_stream, _raw_stream, _want
 
 _err = {}        # error word by device
 _workspaces = {}  # by (device, stream): calls on different streams may overlap
@@ -22,7 +23,7 @@ class TokenLogprobs(NamedTuple):
     logprob: torch.Tensor        # [rows] log probability of the target (0 where it is negative)
     entropy: torch.Tensor        # [rows]
     lse: torch.Tensor            # [rows] log sum exp of the scaled logits
-    row_stats: torch.Tensor      # [rows][2], for the gradient
+    row_stats: torch.Tensor      # [rows * 2], for the gradient
     top_ids: torch.Tensor | None       # int32 [rows][top], 0x7fffffff past the tokens that can occur
     top_logprobs: torch.Tensor | None  # [rows][top]
 
@@ -44,15 +45,22 @@ def check(device=None):
         raise J.JfError(J.JF_EDEVICE, "a target was beyond the vocabulary")
 
 
+@functools.lru_cache(maxsize=4096)
+def _need(rows, vocab, top):
+    n = C.c_size_t()
+    _checked(J.load().jf_op_token_logprobs_workspace_bytes(rows, vocab, top, C.byref(n)), "jf_op_token_logprobs_workspace_bytes")
+    return n.value
+
+
 def _logits(t, name="logits"):
     _want(t.is_cuda and t.dim() == 2 and t.shape[1] >= 1 and (t.stride(1) == 1 or t.shape[1] == 1),
-          f"{name}: CUDA [rows][vocab] with contiguous rows is wanted")
+          "{}: CUDA [rows][vocab] with contiguous rows is wanted", name)
     return max(t.stride(0), t.shape[1])
 
 
 def _vector(t, rows, dtype, device, name):
     _want(t.device == device and t.dtype == dtype and t.is_contiguous() and t.numel() == rows,
-          f"{name}: a contiguous {dtype} tensor of {rows} elements on {device} is wanted")
+          "{}: a contiguous {} tensor of {} elements on {} is wanted", name, dtype, rows, device)
     return t.data_ptr()
 
 
@@ -64,18 +72,17 @@ def token_logprobs(logits, targets, top: int = 0, scale: float = 1.0) -> TokenLo
     ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
     dtype = _dtype(logits.dtype)
     tp = _vector(targets, rows, torch.int32, dev, "targets")
-    st = torch.cuda.current_stream(dev).cuda_stream
-    out = torch.empty(5, rows, dtype=torch.float32, device=dev)
-    logprob, entropy, lse, stats = out[0], out[1], out[2], out[3:].view(rows, 2)
+    st = _raw_stream(dev)
+    out = torch.empty(5 * rows, dtype=torch.float32, device=dev)
+    logprob, entropy, lse, stats = torch.split_with_sizes(out, (rows, rows, rows, 2 * rows))
     ids = torch.empty(rows, top, dtype=torch.int32, device=dev) if top else None
     lps = torch.empty(rows, top, dtype=torch.float32, device=dev) if top else None
-    need = C.c_size_t()
-    _checked(lib.jf_op_token_logprobs_workspace_bytes(rows, vocab, top, C.byref(need)), "jf_op_token_logprobs_workspace_bytes")
+    need = _need(rows, vocab, top)
     ws = None
-    if need.value:
+    if need:
         ws = _workspaces.get((dev, st))
-        if ws is None or ws.numel() < need.value:
-            ws = _workspaces[dev, st] = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        if ws is None or ws.numel() < need:
+            ws = _workspaces[dev, st] = torch.empty(need, dtype=torch.uint8, device=dev)
     _checked(lib.jf_op_token_logprobs(dtype, logits.data_ptr(), ld, rows, vocab, scale, tp, logprob.data_ptr(), entropy.data_ptr(),
                                       lse.data_ptr(), stats.data_ptr(), top, ids.data_ptr() if top else None,
                                       lps.data_ptr() if top else None, ws.data_ptr() if ws is not None else None,
@@ -110,6 +117,6 @@ def token_logprobs_grad(logits, targets, row_stats, entropy, grad_logprob, grad_
     _checked(lib.jf_op_token_logprobs_grad(dtype, logits.data_ptr(), ld, rows, vocab, scale,
                                            _vector(targets, rows, torch.int32, dev, "targets"),
                                            _vector(row_stats, 2 * rows, torch.float32, dev, "row_stats"), ep, gl_p, ge_p,
-                                           out.data_ptr(), ld_out, _error_word(dev).data_ptr(), torch.cuda.current_stream(dev).cuda_stream),
+                                           out.data_ptr(), ld_out, _error_word(dev).data_ptr(), _raw_stream(dev)),
              "jf_op_token_logprobs_grad")
     return out

@@ -595,8 +595,8 @@ def test_refusals(torch):
     refused(inv, lambda: Kv8Cache(c.k, c.v[:1], c.k_exp, c.v_exp, c.page_table))
     refused(inv, lambda: Kv8Cache(c.k, c.v, c.k_exp.int(), c.v_exp, c.page_table))
     refused(inv, lambda: Rows(torch.zeros(1, dtype=torch.int32, device="cuda"), rows.len, 4, 4))
-    odd = torch.zeros(2, 2, PAGE, 32, dtype=torch.uint8, device="cuda")
-    refused(uns, lambda: Kv8Cache(odd, odd, c.k_exp[:2], c.v_exp[:2], c.page_table).append(rows, x[..., :32], x[..., :32]))
+    odd, few = torch.zeros(2, 2, PAGE, 32, dtype=torch.uint8, device="cuda"), torch.zeros(4, 2, 32, device="cuda")
+    refused(uns, lambda: Kv8Cache(odd, odd, c.k_exp[:2], c.v_exp[:2], c.page_table).append(rows, few, few))
     # a workspace that is too small, through the C entry
     need = C.c_size_t()
     assert c.lib.jf_op_kv8_attention_workspace_bytes(C.byref(c.c), C.byref(rows.c), J.JF_F32, 4, C.byref(need)) == J.JF_OK
