@@ -9,9 +9,10 @@
 // accumulates; E follows e_v only when the difference leaves a range in which fp16 keeps p' as well as it keeps p.
 //
 // Work is split evenly whatever the batch: a unit is (sequence, KV head, tile of (token, head) query rows), a
-// chunk a run of keys of one unit, and CTA i of N takes chunks [T i / N, T (i + 1) / N) of all T. A unit that
-// one CTA holds entirely is finished there; of the others each CTA leaves a partial state (m, l, O) in the
-// workspace, at most two a CTA, and k_kv8_combine joins a row's states in CTA order.
+// chunk a run of keys of one unit. Units lie one after the other, each as long as its chunks plus a constant for
+// what a unit costs beside them (its queries, its end), and each of N CTAs takes an N'th of that length. A unit
+// whose chunks one CTA holds entirely is finished there; of the others each CTA leaves a partial state (m, l, O) in
+// the workspace, at most two a CTA, and k_kv8_combine joins a row's states in CTA order.
 #include "../../include/jf_ops.h"
 #include "jf_kv8.cuh"
 #include "jf_once.h"
@@ -30,7 +31,7 @@ struct Kv8AttnParams {
   int mask_words;
   void* out;
   float* lse;
-  int* plan;         // [n_seqs + 1]: chunks of the sequences before b
+  int* plan;         // [n_seqs + 1]: length of the sequences before b
   float* states;     // [2 N][tile rows x hd normalised O, then m, then l]
   int* err;
 };
@@ -48,9 +49,10 @@ JF_DEV uint32_t pack_f16(float lo, float hi) {
 JF_DEV float2 unpack_f16(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
 // ---------------------------------------------------------------------------------------------
-// The plan: which chunks there are. TR: query rows of a tile, CH: keys of a chunk.
+// The plan: which units there are. TR: query rows of a tile, CH: keys of a chunk, UC: what a unit costs beside its
+// chunks, in chunks.
 // ---------------------------------------------------------------------------------------------
-template <int TR, int CH>
+template <int TR, int CH, int UC>
 struct Plan {
   // Chunks of one tile of a sequence's rows.
   static JF_DEV int chunks(const Kv8AttnParams& a, const Kv8Seq& s, int G, int tile) {
@@ -58,15 +60,15 @@ struct Plan {
     return (s.len + last + CH) / CH;
   }
   static JF_DEV int tiles(const Kv8Seq& s, int G) { return (s.n * G + TR - 1) / TR; }
-  // Chunks of a sequence's units, per KV head.
+  // Length of a sequence's units, per KV head.
   static JF_DEV int per_head(const Kv8AttnParams& a, const Kv8Seq& s, int G) {
     const int n = tiles(s, G);
-    if (a.mask) return n > 0 ? n * chunks(a, s, G, 0) : 0;
+    if (a.mask) return n > 0 ? n * (UC + chunks(a, s, G, 0)) : 0;
     int sum = 0;
-    for (int t = 0; t < n; ++t) sum += chunks(a, s, G, t);
+    for (int t = 0; t < n; ++t) sum += UC + chunks(a, s, G, t);
     return sum;
   }
-  // pre[b] = chunks of the sequences before b, pre[n_seqs] = T; by the whole CTA (ends with a barrier).
+  // pre[b] = length of the sequences before b, pre[n_seqs] = of all; by the whole CTA (ends with a barrier).
   static JF_DEV void build(const Kv8AttnParams& a, int G, int* pre) {
     for (int b = threadIdx.x; b < a.c.n_seqs; b += blockDim.x)
       pre[b + 1] = per_head(a, kv8_seq(a.c, a.r, b, a.err), G) * a.c.n_kv_heads;
@@ -91,26 +93,27 @@ struct Plan {
   }
 };
 
-// The chunks of the batch in n shares, the first `more` of them one chunk longer.
+// The batch's length in n shares, the first `more` of them one longer.
 struct Shares {
   int each, more;
   JF_DEV Shares(int total, int n) : each(total / n), more(total - total / n * n) {}
   JF_DEV int begin(int i) const { return i * each + min(i, more); }
   JF_DEV int size(int i) const { return each + (i < more ? 1 : 0); }
-  // The CTA that holds chunk x.
+  // The CTA that holds place x.
   JF_DEV int of(int x) const {
     const int cut = more * (each + 1);
     return x < cut ? x / (each + 1) : more + (x - cut) / each;
   }
-  // Where CTA i leaves its part of a unit whose chunks begin at `first`: a CTA has at most one unit that began
-  // before its share and one that goes on after it.
+  // Where CTA i leaves its part of a unit whose chunks begin at place `first`: a CTA has at most one unit whose
+  // first chunk lies before its share, and one that goes on after it.
   JF_DEV int slot(int first, int i) const { return 2 * i + (begin(i) > first ? 0 : 1); }
 };
 
 // A CTA's walk over the units of its share. Uniform over the CTA.
-template <int TR, int CH>
+template <int TR, int CH, int UC>
 struct Walk {
-  int at, end, first;  // chunks of the whole batch: the next one, the end of the share, the unit's first
+  using P = Plan<TR, CH, UC>;
+  int at, end, first;  // places: the next one, the end of the share, the unit's first chunk
   int b, kvh, tile, n_chunks;
   Kv8Seq s;
 
@@ -129,16 +132,21 @@ struct Walk {
     kvh = off / head;
     int rest = off - kvh * head;
     tile = 0;
-    while (rest >= (n_chunks = Plan<TR, CH>::chunks(a, s, G, tile))) {
-      rest -= n_chunks;
+    while (rest >= UC + (n_chunks = P::chunks(a, s, G, tile))) {
+      rest -= UC + n_chunks;
       ++tile;
     }
-    first = at - rest;
+    first = at - rest + UC;
   }
-  // To the unit that begins where this one ends (at == first + n_chunks < end).
-  JF_DEV void next(const Kv8AttnParams& a, int G) {
-    first = at;
-    if (++tile == Plan<TR, CH>::tiles(s, G)) {
+  // The share's chunks of the unit: [c0, c1), none when it holds the unit's constant alone.
+  JF_DEV int c0() const { return max(0, at - first); }
+  JF_DEV int c1() const { return min(n_chunks, end - first); }
+  // To the unit that begins where this one ends; false at the end of the share.
+  JF_DEV bool next(const Kv8AttnParams& a, int G) {
+    at = first + n_chunks;
+    if (at >= end) return false;
+    first = at + UC;
+    if (++tile == P::tiles(s, G)) {
       tile = 0;
       if (++kvh == a.c.n_kv_heads) {
         kvh = 0;
@@ -146,7 +154,8 @@ struct Walk {
         while (s.n == 0);
       }
     }
-    n_chunks = Plan<TR, CH>::chunks(a, s, G, tile);
+    n_chunks = P::chunks(a, s, G, tile);
+    return true;
   }
 };
 
@@ -214,8 +223,8 @@ JF_DEV int query_shift(float amax) {
 // as it held their scores, and needs these keys' codes at dims NT g + j, j = 0 .. NT - 1, of the n-tiles j.
 // NS: fp16 terms of queries and probabilities (1 for bf16 models, 2 for fp32).
 // ---------------------------------------------------------------------------------------------
-constexpr int W_WARPS = 4, W_TR = 16, W_CH = W_WARPS * kPage;
-constexpr int W_STAGES = 4;
+constexpr int W_WARPS = 4, W_TR = 16, W_CH = W_WARPS * kPage, W_UC = 3;
+constexpr int W_STAGES = 4;  // two pairs of pages
 constexpr float W_LAG = 4.f;             // a row's reference maximum follows its scores when they exceed it by more
 constexpr int W_EV_SET = 5, W_EV_MAX = 10;  // e_v - E: where E is set, largest (p' <= 2^14); smallest 0
 
@@ -253,14 +262,14 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
   __shared__ float s_ml[W_WARPS][W_TR][3];  // m, l, E as 2^E's exponent
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int G = a.n_heads / a.c.n_kv_heads, Hkv = a.c.n_kv_heads;
-  pdl_launch_dependents();
   pdl_wait();
-  using P = Plan<W_TR, W_CH>;
+  pdl_launch_dependents();  // (after the wait: the combine reads the batch's lengths before its own)
+  using P = Plan<W_TR, W_CH, W_UC>;
   P::build(a, G, pre);
   const Shares shares(pre[a.c.n_seqs], gridDim.x);
   if (blockIdx.x == 0)
     for (int b = tid; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
-  Walk<W_TR, W_CH> w;
+  Walk<W_TR, W_CH, W_UC> w;
   {
     const int n = shares.size(blockIdx.x);
     if (n == 0) return;
@@ -272,7 +281,8 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
 
   while (true) {
     const Kv8Seq s = w.s;
-    const int c0 = w.at - w.first, c1 = min(w.n_chunks, w.end - w.first);
+    const int c0 = w.c0(), c1 = w.c1();
+    if (c1 <= c0) return;  // (the share ends within the unit's constant)
     const int keys = s.len + s.n;  // slots that hold a token
     const int rows = s.n * G, r0 = w.tile * W_TR;
     // ---- queries: fragments of this lane's rows g, g + 8, scaled
@@ -311,15 +321,15 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
       }
     }
     float o[NT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    int E = 0;  // o is in units of 2^E; set by the first page
-    bool have_E = false;
+    int E = -4096;  // o is in units of 2^E (set by the first page)
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
     const int tok[2] = {min(r0 + g, rows - 1) / G, min(r0 + g + 8, rows - 1) / G};  // of the lane's rows
 
-    // ---- this warp's pages: page index W_WARPS c + warp of each chunk c, up to the last one that holds a token
+    // ---- this warp's pages: page index W_WARPS c + warp of each chunk c, up to the last one that holds a token.
+    // They go in pairs; a pair's missing second page is loaded as zeros and masked.
     const int p_first = c0 * W_WARPS + warp;
     const int p_end = min(c1 * W_WARPS, (keys + kPage - 1) / kPage);
     const int n_pages = p_end > p_first ? (p_end - p_first + W_WARPS - 1) / W_WARPS : 0;
@@ -336,73 +346,96 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
         }
       }
     };
-    auto issue = [&](int i) {  // loads of the warp's i'th page (zeros for slots without a token)
-      if (i < n_pages) {
-        if ((i & 31) == 0) fetch_ids(i);
-        const int id = __shfl_sync(0xffffffffu, id_l, i & 31);
-        const int slot0 = (p_first + i * W_WARPS) * kPage;
-        const long long off = ((long long)max(id, 0) * Hkv + w.kvh) * PAGE_BYTES;
-        const uint32_t dst = ring + (i % W_STAGES) * (2 * PAGE_BYTES);
+    auto issue = [&](int i0) {  // loads of the warp's i0'th pair of pages (zeros for slots without a token)
+      if (2 * i0 < n_pages) {
+        if ((2 * i0 & 31) == 0) fetch_ids(2 * i0);
 #pragma unroll
-        for (int j = 0; j < PAGE_BYTES / 512; ++j) {
-          const int piece = j * 32 + lane, r = piece / (HD / 16), c = piece % (HD / 16);
-          const bool in = id >= 0 && slot0 + r < keys;
-          cp_async16_zfill(dst + w_piece<HD>(r, c), Kc + off + piece * 16, in);
-          cp_async16_zfill(dst + PAGE_BYTES + w_piece<HD>(r, c), Vc + off + piece * 16, in);
+        for (int x = 0; x < 2; ++x) {
+          const int i = 2 * i0 + x, id = __shfl_sync(0xffffffffu, id_l, i & 31);
+          const int slot0 = (p_first + i * W_WARPS) * kPage;
+          const long long off = ((long long)max(id, 0) * Hkv + w.kvh) * PAGE_BYTES;
+          const uint32_t dst = ring + (i % W_STAGES) * (2 * PAGE_BYTES);
+#pragma unroll
+          for (int j = 0; j < PAGE_BYTES / 512; ++j) {
+            const int piece = j * 32 + lane, r = piece / (HD / 16), c = piece % (HD / 16);
+            const bool in = id >= 0 && slot0 + r < keys;
+            cp_async16_zfill(dst + w_piece<HD>(r, c), Kc + off + piece * 16, in);
+            cp_async16_zfill(dst + PAGE_BYTES + w_piece<HD>(r, c), Vc + off + piece * 16, in);
+          }
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    for (int i = 0; i < W_STAGES - 1; ++i) issue(i);
-    for (int i = 0; i < n_pages; ++i) {
+    auto rescale = [&](float x0, float x1) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) o[j][0] *= x0, o[j][1] *= x0, o[j][2] *= x1, o[j][3] *= x1;
+    };
+    issue(0);
+    for (int i0 = 0; 2 * i0 < n_pages; ++i0) {
+      const int i = 2 * i0;
       if ((i & 31) == 0) e_cur = e_l;  // (the next 32 pages' are fetched later in this group)
-      asm volatile("cp.async.wait_group %0;" ::"n"(W_STAGES - 2) : "memory");
-      __syncwarp();  // every lane's pieces of page i; and every lane is done with the stage that is loaded next
-      issue(i + W_STAGES - 1);
-      const int e2 = __shfl_sync(0xffffffffu, e_cur, i & 31);
-      const int ek = (int)(int8_t)(e2 & 0xff), ev = (int)(int8_t)(e2 >> 8);
-      const uint32_t sk = ring + (i % W_STAGES) * (2 * PAGE_BYTES), sv = sk + PAGE_BYTES;
-      // ---- S: two n-tiles of 8 keys
-      float sc[2][4];
+      issue(i0 + 1);
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+      __syncwarp();  // every lane's pieces of the pair
+      const uint32_t stage = ring + (i % W_STAGES) * (2 * PAGE_BYTES);
+      // ---- S: two n-tiles of 8 keys a page
+      float sc[2][2][4];
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sc[n][k] = 0.f;
-#pragma unroll
-        for (int pc = 0; pc < PK; ++pc) {
-          uint32_t wd[4];
-          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                       : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3])
-                       : "r"(sk + w_piece<HD>(g + 8 * n, PK * t + pc))
-                       : "memory");
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t b0 = e4m3x2_to_f16x2(wd[k]), b1 = e4m3x2_to_f16x2(wd[k] >> 16);
-#pragma unroll
-            for (int x = 0; x < NS; ++x) mma_f16(sc[n], qf[x][pc * 4 + k], b0, b1);
-          }
-        }
-      }
-      const float fu[2] = {pow2i(ek) * f[0], pow2i(ek) * f[1]};
-      const int kp0 = (p_first + i * W_WARPS) * kPage;
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sc[n][k] *= fu[k >> 1];
-      if (kp0 + kPage > s.len) {
+      for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int kp = kp0 + 8 * n + 2 * t + (k & 1);
-            if (kp >= s.len && !(kp < keys && sees_new(a, s, tok[k >> 1], kp))) sc[n][k] = -INFINITY;
+          for (int k = 0; k < 4; ++k) sc[x][n][k] = 0.f;
+#pragma unroll
+      for (int pc = 0; pc < PK; ++pc)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            uint32_t wd[4];
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                         : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3])
+                         : "r"(stage + x * 2 * PAGE_BYTES + w_piece<HD>(g + 8 * n, PK * t + pc))
+                         : "memory");
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t b0 = e4m3x2_to_f16x2(wd[k]), b1 = e4m3x2_to_f16x2(wd[k] >> 16);
+#pragma unroll
+              for (int y = 0; y < NS; ++y) mma_f16(sc[x][n], qf[y][pc * 4 + k], b0, b1);
+            }
           }
+      const int kp0 = (p_first + i * W_WARPS) * kPage;
+      int ev[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int e2 = __shfl_sync(0xffffffffu, e_cur, (i + x) & 31);
+        ev[x] = x == 1 && i + 1 == n_pages ? ev[0] : (int)(int8_t)(e2 >> 8);
+        const float unit = pow2i((int)(int8_t)(e2 & 0xff)), fu[2] = {unit * f[0], unit * f[1]};
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sc[x][n][k] *= fu[k >> 1];
       }
-      // ---- reference maxima (rows g, g + 8) and the reference exponent, raised for the whole warp together
-      const float mx[2] = {fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1])),
-                           fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]))};
-      const bool far_E = !have_E || ev - E > W_EV_MAX || ev < E;
-      if (__any_sync(0xffffffffu, mx[0] > m[0] + W_LAG || mx[1] > m[1] + W_LAG) || far_E) {
+      if (kp0 + (W_WARPS + 1) * kPage > s.len || i + 1 == n_pages) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int kp = kp0 + x * W_WARPS * kPage + 8 * n + 2 * t + (k & 1);
+              if (i + x >= n_pages || (kp >= s.len && !(kp < keys && sees_new(a, s, tok[k >> 1], kp)))) sc[x][n][k] = -INFINITY;
+            }
+      }
+      // ---- reference maxima (rows g, g + 8), raised for the whole warp together
+      float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) mx[k >> 1] = fmaxf(mx[k >> 1], sc[x][n][k]);
+      if (__any_sync(0xffffffffu, mx[0] > m[0] + W_LAG || mx[1] > m[1] + W_LAG)) {
         float al[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -413,67 +446,66 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
           m[k] = mn;
           l[k] *= al[k];
         }
-        if (far_E) {
-          const int E2 = ev - W_EV_SET;
-          // (a step beyond 2^+-126: what was summed is out of the new unit's reach one way or the other)
-          const float step = have_E ? pow2i(max(-126, min(126, E - E2))) : 0.f;
-          al[0] *= step;
-          al[1] *= step;
-          E = E2;
-          have_E = true;
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[j][k] *= al[k >> 1];
+        rescale(al[0], al[1]);
       }
-      // ---- P, then O += P V
       const float nb[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
-      const float up = pow2i(ev - E);
-      uint32_t pf[NS][4];
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const float p0 = ex2_ftz(sc[n][2 * k] + nb[k]), p1 = ex2_ftz(sc[n][2 * k + 1] + nb[k]);
-          l[k] += p0 + p1;
-          float lo = p0 * up, hi = p1 * up;
-#pragma unroll
-          for (int x = 0; x < NS; ++x) {
-            pf[x][2 * n + k] = pack_f16(lo, hi);
-            const float2 got = unpack_f16(pf[x][2 * n + k]);
-            lo -= got.x;
-            hi -= got.y;
-          }
+      for (int x = 0; x < 2; ++x) {
+        // ---- the reference exponent (a step beyond 2^+-126: what was summed is out of the new unit's reach)
+        if (ev[x] < E || ev[x] - E > W_EV_MAX) {
+          const float step = pow2i(max(-126, min(126, E - (ev[x] - W_EV_SET))));
+          E = ev[x] - W_EV_SET;
+          rescale(step, step);
         }
-      // codes of the lane's four keys at NT consecutive dims, as pairs of keys
-      uint32_t vw[4][NT / 4];
+        // ---- P, then O += P V
+        const float up = pow2i(ev[x] - E);
+        uint32_t pf[NS][4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int key = 2 * t + (k & 1) + 8 * (k >> 1);
-        if constexpr (HD == 128)
-          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                       : "=r"(vw[k][0]), "=r"(vw[k][1]), "=r"(vw[k][2]), "=r"(vw[k][3])
-                       : "r"(sv + w_piece<HD>(key, g))
-                       : "memory");
-        else
-          asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];"
-                       : "=r"(vw[k][0]), "=r"(vw[k][1])
-                       : "r"(sv + w_piece<HD>(key, g >> 1) + (g & 1) * 8)
-                       : "memory");
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float p0 = ex2_ftz(sc[x][n][2 * k] + nb[k]), p1 = ex2_ftz(sc[x][n][2 * k + 1] + nb[k]);
+            l[k] += p0 + p1;
+            float lo = p0 * up, hi = p1 * up;
+#pragma unroll
+            for (int y = 0; y < NS; ++y) {
+              pf[y][2 * n + k] = pack_f16(lo, hi);
+              const float2 got = unpack_f16(pf[y][2 * n + k]);
+              lo -= got.x;
+              hi -= got.y;
+            }
+          }
+        // codes of the lane's four keys at NT consecutive dims, as pairs of keys
+        const uint32_t sv = stage + x * 2 * PAGE_BYTES + PAGE_BYTES;
+        uint32_t vw[4][NT / 4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int key = 2 * t + (k & 1) + 8 * (k >> 1);
+          if constexpr (HD == 128)
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                         : "=r"(vw[k][0]), "=r"(vw[k][1]), "=r"(vw[k][2]), "=r"(vw[k][3])
+                         : "r"(sv + w_piece<HD>(key, g))
+                         : "memory");
+          else
+            asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];"
+                         : "=r"(vw[k][0]), "=r"(vw[k][1])
+                         : "r"(sv + w_piece<HD>(key, g >> 1) + (g & 1) * 8)
+                         : "memory");
+        }
+#pragma unroll
+        for (int q = 0; q < NT / 4; ++q)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t sel = h ? 0x7362u : 0x5140u;
+            const uint32_t c0w = __byte_perm(vw[0][q], vw[1][q], sel), c1w = __byte_perm(vw[2][q], vw[3][q], sel);
+#pragma unroll
+            for (int y = 0; y < NS; ++y) {
+              mma_f16(o[4 * q + 2 * h], pf[y], e4m3x2_to_f16x2(c0w), e4m3x2_to_f16x2(c1w));
+              mma_f16(o[4 * q + 2 * h + 1], pf[y], e4m3x2_to_f16x2(c0w >> 16), e4m3x2_to_f16x2(c1w >> 16));
+            }
+          }
       }
-#pragma unroll
-      for (int q = 0; q < NT / 4; ++q)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t sel = h ? 0x7362u : 0x5140u;
-          const uint32_t c0w = __byte_perm(vw[0][q], vw[1][q], sel), c1w = __byte_perm(vw[2][q], vw[3][q], sel);
-#pragma unroll
-          for (int x = 0; x < NS; ++x) {
-            mma_f16(o[4 * q + 2 * h], pf[x], e4m3x2_to_f16x2(c0w), e4m3x2_to_f16x2(c1w));
-            mma_f16(o[4 * q + 2 * h + 1], pf[x], e4m3x2_to_f16x2(c0w >> 16), e4m3x2_to_f16x2(c1w >> 16));
-          }
-        }
+      __syncwarp();  // every lane is done with the stages that the next round loads
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     // ---- join the four warps' states
@@ -526,25 +558,31 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
         if (d == 0) st[W_TR * HD + r] = M, st[W_TR * (HD + 1) + r] = L;
       }
     }
-    w.at = w.first + c1;
-    if (w.at >= w.end) return;
+    if (!w.next(a, G)) return;
     __syncthreads();
-    w.next(a, G);
   }
 }
 
 // ---------------------------------------------------------------------------------------------
-// Joins the partial states of the units that several CTAs share: one warp per (row, query head). n: CTAs of the
-// kernel that left them.
+// Joins the partial states of the units that several CTAs share, by RW warps per (row, query head). n: CTAs of the
+// kernel that left them. Which states there are follows from the batch's lengths, which were complete before
+// that kernel let this one in, so with up to 32 sequences only the states are left to read after the wait.
 // ---------------------------------------------------------------------------------------------
-template <typename T, int HD, int TR, int CH>
-__global__ void __launch_bounds__(256) k_kv8_combine(const Kv8AttnParams a, int n) {
+constexpr int CB_WARPS = 8;
+template <typename T, int HD, int TR, int CH, int UC, int RW>
+__global__ void __launch_bounds__(32 * CB_WARPS) k_kv8_combine(const Kv8AttnParams a, int n) {
+  using P = Plan<TR, CH, UC>;
+  constexpr int D = HD / 32;
+  __shared__ float s_m[CB_WARPS], s_l[CB_WARPS], s_o[RW > 1 ? CB_WARPS : 1][HD];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % RW;
   pdl_launch_dependents();
-  pdl_wait();
-  const int lane = threadIdx.x & 31;
-  const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long i = (long long)blockIdx.x * (CB_WARPS / RW) + warp / RW;
   const int G = a.n_heads / a.c.n_kv_heads;
-  if (i >= (long long)a.r.n_rows * a.n_heads) return;
+  // (uniform over a row's warps; with RW > 1 the CTA holds one row, so it leaves as a whole)
+  if (i >= (long long)a.r.n_rows * a.n_heads) {
+    pdl_wait();
+    return;
+  }
   const int row = (int)(i / a.n_heads), head = (int)(i % a.n_heads);
   // the sequence of the row
   int lo = 0, m = a.c.n_seqs;
@@ -556,61 +594,116 @@ __global__ void __launch_bounds__(256) k_kv8_combine(const Kv8AttnParams a, int 
     m = min(step, m - k * step);
   }
   const Kv8Seq s = kv8_seq(a.c, a.r, lo, a.err);
-  if (row < s.row0 || row >= s.row0 + s.n) return;
+  const bool live = row >= s.row0 && row < s.row0 + s.n;
   const int tr = (row - s.row0) * G + head % G, tile = tr / TR, r = tr % TR;
-  const int base = a.plan[lo], per_head = (a.plan[lo + 1] - base) / a.c.n_kv_heads;
-  const Shares shares(a.plan[a.c.n_seqs], n);
-  using P = Plan<TR, CH>;
   int before = 0;
-  for (int t = lane; t < tile; t += 32) before += P::chunks(a, s, G, t);
-#pragma unroll
-  for (int sh = 16; sh > 0; sh >>= 1) before += __shfl_xor_sync(0xffffffffu, before, sh);
-  const int first = base + head / G * per_head + before, end = first + P::chunks(a, s, G, tile);
-  const int i0 = shares.of(first), i1 = shares.of(end - 1);
+  for (int t = lane; live && t < tile; t += 32) before += UC + P::chunks(a, s, G, t);
+  before = __reduce_add_sync(0xffffffffu, before);
+  int base, per_seq, total;
+  if (a.c.n_seqs <= 32) {
+    const int mine = lane < a.c.n_seqs ? P::per_head(a, kv8_seq(a.c, a.r, lane, a.err), G) * a.c.n_kv_heads : 0;
+    total = __reduce_add_sync(0xffffffffu, mine);
+    base = __reduce_add_sync(0xffffffffu, lane < lo ? mine : 0);
+    per_seq = __shfl_sync(0xffffffffu, mine, lo);
+    pdl_wait();
+  } else {
+    pdl_wait();
+    base = a.plan[lo];
+    per_seq = a.plan[lo + 1] - base;
+    total = a.plan[a.c.n_seqs];
+  }
+  if (!live) return;
+  const Shares shares(total, n);
+  const int first = base + head / G * (per_seq / a.c.n_kv_heads) + before + UC, last = first + P::chunks(a, s, G, tile) - 1;
+  const int i0 = shares.of(first), i1 = shares.of(last);
   if (i0 == i1) return;  // finished by the one CTA that held it
-  auto state = [&](int c) { return c > i1 ? nullptr : a.states + (long long)shares.slot(first, c) * (TR * (HD + 2)); };
-  // each lane: the statistics of every 32nd CTA
-  float M = -INFINITY;
-  for (int c = i0 + lane; c <= i1; c += 32)
-    if (const float* st = state(c)) M = fmaxf(M, st[TR * HD + r]);
-#pragma unroll
-  for (int sh = 16; sh > 0; sh >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, sh));
-  float L = 0.f;
-  for (int c = i0 + lane; c <= i1; c += 32)
-    if (const float* st = state(c)) {
-      const float mc = st[TR * HD + r], lc = st[TR * (HD + 1) + r];
-      L += mc == -INFINITY ? lc : exp2f(mc - M) * lc;  // (nothing seen: 0, or NaN)
-    }
-#pragma unroll
-  for (int sh = 16; sh > 0; sh >>= 1) L += __shfl_xor_sync(0xffffffffu, L, sh);
-  const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
-  constexpr int D = HD / 32;
-  float o[D];
+  auto state = [&](int c) { return a.states + (long long)shares.slot(first, c) * (TR * (HD + 2)); };
+  // this warp's states c = i0 + part, + RW, ...: 32 at a time, lane j the statistics of the j'th, and of these B at a
+  // time in flight
+  constexpr int B = 8;
+  const int mine = i1 - i0 - part >= 0 ? (i1 - i0 - part) / RW + 1 : 0;
+  float M = -INFINITY, L = 0.f, o[D];  // O as the weighted mean of what was joined so far, of weight L 2^M
 #pragma unroll
   for (int j = 0; j < D; ++j) o[j] = 0.f;
-  for (int c0 = i0; c0 <= i1; c0 += 32) {
-    const float* st = state(c0 + lane);
-    float wt = 0.f;
-    if (st) {
-      const float mc = st[TR * HD + r];
-      wt = mc == -INFINITY ? 0.f : exp2f(mc - M) * st[TR * (HD + 1) + r] * il;
-    }
-    for (int k = 0; k < 32 && c0 + k <= i1; ++k) {
-      const unsigned long long pk = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(st), k);
-      const float wk = __shfl_sync(0xffffffffu, wt, k);
-      if (!pk || wk == 0.f) continue;
-      const float* sk = reinterpret_cast<const float*>(pk) + r * HD + D * lane;
+  for (int k0 = 0; k0 < mine; k0 += 32) {
+    const float* st = k0 + lane < mine ? state(i0 + part + (k0 + lane) * RW) : nullptr;
+    float ov[B][D];
+    auto fetch = [&](int k) {
 #pragma unroll
-      for (int j = 0; j < D; ++j) o[j] = fmaf(wk, sk[j], o[j]);
+      for (int x = 0; x < B; ++x) {
+        const float* sx = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(st), k + x));
+#pragma unroll
+        for (int j = 0; j < D; ++j) ov[x][j] = sx ? sx[r * HD + D * lane + j] : 0.f;
+      }
+    };
+    const float mc = st ? st[TR * HD + r] : -INFINITY, lc = st ? st[TR * (HD + 1) + r] : 0.f;
+    fetch(0);
+    float mn = mc;
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) mn = fmaxf(mn, __shfl_xor_sync(0xffffffffu, mn, sh));
+    mn = fmaxf(M, mn);
+    float w = mc == -INFINITY ? lc : exp2f(mc - mn) * lc;  // (nothing seen: 0, or NaN)
+    const float was = M == -INFINITY ? L : exp2f(M - mn) * L;
+    float Ln = w;
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) Ln += __shfl_xor_sync(0xffffffffu, Ln, sh);
+    Ln += was;
+    const float il = Ln == 0.f ? 0.f : 1.f / Ln;
+    w *= il;
+#pragma unroll
+    for (int j = 0; j < D; ++j) o[j] *= was * il;
+    for (int k = 0; k < 32 && k0 + k < mine; k += B) {
+      if (k > 0) fetch(k);
+#pragma unroll
+      for (int x = 0; x < B; ++x) {
+        const float wx = __shfl_sync(0xffffffffu, w, k + x);
+        if (wx != 0.f) {
+#pragma unroll
+          for (int j = 0; j < D; ++j) o[j] = fmaf(wx, ov[x][j], o[j]);
+        }
+      }
     }
+    M = mn;
+    L = Ln;
   }
-  if (!(L >= 0.f))  // NaN scores only
+  if constexpr (RW > 1) {  // the row's warps, in order
+    if (lane == 0) s_m[warp] = M, s_l[warp] = L;
 #pragma unroll
-    for (int j = 0; j < D; ++j) o[j] = L;
+    for (int j = 0; j < D; ++j) s_o[warp][D * lane + j] = o[j];
+    __syncthreads();
+    if (warp > 0) return;
+    float mn = s_m[0];
+    for (int q = 1; q < RW; ++q) mn = fmaxf(mn, s_m[q]);
+    float w[RW], Ln = 0.f;
+#pragma unroll
+    for (int q = 0; q < RW; ++q) {
+      w[q] = s_m[q] == -INFINITY ? s_l[q] : exp2f(s_m[q] - mn) * s_l[q];
+      Ln += w[q];
+    }
+    const float il = Ln == 0.f ? 0.f : 1.f / Ln;
+#pragma unroll
+    for (int j = 0; j < D; ++j) o[j] = 0.f;
+#pragma unroll
+    for (int q = 0; q < RW; ++q)
+      if (w[q] != 0.f) {
+#pragma unroll
+        for (int j = 0; j < D; ++j) o[j] = fmaf(w[q] * il, s_o[q][D * lane + j], o[j]);
+      }
+    M = mn;
+    L = Ln;
+  }
   T* dst = reinterpret_cast<T*>(a.out) + i * HD + D * lane;
 #pragma unroll
   for (int j = 0; j < D; j += 2) store2(dst + j, o[j], o[j + 1]);
   if (a.lse && lane == 0) a.lse[i] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+}
+
+// One warp a row; a CTA a row where rows are few, since then many CTAs share a unit.
+template <typename T, int HD, int TR, int CH, int UC>
+cudaError_t launch_combine(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
+  const long long rows = (long long)a.r.n_rows * a.n_heads;
+  if (rows <= 1024) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, CB_WARPS>, dim3((unsigned)rows), dim3(32 * CB_WARPS), 0, st, a, ctas);
+  return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 1>, dim3((unsigned)((rows + CB_WARPS - 1) / CB_WARPS)), dim3(32 * CB_WARPS), 0, st, a, ctas);
 }
 
 struct DeviceInfo {
@@ -655,8 +748,7 @@ template <typename T, int HD, int NS>
 cudaError_t launch_rows(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
   cudaError_t e = kv8_launch(k_kv8_attn_rows<T, HD, NS>, dim3(ctas), dim3(32 * W_WARPS), w_smem<HD>(), st, a);
   if (e != cudaSuccess) return e;
-  const long long warps = (long long)a.r.n_rows * a.n_heads;
-  return kv8_launch(k_kv8_combine<T, HD, W_TR, W_CH>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a, ctas);
+  return launch_combine<T, HD, W_TR, W_CH, W_UC>(a, ctas, st);
 }
 
 }  // namespace
@@ -691,7 +783,7 @@ extern "C" jf_status jf_op_kv8_attention(const jf_kv8_cache* cache, const jf_kv8
   {  // chunks and rows are counted in 32 bits
     const long long group_rows = (long long)rows->n_rows * (n_heads / cache->n_kv_heads);
     const long long units = (group_rows / W_TR + cache->n_seqs) * cache->n_kv_heads;
-    const long long chunks = (long long)cache->pages_per_seq * kPage / W_CH + 1;
+    const long long chunks = (long long)cache->pages_per_seq * kPage / W_CH + 1 + W_UC;
     if (group_rows * cache->n_kv_heads > 0x3fffffffll || units > 0x7fffffffll / chunks) return JF_EUNSUPPORTED;
   }
   size_t need = 0;
