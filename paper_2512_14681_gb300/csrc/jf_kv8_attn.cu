@@ -10,9 +10,9 @@
 //
 // Work is split evenly whatever the batch: a unit is (sequence, KV head, tile of (token, head) query rows), a
 // chunk a run of keys of one unit. Units lie one after the other, each as long as its chunks plus a constant for
-// what a unit costs beside them (its queries, its end), and each of N CTAs takes an N'th of that length. A unit
-// whose chunks one CTA holds entirely is finished there; of the others each CTA leaves a partial state (m, l, O) in
-// the workspace, at most two a CTA, and k_kv8_combine joins a row's states in CTA order.
+// what a unit costs beside them (its queries, its end), and each of N workers takes an N'th of that length. A unit
+// whose chunks one worker holds entirely is finished there; of the others each worker leaves a partial state (m, l,
+// O) in the workspace, at most two a worker, and k_kv8_combine joins a row's states in their order.
 #include "../../include/jf_ops.h"
 #include "jf_kv8.cuh"
 #include "jf_once.h"
@@ -99,17 +99,17 @@ struct Shares {
   JF_DEV Shares(int total, int n) : each(total / n), more(total - total / n * n) {}
   JF_DEV int begin(int i) const { return i * each + min(i, more); }
   JF_DEV int size(int i) const { return each + (i < more ? 1 : 0); }
-  // The CTA that holds place x.
+  // The worker that holds place x.
   JF_DEV int of(int x) const {
     const int cut = more * (each + 1);
     return x < cut ? x / (each + 1) : more + (x - cut) / each;
   }
-  // Where CTA i leaves its part of a unit whose chunks begin at place `first`: a CTA has at most one unit whose
-  // first chunk lies before its share, and one that goes on after it.
+  // Where worker i leaves its part of a unit whose chunks begin at place `first`: it has at most one unit whose first
+  // chunk lies before its share, and one that goes on after it.
   JF_DEV int slot(int first, int i) const { return 2 * i + (begin(i) > first ? 0 : 1); }
 };
 
-// A CTA's walk over the units of its share. Uniform over the CTA.
+// A worker's walk over the units of its share. Uniform over the worker's threads.
 template <int TR, int CH, int UC>
 struct Walk {
   using P = Plan<TR, CH, UC>;
@@ -212,10 +212,10 @@ JF_DEV int query_shift(float amax) {
 // ---------------------------------------------------------------------------------------------
 // Few query rows per KV head (single-token serving; fp32 at any row count): warp-level products.
 //
-// A CTA's four warps share a tile of 16 query rows; each takes one page (16 keys) of a 64-key chunk at a time and
-// keeps its own softmax state; the four states are joined when the unit's share ends. A warp streams its pages
-// through a ring of its own in shared memory (cp.async, 16-byte pieces swizzled so that both fragment loads are
-// free of bank conflicts), so no barrier stands between loads and products.
+// A worker is one warp, with a tile of 16 query rows and a chunk of two pages (32 keys) a step. It streams its pages
+// through a ring of its own in shared memory (cp.async, 16-byte pieces swizzled so that both fragment loads are free
+// of bank conflicts), so no barrier stands anywhere between loads, products and the end of a unit, and the cost of
+// a unit's ends is hidden by the other warps of the SM.
 //
 // m16n8k16 fragments, lane = 4 g + t. S = Q K^T contracts over dims, whose order is free as long as Q's follows
 // it: lane t's four values of each k-step are four consecutive dims (one 32-bit word of codes) of the 16-byte
@@ -223,16 +223,13 @@ JF_DEV int query_shift(float amax) {
 // as it held their scores, and needs these keys' codes at dims NT g + j, j = 0 .. NT - 1, of the n-tiles j.
 // NS: fp16 terms of queries and probabilities (1 for bf16 models, 2 for fp32).
 // ---------------------------------------------------------------------------------------------
-constexpr int W_WARPS = 4, W_TR = 16, W_CH = W_WARPS * kPage, W_UC = 3;
-constexpr int W_STAGES = 4;  // two pairs of pages
+constexpr int W_WARPS = 4, W_TR = 16, W_CH = 2 * kPage, W_UC = 3;
+constexpr int W_STAGES = 2;  // chunks in a warp's ring
 constexpr float W_LAG = 4.f;             // a row's reference maximum follows its scores when they exceed it by more
 constexpr int W_EV_SET = 5, W_EV_MAX = 10;  // e_v - E: where E is set, largest (p' <= 2^14); smallest 0
 
 template <int HD>
-constexpr int w_smem() {
-  const int ring = W_WARPS * W_STAGES * 2 * kPage * HD, join = W_WARPS * W_TR * (HD + 4) * 4;
-  return ring > join ? ring : join;
-}
+constexpr int w_smem() { return W_WARPS * W_STAGES * 2 * W_CH * HD; }
 
 JF_DEV void cp_async16_zfill(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
@@ -252,73 +249,106 @@ JF_DEV void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t
 }
 
 template <typename T, int HD, int NS>
-__global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows(const Kv8AttnParams a) {
+__global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8AttnParams a) {
   constexpr int KS = HD / 16;   // k-steps of S
   constexpr int NT = HD / 8;    // n-tiles of O
   constexpr int PK = HD / 64;   // 16-byte pieces of a key that a lane reads
-  constexpr int PAGE_BYTES = kPage * HD;
+  constexpr int PAGE_BYTES = kPage * HD, STAGE_BYTES = 4 * PAGE_BYTES;  // K and V of the first page, of the second
   extern __shared__ __align__(128) uint8_t sm[];
   __shared__ int pre[kKv8MaxSeqs + 1];
-  __shared__ float s_ml[W_WARPS][W_TR][3];  // m, l, E as 2^E's exponent
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int G = a.n_heads / a.c.n_kv_heads, Hkv = a.c.n_kv_heads;
   pdl_wait();
   pdl_launch_dependents();  // (after the wait: the combine reads the batch's lengths before its own)
-  using P = Plan<W_TR, W_CH, W_UC>;
-  P::build(a, G, pre);
-  const Shares shares(pre[a.c.n_seqs], gridDim.x);
+  Plan<W_TR, W_CH, W_UC>::build(a, G, pre);
   if (blockIdx.x == 0)
     for (int b = tid; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
+  const int worker = blockIdx.x * W_WARPS + warp;
+  const Shares shares(pre[a.c.n_seqs], gridDim.x * W_WARPS);
+  if (shares.size(worker) == 0) return;
   Walk<W_TR, W_CH, W_UC> w;
-  {
-    const int n = shares.size(blockIdx.x);
-    if (n == 0) return;
-    w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + n);
-  }
-  const uint32_t ring = smem_u32(sm) + warp * (W_STAGES * 2 * PAGE_BYTES);
+  w.start(a, pre, G, shares.begin(worker), shares.begin(worker) + shares.size(worker));
+  const uint32_t ring = smem_u32(sm) + warp * (W_STAGES * STAGE_BYTES);
   const bool q16 = ((uintptr_t)a.q & 15) == 0 && a.ld_q * sizeof(T) % 16 == 0;
   const uint8_t *Kc = reinterpret_cast<const uint8_t*>(a.c.k), *Vc = reinterpret_cast<const uint8_t*>(a.c.v);
 
   while (true) {
     const Kv8Seq s = w.s;
-    const int c0 = w.c0(), c1 = w.c1();
-    if (c1 <= c0) return;  // (the share ends within the unit's constant)
+    const int c0 = w.c0(), c1 = w.c1(), n = c1 - c0;
+    if (n <= 0) return;  // (the share ends within the unit's constant)
     const int keys = s.len + s.n;  // slots that hold a token
     const int rows = s.n * G, r0 = w.tile * W_TR;
+
+    // ---- loads of the n chunks. Lane j of a group of 32 pages: page j's id and exponents (K's and V's packed)
+    const int n_pages = min(2 * c1, (keys + kPage - 1) / kPage) - 2 * c0;
+    int id_l = -1, e_l = 0, e_cur = 0;  // of the pages being loaded; of those in use
+    auto issue = [&](int i) {  // chunk i of the share: zeros for slots without a token
+      if (i < n) {
+        if ((i & 15) == 0) {
+          id_l = -1;
+          e_l = 0;
+          if (2 * i + lane < n_pages) {
+            id_l = kv8_page(a.c, w.b, 2 * (c0 + i) + lane, a.err);
+            if (id_l >= 0) {
+              const long long blk = (long long)id_l * Hkv + w.kvh;
+              e_l = (int)(uint8_t)a.c.k_exp[blk] | (int)(uint8_t)a.c.v_exp[blk] << 8;
+            }
+          }
+        }
+        const uint32_t dst = ring + (i % W_STAGES) * STAGE_BYTES;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int id = __shfl_sync(0xffffffffu, id_l, (2 * i + x) & 31);
+          const int slot0 = (2 * (c0 + i) + x) * kPage;
+          const long long off = ((long long)max(id, 0) * Hkv + w.kvh) * PAGE_BYTES;
+#pragma unroll
+          for (int j = 0; j < PAGE_BYTES / 512; ++j) {
+            const int piece = j * 32 + lane, r = piece / (HD / 16), c = piece % (HD / 16);
+            const bool in = id >= 0 && slot0 + r < keys;
+            cp_async16_zfill(dst + 2 * x * PAGE_BYTES + w_piece<HD>(r, c), Kc + off + piece * 16, in);
+            cp_async16_zfill(dst + (2 * x + 1) * PAGE_BYTES + w_piece<HD>(r, c), Vc + off + piece * 16, in);
+          }
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < W_STAGES - 1; ++i) issue(i);
+
     // ---- queries: fragments of this lane's rows g, g + 8, scaled
     uint32_t qf[NS][KS][4];
     float f[2];
-    {
-      const T* Q = reinterpret_cast<const T*>(a.q);
+    int tok[2];  // of the lane's rows
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int row = r0 + g + 8 * i;
-        const bool live = row < rows;
-        const T* src = Q + (long long)(s.row0 + (live ? row / G : 0)) * a.ld_q + (long long)(w.kvh * G + (live ? row % G : 0)) * HD + PK * 16 * t;
-        float x[4 * KS];
-        float amax = 0.f;
-        load_run<4 * KS>(src, live, q16, x);
+    for (int i = 0; i < 2; ++i) {
+      const bool live = r0 + g + 8 * i < rows;
+      const int row = live ? r0 + g + 8 * i : 0;
+      tok[i] = row / G;
+      const T* src = reinterpret_cast<const T*>(a.q) + (long long)(s.row0 + tok[i]) * a.ld_q +
+                     (long long)(w.kvh * G + row - tok[i] * G) * HD + PK * 16 * t;
+      float x[4 * KS];
+      float amax = 0.f;
+      load_run<4 * KS>(src, live, q16, x);
 #pragma unroll
-        for (int j = 0; j < 4 * KS; ++j) amax = fmaxf(amax, fabsf(x[j]));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-        amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const int sh = query_shift(amax);
-        const float up = pow2i(sh);
-        f[i] = pow2i(-sh) * a.scale_log2;
+      for (int j = 0; j < 4 * KS; ++j) amax = fmaxf(amax, fabsf(x[j]));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+      const int sh = query_shift(amax);
+      const float up = pow2i(sh);
+      f[i] = pow2i(-sh) * a.scale_log2;
 #pragma unroll
-        for (int j = 0; j < KS; ++j)
+      for (int j = 0; j < KS; ++j)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float lo = x[4 * j + 2 * h] * up, hi = x[4 * j + 2 * h + 1] * up;
+        for (int h = 0; h < 2; ++h) {
+          float lo = x[4 * j + 2 * h] * up, hi = x[4 * j + 2 * h + 1] * up;
 #pragma unroll
-            for (int n = 0; n < NS; ++n) {
-              qf[n][j][2 * h + i] = pack_f16(lo, hi);
-              const float2 got = unpack_f16(qf[n][j][2 * h + i]);
-              lo -= got.x;
-              hi -= got.y;
-            }
+          for (int y = 0; y < NS; ++y) {
+            qf[y][j][2 * h + i] = pack_f16(lo, hi);
+            const float2 got = unpack_f16(qf[y][j][2 * h + i]);
+            lo -= got.x;
+            hi -= got.y;
           }
-      }
+        }
     }
     float o[NT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     int E = -4096;  // o is in units of 2^E (set by the first page)
@@ -326,105 +356,64 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[j][i] = 0.f;
-    const int tok[2] = {min(r0 + g, rows - 1) / G, min(r0 + g + 8, rows - 1) / G};  // of the lane's rows
-
-    // ---- this warp's pages: page index W_WARPS c + warp of each chunk c, up to the last one that holds a token.
-    // They go in pairs; a pair's missing second page is loaded as zeros and masked.
-    const int p_first = c0 * W_WARPS + warp;
-    const int p_end = min(c1 * W_WARPS, (keys + kPage - 1) / kPage);
-    const int n_pages = p_end > p_first ? (p_end - p_first + W_WARPS - 1) / W_WARPS : 0;
-    int id_l = -1, e_l = 0, e_cur = 0;  // lane j: page 32 i + j: id, exponents of K and V packed; of the pages in use
-    auto fetch_ids = [&](int i0) {      // 32 pages from the warp's i0'th on
-      id_l = -1;
-      e_l = 0;
-      const int i = i0 + lane;
-      if (i < n_pages) {
-        id_l = kv8_page(a.c, w.b, p_first + i * W_WARPS, a.err);
-        if (id_l >= 0) {
-          const long long blk = (long long)id_l * Hkv + w.kvh;
-          e_l = (int)(uint8_t)a.c.k_exp[blk] | (int)(uint8_t)a.c.v_exp[blk] << 8;
-        }
-      }
-    };
-    auto issue = [&](int i0) {  // loads of the warp's i0'th pair of pages (zeros for slots without a token)
-      if (2 * i0 < n_pages) {
-        if ((2 * i0 & 31) == 0) fetch_ids(2 * i0);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int i = 2 * i0 + x, id = __shfl_sync(0xffffffffu, id_l, i & 31);
-          const int slot0 = (p_first + i * W_WARPS) * kPage;
-          const long long off = ((long long)max(id, 0) * Hkv + w.kvh) * PAGE_BYTES;
-          const uint32_t dst = ring + (i % W_STAGES) * (2 * PAGE_BYTES);
-#pragma unroll
-          for (int j = 0; j < PAGE_BYTES / 512; ++j) {
-            const int piece = j * 32 + lane, r = piece / (HD / 16), c = piece % (HD / 16);
-            const bool in = id >= 0 && slot0 + r < keys;
-            cp_async16_zfill(dst + w_piece<HD>(r, c), Kc + off + piece * 16, in);
-            cp_async16_zfill(dst + PAGE_BYTES + w_piece<HD>(r, c), Vc + off + piece * 16, in);
-          }
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    };
     auto rescale = [&](float x0, float x1) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) o[j][0] *= x0, o[j][1] *= x0, o[j][2] *= x1, o[j][3] *= x1;
     };
-    issue(0);
-    for (int i0 = 0; 2 * i0 < n_pages; ++i0) {
-      const int i = 2 * i0;
-      if ((i & 31) == 0) e_cur = e_l;  // (the next 32 pages' are fetched later in this group)
-      issue(i0 + 1);
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
-      __syncwarp();  // every lane's pieces of the pair
-      const uint32_t stage = ring + (i % W_STAGES) * (2 * PAGE_BYTES);
+
+    for (int i = 0; i < n; ++i) {
+      if ((i & 15) == 0) e_cur = e_l;  // (the next 32 pages' are fetched later in this group)
+      issue(i + W_STAGES - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(W_STAGES - 1) : "memory");
+      __syncwarp();  // every lane's pieces of chunk i
+      const uint32_t stage = ring + (i % W_STAGES) * STAGE_BYTES;
       // ---- S: two n-tiles of 8 keys a page
       float sc[2][2][4];
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sc[x][n][k] = 0.f;
+          for (int k = 0; k < 4; ++k) sc[x][u][k] = 0.f;
 #pragma unroll
       for (int pc = 0; pc < PK; ++pc)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
+          for (int u = 0; u < 2; ++u) {
             uint32_t wd[4];
             asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
                          : "=r"(wd[0]), "=r"(wd[1]), "=r"(wd[2]), "=r"(wd[3])
-                         : "r"(stage + x * 2 * PAGE_BYTES + w_piece<HD>(g + 8 * n, PK * t + pc))
+                         : "r"(stage + 2 * x * PAGE_BYTES + w_piece<HD>(g + 8 * u, PK * t + pc))
                          : "memory");
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               const uint32_t b0 = e4m3x2_to_f16x2(wd[k]), b1 = e4m3x2_to_f16x2(wd[k] >> 16);
 #pragma unroll
-              for (int y = 0; y < NS; ++y) mma_f16(sc[x][n], qf[y][pc * 4 + k], b0, b1);
+              for (int y = 0; y < NS; ++y) mma_f16(sc[x][u], qf[y][pc * 4 + k], b0, b1);
             }
           }
-      const int kp0 = (p_first + i * W_WARPS) * kPage;
+      const int kp0 = (c0 + i) * W_CH;
       int ev[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int e2 = __shfl_sync(0xffffffffu, e_cur, (i + x) & 31);
-        ev[x] = x == 1 && i + 1 == n_pages ? ev[0] : (int)(int8_t)(e2 >> 8);
+        const int e2 = __shfl_sync(0xffffffffu, e_cur, (2 * i + x) & 31);
+        ev[x] = x == 1 && 2 * i + 1 >= n_pages ? ev[0] : (int)(int8_t)(e2 >> 8);  // (no second page: as the first)
         const float unit = pow2i((int)(int8_t)(e2 & 0xff)), fu[2] = {unit * f[0], unit * f[1]};
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sc[x][n][k] *= fu[k >> 1];
+          for (int k = 0; k < 4; ++k) sc[x][u][k] *= fu[k >> 1];
       }
-      if (kp0 + (W_WARPS + 1) * kPage > s.len || i + 1 == n_pages) {
+      if (kp0 + W_CH > s.len) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int n = 0; n < 2; ++n)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const int kp = kp0 + x * W_WARPS * kPage + 8 * n + 2 * t + (k & 1);
-              if (i + x >= n_pages || (kp >= s.len && !(kp < keys && sees_new(a, s, tok[k >> 1], kp)))) sc[x][n][k] = -INFINITY;
+              const int kp = kp0 + 16 * x + 8 * u + 2 * t + (k & 1);
+              if (kp >= s.len && !(kp < keys && sees_new(a, s, tok[k >> 1], kp))) sc[x][u][k] = -INFINITY;
             }
       }
       // ---- reference maxima (rows g, g + 8), raised for the whole warp together
@@ -432,9 +421,9 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) mx[k >> 1] = fmaxf(mx[k >> 1], sc[x][n][k]);
+          for (int k = 0; k < 4; ++k) mx[k >> 1] = fmaxf(mx[k >> 1], sc[x][u][k]);
       if (__any_sync(0xffffffffu, mx[0] > m[0] + W_LAG || mx[1] > m[1] + W_LAG)) {
         float al[2];
 #pragma unroll
@@ -461,22 +450,22 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
         const float up = pow2i(ev[x] - E);
         uint32_t pf[NS][4];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const float p0 = ex2_ftz(sc[x][n][2 * k] + nb[k]), p1 = ex2_ftz(sc[x][n][2 * k + 1] + nb[k]);
+            const float p0 = ex2_ftz(sc[x][u][2 * k] + nb[k]), p1 = ex2_ftz(sc[x][u][2 * k + 1] + nb[k]);
             l[k] += p0 + p1;
             float lo = p0 * up, hi = p1 * up;
 #pragma unroll
             for (int y = 0; y < NS; ++y) {
-              pf[y][2 * n + k] = pack_f16(lo, hi);
-              const float2 got = unpack_f16(pf[y][2 * n + k]);
+              pf[y][2 * u + k] = pack_f16(lo, hi);
+              const float2 got = unpack_f16(pf[y][2 * u + k]);
               lo -= got.x;
               hi -= got.y;
             }
           }
         // codes of the lane's four keys at NT consecutive dims, as pairs of keys
-        const uint32_t sv = stage + x * 2 * PAGE_BYTES + PAGE_BYTES;
+        const uint32_t sv = stage + (2 * x + 1) * PAGE_BYTES;
         uint32_t vw[4][NT / 4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -505,74 +494,57 @@ __global__ void __launch_bounds__(32 * W_WARPS, NS == 1 ? 3 : 2) k_kv8_attn_rows
             }
           }
       }
-      __syncwarp();  // every lane is done with the stages that the next round loads
+      __syncwarp();  // every lane is done with the stage that the next round loads
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    // ---- join the four warps' states
+
+    // ---- the unit's end: normalised here (the sums themselves may be out of fp32's range where the values are near its
+    // end). Lane (g, t) holds dims 32 t .. 32 t + 31 (of 128; 16 t .. of 64) of its rows.
+    const bool whole = c0 == 0 && c1 == w.n_chunks;
+    float* st = a.states + (long long)shares.slot(w.first, worker) * (W_TR * (HD + 2));
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       l[k] += __shfl_xor_sync(0xffffffffu, l[k], 1);
       l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
-    }
-    __syncthreads();  // every warp is done with its ring
-    float* so = reinterpret_cast<float*>(sm) + warp * (W_TR * (HD + 4));
+      const int r = g + 8 * k;
+      if (r0 + r >= rows) continue;
+      const float il = l[k] > 0.f ? 1.f / l[k] : (l[k] == 0.f ? 0.f : l[k]), unit = pow2i(max(E, -126));
+      const long long at = (long long)(s.row0 + tok[k]) * a.n_heads + w.kvh * G + (r0 + r - tok[k] * G);
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) so[(g + 8 * (k >> 1)) * (HD + 4) + NT * ((2 * t + (k & 1))) + j] = o[j][k];
-    if (t == 0) {
-      s_ml[warp][g][0] = m[0], s_ml[warp][g][1] = l[0], s_ml[warp][g][2] = (float)E;
-      s_ml[warp][g + 8][0] = m[1], s_ml[warp][g + 8][1] = l[1], s_ml[warp][g + 8][2] = (float)E;
-    }
-    __syncthreads();
-    const bool whole = c0 == 0 && c1 == w.n_chunks;
-    float* st = a.states + (long long)shares.slot(w.first, blockIdx.x) * (W_TR * (HD + 2));
-    for (int i = tid; i < W_TR * (HD / 2); i += 32 * W_WARPS) {
-      const int r = i / (HD / 2), d = i % (HD / 2) * 2, row = r0 + r;
-      if (row >= rows) break;
-      float M = -INFINITY, Ew = -126.f;
+        for (int j = 0; j < NT; j += 4) {
+          const int d = NT * (2 * t + h) + j;
+          float v[4];
 #pragma unroll
-      for (int q = 0; q < W_WARPS; ++q) {
-        M = fmaxf(M, s_ml[q][r][0]);
-        if (s_ml[q][r][0] != -INFINITY) Ew = fmaxf(Ew, s_ml[q][r][2]);
-      }
-      float L = 0.f, x = 0.f, y = 0.f;  // x, y in units of 2^Ew
-#pragma unroll
-      for (int q = 0; q < W_WARPS; ++q) {
-        const float wt = s_ml[q][r][0] == -INFINITY ? 0.f : exp2f(s_ml[q][r][0] - M);
-        L = fmaf(wt, s_ml[q][r][1], L);
-        const float wo = wt * pow2i((int)fmaxf(s_ml[q][r][2] - Ew, -126.f));
-        const float* src = reinterpret_cast<float*>(sm) + q * (W_TR * (HD + 4)) + r * (HD + 4) + d;
-        if (wt != 0.f) x = fmaf(wo, src[0], x), y = fmaf(wo, src[1], y);
-      }
-      // normalised here: the sums themselves may be out of fp32's range where the values are near its end
-      const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L), unit = pow2i((int)Ew);
-      x = x * il * unit;
-      y = y * il * unit;
-      if (whole) {
-        const long long at = (long long)(s.row0 + row / G) * a.n_heads + w.kvh * G + row % G;
-        store2(reinterpret_cast<T*>(a.out) + at * HD + d, x, y);
-        if (a.lse && d == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
-      } else {
-        store2(st + r * HD + d, x, y);
-        if (d == 0) st[W_TR * HD + r] = M, st[W_TR * (HD + 1) + r] = L;
+          for (int q = 0; q < 4; ++q) v[q] = o[j + q][2 * k + h] * il * unit;
+          if (whole) {
+            T* dst = reinterpret_cast<T*>(a.out) + at * HD + d;
+            store2(dst, v[0], v[1]);
+            store2(dst + 2, v[2], v[3]);
+          } else {
+            store2(st + r * HD + d, v[0], v[1]);
+            store2(st + r * HD + d + 2, v[2], v[3]);
+          }
+        }
+      if (t == 0) {
+        if (!whole) st[W_TR * HD + r] = m[k], st[W_TR * (HD + 1) + r] = l[k];
+        else if (a.lse) a.lse[at] = l[k] == 0.f ? -INFINITY : (m[k] + log2f(l[k])) * 0.69314718055994531f;
       }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
     if (!w.next(a, G)) return;
-    __syncthreads();
   }
 }
 
 // ---------------------------------------------------------------------------------------------
-// Joins the partial states of the units that several CTAs share, by RW warps per (row, query head). n: CTAs of the
-// kernel that left them. Which states there are follows from the batch's lengths, which were complete before
+// Joins the partial states of the units that several workers share, by RW warps per (row, query head). n: workers of
+// the kernel that left them. Which states there are follows from the batch's lengths, which were complete before
 // that kernel let this one in, so with up to 32 sequences only the states are left to read after the wait.
 // ---------------------------------------------------------------------------------------------
-constexpr int CB_WARPS = 8;
 template <typename T, int HD, int TR, int CH, int UC, int RW>
-__global__ void __launch_bounds__(32 * CB_WARPS) k_kv8_combine(const Kv8AttnParams a, int n) {
+__global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv8AttnParams a, int n) {
   using P = Plan<TR, CH, UC>;
-  constexpr int D = HD / 32;
+  constexpr int D = HD / 32, CB_WARPS = RW > 8 ? RW : 8;
   __shared__ float s_m[CB_WARPS], s_l[CB_WARPS], s_o[RW > 1 ? CB_WARPS : 1][HD];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % RW;
   pdl_launch_dependents();
@@ -616,7 +588,7 @@ __global__ void __launch_bounds__(32 * CB_WARPS) k_kv8_combine(const Kv8AttnPara
   const Shares shares(total, n);
   const int first = base + head / G * (per_seq / a.c.n_kv_heads) + before + UC, last = first + P::chunks(a, s, G, tile) - 1;
   const int i0 = shares.of(first), i1 = shares.of(last);
-  if (i0 == i1) return;  // finished by the one CTA that held it
+  if (i0 == i1) return;  // finished by the one worker that held it
   auto state = [&](int c) { return a.states + (long long)shares.slot(first, c) * (TR * (HD + 2)); };
   // this warp's states c = i0 + part, + RW, ...: 32 at a time, lane j the statistics of the j'th, and of these B at a
   // time in flight
@@ -698,12 +670,14 @@ __global__ void __launch_bounds__(32 * CB_WARPS) k_kv8_combine(const Kv8AttnPara
   if (a.lse && lane == 0) a.lse[i] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-// One warp a row; a CTA a row where rows are few, since then many CTAs share a unit.
+// The fewer rows there are, the more workers share a unit, and the more warps join a row's states: a CTA of 16 up to
+// 256 rows, of 8 up to 2048, then a warp each.
 template <typename T, int HD, int TR, int CH, int UC>
-cudaError_t launch_combine(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
+cudaError_t launch_combine(const Kv8AttnParams& a, int workers, cudaStream_t st) {
   const long long rows = (long long)a.r.n_rows * a.n_heads;
-  if (rows <= 1024) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, CB_WARPS>, dim3((unsigned)rows), dim3(32 * CB_WARPS), 0, st, a, ctas);
-  return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 1>, dim3((unsigned)((rows + CB_WARPS - 1) / CB_WARPS)), dim3(32 * CB_WARPS), 0, st, a, ctas);
+  if (rows <= 256) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 16>, dim3((unsigned)rows), dim3(512), 0, st, a, workers);
+  if (rows <= 2048) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 8>, dim3((unsigned)rows), dim3(256), 0, st, a, workers);
+  return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a, workers);
 }
 
 struct DeviceInfo {
@@ -737,10 +711,11 @@ const DeviceInfo* device_info() {
 }
 
 struct Form {
-  int ctas, tile_rows;
+  int ctas, workers, tile_rows;
 };
 Form choose(const DeviceInfo& d, const jf_kv8_cache& c, const jf_kv8_rows& r, int dtype, int n_heads) {
-  return {d.sms * d.rows_ctas[(dtype == JF_F32 ? 2 : 0) + (c.head_dim == 128 ? 1 : 0)], W_TR};
+  const int ctas = d.sms * d.rows_ctas[(dtype == JF_F32 ? 2 : 0) + (c.head_dim == 128 ? 1 : 0)];
+  return {ctas, ctas * W_WARPS, W_TR};
 }
 size_t plan_bytes(const jf_kv8_cache& c) { return ((size_t)(c.n_seqs + 1) * 4 + 255) / 256 * 256; }
 
@@ -748,7 +723,7 @@ template <typename T, int HD, int NS>
 cudaError_t launch_rows(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
   cudaError_t e = kv8_launch(k_kv8_attn_rows<T, HD, NS>, dim3(ctas), dim3(32 * W_WARPS), w_smem<HD>(), st, a);
   if (e != cudaSuccess) return e;
-  return launch_combine<T, HD, W_TR, W_CH, W_UC>(a, ctas, st);
+  return launch_combine<T, HD, W_TR, W_CH, W_UC>(a, ctas * W_WARPS, st);
 }
 
 }  // namespace
@@ -764,7 +739,7 @@ extern "C" jf_status jf_op_kv8_attention_workspace_bytes(const jf_kv8_cache* cac
   const DeviceInfo* d = device_info();
   if (!d) return JF_ECUDA;
   const Form f = choose(*d, *cache, *rows, dtype, n_heads);
-  *out_bytes = plan_bytes(*cache) + (size_t)2 * f.ctas * f.tile_rows * (cache->head_dim + 2) * 4;
+  *out_bytes = plan_bytes(*cache) + (size_t)2 * f.workers * f.tile_rows * (cache->head_dim + 2) * 4;
   return JF_OK;
 }
 
