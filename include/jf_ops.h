@@ -122,7 +122,7 @@ jf_status jf_op_kv8_attention_workspace_bytes(const jf_kv8_cache* cache, const j
 /* Attention of the rows, whose keys and values have been appended, over the cache: out = softmax(scale *
  * q k^T) v for each of n_heads query heads (a multiple of n_kv_heads; head h reads KV head
  * h / (n_heads / n_kv_heads)), over the keys that the row sees. dtype: type of q and out. q: rows ld_q
- * elements apart (rotated: jf_op_kv8_append's q_out); out: [n_rows][n_heads][head_dim].
+ * elements apart (rotated: jf_op_kv8_append's q_out); out: [n_rows][n_heads][head_dim], 16-byte aligned.
  * mask NULL: row i of a sequence sees slots 0 .. len + i. Else mask is [n_rows][mask_words] 32-bit words,
  * 32 * mask_words >= max_rows: the row sees slots 0 .. len - 1, and slot len + j if bit j % 32 of word j / 32
  * is set (a tree of drafts and candidates). lse (optional): fp32 [n_rows][n_heads], the natural logarithm of

@@ -537,6 +537,536 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 }
 
 // ---------------------------------------------------------------------------------------------
+// Many query rows per KV head (drafts, prompt chunks; 16-bit models): tcgen05.
+//
+// A CTA takes a unit of up to 256 query rows over 128-key chunks as two streams, each with an S and an O accumulator of
+// its own in tensor memory (128 lanes x 128 columns; P in fp16 takes the place of the S it came from): rows 0..127
+// and 128..255 over every chunk, or, in a unit of up to 128 rows, all rows over the even and the odd chunks, whose
+// states are joined at the unit's end. While the softmax of one stream runs, the tensor core works for the other.
+//
+// Warps 0-3 and 4-7: softmax of stream 0 and 1 (a thread per row); warp 8 issues the products; warps 9-12 fetch codes
+// (16 bytes a load, one chunk ahead in registers), convert them to fp16 and store them as the images of tensor-core
+// operands: per page of 16 keys two 8-key groups, each of HD / 64 halves of 8 rows x 128 bytes with the 128-byte
+// swizzle; K is read K-major, V MN-major. Exponents stay out of the operands: K's go into the scores, V's into P as in
+// the warp-level form, against the chunk's reference E. Where a chunk's value exponents lie further apart than P
+// can carry, its pages go in groups, one step of the stream each (Kv8Info).
+// ---------------------------------------------------------------------------------------------
+constexpr int T_TR = 256, T_CH = 128, T_UC = 2;
+constexpr int T_CONV_WARPS = 4, T_THREADS = 32 * (8 + 1 + T_CONV_WARPS);
+constexpr int T_PAGES = T_CH / kPage, T_STAGES = 2, T_INFO = 4;
+constexpr int TM_COLS = 512;
+template <int HD>
+struct TLayout {
+  static constexpr int Q = 128 * HD * 2, KV = T_CH * HD * 2, PAGE = kPage * HD * 2;  // bytes of fp16 operands
+  static constexpr int OFF_K = 2 * Q, OFF_V = OFF_K + T_STAGES * KV, TOTAL = OFF_V + T_STAGES * KV + 1024;  // + alignment
+  static constexpr int GROUP = HD * 16;  // 8 keys of a page: HD / 64 halves of 1024 bytes
+  // byte offset of 16-byte piece c (8 dims) of key r of a page
+  static JF_DEV uint32_t page_piece(int r, int c) {
+    return (uint32_t)((r >> 3) * GROUP + (c >> 3) * 1024 + (r & 7) * 128 + (((c & 7) ^ (r & 7)) << 4));
+  }
+  static JF_DEV uint32_t q_piece(int r, int c) {
+    return (uint32_t)((c >> 3) * 16384 + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+  }
+};
+
+// What the steps of a chunk need beside its operands. groups: how many steps; pages[j]: pages of step j as bits; E[j]:
+// its reference exponent.
+struct Kv8Info {
+  int groups;
+  uint8_t pages[T_PAGES];
+  int8_t E[T_PAGES], ek[T_PAGES], ev[T_PAGES];
+};
+
+template <int HD>
+__global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnParams a) {
+  using Lay = TLayout<HD>;
+  using W = Walk<T_TR, T_CH, T_UC>;
+  extern __shared__ uint8_t sm_raw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sQ = smem_u32(sm), sK = sQ + Lay::OFF_K, sV = sQ + Lay::OFF_V;
+  // per stage: loaded, and read by both streams (a unit of one tile: by its stream, counted twice); per stream: queries
+  // there, S ready (the products, and the MMA thread itself, which passes on the chunk's Kv8Info), P ready, P V done; all
+  // products done
+  __shared__ __align__(8) uint64_t b_kfull[T_STAGES], b_kfree[T_STAGES], b_vfull[T_STAGES], b_vfree[T_STAGES], b_q[2], b_s[2], b_p[2],
+      b_o[2], b_all;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int pre[kKv8MaxSeqs + 1];
+  __shared__ Kv8Info s_info[T_INFO];
+  __shared__ float s_ml[2][128][2];
+  __shared__ int s_E[2];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.n_heads / a.c.n_kv_heads, Hkv = a.c.n_kv_heads;
+  if (tid == 0) {
+    for (int i = 0; i < T_STAGES; ++i) {
+      mbar_init(smem_u32(&b_kfull[i]), T_CONV_WARPS);
+      mbar_init(smem_u32(&b_vfull[i]), T_CONV_WARPS);
+      mbar_init(smem_u32(&b_kfree[i]), 2);
+      mbar_init(smem_u32(&b_vfree[i]), 2);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&b_q[i]), 4);
+      mbar_init(smem_u32(&b_s[i]), 2);
+      mbar_init(smem_u32(&b_p[i]), 4);
+      mbar_init(smem_u32(&b_o[i]), 1);
+    }
+    mbar_init(smem_u32(&b_all), 1);
+    fence_mbar_init();
+  }
+  pdl_wait();
+  pdl_launch_dependents();  // (after the wait: the combine reads the batch's lengths before its own)
+  W::P::build(a, G, pre);
+  if (blockIdx.x == 0)
+    for (int b = tid; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
+  const Shares shares(pre[a.c.n_seqs], gridDim.x);
+  if (shares.size(blockIdx.x) == 0) return;
+  if (warp == 8) {
+    tmem_alloc(smem_u32(&tmem_slot), TM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  W w;
+  w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + shares.size(blockIdx.x));
+  const unsigned long long limit = kWaitLimitDefaultNs;
+  auto wait = [&](uint64_t& bar, int uses) {  // for completion number `uses` (from 0); the warp agrees
+    const bool ok = mbar_wait_bounded(smem_u32(&bar), (uint32_t)uses & 1u, limit);
+    return __all_sync(0xffffffffu, ok) != 0;
+  };
+  auto tile_rows = [&]() { return min(w.s.n * G - w.tile * T_TR, T_TR); };
+
+  if (warp > 8) {
+    // ---- codes to operands. Thread: pieces of 16 dims, rows 4 cw .. of each 32 keys. The lanes of a quarter warp
+    // (8 x 16 bytes) hold two rows, so that their stores meet different banks.
+    const int cw = warp - 9;
+    constexpr int PR = HD / 16;             // pieces per key
+    constexpr int RW = 32 / PR;             // keys per warp and round
+    constexpr int ROUNDS = T_CH / (RW * T_CONV_WARPS);
+    const int lr = PR == 8 ? ((lane >> 2) & 1) + 2 * (lane >> 4) : lane >> 2, lc = PR == 8 ? (lane & 3) + 4 * ((lane >> 3) & 1) : lane & 3;
+    struct Ahead {  // a chunk whose page ids are on their way; lane j < 8: page j
+      int id, ek, ev, kp0, keys, kvh;
+      bool there;
+    };
+    int chunk = w.c0();
+    bool more = w.c1() > chunk;
+    auto look = [&]() {  // the next chunk of the share
+      Ahead n;
+      n.there = more;
+      n.id = -1;
+      n.ek = n.ev = 0;
+      n.kp0 = chunk * T_CH;
+      n.keys = w.s.len + w.s.n;
+      n.kvh = w.kvh;
+      if (more) {
+        if (lane < T_PAGES && n.kp0 + lane * kPage < n.keys) {
+          n.id = kv8_page(a.c, w.b, chunk * T_PAGES + lane, a.err);
+          if (n.id >= 0) {
+            const long long blk = (long long)n.id * Hkv + w.kvh;
+            n.ek = a.c.k_exp[blk];
+            n.ev = a.c.v_exp[blk];
+          }
+        }
+        if (++chunk >= w.c1()) {
+          more = w.next(a, G) && w.c1() > 0;
+          chunk = 0;
+        }
+      }
+      return n;
+    };
+    auto fetch = [&](const Ahead& n, const void* pool, uint4 (&x)[ROUNDS]) {
+#pragma unroll
+      for (int j = 0; j < ROUNDS; ++j) {
+        const int r = (j * T_CONV_WARPS + cw) * RW + lr, page = r / kPage;  // (a warp's rows of a round lie in one page)
+        const int id = __shfl_sync(0xffffffffu, n.id, page);
+        x[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (n.there && id >= 0 && n.kp0 + r < n.keys)
+          x[j] = __ldcg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(pool) +
+                                                      (((long long)id * Hkv + n.kvh) * kPage + r % kPage) * HD + lc * 16));
+      }
+    };
+    auto put = [&](const uint4 (&x)[ROUNDS], uint32_t dst) {
+#pragma unroll
+      for (int j = 0; j < ROUNDS; ++j) {
+        const int r = (j * T_CONV_WARPS + cw) * RW + lr;
+        const uint32_t wd[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+        const uint32_t page = dst + (uint32_t)(r / kPage * Lay::PAGE);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t p = page + Lay::page_piece(r % kPage, 2 * lc + h);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(e4m3x2_to_f16x2(wd[2 * h])),
+                       "r"(e4m3x2_to_f16x2(wd[2 * h] >> 16)), "r"(e4m3x2_to_f16x2(wd[2 * h + 1])),
+                       "r"(e4m3x2_to_f16x2(wd[2 * h + 1] >> 16))
+                       : "memory");
+        }
+      }
+      fence_proxy_async_smem();  // this thread's stores -> tensor-core operand reads
+      __syncwarp();
+    };
+    int E_run = -126;
+    Ahead cur = look();
+    uint4 xk[ROUNDS], xv[ROUNDS];
+    fetch(cur, a.c.k, xk);
+    fetch(cur, a.c.v, xv);
+    for (int g = 0; cur.there; ++g) {
+      const Ahead next = look();
+      const int stage = g % T_STAGES, use = g / T_STAGES;
+      if (use > 0 && !wait(b_kfree[stage], use - 1)) {
+        if (lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+        break;
+      }
+      if (cw == 0) {
+        Kv8Info& info = s_info[g % T_INFO];
+        const bool holds = lane < T_PAGES && cur.kp0 + lane * kPage < cur.keys;
+        unsigned rest = __ballot_sync(0xffffffffu, holds);
+        int n = 0;
+        while (rest) {
+          const bool in = rest >> lane & 1u;
+          const int hi = __reduce_max_sync(0xffffffffu, in ? cur.ev : -1000);
+          const unsigned now = __ballot_sync(0xffffffffu, in && cur.ev >= hi - W_EV_MAX);
+          const int lo = __reduce_min_sync(0xffffffffu, now >> lane & 1u ? cur.ev : 1000);
+          if (E_run > lo || hi - E_run > W_EV_MAX) E_run = max(max(min(lo, hi - W_EV_SET), hi - W_EV_MAX), -126);
+          if (lane == 0) info.pages[n] = (uint8_t)now, info.E[n] = (int8_t)E_run;
+          ++n;
+          rest &= ~now;
+        }
+        if (lane < T_PAGES) info.ek[lane] = (int8_t)cur.ek, info.ev[lane] = (int8_t)cur.ev;
+        if (lane == 0) info.groups = n;
+      }
+      put(xk, sK + stage * Lay::KV);
+      if (lane == 0) mbar_arrive(smem_u32(&b_kfull[stage]));
+      fetch(next, a.c.k, xk);
+      if (use > 0 && !wait(b_vfree[stage], use - 1)) {
+        if (lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+        break;
+      }
+      put(xv, sV + stage * Lay::KV);
+      if (lane == 0) mbar_arrive(smem_u32(&b_vfull[stage]));
+      fetch(next, a.c.v, xv);
+      cur = next;
+    }
+  } else if (warp == 8) {
+    // ---- products. A stream's next S goes in when its P V is complete (P lies where S will): meanwhile the other
+    // stream's are queued.
+    constexpr uint32_t idesc_s = idesc_f16_f32(128, T_CH), idesc_pv = idesc_f16_f32(128, HD) | (1u << 16);  // V MN-major
+    const uint64_t dq = sdesc_k_sw128(sQ), dk = sdesc_k_sw128(sK, Lay::GROUP), dv = sdesc_mn_sw128(sV, 1024u, Lay::GROUP);
+    bool ok = true;
+    int steps[2] = {0, 0}, unit = 0;            // of a stream: products P V so far; units so far
+    int g = 0;                                  // chunks so far
+    while (ok) {
+      const bool two = tile_rows() > 128;
+      const int c0 = w.c0(), n = w.c1() - c0;
+      if (n <= 0) break;
+      int pend_stage[2] = {-1, -1}, pend_use[2] = {0, 0}, pend_pages[2] = {0, 0};  // a P V that is still to go
+      bool pend_last[2] = {false, false}, fresh[2] = {true, true};
+      // (both streams' queries, also of a stream without a step: a barrier must not run two completions ahead)
+      ok = wait(b_q[0], unit) && wait(b_q[1], unit);
+      ++unit;
+      auto pv = [&](int s) {
+        if (pend_stage[s] < 0) return true;
+        const int st = pend_stage[s];
+        if (!wait(b_vfull[st], pend_use[s]) || !wait(b_p[s], steps[s])) return false;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint32_t o = tmem + 256 + s * 128, p = tmem + s * 128;
+          const uint64_t d = dv + (uint64_t)(st * (Lay::KV >> 4));
+#pragma unroll
+          for (int kk = 0; kk < T_PAGES; ++kk)
+            if (kk < pend_pages[s])
+              tc_mma_f16_ts(o, p + kk * 8, d + (uint64_t)(kk * (Lay::PAGE >> 4)), idesc_pv, kk > 0 || !fresh[s] ? 1u : 0u);
+          tc_commit(smem_u32(&b_o[s]));
+          if (pend_last[s]) {
+            tc_commit(smem_u32(&b_vfree[st]));
+            if (!two) tc_commit(smem_u32(&b_vfree[st]));
+          }
+        }
+        __syncwarp();
+        fresh[s] = false;
+        pend_stage[s] = -1;
+        return wait(b_o[s], steps[s]++);
+      };
+      for (int c = 0; c < n && ok; ++c, ++g) {
+        const int stage = g % T_STAGES;
+        const Kv8Info& info = s_info[g % T_INFO];
+        const int keys = w.s.len + w.s.n - (c0 + c) * T_CH, pages = min(T_PAGES, (keys + kPage - 1) / kPage);
+        int groups = 1;
+        for (int j = 0; j < groups && ok; ++j)
+          for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
+            const int s = two ? x : c & 1;
+            ok = pv(s);
+            if (ok && j == 0 && (x == 0 || !two)) {
+              ok = wait(b_kfull[stage], g / T_STAGES);
+              if (ok) groups = info.groups;
+            }
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t d = tmem + s * 128;
+              const uint64_t da = dq + (uint64_t)(s * (Lay::Q >> 4)), db = dk + (uint64_t)(stage * (Lay::KV >> 4));
+#pragma unroll
+              for (int kk = 0; kk < HD / 16; ++kk)
+                tc_mma_bf16(d, da + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), db + (uint64_t)((kk >> 2) * 64 + (kk & 3) * 2),
+                            idesc_s, kk > 0 ? 1u : 0u);
+              tc_commit(smem_u32(&b_s[s]));
+              mbar_arrive(smem_u32(&b_s[s]));
+              if (j == groups - 1) {
+                tc_commit(smem_u32(&b_kfree[stage]));
+                if (!two) tc_commit(smem_u32(&b_kfree[stage]));
+              }
+            }
+            __syncwarp();
+            pend_stage[s] = stage;
+            pend_use[s] = g / T_STAGES;
+            pend_pages[s] = pages;
+            pend_last[s] = j == groups - 1;
+          }
+      }
+      if (ok) ok = pv(0);
+      if (ok) ok = pv(1);
+      if (!ok || !w.next(a, G)) break;
+    }
+    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+    // every product is complete before the CTA may leave, also after a wait that gave up
+    if (elect_one()) tc_commit(smem_u32(&b_all));
+    __syncwarp();
+    mbar_wait_bounded(smem_u32(&b_all), 0u, limit);
+    __syncwarp();
+  } else {
+    // ---- softmax of stream s: row `lr` of its 128
+    const int s = warp >> 2, lr = (warp & 3) * 32 + lane;
+    const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_row + s * 128, t_o = t_row + 256 + s * 128;
+    const bool q16 = ((uintptr_t)a.q & 15) == 0 && a.ld_q % 8 == 0;
+    bool ok = true;
+    int steps = 0, g = 0;  // steps of the stream so far; chunks of the share so far
+    while (true) {
+      const int rows = tile_rows();
+      const bool two = rows > 128;
+      const int c0 = w.c0(), n = w.c1() - c0;
+      if (n <= 0) break;
+      const Kv8Seq sq = w.s;
+      const int r = (two ? s * 128 : 0) + lr;  // of the tile
+      const bool live = r < rows;
+      const int tr = w.tile * T_TR + (live ? r : 0), tok = tr / G;
+      const long long at = (long long)(sq.row0 + tok) * a.n_heads + w.kvh * G + (tr - tok * G);
+      float f;
+      {  // queries, scaled; the softmax scale's sign goes with them, so that f >= 0
+        const bf16* src = reinterpret_cast<const bf16*>(a.q) + (long long)(sq.row0 + tok) * a.ld_q + (long long)(w.kvh * G + (tr - tok * G)) * HD;
+        float amax = 0.f;
+#pragma unroll 4
+        for (int c = 0; c < HD / 8; ++c) {
+          float x[8];
+          load_run<8>(src + 8 * c, live, q16, x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[i]));
+        }
+        const int sh = query_shift(amax);
+        const float up = a.scale_log2 < 0.f ? -pow2i(sh) : pow2i(sh);
+        f = pow2i(-sh) * fabsf(a.scale_log2);
+#pragma unroll 4
+        for (int c = 0; c < HD / 8; ++c) {
+          float x[8];
+          load_run<8>(src + 8 * c, live, q16, x);
+          const uint32_t p = sQ + (uint32_t)(s * Lay::Q) + Lay::q_piece(lr, c);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(pack_f16(x[0] * up, x[1] * up)), "r"(pack_f16(x[2] * up, x[3] * up)),
+                       "r"(pack_f16(x[4] * up, x[5] * up)), "r"(pack_f16(x[6] * up, x[7] * up))
+                       : "memory");
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&b_q[s]));
+      }
+      float m_ref = -INFINITY, l = 0.f;
+      int E = 0;
+      bool first = true;
+      for (int c = 0; c < n && ok; ++c, ++g) {
+        if (!two && (c & 1) != s) continue;
+        const Kv8Info& info = s_info[g % T_INFO];
+        const int kp0 = (c0 + c) * T_CH;
+        // bits of the 32 keys from column 32 h on that the row sees
+        const bool cut = kp0 + T_CH > sq.len;
+        auto visible = [&](int h) -> uint32_t {
+          if (!cut) return 0xffffffffu;
+          const int jb = kp0 + 32 * h - sq.len;  // as a new row
+          uint32_t v;
+          if (a.mask) {
+            const uint32_t* mw = a.mask + (long long)(sq.row0 + tok) * a.mask_words;
+            auto word = [&](int i) { return i >= 0 && i < a.mask_words ? mw[i] : 0u; };
+            const int i = jb >> 5, b = jb & 31;
+            v = b ? word(i) >> b | word(i + 1) << (32 - b) : word(i);
+            const int left = sq.n - jb;  // new rows from here on
+            if (left < 32) v &= left <= 0 ? 0u : (1u << left) - 1u;
+          } else {
+            const int seen = tok - jb + 1;
+            v = seen >= 32 ? 0xffffffffu : (seen <= 0 ? 0u : (1u << seen) - 1u);
+          }
+          if (jb < 0) v |= jb <= -32 ? 0xffffffffu : (1u << -jb) - 1u;
+          return v;
+        };
+        int groups = 1;
+        for (int j = 0; j < groups; ++j) {
+          if (!wait(b_s[s], steps)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          groups = info.groups;
+          const uint32_t pages = info.pages[j];
+          const int E_new = info.E[j];
+          auto shown = [&](int h) {
+            uint32_t v = visible(h);
+            if (!(pages >> (2 * h) & 1u)) v &= 0xffff0000u;
+            if (!(pages >> (2 * h + 1) & 1u)) v &= 0x0000ffffu;
+            return v;
+          };
+          float mc = -INFINITY;
+          // (loops over 32 columns stay rolled: the code of a step has to stay in the instruction cache)
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            float v[32];
+            tmem_ld32(t_s + 32 * h, v);
+            const uint32_t see = shown(h);
+            if (see != 0xffffffffu) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = see >> i & 1u ? v[i] : -INFINITY;
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float mx = v[16 * x];
+#pragma unroll
+              for (int i = 1; i < 16; ++i) mx = fmaxf(mx, v[16 * x + i]);
+              const float sc = mx * (f * pow2i(info.ek[2 * h + x]));
+              if (mx > -INFINITY) mc = fmaxf(mc, sc);  // (f may be 0)
+            }
+          }
+          const bool raise = mc > m_ref + W_LAG;
+          if (!first && (__any_sync(0xffffffffu, raise) || E_new != E)) {
+            const float al = raise ? (m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - mc)) : 1.f;
+            l *= al;
+            const float x = al * pow2i(max(-126, min(126, E - E_new)));
+#pragma unroll 1
+            for (int h = 0; h < HD / 16; ++h) {
+              float v[16];
+              uint32_t u[16];
+              tmem_ld16(t_o + 16 * h, v);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(v[i] * x);
+              tmem_st16(t_o + 16 * h, u);
+            }
+          }
+          if (raise) m_ref = mc;
+          E = E_new;
+          first = false;
+          const float nb = m_ref == -INFINITY ? 0.f : -m_ref;
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            float v[32];
+            uint32_t u[16];
+            tmem_ld32(t_s + 32 * h, v);
+            const uint32_t see = shown(h);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int d = info.ev[2 * h + x] - E;  // 0 .. W_EV_MAX for a page of the group
+              const float fu = f * pow2i(info.ek[2 * h + x]), b = nb + (float)d;
+              float ls[2] = {0.f, 0.f};
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                v[16 * x + i] = ex2_ftz(fmaf(v[16 * x + i], fu, b));
+              }
+              if (see != 0xffffffffu) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[16 * x + i] = see >> (16 * x + i) & 1u ? v[16 * x + i] : 0.f;
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) ls[i & 1] += v[16 * x + i];
+              if (pages >> (2 * h + x) & 1u) l = fmaf(ls[0] + ls[1], pow2i(-d), l);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) u[i] = pack_f16(v[2 * i], v[2 * i + 1]);
+            tmem_st16(t_s + 16 * h, u);
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&b_p[s]));
+          ++steps;
+        }
+      }
+      if (!first && ok) {  // the unit's last P V of the stream
+        ok = wait(b_o[s], steps - 1);
+        tc_fence_after();
+      }
+      if (!two) {
+        s_ml[s][lr][0] = m_ref;
+        s_ml[s][lr][1] = l;
+        if (lr == 0) s_E[s] = first ? -4096 : E;
+      }
+      ok = sync_and<1, 256>(ok);  // both streams leave a unit together (barrier 0 is __syncthreads)
+      if (!ok) break;
+      // ---- the unit's end: rows normalised, into out or the state that the CTA leaves
+      const bool whole = c0 == 0 && n == w.n_chunks;
+      float* st = a.states + (long long)shares.slot(w.first, blockIdx.x) * (T_TR * (HD + 2));
+      float M = m_ref, L = l, w0 = 1.f, w1 = 0.f;  // weights of this stream's O (two tiles), or of both streams'
+      int Em = E, d0 = 0, d1 = HD;                 // their unit 2^Em; the dims that this thread finishes
+      if (!two) {
+        const float m0 = s_ml[0][lr][0], m1 = s_ml[1][lr][0], l0 = s_ml[0][lr][1], l1 = s_ml[1][lr][1];
+        M = fmaxf(m0, m1);
+        const float a0 = m0 == -INFINITY ? 0.f : exp2f(m0 - M), a1 = m1 == -INFINITY ? 0.f : exp2f(m1 - M);
+        L = (m0 == -INFINITY ? l0 : a0 * l0) + (m1 == -INFINITY ? l1 : a1 * l1);  // (nothing seen: 0, or NaN)
+        Em = max(s_E[0], s_E[1]);  // (of a stream without a step: far below)
+        w0 = a0 * pow2i(max(s_E[0] - Em, -126));
+        w1 = a1 * pow2i(max(s_E[1] - Em, -126));
+        d0 = s * (HD / 2);
+        d1 = d0 + HD / 2;
+      }
+      const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L), unit = pow2i(Em);
+      const uint32_t t_first = two ? t_o : t_row + 256;
+      const bool second = !two && n > 1;  // (a stream without a step holds nothing)
+#pragma unroll 1
+      for (int d = d0; d < d1; d += 16) {
+        float x[16], y[16];
+        tmem_ld16(t_first + d, x);
+        if (second) tmem_ld16(t_row + 384 + d, y);
+        if (live) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float v = w0 == 0.f ? 0.f : w0 * x[i];
+            if (second && w1 != 0.f) v = fmaf(w1, y[i], v);
+            x[i] = v * il * unit;
+          }
+          if (whole) {
+            uint32_t u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+              u[i] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at * HD + d);
+            dst[0] = make_uint4(u[0], u[1], u[2], u[3]);
+            dst[1] = make_uint4(u[4], u[5], u[6], u[7]);
+          } else {
+            float4* dst = reinterpret_cast<float4*>(st + r * HD + d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+          }
+        }
+      }
+      if (live && d0 == 0) {
+        if (!whole) st[T_TR * HD + r] = M, st[T_TR * (HD + 1) + r] = L;
+        else if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+      }
+      tc_fence_before();
+      sync_and<1, 256>(true);  // both streams have read both accumulators
+      if (!w.next(a, G)) break;
+    }
+    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tmem_dealloc(tmem, TM_COLS);
+}
+
+// ---------------------------------------------------------------------------------------------
 // Joins the partial states of the units that several workers share, by RW warps per (row, query head). n: workers of
 // the kernel that left them. Which states there are follows from the batch's lengths, which were complete before
 // that kernel let this one in, so with up to 32 sequences only the states are left to read after the wait.
@@ -705,17 +1235,21 @@ const DeviceInfo* device_info() {
     if (e == cudaSuccess) e = prepare_rows<bf16, 128, 1>(&d.rows_ctas[1]);
     if (e == cudaSuccess) e = prepare_rows<float, 64, 2>(&d.rows_ctas[2]);
     if (e == cudaSuccess) e = prepare_rows<float, 128, 2>(&d.rows_ctas[3]);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_kv8_attn_tile<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TLayout<64>::TOTAL);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_kv8_attn_tile<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TLayout<128>::TOTAL);
     return (int)e;
   });
   return rc == 0 ? &g_info[dev] : nullptr;
 }
 
 struct Form {
+  bool tile;  // k_kv8_attn_tile
   int ctas, workers, tile_rows;
 };
 Form choose(const DeviceInfo& d, const jf_kv8_cache& c, const jf_kv8_rows& r, int dtype, int n_heads) {
+  if (dtype == JF_BF16 && (long long)r.max_rows * (n_heads / c.n_kv_heads) > W_TR) return {true, d.sms, d.sms, T_TR};
   const int ctas = d.sms * d.rows_ctas[(dtype == JF_F32 ? 2 : 0) + (c.head_dim == 128 ? 1 : 0)];
-  return {ctas, ctas * W_WARPS, W_TR};
+  return {false, ctas, ctas * W_WARPS, W_TR};
 }
 size_t plan_bytes(const jf_kv8_cache& c) { return ((size_t)(c.n_seqs + 1) * 4 + 255) / 256 * 256; }
 
@@ -724,6 +1258,12 @@ cudaError_t launch_rows(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
   cudaError_t e = kv8_launch(k_kv8_attn_rows<T, HD, NS>, dim3(ctas), dim3(32 * W_WARPS), w_smem<HD>(), st, a);
   if (e != cudaSuccess) return e;
   return launch_combine<T, HD, W_TR, W_CH, W_UC>(a, ctas * W_WARPS, st);
+}
+
+template <int HD>
+cudaError_t launch_tile(const Kv8AttnParams& a, int ctas, cudaStream_t st) {
+  const cudaError_t e = kv8_launch(k_kv8_attn_tile<HD>, dim3(ctas), dim3(T_THREADS), TLayout<HD>::TOTAL, st, a);
+  return e != cudaSuccess ? e : launch_combine<bf16, HD, T_TR, T_CH, T_UC>(a, ctas, st);
 }
 
 }  // namespace
@@ -753,7 +1293,7 @@ extern "C" jf_status jf_op_kv8_attention(const jf_kv8_cache* cache, const jf_kv8
   if (ld_q < (long long)n_heads * cache->head_dim || !(scale == scale)) return JF_EINVAL;
   if (rows->n_rows == 0) return JF_OK;
   const uintptr_t type_mask = dtype == JF_BF16 ? 1 : 3;
-  if (!q || !out || ((uintptr_t)q & type_mask) || ((uintptr_t)out & (2 * type_mask + 1)) || ((uintptr_t)workspace & 15)) return JF_EINVAL;
+  if (!q || !out || ((uintptr_t)q & type_mask) || ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15)) return JF_EINVAL;
   if (mask && (mask_words < 1 || (long long)mask_words * 32 < rows->max_rows)) return JF_EINVAL;
   {  // chunks and rows are counted in 32 bits
     const long long group_rows = (long long)rows->n_rows * (n_heads / cache->n_kv_heads);
@@ -773,7 +1313,9 @@ extern "C" jf_status jf_op_kv8_attention(const jf_kv8_cache* cache, const jf_kv8
                      reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + plan_bytes(*cache)), err_word};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
-  if (dtype == JF_BF16)
+  if (f.tile)
+    e = cache->head_dim == 128 ? launch_tile<128>(a, f.ctas, st) : launch_tile<64>(a, f.ctas, st);
+  else if (dtype == JF_BF16)
     e = cache->head_dim == 128 ? launch_rows<bf16, 128, 1>(a, f.ctas, st) : launch_rows<bf16, 64, 1>(a, f.ctas, st);
   else
     e = cache->head_dim == 128 ? launch_rows<float, 128, 2>(a, f.ctas, st) : launch_rows<float, 64, 2>(a, f.ctas, st);

@@ -203,7 +203,7 @@ class Kv8Cache:
             words = mask.shape[1]
             _device_i32(mask, rows.n_rows * words, "mask")
         st = _raw_stream(self.device)
-        key = (dtype, heads, rows.n_rows, rows.max_rows)
+        key = (dtype, heads, rows.c.n_rows, rows.c.max_rows)
         need = self._need.get(key)
         if need is None:
             n = C.c_size_t()
