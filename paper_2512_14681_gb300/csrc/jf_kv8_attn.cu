@@ -13,6 +13,8 @@
 // what a unit costs beside them (its queries, its end), and each of N workers takes an N'th of that length. A unit
 // whose chunks one worker holds entirely is finished there; of the others each worker leaves a partial state (m, l,
 // O) in the workspace, at most two a worker, and k_kv8_combine joins a row's states in their order.
+#include <type_traits>
+
 #include "../../include/jf_ops.h"
 #include "jf_kv8.cuh"
 #include "jf_once.h"
@@ -544,15 +546,16 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // and 128..255 over every chunk, or, in a unit of up to 128 rows, all rows over the even and the odd chunks, whose
 // states are joined at the unit's end. While the softmax of one stream runs, the tensor core works for the other.
 //
-// Warps 0-3 and 4-7: softmax of stream 0 and 1 (a thread per row); warp 8 issues the products; warps 9-12 fetch codes
-// (16 bytes a load, one chunk ahead in registers), convert them to fp16 and store them as the images of tensor-core
+// Warps 0-3 and 4-7: stream 0 and 1, a thread per row; the stream's first warp also
+// issues its products (a stream has nothing else to do until they are complete). Warps 8-11 fetch codes (16 bytes a
+// load, one chunk ahead in registers), convert them to fp16 and store them as the images of tensor-core
 // operands: per page of 16 keys two 8-key groups, each of HD / 64 halves of 8 rows x 128 bytes with the 128-byte
 // swizzle; K is read K-major, V MN-major. Exponents stay out of the operands: K's go into the scores, V's into P as in
 // the warp-level form, against the chunk's reference E. Where a chunk's value exponents lie further apart than P
 // can carry, its pages go in groups, one step of the stream each (Kv8Info).
 // ---------------------------------------------------------------------------------------------
 constexpr int T_TR = 256, T_CH = 128, T_UC = 2;
-constexpr int T_CONV_WARPS = 4, T_THREADS = 32 * (8 + 1 + T_CONV_WARPS);
+constexpr int T_CONV_WARPS = 4, T_THREADS = 32 * (8 + T_CONV_WARPS);  // 168 registers a thread
 constexpr int T_PAGES = T_CH / kPage, T_STAGES = 2, T_INFO = 4;
 constexpr int TM_COLS = 512;
 template <int HD>
@@ -570,12 +573,53 @@ struct TLayout {
 };
 
 // What the steps of a chunk need beside its operands. groups: how many steps; pages[j]: pages of step j as bits; E[j]:
-// its reference exponent.
+// its reference exponent, d[j]: of a page of the step e_v - E, and w[j]: 2^-d, 0 for other pages; fk: 2^(e_k).
 struct Kv8Info {
-  int groups;
-  uint8_t pages[T_PAGES];
-  int8_t E[T_PAGES], ek[T_PAGES], ev[T_PAGES];
+  float fk[T_PAGES], d[T_PAGES][T_PAGES], w[T_PAGES][T_PAGES];
+  int groups, E[T_PAGES], pages[T_PAGES];
 };
+
+// x * y + z and x + y on two values at a time.
+JF_DEV float2 fma2(float2 x, float2 y, float2 z) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y), "f"(z.x), "f"(z.y));
+  return r;
+}
+JF_DEV float2 add2(float2 x, float2 y) {
+  float2 r;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
+  return r;
+}
+// 32 columns of this warp's lanes, without waiting for them (tmem_wait_ld).
+JF_DEV void tmem_ld32_start(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+// (the values pass through, so that no use of them moves ahead of the wait)
+JF_DEV void tmem_wait_ld(float (&v)[32], float (&w)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(v[i]), "+f"(w[i]));
+}
+JF_DEV void tmem_wait_ld(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(v[i]));
+}
 
 template <int HD>
 __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnParams a) {
@@ -584,11 +628,9 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
   extern __shared__ uint8_t sm_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sQ = smem_u32(sm), sK = sQ + Lay::OFF_K, sV = sQ + Lay::OFF_V;
-  // per stage: loaded, and read by both streams (a unit of one tile: by its stream, counted twice); per stream: queries
-  // there, S ready (the products, and the MMA thread itself, which passes on the chunk's Kv8Info), P ready, P V done; all
-  // products done
-  __shared__ __align__(8) uint64_t b_kfull[T_STAGES], b_kfree[T_STAGES], b_vfull[T_STAGES], b_vfree[T_STAGES], b_q[2], b_s[2], b_p[2],
-      b_o[2], b_all;
+  // per stage: loaded, and read by both streams (a unit of one tile: by its stream, counted twice); per stream: S ready
+  // (the products, and the thread that issued them, which passes on the chunk's Kv8Info), P V done, everything done
+  __shared__ __align__(8) uint64_t b_kfull[T_STAGES], b_kfree[T_STAGES], b_vfull[T_STAGES], b_vfree[T_STAGES], b_s[2], b_o[2], b_all[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int pre[kKv8MaxSeqs + 1];
   __shared__ Kv8Info s_info[T_INFO];
@@ -604,12 +646,10 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       mbar_init(smem_u32(&b_vfree[i]), 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&b_q[i]), 4);
       mbar_init(smem_u32(&b_s[i]), 2);
-      mbar_init(smem_u32(&b_p[i]), 4);
       mbar_init(smem_u32(&b_o[i]), 1);
+      mbar_init(smem_u32(&b_all[i]), 1);
     }
-    mbar_init(smem_u32(&b_all), 1);
     fence_mbar_init();
   }
   pdl_wait();
@@ -627,19 +667,20 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  W w;
-  w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + shares.size(blockIdx.x));
   const unsigned long long limit = kWaitLimitDefaultNs;
   auto wait = [&](uint64_t& bar, int uses) {  // for completion number `uses` (from 0); the warp agrees
     const bool ok = mbar_wait_bounded(smem_u32(&bar), (uint32_t)uses & 1u, limit);
     return __all_sync(0xffffffffu, ok) != 0;
   };
-  auto tile_rows = [&]() { return min(w.s.n * G - w.tile * T_TR, T_TR); };
+  auto start = [&](W& w) { w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + shares.size(blockIdx.x)); };
+  auto tile_rows = [&](const W& w) { return min(w.s.n * G - w.tile * T_TR, T_TR); };
 
-  if (warp > 8) {
+  if (warp >= 8) {
     // ---- codes to operands. Thread: pieces of 16 dims, rows 4 cw .. of each 32 keys. The lanes of a quarter warp
     // (8 x 16 bytes) hold two rows, so that their stores meet different banks.
-    const int cw = warp - 9;
+    W w;
+    start(w);
+    const int cw = warp - 8;
     constexpr int PR = HD / 16;             // pieces per key
     constexpr int RW = 32 / PR;             // keys per warp and round
     constexpr int ROUNDS = T_CH / (RW * T_CONV_WARPS);
@@ -726,11 +767,16 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           const unsigned now = __ballot_sync(0xffffffffu, in && cur.ev >= hi - W_EV_MAX);
           const int lo = __reduce_min_sync(0xffffffffu, now >> lane & 1u ? cur.ev : 1000);
           if (E_run > lo || hi - E_run > W_EV_MAX) E_run = max(max(min(lo, hi - W_EV_SET), hi - W_EV_MAX), -126);
-          if (lane == 0) info.pages[n] = (uint8_t)now, info.E[n] = (int8_t)E_run;
+          if (lane == 0) info.pages[n] = (int)now, info.E[n] = E_run;
+          if (lane < T_PAGES) {
+            const bool mine = now >> lane & 1u;
+            info.d[n][lane] = mine ? (float)(cur.ev - E_run) : 0.f;
+            info.w[n][lane] = mine ? pow2i(E_run - cur.ev) : 0.f;
+          }
           ++n;
           rest &= ~now;
         }
-        if (lane < T_PAGES) info.ek[lane] = (int8_t)cur.ek, info.ev[lane] = (int8_t)cur.ev;
+        if (lane < T_PAGES) info.fk[lane] = pow2i(cur.ek);
         if (lane == 0) info.groups = n;
       }
       put(xk, sK + stage * Lay::KV);
@@ -745,101 +791,58 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       fetch(next, a.c.v, xv);
       cur = next;
     }
-  } else if (warp == 8) {
-    // ---- products. A stream's next S goes in when its P V is complete (P lies where S will): meanwhile the other
-    // stream's are queued.
-    constexpr uint32_t idesc_s = idesc_f16_f32(128, T_CH), idesc_pv = idesc_f16_f32(128, HD) | (1u << 16);  // V MN-major
-    const uint64_t dq = sdesc_k_sw128(sQ), dk = sdesc_k_sw128(sK, Lay::GROUP), dv = sdesc_mn_sw128(sV, 1024u, Lay::GROUP);
-    bool ok = true;
-    int steps[2] = {0, 0}, unit = 0;            // of a stream: products P V so far; units so far
-    int g = 0;                                  // chunks so far
-    while (ok) {
-      const bool two = tile_rows() > 128;
-      const int c0 = w.c0(), n = w.c1() - c0;
-      if (n <= 0) break;
-      int pend_stage[2] = {-1, -1}, pend_use[2] = {0, 0}, pend_pages[2] = {0, 0};  // a P V that is still to go
-      bool pend_last[2] = {false, false}, fresh[2] = {true, true};
-      // (both streams' queries, also of a stream without a step: a barrier must not run two completions ahead)
-      ok = wait(b_q[0], unit) && wait(b_q[1], unit);
-      ++unit;
-      auto pv = [&](int s) {
-        if (pend_stage[s] < 0) return true;
-        const int st = pend_stage[s];
-        if (!wait(b_vfull[st], pend_use[s]) || !wait(b_p[s], steps[s])) return false;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint32_t o = tmem + 256 + s * 128, p = tmem + s * 128;
-          const uint64_t d = dv + (uint64_t)(st * (Lay::KV >> 4));
-#pragma unroll
-          for (int kk = 0; kk < T_PAGES; ++kk)
-            if (kk < pend_pages[s])
-              tc_mma_f16_ts(o, p + kk * 8, d + (uint64_t)(kk * (Lay::PAGE >> 4)), idesc_pv, kk > 0 || !fresh[s] ? 1u : 0u);
-          tc_commit(smem_u32(&b_o[s]));
-          if (pend_last[s]) {
-            tc_commit(smem_u32(&b_vfree[st]));
-            if (!two) tc_commit(smem_u32(&b_vfree[st]));
-          }
-        }
-        __syncwarp();
-        fresh[s] = false;
-        pend_stage[s] = -1;
-        return wait(b_o[s], steps[s]++);
-      };
-      for (int c = 0; c < n && ok; ++c, ++g) {
-        const int stage = g % T_STAGES;
-        const Kv8Info& info = s_info[g % T_INFO];
-        const int keys = w.s.len + w.s.n - (c0 + c) * T_CH, pages = min(T_PAGES, (keys + kPage - 1) / kPage);
-        int groups = 1;
-        for (int j = 0; j < groups && ok; ++j)
-          for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
-            const int s = two ? x : c & 1;
-            ok = pv(s);
-            if (ok && j == 0 && (x == 0 || !two)) {
-              ok = wait(b_kfull[stage], g / T_STAGES);
-              if (ok) groups = info.groups;
-            }
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-              const uint32_t d = tmem + s * 128;
-              const uint64_t da = dq + (uint64_t)(s * (Lay::Q >> 4)), db = dk + (uint64_t)(stage * (Lay::KV >> 4));
-#pragma unroll
-              for (int kk = 0; kk < HD / 16; ++kk)
-                tc_mma_bf16(d, da + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), db + (uint64_t)((kk >> 2) * 64 + (kk & 3) * 2),
-                            idesc_s, kk > 0 ? 1u : 0u);
-              tc_commit(smem_u32(&b_s[s]));
-              mbar_arrive(smem_u32(&b_s[s]));
-              if (j == groups - 1) {
-                tc_commit(smem_u32(&b_kfree[stage]));
-                if (!two) tc_commit(smem_u32(&b_kfree[stage]));
-              }
-            }
-            __syncwarp();
-            pend_stage[s] = stage;
-            pend_use[s] = g / T_STAGES;
-            pend_pages[s] = pages;
-            pend_last[s] = j == groups - 1;
-          }
-      }
-      if (ok) ok = pv(0);
-      if (ok) ok = pv(1);
-      if (!ok || !w.next(a, G)) break;
-    }
-    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
-    // every product is complete before the CTA may leave, also after a wait that gave up
-    if (elect_one()) tc_commit(smem_u32(&b_all));
-    __syncwarp();
-    mbar_wait_bounded(smem_u32(&b_all), 0u, limit);
-    __syncwarp();
   } else {
-    // ---- softmax of stream s: row `lr` of its 128
+    // ---- stream s: row `lr` of its 128
     const int s = warp >> 2, lr = (warp & 3) * 32 + lane;
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_row + s * 128, t_o = t_row + 256 + s * 128;
+    const bool issuer = (warp & 3) == 0;
+    constexpr uint32_t idesc_s = idesc_f16_f32(128, T_CH), idesc_pv = idesc_f16_f32(128, HD) | (1u << 16);  // V MN-major
+    const uint64_t dq = sdesc_k_sw128(sQ + s * Lay::Q), dk = sdesc_k_sw128(sK, Lay::GROUP), dv = sdesc_mn_sw128(sV, 1024u, Lay::GROUP);
+    // S of a step, by the stream's first warp; both = a unit of two tiles
+    auto issue_s = [&](int g, bool last, bool both) {
+      const int stage = g % T_STAGES;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t db = dk + (uint64_t)(stage * (Lay::KV >> 4));
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk)
+          tc_mma_bf16(tmem + s * 128, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
+                      db + (uint64_t)((kk >> 2) * 64 + (kk & 3) * 2), idesc_s, kk > 0 ? 1u : 0u);
+        tc_commit(smem_u32(&b_s[s]));
+        mbar_arrive(smem_u32(&b_s[s]));
+        if (last) {
+          tc_commit(smem_u32(&b_kfree[stage]));
+          if (!both) tc_commit(smem_u32(&b_kfree[stage]));
+        }
+      }
+      __syncwarp();
+    };
+    auto issue_pv = [&](int g, int pages, bool fresh, bool last, bool both) {
+      const int stage = g % T_STAGES;
+      tc_fence_after();
+      if (elect_one()) {
+        const uint64_t d = dv + (uint64_t)(stage * (Lay::KV >> 4));
+#pragma unroll
+        for (int kk = 0; kk < T_PAGES; ++kk)
+          if (kk < pages)
+            tc_mma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + kk * 8, d + (uint64_t)(kk * (Lay::PAGE >> 4)), idesc_pv,
+                          kk > 0 || !fresh ? 1u : 0u);
+        tc_commit(smem_u32(&b_o[s]));
+        if (last) {
+          tc_commit(smem_u32(&b_vfree[stage]));
+          if (!both) tc_commit(smem_u32(&b_vfree[stage]));
+        }
+      }
+      __syncwarp();
+    };
+    auto stream_and = [&](bool ok) { return s ? sync_and<2, 128>(ok) : sync_and<1, 128>(ok); };
     const bool q16 = ((uintptr_t)a.q & 15) == 0 && a.ld_q % 8 == 0;
+    W w;
+    start(w);
     bool ok = true;
     int steps = 0, g = 0;  // steps of the stream so far; chunks of the share so far
     while (true) {
-      const int rows = tile_rows();
+      const int rows = tile_rows(w);
       const bool two = rows > 128;
       const int c0 = w.c0(), n = w.c1() - c0;
       if (n <= 0) break;
@@ -872,15 +875,22 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
                        : "memory");
         }
         fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&b_q[s]));
       }
       float m_ref = -INFINITY, l = 0.f;
       int E = 0;
       bool first = true;
-      for (int c = 0; c < n && ok; ++c, ++g) {
-        if (!two && (c & 1) != s) continue;
-        const Kv8Info& info = s_info[g % T_INFO];
+      const int c_step = two ? 1 : 2, c_first = two ? 0 : s, g0 = g;  // the stream's chunks c_first, + c_step, ...
+      g += n;
+      ok = stream_and(ok);  // the stream's queries are there
+      if (issuer && c_first < n && ok) {
+        ok = wait(b_kfull[(g0 + c_first) % T_STAGES], (g0 + c_first) / T_STAGES);
+        if (ok) issue_s(g0 + c_first, s_info[(g0 + c_first) % T_INFO].groups == 1, two);
+      }
+      bool fresh = true;  // no P V of the unit yet
+      bool go = true;     // (left by all warps of the stream together)
+      for (int c = c_first; c < n && go; c += c_step) {
+        const int gc = g0 + c;
+        const Kv8Info& info = s_info[gc % T_INFO];
         const int kp0 = (c0 + c) * T_CH;
         // bits of the 32 keys from column 32 h on that the row sees
         const bool cut = kp0 + T_CH > sq.len;
@@ -902,42 +912,52 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           if (jb < 0) v |= jb <= -32 ? 0xffffffffu : (1u << -jb) - 1u;
           return v;
         };
+        const int held = min(T_PAGES, (sq.len + sq.n - kp0 + kPage - 1) / kPage);  // pages with a token
         int groups = 1;
         for (int j = 0; j < groups; ++j) {
-          if (!wait(b_s[s], steps)) {
-            ok = false;
-            break;
-          }
+          ok = wait(b_s[s], steps) && ok;
           tc_fence_after();
+          if (ok) {
+          // The row's scores, 32 at a time: the maximum of columns 64 .. 127, then of 0 .. 63, which stay in registers
+          // until their exponentials; 64 .. 127 are read again, each 32 while the 32 before them are worked on. (P of
+          // column c goes to c / 2, which has been read by then.)
+          float v0[32], v1[32];
+          tmem_ld32_start(t_s + 64, v0);
+          tmem_ld32_start(t_s + 96, v1);
           groups = info.groups;
-          const uint32_t pages = info.pages[j];
-          const int E_new = info.E[j];
-          auto shown = [&](int h) {
-            uint32_t v = visible(h);
-            if (!(pages >> (2 * h) & 1u)) v &= 0xffff0000u;
-            if (!(pages >> (2 * h + 1) & 1u)) v &= 0x0000ffffu;
-            return v;
+          const int pages = info.pages[j], E_new = info.E[j];
+          auto hide = [&](int h, float (&v)[32]) {
+            if (!cut && pages == 255) return;
+            uint32_t see = visible(h);
+            if (!(pages >> (2 * h) & 1)) see &= 0xffff0000u;
+            if (!(pages >> (2 * h + 1) & 1)) see &= 0x0000ffffu;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = see >> i & 1u ? v[i] : -INFINITY;
           };
+          // of a page's scores; above 0, so that a hidden key's -inf stays one
+          auto factor = [&](int page) { return fmaxf(f * info.fk[page], 7.888609e-31f /* 2^-100 */); };
           float mc = -INFINITY;
-          // (loops over 32 columns stay rolled: the code of a step has to stay in the instruction cache)
-#pragma unroll 1
-          for (int h = 0; h < 4; ++h) {
-            float v[32];
-            tmem_ld32(t_s + 32 * h, v);
-            const uint32_t see = shown(h);
-            if (see != 0xffffffffu) {
+          auto largest = [&](int h, const float (&v)[32]) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = see >> i & 1u ? v[i] : -INFINITY;
+            for (int y = 0; y < 2; ++y) {
+              float mx = v[16 * y];
+#pragma unroll
+              for (int i = 1; i < 16; ++i) mx = fmaxf(mx, v[16 * y + i]);
+              mc = fmaxf(mc, mx * factor(2 * h + y));
             }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              float mx = v[16 * x];
-#pragma unroll
-              for (int i = 1; i < 16; ++i) mx = fmaxf(mx, v[16 * x + i]);
-              const float sc = mx * (f * pow2i(info.ek[2 * h + x]));
-              if (mx > -INFINITY) mc = fmaxf(mc, sc);  // (f may be 0)
-            }
-          }
+          };
+          tmem_wait_ld(v0, v1);
+          hide(2, v0);
+          largest(2, v0);
+          hide(3, v1);
+          largest(3, v1);
+          tmem_ld32_start(t_s, v0);
+          tmem_ld32_start(t_s + 32, v1);
+          tmem_wait_ld(v0, v1);
+          hide(0, v0);
+          largest(0, v0);
+          hide(1, v1);
+          largest(1, v1);
           const bool raise = mc > m_ref + W_LAG;
           if (!first && (__any_sync(0xffffffffu, raise) || E_new != E)) {
             const float al = raise ? (m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - mc)) : 1.f;
@@ -945,11 +965,11 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
             const float x = al * pow2i(max(-126, min(126, E - E_new)));
 #pragma unroll 1
             for (int h = 0; h < HD / 16; ++h) {
-              float v[16];
+              float o[16];
               uint32_t u[16];
-              tmem_ld16(t_o + 16 * h, v);
+              tmem_ld16(t_o + 16 * h, o);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(v[i] * x);
+              for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(o[i] * x);
               tmem_st16(t_o + 16 * h, u);
             }
           }
@@ -957,37 +977,51 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           E = E_new;
           first = false;
           const float nb = m_ref == -INFINITY ? 0.f : -m_ref;
-#pragma unroll 1
-          for (int h = 0; h < 4; ++h) {
-            float v[32];
+          auto exponentials = [&](int h, const float (&v)[32]) {
             uint32_t u[16];
-            tmem_ld32(t_s + 32 * h, v);
-            const uint32_t see = shown(h);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int d = info.ev[2 * h + x] - E;  // 0 .. W_EV_MAX for a page of the group
-              const float fu = f * pow2i(info.ek[2 * h + x]), b = nb + (float)d;
-              float ls[2] = {0.f, 0.f};
+            for (int y = 0; y < 2; ++y) {
+              const float fx = factor(2 * h + y), b = nb + info.d[j][2 * h + y];
+              float2 ls = make_float2(0.f, 0.f);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                v[16 * x + i] = ex2_ftz(fmaf(v[16 * x + i], fu, b));
+              for (int i = 0; i < 8; ++i) {
+                float2 p = fma2(make_float2(v[16 * y + 2 * i], v[16 * y + 2 * i + 1]), make_float2(fx, fx), make_float2(b, b));
+                p.x = ex2_ftz(p.x);
+                p.y = ex2_ftz(p.y);
+                ls = add2(ls, p);
+                u[8 * y + i] = pack_f16(p.x, p.y);
               }
-              if (see != 0xffffffffu) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[16 * x + i] = see >> (16 * x + i) & 1u ? v[16 * x + i] : 0.f;
-              }
-#pragma unroll
-              for (int i = 0; i < 16; ++i) ls[i & 1] += v[16 * x + i];
-              if (pages >> (2 * h + x) & 1u) l = fmaf(ls[0] + ls[1], pow2i(-d), l);
+              l = fmaf(ls.x + ls.y, info.w[j][2 * h + y], l);
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) u[i] = pack_f16(v[2 * i], v[2 * i + 1]);
             tmem_st16(t_s + 16 * h, u);
-          }
+          };
+          exponentials(0, v0);
+          tmem_ld32_start(t_s + 64, v0);
+          exponentials(1, v1);
+          tmem_wait_ld(v0);
+          tmem_ld32_start(t_s + 96, v1);
+          hide(2, v0);
+          exponentials(2, v0);
+          tmem_wait_ld(v1);
+          hide(3, v1);
+          exponentials(3, v1);
           tmem_wait_st();
+          }
           tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&b_p[s]));
+          go = ok = stream_and(ok);  // P of all rows is there
+          if (!go) break;
+          if (issuer) {
+            const bool last = j == groups - 1;
+            ok = wait(b_vfull[gc % T_STAGES], gc / T_STAGES);
+            if (ok) issue_pv(gc, held, fresh, last, two);
+            // the stream's next S, once P (which lies where S will) has been read
+            const int gn = last ? gc + c_step : gc, jn = last ? 0 : j + 1;
+            if (ok && (!last || c + c_step < n)) {
+              ok = wait(b_o[s], steps) && wait(b_kfull[gn % T_STAGES], gn / T_STAGES);
+              if (ok) issue_s(gn, s_info[gn % T_INFO].groups == jn + 1, two);
+            }
+          }
+          fresh = false;
           ++steps;
         }
       }
@@ -1000,7 +1034,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         s_ml[s][lr][1] = l;
         if (lr == 0) s_E[s] = first ? -4096 : E;
       }
-      ok = sync_and<1, 256>(ok);  // both streams leave a unit together (barrier 0 is __syncthreads)
+      ok = sync_and<3, 256>(ok);  // both streams leave a unit together (barrier 0 is __syncthreads)
       if (!ok) break;
       // ---- the unit's end: rows normalised, into out or the state that the CTA leaves
       const bool whole = c0 == 0 && n == w.n_chunks;
@@ -1055,10 +1089,18 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         else if (a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
       }
       tc_fence_before();
-      sync_and<1, 256>(true);  // both streams have read both accumulators
+      sync_and<3, 256>(true);  // both streams have read both accumulators
       if (!w.next(a, G)) break;
     }
     if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+    // every product is complete before the CTA may leave, also after a wait that gave up
+    if (issuer) {
+      __syncwarp();
+      if (elect_one()) tc_commit(smem_u32(&b_all[s]));
+      __syncwarp();
+      mbar_wait_bounded(smem_u32(&b_all[s]), 0u, limit);
+    }
+    __syncwarp();
   }
   tc_fence_before();
   __syncthreads();
@@ -1224,6 +1266,11 @@ cudaError_t prepare_rows(int* per_sm) {
   return e == cudaSuccess && *per_sm < 1 ? cudaErrorInvalidConfiguration : e;
 }
 
+template <int HD>
+cudaError_t prepare_tile() {
+  return cudaFuncSetAttribute(k_kv8_attn_tile<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, TLayout<HD>::TOTAL);
+}
+
 // Kernel attributes and sizes of the current device (set once per device).
 const DeviceInfo* device_info() {
   int dev = 0;
@@ -1235,8 +1282,8 @@ const DeviceInfo* device_info() {
     if (e == cudaSuccess) e = prepare_rows<bf16, 128, 1>(&d.rows_ctas[1]);
     if (e == cudaSuccess) e = prepare_rows<float, 64, 2>(&d.rows_ctas[2]);
     if (e == cudaSuccess) e = prepare_rows<float, 128, 2>(&d.rows_ctas[3]);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_kv8_attn_tile<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TLayout<64>::TOTAL);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_kv8_attn_tile<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TLayout<128>::TOTAL);
+    if (e == cudaSuccess) e = prepare_tile<64>();
+    if (e == cudaSuccess) e = prepare_tile<128>();
     return (int)e;
   });
   return rc == 0 ? &g_info[dev] : nullptr;
