@@ -227,8 +227,8 @@ JF_DEV int query_shift(float amax) {
 // ---------------------------------------------------------------------------------------------
 constexpr int W_WARPS = 4, W_TR = 16, W_CH = 2 * kPage, W_UC = 3;
 constexpr int W_STAGES = 2;  // chunks in a warp's ring
-constexpr float W_LAG = 4.f;             // a row's reference maximum follows its scores when they exceed it by more
-constexpr int W_EV_SET = 5, W_EV_MAX = 10;  // e_v - E: where E is set, largest (p' <= 2^14); smallest 0
+constexpr float W_LAG = 8.f;             // a row's reference maximum follows its scores when they exceed it by more
+constexpr int W_EV_SET = 4, W_EV_MAX = 7;  // e_v - E: where E is set, largest (p' <= 2^15); smallest 0
 
 template <int HD>
 constexpr int w_smem() { return W_WARPS * W_STAGES * 2 * W_CH * HD; }
@@ -685,29 +685,19 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
     constexpr int RW = 32 / PR;             // keys per warp and round
     constexpr int ROUNDS = T_CH / (RW * T_CONV_WARPS);
     const int lr = PR == 8 ? ((lane >> 2) & 1) + 2 * (lane >> 4) : lane >> 2, lc = PR == 8 ? (lane & 3) + 4 * ((lane >> 3) & 1) : lane & 3;
-    struct Ahead {  // a chunk whose page ids are on their way; lane j < 8: page j
-      int id, ek, ev, kp0, keys, kvh;
+    // A chunk on its way: its page ids are asked for three chunks ahead of its conversion, exponents two, codes one, so
+    // that nothing waits for what it has just asked for. Lane j < 8: page j.
+    struct Ahead {
+      int raw, ek, ev, kp0, keys, kvh;
       bool there;
     };
     int chunk = w.c0();
     bool more = w.c1() > chunk;
     auto look = [&]() {  // the next chunk of the share
-      Ahead n;
-      n.there = more;
-      n.id = -1;
-      n.ek = n.ev = 0;
-      n.kp0 = chunk * T_CH;
-      n.keys = w.s.len + w.s.n;
-      n.kvh = w.kvh;
+      Ahead n = {0, 0, 0, chunk * T_CH, w.s.len + w.s.n, w.kvh, more};
       if (more) {
-        if (lane < T_PAGES && n.kp0 + lane * kPage < n.keys) {
-          n.id = kv8_page(a.c, w.b, chunk * T_PAGES + lane, a.err);
-          if (n.id >= 0) {
-            const long long blk = (long long)n.id * Hkv + w.kvh;
-            n.ek = a.c.k_exp[blk];
-            n.ev = a.c.v_exp[blk];
-          }
-        }
+        if (lane < T_PAGES && n.kp0 + lane * kPage < n.keys)
+          n.raw = a.c.page_table[(long long)w.b * a.c.pages_per_seq + chunk * T_PAGES + lane];
         if (++chunk >= w.c1()) {
           more = w.next(a, G) && w.c1() > 0;
           chunk = 0;
@@ -715,18 +705,36 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       }
       return n;
     };
-    auto fetch = [&](const Ahead& n, const void* pool, uint4 (&x)[ROUNDS]) {
-#pragma unroll
-      for (int j = 0; j < ROUNDS; ++j) {
-        const int r = (j * T_CONV_WARPS + cw) * RW + lr, page = r / kPage;  // (a warp's rows of a round lie in one page)
-        const int id = __shfl_sync(0xffffffffu, n.id, page);
-        x[j] = make_uint4(0u, 0u, 0u, 0u);
-        if (n.there && id >= 0 && n.kp0 + r < n.keys)
-          x[j] = __ldcg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(pool) +
-                                                      (((long long)id * Hkv + n.kvh) * kPage + r % kPage) * HD + lc * 16));
+    auto block_of = [&](Ahead& n) {  // ids outside the pool are reported, and page 0 read in their place
+      if (n.raw < 0 || n.raw >= a.c.n_pages) {
+        if (n.there) jf_set_error(a.err, JF_DERR_BOUNDS);
+        n.raw = 0;
+      }
+      return (long long)n.raw * Hkv + n.kvh;
+    };
+    auto exponents = [&](Ahead& n) {
+      if (n.there && lane < T_PAGES && n.kp0 + lane * kPage < n.keys) {
+        const long long blk = block_of(n);
+        n.ek = a.c.k_exp[blk];
+        n.ev = a.c.v_exp[blk];
       }
     };
-    auto put = [&](const uint4 (&x)[ROUNDS], uint32_t dst) {
+    auto fetch = [&](const Ahead& n, const void* pool, uint4 (&x)[ROUNDS]) {
+      // (slots past the last token are read too, and replaced by zeros when they are converted)
+      const unsigned long long base = reinterpret_cast<unsigned long long>(pool) + ((long long)n.raw * Hkv + n.kvh) * (kPage * HD);
+#pragma unroll
+      for (int j = 0; j < ROUNDS; ++j) {
+        const int r = (j * T_CONV_WARPS + cw) * RW + lr;  // (a warp's rows of a round lie in one page)
+        const unsigned long long p = __shfl_sync(0xffffffffu, base, (j * T_CONV_WARPS + cw) * RW / kPage);
+        if (n.there) x[j] = __ldcg(reinterpret_cast<const uint4*>(p + (r % kPage) * HD + lc * 16));
+      }
+    };
+    auto put = [&](uint4 (&x)[ROUNDS], uint32_t dst, int held) {  // held: slots with a token
+      if (held < T_CH) {
+#pragma unroll
+        for (int j = 0; j < ROUNDS; ++j)
+          if ((j * T_CONV_WARPS + cw) * RW + lr >= held) x[j] = make_uint4(0u, 0u, 0u, 0u);
+      }
 #pragma unroll
       for (int j = 0; j < ROUNDS; ++j) {
         const int r = (j * T_CONV_WARPS + cw) * RW + lr;
@@ -745,12 +753,13 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       __syncwarp();
     };
     int E_run = -126;
-    Ahead cur = look();
+    Ahead cur = look(), next = look(), after = look();
     uint4 xk[ROUNDS], xv[ROUNDS];
+    exponents(cur);
     fetch(cur, a.c.k, xk);
     fetch(cur, a.c.v, xv);
+    exponents(next);
     for (int g = 0; cur.there; ++g) {
-      const Ahead next = look();
       const int stage = g % T_STAGES, use = g / T_STAGES;
       if (use > 0 && !wait(b_kfree[stage], use - 1)) {
         if (lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
@@ -779,17 +788,20 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         if (lane < T_PAGES) info.fk[lane] = pow2i(cur.ek);
         if (lane == 0) info.groups = n;
       }
-      put(xk, sK + stage * Lay::KV);
+      put(xk, sK + stage * Lay::KV, cur.keys - cur.kp0);
       if (lane == 0) mbar_arrive(smem_u32(&b_kfull[stage]));
       fetch(next, a.c.k, xk);
       if (use > 0 && !wait(b_vfree[stage], use - 1)) {
         if (lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
         break;
       }
-      put(xv, sV + stage * Lay::KV);
+      put(xv, sV + stage * Lay::KV, cur.keys - cur.kp0);
       if (lane == 0) mbar_arrive(smem_u32(&b_vfull[stage]));
       fetch(next, a.c.v, xv);
       cur = next;
+      next = after;
+      exponents(next);
+      after = look();
     }
   } else {
     // ---- stream s: row `lr` of its 128
@@ -854,24 +866,38 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       float f;
       {  // queries, scaled; the softmax scale's sign goes with them, so that f >= 0
         const bf16* src = reinterpret_cast<const bf16*>(a.q) + (long long)(sq.row0 + tok) * a.ld_q + (long long)(w.kvh * G + (tr - tok * G)) * HD;
+        uint4 raw[HD / 8];
         float amax = 0.f;
-#pragma unroll 4
-        for (int c = 0; c < HD / 8; ++c) {
-          float x[8];
-          load_run<8>(src + 8 * c, live, q16, x);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(x[i]));
+        for (int c = 0; c < HD / 8; ++c) {
+          if (!live) {
+            raw[c] = make_uint4(0u, 0u, 0u, 0u);
+          } else if (q16) {
+            raw[c] = *reinterpret_cast<const uint4*>(src + 8 * c);
+          } else {
+            uint32_t h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              h[i] = (uint32_t)__bfloat16_as_ushort(src[8 * c + 2 * i]) | (uint32_t)__bfloat16_as_ushort(src[8 * c + 2 * i + 1]) << 16;
+            raw[c] = make_uint4(h[0], h[1], h[2], h[3]);
+          }
+        }
+        auto lo = [](uint32_t h) { return __uint_as_float(h << 16); };
+        auto hi = [](uint32_t h) { return __uint_as_float(h & 0xffff0000u); };
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c) {
+          amax = fmaxf(amax, fmaxf(fmaxf(fabsf(lo(raw[c].x)), fabsf(hi(raw[c].x))), fmaxf(fabsf(lo(raw[c].y)), fabsf(hi(raw[c].y)))));
+          amax = fmaxf(amax, fmaxf(fmaxf(fabsf(lo(raw[c].z)), fabsf(hi(raw[c].z))), fmaxf(fabsf(lo(raw[c].w)), fabsf(hi(raw[c].w)))));
         }
         const int sh = query_shift(amax);
         const float up = a.scale_log2 < 0.f ? -pow2i(sh) : pow2i(sh);
         f = pow2i(-sh) * fabsf(a.scale_log2);
-#pragma unroll 4
+#pragma unroll
         for (int c = 0; c < HD / 8; ++c) {
-          float x[8];
-          load_run<8>(src + 8 * c, live, q16, x);
           const uint32_t p = sQ + (uint32_t)(s * Lay::Q) + Lay::q_piece(lr, c);
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(pack_f16(x[0] * up, x[1] * up)), "r"(pack_f16(x[2] * up, x[3] * up)),
-                       "r"(pack_f16(x[4] * up, x[5] * up)), "r"(pack_f16(x[6] * up, x[7] * up))
+          auto two_f16 = [&](uint32_t h) { return pack_f16(lo(h) * up, hi(h) * up); };
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(two_f16(raw[c].x)), "r"(two_f16(raw[c].y)),
+                       "r"(two_f16(raw[c].z)), "r"(two_f16(raw[c].w))
                        : "memory");
         }
         fence_proxy_async_smem();
@@ -1122,7 +1148,7 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
   pdl_launch_dependents();
   const long long i = (long long)blockIdx.x * (CB_WARPS / RW) + warp / RW;
   const int G = a.n_heads / a.c.n_kv_heads;
-  // (uniform over a row's warps; with RW > 1 the CTA holds one row, so it leaves as a whole)
+  // (a row's warps stay together: they meet at a barrier of their own)
   if (i >= (long long)a.r.n_rows * a.n_heads) {
     pdl_wait();
     return;
@@ -1214,14 +1240,16 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
     if (lane == 0) s_m[warp] = M, s_l[warp] = L;
 #pragma unroll
     for (int j = 0; j < D; ++j) s_o[warp][D * lane + j] = o[j];
-    __syncthreads();
-    if (warp > 0) return;
-    float mn = s_m[0];
-    for (int q = 1; q < RW; ++q) mn = fmaxf(mn, s_m[q]);
+    const int w0 = warp - part;
+    if (RW == CB_WARPS || w0 == 0) sync_and<1, 32 * RW>(true);
+    else sync_and<2, 32 * RW>(true);  // (two rows a CTA)
+    if (part > 0) return;
+    float mn = s_m[w0];
+    for (int q = 1; q < RW; ++q) mn = fmaxf(mn, s_m[w0 + q]);
     float w[RW], Ln = 0.f;
 #pragma unroll
     for (int q = 0; q < RW; ++q) {
-      w[q] = s_m[q] == -INFINITY ? s_l[q] : exp2f(s_m[q] - mn) * s_l[q];
+      w[q] = s_m[w0 + q] == -INFINITY ? s_l[w0 + q] : exp2f(s_m[w0 + q] - mn) * s_l[w0 + q];
       Ln += w[q];
     }
     const float il = Ln == 0.f ? 0.f : 1.f / Ln;
@@ -1231,7 +1259,7 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
     for (int q = 0; q < RW; ++q)
       if (w[q] != 0.f) {
 #pragma unroll
-        for (int j = 0; j < D; ++j) o[j] = fmaf(w[q] * il, s_o[q][D * lane + j], o[j]);
+        for (int j = 0; j < D; ++j) o[j] = fmaf(w[q] * il, s_o[w0 + q][D * lane + j], o[j]);
       }
     M = mn;
     L = Ln;
@@ -1242,13 +1270,16 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
   if (a.lse && lane == 0) a.lse[i] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-// The fewer rows there are, the more workers share a unit, and the more warps join a row's states: a CTA of 16 up to
-// 256 rows, of 8 up to 2048, then a warp each.
+// Warps a row: for the states of a row there may be (workers over units, of which there are at least the tiles of all
+// rows together, and one for each sequence that has rows and KV head), four a warp.
 template <typename T, int HD, int TR, int CH, int UC>
 cudaError_t launch_combine(const Kv8AttnParams& a, int workers, cudaStream_t st) {
-  const long long rows = (long long)a.r.n_rows * a.n_heads;
-  if (rows <= 256) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 16>, dim3((unsigned)rows), dim3(512), 0, st, a, workers);
-  if (rows <= 2048) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 8>, dim3((unsigned)rows), dim3(256), 0, st, a, workers);
+  const long long rows = (long long)a.r.n_rows * a.n_heads, group_rows = (long long)a.r.n_rows * (a.n_heads / a.c.n_kv_heads);
+  const long long tiles = (group_rows + TR - 1) / TR;
+  const long long states = workers / (tiles * a.c.n_kv_heads);
+  if (states > 32 && rows < 0x7fffffff)
+    return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 16>, dim3((unsigned)rows), dim3(512), 0, st, a, workers);
+  if (states > 4) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, st, a, workers);
   return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a, workers);
 }
 
