@@ -34,7 +34,7 @@ struct Kv8AttnParams {
   void* out;
   float* lse;
   int* plan;         // [n_seqs + 1]: length of the sequences before b
-  float* states;     // [2 N][tile rows x hd normalised O, then m, then l]
+  float* states;     // [2 N][tile rows x hd normalised O, then m, then l of the tile's rows]
   int* err;
 };
 
@@ -547,21 +547,23 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // states are joined at the unit's end. While the softmax of one stream runs, the tensor core works for the other.
 //
 // Warps 0-3 and 4-7: stream 0 and 1, a thread per row; the stream's first warp also
-// issues its products (a stream has nothing else to do until they are complete). Warps 8-11 fetch codes (16 bytes a
-// load, one chunk ahead in registers), convert them to fp16 and store them as the images of tensor-core
+// issues its products (a stream has nothing else to do until they are complete). Warp 11 asks for codes, page by page as
+// bulk copies up to three chunks ahead; warps 8-10 convert them to fp16 and store them as the images of tensor-core
 // operands: per page of 16 keys two 8-key groups, each of HD / 64 halves of 8 rows x 128 bytes with the 128-byte
 // swizzle; K is read K-major, V MN-major. Exponents stay out of the operands: K's go into the scores, V's into P as in
 // the warp-level form, against the chunk's reference E. Where a chunk's value exponents lie further apart than P
 // can carry, its pages go in groups, one step of the stream each (Kv8Info).
 // ---------------------------------------------------------------------------------------------
 constexpr int T_TR = 256, T_CH = 128, T_UC = 2;
-constexpr int T_CONV_WARPS = 4, T_THREADS = 32 * (8 + T_CONV_WARPS);  // 168 registers a thread
-constexpr int T_PAGES = T_CH / kPage, T_STAGES = 2, T_INFO = 4;
+constexpr int T_CONV_WARPS = 3, T_THREADS = 32 * (8 + T_CONV_WARPS + 1);  // 168 registers a thread
+constexpr int T_PAGES = T_CH / kPage, T_RAW = 3, T_INFO = 8;  // chunks of codes, of Kv8Info in shared memory
 constexpr int TM_COLS = 512;
 template <int HD>
 struct TLayout {
   static constexpr int Q = 128 * HD * 2, KV = T_CH * HD * 2, PAGE = kPage * HD * 2;  // bytes of fp16 operands
-  static constexpr int OFF_K = 2 * Q, OFF_V = OFF_K + T_STAGES * KV, TOTAL = OFF_V + T_STAGES * KV + 1024;  // + alignment
+  static constexpr int RAW = T_CH * HD;                                                                      // codes of a chunk
+  static constexpr int OFF_K = 2 * Q, OFF_V = OFF_K + KV, OFF_RAW = OFF_V + KV;  // RAW: a stage holds K's, then V's
+  static constexpr int TOTAL = OFF_RAW + T_RAW * 2 * RAW + 1024;                 // + alignment
   static constexpr int GROUP = HD * 16;  // 8 keys of a page: HD / 64 halves of 1024 bytes
   // byte offset of 16-byte piece c (8 dims) of key r of a page
   static JF_DEV uint32_t page_piece(int r, int c) {
@@ -572,11 +574,13 @@ struct TLayout {
   }
 };
 
-// What the steps of a chunk need beside its operands. groups: how many steps; pages[j]: pages of step j as bits; E[j]:
-// its reference exponent, d[j]: of a page of the step e_v - E, and w[j]: 2^-d, 0 for other pages; fk: 2^(e_k).
+// What the steps of a chunk need beside its operands. held: slots with a token (0: no chunk, the share has ended).
+// groups: how many steps; pages[j]: pages of step j as bits; E[j]: its reference exponent. fk, ev: 2^(e_k), e_v of a page.
 struct Kv8Info {
-  float fk[T_PAGES], d[T_PAGES][T_PAGES], w[T_PAGES][T_PAGES];
-  int groups, E[T_PAGES], pages[T_PAGES];
+  float fk[T_PAGES];
+  int ev[T_PAGES], E[T_PAGES];
+  uint8_t pages[T_PAGES];
+  int groups, held;
 };
 
 // x * y + z and x + y on two values at a time.
@@ -596,31 +600,6 @@ JF_DEV float2 add2(float2 x, float2 y) {
       : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
   return r;
 }
-// 32 columns of this warp's lanes, without waiting for them (tmem_wait_ld).
-JF_DEV void tmem_ld32_start(uint32_t taddr, float* v) {
-  uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr)
-      : "memory");
-}
-// (the values pass through, so that no use of them moves ahead of the wait)
-JF_DEV void tmem_wait_ld(float (&v)[32], float (&w)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(v[i]), "+f"(w[i]));
-}
-JF_DEV void tmem_wait_ld(float (&v)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) asm volatile("" : "+f"(v[i]));
-}
-
 template <int HD>
 __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnParams a) {
   using Lay = TLayout<HD>;
@@ -628,27 +607,31 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
   extern __shared__ uint8_t sm_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sQ = smem_u32(sm), sK = sQ + Lay::OFF_K, sV = sQ + Lay::OFF_V;
-  // per stage: loaded, and read by both streams (a unit of one tile: by its stream, counted twice); per stream: S ready
-  // (the products, and the thread that issued them, which passes on the chunk's Kv8Info), P V done, everything done
-  __shared__ __align__(8) uint64_t b_kfull[T_STAGES], b_kfree[T_STAGES], b_vfull[T_STAGES], b_vfree[T_STAGES], b_s[2], b_o[2], b_all[2];
+  // a stage of codes: landed, converted; operands K and V: there, and read by both streams (a unit of one tile: by its
+  // stream, counted twice; that they are there, on one barrier for even and one for odd chunks: a stream that waits for every
+  // second one must not meet a barrier a completion ahead or behind); per stream: S ready (the products, and the thread that issued them, which passes on the
+  // chunk's Kv8Info), P V done, everything done
+  __shared__ __align__(8) uint64_t b_raw[T_RAW], b_rawfree[T_RAW], b_kfull[2], b_kfree, b_vfull[2], b_vfree, b_s[2], b_o[2], b_all[2], b_turn[2];
   __shared__ uint32_t tmem_slot;
-  __shared__ int pre[kKv8MaxSeqs + 1];
   __shared__ Kv8Info s_info[T_INFO];
-  __shared__ float s_ml[2][128][2];
-  __shared__ int s_E[2];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int* pre = reinterpret_cast<int*>(sm + Lay::OFF_RAW);  // (until the first codes are asked for)
+  // (shuffles tell the compiler that warp numbers and the TMEM address are uniform: operand descriptors then are)
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.n_heads / a.c.n_kv_heads, Hkv = a.c.n_kv_heads;
   if (tid == 0) {
-    for (int i = 0; i < T_STAGES; ++i) {
+    for (int i = 0; i < T_RAW; ++i) {
+      mbar_init(smem_u32(&b_raw[i]), 1);
+      mbar_init(smem_u32(&b_rawfree[i]), T_CONV_WARPS);
+    }
+    mbar_init(smem_u32(&b_kfree), 2);
+    mbar_init(smem_u32(&b_vfree), 2);
+    for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&b_kfull[i]), T_CONV_WARPS);
       mbar_init(smem_u32(&b_vfull[i]), T_CONV_WARPS);
-      mbar_init(smem_u32(&b_kfree[i]), 2);
-      mbar_init(smem_u32(&b_vfree[i]), 2);
-    }
-    for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&b_s[i]), 2);
       mbar_init(smem_u32(&b_o[i]), 1);
       mbar_init(smem_u32(&b_all[i]), 1);
+      mbar_init(smem_u32(&b_turn[i]), 1);
     }
     fence_mbar_init();
   }
@@ -663,41 +646,33 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
     tmem_alloc(smem_u32(&tmem_slot), TM_COLS);
     tmem_relinquish();
   }
+  W w;
+  w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + shares.size(blockIdx.x));
+  fence_proxy_async_smem();  // the plan's place is taken by copies
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
   const unsigned long long limit = kWaitLimitDefaultNs;
   auto wait = [&](uint64_t& bar, int uses) {  // for completion number `uses` (from 0); the warp agrees
     const bool ok = mbar_wait_bounded(smem_u32(&bar), (uint32_t)uses & 1u, limit);
     return __all_sync(0xffffffffu, ok) != 0;
   };
-  auto start = [&](W& w) { w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + shares.size(blockIdx.x)); };
   auto tile_rows = [&](const W& w) { return min(w.s.n * G - w.tile * T_TR, T_TR); };
 
-  if (warp >= 8) {
-    // ---- codes to operands. Thread: pieces of 16 dims, rows 4 cw .. of each 32 keys. The lanes of a quarter warp
-    // (8 x 16 bytes) hold two rows, so that their stores meet different banks.
-    W w;
-    start(w);
-    const int cw = warp - 8;
-    constexpr int PR = HD / 16;             // pieces per key
-    constexpr int RW = 32 / PR;             // keys per warp and round
-    constexpr int ROUNDS = T_CH / (RW * T_CONV_WARPS);
-    const int lr = PR == 8 ? ((lane >> 2) & 1) + 2 * (lane >> 4) : lane >> 2, lc = PR == 8 ? (lane & 3) + 4 * ((lane >> 3) & 1) : lane & 3;
-    // A chunk on its way: its page ids are asked for three chunks ahead of its conversion, exponents two, codes one, so
-    // that nothing waits for what it has just asked for. Lane j < 8: page j.
+  if (warp == 11) {
+    // ---- asks for codes: page ids are read two chunks ahead of them, exponents one, so that nothing waits for what has
+    // just been asked for. Lane j < 8: page j.
     struct Ahead {
-      int raw, ek, ev, kp0, keys, kvh;
-      bool there;
+      int id, ek, ev, held, kvh;
     };
     int chunk = w.c0();
     bool more = w.c1() > chunk;
     auto look = [&]() {  // the next chunk of the share
-      Ahead n = {0, 0, 0, chunk * T_CH, w.s.len + w.s.n, w.kvh, more};
+      const int kp0 = chunk * T_CH;
+      Ahead n = {0, 0, 0, more ? min(T_CH, w.s.len + w.s.n - kp0) : 0, w.kvh};
       if (more) {
-        if (lane < T_PAGES && n.kp0 + lane * kPage < n.keys)
-          n.raw = a.c.page_table[(long long)w.b * a.c.pages_per_seq + chunk * T_PAGES + lane];
+        if (lane * kPage < n.held) n.id = a.c.page_table[(long long)w.b * a.c.pages_per_seq + chunk * T_PAGES + lane];
         if (++chunk >= w.c1()) {
           more = w.next(a, G) && w.c1() > 0;
           chunk = 0;
@@ -705,104 +680,124 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       }
       return n;
     };
-    auto block_of = [&](Ahead& n) {  // ids outside the pool are reported, and page 0 read in their place
-      if (n.raw < 0 || n.raw >= a.c.n_pages) {
-        if (n.there) jf_set_error(a.err, JF_DERR_BOUNDS);
-        n.raw = 0;
-      }
-      return (long long)n.raw * Hkv + n.kvh;
-    };
     auto exponents = [&](Ahead& n) {
-      if (n.there && lane < T_PAGES && n.kp0 + lane * kPage < n.keys) {
-        const long long blk = block_of(n);
+      if (lane * kPage < n.held) {
+        if (n.id < 0 || n.id >= a.c.n_pages) {  // reported, and page 0 read in its place
+          jf_set_error(a.err, JF_DERR_BOUNDS);
+          n.id = 0;
+        }
+        const long long blk = (long long)n.id * Hkv + n.kvh;
         n.ek = a.c.k_exp[blk];
         n.ev = a.c.v_exp[blk];
       }
     };
-    auto fetch = [&](const Ahead& n, const void* pool, uint4 (&x)[ROUNDS]) {
-      // (slots past the last token are read too, and replaced by zeros when they are converted)
-      const unsigned long long base = reinterpret_cast<unsigned long long>(pool) + ((long long)n.raw * Hkv + n.kvh) * (kPage * HD);
-#pragma unroll
-      for (int j = 0; j < ROUNDS; ++j) {
-        const int r = (j * T_CONV_WARPS + cw) * RW + lr;  // (a warp's rows of a round lie in one page)
-        const unsigned long long p = __shfl_sync(0xffffffffu, base, (j * T_CONV_WARPS + cw) * RW / kPage);
-        if (n.there) x[j] = __ldcg(reinterpret_cast<const uint4*>(p + (r % kPage) * HD + lc * 16));
+    Ahead cur = look(), next = look();
+    exponents(cur);
+    int E_run = -126, g = 0;
+    bool ok = true;
+    for (;; ++g) {  // (the last round asks for nothing and tells the converters so)
+      const int stage = g % T_RAW;
+      if (g >= T_RAW && !wait(b_rawfree[stage], g / T_RAW - 1)) {
+        ok = false;
+        break;
       }
-    };
-    auto put = [&](uint4 (&x)[ROUNDS], uint32_t dst, int held) {  // held: slots with a token
-      if (held < T_CH) {
+      // the copies first: what describes them has time until they have landed
+      const bool mine = lane * kPage < cur.held;
+      const uint32_t bar = smem_u32(&b_raw[stage]), dst = sQ + Lay::OFF_RAW + stage * 2 * Lay::RAW + lane * (kPage * HD);
+      const long long off = ((long long)cur.id * Hkv + cur.kvh) * (kPage * HD);
+      if (mine) {
+        bulk_load(dst, reinterpret_cast<const uint8_t*>(a.c.k) + off, kPage * HD, bar);
+        bulk_load(dst + Lay::RAW, reinterpret_cast<const uint8_t*>(a.c.v) + off, kPage * HD, bar);
+      }
+      Kv8Info& info = s_info[g % T_INFO];
+      unsigned rest = __ballot_sync(0xffffffffu, mine);
+      const int bytes = __popc(rest) * (2 * kPage * HD);
+      int groups = 0;
+      while (rest) {
+        const bool in = rest >> lane & 1u;
+        const int hi = __reduce_max_sync(0xffffffffu, in ? cur.ev : -1000);
+        const unsigned now = __ballot_sync(0xffffffffu, in && cur.ev >= hi - W_EV_MAX);
+        const int lo = __reduce_min_sync(0xffffffffu, now >> lane & 1u ? cur.ev : 1000);
+        if (E_run > lo || hi - E_run > W_EV_MAX) E_run = max(max(min(lo, hi - W_EV_SET), hi - W_EV_MAX), -126);
+        if (lane == 0) info.pages[groups] = (uint8_t)now, info.E[groups] = E_run;
+        ++groups;
+        rest &= ~now;
+      }
+      if (lane < T_PAGES) info.fk[lane] = pow2i(cur.ek), info.ev[lane] = cur.ev;
+      if (lane == 0) info.groups = groups, info.held = cur.held;
+      __syncwarp();
+      if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
+      if (cur.held == 0) break;
+      cur = next;
+      exponents(cur);
+      next = look();
+    }
+    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+    // every copy has landed before the CTA may leave, also after a wait that gave up. (The last round has completed its
+    // stage's barrier once more; the chunk before it there has been converted.)
+    for (int k = max(0, g - T_RAW + (ok ? 1 : 0)); k < g; ++k)
+      if (!wait(b_raw[k % T_RAW], k / T_RAW)) break;
+  } else if (warp >= 8) {
+    // ---- codes to operands. Thread: pieces of 16 dims; a warp has pages 3 cw .. of K and 5 - 3 cw .. of V (three, three
+    // and two of 8), a round is 4 (8) keys. The lanes of a quarter warp (8 x 16 bytes) read two rows and write two rows so
+    // that neither meets a bank twice.
+    const int cw = warp - 8;
+    constexpr int PR = HD / 16, ROUNDS = kPage * PR / 32;  // pieces per key; rounds per page
+    const int lr = PR == 8 ? 2 * ((lane >> 3) & 1) + ((lane >> 2) & 1) : lane >> 2;
+    const int lc = PR == 8 ? (lane & 3) + 4 * (((lane >> 2) & 1) ^ (lane >> 4)) : lane & 3;
+    auto put = [&](uint32_t src, uint32_t dst, int first, int held) {
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const int page = first + q;
+        if (page < 0 || page >= T_PAGES) continue;
+        uint4 x[ROUNDS];
 #pragma unroll
         for (int j = 0; j < ROUNDS; ++j)
-          if ((j * T_CONV_WARPS + cw) * RW + lr >= held) x[j] = make_uint4(0u, 0u, 0u, 0u);
-      }
-#pragma unroll
-      for (int j = 0; j < ROUNDS; ++j) {
-        const int r = (j * T_CONV_WARPS + cw) * RW + lr;
-        const uint32_t wd[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
-        const uint32_t page = dst + (uint32_t)(r / kPage * Lay::PAGE);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t p = page + Lay::page_piece(r % kPage, 2 * lc + h);
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(e4m3x2_to_f16x2(wd[2 * h])),
-                       "r"(e4m3x2_to_f16x2(wd[2 * h] >> 16)), "r"(e4m3x2_to_f16x2(wd[2 * h + 1])),
-                       "r"(e4m3x2_to_f16x2(wd[2 * h + 1] >> 16))
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(x[j].x), "=r"(x[j].y), "=r"(x[j].z), "=r"(x[j].w)
+                       : "r"(src + page * (kPage * HD) + (j * (32 / PR) + lr) * HD + lc * 16)
                        : "memory");
+        if (held < T_CH) {  // slots without a token
+#pragma unroll
+          for (int j = 0; j < ROUNDS; ++j)
+            if (page * kPage + j * (32 / PR) + lr >= held) x[j] = make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int j = 0; j < ROUNDS; ++j) {
+          const uint32_t wd[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t p = dst + page * Lay::PAGE + Lay::page_piece(j * (32 / PR) + lr, 2 * lc + h);
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(e4m3x2_to_f16x2(wd[2 * h])),
+                         "r"(e4m3x2_to_f16x2(wd[2 * h] >> 16)), "r"(e4m3x2_to_f16x2(wd[2 * h + 1])),
+                         "r"(e4m3x2_to_f16x2(wd[2 * h + 1] >> 16))
+                         : "memory");
+          }
         }
       }
-      fence_proxy_async_smem();  // this thread's stores -> tensor-core operand reads
+      fence_proxy_async_smem();  // this thread's stores -> operand reads; its reads of the codes -> the next copies
       __syncwarp();
     };
-    int E_run = -126;
-    Ahead cur = look(), next = look(), after = look();
-    uint4 xk[ROUNDS], xv[ROUNDS];
-    exponents(cur);
-    fetch(cur, a.c.k, xk);
-    fetch(cur, a.c.v, xv);
-    exponents(next);
-    for (int g = 0; cur.there; ++g) {
-      const int stage = g % T_STAGES, use = g / T_STAGES;
-      if (use > 0 && !wait(b_kfree[stage], use - 1)) {
-        if (lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
-        break;
+    bool ok = true;
+    for (int g = 0; ok; ++g) {
+      const int stage = g % T_RAW;
+      const uint32_t src = sQ + Lay::OFF_RAW + stage * 2 * Lay::RAW;
+      ok = wait(b_raw[stage], g / T_RAW);
+      const int held = s_info[g % T_INFO].held;
+      if (!ok || held == 0) break;
+      ok = g == 0 || wait(b_kfree, g - 1);
+      if (!ok) break;
+      put(src, sK, 3 * cw, held);
+      if (lane == 0) mbar_arrive(smem_u32(&b_kfull[g & 1]));
+      ok = g == 0 || wait(b_vfree, g - 1);
+      if (!ok) break;
+      put(src + Lay::RAW, sV, 5 - 3 * cw, held);
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&b_vfull[g & 1]));
+        mbar_arrive(smem_u32(&b_rawfree[stage]));
       }
-      if (cw == 0) {
-        Kv8Info& info = s_info[g % T_INFO];
-        const bool holds = lane < T_PAGES && cur.kp0 + lane * kPage < cur.keys;
-        unsigned rest = __ballot_sync(0xffffffffu, holds);
-        int n = 0;
-        while (rest) {
-          const bool in = rest >> lane & 1u;
-          const int hi = __reduce_max_sync(0xffffffffu, in ? cur.ev : -1000);
-          const unsigned now = __ballot_sync(0xffffffffu, in && cur.ev >= hi - W_EV_MAX);
-          const int lo = __reduce_min_sync(0xffffffffu, now >> lane & 1u ? cur.ev : 1000);
-          if (E_run > lo || hi - E_run > W_EV_MAX) E_run = max(max(min(lo, hi - W_EV_SET), hi - W_EV_MAX), -126);
-          if (lane == 0) info.pages[n] = (int)now, info.E[n] = E_run;
-          if (lane < T_PAGES) {
-            const bool mine = now >> lane & 1u;
-            info.d[n][lane] = mine ? (float)(cur.ev - E_run) : 0.f;
-            info.w[n][lane] = mine ? pow2i(E_run - cur.ev) : 0.f;
-          }
-          ++n;
-          rest &= ~now;
-        }
-        if (lane < T_PAGES) info.fk[lane] = pow2i(cur.ek);
-        if (lane == 0) info.groups = n;
-      }
-      put(xk, sK + stage * Lay::KV, cur.keys - cur.kp0);
-      if (lane == 0) mbar_arrive(smem_u32(&b_kfull[stage]));
-      fetch(next, a.c.k, xk);
-      if (use > 0 && !wait(b_vfree[stage], use - 1)) {
-        if (lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
-        break;
-      }
-      put(xv, sV + stage * Lay::KV, cur.keys - cur.kp0);
-      if (lane == 0) mbar_arrive(smem_u32(&b_vfull[stage]));
-      fetch(next, a.c.v, xv);
-      cur = next;
-      next = after;
-      exponents(next);
-      after = look();
     }
+    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
   } else {
     // ---- stream s: row `lr` of its 128
     const int s = warp >> 2, lr = (warp & 3) * 32 + lane;
@@ -811,48 +806,42 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
     constexpr uint32_t idesc_s = idesc_f16_f32(128, T_CH), idesc_pv = idesc_f16_f32(128, HD) | (1u << 16);  // V MN-major
     const uint64_t dq = sdesc_k_sw128(sQ + s * Lay::Q), dk = sdesc_k_sw128(sK, Lay::GROUP), dv = sdesc_mn_sw128(sV, 1024u, Lay::GROUP);
     // S of a step, by the stream's first warp; both = a unit of two tiles
-    auto issue_s = [&](int g, bool last, bool both) {
-      const int stage = g % T_STAGES;
+    auto issue_s = [&](bool last, bool both) {
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t db = dk + (uint64_t)(stage * (Lay::KV >> 4));
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk)
           tc_mma_bf16(tmem + s * 128, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
-                      db + (uint64_t)((kk >> 2) * 64 + (kk & 3) * 2), idesc_s, kk > 0 ? 1u : 0u);
+                      dk + (uint64_t)((kk >> 2) * 64 + (kk & 3) * 2), idesc_s, kk > 0 ? 1u : 0u);
         tc_commit(smem_u32(&b_s[s]));
         mbar_arrive(smem_u32(&b_s[s]));
         if (last) {
-          tc_commit(smem_u32(&b_kfree[stage]));
-          if (!both) tc_commit(smem_u32(&b_kfree[stage]));
+          tc_commit(smem_u32(&b_kfree));
+          if (!both) tc_commit(smem_u32(&b_kfree));
         }
       }
       __syncwarp();
     };
-    auto issue_pv = [&](int g, int pages, bool fresh, bool last, bool both) {
-      const int stage = g % T_STAGES;
+    auto issue_pv = [&](int pages, bool fresh, bool last, bool both) {
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t d = dv + (uint64_t)(stage * (Lay::KV >> 4));
 #pragma unroll
         for (int kk = 0; kk < T_PAGES; ++kk)
           if (kk < pages)
-            tc_mma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + kk * 8, d + (uint64_t)(kk * (Lay::PAGE >> 4)), idesc_pv,
+            tc_mma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + kk * 8, dv + (uint64_t)(kk * (Lay::PAGE >> 4)), idesc_pv,
                           kk > 0 || !fresh ? 1u : 0u);
         tc_commit(smem_u32(&b_o[s]));
         if (last) {
-          tc_commit(smem_u32(&b_vfree[stage]));
-          if (!both) tc_commit(smem_u32(&b_vfree[stage]));
+          tc_commit(smem_u32(&b_vfree));
+          if (!both) tc_commit(smem_u32(&b_vfree));
         }
       }
       __syncwarp();
     };
     auto stream_and = [&](bool ok) { return s ? sync_and<2, 128>(ok) : sync_and<1, 128>(ok); };
     const bool q16 = ((uintptr_t)a.q & 15) == 0 && a.ld_q % 8 == 0;
-    W w;
-    start(w);
     bool ok = true;
-    int steps = 0, g = 0;  // steps of the stream so far; chunks of the share so far
+    int steps = 0, g = 0, turns = 0;  // steps of the stream so far; chunks of the share so far; turns taken
     while (true) {
       const int rows = tile_rows(w);
       const bool two = rows > 128;
@@ -864,42 +853,55 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       const int tr = w.tile * T_TR + (live ? r : 0), tok = tr / G;
       const long long at = (long long)(sq.row0 + tok) * a.n_heads + w.kvh * G + (tr - tok * G);
       float f;
-      {  // queries, scaled; the softmax scale's sign goes with them, so that f >= 0
-        const bf16* src = reinterpret_cast<const bf16*>(a.q) + (long long)(sq.row0 + tok) * a.ld_q + (long long)(w.kvh * G + (tr - tok * G)) * HD;
-        uint4 raw[HD / 8];
-        float amax = 0.f;
+      {  // queries: a warp copies its rows whole, HD / 8 lanes a row; then each thread scales its own row in place. The
+        // softmax scale's sign goes with them, so that f >= 0. (Rolled loops: the code is new to the instruction cache.)
+        constexpr int LPR = HD / 8, RPI = 32 / LPR;
+        const bf16* mine = live ? reinterpret_cast<const bf16*>(a.q) + (long long)(sq.row0 + tok) * a.ld_q + (long long)(w.kvh * G + (tr - tok * G)) * HD
+                                : nullptr;
+        const uint32_t sq_s = sQ + (uint32_t)(s * Lay::Q);
+        if (q16) {
+#pragma unroll 4
+          for (int i = 0; i < LPR; ++i) {
+            const int rl = i * RPI + lane / LPR, c = lane % LPR;
+            const bf16* src = reinterpret_cast<const bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), rl));
+            cp_async16_zfill(sq_s + Lay::q_piece((warp & 3) * 32 + rl, c), src ? src + c * 8 : reinterpret_cast<const bf16*>(a.q), src != nullptr);
+          }
+          asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
+          __syncwarp();
+        } else {
+#pragma unroll 1
+          for (int c = 0; c < LPR; ++c) {
+            uint32_t h[4] = {0u, 0u, 0u, 0u};
+            if (live) {
 #pragma unroll
-        for (int c = 0; c < HD / 8; ++c) {
-          if (!live) {
-            raw[c] = make_uint4(0u, 0u, 0u, 0u);
-          } else if (q16) {
-            raw[c] = *reinterpret_cast<const uint4*>(src + 8 * c);
-          } else {
-            uint32_t h[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              h[i] = (uint32_t)__bfloat16_as_ushort(src[8 * c + 2 * i]) | (uint32_t)__bfloat16_as_ushort(src[8 * c + 2 * i + 1]) << 16;
-            raw[c] = make_uint4(h[0], h[1], h[2], h[3]);
+              for (int k = 0; k < 4; ++k)
+                h[k] = (uint32_t)__bfloat16_as_ushort(mine[c * 8 + 2 * k]) | (uint32_t)__bfloat16_as_ushort(mine[c * 8 + 2 * k + 1]) << 16;
+            }
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(sq_s + Lay::q_piece(lr, c)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
           }
         }
-        auto lo = [](uint32_t h) { return __uint_as_float(h << 16); };
-        auto hi = [](uint32_t h) { return __uint_as_float(h & 0xffff0000u); };
-#pragma unroll
-        for (int c = 0; c < HD / 8; ++c) {
-          amax = fmaxf(amax, fmaxf(fmaxf(fabsf(lo(raw[c].x)), fabsf(hi(raw[c].x))), fmaxf(fabsf(lo(raw[c].y)), fabsf(hi(raw[c].y)))));
-          amax = fmaxf(amax, fmaxf(fmaxf(fabsf(lo(raw[c].z)), fabsf(hi(raw[c].z))), fmaxf(fabsf(lo(raw[c].w)), fabsf(hi(raw[c].w)))));
+        constexpr uint32_t mag = 0x7fff7fffu;
+        uint32_t most = 0;  // the largest magnitudes as bit patterns
+        auto piece = [&](int c, uint32_t (&x)[4]) {
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(sq_s + Lay::q_piece(lr, c)) : "memory");
+        };
+#pragma unroll 4
+        for (int c = 0; c < LPR; ++c) {
+          uint32_t x[4];
+          piece(c, x);
+          most = __vmaxu2(most, __vmaxu2(__vmaxu2(x[0] & mag, x[1] & mag), __vmaxu2(x[2] & mag, x[3] & mag)));
         }
-        const int sh = query_shift(amax);
-        const float up = a.scale_log2 < 0.f ? -pow2i(sh) : pow2i(sh);
-        f = pow2i(-sh) * fabsf(a.scale_log2);
+        const int my_shift = query_shift(__uint_as_float(max(most & 0xffffu, most >> 16) << 16));
+        const float up = a.scale_log2 < 0.f ? -pow2i(my_shift) : pow2i(my_shift);
+#pragma unroll 4
+        for (int c = 0; c < LPR; ++c) {
+          uint32_t x[4];
+          piece(c, x);
 #pragma unroll
-        for (int c = 0; c < HD / 8; ++c) {
-          const uint32_t p = sQ + (uint32_t)(s * Lay::Q) + Lay::q_piece(lr, c);
-          auto two_f16 = [&](uint32_t h) { return pack_f16(lo(h) * up, hi(h) * up); };
-          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(p), "r"(two_f16(raw[c].x)), "r"(two_f16(raw[c].y)),
-                       "r"(two_f16(raw[c].z)), "r"(two_f16(raw[c].w))
-                       : "memory");
+          for (int k = 0; k < 4; ++k) x[k] = pack_f16(__uint_as_float(x[k] << 16) * up, __uint_as_float(x[k] & 0xffff0000u) * up);
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(sq_s + Lay::q_piece(lr, c)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
         }
+        f = pow2i(-my_shift) * fabsf(a.scale_log2);
         fence_proxy_async_smem();
       }
       float m_ref = -INFINITY, l = 0.f;
@@ -909,8 +911,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       g += n;
       ok = stream_and(ok);  // the stream's queries are there
       if (issuer && c_first < n && ok) {
-        ok = wait(b_kfull[(g0 + c_first) % T_STAGES], (g0 + c_first) / T_STAGES);
-        if (ok) issue_s(g0 + c_first, s_info[(g0 + c_first) % T_INFO].groups == 1, two);
+        ok = wait(b_kfull[(g0 + c_first) & 1], (g0 + c_first) >> 1);
+        if (ok) issue_s(s_info[(g0 + c_first) % T_INFO].groups == 1, two);
       }
       bool fresh = true;  // no P V of the unit yet
       bool go = true;     // (left by all warps of the stream together)
@@ -944,12 +946,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           ok = wait(b_s[s], steps) && ok;
           tc_fence_after();
           if (ok) {
-          // The row's scores, 32 at a time: the maximum of columns 64 .. 127, then of 0 .. 63, which stay in registers
-          // until their exponentials; 64 .. 127 are read again, each 32 while the 32 before them are worked on. (P of
-          // column c goes to c / 2, which has been read by then.)
-          float v0[32], v1[32];
-          tmem_ld32_start(t_s + 64, v0);
-          tmem_ld32_start(t_s + 96, v1);
+          // The row's scores, 32 at a time, for the maximum and again for the exponentials (P of column c goes to c / 2,
+          // which has been read by then). Rolled loops: the code of a step has to stay in the instruction cache.
           groups = info.groups;
           const int pages = info.pages[j], E_new = info.E[j];
           auto hide = [&](int h, float (&v)[32]) {
@@ -972,18 +970,13 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
               mc = fmaxf(mc, mx * factor(2 * h + y));
             }
           };
-          tmem_wait_ld(v0, v1);
-          hide(2, v0);
-          largest(2, v0);
-          hide(3, v1);
-          largest(3, v1);
-          tmem_ld32_start(t_s, v0);
-          tmem_ld32_start(t_s + 32, v1);
-          tmem_wait_ld(v0, v1);
-          hide(0, v0);
-          largest(0, v0);
-          hide(1, v1);
-          largest(1, v1);
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            float v[32];
+            tmem_ld32(t_s + 32 * h, v);
+            hide(h, v);
+            largest(h, v);
+          }
           const bool raise = mc > m_ref + W_LAG;
           if (!first && (__any_sync(0xffffffffu, raise) || E_new != E)) {
             const float al = raise ? (m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - mc)) : 1.f;
@@ -1007,7 +1000,8 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
             uint32_t u[16];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const float fx = factor(2 * h + y), b = nb + info.d[j][2 * h + y];
+              const int d = pages >> (2 * h + y) & 1 ? info.ev[2 * h + y] - E : 0;  // (other pages' are hidden)
+              const float fx = factor(2 * h + y), b = nb + (float)d;
               float2 ls = make_float2(0.f, 0.f);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
@@ -1017,20 +1011,17 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
                 ls = add2(ls, p);
                 u[8 * y + i] = pack_f16(p.x, p.y);
               }
-              l = fmaf(ls.x + ls.y, info.w[j][2 * h + y], l);
+              l = fmaf(ls.x + ls.y, pow2i(-d), l);
             }
             tmem_st16(t_s + 16 * h, u);
           };
-          exponentials(0, v0);
-          tmem_ld32_start(t_s + 64, v0);
-          exponentials(1, v1);
-          tmem_wait_ld(v0);
-          tmem_ld32_start(t_s + 96, v1);
-          hide(2, v0);
-          exponentials(2, v0);
-          tmem_wait_ld(v1);
-          hide(3, v1);
-          exponentials(3, v1);
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            float v[32];
+            tmem_ld32(t_s + 32 * h, v);
+            hide(h, v);
+            exponentials(h, v);
+          }
           tmem_wait_st();
           }
           tc_fence_before();
@@ -1038,13 +1029,20 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           if (!go) break;
           if (issuer) {
             const bool last = j == groups - 1;
-            ok = wait(b_vfull[gc % T_STAGES], gc / T_STAGES);
-            if (ok) issue_pv(gc, held, fresh, last, two);
+            // with two tiles the streams take turns: products of both at once would end later for both, and leave the
+            // tensor core idle while both are at their softmax
+            if (two && (s || turns > 0)) ok = wait(b_turn[s], s ? turns : turns - 1);
+            ok = ok && wait(b_vfull[gc & 1], gc >> 1);
+            if (ok) issue_pv(held, fresh, last, two);
             // the stream's next S, once P (which lies where S will) has been read
             const int gn = last ? gc + c_step : gc, jn = last ? 0 : j + 1;
             if (ok && (!last || c + c_step < n)) {
-              ok = wait(b_o[s], steps) && wait(b_kfull[gn % T_STAGES], gn / T_STAGES);
-              if (ok) issue_s(gn, s_info[gn % T_INFO].groups == jn + 1, two);
+              ok = wait(b_o[s], steps) && wait(b_kfull[gn & 1], gn >> 1);
+              if (ok) issue_s(s_info[gn % T_INFO].groups == jn + 1, two);
+            }
+            if (two) {
+              if (lane == 0) mbar_arrive(smem_u32(&b_turn[s ^ 1]));
+              ++turns;
             }
           }
           fresh = false;
@@ -1056,9 +1054,9 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         tc_fence_after();
       }
       if (!two) {
-        s_ml[s][lr][0] = m_ref;
-        s_ml[s][lr][1] = l;
-        if (lr == 0) s_E[s] = first ? -4096 : E;
+        // (where the stream's queries were)
+        reinterpret_cast<float2*>(sm + s * Lay::Q)[lr] = make_float2(m_ref, l);
+        if (lr == 0) reinterpret_cast<int*>(sm + s * Lay::Q)[256] = first ? -4096 : E;
       }
       ok = sync_and<3, 256>(ok);  // both streams leave a unit together (barrier 0 is __syncthreads)
       if (!ok) break;
@@ -1068,13 +1066,15 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       float M = m_ref, L = l, w0 = 1.f, w1 = 0.f;  // weights of this stream's O (two tiles), or of both streams'
       int Em = E, d0 = 0, d1 = HD;                 // their unit 2^Em; the dims that this thread finishes
       if (!two) {
-        const float m0 = s_ml[0][lr][0], m1 = s_ml[1][lr][0], l0 = s_ml[0][lr][1], l1 = s_ml[1][lr][1];
+        const float2 ml0 = reinterpret_cast<const float2*>(sm)[lr], ml1 = reinterpret_cast<const float2*>(sm + Lay::Q)[lr];
+        const int E0 = reinterpret_cast<const int*>(sm)[256], E1 = reinterpret_cast<const int*>(sm + Lay::Q)[256];
+        const float m0 = ml0.x, m1 = ml1.x, l0 = ml0.y, l1 = ml1.y;
         M = fmaxf(m0, m1);
         const float a0 = m0 == -INFINITY ? 0.f : exp2f(m0 - M), a1 = m1 == -INFINITY ? 0.f : exp2f(m1 - M);
         L = (m0 == -INFINITY ? l0 : a0 * l0) + (m1 == -INFINITY ? l1 : a1 * l1);  // (nothing seen: 0, or NaN)
-        Em = max(s_E[0], s_E[1]);  // (of a stream without a step: far below)
-        w0 = a0 * pow2i(max(s_E[0] - Em, -126));
-        w1 = a1 * pow2i(max(s_E[1] - Em, -126));
+        Em = max(E0, E1);  // (of a stream without a step: far below)
+        w0 = a0 * pow2i(max(E0 - Em, -126));
+        w1 = a1 * pow2i(max(E1 - Em, -126));
         d0 = s * (HD / 2);
         d1 = d0 + HD / 2;
       }
@@ -1190,7 +1190,7 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
   auto state = [&](int c) { return a.states + (long long)shares.slot(first, c) * (TR * (HD + 2)); };
   // this warp's states c = i0 + part, + RW, ...: 32 at a time, lane j the statistics of the j'th, and of these B at a
   // time in flight
-  constexpr int B = 8;
+  constexpr int B = 16;
   const int mine = i1 - i0 - part >= 0 ? (i1 - i0 - part) / RW + 1 : 0;
   float M = -INFINITY, L = 0.f, o[D];  // O as the weighted mean of what was joined so far, of weight L 2^M
 #pragma unroll
@@ -1202,8 +1202,13 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
 #pragma unroll
       for (int x = 0; x < B; ++x) {
         const float* sx = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(st), k + x));
-#pragma unroll
-        for (int j = 0; j < D; ++j) ov[x][j] = sx ? sx[r * HD + D * lane + j] : 0.f;
+        if constexpr (D == 4) {
+          const float4 v = sx ? __ldcg(reinterpret_cast<const float4*>(sx + r * HD) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+          ov[x][0] = v.x, ov[x][1] = v.y, ov[x][2] = v.z, ov[x][3] = v.w;
+        } else {
+          const float2 v = sx ? __ldcg(reinterpret_cast<const float2*>(sx + r * HD) + lane) : make_float2(0.f, 0.f);
+          ov[x][0] = v.x, ov[x][1] = v.y;
+        }
       }
     };
     const float mc = st ? st[TR * HD + r] : -INFINITY, lc = st ? st[TR * (HD + 1) + r] : 0.f;
@@ -1270,16 +1275,18 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
   if (a.lse && lane == 0) a.lse[i] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-// Warps a row: for the states of a row there may be (workers over units, of which there are at least the tiles of all
-// rows together, and one for each sequence that has rows and KV head), four a warp.
+// Warps a row, by the states that a row may have (workers over units, of which there are at least the tiles of all rows
+// together for each KV head): what a warp does before its first state costs as much as 30 states, so a second one
+// pays late. One 7B draft of 32 rows over 32,768 tokens (up to 38 states a row), all of the attention: 47.1 us with 4
+// warps a row, 55.7 with 16, 40.3 with one.
 template <typename T, int HD, int TR, int CH, int UC>
 cudaError_t launch_combine(const Kv8AttnParams& a, int workers, cudaStream_t st) {
   const long long rows = (long long)a.r.n_rows * a.n_heads, group_rows = (long long)a.r.n_rows * (a.n_heads / a.c.n_kv_heads);
   const long long tiles = (group_rows + TR - 1) / TR;
   const long long states = workers / (tiles * a.c.n_kv_heads);
-  if (states > 32 && rows < 0x7fffffff)
+  if (states > 192 && rows < 0x7fffffff)
     return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 16>, dim3((unsigned)rows), dim3(512), 0, st, a, workers);
-  if (states > 4) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, st, a, workers);
+  if (states > 48) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, st, a, workers);
   return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a, workers);
 }
 
