@@ -4,10 +4,13 @@
 //   S = sum e^(scale d),  T = sum e^(scale d) d,   lse = scale m + ln S,   entropy = ln S - scale T / S,
 // and when m grows, T takes the step times S before both shrink. (The difference comes first: where every logit is
 // the type's lowest value, as in a row that a mask has emptied, x log2 e would overflow.) Every thread keeps its own (m, S, T); they are joined in
-// thread order. The top list is kept per warp: a buffer of candidates that exceed the warp's n_top'th best so
-// far, ordered by (value, lower index) as one 64-bit key, and cut back to n_top whenever it fills, so the list does
-// not depend on the order in which candidates arrive. Few rows are cut into segments (one CTA each), whose states
+// thread order. The top list is kept per CTA: a buffer of candidates that exceed its n_top'th best so far, ordered by
+// (value, lower index) as one 64-bit key, and cut back to n_top when it fills, so the list does not depend on the
+// order in which candidates arrive. The n_top'th largest of the threads' first maxima is a bound to begin with: about
+// 100 of a row's 152,064 logits ever become candidates for a list of 20. Few rows are cut into segments (one CTA each), whose states
 // and lists a second kernel joins in segment order.
+#include <type_traits>
+
 #include "../../include/jf_ops.h"
 #include "jf_device.cuh"
 #include "jf_internal.h"
@@ -16,7 +19,7 @@ namespace jf {
 namespace {
 
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
-constexpr int LP_BUF = 512;         // candidates a warp holds
+constexpr int LP_BUF = 512;         // candidates a CTA holds; of a warp that joins segments
 constexpr int LP_SEG_MIN = 4096;    // fewest logits of a segment
 constexpr int LP_CTAS = 608;        // CTAs that fill the GPU (152 SMs x 4)
 constexpr float LOG2E = 1.4426950408889634f;
@@ -91,56 +94,85 @@ struct Vec<bf16> {
   }
 };
 
-// A row as 16-byte vectors from the boundary at or before its first element: vector v holds elements
-// v N - skew .. v N - skew + N - 1, of which those in [0, V) exist.
+// A row as `n_vec` whole 16-byte vectors of the memory it lies in, the elements before them (fewer than a vector) and
+// those behind.
 template <typename T>
 struct Row {
   const T* p;
-  int skew, n_vec, V;
+  int head, n_vec, V;
   JF_DEV Row(const T* base, int V_) : p(base), V(V_) {
-    skew = (int)(((uintptr_t)base & 15) / sizeof(T));
-    n_vec = (int)(((long long)V + skew + Vec<T>::N - 1) / Vec<T>::N);
+    const int skew = (int)(((uintptr_t)base & 15) / sizeof(T));
+    head = min(V, skew ? Vec<T>::N - skew : 0);
+    n_vec = (V - head) / Vec<T>::N;
   }
-  JF_DEV long long first(int v) const { return (long long)v * Vec<T>::N - skew; }
-  JF_DEV bool whole(int v) const { return first(v) >= 0 && first(v) + Vec<T>::N <= V; }
-  JF_DEV void load(int v, bool live, float (&x)[Vec<T>::N]) const {
-    if (live && whole(v)) {
-      Vec<T>::load(p + first(v), x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < Vec<T>::N; ++i) {
-        const long long e = first(v) + i;
-        x[i] = live && e >= 0 && e < V ? act_to_f32(p[e]) : -INFINITY;
-      }
-    }
+  JF_DEV const T* vec(int v) const { return p + head + (long long)v * Vec<T>::N; }
+  // Index of edge element t (0 .. 2 N - 1: the head's, then the tail's), or -1.
+  JF_DEV int edge(int t) const {
+    constexpr int N = Vec<T>::N;
+    const int tail = head + n_vec * N + t - N;
+    return t < N ? (t < head ? t : -1) : (t < 2 * N && tail < V ? tail : -1);
   }
+  JF_DEV bool has_edges() const { return n_vec * Vec<T>::N < V; }
 };
 
-// The n largest of buf[0 .. count) (n <= 64, distinct keys but for 0), in falling order into buf[0 .. n), zeros after
-// the last; returns the n'th. By one whole warp. CAP: most entries.
-template <int CAP>
-JF_DEV unsigned long long lp_cut(unsigned long long* buf, int count, int n) {
-  constexpr int R = CAP / 32;
-  const int lane = threadIdx.x & 31;
+// The largest float below v (v itself at -infinity).
+JF_DEV float lp_below(float v) {
+  if (v == 0.f) return -1.4e-45f;
+  const int b = __float_as_int(v);
+  return v == -INFINITY ? v : __int_as_float(v > 0.f ? b - 1 : b + 1);
+}
+
+// The n largest of buf[0 .. count) (count <= LP_BUF, distinct keys but for zeros) in falling order into buf[0 .. n), zeros after the
+// last: a key's place is the number of larger ones. By the whole CTA, buf ready.
+JF_DEV void lp_cut_cta(unsigned long long* buf, int count, int n) {
+  constexpr int R = LP_BUF / LP_THREADS;
   unsigned long long e[R];
-  __syncwarp();
+  int place[R];
 #pragma unroll
-  for (int i = 0; i < R; ++i) e[i] = i * 32 + lane < count ? buf[i * 32 + lane] : 0ull;
-  __syncwarp();
-  unsigned long long best = 0;
-  for (int k = 0; k < n; ++k) {
-    unsigned long long v = 0;
-#pragma unroll
-    for (int i = 0; i < R; ++i) v = e[i] > v ? e[i] : v;
-    const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32));
-    const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
-    best = (unsigned long long)hi << 32 | lo;
-    if (lane == 0) buf[k] = best;
-#pragma unroll
-    for (int i = 0; i < R; ++i) e[i] = e[i] == best ? 0ull : e[i];
+  for (int k = 0; k < R; ++k) {
+    const int i = threadIdx.x + k * LP_THREADS;
+    e[k] = i < count ? buf[i] : 0ull;
+    place[k] = 0;
   }
-  __syncwarp();
-  return best;
+  for (int i = 0; i < count; ++i) {
+    const unsigned long long o = buf[i];
+#pragma unroll
+    for (int k = 0; k < R; ++k) place[k] += o > e[k];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += LP_THREADS) buf[i] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < R; ++k)
+    if (e[k] && place[k] < n) buf[place[k]] = e[k];
+  __syncthreads();
+}
+
+// x - m, x * c and sums on two values at a time.
+struct F2 {
+  float x, y;
+};
+JF_DEV F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+JF_DEV F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+JF_DEV F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\t"
+      "mov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
 }
 
 struct LpParams {
@@ -187,13 +219,20 @@ JF_DEV void lp_finish(const LpParams& a, int row, const LpStat& st, const unsign
   }
 }
 
+// A CTA's candidates.
+struct LpTop {
+  unsigned long long buf[LP_BUF];
+  int count;
+};
+
 // CTA (row, segment). TOP: a list is asked for.
 template <typename T, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS) k_logprobs(const LpParams a) {
+__global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
   constexpr int N = Vec<T>::N;
-  constexpr int U = 4;  // vectors in flight per thread
-  __shared__ unsigned long long s_buf[TOP ? LP_WARPS : 1][TOP ? LP_BUF : 1];
-  __shared__ int s_count[LP_WARPS];
+  constexpr int U = sizeof(T) == 2 ? 2 : 4;  // vectors a thread takes at a time
+  __shared__ LpTop top;
+  __shared__ unsigned long long first[TOP ? LP_THREADS : 1];
+  __shared__ float s_bound;
   __shared__ LpStat s_stat[LP_WARPS];
   pdl_launch_dependents();
   pdl_wait();
@@ -202,92 +241,143 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs(const LpParams a) {
   const Row<T> r(reinterpret_cast<const T*>(a.logits) + row * a.ld, a.V);
   const int v_begin = (int)((long long)r.n_vec * seg / a.segs), v_end = (int)((long long)r.n_vec * (seg + 1) / a.segs);
   const float c = a.scale * LOG2E;
-  float m = -INFINITY, s = 0.f, t = 0.f;
+  float m = -INFINITY;
+  F2 s = {0.f, 0.f}, t = {0.f, 0.f};
   unsigned long long thr = 0;  // the n_top'th best key so far
-  float thr_v = -INFINITY;
-  if (TOP && lane == 0) s_count[warp] = 0;
-  if (TOP) __syncwarp();
-  for (int v0 = v_begin + warp * 32; v0 < v_end; v0 += LP_THREADS * U) {
-    float x[U][N];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = v0 + u * LP_THREADS + lane;
-      r.load(v, v < v_end, x[u]);
+  float thr_v = -INFINITY;     // candidates exceed it
+  if (TOP && tid == 0) top.count = 0;
+  if (TOP) __syncthreads();
+
+  auto raise = [&](float mx) {  // the thread's maximum
+    if (mx > m) {
+      if (m > -INFINITY) {  // (before the first number the sums are 0, or NaN)
+        const float d = m - mx, al = ex2_ftz(d * c), dd = fmaxf(d, -1e30f);
+        t = {al * fmaf(dd, s.x, t.x), al * fmaf(dd, s.y, t.y)};
+        s = {al * s.x, al * s.y};
+      }
+      m = mx;
     }
+  };
+  auto add = [&](F2 x, float base) {
+    const F2 d = add2(x, {base, base});
+    F2 e = mul2(d, {c, c});
+    e = {ex2_ftz(e.x), ex2_ftz(e.y)};
+    s = add2(s, e);
+    t = fma2(e, {fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)}, t);  // (0 where x = -inf)
+  };
+  auto cut = [&]() {  // by the whole CTA, all candidates in place
+    const int count = top.count;
+    lp_cut_cta(top.buf, count, a.n_top);
+    if (tid == 0) top.count = min(count, a.n_top);
+    thr = top.buf[a.n_top - 1];
+    if (thr) thr_v = fmaxf(thr_v, lp_below(lp_key_value(thr)));  // (an equal value of a lower index may still come)
+    __syncthreads();
+  };
+  // M values of each thread, index(i) that of x[i]; some thread has one above thr_v
+  auto offer = [&](const auto& x, auto index, auto m_const) {
+    constexpr int M = decltype(m_const)::value;
+    const int before = top.count;
+    __syncthreads();
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float mx = x[u][0];
-#pragma unroll
-      for (int i = 1; i < N; ++i) mx = fmaxf(mx, x[u][i]);
-      if (TOP && __any_sync(0xffffffffu, mx > thr_v)) {
-        const long long e0 = r.first(v0 + u * LP_THREADS + lane);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          if (x[u][i] > thr_v) {
-            const unsigned long long key = lp_key(x[u][i], (int)(e0 + i));
-            if (key > thr) s_buf[warp][atomicAdd(&s_count[warp], 1)] = key;
-          }
+    for (int i = 0; i < M; ++i) {
+      if (x[i] > thr_v) {
+        const unsigned long long key = lp_key(x[i], index(i));
+        if (key > thr) {
+          const int at = atomicAdd(&top.count, 1);
+          if (at < LP_BUF) top.buf[at] = key;
         }
-        __syncwarp();
-        const int count = s_count[warp];
-        if (count > LP_BUF - 32 * N) {
-          thr = lp_cut<LP_BUF>(s_buf[warp], count, a.n_top);
-          thr_v = thr ? lp_key_value(thr) : -INFINITY;
-          if (lane == 0) s_count[warp] = min(count, a.n_top);
-          __syncwarp();
-        }
-      }
-      if (mx > m) {
-        if (m > -INFINITY) {  // (before the first number the sums are 0, or NaN)
-          const float d = m - mx, al = ex2_ftz(d * c);
-          t = al * fmaf(fmaxf(d, -1e30f), s, t);
-          s = al * s;
-        }
-        m = mx;
-      }
-      const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float d = x[u][i] - base, e = ex2_ftz(d * c);
-        s += e;
-        t = fmaf(e, fmaxf(d, -1e30f), t);  // (0 where x = -inf)
       }
     }
+    __syncthreads();
+    if (top.count > LP_BUF) {  // more than fit (a row that climbs): one value of each thread at a time
+      __syncthreads();
+      if (tid == 0) top.count = before;
+      __syncthreads();
+#pragma unroll 1
+      for (int i = 0; i < M; ++i) {
+        if (top.count > LP_BUF - LP_THREADS) cut();
+        float xi = x[0];
+#pragma unroll
+        for (int k = 1; k < M; ++k)
+          if (i == k) xi = x[k];
+        const unsigned long long key = lp_key(xi, index(i));
+        if (xi > thr_v && key > thr) top.buf[atomicAdd(&top.count, 1)] = key;
+        __syncthreads();
+      }
+    }
+    if (top.count > LP_BUF / 2) cut();
+  };
+
+  if (r.has_edges()) {
+    const int e = r.edge(tid);
+    const bool mine = e >= 0 && seg == (tid < N ? 0 : a.segs - 1);
+    const float x[1] = {mine ? act_to_f32(r.p[e]) : -INFINITY};
+    if (TOP && __syncthreads_or(x[0] > thr_v)) offer(x, [&](int) { return e; }, std::integral_constant<int, 1>{});
+    raise(x[0]);
+    if (mine) add({x[0], -INFINITY}, m == -INFINITY ? 0.f : -m);
   }
-  LpStat st = {m, s, t};
+  bool bound = TOP;  // a first bound is to be taken
+  for (int v0 = v_begin; v0 < v_end; v0 += LP_THREADS * U) {
+    float x[U * N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int v = v0 + u * LP_THREADS + tid;
+      float(&xu)[N] = *reinterpret_cast<float(*)[N]>(x + u * N);
+      if (v < v_end) {
+        Vec<T>::load(r.vec(v), xu);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) xu[i] = -INFINITY;
+      }
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < U * N; ++i) mx = fmaxf(mx, x[i]);
+    if (TOP) {
+      if (bound) {  // n_top logits are at least the n_top'th largest of the threads' maxima
+        bound = false;
+        first[tid] = mx > -INFINITY ? lp_key(mx, tid) : 0ull;
+        if (tid == 0) s_bound = -INFINITY;
+        __syncthreads();
+        const unsigned long long mine = first[tid];
+        int larger = 0;
+        for (int i = 0; i < LP_THREADS; ++i) larger += first[i] > mine;
+        if (mine && larger == a.n_top - 1) s_bound = lp_below(mx);
+        __syncthreads();
+        thr_v = fmaxf(thr_v, s_bound);
+      }
+      if (__syncthreads_or(mx > thr_v))
+        offer(x, [&](int i) { return r.head + (v0 + i / N * LP_THREADS + tid) * N + i % N; }, std::integral_constant<int, U * N>{});
+    }
+    raise(mx);
+    const float base = m == -INFINITY ? 0.f : -m;
+#pragma unroll
+    for (int i = 0; i < U * N; i += 2) add({x[i], x[i + 1]}, base);
+  }
+  LpStat st = {m, s.x + s.y, t.x + t.y};
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     LpStat b = {__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.t, o)};
     st = lane & o ? lp_join(b, st, c) : lp_join(st, b, c);
   }
   if (lane == 0) s_stat[warp] = st;
-  if (TOP) lp_cut<LP_BUF>(s_buf[warp], s_count[warp], a.n_top);
   __syncthreads();
-  if (warp == 0) {
-    st = s_stat[0];
-    for (int w = 1; w < LP_WARPS; ++w) st = lp_join(st, s_stat[w], c);
-    if (TOP) {  // the warps' lists, one after the other (8 x 64 at most)
-      unsigned long long* all = s_buf[0];
-      for (int w = 1; w < LP_WARPS; ++w)
-        for (int k = lane; k < a.n_top; k += 32) all[w * a.n_top + k] = s_buf[w][k];
-      lp_cut<LP_BUF>(all, LP_WARPS * a.n_top, a.n_top);
-    }
-    if (lane == 0) s_stat[0] = st;
-  }
-  __syncthreads();
+  if (TOP) cut();
+  st = s_stat[0];
+  for (int w = 1; w < LP_WARPS; ++w) st = lp_join(st, s_stat[w], c);
   if (a.segs == 1) {
-    lp_finish<T>(a, row, s_stat[0], s_buf[0], tid);
+    lp_finish<T>(a, row, st, top.buf, tid);
   } else {
-    if (tid == 0) a.stats[blockIdx.x] = make_float4(s_stat[0].m, s_stat[0].s, s_stat[0].t, 0.f);
+    if (tid == 0) a.stats[blockIdx.x] = make_float4(st.m, st.s, st.t, 0.f);
     if (TOP)
-      for (int k = tid; k < a.n_top; k += LP_THREADS) a.lists[(long long)blockIdx.x * a.n_top + k] = s_buf[0][k];
+      for (int k = tid; k < a.n_top; k += LP_THREADS) a.lists[(long long)blockIdx.x * a.n_top + k] = top.buf[k];
   }
 }
 
 // Joins a row's segments: one CTA a row.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(LP_THREADS) k_logprobs_join(const LpParams a) {
-  __shared__ unsigned long long s_buf[TOP ? LP_WARPS : 1][TOP ? LP_BUF : 1];
+  __shared__ unsigned long long s_buf[LP_BUF];
   __shared__ LpStat s_stat;
   pdl_launch_dependents();
   pdl_wait();
@@ -306,31 +396,19 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_join(const LpParams a) 
     }
     if (lane == 0) s_stat = st;
   }
-  if (TOP) {
-    // a warp takes every 8th run of LP_BUF - 64 entries
+  if (TOP) {  // the segments' lists, as many at a time as fit
     const unsigned long long* list = a.lists + (long long)row * a.segs * a.n_top;
     const int total = a.segs * a.n_top;
-    constexpr int RUN = LP_BUF - 64;
-    int have = 0;
-    for (int i0 = warp * RUN; i0 < total; i0 += LP_WARPS * RUN) {
-      const int n = min(RUN, total - i0);
-      __syncwarp();
-      for (int i = lane; i < n; i += 32) s_buf[warp][have + i] = list[i0 + i];
-      lp_cut<LP_BUF>(s_buf[warp], have + n, a.n_top);
-      have = a.n_top;
+    for (int i0 = 0, have = 0; i0 < total; have = a.n_top) {
+      const int n = min(LP_BUF - have, total - i0);
+      for (int i = tid; i < n; i += LP_THREADS) s_buf[have + i] = list[i0 + i];
+      __syncthreads();
+      lp_cut_cta(s_buf, have + n, a.n_top);
+      i0 += n;
     }
-    if (!have)
-      for (int i = lane; i < a.n_top; i += 32) s_buf[warp][i] = 0;
   }
   __syncthreads();
-  if (TOP && warp == 0) {
-    unsigned long long* all = s_buf[0];
-    for (int w = 1; w < LP_WARPS; ++w)
-      for (int k = lane; k < a.n_top; k += 32) all[w * a.n_top + k] = s_buf[w][k];
-    lp_cut<LP_BUF>(all, LP_WARPS * a.n_top, a.n_top);
-  }
-  __syncthreads();
-  lp_finish<T>(a, row, s_stat, s_buf[0], tid);
+  lp_finish<T>(a, row, s_stat, s_buf, tid);
 }
 
 struct LpGradParams {
@@ -346,7 +424,7 @@ struct LpGradParams {
 
 constexpr int LP_GRAD_VECS = 4;  // vectors per thread
 
-// CTA (row, run of LP_GRAD_VECS x 256 vectors).
+// CTA (row, run of LP_GRAD_VECS x 256 vectors); the first run's CTA takes the row's edges too.
 template <typename T>
 __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams a) {
   constexpr int N = Vec<T>::N;
@@ -364,29 +442,34 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams
     g = 0.f;
   }
   const bool none = m == -INFINITY && ls == -INFINITY;
+  auto of = [&](float x, int i) {
+    const float lp = fmaf(x - m, a.scale, -ls), p = ex2_ftz(lp * LOG2E);
+    // -g p - gh p (lp + H), the logit of probability 0 without its infinite lp
+    const float share = g + gh * (fmaxf(lp, -1e4f) + H);
+    return none ? 0.f : a.scale * ((i == target ? g : 0.f) - p * share);
+  };
   float x[LP_GRAD_VECS][N];
   const int v0 = seg * (LP_GRAD_VECS * LP_THREADS) + threadIdx.x;
 #pragma unroll
-  for (int u = 0; u < LP_GRAD_VECS; ++u) r.load(v0 + u * LP_THREADS, v0 + u * LP_THREADS < r.n_vec, x[u]);
+  for (int u = 0; u < LP_GRAD_VECS; ++u)
+    if (v0 + u * LP_THREADS < r.n_vec) Vec<T>::load(r.vec(v0 + u * LP_THREADS), x[u]);
+  if (seg == 0) {
+    const int e = r.edge(threadIdx.x);
+    if (e >= 0) out[e] = to_act<T>(of(act_to_f32(r.p[e]), e));
+  }
 #pragma unroll
   for (int u = 0; u < LP_GRAD_VECS; ++u) {
     const int v = v0 + u * LP_THREADS;
     if (v >= r.n_vec) break;
-    const long long e0 = r.first(v);
+    const int e0 = r.head + v * N;
     float d[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float lp = fmaf(x[u][i] - m, a.scale, -ls), p = ex2_ftz(lp * LOG2E);
-      // -g p - gh p (lp + H), the logit of probability 0 without its infinite lp
-      const float share = g + gh * (fmaxf(lp, -1e4f) + H);
-      d[i] = none ? 0.f : a.scale * ((e0 + i == target ? g : 0.f) - p * share);
-    }
-    if (same && r.whole(v)) {
+    for (int i = 0; i < N; ++i) d[i] = of(x[u][i], e0 + i);
+    if (same) {
       Vec<T>::store(out + e0, d);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (e0 + i >= 0 && e0 + i < a.V) out[e0 + i] = to_act<T>(d[i]);
+      for (int i = 0; i < N; ++i) out[e0 + i] = to_act<T>(d[i]);
     }
   }
 }
@@ -472,7 +555,7 @@ extern "C" jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, lo
   if (grad_logits == logits && ld_grad != ld) return JF_EINVAL;
   const int n = dtype == JF_BF16 ? Vec<bf16>::N : Vec<float>::N;
   const int per_cta = LP_GRAD_VECS * LP_THREADS * n;
-  const int segs = (int)(((long long)vocab + n - 1 + per_cta - 1) / per_cta);  // (a row may begin n - 1 elements into a vector)
+  const int segs = (vocab + per_cta - 1) / per_cta;
   const LpGradParams a = {logits, ld, ld_grad, rows, vocab, segs, scale, targets, row_stats, entropy, grad_logprob, grad_entropy,
                           grad_logits, err_word};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
