@@ -19,7 +19,7 @@ namespace jf {
 namespace {
 
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
-constexpr int LP_BUF = 512;         // candidates a CTA holds; of a warp that joins segments
+constexpr int LP_BUF = 2 * LP_THREADS;         // candidates a CTA holds; of a warp that joins segments
 constexpr int LP_SEG_MIN = 4096;    // fewest logits of a segment
 constexpr int LP_CTAS = 608;        // CTAs that fill the GPU (152 SMs x 4)
 constexpr float LOG2E = 1.4426950408889634f;
@@ -134,10 +134,16 @@ JF_DEV void lp_cut_cta(unsigned long long* buf, int count, int n) {
     e[k] = i < count ? buf[i] : 0ull;
     place[k] = 0;
   }
-  for (int i = 0; i < count; ++i) {
-    const unsigned long long o = buf[i];
-#pragma unroll
-    for (int k = 0; k < R; ++k) place[k] += o > e[k];
+  if (__any_sync(0xffffffffu, e[1] != 0)) {
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) {
+      const unsigned long long o = buf[i];
+      place[0] += o > e[0];
+      place[1] += o > e[1];
+    }
+  } else if (__any_sync(0xffffffffu, e[0] != 0)) {  // (warps without a key have nothing to place)
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) place[0] += buf[i] > e[0];
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += LP_THREADS) buf[i] = 0;
@@ -231,8 +237,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
   constexpr int N = Vec<T>::N;
   constexpr int U = sizeof(T) == 2 ? 2 : 4;  // vectors a thread takes at a time
   __shared__ LpTop top;
-  __shared__ unsigned long long first[TOP ? LP_THREADS : 1];
-  __shared__ float s_bound;
+  __shared__ int s_first;
   __shared__ LpStat s_stat[LP_WARPS];
   pdl_launch_dependents();
   pdl_wait();
@@ -245,6 +250,9 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
   F2 s = {0.f, 0.f}, t = {0.f, 0.f};
   unsigned long long thr = 0;  // the n_top'th best key so far
   float thr_v = -INFINITY;     // candidates exceed it
+  // A cut costs the square of what it looks at; each tightens the bound: at twice the list, a row of random logits has
+  // about five.
+  const int cut_at = a.n_top + max(a.n_top, 32);
   if (TOP && tid == 0) top.count = 0;
   if (TOP) __syncthreads();
 
@@ -273,25 +281,31 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
     if (thr) thr_v = fmaxf(thr_v, lp_below(lp_key_value(thr)));  // (an equal value of a lower index may still come)
     __syncthreads();
   };
-  // M values of each thread, index(i) that of x[i]; some thread has one above thr_v
-  auto offer = [&](const auto& x, auto index, auto m_const) {
+  // M values of each thread, index(i) that of x[i]; by the whole CTA. One barrier where nothing special happens: after
+  // it candidates of the next call may already arrive, so what it decides goes by the places that threads were given.
+  auto offer = [&](const auto& x, float mx, auto index, auto m_const) {
     constexpr int M = decltype(m_const)::value;
-    const int before = top.count;
-    __syncthreads();
+    int first_at = LP_BUF, last_at = -1;
+    if (mx > thr_v) {
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-      if (x[i] > thr_v) {
-        const unsigned long long key = lp_key(x[i], index(i));
-        if (key > thr) {
-          const int at = atomicAdd(&top.count, 1);
-          if (at < LP_BUF) top.buf[at] = key;
+      for (int i = 0; i < M; ++i) {
+        if (x[i] > thr_v) {
+          const unsigned long long key = lp_key(x[i], index(i));
+          if (key > thr) {
+            last_at = atomicAdd(&top.count, 1);
+            first_at = min(first_at, last_at);
+            if (last_at < LP_BUF) top.buf[last_at] = key;
+          }
         }
       }
     }
-    __syncthreads();
-    if (top.count > LP_BUF) {  // more than fit (a row that climbs): one value of each thread at a time
+    if (!__syncthreads_or(last_at >= cut_at)) return;
+    if (top.count > LP_BUF) {  // more than fit (a row that climbs): again, one value of each thread at a time
+      if (tid == 0) s_first = LP_BUF;
       __syncthreads();
-      if (tid == 0) top.count = before;
+      atomicMin(&s_first, first_at);
+      __syncthreads();
+      if (tid == 0) top.count = s_first;
       __syncthreads();
 #pragma unroll 1
       for (int i = 0; i < M; ++i) {
@@ -301,18 +315,19 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
         for (int k = 1; k < M; ++k)
           if (i == k) xi = x[k];
         const unsigned long long key = lp_key(xi, index(i));
+        __syncthreads();
         if (xi > thr_v && key > thr) top.buf[atomicAdd(&top.count, 1)] = key;
         __syncthreads();
       }
     }
-    if (top.count > LP_BUF / 2) cut();
+    cut();
   };
 
   if (r.has_edges()) {
     const int e = r.edge(tid);
     const bool mine = e >= 0 && seg == (tid < N ? 0 : a.segs - 1);
     const float x[1] = {mine ? act_to_f32(r.p[e]) : -INFINITY};
-    if (TOP && __syncthreads_or(x[0] > thr_v)) offer(x, [&](int) { return e; }, std::integral_constant<int, 1>{});
+    if (TOP) offer(x, x[0], [&](int) { return e; }, std::integral_constant<int, 1>{});
     raise(x[0]);
     if (mine) add({x[0], -INFINITY}, m == -INFINITY ? 0.f : -m);
   }
@@ -334,20 +349,20 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
 #pragma unroll
     for (int i = 1; i < U * N; ++i) mx = fmaxf(mx, x[i]);
     if (TOP) {
-      if (bound) {  // n_top logits are at least the n_top'th largest of the threads' maxima
+      if (bound) {  // n_top logits are at least a value that n_top of the threads' maxima reach: a close one by bisection
         bound = false;
-        first[tid] = mx > -INFINITY ? lp_key(mx, tid) : 0ull;
-        if (tid == 0) s_bound = -INFINITY;
-        __syncthreads();
-        const unsigned long long mine = first[tid];
-        int larger = 0;
-        for (int i = 0; i < LP_THREADS; ++i) larger += first[i] > mine;
-        if (mine && larger == a.n_top - 1) s_bound = lp_below(mx);
-        __syncthreads();
-        thr_v = fmaxf(thr_v, s_bound);
+        const uint32_t mine = mx > -INFINITY ? (uint32_t)(lp_key(mx, 0) >> 32) : 0u;
+        uint32_t lo = 0u, hi = 0xffffffffu;
+        for (int k = 0; k < 32; ++k) {
+          const uint32_t mid = lo + (hi - lo) / 2 + 1;
+          const int n = __syncthreads_count(mine >= mid);
+          if (n >= a.n_top) lo = mid;
+          else hi = mid - 1;
+          if (lo == hi || (n >= a.n_top && n <= a.n_top + a.n_top / 4)) break;
+        }
+        if (lo > 0u) thr_v = fmaxf(thr_v, lp_below(lp_key_value((unsigned long long)lo << 32)));
       }
-      if (__syncthreads_or(mx > thr_v))
-        offer(x, [&](int i) { return r.head + (v0 + i / N * LP_THREADS + tid) * N + i % N; }, std::integral_constant<int, U * N>{});
+      offer(x, mx, [&](int i) { return r.head + (v0 + i / N * LP_THREADS + tid) * N + i % N; }, std::integral_constant<int, U * N>{});
     }
     raise(mx);
     const float base = m == -INFINITY ? 0.f : -m;
@@ -377,7 +392,8 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
 // Joins a row's segments: one CTA a row.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(LP_THREADS) k_logprobs_join(const LpParams a) {
-  __shared__ unsigned long long s_buf[LP_BUF];
+  __shared__ unsigned long long s_buf[LP_BUF], s_bound;
+  __shared__ int s_count;
   __shared__ LpStat s_stat;
   pdl_launch_dependents();
   pdl_wait();
@@ -396,15 +412,34 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_join(const LpParams a) 
     }
     if (lane == 0) s_stat = st;
   }
-  if (TOP) {  // the segments' lists, as many at a time as fit
+  if (TOP) {
+    // The n_top best keys are among those that reach the largest of the lists' last keys; where these do not fit, the
+    // lists go in runs.
     const unsigned long long* list = a.lists + (long long)row * a.segs * a.n_top;
     const int total = a.segs * a.n_top;
-    for (int i0 = 0, have = 0; i0 < total; have = a.n_top) {
-      const int n = min(LP_BUF - have, total - i0);
-      for (int i = tid; i < n; i += LP_THREADS) s_buf[have + i] = list[i0 + i];
-      __syncthreads();
-      lp_cut_cta(s_buf, have + n, a.n_top);
-      i0 += n;
+    if (tid == 0) s_bound = 0, s_count = 0;
+    __syncthreads();
+    for (int i = tid; i < a.segs; i += LP_THREADS) atomicMax(&s_bound, list[(long long)i * a.n_top + a.n_top - 1]);
+    __syncthreads();
+    const unsigned long long bound = max(s_bound, 1ull);
+    for (int i = tid; i < total; i += LP_THREADS) {
+      const unsigned long long key = list[i];
+      if (key >= bound) {
+        const int at = atomicAdd(&s_count, 1);
+        if (at < LP_BUF) s_buf[at] = key;
+      }
+    }
+    __syncthreads();
+    if (s_count <= LP_BUF) {
+      lp_cut_cta(s_buf, s_count, a.n_top);
+    } else {
+      for (int i0 = 0, have = 0; i0 < total; have = a.n_top) {
+        const int n = min(LP_BUF - have, total - i0);
+        for (int i = tid; i < n; i += LP_THREADS) s_buf[have + i] = list[i0 + i];
+        __syncthreads();
+        lp_cut_cta(s_buf, have + n, a.n_top);
+        i0 += n;
+      }
     }
   }
   __syncthreads();
