@@ -63,10 +63,11 @@ struct Vec;
 template <>
 struct Vec<float> {
   static constexpr int N = 4;
-  static JF_DEV void load(const float* p, float (&x)[4]) {
-    const float4 v = __ldcs(reinterpret_cast<const float4*>(p));
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  static JF_DEV uint4 raw(const float* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
+  static JF_DEV void unpack(uint4 v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
   }
+  static JF_DEV uint4 nothing() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }  // -infinities
   static JF_DEV void store(float* p, const float (&x)[4]) {
     __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
   }
@@ -74,8 +75,9 @@ struct Vec<float> {
 template <>
 struct Vec<bf16> {
   static constexpr int N = 8;
-  static JF_DEV void load(const bf16* p, float (&x)[8]) {
-    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
+  static JF_DEV uint4 raw(const bf16* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
+  static JF_DEV uint4 nothing() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }  // -infinities
+  static JF_DEV void unpack(uint4 v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -332,19 +334,20 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
     if (mine) add({x[0], -INFINITY}, m == -INFINITY ? 0.f : -m);
   }
   bool bound = TOP;  // a first bound is to be taken
-  for (int v0 = v_begin; v0 < v_end; v0 += LP_THREADS * U) {
-    float x[U * N];
+  uint4 next[U];     // the next round's vectors are on their way while one is worked on
+  auto ask = [&](int v0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int v = v0 + u * LP_THREADS + tid;
-      float(&xu)[N] = *reinterpret_cast<float(*)[N]>(x + u * N);
-      if (v < v_end) {
-        Vec<T>::load(r.vec(v), xu);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) xu[i] = -INFINITY;
-      }
+      next[u] = v < v_end ? Vec<T>::raw(r.vec(v)) : Vec<T>::nothing();
     }
+  };
+  ask(v_begin);
+  for (int v0 = v_begin; v0 < v_end; v0 += LP_THREADS * U) {
+    float x[U * N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) Vec<T>::unpack(next[u], *reinterpret_cast<float(*)[N]>(x + u * N));
+    ask(v0 + LP_THREADS * U);
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < U * N; ++i) mx = fmaxf(mx, x[i]);
@@ -487,7 +490,7 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams
   const int v0 = seg * (LP_GRAD_VECS * LP_THREADS) + threadIdx.x;
 #pragma unroll
   for (int u = 0; u < LP_GRAD_VECS; ++u)
-    if (v0 + u * LP_THREADS < r.n_vec) Vec<T>::load(r.vec(v0 + u * LP_THREADS), x[u]);
+    if (v0 + u * LP_THREADS < r.n_vec) Vec<T>::unpack(Vec<T>::raw(r.vec(v0 + u * LP_THREADS)), x[u]);
   if (seg == 0) {
     const int e = r.edge(threadIdx.x);
     if (e >= 0) out[e] = to_act<T>(of(act_to_f32(r.p[e]), e));
