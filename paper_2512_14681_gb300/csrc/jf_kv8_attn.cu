@@ -1081,33 +1081,51 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L), unit = pow2i(Em);
       const uint32_t t_first = two ? t_o : t_row + 256;
       const bool second = !two && n > 1;  // (a stream without a step holds nothing)
+      // A state leaves through shared memory (32 rows x 32 dims a warp, 16-byte pieces swizzled, in the upper half of the
+      // stream's queries' place), so that a row's pieces are written side by side.
+      const uint32_t turn_buf = sQ + (uint32_t)(s * Lay::Q + Lay::Q / 2 + (warp & 3) * 4096);
 #pragma unroll 1
-      for (int d = d0; d < d1; d += 16) {
-        float x[16], y[16];
-        tmem_ld16(t_first + d, x);
-        if (second) tmem_ld16(t_row + 384 + d, y);
-        if (live) {
+      for (int d = d0; d < d1; d += 32) {
+        float x[32], y[32];
+        tmem_ld32(t_first + d, x);
+        if (second) tmem_ld32(t_row + 384 + d, y);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float v = w0 == 0.f ? 0.f : w0 * x[i];
-            if (second && w1 != 0.f) v = fmaf(w1, y[i], v);
-            x[i] = v * il * unit;
-          }
-          if (whole) {
-            uint32_t u[8];
+        for (int i = 0; i < 32; ++i) {
+          float v = w0 == 0.f ? 0.f : w0 * x[i];
+          if (second && w1 != 0.f) v = fmaf(w1, y[i], v);
+          x[i] = v * il * unit;
+        }
+        if (whole) {
+          if (live) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-              u[i] = *reinterpret_cast<const uint32_t*>(&v);
+            for (int h = 0; h < 4; ++h) {
+              uint32_t u[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(x[8 * h + 2 * i], x[8 * h + 2 * i + 1]);
+                u[i] = *reinterpret_cast<const uint32_t*>(&v);
+              }
+              reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at * HD + d)[h] = make_uint4(u[0], u[1], u[2], u[3]);
             }
-            uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at * HD + d);
-            dst[0] = make_uint4(u[0], u[1], u[2], u[3]);
-            dst[1] = make_uint4(u[4], u[5], u[6], u[7]);
-          } else {
-            float4* dst = reinterpret_cast<float4*>(st + r * HD + d);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) dst[i] = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
           }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 8; ++h)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn_buf + lane * 128 + ((h ^ (lane & 7)) << 4)), "f"(x[4 * h]),
+                         "f"(x[4 * h + 1]), "f"(x[4 * h + 2]), "f"(x[4 * h + 3])
+                         : "memory");
+          __syncwarp();
+#pragma unroll
+          for (int h = 0; h < 8; ++h) {
+            const int rl = 4 * h + (lane >> 3), rt = (two ? s * 128 : 0) + (warp & 3) * 32 + rl;
+            float4 v;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                         : "r"(turn_buf + rl * 128 + (((lane & 7) ^ (rl & 7)) << 4))
+                         : "memory");
+            if (rt < rows) reinterpret_cast<float4*>(st + rt * HD + d)[lane & 7] = v;
+          }
+          __syncwarp();
         }
       }
       if (live && d0 == 0) {
@@ -1286,7 +1304,7 @@ cudaError_t launch_combine(const Kv8AttnParams& a, int workers, cudaStream_t st)
   const long long states = workers / (tiles * a.c.n_kv_heads);
   if (states > 192 && rows < 0x7fffffff)
     return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 16>, dim3((unsigned)rows), dim3(512), 0, st, a, workers);
-  if (states > 48) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, st, a, workers);
+  if (states > 16) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, st, a, workers);
   return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a, workers);
 }
 
