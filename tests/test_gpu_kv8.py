@@ -606,3 +606,51 @@ def test_refusals(torch):
     assert c.lib.jf_op_kv8_attention(*args, need.value, None, None) == J.JF_EINVAL
     torch.cuda.synchronize()
     c.check()
+
+
+@pytest.mark.parametrize("spread", [0, 9, 25])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,hd,new,lens,masked", [
+    (28, 4, 128, [64], [20000], False),              # two row tiles, several chunks of keys a CTA
+    (28, 4, 128, [3, 64, 20], [9000, 20000, 130], False),  # units of one and of two tiles in one CTA's share
+    (12, 2, 128, [40, 21], [12001, 25000], True),
+    (8, 1, 64, [30, 100], [16383, 9000], False),
+    (28, 4, 128, [1, 1, 2], [40000, 17, 21111], False),
+])
+def test_many_chunks_a_share(torch, Hq, Hkv, hd, new, lens, masked, dtype, spread):
+    """Long contexts, so that every CTA walks through several chunks and units; values' exponents alike, or differing so much
+    that the pages of a chunk go in several steps. (No launch runs into the limit of a wait, which is 2 s.)"""
+    import time
+
+    totals = [a + n for a, n in zip(lens, new)]
+    pool = fill(torch, Hkv, hd, totals, seed=12, v_spread=spread)
+    q = queries(torch, sum(new), Hq, hd, dtype, 5, 0.5)
+    sees, mask = None, None
+    if masked:
+        rng = np.random.default_rng(6)
+        sees = [rng.random((n, n)) < 0.5 for n in new]
+        mask = torch.from_numpy(np.concatenate([tree_bits(s, 2) for s in sees])).cuda()
+    scale = hd ** -0.5
+    out = pool.cache.attention(rows_of(new, lens), q, scale, mask=mask)
+    torch.cuda.synchronize()
+    began = time.monotonic()
+    again = pool.cache.attention(rows_of(new, lens), q, scale, mask=mask)
+    pool.cache.check()
+    assert time.monotonic() - began < 1.0
+    assert torch.equal(out, again)
+    r = 0
+    for b, (a, n) in enumerate(zip(lens, new)):
+        pages = torch.from_numpy(pool.table[b, :-(-(a + n) // PAGE)].astype(np.int64)).cuda()
+        k, v = (((c[pages].view(torch.float8_e4m3fn).double() * 2.0 ** e[pages].double()[:, :, None, None]).transpose(1, 2).reshape(-1, Hkv, hd)[:a + n])
+                for c, e in ((pool.cache.k, pool.cache.k_exp), (pool.cache.v, pool.cache.v_exp)))
+        see = torch.ones(n, a + n, dtype=torch.bool, device="cuda")
+        see[:, a:] = torch.from_numpy(sees[b]).cuda() if masked else torch.ones(n, n, device="cuda").tril().bool()
+        for h in range(Hq):
+            kv, qh = h // (Hq // Hkv), q[r:r + n, h].double()
+            p = torch.softmax((qh @ k[:, kv].T * scale).masked_fill(~see, -float("inf")), -1)
+            ref, A = p @ v[:, kv], p @ v[:, kv].abs()
+            dS = (qh.abs() @ k[:, kv].abs().T).masked_fill(~see, 0).max(1).values * scale * hd * 2.0 ** -23
+            tol = (2 * dS + (2.0 ** -11 if dtype == "bf16" else 2.0 ** -20))[:, None] * A + (2.0 ** -8 * ref.abs() if dtype == "bf16" else 0)
+            off = (out[r:r + n, h].double() - ref).abs()
+            assert (off <= tol).all(), (b, h, float((off / tol).max()))
+        r += n
