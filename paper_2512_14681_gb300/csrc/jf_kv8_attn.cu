@@ -1164,14 +1164,14 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
   __shared__ float s_m[CB_WARPS], s_l[CB_WARPS], s_o[RW > 1 ? CB_WARPS : 1][HD];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % RW;
   pdl_launch_dependents();
-  const long long i = (long long)blockIdx.x * (CB_WARPS / RW) + warp / RW;
+  const uint32_t i = blockIdx.x * (CB_WARPS / RW) + warp / RW;  // (n_rows * n_heads is below 2^30)
   const int G = a.n_heads / a.c.n_kv_heads;
   // (a row's warps stay together: they meet at a barrier of their own)
-  if (i >= (long long)a.r.n_rows * a.n_heads) {
+  if (i >= (uint32_t)(a.r.n_rows * a.n_heads)) {
     pdl_wait();
     return;
   }
-  const int row = (int)(i / a.n_heads), head = (int)(i % a.n_heads);
+  const int row = (int)(i / (uint32_t)a.n_heads), head = (int)i - row * a.n_heads;
   // the sequence of the row
   int lo = 0, m = a.c.n_seqs;
   while (m > 1) {
@@ -1287,24 +1287,25 @@ __global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv
     M = mn;
     L = Ln;
   }
-  T* dst = reinterpret_cast<T*>(a.out) + i * HD + D * lane;
+  T* dst = reinterpret_cast<T*>(a.out) + (long long)i * HD + D * lane;
 #pragma unroll
   for (int j = 0; j < D; j += 2) store2(dst + j, o[j], o[j + 1]);
   if (a.lse && lane == 0) a.lse[i] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
 // Warps a row, by the states that a row may have (workers over units, of which there are at least the tiles of all rows
-// together for each KV head): what a warp does before its first state costs as much as 30 states, so a second one
-// pays late. One 7B draft of 32 rows over 32,768 tokens (up to 38 states a row), all of the attention: 47.1 us with 4
-// warps a row, 55.7 with 16, 40.3 with one.
+// together for each KV head): what a warp does before its first state costs as much as some 30 states, so more than one
+// pays where states are many and rows few. All of the attention, us with 1 / 4 / 8 / 16 warps a row: 28 rows (heads of
+// one token) of up to 304 states 49.5 / 23.5 / 19.2 / 21.6 over 32,768 tokens, 12.7 / 9.7 / 9.9 / 11.1 over 1,024; 448 rows of up to 43
+// 50.4 / 47.4; 896 rows of up to 38 17.9 / 20.4 over 128 tokens, 40.1 / 40.3 over 32,768.
 template <typename T, int HD, int TR, int CH, int UC>
 cudaError_t launch_combine(const Kv8AttnParams& a, int workers, cudaStream_t st) {
   const long long rows = (long long)a.r.n_rows * a.n_heads, group_rows = (long long)a.r.n_rows * (a.n_heads / a.c.n_kv_heads);
   const long long tiles = (group_rows + TR - 1) / TR;
   const long long states = workers / (tiles * a.c.n_kv_heads);
-  if (states > 192 && rows < 0x7fffffff)
-    return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 16>, dim3((unsigned)rows), dim3(512), 0, st, a, workers);
-  if (states > 16) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, st, a, workers);
+  if (states > 192)
+    return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 8>, dim3((unsigned)rows), dim3(256), 0, st, a, workers);
+  if (states > 16 && rows <= 512) return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 4>, dim3((unsigned)((rows + 1) / 2)), dim3(256), 0, st, a, workers);
   return kv8_launch(k_kv8_combine<T, HD, TR, CH, UC, 1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a, workers);
 }
 
