@@ -1081,16 +1081,25 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L), unit = pow2i(Em);
       const uint32_t t_first = two ? t_o : t_row + 256;
       const bool second = !two && n > 1;  // (a stream without a step holds nothing)
-      // A state leaves through shared memory (32 rows x 32 dims a warp, 16-byte pieces swizzled, in the upper half of the
+      // A state leaves through shared memory (32 rows x DW dims a warp, 16-byte pieces swizzled, in the upper half of the
       // stream's queries' place), so that a row's pieces are written side by side.
-      const uint32_t turn_buf = sQ + (uint32_t)(s * Lay::Q + Lay::Q / 2 + (warp & 3) * 4096);
+      constexpr int DW = HD / 4, PW = DW / 4;  // dims at a time; pieces of a row
+      static_assert(4 * 32 * DW * 4 <= Lay::Q / 2, "four warps' pieces");
+      const uint32_t turn_buf = sQ + (uint32_t)(s * Lay::Q + Lay::Q / 2 + (warp & 3) * (32 * DW * 4));
+      auto place = [&](int row, int piece) {
+        return turn_buf + row * (DW * 4) + ((piece ^ (PW == 8 ? row & 7 : row >> 1 & 3)) << 4);
+      };
 #pragma unroll 1
-      for (int d = d0; d < d1; d += 32) {
-        float x[32], y[32];
-        tmem_ld32(t_first + d, x);
-        if (second) tmem_ld32(t_row + 384 + d, y);
+      for (int d = d0; d < d1; d += DW) {
+        float x[DW], y[DW];
+        if constexpr (DW == 32) tmem_ld32(t_first + d, x);
+        else tmem_ld16(t_first + d, x);
+        if (second) {
+          if constexpr (DW == 32) tmem_ld32(t_row + 384 + d, y);
+          else tmem_ld16(t_row + 384 + d, y);
+        }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < DW; ++i) {
           float v = w0 == 0.f ? 0.f : w0 * x[i];
           if (second && w1 != 0.f) v = fmaf(w1, y[i], v);
           x[i] = v * il * unit;
@@ -1098,7 +1107,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         if (whole) {
           if (live) {
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
+            for (int h = 0; h < PW / 2; ++h) {
               uint32_t u[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
@@ -1110,20 +1119,20 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           }
         } else {
 #pragma unroll
-          for (int h = 0; h < 8; ++h)
-            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn_buf + lane * 128 + ((h ^ (lane & 7)) << 4)), "f"(x[4 * h]),
-                         "f"(x[4 * h + 1]), "f"(x[4 * h + 2]), "f"(x[4 * h + 3])
+          for (int h = 0; h < PW; ++h)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(place(lane, h)), "f"(x[4 * h]), "f"(x[4 * h + 1]), "f"(x[4 * h + 2]),
+                         "f"(x[4 * h + 3])
                          : "memory");
           __syncwarp();
 #pragma unroll
-          for (int h = 0; h < 8; ++h) {
-            const int rl = 4 * h + (lane >> 3), rt = (two ? s * 128 : 0) + (warp & 3) * 32 + rl;
+          for (int h = 0; h < PW; ++h) {
+            const int rl = 32 / PW * h + lane / PW, rt = (two ? s * 128 : 0) + (warp & 3) * 32 + rl;
             float4 v;
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
                          : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                         : "r"(turn_buf + rl * 128 + (((lane & 7) ^ (rl & 7)) << 4))
+                         : "r"(place(rl, lane % PW))
                          : "memory");
-            if (rt < rows) reinterpret_cast<float4*>(st + rt * HD + d)[lane & 7] = v;
+            if (rt < rows) reinterpret_cast<float4*>(st + rt * HD + d)[lane % PW] = v;
           }
           __syncwarp();
         }
