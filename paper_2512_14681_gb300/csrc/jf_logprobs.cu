@@ -6,8 +6,8 @@
 // the type's lowest value, as in a row that a mask has emptied, x log2 e would overflow.) Every thread keeps its own (m, S, T); they are joined in
 // thread order. The top list is kept per CTA: a buffer of candidates that exceed its n_top'th best so far, ordered by
 // (value, lower index) as one 64-bit key, and cut back to n_top when it fills, so the list does not depend on the
-// order in which candidates arrive. The n_top'th largest of the threads' first maxima is a bound to begin with: about
-// 100 of a row's 152,064 logits ever become candidates for a list of 20. Few rows are cut into segments (one CTA each), whose states
+// order in which candidates arrive. A bound comes first, from a sample of the row: some 150 of 152,064 logits then are
+// candidates for a list of 20. Few rows are cut into segments (one CTA each), whose states
 // and lists a second kernel joins in segment order.
 #include <type_traits>
 
@@ -252,8 +252,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
   F2 s = {0.f, 0.f}, t = {0.f, 0.f};
   unsigned long long thr = 0;  // the n_top'th best key so far
   float thr_v = -INFINITY;     // candidates exceed it
-  // A cut costs the square of what it looks at; each tightens the bound: at twice the list, a row of random logits has
-  // about five.
+  // A cut costs the square of what it looks at, and tightens the bound.
   const int cut_at = a.n_top + max(a.n_top, 32);
   if (TOP && tid == 0) top.count = 0;
   if (TOP) __syncthreads();
@@ -325,16 +324,7 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
     cut();
   };
 
-  if (r.has_edges()) {
-    const int e = r.edge(tid);
-    const bool mine = e >= 0 && seg == (tid < N ? 0 : a.segs - 1);
-    const float x[1] = {mine ? act_to_f32(r.p[e]) : -INFINITY};
-    if (TOP) offer(x, x[0], [&](int) { return e; }, std::integral_constant<int, 1>{});
-    raise(x[0]);
-    if (mine) add({x[0], -INFINITY}, m == -INFINITY ? 0.f : -m);
-  }
-  bool bound = TOP;  // a first bound is to be taken
-  uint4 next[U];     // the next round's vectors are on their way while one is worked on
+  uint4 next[U];  // the next round's vectors are on their way while one is worked on
   auto ask = [&](int v0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -342,35 +332,89 @@ __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
       next[u] = v < v_end ? Vec<T>::raw(r.vec(v)) : Vec<T>::nothing();
     }
   };
-  ask(v_begin);
-  for (int v0 = v_begin; v0 < v_end; v0 += LP_THREADS * U) {
-    float x[U * N];
+  auto unpack = [&](float (&x)[U * N]) {
 #pragma unroll
     for (int u = 0; u < U; ++u) Vec<T>::unpack(next[u], *reinterpret_cast<float(*)[N]>(x + u * N));
-    ask(v0 + LP_THREADS * U);
+  };
+  auto largest = [&](const float (&x)[U * N]) {
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < U * N; ++i) mx = fmaxf(mx, x[i]);
-    if (TOP) {
-      if (bound) {  // n_top logits are at least a value that n_top of the threads' maxima reach: a close one by bisection
-        bound = false;
-        const uint32_t mine = mx > -INFINITY ? (uint32_t)(lp_key(mx, 0) >> 32) : 0u;
-        uint32_t lo = 0u, hi = 0xffffffffu;
-        for (int k = 0; k < 32; ++k) {
-          const uint32_t mid = lo + (hi - lo) / 2 + 1;
-          const int n = __syncthreads_count(mine >= mid);
-          if (n >= a.n_top) lo = mid;
-          else hi = mid - 1;
-          if (lo == hi || (n >= a.n_top && n <= a.n_top + a.n_top / 4)) break;
-        }
-        if (lo > 0u) thr_v = fmaxf(thr_v, lp_below(lp_key_value((unsigned long long)lo << 32)));
-      }
-      offer(x, mx, [&](int i) { return r.head + (v0 + i / N * LP_THREADS + tid) * N + i % N; }, std::integral_constant<int, U * N>{});
+    return mx;
+  };
+  auto index_of = [&](int v0) {
+    return [=](int i) { return r.head + (v0 + i / N * LP_THREADS + tid) * N + i % N; };
+  };
+  const int edge = r.has_edges() ? r.edge(tid) : -1;
+  const bool mine = edge >= 0 && seg == (tid < N ? 0 : a.segs - 1);
+  const float at_edge[1] = {mine ? act_to_f32(r.p[edge]) : -INFINITY};
+  if (TOP) {
+    // The bound that the whole segment's candidates have to exceed: n_top logits are at least a value that n_top of the
+    // threads' maxima over a sample of rounds reach; a close one by bisection. A sample of 1 / stride leaves some n_top *
+    // stride candidates, which fit.
+    const int stride = LP_THREADS * U * min(8, max(2, 300 / a.n_top));
+    float mx = -INFINITY, x[U * N];
+    for (int v0 = v_begin; v0 < v_end; v0 += stride) {
+      ask(v0);
+      unpack(x);
+      mx = fmaxf(mx, largest(x));
     }
+    const uint32_t ours = mx > -INFINITY ? (uint32_t)(lp_key(mx, 0) >> 32) : 0u;
+    uint32_t lo = 0u, hi = 0xffffffffu;
+    for (int k = 0; k < 32; ++k) {
+      const uint32_t mid = lo + (hi - lo) / 2 + 1;
+      const int n = __syncthreads_count(ours >= mid);
+      if (n >= a.n_top) lo = mid;
+      else hi = mid - 1;
+      if (lo == hi || (n >= a.n_top && n <= a.n_top + a.n_top / 4)) break;
+    }
+    if (lo > 0u) thr_v = lp_below(lp_key_value((unsigned long long)lo << 32));
+  }
+  // candidates, without a barrier; whether they fitted is seen at the end
+  auto push = [&](const auto& x, float mx, auto index, auto m_const) {
+    constexpr int M = decltype(m_const)::value;
+    if (mx > thr_v) {
+#pragma unroll
+      for (int i = 0; i < M; ++i)
+        if (x[i] > thr_v) {
+          const int at = atomicAdd(&top.count, 1);
+          if (at < LP_BUF) top.buf[at] = lp_key(x[i], index(i));
+        }
+    }
+  };
+  using One = std::integral_constant<int, 1>;
+  using All = std::integral_constant<int, U * N>;
+  if (r.has_edges()) {
+    if (TOP) push(at_edge, at_edge[0], [&](int) { return edge; }, One{});
+    raise(at_edge[0]);
+    if (mine) add({at_edge[0], -INFINITY}, m == -INFINITY ? 0.f : -m);
+  }
+  ask(v_begin);
+  for (int v0 = v_begin; v0 < v_end; v0 += LP_THREADS * U) {
+    float x[U * N];
+    unpack(x);
+    ask(v0 + LP_THREADS * U);
+    const float mx = largest(x);
+    if (TOP) push(x, mx, index_of(v0), All{});
     raise(mx);
     const float base = m == -INFINITY ? 0.f : -m;
 #pragma unroll
     for (int i = 0; i < U * N; i += 2) add({x[i], x[i + 1]}, base);
+  }
+  if (TOP) {
+    __syncthreads();
+    if (top.count > LP_BUF) {  // more than fit (many equal values, a row that climbs between sampled rounds): once more,
+      __syncthreads();         // with cuts on the way
+      if (tid == 0) top.count = 0;
+      __syncthreads();
+      offer(at_edge, at_edge[0], [&](int) { return edge; }, One{});
+      for (int v0 = v_begin; v0 < v_end; v0 += LP_THREADS * U) {
+        float x[U * N];
+        ask(v0);
+        unpack(x);
+        offer(x, largest(x), index_of(v0), All{});
+      }
+    }
   }
   LpStat st = {m, s.x + s.y, t.x + t.y};
 #pragma unroll
