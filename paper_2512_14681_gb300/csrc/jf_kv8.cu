@@ -1,13 +1,19 @@
 // The 8-bit paged cache (jf_ops.h: jf_kv8_cache): rows appended with the rotary embedding on the way, and the
 // values that it stands for read back.
 //
-// Append. A block of the cache (one page of 16 tokens, one KV head) takes one CTA, which also rotates the
-// queries of the head's group for the page's rows. With c, s the cosine and sine of the row's position,
+// Append. A block of the cache (one page of 16 tokens, one KV head) takes one CTA, and the page's rows of
+// queries one more for each KV head's group. With c, s the cosine and sine of the row's position,
 //   x'_i = x_i c_i - x_{i+hd/2} s_i,   x'_{i+hd/2} = x_{i+hd/2} c_i + x_i s_i
 // for keys and queries; then, for keys and values alike, e = the smallest exponent with max |x'| <= 448 2^e
 // (not below the block's own where it holds earlier tokens) and code = e4m3(x' 2^-e). One thread holds 16 values
 // of one row (8 pairs), so the block's new values stay in registers between the maximum and the rounding, and
 // what the block held before is read once, and written only where its exponent grew.
+//
+// Queries are rotated by CTAs of their own in the same launch, so that they neither wait for a block's maximum nor for
+// its page. Both kinds wait for memory, so what counts is how many are resident: at 5 CTAs of 256 threads (48
+// registers) 8,192 rows of 28 + 2 x 4 bf16 heads of 128 (143 MB in and out) take 30 us, 4.8 TB/s; with the queries
+// behind the keys in the same CTA 34 us, with two heads in a thread's registers (4 CTAs) 35 us, with 8 CTAs (and
+// spills) 47 us. One row: 2.3 us, the length of the chain row -> sequence -> page -> block.
 #include "jf_kv8.cuh"
 
 namespace jf {
@@ -93,25 +99,28 @@ JF_DEV void store8(bf16* p, const float (&x)[8]) {
   }
 }
 
-// a, b: 8 pairs of a head. Products and sum rounded one by one (no fma), so that the rotated key, and with it its
-// code, is the same wherever the formula is evaluated in fp32.
+// (cos, sin) of 8 pairs.
 template <bool VEC>
-JF_DEV void rotate8(float (&a)[8], float (&b)[8], const float* cs) {
+JF_DEV void load_turns(const float* p, float (&c)[8], float (&s)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
-    float c0, s0, c1, s1;
     if constexpr (VEC) {
-      const float4 t = *reinterpret_cast<const float4*>(cs + 2 * i);
-      c0 = t.x, s0 = t.y, c1 = t.z, s1 = t.w;
+      const float4 t = *reinterpret_cast<const float4*>(p + 2 * i);
+      c[i] = t.x, s[i] = t.y, c[i + 1] = t.z, s[i + 1] = t.w;
     } else {
-      const float2 t = *reinterpret_cast<const float2*>(cs + 2 * i), u = *reinterpret_cast<const float2*>(cs + 2 * i + 2);
-      c0 = t.x, s0 = t.y, c1 = u.x, s1 = u.y;
+      const float2 t = *reinterpret_cast<const float2*>(p + 2 * i), u = *reinterpret_cast<const float2*>(p + 2 * i + 2);
+      c[i] = t.x, s[i] = t.y, c[i + 1] = u.x, s[i + 1] = u.y;
     }
-    const float x0 = a[i], y0 = b[i], x1 = a[i + 1], y1 = b[i + 1];
-    a[i] = __fsub_rn(__fmul_rn(x0, c0), __fmul_rn(y0, s0));
-    b[i] = __fadd_rn(__fmul_rn(y0, c0), __fmul_rn(x0, s0));
-    a[i + 1] = __fsub_rn(__fmul_rn(x1, c1), __fmul_rn(y1, s1));
-    b[i + 1] = __fadd_rn(__fmul_rn(y1, c1), __fmul_rn(x1, s1));
+  }
+}
+// a, b: 8 pairs of a head. Products and sum rounded one by one (no fma), so that the rotated key, and with it its
+// code, is the same wherever the formula is evaluated in fp32.
+JF_DEV void rotate8(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = a[i], y = b[i];
+    a[i] = __fsub_rn(__fmul_rn(x, c[i]), __fmul_rn(y, s[i]));
+    b[i] = __fadd_rn(__fmul_rn(y, c[i]), __fmul_rn(x, s[i]));
   }
 }
 
@@ -130,46 +139,71 @@ JF_DEV void decode4(uint32_t w, float unit, float* x) {
   }
 }
 
-// T: type of q, k, v; TO: of q_out.
+// Position of a row in the table; one that it does not have is reported and read as 0.
+JF_DEV long long turn_at(const AppendArgs& a, int row, int at) {
+  int pos = a.positions ? a.positions[row] : at;
+  if (pos < 0 || pos >= a.rope_len) {
+    jf_set_error(a.err, JF_DERR_BOUNDS);
+    pos = 0;
+  }
+  return pos;
+}
+
+// T: type of q, k, v; TO: of q_out. blockIdx.y: a KV head, first of its blocks, then (with queries) of its query heads.
 template <typename T, typename TO, int HD, bool VEC>
-__global__ void __launch_bounds__(4 * HD / 2) k_kv8_append(const jf_kv8_cache c, const jf_kv8_rows r, const AppendArgs a) {
+__global__ void __launch_bounds__(4 * HD / 2, 640 / HD) k_kv8_append(const jf_kv8_cache c, const jf_kv8_rows r, const AppendArgs a) {
   constexpr int TPR = HD / 16;           // threads per row of a block
   constexpr int HALF_THREADS = 16 * TPR; // the first half of the CTA holds keys, the second values
   __shared__ uint32_t s_amax[2 * HALF_THREADS / 32];
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31;
-  const int b = kv8_find_seq(r, c.n_seqs, blockIdx.x, lane), h = blockIdx.y;
+  const bool turning = blockIdx.y >= c.n_kv_heads;
+  const int b = kv8_find_seq(r, c.n_seqs, blockIdx.x, lane), h = turning ? blockIdx.y - c.n_kv_heads : blockIdx.y;
   const Kv8Seq sq = kv8_seq(c, r, b, a.err);
   const int nth = (int)blockIdx.x - (sq.row0 / kPage + 2 * b);  // of the pages that the rows touch
   const int page = sq.len / kPage + nth, slot0 = page * kPage;
   if (sq.n == 0 || nth < 0 || slot0 >= sq.len + sq.n) return;
-  const int id = kv8_page(c, b, page, a.err);
-  if (id < 0) return;
   const int old = max(0, sq.len - slot0), last = min(kPage, sq.len + sq.n - slot0);  // new slots: old .. last - 1
   const int row_first = sq.row0 + slot0 + old - sq.len;                              // of slot `old`
 
   const bool is_k = tid < HALF_THREADS;
   const int t = is_k ? tid : tid - HALF_THREADS, slot = t / TPR, d = t % TPR * 8;
+  const bool fresh = slot >= old && slot < last;
+  const int row = row_first + slot - old;
+  float cs[8], sn[8];
+  if (turning) {
+    // Even heads by the first half of the CTA, odd ones by the second.
+    if (!fresh) return;
+    const int G = a.n_heads / c.n_kv_heads;
+    const T* src = reinterpret_cast<const T*>(a.q) + row * a.ld_q + (long long)h * G * HD + d;
+    TO* dst = reinterpret_cast<TO*>(a.q_out) + ((long long)row * a.n_heads + h * G) * HD + d;
+    if (a.rope) load_turns<VEC>(a.rope + (turn_at(a, row, slot0 + slot) * (HD / 2) + d) * 2, cs, sn);
+    for (int g = is_k ? 0 : 1; g < G; g += 2) {
+      float x[8], y[8];
+      load8<VEC>(src + g * HD, x);
+      load8<VEC>(src + g * HD + HD / 2, y);
+      if (a.rope) rotate8(x, y, cs, sn);
+      store8<VEC>(dst + g * HD, x);
+      store8<VEC>(dst + g * HD + HD / 2, y);
+    }
+    return;
+  }
+  const int id = kv8_page(c, b, page, a.err);
+  if (id < 0) return;
   const long long block = (long long)id * c.n_kv_heads + h;
   uint8_t* codes = reinterpret_cast<uint8_t*>(is_k ? c.k : c.v) + (block * kPage + slot) * HD + d;
   int8_t* exps = (is_k ? c.k_exp : c.v_exp) + block;
-  const bool fresh = slot >= old && slot < last;
   float x[8], y[8];
   uint32_t amax = 0;
   bool odd = false;  // met a value that is no finite number
   if (fresh) {
-    const int row = row_first + slot - old;
     const T* src = reinterpret_cast<const T*>(is_k ? a.k : a.v) + row * (is_k ? a.ld_k : a.ld_v) + h * HD + d;
     load8<VEC>(src, x);
     load8<VEC>(src + HD / 2, y);
     if (is_k && a.rope) {
-      int pos = a.positions ? a.positions[row] : slot0 + slot;
-      if (pos < 0 || pos >= a.rope_len) {
-        jf_set_error(a.err, JF_DERR_BOUNDS);
-        pos = 0;
-      }
-      rotate8<VEC>(x, y, a.rope + ((long long)pos * (HD / 2) + d) * 2);
+      load_turns<VEC>(a.rope + (turn_at(a, row, slot0 + slot) * (HD / 2) + d) * 2, cs, sn);
+      rotate8(x, y, cs, sn);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -209,25 +243,10 @@ __global__ void __launch_bounds__(4 * HD / 2) k_kv8_append(const jf_kv8_cache c,
       *p = encode8(x, shrink);
     }
   }
-  if (!a.q) return;
-  // the group's queries of the page's rows
-  const int G = a.n_heads / c.n_kv_heads;
-  for (int i = tid; i < (last - old) * G * TPR; i += 2 * HALF_THREADS) {
-    const int d = i % TPR * 8, g = i / TPR % G, s = old + i / (TPR * G), row = row_first + s - old;
-    const T* src = reinterpret_cast<const T*>(a.q) + row * a.ld_q + (long long)(h * G + g) * HD + d;
-    TO* dst = reinterpret_cast<TO*>(a.q_out) + ((long long)row * a.n_heads + h * G + g) * HD + d;
-    load8<VEC>(src, x);
-    load8<VEC>(src + HD / 2, y);
-    if (a.rope) {
-      const int pos = a.positions ? a.positions[row] : slot0 + s;
-      rotate8<VEC>(x, y, a.rope + ((pos < 0 || pos >= a.rope_len ? 0ll : pos) * (HD / 2) + d) * 2);
-    }
-    store8<VEC>(dst, x);
-    store8<VEC>(dst + HD / 2, y);
-  }
 }
 
-// The same grid; a thread decodes 16 codes.
+// A CTA per block; a thread decodes 16 codes and writes them out. Bound by latency: 8,192 rows of 2 x 4 heads of 128
+// (8 MB in, 34 MB out in bf16, held by L2) take 5.8 us, one row 1.9 us.
 template <typename TO, int HD, bool VEC>
 __global__ void __launch_bounds__(4 * HD / 2)
     k_kv8_read(const jf_kv8_cache c, const jf_kv8_rows r, TO* k_out, TO* v_out, int* err) {
@@ -267,7 +286,7 @@ cudaError_t launch_append(const jf_kv8_cache& c, const jf_kv8_rows& r, const App
   constexpr int per16 = 16 / (int)sizeof(T);
   const bool vec = aligned16(a.k) && aligned16(a.v) && aligned16(a.q) && aligned16(a.q_out) && aligned16(a.rope) &&
                    a.ld_k % per16 == 0 && a.ld_v % per16 == 0 && (!a.q || a.ld_q % per16 == 0);
-  const dim3 grid(kv8_page_grid(c, r), c.n_kv_heads);
+  const dim3 grid(kv8_page_grid(c, r), a.q ? 2 * c.n_kv_heads : c.n_kv_heads);
   if (c.head_dim == 128)
     return vec ? kv8_launch(k_kv8_append<T, TO, 128, true>, grid, dim3(256), 0, st, c, r, a)
                : kv8_launch(k_kv8_append<T, TO, 128, false>, grid, dim3(256), 0, st, c, r, a);
