@@ -224,6 +224,12 @@ JF_DEV int query_shift(float amax) {
 // pieces PK t .. PK t + PK - 1 of keys g and g + 8. O = P V: lane (g, t) holds keys 2t, 2t + 1, 2t + 8, 2t + 9 of P
 // as it held their scores, and needs these keys' codes at dims NT g + j, j = 0 .. NT - 1, of the n-tiles j.
 // NS: fp16 terms of queries and probabilities (1 for bf16 models, 2 for fp32).
+//
+// Bound by the codes' bytes where there are many: 16 sequences of one token, 28 query heads on 4 KV heads of 128, over
+// 301 to 32,768 tokens each (231 MB of codes) take 47 us with the join, 4.9 TB/s; the kernel alone reads at 5.1 TB/s,
+// with a third of the issue slots and a third of the warp-level tensor rate taken by fragments that hold 7 rows of 16.
+// One sequence over 1,024 tokens takes 9.7 us, the length of the chain lengths -> page table -> codes -> scores -> sums
+// -> join.
 // ---------------------------------------------------------------------------------------------
 constexpr int W_WARPS = 4, W_TR = 16, W_CH = 2 * kPage, W_UC = 3;
 constexpr int W_STAGES = 2;  // chunks in a warp's ring
@@ -553,6 +559,13 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // swizzle; K is read K-major, V MN-major. Exponents stay out of the operands: K's go into the scores, V's into P as in
 // the warp-level form, against the chunk's reference E. Where a chunk's value exponents lie further apart than P
 // can carry, its pages go in groups, one step of the stream each (Kv8Info).
+//
+// Bound by a stream's chain from product to softmax to product: two streams take about 5,400 cycles a chunk, of which
+// the softmax of 128 x 128 scores is 2,900 and the products' issue and completion 2,500, and a stream's chain leaves
+// the tensor core idle for all but 28% of the time. Times with the join, 28 query heads on 4 KV heads of 128: 512 rows
+// over 8,192 tokens (62 GFLOP) 110 us, 0.57 PFLOP/s; 32 rows over 32,768 tokens 38 us, of which about 16 are the
+// launch, the first chunk's loads and the join. Chunks of 64 keys with two score accumulators a stream and a warp of
+// its own for the products: 129 us for the former, as asking and converting cost per chunk and not per key.
 // ---------------------------------------------------------------------------------------------
 constexpr int T_TR = 256, T_CH = 128, T_UC = 2;
 constexpr int T_CONV_WARPS = 3, T_THREADS = 32 * (8 + T_CONV_WARPS + 1);  // 168 registers a thread
@@ -1359,6 +1372,11 @@ struct Form {
   bool tile;  // k_kv8_attn_tile
   int ctas, workers, tile_rows;
 };
+// The warp-level form where a KV head's query rows of a sequence fit its tile: it starts faster and wastes fewer rows. With
+// more rows it reads the codes again for every 16, and the tile form leads as soon as there is much to read. us of tile /
+// warp-level form, 28 query heads on 4: one sequence of 3 rows (21 of a KV head) over 100 tokens 11.4 / 10.2, over 30,000
+// 25.2 / 25.9; of 32 rows over 30,000 37.2 / 69.7; four of 18 rows over 30,000 69.6 / 129.4. fp32 has the warp-level form
+// alone: its two-term products are not what a cache of 8-bit codes is served with.
 Form choose(const DeviceInfo& d, const jf_kv8_cache& c, const jf_kv8_rows& r, int dtype, int n_heads) {
   if (dtype == JF_BF16 && (long long)r.max_rows * (n_heads / c.n_kv_heads) > W_TR) return {true, d.sms, d.sms, T_TR};
   const int ctas = d.sms * d.rows_ctas[(dtype == JF_F32 ? 2 : 0) + (c.head_dim == 128 ? 1 : 0)];

@@ -19,7 +19,7 @@ namespace jf {
 namespace {
 
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
-constexpr int LP_BUF = 2 * LP_THREADS;         // candidates a CTA holds; of a warp that joins segments
+constexpr int LP_BUF = 2 * LP_THREADS;         // candidates a CTA holds
 constexpr int LP_SEG_MIN = 4096;    // fewest logits of a segment
 constexpr int LP_CTAS = 608;        // CTAs that fill the GPU (152 SMs x 4)
 constexpr float LOG2E = 1.4426950408889634f;
@@ -233,7 +233,10 @@ struct LpTop {
   int count;
 };
 
-// CTA (row, segment). TOP: a list is asked for.
+// CTA (row, segment). TOP: a list is asked for. Bound by the logits' bytes and, at 5 instructions and an exponential a
+// logit, by the issue of instructions, about alike: 512 rows of 152,064 bf16 logits (156 MB) take 32 us without a list
+// (4.9 TB/s), 46 with 20 alternatives (the sample, 6 us, then a comparison a pair and some 150 candidates a row), 56
+// with 64; fp32 (311 MB) 48 and 56. One fp32 row of 151,936: 9.6 us in 38 segments, most of it the chain of two launches.
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LpParams a) {
   constexpr int N = Vec<T>::N;
@@ -511,7 +514,10 @@ struct LpGradParams {
 
 constexpr int LP_GRAD_VECS = 4;  // vectors per thread
 
-// CTA (row, run of LP_GRAD_VECS x 256 vectors); the first run's CTA takes the row's edges too.
+// d/dx_i of g logprob + h entropy = scale ((i = target) g - p_i (g + h (ln p_i + H))), from the row's (m, ln S) and entropy H.
+// CTA (row, run of LP_GRAD_VECS x 256 vectors); the first run's CTA takes the row's edges too. Bound by the bytes, each
+// logit read and each gradient written once with four vectors of a thread in flight: 512 rows of 152,064 fp32 logits
+// (623 MB) take 94 us, 6.6 TB/s.
 template <typename T>
 __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams a) {
   constexpr int N = Vec<T>::N;
