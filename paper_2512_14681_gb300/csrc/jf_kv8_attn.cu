@@ -560,22 +560,28 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // the warp-level form, against the chunk's reference E. Where a chunk's value exponents lie further apart than P
 // can carry, its pages go in groups, one step of the stream each (Kv8Info).
 //
-// Bound by a stream's chain from product to softmax to product: two streams take about 5,400 cycles a chunk, of which
-// the softmax of 128 x 128 scores is 2,900 and the products' issue and completion 2,500, and a stream's chain leaves
-// the tensor core idle for all but 28% of the time. Times with the join, 28 query heads on 4 KV heads of 128: 512 rows
-// over 8,192 tokens (62 GFLOP) 110 us, 0.57 PFLOP/s; 32 rows over 32,768 tokens 38 us, of which about 16 are the
-// launch, the first chunk's loads and the join. Chunks of 64 keys with two score accumulators a stream and a warp of
-// its own for the products: 129 us for the former, as asking and converting cost per chunk and not per key.
+// K and V of a chunk are converted into a ring of three operands, so that the converters are done with a chunk before its
+// products are due. Bound by a stream's chain: of about 4,600 cycles a chunk, 1,900 are the softmax of 128 x 128 scores and the
+// rest the products (2 x 8 of 64 cycles each, 300 before the first is complete) and the waits between them; the streams share the
+// tensor core, which is busy for half of that time. Neither the exponentials (without them the time is the same), nor
+// conversion (half its stores left out: the same), nor the codes' bytes bound it. Times with the join, 28 query heads on 4 KV
+// heads of 128: 512 rows over 8,192 tokens (62 GFLOP) 97 us, 0.64 PFLOP/s, over 65,536 460 us, 1.06 PFLOP/s; 32 rows over 32,768
+// 35 us, of which about 16 are the launch, the first chunk's loads and the join. Measured and not kept: chunks of 64 keys with
+// two score accumulators a stream and a warp of its own for the products, 129 us for the first of these (its other step then
+// 110); 16 softmax warps, each half of a row's keys, the same within 2% and spills at 96 registers; the streams taking turns with
+// their products, the same.
 // ---------------------------------------------------------------------------------------------
-constexpr int T_TR = 256, T_CH = 128, T_UC = 2;
+// (T_UC 2 / 4: 512 rows over 8,192 tokens 99.9 / 97.0 us, four sequences of 32 rows over 4,096 31.0 / 28.5, eight of 16 over 100
+// to 2,000 19.5 / 21.7.)
+constexpr int T_TR = 256, T_CH = 128, T_UC = 4;
 constexpr int T_CONV_WARPS = 3, T_THREADS = 32 * (8 + T_CONV_WARPS + 1);  // 168 registers a thread
-constexpr int T_PAGES = T_CH / kPage, T_RAW = 3, T_INFO = 8;  // chunks of codes, of Kv8Info in shared memory
+constexpr int T_PAGES = T_CH / kPage, T_RAW = 2, T_OPS = 3, T_INFO = 4;  // chunks of codes, operands, chunks of Kv8Info in shared memory
 constexpr int TM_COLS = 512;
 template <int HD>
 struct TLayout {
   static constexpr int Q = 128 * HD * 2, KV = T_CH * HD * 2, PAGE = kPage * HD * 2;  // bytes of fp16 operands
   static constexpr int RAW = T_CH * HD;                                                                      // codes of a chunk
-  static constexpr int OFF_K = 2 * Q, OFF_V = OFF_K + KV, OFF_RAW = OFF_V + KV;  // RAW: a stage holds K's, then V's
+  static constexpr int OFF_OPS = 2 * Q, OFF_RAW = OFF_OPS + T_OPS * KV;  // RAW: a stage holds K's, then V's
   static constexpr int TOTAL = OFF_RAW + T_RAW * 2 * RAW + 1024;                 // + alignment
   static constexpr int GROUP = HD * 16;  // 8 keys of a page: HD / 64 halves of 1024 bytes
   // byte offset of 16-byte piece c (8 dims) of key r of a page
@@ -587,11 +593,13 @@ struct TLayout {
   }
 };
 
-// What the steps of a chunk need beside its operands. held: slots with a token (0: no chunk, the share has ended).
-// groups: how many steps; pages[j]: pages of step j as bits; E[j]: its reference exponent. fk, ev: 2^(e_k), e_v of a page.
-struct Kv8Info {
-  float fk[T_PAGES];
-  int ev[T_PAGES], E[T_PAGES];
+// What the steps of a chunk need beside its operands. page: 2^(e_k), e_v - E, 2^(E - e_v) of a page, E the reference exponent of
+// its step. held: slots with a token (0: no chunk, the share has ended). groups: how many steps; pages[j]: pages of step j as
+// bits; E[j]: its reference exponent. T_INFO of them are enough: chunk g is asked for when the codes of V of chunk g - 2 are
+// converted, after K of g - 2, into the place of V of g - 4, whose chunk is done with.
+struct __align__(16) Kv8Info {
+  float4 page[T_PAGES];
+  int16_t E[T_PAGES];
   uint8_t pages[T_PAGES];
   int groups, held;
 };
@@ -613,18 +621,42 @@ JF_DEV float2 add2(float2 x, float2 y) {
       : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
   return r;
 }
+// Products and their commit by the one lane whose `on` is set, in code that the warp goes through together: descriptors then
+// stay in uniform registers, and a product takes its 64 cycles of the tensor core (in a branch of one lane some 100).
+JF_DEV void mma_f16_ss_on(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+JF_DEV void mma_f16_ts_on(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+JF_DEV void commit_on(uint32_t bar, uint32_t on) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(on)
+      : "memory");
+}
 template <int HD>
 __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnParams a) {
   using Lay = TLayout<HD>;
   using W = Walk<T_TR, T_CH, T_UC>;
   extern __shared__ uint8_t sm_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
-  const uint32_t sQ = smem_u32(sm), sK = sQ + Lay::OFF_K, sV = sQ + Lay::OFF_V;
-  // a stage of codes: landed, converted; operands K and V: there, and read by both streams (a unit of one tile: by its
-  // stream, counted twice; that they are there, on one barrier for even and one for odd chunks: a stream that waits for every
-  // second one must not meet a barrier a completion ahead or behind); per stream: S ready (the products, and the thread that issued them, which passes on the
-  // chunk's Kv8Info), P V done, everything done
-  __shared__ __align__(8) uint64_t b_raw[T_RAW], b_rawfree[T_RAW], b_kfull[2], b_kfree, b_vfull[2], b_vfree, b_s[2], b_o[2], b_all[2], b_turn[2];
+  const uint32_t sQ = smem_u32(sm), sOps = sQ + Lay::OFF_OPS;
+  // a stage of codes: landed, converted; operands K and V (number 2 g and 2 g + 1 of the share, in a ring of T_OPS): there, and
+  // a place of the ring read by both streams (a unit of one tile: by its stream, counted twice; that they are there, on one
+  // barrier for even and one for odd chunks: a stream that waits for every second one must not meet a barrier a completion
+  // ahead or behind); per stream: S ready (the products, and the thread that issued them, which passes on the chunk's
+  // Kv8Info), P V done, everything done
+  __shared__ __align__(8) uint64_t b_raw[T_RAW], b_rawfree[T_RAW], b_kfull[2], b_vfull[2], b_free[T_OPS], b_s[2], b_o[2], b_all[2];
   __shared__ uint32_t tmem_slot;
   __shared__ Kv8Info s_info[T_INFO];
   int* pre = reinterpret_cast<int*>(sm + Lay::OFF_RAW);  // (until the first codes are asked for)
@@ -636,15 +668,13 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       mbar_init(smem_u32(&b_raw[i]), 1);
       mbar_init(smem_u32(&b_rawfree[i]), T_CONV_WARPS);
     }
-    mbar_init(smem_u32(&b_kfree), 2);
-    mbar_init(smem_u32(&b_vfree), 2);
+    for (int i = 0; i < T_OPS; ++i) mbar_init(smem_u32(&b_free[i]), 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&b_kfull[i]), T_CONV_WARPS);
       mbar_init(smem_u32(&b_vfull[i]), T_CONV_WARPS);
       mbar_init(smem_u32(&b_s[i]), 2);
       mbar_init(smem_u32(&b_o[i]), 1);
       mbar_init(smem_u32(&b_all[i]), 1);
-      mbar_init(smem_u32(&b_turn[i]), 1);
     }
     fence_mbar_init();
   }
@@ -725,18 +755,22 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       Kv8Info& info = s_info[g % T_INFO];
       unsigned rest = __ballot_sync(0xffffffffu, mine);
       const int bytes = __popc(rest) * (2 * kPage * HD);
-      int groups = 0;
+      int groups = 0, E_mine = 0;
       while (rest) {
         const bool in = rest >> lane & 1u;
         const int hi = __reduce_max_sync(0xffffffffu, in ? cur.ev : -1000);
         const unsigned now = __ballot_sync(0xffffffffu, in && cur.ev >= hi - W_EV_MAX);
         const int lo = __reduce_min_sync(0xffffffffu, now >> lane & 1u ? cur.ev : 1000);
         if (E_run > lo || hi - E_run > W_EV_MAX) E_run = max(max(min(lo, hi - W_EV_SET), hi - W_EV_MAX), -126);
-        if (lane == 0) info.pages[groups] = (uint8_t)now, info.E[groups] = E_run;
+        if (now >> lane & 1u) E_mine = E_run;
+        if (lane == 0) info.pages[groups] = (uint8_t)now, info.E[groups] = (int16_t)E_run;
         ++groups;
         rest &= ~now;
       }
-      if (lane < T_PAGES) info.fk[lane] = pow2i(cur.ek), info.ev[lane] = cur.ev;
+      if (lane < T_PAGES) {
+        const int d = mine ? cur.ev - E_mine : 0;
+        info.page[lane] = make_float4(pow2i(cur.ek), (float)d, pow2i(-d), 0.f);
+      }
       if (lane == 0) info.groups = groups, info.held = cur.held;
       __syncwarp();
       if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
@@ -798,13 +832,14 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       ok = wait(b_raw[stage], g / T_RAW);
       const int held = s_info[g % T_INFO].held;
       if (!ok || held == 0) break;
-      ok = g == 0 || wait(b_kfree, g - 1);
+      const int kn = 2 * g, vn = kn + 1;  // the operands' numbers
+      ok = kn < T_OPS || wait(b_free[kn % T_OPS], kn / T_OPS - 1);
       if (!ok) break;
-      put(src, sK, 3 * cw, held);
+      put(src, sOps + kn % T_OPS * Lay::KV, 3 * cw, held);
       if (lane == 0) mbar_arrive(smem_u32(&b_kfull[g & 1]));
-      ok = g == 0 || wait(b_vfree, g - 1);
+      ok = vn < T_OPS || wait(b_free[vn % T_OPS], vn / T_OPS - 1);
       if (!ok) break;
-      put(src + Lay::RAW, sV, 5 - 3 * cw, held);
+      put(src + Lay::RAW, sOps + vn % T_OPS * Lay::KV, 5 - 3 * cw, held);
       if (lane == 0) {
         mbar_arrive(smem_u32(&b_vfull[g & 1]));
         mbar_arrive(smem_u32(&b_rawfree[stage]));
@@ -817,44 +852,43 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_row + s * 128, t_o = t_row + 256 + s * 128;
     const bool issuer = (warp & 3) == 0;
     constexpr uint32_t idesc_s = idesc_f16_f32(128, T_CH), idesc_pv = idesc_f16_f32(128, HD) | (1u << 16);  // V MN-major
-    const uint64_t dq = sdesc_k_sw128(sQ + s * Lay::Q), dk = sdesc_k_sw128(sK, Lay::GROUP), dv = sdesc_mn_sw128(sV, 1024u, Lay::GROUP);
+    const uint64_t dq = sdesc_k_sw128(sQ + s * Lay::Q), dk0 = sdesc_k_sw128(sOps, Lay::GROUP), dv0 = sdesc_mn_sw128(sOps, 1024u, Lay::GROUP);
     // S of a step, by the stream's first warp; both = a unit of two tiles
-    auto issue_s = [&](bool last, bool both) {
+    auto issue_s = [&](int gc, bool last, bool both) {
+      const int place = __shfl_sync(0xffffffffu, 2 * gc % T_OPS, 0);
+      uint64_t dk = dk0 + (uint64_t)(place * (Lay::KV >> 4)), dqn = dq;
+      asm volatile("" : "+l"(dk), "+l"(dqn));  // (the sums below are not kept from step to step)
       tc_fence_after();
-      if (elect_one()) {
+      const uint32_t on = elect_one();
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk)
-          tc_mma_bf16(tmem + s * 128, dq + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2),
-                      dk + (uint64_t)((kk >> 2) * 64 + (kk & 3) * 2), idesc_s, kk > 0 ? 1u : 0u);
-        tc_commit(smem_u32(&b_s[s]));
-        mbar_arrive(smem_u32(&b_s[s]));
-        if (last) {
-          tc_commit(smem_u32(&b_kfree));
-          if (!both) tc_commit(smem_u32(&b_kfree));
-        }
-      }
+      for (int kk = 0; kk < HD / 16; ++kk)
+        mma_f16_ss_on(tmem + s * 128, dqn + (uint64_t)((kk >> 2) * (16384 >> 4) + (kk & 3) * 2), dk + (uint64_t)((kk >> 2) * 64 + (kk & 3) * 2),
+                      idesc_s, kk > 0 ? 1u : 0u, on);
+      commit_on(smem_u32(&b_s[s]), on);
+      if (lane == 0) mbar_arrive(smem_u32(&b_s[s]));
+      commit_on(smem_u32(&b_free[place]), on && last);
+      commit_on(smem_u32(&b_free[place]), on && last && !both);
       __syncwarp();
     };
-    auto issue_pv = [&](int pages, bool fresh, bool last, bool both) {
+    auto issue_pv = [&](int gc, bool fresh, bool last, bool both) {
+      const int place = __shfl_sync(0xffffffffu, (2 * gc + 1) % T_OPS, 0);
+      uint64_t dv = dv0 + (uint64_t)(place * (Lay::KV >> 4));
+      asm volatile("" : "+l"(dv));
       tc_fence_after();
-      if (elect_one()) {
+      const uint32_t on = elect_one();
 #pragma unroll
-        for (int kk = 0; kk < T_PAGES; ++kk)
-          if (kk < pages)
-            tc_mma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + kk * 8, dv + (uint64_t)(kk * (Lay::PAGE >> 4)), idesc_pv,
-                          kk > 0 || !fresh ? 1u : 0u);
-        tc_commit(smem_u32(&b_o[s]));
-        if (last) {
-          tc_commit(smem_u32(&b_vfree));
-          if (!both) tc_commit(smem_u32(&b_vfree));
-        }
-      }
+      for (int kk = 0; kk < T_PAGES; ++kk)
+        mma_f16_ts_on(tmem + 256 + s * 128, tmem + s * 128 + kk * 8, dv + (uint64_t)(kk * (Lay::PAGE >> 4)), idesc_pv,
+                      kk > 0 || !fresh ? 1u : 0u, on);
+      commit_on(smem_u32(&b_o[s]), on);
+      commit_on(smem_u32(&b_free[place]), on && last);
+      commit_on(smem_u32(&b_free[place]), on && last && !both);
       __syncwarp();
     };
     auto stream_and = [&](bool ok) { return s ? sync_and<2, 128>(ok) : sync_and<1, 128>(ok); };
     const bool q16 = ((uintptr_t)a.q & 15) == 0 && a.ld_q % 8 == 0;
     bool ok = true;
-    int steps = 0, g = 0, turns = 0;  // steps of the stream so far; chunks of the share so far; turns taken
+    int steps = 0, g = 0;  // steps of the stream so far; chunks of the share so far
     while (true) {
       const int rows = tile_rows(w);
       const bool two = rows > 128;
@@ -925,7 +959,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       ok = stream_and(ok);  // the stream's queries are there
       if (issuer && c_first < n && ok) {
         ok = wait(b_kfull[(g0 + c_first) & 1], (g0 + c_first) >> 1);
-        if (ok) issue_s(s_info[(g0 + c_first) % T_INFO].groups == 1, two);
+        if (ok) issue_s(g0 + c_first, s_info[(g0 + c_first) % T_INFO].groups == 1, two);
       }
       bool fresh = true;  // no P V of the unit yet
       bool go = true;     // (left by all warps of the stream together)
@@ -953,68 +987,80 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           if (jb < 0) v |= jb <= -32 ? 0xffffffffu : (1u << -jb) - 1u;
           return v;
         };
-        const int held = min(T_PAGES, (sq.len + sq.n - kp0 + kPage - 1) / kPage);  // pages with a token
         int groups = 1;
         for (int j = 0; j < groups; ++j) {
           ok = wait(b_s[s], steps) && ok;
           tc_fence_after();
           if (ok) {
           // The row's scores, 32 at a time, for the maximum and again for the exponentials (P of column c goes to c / 2,
-          // which has been read by then). Rolled loops: the code of a step has to stay in the instruction cache.
+          // which has been read by then). What a row does not see, in the few chunks that hold new rows, is written over with
+          // -inf beforehand: in the loops themselves it would cost every chunk 6%, and as much what a page's factors are made of.
+          // (512 rows over 65,536 tokens: 461 us; with the loops rolled 489; in one pass, P in registers until the maximum is
+          // known, 686, for it spills.)
           groups = info.groups;
           const int pages = info.pages[j], E_new = info.E[j];
-          auto hide = [&](int h, float (&v)[32]) {
-            if (!cut && pages == 255) return;
-            uint32_t see = visible(h);
-            if (!(pages >> (2 * h) & 1)) see &= 0xffff0000u;
-            if (!(pages >> (2 * h + 1) & 1)) see &= 0x0000ffffu;
+          if (cut || pages != 255) {
+#pragma unroll 1
+            for (int h = 0; h < 4; ++h) {
+              uint32_t see = visible(h);
+              if (!(pages >> (2 * h) & 1)) see &= 0xffff0000u;
+              if (!(pages >> (2 * h + 1) & 1)) see &= 0x0000ffffu;
+#pragma unroll 1
+              for (int y = 0; y < 2; ++y, see >>= 16) {
+                float v[16];
+                uint32_t u[16];
+                tmem_ld16(t_s + 32 * h + 16 * y, v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = see >> i & 1u ? v[i] : -INFINITY;
-          };
+                for (int i = 0; i < 16; ++i) u[i] = see >> i & 1u ? __float_as_uint(v[i]) : 0xff800000u;
+                tmem_st16(t_s + 32 * h + 16 * y, u);
+              }
+            }
+            tmem_wait_st();
+          }
           // of a page's scores; above 0, so that a hidden key's -inf stays one
-          auto factor = [&](int page) { return fmaxf(f * info.fk[page], 7.888609e-31f /* 2^-100 */); };
+          auto factor = [&](float fk) { return fmaxf(f * fk, 7.888609e-31f /* 2^-100 */); };
           float mc = -INFINITY;
-          auto largest = [&](int h, const float (&v)[32]) {
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            float v[32];
+            const float fk[2] = {info.page[2 * h].x, info.page[2 * h + 1].x};
+            tmem_ld32(t_s + 32 * h, v);
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
               float mx = v[16 * y];
 #pragma unroll
               for (int i = 1; i < 16; ++i) mx = fmaxf(mx, v[16 * y + i]);
-              mc = fmaxf(mc, mx * factor(2 * h + y));
+              mc = fmaxf(mc, mx * factor(fk[y]));
             }
-          };
+          }
+          const bool raise = mc > m_ref + W_LAG, any = __any_sync(0xffffffffu, raise);
+          const float al = raise ? (m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - mc)) : 1.f;
+          l *= al;
+            if (!first && (any || E_new != E)) {
+              const float x = al * pow2i(max(-126, min(126, E - E_new)));
 #pragma unroll 1
+              for (int h = 0; h < HD / 16; ++h) {
+                float o[16];
+                uint32_t y[16];
+                tmem_ld16(t_o + 16 * h, o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(o[i] * x);
+                tmem_st16(t_o + 16 * h, y);
+              }
+            }
+            E = E_new;
+            first = false;
+          if (raise) m_ref = mc;
+          const float nb = m_ref == -INFINITY ? 0.f : -m_ref;
+#pragma unroll
           for (int h = 0; h < 4; ++h) {
             float v[32];
-            tmem_ld32(t_s + 32 * h, v);
-            hide(h, v);
-            largest(h, v);
-          }
-          const bool raise = mc > m_ref + W_LAG;
-          if (!first && (__any_sync(0xffffffffu, raise) || E_new != E)) {
-            const float al = raise ? (m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - mc)) : 1.f;
-            l *= al;
-            const float x = al * pow2i(max(-126, min(126, E - E_new)));
-#pragma unroll 1
-            for (int h = 0; h < HD / 16; ++h) {
-              float o[16];
-              uint32_t u[16];
-              tmem_ld16(t_o + 16 * h, o);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(o[i] * x);
-              tmem_st16(t_o + 16 * h, u);
-            }
-          }
-          if (raise) m_ref = mc;
-          E = E_new;
-          first = false;
-          const float nb = m_ref == -INFINITY ? 0.f : -m_ref;
-          auto exponentials = [&](int h, const float (&v)[32]) {
             uint32_t u[16];
+            const float4 page[2] = {info.page[2 * h], info.page[2 * h + 1]};
+            tmem_ld32(t_s + 32 * h, v);
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              const int d = pages >> (2 * h + y) & 1 ? info.ev[2 * h + y] - E : 0;  // (other pages' are hidden)
-              const float fx = factor(2 * h + y), b = nb + (float)d;
+              const float fx = factor(page[y].x), b = nb + page[y].y;
               float2 ls = make_float2(0.f, 0.f);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
@@ -1024,16 +1070,9 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
                 ls = add2(ls, p);
                 u[8 * y + i] = pack_f16(p.x, p.y);
               }
-              l = fmaf(ls.x + ls.y, pow2i(-d), l);
+              l = fmaf(ls.x + ls.y, page[y].z, l);
             }
             tmem_st16(t_s + 16 * h, u);
-          };
-#pragma unroll 1
-          for (int h = 0; h < 4; ++h) {
-            float v[32];
-            tmem_ld32(t_s + 32 * h, v);
-            hide(h, v);
-            exponentials(h, v);
           }
           tmem_wait_st();
           }
@@ -1042,20 +1081,15 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           if (!go) break;
           if (issuer) {
             const bool last = j == groups - 1;
-            // with two tiles the streams take turns: products of both at once would end later for both, and leave the
-            // tensor core idle while both are at their softmax
-            if (two && (s || turns > 0)) ok = wait(b_turn[s], s ? turns : turns - 1);
-            ok = ok && wait(b_vfull[gc & 1], gc >> 1);
-            if (ok) issue_pv(held, fresh, last, two);
+            ok = wait(b_vfull[gc & 1], gc >> 1);
+            if (ok) issue_pv(gc, fresh, last, two);
             // the stream's next S, once P (which lies where S will) has been read
             const int gn = last ? gc + c_step : gc, jn = last ? 0 : j + 1;
             if (ok && (!last || c + c_step < n)) {
-              ok = wait(b_o[s], steps) && wait(b_kfull[gn & 1], gn >> 1);
-              if (ok) issue_s(s_info[gn % T_INFO].groups == jn + 1, two);
-            }
-            if (two) {
-              if (lane == 0) mbar_arrive(smem_u32(&b_turn[s ^ 1]));
-              ++turns;
+              ok = wait(b_kfull[gn & 1], gn >> 1);
+              const bool last_s = s_info[gn % T_INFO].groups == jn + 1;
+              ok = ok && wait(b_o[s], steps);
+              if (ok) issue_s(gn, last_s, two);
             }
           }
           fresh = false;
@@ -1373,10 +1407,11 @@ struct Form {
   int ctas, workers, tile_rows;
 };
 // The warp-level form where a KV head's query rows of a sequence fit its tile: it starts faster and wastes fewer rows. With
-// more rows it reads the codes again for every 16, and the tile form leads as soon as there is much to read. us of tile /
-// warp-level form, 28 query heads on 4: one sequence of 3 rows (21 of a KV head) over 100 tokens 11.4 / 10.2, over 30,000
-// 25.2 / 25.9; of 32 rows over 30,000 37.2 / 69.7; four of 18 rows over 30,000 69.6 / 129.4. fp32 has the warp-level form
-// alone: its two-term products are not what a cache of 8-bit codes is served with.
+// more rows it reads the codes again for every 16, and the tile form leads as soon as there is much to read (which only the
+// device knows). us of tile / warp-level form, 28 query heads on 4: one sequence of 3 rows (21 of a KV head) over 100 tokens
+// 11.1 / 10.4, over 1,000 14.0 / 11.6, over 30,000 23.0 / 25.8; of 32 rows over 30,000 34.8 / 66.5; four of 18 rows over 30,000 55.1 /
+// 129.6; sixteen of 3 rows over 1,000 21.3 / 18.1, of 8 rows 25.0 / 25.4. fp32 has the warp-level form alone: its two-term
+// products are not what a cache of 8-bit codes is served with.
 Form choose(const DeviceInfo& d, const jf_kv8_cache& c, const jf_kv8_rows& r, int dtype, int n_heads) {
   if (dtype == JF_BF16 && (long long)r.max_rows * (n_heads / c.n_kv_heads) > W_TR) return {true, d.sms, d.sms, T_TR};
   const int ctas = d.sms * d.rows_ctas[(dtype == JF_F32 ? 2 : 0) + (c.head_dim == 128 ? 1 : 0)];
