@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // rest the products (2 x 8 of 64 cycles each, 300 before the first is complete) and the waits between them; the streams share the
 // tensor core, which is busy for half of that time. Neither the exponentials (without them the time is the same), nor
 // conversion (half its stores left out: the same), nor the codes' bytes bound it. Times with the join, 28 query heads on 4 KV
-// heads of 128: 512 rows over 8,192 tokens (62 GFLOP) 97 us, 0.64 PFLOP/s, over 65,536 460 us, 1.06 PFLOP/s; 32 rows over 32,768
+// heads of 128: 512 rows over 8,192 tokens (62 GFLOP) 97 us, 0.64 PFLOP/s, over 65,536 460 us, 1.05 PFLOP/s; 32 rows over 32,768
 // 35 us, of which about 16 are the launch, the first chunk's loads and the join. Measured and not kept: chunks of 64 keys with
 // two score accumulators a stream and a warp of its own for the products, 129 us for the first of these (its other step then
 // 110); 16 softmax warps, each half of a row's keys, the same within 2% and spills at 96 registers; the streams taking turns with
