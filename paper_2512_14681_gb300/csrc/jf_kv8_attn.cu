@@ -33,7 +33,7 @@ struct Kv8AttnParams {
   int mask_words;
   void* out;
   float* lse;
-  int* plan;         // [n_seqs + 1]: length of the sequences before b
+  int* plan;         // [n_seqs + 1]: length of the sequences before b (of more than 32)
   float* states;     // [2 N][tile rows x hd normalised O, then m, then l of the tile's rows]
   int* err;
 };
@@ -70,8 +70,31 @@ struct Plan {
     for (int t = 0; t < n; ++t) sum += UC + chunks(a, s, G, t);
     return sum;
   }
-  // pre[b] = length of the sequences before b, pre[n_seqs] = of all; by the whole CTA (ends with a barrier).
-  static JF_DEV void build(const Kv8AttnParams& a, int G, int* pre) {
+  // Up to 32 sequences: a warp finds out by itself, lane b for sequence b, and nothing is read twice or passed on. Returns
+  // the batch's length.
+  struct Few {
+    Kv8Seq s;
+    int before, length;  // of the sequences before b, of b
+  };
+  static JF_DEV int build_few(const Kv8AttnParams& a, int G, int lane, Few& f) {
+    f.s = {0, 0, 0};
+    f.length = 0;
+    if (lane < a.c.n_seqs) {
+      f.s = kv8_seq(a.c, a.r, lane, a.err);
+      f.length = per_head(a, f.s, G) * a.c.n_kv_heads;
+    }
+    int sum = f.length;
+#pragma unroll
+    for (int sh = 1; sh < 32; sh <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, sum, sh);
+      if (lane >= sh) sum += u;
+    }
+    f.before = sum - f.length;
+    return __shfl_sync(0xffffffffu, sum, 31);
+  }
+  // pre[b] = length of the sequences before b, pre[n_seqs] = of all (returned); by the whole CTA. The first CTA leaves it for
+  // the combine.
+  static JF_DEV int build(const Kv8AttnParams& a, int G, int* pre) {
     for (int b = threadIdx.x; b < a.c.n_seqs; b += blockDim.x)
       pre[b + 1] = per_head(a, kv8_seq(a.c, a.r, b, a.err), G) * a.c.n_kv_heads;
     __syncthreads();
@@ -92,6 +115,9 @@ struct Plan {
       }
     }
     __syncthreads();
+    if (blockIdx.x == 0)
+      for (int b = threadIdx.x; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
+    return pre[a.c.n_seqs];
   }
 };
 
@@ -130,7 +156,18 @@ struct Walk {
     }
     b = lo;
     s = kv8_seq(a.c, a.r, b, a.err);
-    const int head = (pre[b + 1] - pre[b]) / a.c.n_kv_heads, off = at - pre[b];
+    enter(a, G, at - pre[b], pre[b + 1] - pre[b]);
+  }
+  JF_DEV void start_few(const Kv8AttnParams& a, const typename P::Few& f, int G, int at_, int end_) {
+    at = at_;
+    end = end_;
+    b = 31 - __clz(__ballot_sync(0xffffffffu, f.before <= at));  // (lanes without a sequence: before = all)
+    s = {__shfl_sync(0xffffffffu, f.s.n, b), __shfl_sync(0xffffffffu, f.s.row0, b), __shfl_sync(0xffffffffu, f.s.len, b)};
+    enter(a, G, at - __shfl_sync(0xffffffffu, f.before, b), __shfl_sync(0xffffffffu, f.length, b));
+  }
+  // At place `off` of sequence b, which is `length` long.
+  JF_DEV void enter(const Kv8AttnParams& a, int G, int off, int length) {
+    const int head = length / a.c.n_kv_heads;
     kvh = off / head;
     int rest = off - kvh * head;
     tile = 0;
@@ -268,14 +305,16 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
   const int G = a.n_heads / a.c.n_kv_heads, Hkv = a.c.n_kv_heads;
   pdl_wait();
   pdl_launch_dependents();  // (after the wait: the combine reads the batch's lengths before its own)
-  Plan<W_TR, W_CH, W_UC>::build(a, G, pre);
-  if (blockIdx.x == 0)
-    for (int b = tid; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
-  const int worker = blockIdx.x * W_WARPS + warp;
-  const Shares shares(pre[a.c.n_seqs], gridDim.x * W_WARPS);
-  if (shares.size(worker) == 0) return;
-  Walk<W_TR, W_CH, W_UC> w;
-  w.start(a, pre, G, shares.begin(worker), shares.begin(worker) + shares.size(worker));
+  using W = Walk<W_TR, W_CH, W_UC>;
+  const bool few = a.c.n_seqs <= 32;
+  typename W::P::Few f;
+  const int worker = blockIdx.x * W_WARPS + warp, total = few ? W::P::build_few(a, G, lane, f) : W::P::build(a, G, pre);
+  const Shares shares(total, gridDim.x * W_WARPS);
+  const int begin = shares.begin(worker), end = begin + shares.size(worker);
+  if (begin == end) return;
+  W w;
+  if (few) w.start_few(a, f, G, begin, end);
+  else w.start(a, pre, G, begin, end);
   const uint32_t ring = smem_u32(sm) + warp * (W_STAGES * STAGE_BYTES);
   const bool q16 = ((uintptr_t)a.q & 15) == 0 && a.ld_q * sizeof(T) % 16 == 0;
   const uint8_t *Kc = reinterpret_cast<const uint8_t*>(a.c.k), *Vc = reinterpret_cast<const uint8_t*>(a.c.v);
@@ -680,17 +719,18 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
   }
   pdl_wait();
   pdl_launch_dependents();  // (after the wait: the combine reads the batch's lengths before its own)
-  W::P::build(a, G, pre);
-  if (blockIdx.x == 0)
-    for (int b = tid; b <= a.c.n_seqs; b += blockDim.x) a.plan[b] = pre[b];
-  const Shares shares(pre[a.c.n_seqs], gridDim.x);
-  if (shares.size(blockIdx.x) == 0) return;
+  const bool few = a.c.n_seqs <= 32;
+  typename W::P::Few f;
+  const Shares shares(few ? W::P::build_few(a, G, lane, f) : W::P::build(a, G, pre), gridDim.x);
+  const int begin = shares.begin(blockIdx.x), end = begin + shares.size(blockIdx.x);
+  if (begin == end) return;
   if (warp == 8) {
     tmem_alloc(smem_u32(&tmem_slot), TM_COLS);
     tmem_relinquish();
   }
   W w;
-  w.start(a, pre, G, shares.begin(blockIdx.x), shares.begin(blockIdx.x) + shares.size(blockIdx.x));
+  if (few) w.start_few(a, f, G, begin, end);
+  else w.start(a, pre, G, begin, end);
   fence_proxy_async_smem();  // the plan's place is taken by copies
   tc_fence_before();
   __syncthreads();
