@@ -654,3 +654,24 @@ def test_many_chunks_a_share(torch, Hq, Hkv, hd, new, lens, masked, dtype, sprea
             off = (out[r:r + n, h].double() - ref).abs()
             assert (off <= tol).all(), (b, h, float((off / tol).max()))
         r += n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,most", [(32, 3), (33, 2), (33, 14), (100, 3), (100, 40), (1024, 2), (1024, 6)])
+def test_many_sequences(torch, dtype, n, most):
+    """Batches on both sides of the 32 sequences that a warp plans by itself, up to the largest; some without rows."""
+    rng = np.random.default_rng(n + most)
+    new = [int(x) for x in rng.integers(0, most + 1, n)]
+    new[n // 2] = most
+    lens = [int(x) for x in rng.integers(0, 70, n)]
+    lens[-1] = 900
+    pool = fill(torch, 2, 64, [a + k for a, k in zip(lens, new)], seed=n)
+    check_attention(torch, pool, queries(torch, sum(new), 12, 64, dtype, n), new, lens, 0.125)
+
+
+def test_append_to_many_sequences(torch):
+    rng = np.random.default_rng(3)
+    for n in (33, 200):
+        new = [int(x) for x in rng.integers(0, 20, n)]
+        lens = [int(x) for x in rng.integers(0, 60, n)]
+        test_append_rotates_and_rounds_to_the_nearest_code(torch, 4, 2, 64, new, lens, "bf16", "f32", False, "packed")
