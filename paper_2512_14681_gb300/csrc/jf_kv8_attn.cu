@@ -591,9 +591,9 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // and 128..255 over every chunk, or, in a unit of up to 128 rows, all rows over the even and the odd chunks, whose
 // states are joined at the unit's end. While the softmax of one stream runs, the tensor core works for the other.
 //
-// Warps 0-3 and 4-7: stream 0 and 1, a thread per row; the stream's first warp also
-// issues its products (a stream has nothing else to do until they are complete). Warp 11 asks for codes, page by page as
-// bulk copies up to three chunks ahead; warps 8-10 convert them to fp16 and store them as the images of tensor-core
+// Warps 0-3 and 4-7: stream 0 and 1, a thread per row; the stream's first warp also issues its products (a stream has
+// nothing else to do until they are complete). Warp 11 asks for codes, page by page as bulk copies up to two chunks ahead
+// of the converters; warps 8-10 convert them to fp16 and store them as the images of tensor-core
 // operands: per page of 16 keys two 8-key groups, each of HD / 64 halves of 8 rows x 128 bytes with the 128-byte
 // swizzle; K is read K-major, V MN-major. Exponents stay out of the operands: K's go into the scores, V's into P as in
 // the warp-level form, against the chunk's reference E. Where a chunk's value exponents lie further apart than P
@@ -607,7 +607,7 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // heads of 128: 512 rows over 8,192 tokens (62 GFLOP) 97 us, 0.64 PFLOP/s, over 65,536 460 us, 1.05 PFLOP/s; 32 rows over 32,768
 // 35 us, of which about 16 are the launch, the first chunk's loads and the join. Measured and not kept: chunks of 64 keys with
 // two score accumulators a stream and a warp of its own for the products, 129 us for the first of these (its other step then
-// 110); 16 softmax warps, each half of a row's keys, the same within 2% and spills at 96 registers; the streams taking turns with
+// 110); 16 softmax warps, each half of a row's keys, the same within 4% and spills at 96 registers; the streams taking turns with
 // their products, the same.
 // ---------------------------------------------------------------------------------------------
 // (T_UC 2 / 4: 512 rows over 8,192 tokens 99.9 / 97.0 us, four sequences of 32 rows over 4,096 31.0 / 28.5, eight of 16 over 100
