@@ -5,8 +5,9 @@
 // scaling undone, the softmax scale, log2 e), and
 //   out = sum_j 2^(s_j - m) 2^(e_v_j) c_v_j / sum_j 2^(s_j - m).
 // Codes are exact in fp16, so both products run on fp16 operands with fp32 sums. The values' exponents go into
-// the probabilities: p' = 2^(s - m) 2^(e_v - E) in fp16, against a running reference E in whose unit the output
-// accumulates; E follows e_v only when the difference leaves a range in which fp16 keeps p' as well as it keeps p.
+// the probabilities: p' = 2^(s - m) 2^(e_v - E) in fp16, against a running reference E of each row in whose unit its
+// output accumulates; E follows e_v only when the difference leaves a range in which fp16 keeps p' as well as it keeps
+// p, and only as far as the row's weights and what it has summed allow (unit_down, unit_up).
 //
 // Work is split evenly whatever the batch: a unit is (sequence, KV head, tile of (token, head) query rows), a
 // chunk a run of keys of one unit. Units lie one after the other, each as long as its chunks plus a constant for
@@ -248,6 +249,25 @@ JF_DEV int query_shift(float amax) {
   return x == 0 || x == 255 ? (x == 0 && amax > 0.f ? 126 : 0) : min(14 - (x - 127), 126);
 }
 
+// The exponent E in whose unit a row's output goes on accumulating when values come that would best be added at R.
+// Smaller ones lower it, as far as what is summed (most: its largest magnitude) stays below 2^126; what is added beside it
+// afterwards is below 2^54 (2^30 keys, probabilities of 2^15, codes of 2^9). A block of zeros, at the format's smallest
+// exponent, is such a case.
+JF_DEV int unit_down(int E, int R, float most) {
+  return R < E ? min(E, max(R, E - (252 - (__float_as_int(most) >> 23)))) : E;
+}
+// Larger ones raise it, less far where the row gives them little weight: s is its largest score among them (-inf: it sees
+// none, and they leave it as it is), m its reference maximum, and at s = m - x they need R - x only (and R - 122 where the
+// probabilities' factor 2^(e_v - E) has to remain a number).
+JF_DEV int unit_up(int E, int R, float s, float m) {
+  return R > E && s > -INFINITY ? max(max(E, R - (int)fminf(fmaxf(m - s, 0.f), 1000.f)), max(R - 122, -126)) : E;
+}
+// 2^e as two factors, each a number (what lies beyond them is out of fp32's range in any case).
+JF_DEV float2 pow2_pair(int e) {
+  const int x = max(-126, min(126, e));
+  return make_float2(pow2i(x), pow2i(max(-126, min(126, e - x))));
+}
+
 // ---------------------------------------------------------------------------------------------
 // Few query rows per KV head (single-token serving; fp32 at any row count): warp-level products.
 //
@@ -398,7 +418,7 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
         }
     }
     float o[NT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    int E = -4096;  // o is in units of 2^E (set by the first page)
+    int E[2] = {0, 0};  // a row's o is in units of 2^E (set by the first page)
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -406,6 +426,14 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
     auto rescale = [&](float x0, float x1) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) o[j][0] *= x0, o[j][1] *= x0, o[j][2] *= x1, o[j][3] *= x1;
+    };
+
+    auto move_to = [&](const int (&to)[2]) {  // to units of 2^to
+      const float2 a = pow2_pair(E[0] - to[0]), b = pow2_pair(E[1] - to[1]);
+      rescale(a.x, b.x);
+      if (__any_sync(0xffffffffu, a.y != 1.f || b.y != 1.f)) rescale(a.y, b.y);
+      E[0] = to[0];
+      E[1] = to[1];
     };
 
     for (int i = 0; i < n; ++i) {
@@ -485,16 +513,41 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
         rescale(al[0], al[1]);
       }
       const float nb[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
+      // ---- the rows' reference exponents: down for both pages together, so that one of large values and little weight
+      // before one of small values that outweigh it is added in a unit that holds it; up before each
+      const int ev_min = min(ev[0], ev[1]), ev_max = max(ev[0], ev[1]);
+      if (i == 0) E[0] = E[1] = ev_min - W_EV_SET;
+      const bool apart = __any_sync(0xffffffffu, ev_min < max(E[0], E[1]) || ev_max - min(E[0], E[1]) > W_EV_MAX);
+      if (apart && __any_sync(0xffffffffu, ev_min < E[0] || ev_min < E[1])) {
+        int to[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float most = 0.f;
+#pragma unroll
+          for (int j = 0; j < NT; ++j) most = fmaxf(most, fmaxf(fabsf(o[j][2 * k]), fabsf(o[j][2 * k + 1])));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+          to[k] = ev_min < E[k] ? unit_down(E[k], ev_min - W_EV_SET, most) : E[k];
+        }
+        move_to(to);
+      }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        // ---- the reference exponent (a step beyond 2^+-126: what was summed is out of the new unit's reach)
-        if (ev[x] < E || ev[x] - E > W_EV_MAX) {
-          const float step = pow2i(max(-126, min(126, E - (ev[x] - W_EV_SET))));
-          E = ev[x] - W_EV_SET;
-          rescale(step, step);
+        if (apart && __any_sync(0xffffffffu, ev[x] - E[0] > W_EV_MAX || ev[x] - E[1] > W_EV_MAX)) {
+          int to[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float most = fmaxf(fmaxf(sc[x][0][2 * k], sc[x][0][2 * k + 1]), fmaxf(sc[x][1][2 * k], sc[x][1][2 * k + 1]));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            to[k] = ev[x] - E[k] > W_EV_MAX ? unit_up(E[k], ev[x] - W_EV_SET, most, m[k]) : E[k];
+          }
+          move_to(to);
         }
         // ---- P, then O += P V
-        const float up = pow2i(ev[x] - E);
+        float up[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) up[k] = pow2i(max(-126, min(126, ev[x] - E[k])));
         uint32_t pf[NS][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -502,7 +555,7 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
           for (int k = 0; k < 2; ++k) {
             const float p0 = ex2_ftz(sc[x][u][2 * k] + nb[k]), p1 = ex2_ftz(sc[x][u][2 * k + 1] + nb[k]);
             l[k] += p0 + p1;
-            float lo = p0 * up, hi = p1 * up;
+            float lo = p0 * up[k], hi = p1 * up[k];
 #pragma unroll
             for (int y = 0; y < NS; ++y) {
               pf[y][2 * u + k] = pack_f16(lo, hi);
@@ -554,7 +607,7 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
       l[k] += __shfl_xor_sync(0xffffffffu, l[k], 2);
       const int r = g + 8 * k;
       if (r0 + r >= rows) continue;
-      const float il = l[k] > 0.f ? 1.f / l[k] : (l[k] == 0.f ? 0.f : l[k]), unit = pow2i(max(E, -126));
+      const float il = l[k] > 0.f ? 1.f / l[k] : (l[k] == 0.f ? 0.f : l[k]), unit = pow2i(E[k]);
       const long long at = (long long)(s.row0 + tok[k]) * a.n_heads + w.kvh * G + (r0 + r - tok[k] * G);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -616,6 +669,7 @@ constexpr int T_TR = 256, T_CH = 128, T_UC = 4;
 constexpr int T_CONV_WARPS = 3, T_THREADS = 32 * (8 + T_CONV_WARPS + 1);  // 168 registers a thread
 constexpr int T_PAGES = T_CH / kPage, T_RAW = 2, T_OPS = 3, T_INFO = 4;  // chunks of codes, operands, chunks of Kv8Info in shared memory
 constexpr int TM_COLS = 512;
+constexpr int UNITS_DIFFER = -4096;  // in place of the exponent that a warp's rows share
 template <int HD>
 struct TLayout {
   static constexpr int Q = 128 * HD * 2, KV = T_CH * HD * 2, PAGE = kPage * HD * 2;  // bytes of fp16 operands
@@ -633,9 +687,10 @@ struct TLayout {
 };
 
 // What the steps of a chunk need beside its operands. page: 2^(e_k), e_v - E, 2^(E - e_v) of a page, E the reference exponent of
-// its step. held: slots with a token (0: no chunk, the share has ended). groups: how many steps; pages[j]: pages of step j as
-// bits; E[j]: its reference exponent. T_INFO of them are enough: chunk g is asked for when the codes of V of chunk g - 2 are
-// converted, after K of g - 2, into the place of V of g - 4, whose chunk is done with.
+// its step (0 to 7 below e_v), which the rows' own follow. held: slots with a token (0: no chunk, the share has
+// ended). groups: how many steps; pages[j]: pages of step j as bits; E[j]: its reference exponent. T_INFO of them are enough:
+// chunk g is asked for when the codes of V of chunk g - 2 are converted, after K of g - 2, into the place of V of g - 4, whose
+// chunk is done with.
 struct __align__(16) Kv8Info {
   float4 page[T_PAGES];
   int16_t E[T_PAGES];
@@ -683,6 +738,36 @@ JF_DEV void commit_on(uint32_t bar, uint32_t on) {
       "r"(on)
       : "memory");
 }
+// The unit that a row's O (in columns t_o .., in units of 2^was) goes on in, of a step whose reference exponent is another
+// one; called by whole warps. Not inlined: seldom needed, and its registers would cost every step.
+template <int HD>
+__device__ __noinline__ int unit_of_row(uint32_t t_o, int was, int E_step, float mc, float m_ref, float al) {
+  float most = 0.f;
+  if (__any_sync(0xffffffffu, E_step < was)) {
+#pragma unroll 1
+    for (int h = 0; h < HD / 16; ++h) {
+      float o[16];
+      tmem_ld16(t_o + 16 * h, o);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(o[i]));
+    }
+  }
+  return E_step < was ? (mc > -INFINITY ? unit_down(was, E_step, most * al) : was) : unit_up(was, E_step, mc, m_ref);
+}
+// O *= x.x x.y
+template <int HD>
+__device__ __noinline__ void scale_o(uint32_t t_o, float x, float y) {
+#pragma unroll 1
+  for (int h = 0; h < HD / 16; ++h) {
+    float o[16];
+    uint32_t u[16];
+    tmem_ld16(t_o + 16 * h, o);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(o[i] * x * y);
+    tmem_st16(t_o + 16 * h, u);
+  }
+}
+
 template <int HD>
 __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnParams a) {
   using Lay = TLayout<HD>;
@@ -698,6 +783,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
   __shared__ __align__(8) uint64_t b_raw[T_RAW], b_rawfree[T_RAW], b_kfull[2], b_vfull[2], b_free[T_OPS], b_s[2], b_o[2], b_all[2];
   __shared__ uint32_t tmem_slot;
   __shared__ Kv8Info s_info[T_INFO];
+  __shared__ int16_t s_unit[256];
   int* pre = reinterpret_cast<int*>(sm + Lay::OFF_RAW);  // (until the first codes are asked for)
   // (shuffles tell the compiler that warp numbers and the TMEM address are uniform: operand descriptors then are)
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
@@ -992,7 +1078,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         fence_proxy_async_smem();
       }
       float m_ref = -INFINITY, l = 0.f;
-      int E = 0;
+      int E_all = 0;  // the warp's rows' O are in units of 2^E_all, or each in its own (UNITS_DIFFER: s_unit)
       bool first = true;
       const int c_step = two ? 1 : 2, c_first = two ? 0 : s, g0 = g;  // the stream's chunks c_first, + c_step, ...
       g += n;
@@ -1038,7 +1124,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
           // (512 rows over 65,536 tokens: 461 us; with the loops rolled 489; in one pass, P in registers until the maximum is
           // known, 686, for it spills.)
           groups = info.groups;
-          const int pages = info.pages[j], E_new = info.E[j];
+          const int pages = info.pages[j], E_step = info.E[j];
           if (cut || pages != 255) {
 #pragma unroll 1
             for (int h = 0; h < 4; ++h) {
@@ -1073,25 +1159,30 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
               mc = fmaxf(mc, mx * factor(fk[y]));
             }
           }
-          const bool raise = mc > m_ref + W_LAG, any = __any_sync(0xffffffffu, raise);
+          const bool raise = mc > m_ref + W_LAG;
           const float al = raise ? (m_ref == -INFINITY ? 0.f : ex2_ftz(m_ref - mc)) : 1.f;
           l *= al;
-            if (!first && (any || E_new != E)) {
-              const float x = al * pow2i(max(-126, min(126, E - E_new)));
-#pragma unroll 1
-              for (int h = 0; h < HD / 16; ++h) {
-                float o[16];
-                uint32_t y[16];
-                tmem_ld16(t_o + 16 * h, o);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(o[i] * x);
-                tmem_st16(t_o + 16 * h, y);
-              }
-            }
-            E = E_new;
-            first = false;
           if (raise) m_ref = mc;
-          const float nb = m_ref == -INFINITY ? 0.f : -m_ref;
+          float nb = m_ref == -INFINITY ? 0.f : -m_ref, l_before = 0.f;
+          if (first) E_all = E_step;
+          const bool apart = E_step != E_all;  // (seldom)
+          if (apart) {
+            const int was = E_all == UNITS_DIFFER ? s_unit[tid] : E_all, E = unit_of_row<HD>(t_o, was, E_step, mc, m_ref, al);
+            E_all = __all_sync(0xffffffffu, E == E_step) ? E_step : UNITS_DIFFER;
+            s_unit[tid] = (int16_t)E;
+            if (__any_sync(0xffffffffu, raise || E != was)) {
+              const float2 step = pow2_pair(was - E);
+              scale_o<HD>(t_o, al * step.x, step.y);
+            }
+            // Probabilities of the step are 2^(E_step - E) of what the page's exponent makes of them. (What lies 2^60 below the
+            // row's unit is nothing in fp16 in any case, but its sum counts.)
+            nb += (float)max(-60, min(122, E_step - E));
+            l_before = l;
+            l = 0.f;
+          } else if (__any_sync(0xffffffffu, raise) && !first) {
+            scale_o<HD>(t_o, al, 1.f);
+          }
+          first = false;
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
             float v[32];
@@ -1114,6 +1205,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
             }
             tmem_st16(t_s + 16 * h, u);
           }
+          if (apart) l = fmaf(l, pow2i(-max(-60, min(122, E_step - s_unit[tid]))), l_before);
           tmem_wait_st();
           }
           tc_fence_before();
@@ -1140,10 +1232,11 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         ok = wait(b_o[s], steps - 1);
         tc_fence_after();
       }
+      const int E = E_all == UNITS_DIFFER ? s_unit[tid] : E_all;
       if (!two) {
         // (where the stream's queries were)
         reinterpret_cast<float2*>(sm + s * Lay::Q)[lr] = make_float2(m_ref, l);
-        if (lr == 0) reinterpret_cast<int*>(sm + s * Lay::Q)[256] = first ? -4096 : E;
+        reinterpret_cast<int*>(sm + s * Lay::Q)[256 + lr] = E;
       }
       ok = sync_and<3, 256>(ok);  // both streams leave a unit together (barrier 0 is __syncthreads)
       if (!ok) break;
@@ -1154,14 +1247,15 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       int Em = E, d0 = 0, d1 = HD;                 // their unit 2^Em; the dims that this thread finishes
       if (!two) {
         const float2 ml0 = reinterpret_cast<const float2*>(sm)[lr], ml1 = reinterpret_cast<const float2*>(sm + Lay::Q)[lr];
-        const int E0 = reinterpret_cast<const int*>(sm)[256], E1 = reinterpret_cast<const int*>(sm + Lay::Q)[256];
+        const int E0 = reinterpret_cast<const int*>(sm)[256 + lr], E1 = reinterpret_cast<const int*>(sm + Lay::Q)[256 + lr];
         const float m0 = ml0.x, m1 = ml1.x, l0 = ml0.y, l1 = ml1.y;
         M = fmaxf(m0, m1);
         const float a0 = m0 == -INFINITY ? 0.f : exp2f(m0 - M), a1 = m1 == -INFINITY ? 0.f : exp2f(m1 - M);
         L = (m0 == -INFINITY ? l0 : a0 * l0) + (m1 == -INFINITY ? l1 : a1 * l1);  // (nothing seen: 0, or NaN)
-        Em = max(E0, E1);  // (of a stream without a step: far below)
-        w0 = a0 * pow2i(max(E0 - Em, -126));
-        w1 = a1 * pow2i(max(E1 - Em, -126));
+        // (a stream that has no weight, or saw nothing, has no say in the unit)
+        Em = max(a0 > 0.f ? E0 : -126, a1 > 0.f ? E1 : -126);
+        w0 = a0 * pow2i(max(-126, min(0, E0 - Em)));
+        w1 = a1 * pow2i(max(-126, min(0, E1 - Em)));
         d0 = s * (HD / 2);
         d1 = d0 + HD / 2;
       }
