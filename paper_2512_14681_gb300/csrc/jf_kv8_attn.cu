@@ -346,7 +346,9 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
     const int keys = s.len + s.n;  // slots that hold a token
     const int rows = s.n * G, r0 = w.tile * W_TR;
 
-    // ---- loads of the n chunks. Lane j of a group of 32 pages: page j's id and exponents (K's and V's packed)
+    // ---- loads of the n chunks. Lane j of a group of 32 pages: page j's id and exponents (K's and V's packed; NO_PAGE for one
+    // outside the pool, whose keys no row sees)
+    constexpr int NO_PAGE = 1 << 16;
     const int n_pages = min(2 * c1, (keys + kPage - 1) / kPage) - 2 * c0;
     int id_l = -1, e_l = 0, e_cur = 0;  // of the pages being loaded; of those in use
     auto issue = [&](int i) {  // chunk i of the share: zeros for slots without a token
@@ -359,6 +361,8 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
             if (id_l >= 0) {
               const long long blk = (long long)id_l * Hkv + w.kvh;
               e_l = (int)(uint8_t)a.c.k_exp[blk] | (int)(uint8_t)a.c.v_exp[blk] << 8;
+            } else {
+              e_l = NO_PAGE;
             }
           }
         }
@@ -478,7 +482,7 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sc[x][u][k] *= fu[k >> 1];
+          for (int k = 0; k < 4; ++k) sc[x][u][k] = e2 & NO_PAGE ? -INFINITY : sc[x][u][k] * fu[k >> 1];
       }
       if (kp0 + W_CH > s.len) {
 #pragma unroll
@@ -688,14 +692,14 @@ struct TLayout {
 
 // What the steps of a chunk need beside its operands. page: 2^(e_k), e_v - E, 2^(E - e_v) of a page, E the reference exponent of
 // its step (0 to 7 below e_v), which the rows' own follow. held: slots with a token (0: no chunk, the share has
-// ended). groups: how many steps; pages[j]: pages of step j as bits; E[j]: its reference exponent. T_INFO of them are enough:
+// ended). there: its pages (those outside the pool are left out) as bits. groups: how many steps; pages[j]: pages of step j as bits; E[j]: its reference exponent. T_INFO of them are enough:
 // chunk g is asked for when the codes of V of chunk g - 2 are converted, after K of g - 2, into the place of V of g - 4, whose
 // chunk is done with.
 struct __align__(16) Kv8Info {
   float4 page[T_PAGES];
   int16_t E[T_PAGES];
   uint8_t pages[T_PAGES];
-  int groups, held;
+  int groups, held, there;
 };
 
 // x * y + z and x + y on two values at a time.
@@ -851,13 +855,14 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
     };
     auto exponents = [&](Ahead& n) {
       if (lane * kPage < n.held) {
-        if (n.id < 0 || n.id >= a.c.n_pages) {  // reported, and page 0 read in its place
+        if (n.id >= 0 && n.id < a.c.n_pages) {
+          const long long blk = (long long)n.id * Hkv + n.kvh;
+          n.ek = a.c.k_exp[blk];
+          n.ev = a.c.v_exp[blk];
+        } else {  // reported and left out
           jf_set_error(a.err, JF_DERR_BOUNDS);
-          n.id = 0;
+          n.id = -1;
         }
-        const long long blk = (long long)n.id * Hkv + n.kvh;
-        n.ek = a.c.k_exp[blk];
-        n.ev = a.c.v_exp[blk];
       }
     };
     Ahead cur = look(), next = look();
@@ -871,7 +876,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         break;
       }
       // the copies first: what describes them has time until they have landed
-      const bool mine = lane * kPage < cur.held;
+      const bool mine = lane * kPage < cur.held && cur.id >= 0;
       const uint32_t bar = smem_u32(&b_raw[stage]), dst = sQ + Lay::OFF_RAW + stage * 2 * Lay::RAW + lane * (kPage * HD);
       const long long off = ((long long)cur.id * Hkv + cur.kvh) * (kPage * HD);
       if (mine) {
@@ -880,8 +885,12 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       }
       Kv8Info& info = s_info[g % T_INFO];
       unsigned rest = __ballot_sync(0xffffffffu, mine);
-      const int bytes = __popc(rest) * (2 * kPage * HD);
+      const int there = (int)rest, bytes = __popc(rest) * (2 * kPage * HD);
       int groups = 0, E_mine = 0;
+      if (rest == 0) {  // (a step without a key)
+        if (lane == 0) info.pages[0] = 0, info.E[0] = (int16_t)E_run;
+        groups = 1;
+      }
       while (rest) {
         const bool in = rest >> lane & 1u;
         const int hi = __reduce_max_sync(0xffffffffu, in ? cur.ev : -1000);
@@ -897,7 +906,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
         const int d = mine ? cur.ev - E_mine : 0;
         info.page[lane] = make_float4(pow2i(cur.ek), (float)d, pow2i(-d), 0.f);
       }
-      if (lane == 0) info.groups = groups, info.held = cur.held;
+      if (lane == 0) info.groups = groups, info.held = cur.held, info.there = there;
       __syncwarp();
       if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
       if (cur.held == 0) break;
@@ -918,7 +927,7 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
     constexpr int PR = HD / 16, ROUNDS = kPage * PR / 32;  // pieces per key; rounds per page
     const int lr = PR == 8 ? 2 * ((lane >> 3) & 1) + ((lane >> 2) & 1) : lane >> 2;
     const int lc = PR == 8 ? (lane & 3) + 4 * (((lane >> 2) & 1) ^ (lane >> 4)) : lane & 3;
-    auto put = [&](uint32_t src, uint32_t dst, int first, int held) {
+    auto put = [&](uint32_t src, uint32_t dst, int first, int held, int there) {
 #pragma unroll
       for (int q = 0; q < 3; ++q) {
         const int page = first + q;
@@ -930,10 +939,10 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
                        : "=r"(x[j].x), "=r"(x[j].y), "=r"(x[j].z), "=r"(x[j].w)
                        : "r"(src + page * (kPage * HD) + (j * (32 / PR) + lr) * HD + lc * 16)
                        : "memory");
-        if (held < T_CH) {  // slots without a token
+        if (held < T_CH || there != 255) {  // slots without a token, pages outside the pool
 #pragma unroll
           for (int j = 0; j < ROUNDS; ++j)
-            if (page * kPage + j * (32 / PR) + lr >= held) x[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (page * kPage + j * (32 / PR) + lr >= held || !(there >> page & 1)) x[j] = make_uint4(0u, 0u, 0u, 0u);
         }
 #pragma unroll
         for (int j = 0; j < ROUNDS; ++j) {
@@ -956,16 +965,16 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
       const int stage = g % T_RAW;
       const uint32_t src = sQ + Lay::OFF_RAW + stage * 2 * Lay::RAW;
       ok = wait(b_raw[stage], g / T_RAW);
-      const int held = s_info[g % T_INFO].held;
+      const int held = s_info[g % T_INFO].held, there = s_info[g % T_INFO].there;
       if (!ok || held == 0) break;
       const int kn = 2 * g, vn = kn + 1;  // the operands' numbers
       ok = kn < T_OPS || wait(b_free[kn % T_OPS], kn / T_OPS - 1);
       if (!ok) break;
-      put(src, sOps + kn % T_OPS * Lay::KV, 3 * cw, held);
+      put(src, sOps + kn % T_OPS * Lay::KV, 3 * cw, held, there);
       if (lane == 0) mbar_arrive(smem_u32(&b_kfull[g & 1]));
       ok = vn < T_OPS || wait(b_free[vn % T_OPS], vn / T_OPS - 1);
       if (!ok) break;
-      put(src + Lay::RAW, sOps + vn % T_OPS * Lay::KV, 5 - 3 * cw, held);
+      put(src + Lay::RAW, sOps + vn % T_OPS * Lay::KV, 5 - 3 * cw, held, there);
       if (lane == 0) {
         mbar_arrive(smem_u32(&b_vfull[g & 1]));
         mbar_arrive(smem_u32(&b_rawfree[stage]));

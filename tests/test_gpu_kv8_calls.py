@@ -1,0 +1,45 @@
+"""Calls of the 8-bit cache's operators that go wrong easily: pages, rows, tensors, streams and devices that do not fit."""
+import numpy as np
+import pytest
+
+from tests.parity import need_gpu
+from tests.test_gpu_kv8 import PAGE, fill, queries, reference, rows_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    return need_gpu()
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 2), ("bf16", 50), ("f32", 5)])
+@pytest.mark.parametrize("bad", [-1, 10 ** 6])
+def test_a_page_outside_the_pool_is_reported_and_its_keys_left_out(torch, dtype, n, bad):
+    """In the middle of a context, at its end, and a sequence of one page (whose rows then see nothing), beside a sequence
+    that is in order."""
+    from paper_2512_14681_gb300._lib import JfError
+
+    new, lens = [n, n, n], [1000 - n, 500, 0]
+    for lost in ((0, 20), (0, 62), (1, 3), (2, 0)):
+        pool = fill(torch, 4, 128, [a + k for a, k in zip(lens, new)], seed=31)
+        pool.cache.page_table[lost[0], lost[1]] = bad
+        q = queries(torch, sum(new), 28, 128, dtype, 7, 0.3)
+
+        def see(b):
+            vis = np.arange(lens[b] + n)[None, :] <= lens[b] + np.arange(n)[:, None]
+            if b == lost[0]:
+                vis[:, lost[1] * PAGE:(lost[1] + 1) * PAGE] = False
+            return vis
+
+        out, lse = pool.cache.attention(rows_of(new, lens), q, 128 ** -0.5, want_lse=True)
+        with pytest.raises(JfError, match="out of range"):
+            pool.cache.check()
+        ref, A, ref_lse, dS = reference(pool, q.double().cpu().numpy(), new, lens, 128 ** -0.5, see)
+        bf16 = dtype == "bf16"
+        tol = (2 * dS + (2.0 ** -11 if bf16 else 2.0 ** -20))[..., None] * A + (2.0 ** -8 * np.abs(ref) if bf16 else 0) + 1e-37
+        assert (np.abs(out.double().cpu().numpy() - ref) <= tol).all()
+        got, none = lse.double().cpu().numpy(), ref_lse == -np.inf
+        assert (got[none] == -np.inf).all()
+        ref_lse = np.where(none, 0, ref_lse)
+        assert (np.abs(np.where(none, 0, got) - ref_lse) <= 2 * dS + 1e-6 * (1 + np.abs(ref_lse))).all()
