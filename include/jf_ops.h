@@ -81,9 +81,10 @@ typedef struct {
 /* The new rows of a batch: rows row_start[b] .. row_start[b+1]-1 are the tokens of sequence b at its
  * slots len[b], len[b]+1, ... (b may have none). row_start [n_seqs + 1] ascending from 0 to n_rows and
  * len [n_seqs] are DEVICE arrays, read when the kernels run (a captured graph follows them); n_rows and
- * max_rows (>= every sequence's row count: it chooses the attention's form, any value gives the same
- * numbers up to rounding) are host numbers. A sequence whose rows lie outside its page table, and pages
- * outside the pool, are reported through err_word (as JF_EDEVICE's bounds code 4) and left out. */
+ * max_rows (every sequence's row count or more: it chooses the attention's form; where row_start has changed
+ * since, the numbers are the same up to rounding) are host numbers. A sequence whose rows lie outside its
+ * page table, and pages outside the pool, are reported through err_word (as JF_EDEVICE's bounds code 4) and
+ * left out. */
 typedef struct {
   const int32_t *row_start, *len;
   int n_rows, max_rows;
@@ -125,7 +126,7 @@ jf_status jf_op_kv8_attention_workspace_bytes(const jf_kv8_cache* cache, const j
  * elements apart (rotated: jf_op_kv8_append's q_out); out: [n_rows][n_heads][head_dim], 16-byte aligned.
  * mask NULL: row i of a sequence sees slots 0 .. len + i. Else mask is [n_rows][mask_words] 32-bit words,
  * 32 * mask_words >= max_rows: the row sees slots 0 .. len - 1, and slot len + j if bit j % 32 of word j / 32
- * is set (a tree of drafts and candidates). lse (optional): fp32 [n_rows][n_heads], the natural logarithm of
+ * is set (a tree of drafts and candidates); a word that the mask does not have counts as 0. lse (optional): fp32 [n_rows][n_heads], the natural logarithm of
  * the sum of exponentials. A row that sees nothing gets out 0 and lse -infinity; a NaN in a row's query
  * reaches that row's outputs only.
  * Softmax statistics and sums are fp32. JF_BF16: products of fp16 operands (codes exactly; queries scaled

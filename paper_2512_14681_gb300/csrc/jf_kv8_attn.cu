@@ -199,11 +199,12 @@ struct Walk {
   }
 };
 
-// Whether new row i of the sequence sees slot kp (>= len).
+// Whether new row i of the sequence sees slot kp (>= len). (A sequence may have more rows than a mask row has bits: the host
+// sees only what max_rows says.)
 JF_DEV bool sees_new(const Kv8AttnParams& a, const Kv8Seq& s, int i, int kp) {
   const int j = kp - s.len;
   if (!a.mask) return j <= i;
-  return j < s.n && (a.mask[(long long)(s.row0 + i) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
+  return j < s.n && j >> 5 < a.mask_words && (a.mask[(long long)(s.row0 + i) * a.mask_words + (j >> 5)] >> (j & 31) & 1u);
 }
 
 // N consecutive values as fp32 (zeros unless live); by 16-byte loads where the caller's rows allow it.

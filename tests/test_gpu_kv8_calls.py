@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from tests.parity import need_gpu
-from tests.test_gpu_kv8 import PAGE, fill, queries, reference, rows_of
+from tests.test_gpu_kv8 import PAGE, check_attention, fill, queries, reference, rows_of, tree_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +43,26 @@ def test_a_page_outside_the_pool_is_reported_and_its_keys_left_out(torch, dtype,
         assert (got[none] == -np.inf).all()
         ref_lse = np.where(none, 0, ref_lse)
         assert (np.abs(np.where(none, 0, got) - ref_lse) <= 2 * dS + 1e-6 * (1 + np.abs(ref_lse))).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hint", [1, 8, 33, 70])
+def test_a_mask_narrower_than_a_sequences_rows(torch, dtype, hint):
+    """row_start may hold more rows a sequence than the host's max_rows says (a captured graph's batch has changed): a row
+    sees no new row beyond its mask's words, in either form, and no other row's words count."""
+    new, lens, words = [5, 70, 40], [200, 33, 0], 1 + (hint - 1) // 32
+    pool = fill(torch, 4, 128, [a + n for a, n in zip(lens, new)], seed=41)
+    rng = np.random.default_rng(3)
+    bits = [rng.random((n, 32 * words)) < 0.7 for n in new]
+    mask = torch.from_numpy(np.concatenate([tree_bits(b, words) for b in bits])).cuda()
+    store = torch.full((mask.numel() + 64,), -1, dtype=torch.int32, device="cuda")  # (what follows the mask would show)
+    store[:mask.numel()] = mask.flatten()
+
+    def see(b):
+        new_rows = np.zeros((new[b], new[b]), bool)
+        n = min(new[b], 32 * words)
+        new_rows[:, :n] = bits[b][:, :n]
+        return np.concatenate([np.ones((new[b], lens[b]), bool), new_rows], 1)
+
+    check_attention(torch, pool, queries(torch, sum(new), 28, 128, dtype, 9, 0.3), new, lens, 128 ** -0.5,
+                    store[:mask.numel()].view(-1, words), see, max_rows=hint)
