@@ -60,6 +60,15 @@ def _on_stream(call):
     return wrapped
 
 
+def _row_stride(t, width, name):
+    """Elements from row to row of t, whose rows are `width` long and must not share memory (a broadcast row does)."""
+    if t.shape[0] <= 1:
+        return width  # (one row's stride may be anything)
+    _want(t.stride(0) >= width, "{}: rows {} elements apart that are {} long (contiguous() gives them memory of their own)",
+          name, t.stride(0), width)
+    return t.stride(0)
+
+
 def _device_i32(t, n, name):
     _want(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n,
           "{}: a contiguous int32 CUDA tensor of {} elements is wanted", name, n)
@@ -141,7 +150,7 @@ class Kv8Cache:
             ok = t.dim() == 2 and t.shape[1] == width and t.stride(1) == 1
         _want(ok and t.shape[0] == rows.n_rows and t.device == self.device,
               "{}: [{}][{} x {}] with contiguous heads on {} is wanted", name, rows.n_rows, heads, self.head_dim, self.device)
-        return max(t.stride(0), width)  # (one row's stride may be anything)
+        return _row_stride(t, width, name)
 
     def _batch(self, rows):
         _want(rows.len.numel() == self.page_table.shape[0] and rows.len.device == self.device,

@@ -13,7 +13,7 @@ from typing import NamedTuple
 import torch
 
 from . import _lib as J
-from .kv8 import _checked, _dtype, _on_stream, _raw_stream, _want
+from .kv8 import _checked, _dtype, _on_stream, _raw_stream, _row_stride, _want
 
 _err = {}        # error word by device
 _workspaces = {}  # by (device, stream): calls on different streams may overlap
@@ -55,7 +55,7 @@ def _need(rows, vocab, top):
 def _logits(t, name="logits"):
     _want(t.is_cuda and t.dim() == 2 and t.shape[1] >= 1 and (t.stride(1) == 1 or t.shape[1] == 1),
           "{}: CUDA [rows][vocab] with contiguous rows is wanted", name)
-    return max(t.stride(0), t.shape[1])
+    return _row_stride(t, t.shape[1], name)
 
 
 def _vector(t, rows, dtype, device, name):
@@ -66,8 +66,8 @@ def _vector(t, rows, dtype, device, name):
 
 @_on_stream
 def token_logprobs(logits, targets, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
-    """logits: CUDA [rows][vocab] (float32 or bfloat16, any row stride); targets: int32 [rows]; scale: inverse
-    temperature; top: alternatives listed per row (at most 64)."""
+    """logits: CUDA [rows][vocab] (float32 or bfloat16, rows any distance apart but not one over the other); targets:
+    int32 [rows]; scale: inverse temperature; top: alternatives listed per row (at most 64)."""
     lib = J.load()
     ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
     dtype = _dtype(logits.dtype)

@@ -66,3 +66,27 @@ def test_a_mask_narrower_than_a_sequences_rows(torch, dtype, hint):
 
     check_attention(torch, pool, queries(torch, sum(new), 28, 128, dtype, 9, 0.3), new, lens, 128 ** -0.5,
                     store[:mask.numel()].view(-1, words), see, max_rows=hint)
+
+
+def test_rows_that_share_memory_are_refused(torch):
+    """Broadcast and overlapping rows of every input; one row may have any stride."""
+    from paper_2512_14681_gb300 import _lib as J
+
+    pool = fill(torch, 2, 64, [40], seed=1)
+    c, rows = pool.cache, rows_of([4], [20])
+    x, q = torch.ones(4, 2, 64, device="cuda"), torch.ones(4, 4, 64, device="cuda")
+    for kind in ("broadcast", "overlapping"):
+        def shared(t):
+            return t[:1].expand(t.shape) if kind == "broadcast" else \
+                torch.ones(4 * t[0].numel(), device="cuda").as_strided(t.shape, (t[0].numel() - 1, *t.stride()[1:]))
+        for call in (lambda: c.append(rows, shared(x), x), lambda: c.append(rows, x, shared(x)), lambda: c.append(rows, x, x, q=shared(q)),
+                     lambda: c.append(rows, shared(x.view(4, 128)), x), lambda: c.attention(rows, shared(q), 0.1),
+                     lambda: c.attention(rows, shared(q.view(4, 256)), 0.1)):
+            with pytest.raises(J.JfError, match="apart") as e:
+                call()
+            assert e.value.status == J.JF_EINVAL
+    one = rows_of([1], [20])
+    want = c.attention(one, q[:1], 0.1)
+    for stride in (0, 7, 10 ** 6):
+        assert torch.equal(c.attention(one, q.as_strided((1, 4, 64), (stride, 64, 1)), 0.1), want)
+    c.check()
