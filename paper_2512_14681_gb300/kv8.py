@@ -128,7 +128,6 @@ class Kv8Cache:
                             page_table.shape[0], k.shape[0], page_table.shape[1], k.shape[1], k.shape[3])
         self.err = torch.zeros(1, dtype=torch.int32, device=k.device)
         torch.cuda.current_stream(k.device).synchronize()  # zero for every stream
-        self._workspaces = {}  # by stream: calls on different streams may overlap
         self._need = {}
 
     @classmethod
@@ -219,9 +218,9 @@ class Kv8Cache:
             _checked(self.lib.jf_op_kv8_attention_workspace_bytes(C.byref(self.c), C.byref(rows.c), dtype, heads, C.byref(n)),
                      "jf_op_kv8_attention_workspace_bytes")
             need = self._need[key] = n.value
-        ws = self._workspaces.get(st)
-        if ws is None or ws.numel() < need:
-            ws = self._workspaces[st] = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
+        # A workspace of the call's own: PyTorch's allocator hands its memory to the stream's next call, but not to another
+        # stream, nor to a thread whose launches come between this call's two, nor (from a captured graph's pool) to anyone.
+        ws = torch.empty(need, dtype=torch.uint8, device=self.device)
         out = torch.empty(rows.n_rows, heads, self.head_dim, dtype=q.dtype, device=self.device)
         lse = torch.empty(rows.n_rows, heads, dtype=torch.float32, device=self.device) if want_lse else None
         _checked(self.lib.jf_op_kv8_attention(

@@ -15,8 +15,7 @@ import torch
 from . import _lib as J
 from .kv8 import _checked, _dtype, _on_stream, _raw_stream, _row_stride, _want
 
-_err = {}        # error word by device
-_workspaces = {}  # by (device, stream): calls on different streams may overlap
+_err = {}  # error word by device
 
 
 class TokenLogprobs(NamedTuple):
@@ -78,11 +77,7 @@ def token_logprobs(logits, targets, top: int = 0, scale: float = 1.0) -> TokenLo
     ids = torch.empty(rows, top, dtype=torch.int32, device=dev) if top else None
     lps = torch.empty(rows, top, dtype=torch.float32, device=dev) if top else None
     need = _need(rows, vocab, top)
-    ws = None
-    if need:
-        ws = _workspaces.get((dev, st))
-        if ws is None or ws.numel() < need:
-            ws = _workspaces[dev, st] = torch.empty(need, dtype=torch.uint8, device=dev)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # the call's own, as in Kv8Cache.attention
     _checked(lib.jf_op_token_logprobs(dtype, logits.data_ptr(), ld, rows, vocab, scale, tp, logprob.data_ptr(), entropy.data_ptr(),
                                       lse.data_ptr(), stats.data_ptr(), top, ids.data_ptr() if top else None,
                                       lps.data_ptr() if top else None, ws.data_ptr() if ws is not None else None,

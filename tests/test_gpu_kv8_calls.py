@@ -90,3 +90,79 @@ def test_rows_that_share_memory_are_refused(torch):
     for stride in (0, 7, 10 ** 6):
         assert torch.equal(c.attention(one, q.as_strided((1, 4, 64), (stride, 64, 1)), 0.1), want)
     c.check()
+
+
+def test_a_captured_call_keeps_its_memory(torch):
+    """Warmed up and captured on one stream; a larger eager call there, then fresh tensors: replays leave those alone, and
+    their results are right. Two graphs of the same capture stream replayed on two others at the same time."""
+    pool = fill(torch, 4, 128, [5000], seed=51)
+    c, st = pool.cache, torch.cuda.Stream()
+    q1, q2, big = (queries(torch, n, 28, 128, "bf16", s) for n, s in ((1, 1), (1, 2), (300, 3)))
+    r1, r2 = rows_of([1], [4000]), rows_of([1], [3000])
+    want1, want2 = c.attention(r1, q1, 0.1), c.attention(r2, q2, 0.1)
+    rb = rows_of([300], [4000])
+    torch.cuda.synchronize()
+    c.attention(r1, q1, 0.1, stream=st)
+    st.synchronize()
+    graphs, outs = [], []
+    for r, q in ((r1, q1), (r2, q2)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=st):
+            outs.append(c.attention(r, q, 0.1))
+    c.attention(rb, big, 0.1, stream=st)
+    st.synchronize()
+    with torch.cuda.stream(st):
+        fresh = [torch.full((1 << 18,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(64)]
+        fresh += [torch.full((1 << 22,), 0x5A, dtype=torch.uint8, device="cuda") for _ in range(16)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        graphs[0].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want1) and all((t == 0x5A).all() for t in fresh)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(50):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want1) and torch.equal(outs[1], want2)
+    c.check()
+
+
+def test_threads_on_one_stream(torch):
+    """Calls of several threads, whose launches may come in any order."""
+    import threading
+
+    pool = fill(torch, 4, 128, [6000, 900], seed=52)
+    work = [(rows_of([1, 1], [5000 + i, 100 * i + 7]), queries(torch, 2, 28, 128, "bf16", i)) for i in range(4)] + \
+        [(rows_of([20, 9], [5000 + i, 100 * i + 7]), queries(torch, 29, 28, 128, "bf16", i)) for i in range(4)]
+    want = [pool.cache.attention(r, q, 0.1) for r, q in work]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(i):
+        for _ in range(150):
+            if not torch.equal(pool.cache.attention(*work[i], 0.1), want[i]):
+                wrong.append(i)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(work))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+    pool.cache.check()
+
+
+def test_caches_hold_no_workspaces(torch):
+    """What a call needs beside its outputs goes back to the allocator: many caches cost no more than one."""
+    from paper_2512_14681_gb300.kv8 import Kv8Cache
+
+    caches = [Kv8Cache.empty(1, 1024, 2, 128) for _ in range(6)]
+    x, q = torch.randn(64, 2, 128, device="cuda"), queries(torch, 64, 12, 128, "bf16", 1)
+    before = torch.cuda.memory_allocated()
+    for c in caches:
+        c.append(rows_of([64], [0]), x, x)
+        c.attention(rows_of([64], [0]), q, 0.1)
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() - before < 1 << 20

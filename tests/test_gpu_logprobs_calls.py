@@ -28,3 +28,57 @@ def test_rows_that_share_memory_are_refused(torch, kind):
         one = L.token_logprobs(x.as_strided((1, 500), (stride, 1)), target[:1])
         assert torch.equal(one.logprob, r.logprob[:1])
     L.check()
+
+
+def test_a_captured_call_keeps_its_memory(torch):
+    """Captured on a warmed-up stream; a larger eager call there, then fresh tensors: replays leave those alone."""
+    from paper_2512_14681_gb300 import logprobs as L
+
+    x, target = torch.randn(1, 100000, device="cuda"), torch.tensor([5], dtype=torch.int32, device="cuda")
+    more = torch.randn(12, 150000, device="cuda")
+    want, st = L.token_logprobs(x, target, top=2), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    L.token_logprobs(x, target, top=2, stream=st)
+    st.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        got = L.token_logprobs(x, target, top=2)
+    L.token_logprobs(more, target.repeat(12), top=64, stream=st)
+    st.synchronize()
+    with torch.cuda.stream(st):
+        fresh = [torch.full((n,), 0x5A, dtype=torch.uint8, device="cuda") for n in (512, 1 << 12, 1 << 17, 1 << 19) for _ in range(40)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert all((t == 0x5A).all() for t in fresh)
+    L.check()
+
+
+def test_threads_on_one_stream(torch):
+    """Calls of several threads, whose launches may come in any order."""
+    import threading
+
+    from paper_2512_14681_gb300 import logprobs as L
+
+    x = [torch.randn(3, 60000, device="cuda") for _ in range(6)]
+    target = torch.tensor([5, 50000, -1], dtype=torch.int32, device="cuda")
+    want = [L.token_logprobs(v, target, top=9) for v in x]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(i):
+        for _ in range(150):
+            got = L.token_logprobs(x[i], target, top=9)
+            if not all(torch.equal(a, b) for a, b in zip(got, want[i])):
+                wrong.append(i)
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(len(x))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+    L.check()
