@@ -37,7 +37,9 @@ def _error_word(device):
 def check(device=None):
     """Raise what the device has reported since the last check (synchronises), and clear it: a target beyond the
     vocabulary."""
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    device = torch.device("cuda" if device is None else device)
+    if device.index is None:
+        device = torch.device(device.type, torch.cuda.current_device())
     word = _err.get(device)
     if word is not None and int(word.item()):
         word.zero_()

@@ -82,3 +82,15 @@ def test_threads_on_one_stream(torch):
         t.join()
     assert not wrong
     L.check()
+
+
+def test_check_takes_a_device_in_any_form(torch):
+    from paper_2512_14681_gb300 import _lib as J
+    from paper_2512_14681_gb300 import logprobs as L
+
+    x, beyond = torch.randn(1, 50, device="cuda"), torch.tensor([50], dtype=torch.int32, device="cuda")
+    for device in (None, "cuda", "cuda:0", torch.device("cuda"), torch.device("cuda", 0)):
+        L.token_logprobs(x, beyond)
+        with pytest.raises(J.JfError, match="vocabulary"):
+            L.check(device)
+        L.check(device)
