@@ -9,7 +9,7 @@ memory comes from PyTorch.
     rows = Rows.of(new=[32], lens=[1000])                 # 32 new tokens behind 1000 cached ones
     q = cache.append(rows, k, v, q=q, rope=rope_table(4096, 128, 1e6))
     out = cache.attention(rows, q, scale=128 ** -0.5)
-    cache.check()                                         # what the device reported (synchronises)
+    cache.check()                                         # what the device reported (waits for it)
 """
 from __future__ import annotations
 
@@ -230,7 +230,8 @@ class Kv8Cache:
         return (out, lse) if want_lse else out
 
     def check(self):
-        """Raise what the device has reported since the last check (synchronises), and clear it."""
+        """Raise what the device has reported since the last check (waits for all of its streams), and clear it."""
+        torch.cuda.synchronize(self.device)
         code = int(self.err.item())
         if code:
             self.err.zero_()

@@ -35,13 +35,16 @@ def _error_word(device):
 
 
 def check(device=None):
-    """Raise what the device has reported since the last check (synchronises), and clear it: a target beyond the
-    vocabulary."""
+    """Raise what the device has reported since the last check (waits for all of its streams), and clear it: a target
+    beyond the vocabulary."""
     device = torch.device("cuda" if device is None else device)
     if device.index is None:
         device = torch.device(device.type, torch.cuda.current_device())
     word = _err.get(device)
-    if word is not None and int(word.item()):
+    if word is None:
+        return
+    torch.cuda.synchronize(device)
+    if int(word.item()):
         word.zero_()
         raise J.JfError(J.JF_EDEVICE, "a target was beyond the vocabulary")
 

@@ -166,3 +166,17 @@ def test_caches_hold_no_workspaces(torch):
         c.attention(rows_of([64], [0]), q, 0.1)
     torch.cuda.synchronize()
     assert torch.cuda.memory_allocated() - before < 1 << 20
+
+
+def test_check_waits_for_every_stream(torch):
+    from paper_2512_14681_gb300._lib import JfError
+
+    pool = fill(torch, 2, 64, [40], seed=1)
+    q, st = torch.ones(1, 4, 64, device="cuda"), torch.cuda.Stream()
+    beyond = rows_of([1], [10 ** 6])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(200_000_000)
+    pool.cache.attention(beyond, q, 0.1, stream=st)
+    with pytest.raises(JfError, match="out of range"):
+        pool.cache.check()

@@ -94,3 +94,19 @@ def test_check_takes_a_device_in_any_form(torch):
         with pytest.raises(J.JfError, match="vocabulary"):
             L.check(device)
         L.check(device)
+
+
+def test_check_waits_for_every_stream(torch):
+    from paper_2512_14681_gb300 import _lib as J
+    from paper_2512_14681_gb300 import logprobs as L
+
+    x, beyond = torch.randn(1, 50, device="cuda"), torch.tensor([50], dtype=torch.int32, device="cuda")
+    L.token_logprobs(x, beyond)
+    with pytest.raises(J.JfError):
+        L.check()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(200_000_000)
+    L.token_logprobs(x, beyond, stream=st)
+    with pytest.raises(J.JfError, match="vocabulary"):
+        L.check()
