@@ -28,10 +28,12 @@ class TokenLogprobs(NamedTuple):
 
 
 def _error_word(device):
-    if device not in _err:
-        _err[device] = torch.zeros(1, dtype=torch.int32, device=device)
+    word = _err.get(device)
+    if word is None:
+        word = torch.zeros(1, dtype=torch.int32, device=device)
         torch.cuda.current_stream(device).synchronize()  # zero for every stream
-    return _err[device]
+        word = _err.setdefault(device, word)  # (the first of several threads')
+    return word
 
 
 def check(device=None):

@@ -110,3 +110,27 @@ def test_check_waits_for_every_stream(torch):
     L.token_logprobs(x, beyond, stream=st)
     with pytest.raises(J.JfError, match="vocabulary"):
         L.check()
+
+
+def test_threads_share_the_first_error_word(torch, monkeypatch):
+    """Threads whose first calls come together report into the word that check() reads."""
+    import threading
+    import time
+
+    from paper_2512_14681_gb300 import logprobs as L
+
+    zeros, device = torch.zeros, torch.device("cuda", torch.cuda.current_device())
+    monkeypatch.setattr(L, "_err", {})
+    monkeypatch.setattr(torch, "zeros", lambda *a, **k: (time.sleep(0.05), zeros(*a, **k))[1])
+    got, start = [], threading.Barrier(8)
+
+    def first():
+        start.wait()
+        got.append(L._error_word(device).data_ptr())
+
+    threads = [threading.Thread(target=first) for _ in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert set(got) == {L._err[device].data_ptr()}
