@@ -60,6 +60,16 @@ def _on_stream(call):
     return wrapped
 
 
+def _take_error(word) -> int:
+    """The code in an error word, once all of its device's streams are done; the word is clear for each of them after."""
+    torch.cuda.synchronize(word.device)
+    code = int(word.item())
+    if code:
+        word.zero_()
+        torch.cuda.current_stream(word.device).synchronize()  # (a later report must not be cleared with this one)
+    return code
+
+
 def _row_stride(t, width, name):
     """Elements from row to row of t, whose rows are `width` long and must not share memory (a broadcast row does)."""
     if t.shape[0] <= 1:
@@ -231,8 +241,6 @@ class Kv8Cache:
 
     def check(self):
         """Raise what the device has reported since the last check (waits for all of its streams), and clear it."""
-        torch.cuda.synchronize(self.device)
-        code = int(self.err.item())
+        code = _take_error(self.err)
         if code:
-            self.err.zero_()
             raise J.JfError(J.JF_EDEVICE, DEVICE_CODES.get(code, f"device code {code}"))

@@ -13,7 +13,7 @@ from typing import NamedTuple
 import torch
 
 from . import _lib as J
-from .kv8 import _checked, _dtype, _on_stream, _raw_stream, _row_stride, _want
+from .kv8 import _checked, _dtype, _on_stream, _raw_stream, _row_stride, _take_error, _want
 
 _err = {}  # error word by device
 
@@ -45,9 +45,7 @@ def check(device=None):
     word = _err.get(device)
     if word is None:
         return
-    torch.cuda.synchronize(device)
-    if int(word.item()):
-        word.zero_()
+    if _take_error(word):
         raise J.JfError(J.JF_EDEVICE, "a target was beyond the vocabulary")
 
 

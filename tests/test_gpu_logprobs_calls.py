@@ -134,3 +134,21 @@ def test_threads_share_the_first_error_word(torch, monkeypatch):
     for t in threads:
         t.join()
     assert set(got) == {L._err[device].data_ptr()}
+
+
+def test_check_clears_only_what_it_raised(torch, monkeypatch):
+    """A report on another stream right after check() is not cleared with the one before, however late the clearing runs."""
+    from paper_2512_14681_gb300 import _lib as J
+    from paper_2512_14681_gb300 import logprobs as L
+
+    x, beyond = torch.randn(1, 50, device="cuda"), torch.tensor([50], dtype=torch.int32, device="cuda")
+    zero = torch.Tensor.zero_
+    monkeypatch.setattr(torch.Tensor, "zero_", lambda t: (torch.cuda._sleep(100_000_000), zero(t))[1])
+    st = torch.cuda.Stream()
+    L.token_logprobs(x, beyond)
+    with pytest.raises(J.JfError):
+        L.check()
+    L.token_logprobs(x, beyond, stream=st)
+    with pytest.raises(J.JfError, match="vocabulary"):
+        L.check()
+    L.check()
