@@ -15,15 +15,15 @@ import argparse
 import numpy as np
 import torch
 
+from . import _lib as J
 from . import inputs as I
 from .jacobi import Context, op_gemm
-from .kv8 import Kv8Cache, Rows, rope_table
+from .kv8 import Kv8Cache, Rows, _take_error, rope_table
 from .logprobs import TokenLogprobs, token_logprobs, token_logprobs_grad
 from .logprobs import check as check_targets
 
 
-def _projection(W, x):
-    return op_gemm(W, x)[0]
+WAIT_CODES = (1, 2, 3)  # of jf_op_gemm: a wait on a copy, a product or an accumulator ran out
 
 
 class Scorer:
@@ -49,6 +49,12 @@ class Scorer:
         self.caches = [Kv8Cache.empty(n_seqs, max_ctx, Hkv, hd) for _ in self.layers]
         self.rope = rope_table(max_ctx, hd, shape.rope_theta)
         self.lens = [0] * n_seqs  # tokens that each sequence's pages hold
+        self.err = torch.zeros(1, dtype=torch.int32, device="cuda")  # of the projections
+
+    def _projection(self, W, x):
+        y, err, _ = op_gemm(W, x)
+        torch.maximum(self.err, err, out=self.err)
+        return y
 
     def _norm(self, x, gain):
         return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + self.shape.rms_eps) * gain).to(self.type)
@@ -61,15 +67,15 @@ class Scorer:
         rows = Rows.of([len(t) for t in tokens], self.lens)
         x = self.embedding[torch.tensor([t for seq in tokens for t in seq], device="cuda")].float()
         for w, cache in zip(self.layers, self.caches):
-            qkv = _projection(w["qkv"], self._norm(x, w["n1"]))
+            qkv = self._projection(w["qkv"], self._norm(x, w["n1"]))
             if "b" in w:
                 qkv = qkv + w["b"]
             q, k, v = qkv.split([Hq * hd, Hkv * hd, Hkv * hd], 1)
             q = cache.append(rows, k, v, q=q, rope=self.rope, positions=positions, q_dtype=self.type)
             att = cache.attention(rows, q, hd ** -0.5, mask=mask)
-            x = x + _projection(w["o"], att.view(-1, Hq * hd))
-            g, u = _projection(w["gu"], self._norm(x, w["n2"])).chunk(2, 1)
-            x = x + _projection(w["down"], (g * torch.sigmoid(g) * u).to(self.type))
+            x = x + self._projection(w["o"], att.view(-1, Hq * hd))
+            g, u = self._projection(w["gu"], self._norm(x, w["n2"])).chunk(2, 1)
+            x = x + self._projection(w["down"], (g * torch.sigmoid(g) * u).to(self.type))
         self.lens = [n + len(t) for n, t in zip(self.lens, tokens)]
         return self._norm(x, self.final_gain)
 
@@ -80,14 +86,14 @@ class Scorer:
         """Log probabilities of `targets` (the token after each new one; negative: none), rows of all sequences in order."""
         h = self.hidden(tokens)
         t = torch.tensor([t for seq in targets for t in seq], dtype=torch.int32, device="cuda")
-        return token_logprobs(_projection(self.head, h), t, top=top)
+        return token_logprobs(self._projection(self.head, h), t, top=top)
 
     def head_gradient(self, tokens, targets):
         """(mean negative log likelihood, its gradient by the head's matrix): one step of training the head on given
         tokens, as on the points of a recorded trajectory."""
         h = self.hidden(tokens)
         t = torch.tensor([t for seq in targets for t in seq], dtype=torch.int32, device="cuda")
-        logits = _projection(self.head, h)
+        logits = self._projection(self.head, h)
         n = max(1, sum(t >= 0 for seq in targets for t in seq))
         r = token_logprobs(logits, t)
         d = token_logprobs_grad(logits, t, r.row_stats, None, -1.0 / n, out=logits)
@@ -95,6 +101,9 @@ class Scorer:
 
     def check(self):
         """Raise what the device has reported (synchronises)."""
+        code = _take_error(self.err)
+        if code:
+            raise J.JfError(J.JF_ETIMEOUT if code in WAIT_CODES else J.JF_EDEVICE, f"a projection reported device code {code}")
         for c in self.caches:
             c.check()
         check_targets()
