@@ -79,9 +79,18 @@ def _row_stride(t, width, name):
     return t.stride(0)
 
 
-def _device_i32(t, n, name):
+_current_device = torch._C._cuda_getDevice
+
+
+def _on_current(device):
+    """Kernels are launched on the current device, in one of its streams."""
+    _want(device.index == _current_device(), "tensors on {}, which is not the current device", device)
+
+
+def _device_i32(t, n, name, device=None):
     _want(t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.numel() >= n,
           "{}: a contiguous int32 CUDA tensor of {} elements is wanted", name, n)
+    _want(device is None or t.device == device, "{}: a tensor on {} is wanted", name, device)
 
 
 def rope_table(n: int, head_dim: int, theta: float, device="cuda"):
@@ -103,7 +112,7 @@ class Rows:
     def __post_init__(self):
         n_seqs = self.len.numel()
         _device_i32(self.row_start, n_seqs + 1, "row_start")
-        _device_i32(self.len, n_seqs, "len")
+        _device_i32(self.len, n_seqs, "len", self.row_start.device)
         self.c = J.Kv8Rows(self.row_start.data_ptr(), self.len.data_ptr(), self.n_rows, self.max_rows)
 
     @classmethod
@@ -162,6 +171,7 @@ class Kv8Cache:
         return _row_stride(t, width, name)
 
     def _batch(self, rows):
+        _on_current(self.device)
         _want(rows.len.numel() == self.page_table.shape[0] and rows.len.device == self.device,
               "rows: as many sequences as the page table, on its device, are wanted")
 
@@ -187,7 +197,7 @@ class Kv8Cache:
                   rope.device == self.device, "rope: contiguous float32 [positions][head_dim / 2][2] is wanted")
             rope_len = rope.shape[0]
         if positions is not None:
-            _device_i32(positions, rows.n_rows, "positions")
+            _device_i32(positions, rows.n_rows, "positions", self.device)
         ptr = lambda t: t.data_ptr() if t is not None else None
         _checked(self.lib.jf_op_kv8_append(
             C.byref(self.c), C.byref(rows.c), _dtype(k.dtype), ptr(q), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, heads,
@@ -219,7 +229,7 @@ class Kv8Cache:
         if mask is not None:
             _want(mask.dim() == 2, "mask: [rows][words] is wanted")
             words = mask.shape[1]
-            _device_i32(mask, rows.n_rows * words, "mask")
+            _device_i32(mask, rows.n_rows * words, "mask", self.device)
         st = _raw_stream(self.device)
         key = (dtype, heads, rows.c.n_rows, rows.c.max_rows)
         need = self._need.get(key)

@@ -13,7 +13,7 @@ from typing import NamedTuple
 import torch
 
 from . import _lib as J
-from .kv8 import _checked, _dtype, _on_stream, _raw_stream, _row_stride, _take_error, _want
+from .kv8 import _checked, _dtype, _on_current, _on_stream, _raw_stream, _row_stride, _take_error, _want
 
 _err = {}  # error word by device
 
@@ -74,6 +74,7 @@ def token_logprobs(logits, targets, top: int = 0, scale: float = 1.0) -> TokenLo
     int32 [rows]; scale: inverse temperature; top: alternatives listed per row (at most 64)."""
     lib = J.load()
     ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
+    _on_current(dev)
     dtype = _dtype(logits.dtype)
     tp = _vector(targets, rows, torch.int32, dev, "targets")
     st = _raw_stream(dev)
@@ -98,6 +99,7 @@ def token_logprobs_grad(logits, targets, row_stats, entropy, grad_logprob, grad_
     grad_entropy: float32 [rows], a number, or None (0). out: where it goes (it may be `logits`)."""
     lib = J.load()
     ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
+    _on_current(dev)
     dtype = _dtype(logits.dtype)
     if out is None:
         out = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)

@@ -180,3 +180,28 @@ def test_check_waits_for_every_stream(torch):
     pool.cache.attention(beyond, q, 0.1, stream=st)
     with pytest.raises(JfError, match="out of range"):
         pool.cache.check()
+
+
+def test_tensors_of_another_device_are_refused(torch, monkeypatch):
+    """Every call whose tensors are not on the current device (a box of one GPU: the current device's number is replaced)."""
+    from paper_2512_14681_gb300 import _lib as J
+    from paper_2512_14681_gb300 import kv8, logprobs
+
+    pool = fill(torch, 2, 64, [40], seed=1)
+    c, rows = pool.cache, rows_of([4], [20])
+    x, q = torch.ones(4, 2, 64, device="cuda"), torch.ones(4, 4, 64, device="cuda")
+    z, t = torch.randn(4, 100, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    r = logprobs.token_logprobs(z, t)
+    monkeypatch.setattr(kv8, "_current_device", lambda: torch.cuda.current_device() + 1)
+    for call in (lambda: c.append(rows, x, x), lambda: c.read(rows), lambda: c.attention(rows, q, 0.1),
+                 lambda: logprobs.token_logprobs(z, t), lambda: logprobs.token_logprobs_grad(z, t, r.row_stats, r.entropy, 1.0)):
+        with pytest.raises(J.JfError, match="current device") as e:
+            call()
+        assert e.value.status == J.JF_EINVAL
+    monkeypatch.undo()
+    for bad in (dict(positions=torch.zeros(4, dtype=torch.int32)), dict(positions=torch.zeros(3, dtype=torch.int32, device="cuda"))):
+        with pytest.raises(J.JfError, match="positions"):
+            c.append(rows, x, x, **bad)
+    with pytest.raises(J.JfError, match="mask"):
+        c.attention(rows, q, 0.1, mask=torch.zeros(4, 1, dtype=torch.int32))
+    c.check()
