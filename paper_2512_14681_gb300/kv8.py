@@ -100,14 +100,26 @@ def rope_table(n: int, head_dim: int, theta: float, device="cuda"):
     return torch.stack([torch.cos(ang), torch.sin(ang)], -1).float().contiguous()
 
 
-@dataclass
-class Rows:
+class _Fixed:
+    """Attributes that are given once: calls go by the C structure that points into these tensors and would not follow."""
+    _fixed = ()
+
+    def __setattr__(self, name, value):
+        _want(name not in self._fixed or self.__dict__.get(name, value) is value,
+              "{} cannot be replaced (write into the tensor, or make another {})", name, type(self).__name__)
+        super().__setattr__(name, value)
+
+
+@dataclass(eq=False)
+class Rows(_Fixed):
     """New rows of a batch (jf_kv8_rows): sequence b has rows row_start[b] .. row_start[b+1]-1 at slots len[b] ...
     Both are int32 CUDA tensors that the kernels read when they run."""
     row_start: torch.Tensor
     len: torch.Tensor
     n_rows: int
     max_rows: int
+
+    _fixed = ("row_start", "len", "n_rows", "max_rows")
 
     def __post_init__(self):
         n_seqs = self.len.numel()
@@ -125,9 +137,11 @@ class Rows:
         return cls(torch.tensor(start, **i32), torch.tensor(list(lens), **i32), start[-1], max(new) if len(new) else 0)
 
 
-class Kv8Cache:
+class Kv8Cache(_Fixed):
     """k, v: [n_pages][n_kv_heads][16][head_dim] codes (uint8 or float8_e4m3fn); k_exp, v_exp: int8
     [n_pages][n_kv_heads]; page_table: int32 [n_seqs][pages_per_seq]. All contiguous CUDA tensors on one device."""
+
+    _fixed = ("k", "v", "k_exp", "v_exp", "page_table", "err")
 
     def __init__(self, k, v, k_exp, v_exp, page_table):
         for name, t in (("k", k), ("v", v)):

@@ -205,3 +205,21 @@ def test_tensors_of_another_device_are_refused(torch, monkeypatch):
     with pytest.raises(J.JfError, match="mask"):
         c.attention(rows, q, 0.1, mask=torch.zeros(4, 1, dtype=torch.int32))
     c.check()
+
+
+def test_tensors_that_calls_point_into_cannot_be_replaced(torch):
+    """An assignment would have no effect on calls, and let the tensor that they read be freed."""
+    from paper_2512_14681_gb300._lib import JfError
+
+    pool, rows = fill(torch, 2, 64, [40], seed=1), rows_of([4], [20])
+    for owner, names in ((pool.cache, ("k", "v", "k_exp", "v_exp", "page_table")), (rows, ("row_start", "len", "n_rows", "max_rows"))):
+        for name in names:
+            was = getattr(owner, name)
+            setattr(owner, name, was)
+            with pytest.raises(JfError, match=f"{name} cannot be replaced"):
+                setattr(owner, name, was.clone() if torch.is_tensor(was) else was + 1)
+            assert getattr(owner, name) is was
+    q = queries(torch, 4, 4, 64, "f32", 1)
+    before = pool.cache.attention(rows, q, 0.1)
+    pool.cache.page_table.copy_(pool.cache.page_table.clone())
+    assert torch.equal(pool.cache.attention(rows, q, 0.1), before)
