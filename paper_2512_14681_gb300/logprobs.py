@@ -71,7 +71,10 @@ def _vector(t, rows, dtype, device, name):
 @_on_stream
 def token_logprobs(logits, targets, top: int = 0, scale: float = 1.0) -> TokenLogprobs:
     """logits: CUDA [rows][vocab] (float32 or bfloat16, rows any distance apart but not one over the other); targets:
-    int32 [rows]; scale: inverse temperature; top: alternatives listed per row (at most 64)."""
+    int32 [rows]; scale: inverse temperature; top: alternatives listed per row (at most 64). No graph is recorded: logits
+    that a loss goes back through are given as logits.detach(), and get token_logprobs_grad's result by logits.backward()."""
+    if logits.requires_grad and torch.is_grad_enabled():
+        raise J.JfError(J.JF_EUNSUPPORTED, "logits require a gradient, which is not recorded: detach() them, and see token_logprobs_grad")
     lib = J.load()
     ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
     _on_current(dev)

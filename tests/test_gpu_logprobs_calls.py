@@ -152,3 +152,23 @@ def test_check_clears_only_what_it_raised(torch, monkeypatch):
     with pytest.raises(J.JfError, match="vocabulary"):
         L.check()
     L.check()
+
+
+def test_logits_that_require_a_gradient(torch):
+    """Refused where autograd would record (a loss would get nothing through the result); by hand they get theirs."""
+    from paper_2512_14681_gb300 import _lib as J
+    from paper_2512_14681_gb300 import logprobs as L
+
+    h, W = torch.randn(3, 16, device="cuda"), torch.randn(200, 16, device="cuda", requires_grad=True)
+    target = torch.tensor([5, 199, 0], dtype=torch.int32, device="cuda")
+    logits = h @ W.t()
+    with pytest.raises(J.JfError, match="gradient") as e:
+        L.token_logprobs(logits, target)
+    assert e.value.status == J.JF_EUNSUPPORTED
+    with torch.no_grad():
+        r = L.token_logprobs(logits, target)
+    assert torch.equal(r.logprob, L.token_logprobs(logits.detach(), target).logprob)
+    logits.backward(L.token_logprobs_grad(logits.detach(), target, r.row_stats, r.entropy, -1.0))
+    want, = torch.autograd.grad(-torch.log_softmax(h.double() @ W.double().t(), -1)[range(3), target.long()].sum(), W)
+    # (a gradient of a logit is off by 2e-5 of |hot - p| <= 1 at most, a sum over 3 rows of them in fp32 by 2^-22 of its terms)
+    assert ((W.grad - want).abs() <= 3e-5 * h.abs().sum(0)).all()
