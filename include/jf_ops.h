@@ -161,7 +161,8 @@ jf_status jf_op_token_logprobs(int dtype, const void* logits, long long ld, int 
  * entropy)). row_stats, entropy: jf_op_token_logprobs' outputs for the same logits, scale and targets (entropy
  * may be NULL without grad_entropy). grad_logits: [rows] of vocab values of the logits' dtype, rows ld_grad
  * elements apart; it may be logits itself (with ld_grad = ld). A negative target has no share of
- * grad_logprob; a logit of -infinity and a row without a token that can occur have gradient 0. */
+ * grad_logprob. A logit of -infinity (p_i = 0) has gradient 0, or, where it is the target, scale * grad_logprob;
+ * a row without a token that can occur has gradient 0. */
 jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld, int rows, int vocab, float scale,
                                     const int32_t* targets, const float* row_stats, const float* entropy,
                                     const float* grad_logprob, const float* grad_entropy, void* grad_logits,
