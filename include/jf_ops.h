@@ -69,7 +69,7 @@ jf_status jf_op_gemm_noalloc(const void* W, const void* X, float* Y, int N, int 
  *   k_exp, v_exp: [n_pages][n_kv_heads] exponents;
  *   page_table: [n_seqs][pages_per_seq]: page of tokens 16 i .. 16 i + 15 of a sequence at entry i
  *     (entries past a sequence's last token are not read).
- * head_dim 64 or 128; n_seqs <= 1024. All pointers DEVICE, all memory the caller's. Slots that no token
+ * head_dim 64 or 128; n_seqs <= 1024; n_kv_heads <= 32767. All pointers DEVICE, all memory the caller's. Slots that no token
  * was appended to may hold anything. */
 typedef struct {
   void *k, *v;

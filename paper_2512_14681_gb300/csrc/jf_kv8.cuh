@@ -6,7 +6,7 @@
 
 namespace jf {
 
-constexpr int kKv8MaxSeqs = 1024;
+constexpr int kKv8MaxSeqs = 1024, kKv8MaxHeads = 32767;  // (append's grid is twice as high as the KV heads with queries)
 constexpr int kKv8ExpMin = -120, kKv8ExpMax = 119;
 
 // 2^e in fp32 for -126 <= e <= 127
@@ -64,7 +64,7 @@ inline jf_status kv8_check(const jf_kv8_cache* c, const jf_kv8_rows* r) {
   if (r->n_rows > 0 && (r->max_rows < 1 || r->max_rows > r->n_rows)) return JF_EINVAL;
   if (c->pages_per_seq > (1 << 26)) return JF_EUNSUPPORTED;  // slots are 32-bit numbers
   if (((uintptr_t)c->k & 15) || ((uintptr_t)c->v & 15)) return JF_EINVAL;
-  if ((c->head_dim != 64 && c->head_dim != 128) || c->n_seqs > kKv8MaxSeqs || c->n_kv_heads > 65535) return JF_EUNSUPPORTED;
+  if ((c->head_dim != 64 && c->head_dim != 128) || c->n_seqs > kKv8MaxSeqs || c->n_kv_heads > kKv8MaxHeads) return JF_EUNSUPPORTED;
   return JF_OK;
 }
 
