@@ -1358,9 +1358,9 @@ __global__ void __launch_bounds__(T_THREADS, 1) k_kv8_attn_tile(const Kv8AttnPar
 // that kernel let this one in, so with up to 32 sequences only the states are left to read after the wait.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int HD, int TR, int CH, int UC, int RW>
-__global__ void __launch_bounds__(RW > 8 ? 32 * RW : 256) k_kv8_combine(const Kv8AttnParams a, int n) {
+__global__ void __launch_bounds__(256) k_kv8_combine(const Kv8AttnParams a, int n) {
   using P = Plan<TR, CH, UC>;
-  constexpr int D = HD / 32, CB_WARPS = RW > 8 ? RW : 8;
+  constexpr int D = HD / 32, CB_WARPS = 8;
   __shared__ float s_m[CB_WARPS], s_l[CB_WARPS], s_o[RW > 1 ? CB_WARPS : 1][HD];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % RW;
   pdl_launch_dependents();
