@@ -518,27 +518,28 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
         rescale(al[0], al[1]);
       }
       const float nb[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};
-      // ---- the rows' reference exponents: down for both pages together, so that one of large values and little weight
-      // before one of small values that outweigh it is added in a unit that holds it; up before each
+      // ---- the rows' reference exponents, before each page: down (before the first for both, so that one of large values and
+      // little weight is added in a unit that holds it when the other, of small values, outweighs it), then up
       const int ev_min = min(ev[0], ev[1]), ev_max = max(ev[0], ev[1]);
       if (i == 0) E[0] = E[1] = ev_min - W_EV_SET;
       const bool apart = __any_sync(0xffffffffu, ev_min < max(E[0], E[1]) || ev_max - min(E[0], E[1]) > W_EV_MAX);
-      if (apart && __any_sync(0xffffffffu, ev_min < E[0] || ev_min < E[1])) {
-        int to[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float most = 0.f;
-#pragma unroll
-          for (int j = 0; j < NT; ++j) most = fmaxf(most, fmaxf(fabsf(o[j][2 * k]), fabsf(o[j][2 * k + 1])));
-          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-          to[k] = ev_min < E[k] ? unit_down(E[k], ev_min - W_EV_SET, most) : E[k];
-        }
-        move_to(to);
-      }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        if (apart && __any_sync(0xffffffffu, ev[x] - E[0] > W_EV_MAX || ev[x] - E[1] > W_EV_MAX)) {
+        const int low = x == 0 ? ev_min : ev[1];
+        if (apart && __any_sync(0xffffffffu, low < max(E[0], E[1]))) {
+          int to[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            float most = 0.f;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) most = fmaxf(most, fmaxf(fabsf(o[j][2 * k]), fabsf(o[j][2 * k + 1])));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            to[k] = low < E[k] ? unit_down(E[k], low - W_EV_SET, most) : E[k];
+          }
+          move_to(to);
+        }
+        if (apart && __any_sync(0xffffffffu, ev[x] - min(E[0], E[1]) > W_EV_MAX)) {
           int to[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {

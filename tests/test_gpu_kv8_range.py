@@ -145,3 +145,21 @@ def test_weights_that_fall_while_values_grow(torch, dtype, n, Hq, Hkv, hd, gap):
     q = torch.zeros(n, Hq, hd, device="cuda", dtype=torch.bfloat16 if dtype == "bf16" else torch.float32)
     q[:, :, 0] = 1.0
     check_attention(torch, pool, q, [n], [total - n], float(np.log(2.0)))
+
+
+@pytest.mark.parametrize("dtype,n,Hq,Hkv,hd", FORMS)
+@pytest.mark.parametrize("apart", [20, 30, 40])
+@pytest.mark.parametrize("order", [(0, 1), (1, 0)])
+def test_small_pages_keep_their_share(torch, dtype, n, Hq, Hkv, hd, apart, order):
+    """Equal weights; every second page's exponent is `apart` larger, but its values are the smallest codes in all dims but
+    one: there the other pages, all of the largest code, hold up to 2^-2 of the output. (The scores are 0, so that nothing
+    but the sums rounds.)"""
+    for total in (n + 31, 150 + n, 1024):
+        pool = fill(torch, Hkv, hd, [total], seed=total)
+        for p in range(-(-total // PAGE)):
+            big, at = p % 2 == order[0], pages_of(torch, pool, p)
+            pool.cache.v_exp[at] = 0 if big else -apart
+            pool.cache.v[at] = 1 if big else 0x7E
+            if big:
+                pool.cache.v[at, :, :, 5] = 0x7E
+        check_attention(torch, pool, queries(torch, n, Hq, hd, dtype, 4, 0.0), [n], [total - n], hd ** -0.5)
