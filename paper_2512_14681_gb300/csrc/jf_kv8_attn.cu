@@ -284,8 +284,8 @@ JF_DEV float2 pow2_pair(int e) {
 // NS: fp16 terms of queries and probabilities (1 for bf16 models, 2 for fp32).
 //
 // Bound by the codes' bytes where there are many: 16 sequences of one token, 28 query heads on 4 KV heads of 128, over
-// 301 to 32,768 tokens each (231 MB of codes) take 47 us with the join, 4.9 TB/s; the kernel alone reads at 5.1 TB/s,
-// with a third of the issue slots and a third of the warp-level tensor rate taken by fragments that hold 7 rows of 16.
+// 301 to 32,768 tokens each (231 MB of codes) take 47 us with the join, 4.9 TB/s,
+// with 37% of the issue slots and 31% of the warp-level tensor rate taken by fragments that hold 7 rows of 16.
 // One sequence over 1,024 tokens takes 9.7 us, the length of the chain lengths -> page table -> codes -> scores -> sums
 // -> join.
 // ---------------------------------------------------------------------------------------------
@@ -655,19 +655,20 @@ __global__ void __launch_bounds__(32 * W_WARPS, 2) k_kv8_attn_rows(const Kv8Attn
 // of the converters; warps 8-10 convert them to fp16 and store them as the images of tensor-core
 // operands: per page of 16 keys two 8-key groups, each of HD / 64 halves of 8 rows x 128 bytes with the 128-byte
 // swizzle; K is read K-major, V MN-major. Exponents stay out of the operands: K's go into the scores, V's into P as in
-// the warp-level form, against the chunk's reference E. Where a chunk's value exponents lie further apart than P
-// can carry, its pages go in groups, one step of the stream each (Kv8Info).
+// the warp-level form, against the chunk's reference E, which the rows' own units follow where they can. Where a chunk's
+// value exponents lie further apart than P can carry, its pages go in groups, one step of the stream each (Kv8Info). A
+// warp's rows share their unit unless they differ: decided row by row in every step, 512 rows over 65,536 tokens took 485 us.
 //
 // K and V of a chunk are converted into a ring of three operands, so that the converters are done with a chunk before its
 // products are due. Bound by a stream's chain: of about 4,600 cycles a chunk, 1,900 are the softmax of 128 x 128 scores and the
 // rest the products (2 x 8 of 64 cycles each, 300 before the first is complete) and the waits between them; the streams share the
 // tensor core, which is busy for half of that time. Neither the exponentials (without them the time is the same), nor
 // conversion (half its stores left out: the same), nor the codes' bytes bound it. Times with the join, 28 query heads on 4 KV
-// heads of 128: 512 rows over 8,192 tokens (62 GFLOP) 97 us, 0.64 PFLOP/s, over 65,536 460 us, 1.05 PFLOP/s; 32 rows over 32,768
-// 35 us, of which about 16 are the launch, the first chunk's loads and the join. Measured and not kept: chunks of 64 keys with
+// heads of 128: 512 rows over 8,192 tokens (62 GFLOP) 97 us, 0.64 PFLOP/s, over 65,536 463 us, 1.04 PFLOP/s; 32 rows over 32,768
+// 36 us, of which about 16 are the launch, the first chunk's loads and the join. Measured and not kept: chunks of 64 keys with
 // two score accumulators a stream and a warp of its own for the products, 129 us for the first of these (its other step then
-// 110); 16 softmax warps, each half of a row's keys, the same within 4% and spills at 96 registers; the streams taking turns with
-// their products, the same.
+// 110; several tests of many chunks failed, so that the time may be of a wrong kernel); 16 softmax warps, each half of a row's
+// keys, the same within 4% and spills at 96 registers; the streams taking turns with their products, the same.
 // ---------------------------------------------------------------------------------------------
 // (T_UC 2 / 4: 512 rows over 8,192 tokens 99.9 / 97.0 us, four sequences of 32 rows over 4,096 31.0 / 28.5, eight of 16 over 100
 // to 2,000 19.5 / 21.7.)

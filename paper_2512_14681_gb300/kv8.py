@@ -3,7 +3,7 @@
 A block of the cache (a page of 16 tokens, one KV head) holds e4m3 codes and one exponent: x ~ code * 2^e. append()
 rotates and rounds new rows into it, attention() reads it, read() gives back the values that it stands for. Every
 method marshals arguments and calls one C entry point, on the current stream or the one given as stream=; device
-memory comes from PyTorch.
+memory comes from PyTorch. No graph is recorded for autograd: results depend on their inputs' values only.
 
     cache = Kv8Cache.empty(n_seqs=1, max_ctx=4096, n_kv_heads=4, head_dim=128)
     rows = Rows.of(new=[32], lens=[1000])                 # 32 new tokens behind 1000 cached ones
