@@ -131,7 +131,8 @@ jf_status jf_op_kv8_attention_workspace_bytes(const jf_kv8_cache* cache, const j
  * reaches that row's outputs only.
  * Softmax statistics and sums are fp32. JF_BF16: products of fp16 operands (codes exactly; queries scaled
  * by a power of two per row, exact above 2^-29 of the row's largest; probabilities rounded to 11 bits).
- * JF_F32: queries and probabilities as two fp16 terms. Results do not depend on the order in which CTAs
+ * JF_F32: queries and probabilities as two fp16 terms. In both, a key whose weight is below 2^-25 of the
+ * row's largest may add nothing to out (lse counts it). Results do not depend on the order in which CTAs
  * run; they depend in rounding on the batch, whose work is split evenly over the GPU. */
 jf_status jf_op_kv8_attention(const jf_kv8_cache* cache, const jf_kv8_rows* rows, int dtype, const void* q, long long ld_q,
                               int n_heads, float scale, const uint32_t* mask, int mask_words, void* out, float* lse,
