@@ -126,9 +126,9 @@ jf_status jf_op_kv8_attention_workspace_bytes(const jf_kv8_cache* cache, const j
  * elements apart (rotated: jf_op_kv8_append's q_out); out: [n_rows][n_heads][head_dim], 16-byte aligned.
  * mask NULL: row i of a sequence sees slots 0 .. len + i. Else mask is [n_rows][mask_words] 32-bit words,
  * 32 * mask_words >= max_rows: the row sees slots 0 .. len - 1, and slot len + j if bit j % 32 of word j / 32
- * is set (a tree of drafts and candidates); a word that the mask does not have counts as 0. lse (optional): fp32 [n_rows][n_heads], the natural logarithm of
- * the sum of exponentials. A row that sees nothing gets out 0 and lse -infinity; a NaN in a row's query
- * reaches that row's outputs only.
+ * is set (a tree of drafts and candidates); a word that the mask does not have counts as 0. lse (optional):
+ * fp32 [n_rows][n_heads], the natural logarithm of the sum of exponentials. A row that sees nothing gets out 0
+ * and lse -infinity; a NaN in a row's query reaches that row's outputs only.
  * Softmax statistics and sums are fp32. JF_BF16: products of fp16 operands (codes exactly; queries scaled
  * by a power of two per row, exact above 2^-29 of the row's largest; probabilities rounded to 11 bits).
  * JF_F32: queries and probabilities as two fp16 terms. In both, a key whose weight is below 2^-25 of the
