@@ -5,6 +5,8 @@
  * 2512.14681, Sec. 2.1 Eq. 3: one pass over all in-flight rows). jf_op_kv8_* keep and read a paged
  * cache held in 8 bits, and jf_op_token_logprobs* score given tokens and give the gradient of that
  * score: a draft's or trajectory's tokens over a long context, and the loss of training on them.
+ * jf_op_policy_loss is such a loss with its gradient, and jf_op_packed_attention* attention of a batch of
+ * whole texts, without a cache, with its backward pass.
  * Same conventions as jf.h: plain pointers, the caller owns all memory, work is ordered on
  * `cuda_stream` (NULL = legacy default stream) and the call does not synchronise; arguments are
  * validated on the host before any launch. `err_word`: device int that receives a device error code
@@ -168,6 +170,71 @@ jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld,
                                     const int32_t* targets, const float* row_stats, const float* entropy,
                                     const float* grad_logprob, const float* grad_entropy, void* grad_logits,
                                     long long ld_grad, int* err_word, void* cuda_stream);
+
+/* The clipped policy loss of given tokens, and its gradient. Logits, scale and targets as in jf_op_token_logprobs; with lp
+ * the target's log probability, x = lp - old_logprob, ratio = e^x, A = advantage, d = ref_logprob - lp, H the row's entropy,
+ *   loss = weight * (-min(ratio * A, min(max(ratio, 1 - below), 1 + above) * A) + kl * (e^d - 1 - d) - entropy * H).
+ * The gradient is that of the sum of all losses by the logits; where both sides of a min or max are equal, the ratio's own.
+ * old_logprob NULL: ratio 1, with the gradient of lp; ref_logprob NULL: kl must be 0; weight NULL: 1. All device fp32 [rows].
+ * Outputs, device fp32 [rows], each optional: loss, logprob (lp), entropy (H), ratio, kl (e^d - 1 - d). grad_logits
+ * (optional): [rows] of vocab values of the logits' dtype, rows ld_grad elements apart; it may be logits itself (with
+ * ld_grad = ld).
+ * A negative target leaves its row out: loss, logprob, ratio, kl and gradient 0 (entropy is the row's). A weight of 0 makes
+ * loss and gradient 0 whatever the other terms are, and an advantage of 0 the first term. A target that cannot occur
+ * (a logit of -infinity) has ratio 0 and, with a ref_logprob, an infinite kl without a gradient. Rows without a token that can occur, NaN
+ * among the logits and targets >= vocab: as in jf_op_token_logprobs (the loss of the last is NaN, its gradient 0). A ratio
+ * beyond the range of fp32 is infinite, as loss and gradient then are where A is negative.
+ * workspace: device, 16-byte aligned, no initialisation needed; calls that may overlap on the GPU need one each. */
+typedef struct {
+  float below, above; /* how far the ratio counts on either side of 1: 0 <= below <= 1, 0 <= above */
+  float kl, entropy;  /* factors of the two other terms */
+} jf_policy_terms;
+jf_status jf_op_policy_loss_workspace_bytes(int dtype, int rows, int vocab, size_t* out_bytes);
+jf_status jf_op_policy_loss(const jf_policy_terms* terms, int dtype, const void* logits, long long ld, int rows, int vocab,
+                            float scale, const int32_t* targets, const float* old_logprob, const float* ref_logprob,
+                            const float* advantage, const float* weight, float* loss, float* logprob, float* entropy,
+                            float* ratio, float* kl, void* grad_logits, long long ld_grad, void* workspace,
+                            size_t workspace_bytes, int* err_word, void* cuda_stream);
+
+/* A batch of texts that lie one behind the other in the rows of a call: text b has rows row_start[b] .. row_start[b+1]-1
+ * (it may have none). row_start [n_seqs + 1] is a DEVICE array, ascending within 0 .. n_rows, read when the kernels run (a
+ * captured graph follows it); n_rows and max_rows (no text is longer) are host numbers. Texts that are not so are reported
+ * through err_word (as JF_EDEVICE's bounds code 4), and the call then computes nothing. Rows before the first text and
+ * behind the last belong to none: their outputs and gradients are 0, their lse -infinity, and what they hold is used
+ * nowhere. n_seqs <= 1024. */
+typedef struct {
+  const int32_t* row_start;
+  int n_seqs, n_rows, max_rows;
+} jf_packed;
+
+/* Device workspace bytes of the two calls below on the current device (backward: 0 or 1; no initialisation needed; calls
+ * that may overlap on the GPU need one each). */
+jf_status jf_op_packed_attention_workspace_bytes(const jf_packed* texts, int dtype, int n_heads, int n_kv_heads, int head_dim,
+                                                 int backward, size_t* out_bytes);
+
+/* Causal attention of packed texts without a cache (prompts, trajectories, a training batch): out = softmax(scale * q k^T) v
+ * for each of n_heads query heads (head h reads KV head h / (n_heads / n_kv_heads), at most 128 heads each), row i of a text
+ * over its rows 0 .. i. dtype (JF_BF16 or JF_F32): type of everything but lse; head_dim 64 or 128. q, k, v: rows of n_heads
+ * or n_kv_heads heads, ld_* elements apart, so that the three may be parts of one projection's rows; bf16 rows are read by tensor copies where
+ * their addresses and ld_* are multiples of 16 bytes, by slower kernels otherwise. out: [n_rows][n_heads][head_dim], 16-byte aligned; lse (optional
+ * here): fp32 [n_rows][n_heads], the natural logarithm of the sum of exponentials.
+ * Softmax statistics and sums are fp32; JF_BF16 rounds the probabilities (relative to a row's running maximum) to bf16
+ * before their product with v. A NaN or an infinity in a text reaches rows of that text only. Results do not depend on the
+ * order in which CTAs run; they depend in rounding on the batch, whose work is split evenly over the GPU. */
+jf_status jf_op_packed_attention(const jf_packed* texts, int dtype, const void* q, long long ld_q, const void* k,
+                                 long long ld_k, const void* v, long long ld_v, int n_heads, int n_kv_heads, int head_dim,
+                                 float scale, void* out, float* lse, void* workspace, size_t workspace_bytes, int* err_word,
+                                 void* cuda_stream);
+
+/* Its backward pass: the gradients dq, dk, dv of a loss by q, k, v from that by out, d_out (rows ld_do elements apart), for
+ * the same texts, q, k, v and scale and that call's out and lse. dq, dk, dv: rows ld_* elements apart (so that they may be
+ * parts of one buffer's rows); they may not overlap the inputs. dk and dv of a KV head are sums over its query heads. No
+ * atomics: the order of every sum is fixed. JF_BF16 rounds probabilities and the scores' gradients to bf16 before their products. */
+jf_status jf_op_packed_attention_grad(const jf_packed* texts, int dtype, const void* q, long long ld_q, const void* k,
+                                      long long ld_k, const void* v, long long ld_v, int n_heads, int n_kv_heads, int head_dim,
+                                      float scale, const void* out, const float* lse, const void* d_out, long long ld_do,
+                                      void* dq, long long ld_dq, void* dk, long long ld_dk, void* dv, long long ld_dv,
+                                      void* workspace, size_t workspace_bytes, int* err_word, void* cuda_stream);
 
 #ifdef __cplusplus
 }

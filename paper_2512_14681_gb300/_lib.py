@@ -28,7 +28,8 @@ EXPORTS = [
     "jf_op_gemm_workspace_bytes", "jf_op_gemm", "jf_op_gemm_noalloc", "jf_tl_enable", "jf_trajectory_noisy_blocks",
     "jf_set_wait_limit", "jf_wait_limit_probe", "jf_op_kv8_append", "jf_op_kv8_read",
     "jf_op_kv8_attention_workspace_bytes", "jf_op_kv8_attention", "jf_op_token_logprobs_workspace_bytes",
-    "jf_op_token_logprobs", "jf_op_token_logprobs_grad",
+    "jf_op_token_logprobs", "jf_op_token_logprobs_grad", "jf_op_policy_loss_workspace_bytes", "jf_op_policy_loss",
+    "jf_op_packed_attention_workspace_bytes", "jf_op_packed_attention", "jf_op_packed_attention_grad",
 ]
 JF_OP_GEMM_NOALLOC_SCRATCH_BYTES = 8 << 20
 
@@ -81,6 +82,14 @@ class Kv8Rows(C.Structure):
     _fields_ = [("row_start", C.c_void_p), ("len", C.c_void_p), ("n_rows", C.c_int), ("max_rows", C.c_int)]
 
 
+class PolicyTerms(C.Structure):
+    _fields_ = [("below", C.c_float), ("above", C.c_float), ("kl", C.c_float), ("entropy", C.c_float)]
+
+
+class Packed(C.Structure):
+    _fields_ = [("row_start", C.c_void_p), ("n_seqs", C.c_int), ("n_rows", C.c_int), ("max_rows", C.c_int)]
+
+
 _lib = None
 
 
@@ -129,6 +138,13 @@ def load():
     L.jf_op_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32, P(C.c_size_t)]
     L.jf_op_token_logprobs.argtypes = [i32, vp, ll, i32, i32, f32, vp, vp, vp, vp, vp, i32, vp, vp, vp, C.c_size_t, vp, vp]
     L.jf_op_token_logprobs_grad.argtypes = [i32, vp, ll, i32, i32, f32, vp, vp, vp, vp, vp, vp, ll, vp, vp]
+    pt, pk, sz = P(PolicyTerms), P(Packed), C.c_size_t
+    L.jf_op_policy_loss_workspace_bytes.argtypes = [i32, i32, i32, P(sz)]
+    L.jf_op_policy_loss.argtypes = [pt, i32, vp, ll, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ll, vp, sz, vp, vp]
+    L.jf_op_packed_attention_workspace_bytes.argtypes = [pk, i32, i32, i32, i32, i32, P(sz)]
+    L.jf_op_packed_attention.argtypes = [pk, i32, vp, ll, vp, ll, vp, ll, i32, i32, i32, f32, vp, vp, vp, sz, vp, vp]
+    L.jf_op_packed_attention_grad.argtypes = [pk, i32, vp, ll, vp, ll, vp, ll, i32, i32, i32, f32, vp, vp, vp, ll, vp, ll, vp, ll, vp, ll,
+                                              vp, sz, vp, vp]
     for name in EXPORTS:
         f = getattr(L, name)
         if name not in ("jf_destroy", "jf_last_error"):

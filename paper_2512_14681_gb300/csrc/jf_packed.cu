@@ -1,0 +1,499 @@
+// Causal attention of packed texts and its backward pass (jf_ops.h: jf_op_packed_attention*): entry points, and the
+// kernels on CUDA cores, for fp32 and for bf16 rows that tensor copies cannot read.
+//
+// For a query row i of a text, s_ij = scale q_i . k_j over its rows j <= i, lse_i = log sum_j e^s_ij, p_ij = e^(s_ij - lse_i):
+//   out_i = sum_j p_ij v_j
+//   delta_i = d_out_i . out_i,  ds_ij = p_ij (d_out_i . v_j - delta_i)
+//   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij d_out_i
+// where a KV head's sums run over the rows of all query heads that read it. Forward: one pass over the keys with the running
+// maximum and sum. Backward: p is computed again from lse; one kernel holds a tile of keys and walks over the queries for
+// dk and dv, another holds queries and walks over the keys for dq, so that every sum has one owner and one order.
+#include "jf_once.h"
+#include "jf_packed.cuh"
+
+namespace jf {
+namespace {
+
+constexpr int PF_T = 64, PF_THREADS = 256;  // rows of a tile (of queries, of keys)
+
+// Values of `rows` rows from p on (row `ld` apart, HD long) as fp32 rows of HD + 4 in shared memory; rows up to PF_T are zeros.
+template <typename T, int HD>
+JF_DEV void pf_load(float* dst, const T* p, long long ld, int rows, bool by16) {
+  constexpr int N = 16 / sizeof(T), C = HD / N;
+  for (int i = threadIdx.x; i < PF_T * C; i += PF_THREADS) {
+    const int r = i / C, c = i % C * N;
+    float x[N];
+    const T* src = p + r * ld + c;
+    if (r >= rows) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = 0.f;
+    } else if (by16) {
+      const uint4 w = *reinterpret_cast<const uint4*>(src);
+      const T* t = reinterpret_cast<const T*>(&w);
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = act_to_f32(t[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = act_to_f32(src[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(dst + r * (HD + 4) + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+  }
+}
+
+// s[i][j] = a row (ty + 16 i) . b row (tx + 16 j)
+template <int HD>
+JF_DEV void pf_dots(const float* a, const float* b, int ty, int tx, float (&s)[4][4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+  for (int d = 0; d < HD; d += 4) {
+    float4 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * (HD + 4) + d);
+      y[i] = *reinterpret_cast<const float4*>(b + (tx + 16 * i) * (HD + 4) + d);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        s[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, s[i][j]))));
+  }
+}
+
+// o[i][.] += sum_c w[ty + 16 i][c] b[c][dims 4 tx + 64 j ..], w in rows of PF_T + 4
+template <int HD>
+JF_DEV void pf_rows_by(const float* w, const float* b, int ty, int tx, float (&o)[4][HD / 16]) {
+#pragma unroll 2
+  for (int c = 0; c < PF_T; c += 4) {
+    float4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * (PF_T + 4) + c);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int j = 0; j < HD / 64; ++j) {
+        const float4 y = *reinterpret_cast<const float4*>(b + (c + k) * (HD + 4) + 4 * tx + 64 * j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = k == 0 ? x[i].x : (k == 1 ? x[i].y : (k == 2 ? x[i].z : x[i].w));
+          o[i][4 * j] = fmaf(f, y.x, o[i][4 * j]);
+          o[i][4 * j + 1] = fmaf(f, y.y, o[i][4 * j + 1]);
+          o[i][4 * j + 2] = fmaf(f, y.z, o[i][4 * j + 2]);
+          o[i][4 * j + 3] = fmaf(f, y.w, o[i][4 * j + 3]);
+        }
+      }
+  }
+}
+
+// o[i][.] += sum_r w[r][4 ty + i] b[r][dims 4 tx + 64 j ..]
+template <int HD>
+JF_DEV void pf_columns_by(const float* w, const float* b, int ty, int tx, float (&o)[4][HD / 16]) {
+#pragma unroll 4
+  for (int r = 0; r < PF_T; ++r) {
+    const float4 x = *reinterpret_cast<const float4*>(w + r * (PF_T + 4) + 4 * ty);
+    const float f[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j) {
+      const float4 y = *reinterpret_cast<const float4*>(b + r * (HD + 4) + 4 * tx + 64 * j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        o[i][4 * j] = fmaf(f[i], y.x, o[i][4 * j]);
+        o[i][4 * j + 1] = fmaf(f[i], y.y, o[i][4 * j + 1]);
+        o[i][4 * j + 2] = fmaf(f[i], y.z, o[i][4 * j + 2]);
+        o[i][4 * j + 3] = fmaf(f[i], y.w, o[i][4 * j + 3]);
+      }
+    }
+  }
+}
+
+template <typename T>
+JF_DEV void pf_store4(T* p, float a, float b, float c, float d) {
+  p[0] = to_act<T>(a), p[1] = to_act<T>(b), p[2] = to_act<T>(c), p[3] = to_act<T>(d);
+}
+
+struct PfTile {
+  int row0, n, first;  // the text's first row and length; the tile's first row in it. n < 0: no tile
+};
+// The tile that CTA x of the grid has: text by text, PF_T rows each. Rows that belong to no text are cleared by `clear(row)`
+// on the way, each by one CTA of the grid.
+template <typename Clear>
+JF_DEV PfTile pf_tile(const PackedParams& a, Clear clear) {
+  __shared__ int s_at[kPackedMaxSeqs], s_bad, s_found;
+  if (threadIdx.x == 0) s_bad = 0, s_found = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.t.n_seqs; b += PF_THREADS) {
+    if (!packed_text_ok(a.t, b)) s_bad = 1;
+    s_at[b] = (a.t.row_start[b + 1] - a.t.row_start[b] + PF_T - 1) / PF_T;
+  }
+  __syncthreads();
+  if (s_bad) {
+    if (threadIdx.x == 0) jf_set_error(a.err, JF_DERR_BOUNDS);
+    return {0, -1, 0};
+  }
+  if (threadIdx.x < 32) {
+    int base = 0;
+    for (int b0 = 0; b0 < a.t.n_seqs; b0 += 32) {
+      const int b = b0 + (int)threadIdx.x, n = b < a.t.n_seqs ? s_at[b] : 0;
+      int sum = n;
+#pragma unroll
+      for (int sh = 1; sh < 32; sh <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, sum, sh);
+        if ((int)threadIdx.x >= sh) sum += u;
+      }
+      const int before = base + sum - n;
+      if ((int)blockIdx.x >= before && (int)blockIdx.x < before + n) {
+        s_found = b;
+        s_at[b] = blockIdx.x - before;
+      }
+      base += __shfl_sync(0xffffffffu, sum, 31);
+    }
+  }
+  const int head = a.t.row_start[0], tail = a.t.row_start[a.t.n_seqs];
+  for (int r = blockIdx.x; r < head; r += gridDim.x) clear(r);
+  for (int r = tail + blockIdx.x; r < a.t.n_rows; r += gridDim.x) clear(r);
+  __syncthreads();
+  const int b = s_found;
+  if (b < 0) return {0, -1, 0};
+  const int s0 = a.t.row_start[b];
+  return {s0, a.t.row_start[b + 1] - s0, s_at[b] * PF_T};
+}
+
+template <typename T>
+JF_DEV bool pf_by16(const void* p, long long ld) {
+  return ((uintptr_t)p & 15) == 0 && ld % (16 / (int)sizeof(T)) == 0;
+}
+
+// Grid (tiles, query heads).
+template <typename T, int HD>
+__global__ void __launch_bounds__(PF_THREADS, 1) k_packed_attn(const PackedParams a) {
+  extern __shared__ float sm[];
+  constexpr int TILE = PF_T * (HD + 4);
+  float *sq = sm, *sk = sm + TILE, *sv = sm + 2 * TILE, *sp = sm + 3 * TILE;
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16, h = blockIdx.y, kvh = h / (a.Hq / a.Hkv);
+  pdl_launch_dependents();
+  pdl_wait();
+  T* out = reinterpret_cast<T*>(a.out);
+  const PfTile t = pf_tile(a, [&](int r) {
+    for (int d = tid; d < HD; d += PF_THREADS) out[((long long)r * a.Hq + h) * HD + d] = to_act<T>(0.f);
+    if (tid == 0 && a.lse) a.lse[(long long)r * a.Hq + h] = -INFINITY;
+  });
+  if (t.n < 0) return;
+  const int rows = min(PF_T, t.n - t.first);
+  const bool q16 = pf_by16<T>(a.q, a.ld_q), k16 = pf_by16<T>(a.k, a.ld_k), v16 = pf_by16<T>(a.v, a.ld_v);
+  pf_load<T, HD>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + t.first) * a.ld_q + h * HD, a.ld_q, rows, q16);
+  float m[4], l[4], o[4][HD / 16] = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
+  const float c = a.scale * kLog2e;
+  for (int k0 = 0; k0 < t.first + rows; k0 += PF_T) {
+    __syncthreads();
+    pf_load<T, HD>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
+    pf_load<T, HD>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
+    __syncthreads();
+    float s[4][4];
+    pf_dots<HD>(sq, sk, ty, tx, s);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int qi = t.first + ty + 16 * i;
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = k0 + tx + 16 * j <= qi ? s[i][j] * c : -INFINITY;
+        mx = fmaxf(mx, s[i][j]);
+      }
+#pragma unroll
+      for (int sh = 8; sh; sh >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, sh));
+      mx = fmaxf(mx, m[i]);
+      const float base = mx == -INFINITY ? 0.f : mx, al = exp2f(m[i] - base);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = exp2f(s[i][j] - base);
+        sum += s[i][j];
+        sp[(ty + 16 * i) * (PF_T + 4) + tx + 16 * j] = s[i][j];
+      }
+#pragma unroll
+      for (int sh = 8; sh; sh >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
+      l[i] = l[i] * al + sum;
+      m[i] = mx;
+#pragma unroll
+      for (int d = 0; d < HD / 16; ++d) o[i][d] *= al;
+    }
+    __syncthreads();
+    pf_rows_by<HD>(sp, sv, ty, tx, o);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty + 16 * i;
+    if (r >= rows) continue;
+    const long long at = (long long)(t.row0 + t.first + r) * a.Hq + h;
+    const float il = l[i] > 0.f ? 1.f / l[i] : (l[i] == 0.f ? 0.f : l[i]);
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j)
+      pf_store4<T>(out + at * HD + 4 * tx + 64 * j, o[i][4 * j] * il, o[i][4 * j + 1] * il, o[i][4 * j + 2] * il, o[i][4 * j + 3] * il);
+    if (tx == 0 && a.lse) a.lse[at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
+  }
+}
+
+// delta[row][head] = d_out . out, a warp per (row, head); rows of no text as well (their d_out may be anything: not used).
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) k_packed_delta(const PackedParams a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const long long i = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (i >= (long long)a.t.n_rows * a.Hq) return;
+  const long long r = i / a.Hq;
+  const T* x = reinterpret_cast<const T*>(a.out) + i * HD;
+  const T* y = reinterpret_cast<const T*>(a.d_out) + r * a.ld_do + (i - r * a.Hq) * HD;
+  float s = 0.f;
+#pragma unroll
+  for (int d = lane; d < HD; d += 32) s = fmaf(act_to_f32(x[d]), act_to_f32(y[d]), s);
+  s = warp_sum(s);
+  if (lane == 0) a.delta[i] = s;
+}
+
+// p and ds of a 64 x 64 tile (queries from q0 on, keys from k0 on) into sp and sds.
+template <int HD>
+JF_DEV void pf_back_tile(const float* sq, const float* sdo, const float* sk, const float* sv, const float* s_lse, const float* s_delta,
+                         int q0, int k0, int n, float c, int ty, int tx, float* sp, float* sds) {
+  float s[4][4], dp[4][4];
+  pf_dots<HD>(sq, sk, ty, tx, s);
+  pf_dots<HD>(sdo, sv, ty, tx, dp);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty + 16 * i;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int kj = k0 + tx + 16 * j;
+      const bool sees = kj <= q0 + r && q0 + r < n;
+      const float p = sees ? exp2f(fmaf(s[i][j], c, -s_lse[r])) : 0.f;
+      if (sp) sp[r * (PF_T + 4) + tx + 16 * j] = p;
+      sds[r * (PF_T + 4) + tx + 16 * j] = sees ? p * (dp[i][j] - s_delta[r]) : 0.f;
+    }
+  }
+}
+
+// Grid (tiles of keys, KV heads): dk and dv.
+template <typename T, int HD>
+__global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dkv(const PackedParams a) {
+  extern __shared__ float sm[];
+  constexpr int TILE = PF_T * (HD + 4);
+  float *sq = sm, *sdo = sm + TILE, *sk = sm + 2 * TILE, *sv = sm + 3 * TILE, *sp = sm + 4 * TILE, *sds = sp + PF_T * (PF_T + 4);
+  __shared__ float s_lse[PF_T], s_delta[PF_T];
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16, kvh = blockIdx.y, G = a.Hq / a.Hkv;
+  pdl_launch_dependents();
+  pdl_wait();
+  T *dk = reinterpret_cast<T*>(a.dk), *dv = reinterpret_cast<T*>(a.dv);
+  const PfTile t = pf_tile(a, [&](int r) {
+    for (int d = tid; d < HD; d += PF_THREADS) dk[r * a.ld_dk + kvh * HD + d] = dv[r * a.ld_dv + kvh * HD + d] = to_act<T>(0.f);
+  });
+  if (t.n < 0) return;
+  const int rows = min(PF_T, t.n - t.first);
+  pf_load<T, HD>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + t.first) * a.ld_k + kvh * HD, a.ld_k, rows, pf_by16<T>(a.k, a.ld_k));
+  pf_load<T, HD>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + t.first) * a.ld_v + kvh * HD, a.ld_v, rows, pf_by16<T>(a.v, a.ld_v));
+  const bool q16 = pf_by16<T>(a.q, a.ld_q), do16 = pf_by16<T>(a.d_out, a.ld_do);
+  float gk[4][HD / 16] = {}, gv[4][HD / 16] = {};
+  for (int h = kvh * G; h < (kvh + 1) * G; ++h)
+    for (int q0 = t.first; q0 < t.n; q0 += PF_T) {
+      __syncthreads();
+      const int nq = min(PF_T, t.n - q0);
+      pf_load<T, HD>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + q0) * a.ld_q + h * HD, a.ld_q, nq, q16);
+      pf_load<T, HD>(sdo, reinterpret_cast<const T*>(a.d_out) + (t.row0 + q0) * a.ld_do + h * HD, a.ld_do, nq, do16);
+      if (tid < nq) {
+        s_lse[tid] = a.lse[(long long)(t.row0 + q0 + tid) * a.Hq + h] * kLog2e;
+        s_delta[tid] = a.delta[(long long)(t.row0 + q0 + tid) * a.Hq + h];
+      }
+      __syncthreads();
+      pf_back_tile<HD>(sq, sdo, sk, sv, s_lse, s_delta, q0, t.first, t.n, a.scale * kLog2e, ty, tx, sp, sds);
+      __syncthreads();
+      pf_columns_by<HD>(sp, sdo, ty, tx, gv);
+      pf_columns_by<HD>(sds, sq, ty, tx, gk);
+    }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * ty + i;
+    if (r >= rows) continue;
+    const long long at = t.row0 + t.first + r;
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j) {
+      const int d = kvh * HD + 4 * tx + 64 * j;
+      pf_store4<T>(dk + at * a.ld_dk + d, a.scale * gk[i][4 * j], a.scale * gk[i][4 * j + 1], a.scale * gk[i][4 * j + 2], a.scale * gk[i][4 * j + 3]);
+      pf_store4<T>(dv + at * a.ld_dv + d, gv[i][4 * j], gv[i][4 * j + 1], gv[i][4 * j + 2], gv[i][4 * j + 3]);
+    }
+  }
+}
+
+// Grid (tiles of queries, query heads): dq.
+template <typename T, int HD>
+__global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dq(const PackedParams a) {
+  extern __shared__ float sm[];
+  constexpr int TILE = PF_T * (HD + 4);
+  float *sq = sm, *sdo = sm + TILE, *sk = sm + 2 * TILE, *sv = sm + 3 * TILE, *sds = sm + 4 * TILE;
+  __shared__ float s_lse[PF_T], s_delta[PF_T];
+  const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16, h = blockIdx.y, kvh = h / (a.Hq / a.Hkv);
+  pdl_launch_dependents();
+  pdl_wait();
+  T* dq = reinterpret_cast<T*>(a.dq);
+  const PfTile t = pf_tile(a, [&](int r) {
+    for (int d = tid; d < HD; d += PF_THREADS) dq[r * a.ld_dq + h * HD + d] = to_act<T>(0.f);
+  });
+  if (t.n < 0) return;
+  const int rows = min(PF_T, t.n - t.first);
+  pf_load<T, HD>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + t.first) * a.ld_q + h * HD, a.ld_q, rows, pf_by16<T>(a.q, a.ld_q));
+  pf_load<T, HD>(sdo, reinterpret_cast<const T*>(a.d_out) + (t.row0 + t.first) * a.ld_do + h * HD, a.ld_do, rows, pf_by16<T>(a.d_out, a.ld_do));
+  if (tid < rows) {
+    s_lse[tid] = a.lse[(long long)(t.row0 + t.first + tid) * a.Hq + h] * kLog2e;
+    s_delta[tid] = a.delta[(long long)(t.row0 + t.first + tid) * a.Hq + h];
+  }
+  const bool k16 = pf_by16<T>(a.k, a.ld_k), v16 = pf_by16<T>(a.v, a.ld_v);
+  float g[4][HD / 16] = {};
+  for (int k0 = 0; k0 < t.first + rows; k0 += PF_T) {
+    __syncthreads();
+    pf_load<T, HD>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
+    pf_load<T, HD>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
+    __syncthreads();
+    pf_back_tile<HD>(sq, sdo, sk, sv, s_lse, s_delta, t.first, k0, t.n, a.scale * kLog2e, ty, tx, nullptr, sds);
+    __syncthreads();
+    pf_rows_by<HD>(sds, sk, ty, tx, g);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty + 16 * i;
+    if (r >= rows) continue;
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j)
+      pf_store4<T>(dq + (t.row0 + t.first + r) * a.ld_dq + h * HD + 4 * tx + 64 * j, a.scale * g[i][4 * j], a.scale * g[i][4 * j + 1],
+                   a.scale * g[i][4 * j + 2], a.scale * g[i][4 * j + 3]);
+  }
+}
+
+template <int HD>
+constexpr int pf_smem(int tiles, int squares) {
+  return (tiles * PF_T * (HD + 4) + squares * PF_T * (PF_T + 4)) * 4;
+}
+template <typename T, int HD>
+cudaError_t pf_prepare() {
+  cudaError_t e = cudaFuncSetAttribute(k_packed_attn<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem<HD>(3, 1));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dkv<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem<HD>(4, 2));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem<HD>(4, 1));
+  return e;
+}
+PerDeviceOnce g_pf_once;
+bool pf_ready() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  return g_pf_once.run(dev, []() -> int {
+    cudaError_t e = pf_prepare<float, 64>();
+    if (e == cudaSuccess) e = pf_prepare<float, 128>();
+    if (e == cudaSuccess) e = pf_prepare<bf16, 64>();
+    if (e == cudaSuccess) e = pf_prepare<bf16, 128>();
+    return (int)e;
+  }) == 0;
+}
+
+unsigned pf_tiles(const jf_packed& t) { return (unsigned)((t.n_rows + PF_T - 1) / PF_T + t.n_seqs); }
+
+template <typename T, int HD>
+cudaError_t pf_forward(const PackedParams& a, cudaStream_t st) {
+  return packed_launch(k_packed_attn<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem<HD>(3, 1), st, a);
+}
+template <typename T, int HD>
+cudaError_t pf_backward(const PackedParams& a, cudaStream_t st) {
+  const long long warps = (long long)a.t.n_rows * a.Hq;
+  cudaError_t e = packed_launch(k_packed_delta<T, HD>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a);
+  if (e == cudaSuccess) e = packed_launch(k_packed_dkv<T, HD>, dim3(pf_tiles(a.t), a.Hkv), dim3(PF_THREADS), pf_smem<HD>(4, 2), st, a);
+  if (e == cudaSuccess) e = packed_launch(k_packed_dq<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem<HD>(4, 1), st, a);
+  return e;
+}
+
+// Arguments that every call has.
+jf_status packed_check(const jf_packed* t, int dtype, int Hq, int Hkv, int hd) {
+  if (!t || !t->row_start || t->n_seqs < 1 || t->n_rows < 0 || t->max_rows < 0 || t->max_rows > t->n_rows) return JF_EINVAL;
+  if ((dtype != JF_F32 && dtype != JF_BF16) || Hq < 1 || Hkv < 1 || Hq % Hkv) return JF_EINVAL;
+  if ((hd != 64 && hd != 128) || t->n_seqs > kPackedMaxSeqs || Hq / Hkv > kPackedMaxGroup || Hq > 65535) return JF_EUNSUPPORTED;
+  // rows of a KV head and the steps of a batch's tiles are counted in 32 bits
+  const long long group_rows = (long long)t->n_rows * (Hq / Hkv) + 128ll * t->n_seqs;
+  if ((long long)t->n_rows * Hq > (1 << 30) || group_rows / 64 * ((long long)t->max_rows / 64 + 2) * Hkv > (1 << 30)) return JF_EUNSUPPORTED;
+  return JF_OK;
+}
+bool packed_rows_ok(const void* p, long long ld, long long width, int dtype) {
+  return p && ((uintptr_t)p & (dtype == JF_BF16 ? 1 : 3)) == 0 && ld >= width;
+}
+
+}  // namespace
+}  // namespace jf
+
+using namespace jf;
+
+extern "C" jf_status jf_op_packed_attention_workspace_bytes(const jf_packed* texts, int dtype, int n_heads, int n_kv_heads,
+                                                            int head_dim, int backward, size_t* out_bytes) {
+  const jf_status s = packed_check(texts, dtype, n_heads, n_kv_heads, head_dim);
+  if (s != JF_OK) return s;
+  if (!out_bytes) return JF_EINVAL;
+  *out_bytes = backward ? (size_t)texts->n_rows * n_heads * 4 : 0;
+  return JF_OK;
+}
+
+extern "C" jf_status jf_op_packed_attention(const jf_packed* texts, int dtype, const void* q, long long ld_q, const void* k,
+                                            long long ld_k, const void* v, long long ld_v, int n_heads, int n_kv_heads,
+                                            int head_dim, float scale, void* out, float* lse, void* workspace,
+                                            size_t workspace_bytes, int* err_word, void* cuda_stream) {
+  jf_status s = packed_check(texts, dtype, n_heads, n_kv_heads, head_dim);
+  if (s != JF_OK) return s;
+  if (!err_word || !(scale - scale == 0.f)) return JF_EINVAL;
+  if (texts->n_rows == 0) return JF_OK;
+  const long long wq = (long long)n_heads * head_dim, wkv = (long long)n_kv_heads * head_dim;
+  if (!packed_rows_ok(q, ld_q, wq, dtype) || !packed_rows_ok(k, ld_k, wkv, dtype) || !packed_rows_ok(v, ld_v, wkv, dtype) || !out ||
+      ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15))
+    return JF_EINVAL;
+  size_t need = 0;
+  s = jf_op_packed_attention_workspace_bytes(texts, dtype, n_heads, n_kv_heads, head_dim, 0, &need);
+  if (s != JF_OK) return s;
+  if (need > 0 && (!workspace || workspace_bytes < need)) return JF_ENOMEM;
+  if (!pf_ready()) return JF_ECUDA;
+  PackedParams a = {};
+  a.t = *texts, a.q = q, a.k = k, a.v = v, a.ld_q = ld_q, a.ld_k = ld_k, a.ld_v = ld_v, a.Hq = n_heads, a.Hkv = n_kv_heads;
+  a.scale = scale, a.out = out, a.lse = lse, a.err = err_word;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e;
+  if (dtype == JF_BF16) e = head_dim == 128 ? pf_forward<bf16, 128>(a, st) : pf_forward<bf16, 64>(a, st);
+  else e = head_dim == 128 ? pf_forward<float, 128>(a, st) : pf_forward<float, 64>(a, st);
+  return e == cudaSuccess ? JF_OK : JF_ECUDA;
+}
+
+extern "C" jf_status jf_op_packed_attention_grad(const jf_packed* texts, int dtype, const void* q, long long ld_q, const void* k,
+                                                 long long ld_k, const void* v, long long ld_v, int n_heads, int n_kv_heads,
+                                                 int head_dim, float scale, const void* out, const float* lse,
+                                                 const void* d_out, long long ld_do, void* dq, long long ld_dq, void* dk,
+                                                 long long ld_dk, void* dv, long long ld_dv, void* workspace,
+                                                 size_t workspace_bytes, int* err_word, void* cuda_stream) {
+  jf_status s = packed_check(texts, dtype, n_heads, n_kv_heads, head_dim);
+  if (s != JF_OK) return s;
+  if (!err_word || !(scale - scale == 0.f)) return JF_EINVAL;
+  if (texts->n_rows == 0) return JF_OK;
+  const long long wq = (long long)n_heads * head_dim, wkv = (long long)n_kv_heads * head_dim;
+  if (!packed_rows_ok(q, ld_q, wq, dtype) || !packed_rows_ok(k, ld_k, wkv, dtype) || !packed_rows_ok(v, ld_v, wkv, dtype) ||
+      !packed_rows_ok(d_out, ld_do, wq, dtype) || !packed_rows_ok(dq, ld_dq, wq, dtype) || !packed_rows_ok(dk, ld_dk, wkv, dtype) ||
+      !packed_rows_ok(dv, ld_dv, wkv, dtype) || !out || ((uintptr_t)out & 15) || !lse || ((uintptr_t)workspace & 15))
+    return JF_EINVAL;
+  size_t need = 0;
+  s = jf_op_packed_attention_workspace_bytes(texts, dtype, n_heads, n_kv_heads, head_dim, 1, &need);
+  if (s != JF_OK) return s;
+  if (!workspace || workspace_bytes < need) return JF_ENOMEM;
+  if (!pf_ready()) return JF_ECUDA;
+  PackedParams a = {};
+  a.t = *texts, a.q = q, a.k = k, a.v = v, a.ld_q = ld_q, a.ld_k = ld_k, a.ld_v = ld_v, a.Hq = n_heads, a.Hkv = n_kv_heads;
+  a.scale = scale, a.out = const_cast<void*>(out), a.lse = const_cast<float*>(lse), a.d_out = d_out, a.ld_do = ld_do;
+  a.dq = dq, a.dk = dk, a.dv = dv, a.ld_dq = ld_dq, a.ld_dk = ld_dk, a.ld_dv = ld_dv;
+  a.delta = reinterpret_cast<float*>(workspace), a.err = err_word;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e;
+  if (dtype == JF_BF16) e = head_dim == 128 ? pf_backward<bf16, 128>(a, st) : pf_backward<bf16, 64>(a, st);
+  else e = head_dim == 128 ? pf_backward<float, 128>(a, st) : pf_backward<float, 64>(a, st);
+  return e == cudaSuccess ? JF_OK : JF_ECUDA;
+}

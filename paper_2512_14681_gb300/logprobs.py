@@ -1,8 +1,10 @@
-"""Log probabilities of given tokens with entropy and top alternatives, and their gradient (jf_op_token_logprobs*
-of include/jf_ops.h), on the current stream or the one given as stream=: scores of a draft's or a trajectory's tokens, and the loss of training on them.
+"""Log probabilities of given tokens with entropy and top alternatives, their gradient, and the clipped policy loss with its own
+(jf_op_token_logprobs* and jf_op_policy_loss of include/jf_ops.h), on the current stream or the one given as stream=: scores of a
+draft's or a trajectory's tokens, and the loss of training on them.
 
     r = token_logprobs(logits, targets, top=5)                                    # r.logprob, r.entropy, r.top_ids, ...
     d = token_logprobs_grad(logits, targets, r.row_stats, r.entropy, -1 / n)      # of the mean negative log likelihood
+    p = policy_loss(logits, targets, old, advantage, ref_logprob=ref, kl=0.02)    # p.loss, p.grad (of p.loss.sum()), ...
 """
 from __future__ import annotations
 
@@ -125,3 +127,51 @@ def token_logprobs_grad(logits, targets, row_stats, entropy, grad_logprob, grad_
                                            out.data_ptr(), ld_out, _error_word(dev).data_ptr(), _raw_stream(dev)),
              "jf_op_token_logprobs_grad")
     return out
+
+
+class PolicyLoss(NamedTuple):
+    loss: torch.Tensor         # [rows]
+    logprob: torch.Tensor      # [rows] log probability of the target
+    entropy: torch.Tensor      # [rows]
+    ratio: torch.Tensor        # [rows] of the target's probability to the old one
+    kl: torch.Tensor           # [rows] e^d - 1 - d, d = ref_logprob - logprob (0 without a reference)
+    grad: torch.Tensor | None  # [rows][vocab] gradient of loss.sum() by the logits, in their type
+
+
+@functools.lru_cache(maxsize=4096)
+def _policy_need(dtype, rows, vocab):
+    n = C.c_size_t()
+    _checked(J.load().jf_op_policy_loss_workspace_bytes(dtype, rows, vocab, C.byref(n)), "jf_op_policy_loss_workspace_bytes")
+    return n.value
+
+
+@_on_stream
+def policy_loss(logits, targets, old_logprob, advantage, weight=None, ref_logprob=None, below: float = 0.2, above: float = 0.2,
+                kl: float = 0.0, entropy: float = 0.0, scale: float = 1.0, want_grad=True, out=None) -> PolicyLoss:
+    """Clipped policy loss of every row's target, and its gradient by the logits (jf_op_policy_loss): with r the ratio of the
+    target's probability to e^old_logprob, weight (-min(r A, min(max(r, 1 - below), 1 + above) A) + kl KL - entropy H). logits,
+    targets, scale: as in token_logprobs; old_logprob (None: r = 1), advantage, weight (None: 1), ref_logprob (None without
+    kl): float32 [rows]. out: where the gradient goes (it may be `logits`). As there, no graph is recorded."""
+    if logits.requires_grad and torch.is_grad_enabled():
+        raise J.JfError(J.JF_EUNSUPPORTED, "logits require a gradient, which is not recorded: detach() them, and give .grad to logits.backward()")
+    lib = J.load()
+    ld, (rows, vocab), dev = _logits(logits), logits.shape, logits.device
+    _on_current(dev)
+    dtype = _dtype(logits.dtype)
+    _want(want_grad or out is None, "out is given, but no gradient is wanted")
+    if want_grad and out is None:
+        out = torch.empty(rows, vocab, dtype=logits.dtype, device=dev)
+    ld_out = 0
+    if want_grad:
+        ld_out = _logits(out, "out")
+        _want(out.dtype == logits.dtype and out.device == dev and out.shape == logits.shape, "out: like logits is wanted")
+    of = lambda t, name: None if t is None else _vector(t, rows, torch.float32, dev, name)
+    r = torch.empty(5, rows, dtype=torch.float32, device=dev).unbind()
+    need = _policy_need(dtype, rows, vocab)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)  # the call's own, as in Kv8Cache.attention
+    _checked(lib.jf_op_policy_loss(C.byref(J.PolicyTerms(below, above, kl, entropy)), dtype, logits.data_ptr(), ld, rows, vocab, scale,
+                                   _vector(targets, rows, torch.int32, dev, "targets"), of(old_logprob, "old_logprob"),
+                                   of(ref_logprob, "ref_logprob"), _vector(advantage, rows, torch.float32, dev, "advantage"),
+                                   of(weight, "weight"), *(t.data_ptr() for t in r), out.data_ptr() if want_grad else None, ld_out,
+                                   ws.data_ptr(), need, _error_word(dev).data_ptr(), _raw_stream(dev)), "jf_op_policy_loss")
+    return PolicyLoss(*r, out)

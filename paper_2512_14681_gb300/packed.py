@@ -1,0 +1,136 @@
+"""Causal attention of packed texts and its backward pass (jf_op_packed_attention* of include/jf_ops.h): whole prompts,
+trajectories or a training batch, one behind the other in the rows of one call and without a cache (attention over a
+cache: kv8.py). Every call marshals arguments for one C entry point, on the current stream or the one given as stream=;
+device memory comes from PyTorch. No graph is recorded for autograd: a loss goes back through attention() by
+attention_grad().
+
+    texts = Packed.of([512, 301, 1])                                    # 814 rows
+    out, lse = attention(texts, q, k, v, 128 ** -0.5, want_lse=True)    # q [814][heads][128], k, v [814][kv heads][128]
+    dq, dk, dv = attention_grad(texts, q, k, v, out, lse, d_out, 128 ** -0.5)
+    check()                                                             # what the device reported (waits for it)
+"""
+from __future__ import annotations
+
+import ctypes as C
+import functools
+from dataclasses import dataclass
+
+import torch
+
+from . import _lib as J
+from .kv8 import _Fixed, _checked, _device_i32, _dtype, _on_current, _on_stream, _raw_stream, _row_stride, _take_error, _want
+
+_err = {}  # error word by device
+
+
+@dataclass(eq=False)
+class Packed(_Fixed):
+    """Texts of a batch (jf_packed): text b has rows row_start[b] .. row_start[b+1]-1 (an int32 CUDA tensor that the kernels
+    read when they run), none of more than max_rows. Of n_rows rows those of no text get 0 (lse: -infinity)."""
+    row_start: torch.Tensor
+    n_rows: int
+    max_rows: int
+
+    _fixed = ("row_start", "n_rows", "max_rows")
+
+    def __post_init__(self):
+        _device_i32(self.row_start, 2, "row_start")
+        self.c = J.Packed(self.row_start.data_ptr(), self.row_start.numel() - 1, self.n_rows, self.max_rows)
+
+    @classmethod
+    def of(cls, lengths, n_rows=None, max_rows=None, device="cuda"):
+        """From a host list of lengths; n_rows, max_rows: room for other lengths in row_start later (as many texts)."""
+        start = [0]
+        for n in lengths:
+            start.append(start[-1] + n)
+        return cls(torch.tensor(start, dtype=torch.int32, device=device), start[-1] if n_rows is None else n_rows,
+                   max(lengths, default=0) if max_rows is None else max_rows)
+
+
+def _error_word(device):
+    word = _err.get(device)
+    if word is None:
+        word = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.current_stream(device).synchronize()  # zero for every stream
+        word = _err.setdefault(device, word)  # (the first of several threads')
+    return word
+
+
+def check(device=None):
+    """Raise what the device has reported since the last check (waits for all of its streams), and clear it."""
+    device = torch.device("cuda" if device is None else device)
+    if device.index is None:
+        device = torch.device(device.type, torch.cuda.current_device())
+    word = _err.get(device)
+    code = _take_error(word) if word is not None else 0
+    if code:
+        what = {4: "texts that do not lie one behind the other in the rows", 1: "a copy's wait ran out", 2: "a product's wait ran out"}
+        raise J.JfError(J.JF_EDEVICE if code == 4 else J.JF_ETIMEOUT, what.get(code, f"device code {code}"))
+
+
+@functools.lru_cache(maxsize=4096)
+def _need(n_seqs, n_rows, max_rows, dtype, heads, kv_heads, head_dim, backward, device):
+    n = C.c_size_t()
+    t = J.Packed(16, n_seqs, n_rows, max_rows)  # (the address is not looked at)
+    _checked(J.load().jf_op_packed_attention_workspace_bytes(C.byref(t), dtype, heads, kv_heads, head_dim, backward, C.byref(n)),
+             "jf_op_packed_attention_workspace_bytes")
+    return n.value
+
+
+def _rows(t, n, like, name):
+    """Row stride of [n][heads][head_dim] values."""
+    _want(t.dim() == 3 and t.shape[0] == n and t.stride(2) == 1 and t.stride(1) == t.shape[2] and t.dtype == like.dtype and t.device == like.device,
+          "{}: [{}][heads][head_dim] of {} with contiguous heads on {} is wanted", name, n, like.dtype, like.device)
+    return _row_stride(t, t.shape[1] * t.shape[2], name)
+
+
+def _arguments(texts, q, k, v):
+    _want(q.is_cuda and texts.row_start.device == q.device, "q: a tensor on the texts' device is wanted")
+    _on_current(q.device)
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
+        raise J.JfError(J.JF_EUNSUPPORTED, "q, k or v requires a gradient, which is not recorded: detach() them, and see attention_grad")
+    n = texts.n_rows
+    lds = [_rows(t, n, q, name) for t, name in ((q, "q"), (k, "k"), (v, "v"))]
+    _want(k.shape == v.shape and k.shape[2] == q.shape[2], "q, k and v differ in head size, or k and v in heads")
+    heads, kv_heads, hd = q.shape[1], k.shape[1], q.shape[2]
+    _want(kv_heads > 0 and heads % kv_heads == 0, "{} query heads over {} KV heads", heads, kv_heads)
+    head = (C.byref(texts.c), _dtype(q.dtype), q.data_ptr(), lds[0], k.data_ptr(), lds[1], v.data_ptr(), lds[2], heads, kv_heads, hd)
+    return head, (texts.c.n_seqs, n, texts.max_rows, head[1], heads, kv_heads, hd)
+
+
+@_on_stream
+def attention(texts: Packed, q, k, v, scale: float, want_lse=False):
+    """Causal attention of every text's rows over its own (jf_op_packed_attention): q [n_rows][heads][head_dim], k and v
+    [n_rows][kv heads][head_dim], bfloat16 or float32, rows any distance apart. Returns out, or (out, lse)."""
+    head, key = _arguments(texts, q, k, v)
+    dev, n = q.device, _need(*key, 0, q.device.index)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None  # the call's own, as in Kv8Cache.attention
+    out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev) if want_lse else None
+    _checked(J.load().jf_op_packed_attention(*head, scale, out.data_ptr(), lse.data_ptr() if want_lse else None,
+                                             ws.data_ptr() if n else None, n, _error_word(dev).data_ptr(), _raw_stream(dev)),
+             "jf_op_packed_attention")
+    return (out, lse) if want_lse else out
+
+
+@_on_stream
+def attention_grad(texts: Packed, q, k, v, out, lse, d_out, scale: float, grads=None):
+    """(dq, dk, dv): gradients by q, k and v of a loss whose gradient by attention()'s out is d_out (jf_op_packed_attention_grad).
+    grads: three tensors that they are written to (parts of one buffer's rows, for the projection's gradient); None: new ones."""
+    head, key = _arguments(texts, q, k, v)
+    dev, n = q.device, texts.n_rows
+    ld_do = _rows(d_out, n, q, "d_out")
+    _want(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous() and d_out.shape == q.shape,
+          "out, d_out: like q (out contiguous) is wanted")
+    _want(lse.shape == q.shape[:2] and lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous(),
+          "lse: contiguous float32 [{}][{}] is wanted", n, q.shape[1])
+    if grads is None:
+        grads = tuple(torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
+    lds = [_rows(g, n, q, name) for g, name in zip(grads, ("dq", "dk", "dv"))]
+    _want(len(grads) == 3 and all(g.shape == t.shape for g, t in zip(grads, (q, k, v))), "grads: shaped like q, k and v is wanted")
+    need = _need(*key, 1, dev.index)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    _checked(J.load().jf_op_packed_attention_grad(
+        *head, scale, out.data_ptr(), lse.data_ptr(), d_out.data_ptr(), ld_do, grads[0].data_ptr(), lds[0], grads[1].data_ptr(), lds[1],
+        grads[2].data_ptr(), lds[2], ws.data_ptr(), need, _error_word(dev).data_ptr(), _raw_stream(dev)), "jf_op_packed_attention_grad")
+    return tuple(grads)
