@@ -18,7 +18,8 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT, "libjf.so")
 SOURCES = ["jf_gemm.cu", "jf_attention.cu", "jf_elementwise.cu", "jf_decode.cu", "jf_runtime.cu", "jf_noalloc.cu",
-           "jf_kv8.cu", "jf_kv8_attn.cu", "jf_logprobs.cu", "jf_policy.cu", "jf_packed.cu"]
+           "jf_kv8.cu", "jf_kv8_attn.cu", "jf_logprobs.cu", "jf_policy.cu", "jf_packed.cu",
+           "jf_packed_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

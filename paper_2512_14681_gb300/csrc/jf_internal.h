@@ -165,5 +165,8 @@ cudaError_t tl_set_decode(void* records, void* counter);
 #endif
 int gemm_default_splits(int n_tiles, int kb_total);
 bool encode_tmap_bf16(CUtensorMap* tm, const void* ptr, long long K, long long rows, int box_rows);
+// 16-bit rank-3 tensor (dims and box innermost first, strides of the outer dims in bytes), 128-byte swizzle.
+bool encode_tmap_bf16_3d(CUtensorMap* tm, const void* ptr, const unsigned long long (&dims)[3], const unsigned long long (&strides)[2],
+                         const unsigned (&box)[3]);
 
 }  // namespace jf

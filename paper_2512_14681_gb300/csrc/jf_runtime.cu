@@ -289,6 +289,12 @@ int jf::gemm_default_splits(int n_tiles, int kb_total) { return splits_for(n_til
 bool jf::encode_tmap_bf16(CUtensorMap* tm, const void* ptr, long long K, long long rows, int box_rows) {
   return make_tmap(tm, ptr, K, rows, box_rows);
 }
+bool jf::encode_tmap_bf16_3d(CUtensorMap* tm, const void* ptr, const unsigned long long (&dims)[3], const unsigned long long (&strides)[2],
+                             const unsigned (&box)[3]) {
+  const cuuint64_t d[3] = {dims[0], dims[1], dims[2]}, s[2] = {strides[0], strides[1]};
+  const cuuint32_t b[3] = {box[0], box[1], box[2]};
+  return make_tmap_3d(tm, ptr, d, s, b);
+}
 
 struct jf_ctx {
   jf_model_config mc;
