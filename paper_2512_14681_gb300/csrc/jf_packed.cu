@@ -435,7 +435,7 @@ extern "C" jf_status jf_op_packed_attention_workspace_bytes(const jf_packed* tex
   const jf_status s = packed_check(texts, dtype, n_heads, n_kv_heads, head_dim);
   if (s != JF_OK) return s;
   if (!out_bytes) return JF_EINVAL;
-  if (dtype == JF_BF16 && !backward) return packed_tc_workspace(*texts, n_heads, n_kv_heads, head_dim, false, out_bytes);
+  if (dtype == JF_BF16) return packed_tc_workspace(*texts, n_heads, n_kv_heads, head_dim, backward != 0, out_bytes);
   *out_bytes = backward ? (size_t)texts->n_rows * n_heads * 4 : 0;
   return JF_OK;
 }
@@ -495,6 +495,8 @@ extern "C" jf_status jf_op_packed_attention_grad(const jf_packed* texts, int dty
   a.delta = reinterpret_cast<float*>(workspace), a.err = err_word;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
+  if (dtype == JF_BF16 && packed_tc_rows(q, ld_q) && packed_tc_rows(k, ld_k) && packed_tc_rows(v, ld_v) && packed_tc_rows(d_out, ld_do))
+    return packed_tc_backward(a, head_dim, workspace, st);
   if (dtype == JF_BF16) e = head_dim == 128 ? pf_backward<bf16, 128>(a, st) : pf_backward<bf16, 64>(a, st);
   else e = head_dim == 128 ? pf_backward<float, 128>(a, st) : pf_backward<float, 64>(a, st);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;

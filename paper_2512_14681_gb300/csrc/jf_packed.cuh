@@ -44,6 +44,7 @@ JF_DEV bool packed_text_ok(const jf_packed& t, int b) {
 bool packed_tc_rows(const void* p, long long ld);
 jf_status packed_tc_workspace(const jf_packed& t, int Hq, int Hkv, int hd, bool backward, size_t* out_bytes);
 jf_status packed_tc_forward(const PackedParams& a, int hd, void* workspace, cudaStream_t st);
+jf_status packed_tc_backward(const PackedParams& a, int hd, void* workspace, cudaStream_t st);
 
 template <typename K, typename... Args>
 cudaError_t packed_launch(K kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {

@@ -23,6 +23,7 @@ constexpr int PT_SNAP = 1;                       // a cut moves to a unit's end 
 // The line of units. Kind says how a text is cut: units(n), steps(n, u) for a text of n rows.
 // ---------------------------------------------------------------------------------------------
 struct ByQueries {  // tiles of `tok` tokens over the key tiles that they see
+  static constexpr bool KEYS = false;
   static constexpr int UC = 2;
   int tok;
   JF_DEV int units(int n) const { return (n + tok - 1) / tok; }
@@ -627,6 +628,683 @@ __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a, 
 }
 
 // ---------------------------------------------------------------------------------------------
+// Backward. Two kernels, each with sums of its own and no atomics: dq by tiles of query rows over the keys, dk and dv by
+// tiles of keys over the query rows; the scores are multiplied out in both (7 products instead of 5).
+//
+// delta = d_out . out loses what out was rounded by, which counts where a row sees few keys. As sum_j ds_ij = 0 for the exact
+// delta, the dq kernel adds up its ds (a row lies in one thread, or two) and corrects delta by it for dk; where a row's keys
+// are one step it takes delta = sum_j p_ij dp_ij to begin with.
+//
+// Tiles come through a ring of four places in pairs, X (needed first and last: K, or Q) and Y (V, or d_out). Y's place is free
+// first and takes the X of two steps on, X's place its Y.
+// Warps 0-3 and 4-7: columns 0-63 and 64-127 of all 128 rows; warp 8: copies; 9: products; 10: row statistics (dk and dv).
+// ---------------------------------------------------------------------------------------------
+struct BackMaps {
+  CUtensorMap q, k, v, d_out;
+};
+JF_DEV int place_x(int j) { return 2 * (j & 1) + (j >> 1 & 1); }
+JF_DEV int place_y(int j) { return 2 * (j & 1) + (~j >> 1 & 1); }
+// Completion number of a place's barriers that step j's tile waits for: the places of a pair are used by turns.
+JF_DEV int use_of(int j) { return j >> 1; }
+
+constexpr int PB_THREADS = 384;
+template <int HD>
+struct BackLayout {
+  static constexpr int T = Tile<HD>::BYTES, OFF_RING = 2 * T;
+  static constexpr int TOTAL = (HD == 128 ? OFF_RING + 4 * T : 7 * 16384) + 1024;  // (one CTA an SM: it has all tensor memory)
+  static constexpr int DQ_STATE = 128 * (HD + 2);  // floats of a part: dq by 4 columns [HD / 4][128 rows][4], sum of ds, delta
+  static constexpr int DKV_STATE = 2 * 128 * HD;   // dv, dk, each by 4 columns
+};
+
+struct BackBarriers {
+  uint64_t fix, fixfree, tile[4], free[4];  // the unit's own two tiles there, read; the ring's places there, read
+  uint64_t s[2], dp, p, ds, o1, o2, all, stat[2], statfree[2];
+};
+JF_DEV void back_init(BackBarriers& b) {
+  mbar_init(smem_u32(&b.fix), 1);
+  mbar_init(smem_u32(&b.fixfree), 1);
+  for (int i = 0; i < 4; ++i) {
+    mbar_init(smem_u32(&b.tile[i]), 1);
+    mbar_init(smem_u32(&b.free[i]), 1);
+  }
+  for (int i = 0; i < 2; ++i) {
+    mbar_init(smem_u32(&b.s[i]), 1);
+    mbar_init(smem_u32(&b.stat[i]), 1);
+    mbar_init(smem_u32(&b.statfree[i]), 8);
+  }
+  mbar_init(smem_u32(&b.dp), 1);
+  mbar_init(smem_u32(&b.p), 8);
+  mbar_init(smem_u32(&b.ds), 8);
+  mbar_init(smem_u32(&b.o1), 1);
+  mbar_init(smem_u32(&b.o2), 1);
+  mbar_init(smem_u32(&b.all), 1);
+  fence_mbar_init();
+}
+
+// Gradients of rows that belong to no text, by `threads` threads.
+template <int HD>
+JF_DEV void clear_rows(const jf_packed& t, void* p, long long ld, int heads, int tid, int threads) {
+  const int head = t.row_start[0], tail = t.row_start[t.n_seqs], width = heads * HD;
+  for (int r = blockIdx.x; r < head + t.n_rows - tail; r += gridDim.x) {
+    const long long row = r < head ? r : tail + r - head;
+    for (int i = tid; i < width; i += threads) reinterpret_cast<bf16*>(p)[row * ld + i] = __float2bfloat16_rn(0.f);
+  }
+}
+
+// The copies of a kernel's run, by warp 8: fix = the unit's own tiles, x and y = a step's.
+template <int HD, typename Kind, typename Fix, typename Step>
+JF_DEV void back_copies(Run<Kind>& w, bool go, BackBarriers& b, uint32_t sm, uint32_t fix_bytes, uint32_t tile_bytes, int* err, Fix fix, Step step) {
+  using Lay = BackLayout<HD>;
+  int units = 0, g = 0;
+  bool ok = true;
+  while (go) {
+    ok = units == 0 || warp_wait(b.fixfree, units - 1);
+    if (!ok) break;
+    if (elect_one()) {
+      mbar_arrive_expect_tx(smem_u32(&b.fix), fix_bytes);
+      fix(sm, smem_u32(&b.fix));
+    }
+    __syncwarp();
+    ++units;
+    for (int j = w.c0(); j < w.c1() && ok; ++j, ++g)
+      for (int y = 0; y < 2 && ok; ++y) {
+        const int place = y ? place_y(g) : place_x(g);
+        ok = g < 2 || warp_wait(b.free[place], use_of(g) - 1);
+        if (!ok) break;
+        if (elect_one()) {
+          mbar_arrive_expect_tx(smem_u32(&b.tile[place]), tile_bytes);
+          step(sm + Lay::OFF_RING + place * Lay::T, smem_u32(&b.tile[place]), j, y);
+        }
+        __syncwarp();
+      }
+    if (!ok) break;
+    go = w.next();
+  }
+  // every copy has landed before the CTA may leave, also after a wait that gave up
+  if (units) warp_wait(b.fix, units - 1);
+  for (int j = max(0, g - 2); j < g; ++j) {
+    warp_wait(b.tile[place_x(j)], use_of(j));
+    warp_wait(b.tile[place_y(j)], use_of(j));
+  }
+  if (!ok && (threadIdx.x & 31) == 0) jf_set_error(err, JF_DERR_TIMEOUT_MMA);
+}
+
+// What both kernels begin with: the line's cuts, tensor memory. False: nothing to do for the whole grid.
+template <typename Kind>
+JF_DEV bool back_begin(Run<Kind>& w, const PackedParams& a, uint8_t* sm, int* s_bad, Cut* s_cut, uint32_t* tmem_slot, bool& go) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_launch_dependents();
+  pdl_wait();
+  if (!w.line.build(reinterpret_cast<int*>(sm), s_bad, a.err)) return false;
+  const int workers = w.line.workers(gridDim.x);
+  if (warp < 2 && (int)blockIdx.x < workers) {
+    const Cut c = w.line.cut(blockIdx.x + warp, workers);
+    if (lane == 0) s_cut[warp] = c;
+  }
+  if (warp == 8) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  fence_proxy_async_smem();  // (the line's place is taken by copies)
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  w.at = s_cut[0], w.end = s_cut[1];
+  go = (int)blockIdx.x < workers && w.line.total > 0 && w.there();
+  return true;
+}
+
+// 16 bf16 products of two runs of memory
+JF_DEV float dot8(const uint4& x, const uint4& y, float s) {
+  const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s = fmaf(__uint_as_float(a[i] << 16), __uint_as_float(b[i] << 16), s);
+    s = fmaf(__uint_as_float(a[i] & 0xffff0000u), __uint_as_float(b[i] & 0xffff0000u), s);
+  }
+  return s;
+}
+
+// dq. Tensor memory: two S, dP (ds in bf16 in its place), dQ.
+template <int HD>
+__global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dq_tc(const PackedParams a, const __grid_constant__ BackMaps maps) {
+  using Lay = BackLayout<HD>;
+  using T = Tile<HD>;
+  extern __shared__ uint8_t sm_raw[];
+  uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sm = smem_u32(smp), sQ = sm, sdO = sm + Lay::T, ring = sm + Lay::OFF_RING;
+  __shared__ __align__(8) BackBarriers b;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int s_bad;
+  __shared__ Cut s_cut[2];
+  __shared__ float s_x[2][2][128];  // (of the two halves of a row, by turns)
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int G = a.Hq / a.Hkv, tok = 128 / G;
+  if (tid == 0) back_init(b);
+  Run<ByQueries> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, {}};
+  bool go, ok = true;
+  if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 256, tQ = tmem + 384;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 8) {
+      back_copies<HD>(
+          w, go, b, sm, (uint32_t)(2 * tok * G * HD * 2), (uint32_t)T::BYTES, a.err,
+          [&](uint32_t dst, uint32_t bar) {
+            T::load(dst, &maps.q, bar, w.at.kvh * G, w.at.row0 + w.at.u * tok);
+            T::load(dst + Lay::T, &maps.d_out, bar, w.at.kvh * G, w.at.row0 + w.at.u * tok);
+          },
+          [&](uint32_t dst, uint32_t bar, int j, int y) { T::load(dst, y ? &maps.v : &maps.k, bar, w.at.kvh, w.at.row0 + j * PT_KEYS); });
+    } else if (warp == 9) {
+      const uint32_t on = elect_one();
+      int g = 0, units = 0;  // steps, units so far
+      auto x_there = [&](int j) { return warp_wait(b.tile[place_x(j)], use_of(j)); };
+      auto issue_s = [&](int j) {  // (its S was read two steps ago)
+        tc_fence_after();
+        T::dots(tS + (j & 1) * 128, sQ, ring + place_x(j) * Lay::T, on);
+        commit_on(smem_u32(&b.s[j & 1]), on);
+      };
+      auto issue_dp = [&](int j) {  // (ds of the step before has been read)
+        ok = warp_wait(b.tile[place_y(j)], use_of(j));
+        if (j > 0) ok = ok && warp_wait(b.o1, j - 1);
+        if (!ok) return;
+        tc_fence_after();
+        T::dots(tP, sdO, ring + place_y(j) * Lay::T, on);
+        commit_on(smem_u32(&b.dp), on);
+        commit_on(smem_u32(&b.free[place_y(j)]), on);
+      };
+      while (go) {
+        const int n = w.c1() - w.c0();
+        ok = warp_wait(b.fix, units++) && x_there(g);
+        if (!ok) break;
+        issue_s(g);
+        issue_dp(g);
+        if (n == 1) commit_on(smem_u32(&b.fixfree), on);
+        if (n > 1 && ok) {
+          ok = x_there(g + 1);
+          if (ok) issue_s(g + 1);
+        }
+        for (int j = 0; j < n && ok; ++j, ++g) {
+          const int held = w.at.n - (w.c0() + j) * PT_KEYS;
+          if (held < PT_KEYS) T::clear_from(ring + place_x(g) * Lay::T, held, lane);
+          ok = warp_wait(b.ds, g);
+          if (!ok) break;
+          tc_fence_after();
+          T::rows(tQ, tP, ring + place_x(g) * Lay::T, j == 0, on, 64);
+          commit_on(smem_u32(&b.o1), on);
+          commit_on(smem_u32(&b.free[place_x(g)]), on);
+          if (j + 1 < n) issue_dp(g + 1);
+          if (j + 2 == n) commit_on(smem_u32(&b.fixfree), on);
+          if (j + 2 < n && ok) {
+            ok = x_there(g + 2);
+            if (ok) issue_s(g + 2);
+          }
+        }
+        go = ok && w.next();
+      }
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
+      commit_on(smem_u32(&b.all), on);
+      __syncwarp();
+      warp_wait(b.all, 0);  // every product is complete before the CTA may leave
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    clear_rows<HD>(a.t, a.dq, a.ld_dq, a.Hq, tid, 256);
+    const int half = warp >> 2, r = (warp & 3) * 32 + lane, r_tok = r / G, r_head = r - r_tok * G;
+    const uint32_t t_row = (uint32_t)((warp & 3) * 32) << 16;
+    const float c = a.scale * kLog2e;
+    int g = 0, turn = 0;
+    // the sum of both halves of a row; all 256 threads meet, and learn whether one's wait gave up: it keeps to the meetings
+    // until then, so that nobody waits at one alone
+    auto join = [&](float x) {
+      s_x[turn][half][r] = x;
+      ok = sync_and<1, 256>(ok);
+      const float sum = s_x[turn][0][r] + s_x[turn][1][r];
+      turn ^= 1;
+      return sum;
+    };
+    while (go) {
+      const int i = w.at.u * tok + r_tok;
+      const bool live = r_tok < tok && i < w.at.n, one = w.at.n_steps == 1;
+      const long long row = w.at.row0 + i, at = row * a.Hq + w.at.kvh * G + r_head;
+      const float nl = live ? -a.lse[at] * kLog2e : -INFINITY;
+      float delta = 0.f, eps = 0.f;
+      if (!one) {
+        if (live) {
+          const uint4* x = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.out) + at * HD + half * (HD / 2));
+          const uint4* y = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.d_out) + row * a.ld_do + (w.at.kvh * G + r_head) * HD + half * (HD / 2));
+#pragma unroll
+          for (int d = 0; d < HD / 16; ++d) delta = dot8(x[d], y[d], delta);
+        }
+        delta = join(delta);
+        if (!ok) break;
+      }
+      bool left = false;  // (after a meeting that ends the run, there is no other)
+      for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
+        const int see = i - j * PT_KEYS - 64 * half;  // columns 0 .. see of the 64
+        const bool cut = (j + 1) * PT_KEYS > w.at.u * tok;
+        ok = warp_wait(b.s[g & 1], g >> 1);
+        if (!ok) break;
+        tc_fence_after();
+        float p[64];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[32];
+          tmem_ld32(tS + t_row + (g & 1) * 128 + 64 * half + 32 * h, v);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const float2 e = fma2(make_float2(v[2 * x], v[2 * x + 1]), make_float2(c, c), make_float2(nl, nl));
+            p[32 * h + 2 * x] = packed_ex2(e.x), p[32 * h + 2 * x + 1] = packed_ex2(e.y);
+          }
+        }
+        if (cut) {
+#pragma unroll
+          for (int x = 0; x < 64; ++x) p[x] = x <= see ? p[x] : 0.f;
+        }
+        ok = warp_wait(b.dp, g);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t t_p = tP + t_row + 64 * half;
+        if (one) {
+          float sum = 0.f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float v[32];
+            tmem_ld32(t_p + 32 * h, v);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) sum += 32 * h + x <= see ? p[32 * h + x] * v[x] : 0.f;
+          }
+          delta = join(sum);
+          left = !ok;
+          if (left) break;
+        }
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[32];
+          uint32_t u[16];
+          tmem_ld32(t_p + 32 * h, v);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            float2 d = add2(make_float2(v[2 * x], v[2 * x + 1]), make_float2(-delta, -delta));
+            d.x *= p[32 * h + 2 * x], d.y *= p[32 * h + 2 * x + 1];
+            if (cut) {  // (what lies behind the text may be anything)
+              d.x = 32 * h + 2 * x <= see ? d.x : 0.f;
+              d.y = 32 * h + 2 * x + 1 <= see ? d.y : 0.f;
+            }
+            sum = add2(sum, d);
+            u[x] = pack_bf16(d.x, d.y);
+          }
+          tmem_st16(t_p + 16 * h, u);
+        }
+        eps += sum.x + sum.y;
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&b.ds));
+      }
+      if (left) break;
+      ok = ok && warp_wait(b.o1, g - 1);
+      if (!one) eps = join(eps);
+      else ok = sync_and<1, 256>(ok);
+      if (!ok) break;
+      tc_fence_after();
+      const bool whole = w.whole();
+      float* st = a.states + (long long)w.slot(blockIdx.x) * Lay::DQ_STATE;
+#pragma unroll 1
+      for (int d = half * (HD / 2); d < (half + 1) * (HD / 2); d += 32) {
+        float o[32];
+        tmem_ld32(tQ + t_row + d, o);
+        if (whole) {
+          if (live) {
+            bf16* dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (w.at.kvh * G + r_head) * HD + d;
+            if (((uintptr_t)dst & 15) == 0) {
+#pragma unroll
+              for (int h = 0; h < 4; ++h)
+                reinterpret_cast<uint4*>(dst)[h] =
+                    make_uint4(pack_bf16(o[8 * h] * a.scale, o[8 * h + 1] * a.scale), pack_bf16(o[8 * h + 2] * a.scale, o[8 * h + 3] * a.scale),
+                               pack_bf16(o[8 * h + 4] * a.scale, o[8 * h + 5] * a.scale), pack_bf16(o[8 * h + 6] * a.scale, o[8 * h + 7] * a.scale));
+            } else {
+#pragma unroll
+              for (int h = 0; h < 32; ++h) dst[h] = __float2bfloat16_rn(o[h] * a.scale);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 8; ++h)
+            reinterpret_cast<float4*>(st)[(d / 4 + h) * 128 + r] = make_float4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]);
+        }
+      }
+      if (half == 0) {
+        if (!whole) st[128 * HD + r] = eps, st[128 * (HD + 1) + r] = delta;
+        else if (live) a.delta[at] = one ? delta : delta + eps;
+      }
+      tc_fence_before();
+      ok = sync_and<1, 256>(ok);  // both halves have read dQ (and what they exchanged)
+      if (!ok) break;
+      go = w.next();
+    }
+    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+struct ByKeys {  // tiles of keys over the tiles of `tok` tokens that see them
+  static constexpr bool KEYS = true;
+  static constexpr int UC = 2;
+  int tok;
+  JF_DEV int units(int n) const { return (n + PT_KEYS - 1) / PT_KEYS; }
+  JF_DEV int first(int u) const { return u * PT_KEYS / tok; }
+  JF_DEV int steps(int n, int u) const { return (n + tok - 1) / tok - first(u); }
+};
+
+// dk and dv. Rows of the products are keys, columns query rows. Tensor memory: S (P in bf16 in its place), dP (ds), dV, dK.
+template <int HD>
+__global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dkv_tc(const PackedParams a, const __grid_constant__ BackMaps maps) {
+  using Lay = BackLayout<HD>;
+  using T = Tile<HD>;
+  extern __shared__ uint8_t sm_raw[];
+  uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sm = smem_u32(smp), sK = sm, sV = sm + Lay::T, ring = sm + Lay::OFF_RING;
+  __shared__ __align__(8) BackBarriers b;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int s_bad;
+  __shared__ Cut s_cut[2];
+  __shared__ __align__(16) float s_nl[2][128], s_nd[2][128];  // of a step's columns: -lse log2 e, -delta
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int G = a.Hq / a.Hkv, tok = 128 / G;
+  if (tid == 0) back_init(b);
+  Run<ByKeys> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, {}};
+  bool go, ok = true;
+  if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 8) {
+      back_copies<HD>(
+          w, go, b, sm, (uint32_t)(2 * T::BYTES), (uint32_t)(tok * G * HD * 2), a.err,
+          [&](uint32_t dst, uint32_t bar) {
+            T::load(dst, &maps.k, bar, w.at.kvh, w.at.row0 + w.at.u * PT_KEYS);
+            T::load(dst + Lay::T, &maps.v, bar, w.at.kvh, w.at.row0 + w.at.u * PT_KEYS);
+          },
+          [&](uint32_t dst, uint32_t bar, int j, int y) {
+            T::load(dst, y ? &maps.d_out : &maps.q, bar, w.at.kvh * G, w.at.row0 + (w.line.kind.first(w.at.u) + j) * tok);
+          });
+    } else if (warp == 9) {
+      const uint32_t on = elect_one();
+      for (int i = 0; i < 4; ++i)
+        if (tok * G < 128) T::clear_from(ring + i * Lay::T, tok * G, lane);  // rows that no copy writes
+      int g = 0, units = 0;
+      // a step's tile, its rows behind the text cleared
+      auto there = [&](int place, int j, int q) {
+        if (!warp_wait(b.tile[place], use_of(j))) return false;
+        const int held = (w.at.n - q * tok) * G;
+        if (held < tok * G) T::clear_from(ring + place * Lay::T, held, lane);
+        return true;
+      };
+      auto issue_s = [&](int j) {
+        tc_fence_after();
+        T::dots(tS, sK, ring + place_x(j) * Lay::T, on);
+        commit_on(smem_u32(&b.s[0]), on);
+      };
+      auto issue_dp = [&](int j) {
+        tc_fence_after();
+        T::dots(tP, sV, ring + place_y(j) * Lay::T, on);
+        commit_on(smem_u32(&b.dp), on);
+      };
+      while (go) {
+        const int n = w.c1() - w.c0(), q0 = w.line.kind.first(w.at.u) + w.c0();
+        // (the last unit's P and ds have been read: its last dK was waited for below)
+        ok = warp_wait(b.fix, units++) && there(place_x(g), g, q0);
+        if (!ok) break;
+        issue_s(g);
+        ok = there(place_y(g), g, q0);
+        if (!ok) break;
+        issue_dp(g);
+        if (n == 1) commit_on(smem_u32(&b.fixfree), on);
+        for (int j = 0; j < n && ok; ++j, ++g) {
+          ok = warp_wait(b.p, g);
+          if (!ok) break;
+          tc_fence_after();
+          T::rows(tV, tS, ring + place_y(g) * Lay::T, j == 0, on, 64);
+          commit_on(smem_u32(&b.o1), on);
+          commit_on(smem_u32(&b.free[place_y(g)]), on);
+          if (j + 1 < n) {
+            ok = there(place_x(g + 1), g + 1, q0 + j + 1) && warp_wait(b.o1, g);
+            if (!ok) break;
+            issue_s(g + 1);
+          }
+          ok = warp_wait(b.ds, g);
+          if (!ok) break;
+          tc_fence_after();
+          T::rows(tK, tP, ring + place_x(g) * Lay::T, j == 0, on, 64);
+          commit_on(smem_u32(&b.o2), on);
+          commit_on(smem_u32(&b.free[place_x(g)]), on);
+          ok = j + 1 == n || there(place_y(g + 1), g + 1, q0 + j + 1);
+          ok = ok && warp_wait(b.o2, g);
+          if (ok && j + 1 < n) {
+            issue_dp(g + 1);
+            if (j + 2 == n) commit_on(smem_u32(&b.fixfree), on);
+          }
+        }
+        go = ok && w.next();
+      }
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
+      commit_on(smem_u32(&b.all), on);
+      __syncwarp();
+      warp_wait(b.all, 0);  // every product is complete before the CTA may leave
+    } else if (warp == 10) {
+      int g = 0;
+      while (go) {
+        for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
+          const int q = w.line.kind.first(w.at.u) + j;
+          float nl[4], nd[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int col = lane + 32 * x, t = col / G, i = q * tok + t;
+            const bool live = t < tok && i < w.at.n;
+            const long long at = (long long)(w.at.row0 + i) * a.Hq + w.at.kvh * G + (col - t * G);
+            nl[x] = live ? -a.lse[at] * kLog2e : -INFINITY;  // (p = 0)
+            nd[x] = live ? -a.delta[at] : 0.f;
+          }
+          ok = g < 2 || warp_wait(b.statfree[g & 1], (g >> 1) - 1);
+          if (!ok) break;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s_nl[g & 1][lane + 32 * x] = nl[x], s_nd[g & 1][lane + 32 * x] = nd[x];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&b.stat[g & 1]));
+        }
+        go = ok && w.next();
+      }
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    clear_rows<HD>(a.t, a.dk, a.ld_dk, a.Hkv, tid, 256);
+    clear_rows<HD>(a.t, a.dv, a.ld_dv, a.Hkv, tid, 256);
+    const int half = warp >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t t_row = (uint32_t)((warp & 3) * 32) << 16;
+    const float c = a.scale * kLog2e;
+    int g = 0;
+    while (go) {
+      const int k = w.at.u * PT_KEYS + r, q0 = w.line.kind.first(w.at.u);
+      for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
+        const int first = (k - (q0 + j) * tok) * G - 64 * half;  // columns from here on see the key
+        const bool cut = (q0 + j) * tok < w.at.u * PT_KEYS + PT_KEYS - 1;
+        ok = warp_wait(b.stat[g & 1], g >> 1) && warp_wait(b.s[0], g);
+        if (!ok) break;
+        tc_fence_after();
+        float p[64];
+        const uint32_t t_s = tS + t_row + 64 * half, t_p = tP + t_row + 64 * half;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[32];
+          tmem_ld32(t_s + 32 * h, v);
+          const float4* nl = reinterpret_cast<const float4*>(s_nl[g & 1] + 64 * half + 32 * h);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const float4 l = nl[x];
+            const float2 e = fma2(make_float2(v[4 * x], v[4 * x + 1]), make_float2(c, c), make_float2(l.x, l.y));
+            const float2 f = fma2(make_float2(v[4 * x + 2], v[4 * x + 3]), make_float2(c, c), make_float2(l.z, l.w));
+            float* o = p + 32 * h + 4 * x;
+            o[0] = packed_ex2(e.x), o[1] = packed_ex2(e.y), o[2] = packed_ex2(f.x), o[3] = packed_ex2(f.y);
+          }
+        }
+        if (cut) {
+#pragma unroll
+          for (int x = 0; x < 64; ++x) p[x] = x >= first ? p[x] : 0.f;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t u[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) u[x] = pack_bf16(p[32 * h + 2 * x], p[32 * h + 2 * x + 1]);
+          tmem_st16(t_s + 16 * h, u);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&b.p));
+        ok = warp_wait(b.dp, g);
+        if (!ok) break;
+        tc_fence_after();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[32];
+          uint32_t u[16];
+          tmem_ld32(t_p + 32 * h, v);
+          const float4* nd = reinterpret_cast<const float4*>(s_nd[g & 1] + 64 * half + 32 * h);
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const float4 d = nd[x];
+            const float2 e = add2(make_float2(v[4 * x], v[4 * x + 1]), make_float2(d.x, d.y));
+            const float2 f = add2(make_float2(v[4 * x + 2], v[4 * x + 3]), make_float2(d.z, d.w));
+            const float* o = p + 32 * h + 4 * x;
+            u[2 * x] = pack_bf16(o[0] * e.x, o[1] * e.y);
+            u[2 * x + 1] = pack_bf16(o[2] * f.x, o[3] * f.y);
+          }
+          tmem_st16(t_p + 16 * h, u);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&b.ds));
+          mbar_arrive(smem_u32(&b.statfree[g & 1]));
+        }
+      }
+      ok = ok && warp_wait(b.o1, g - 1) && warp_wait(b.o2, g - 1);
+      ok = sync_and<1, 256>(ok);
+      if (!ok) break;
+      tc_fence_after();
+      // the first four warps take dV, the others dK
+      const bool whole = w.whole(), live = k < w.at.n;
+      const float f = half ? a.scale : 1.f;
+      float* st = a.states + (long long)w.slot(blockIdx.x) * Lay::DKV_STATE + half * (128 * HD);
+      bf16* dst = half ? reinterpret_cast<bf16*>(a.dk) + (w.at.row0 + k) * a.ld_dk : reinterpret_cast<bf16*>(a.dv) + (w.at.row0 + k) * a.ld_dv;
+      dst += w.at.kvh * HD;
+#pragma unroll 1
+      for (int d = 0; d < HD; d += 32) {
+        float o[32];
+        tmem_ld32((half ? tK : tV) + t_row + d, o);
+        if (whole) {
+          if (live) {
+            if (((uintptr_t)dst & 15) == 0) {
+#pragma unroll
+              for (int h = 0; h < 4; ++h)
+                reinterpret_cast<uint4*>(dst + d)[h] = make_uint4(pack_bf16(o[8 * h] * f, o[8 * h + 1] * f), pack_bf16(o[8 * h + 2] * f, o[8 * h + 3] * f),
+                                                                  pack_bf16(o[8 * h + 4] * f, o[8 * h + 5] * f), pack_bf16(o[8 * h + 6] * f, o[8 * h + 7] * f));
+            } else {
+#pragma unroll
+              for (int h = 0; h < 32; ++h) dst[d + h] = __float2bfloat16_rn(o[h] * f);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 8; ++h)
+            reinterpret_cast<float4*>(st)[(d / 4 + h) * 128 + r] = make_float4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]);
+        }
+      }
+      tc_fence_before();
+      ok = sync_and<1, 256>(ok);  // dV and dK have been read before any warp lets the next unit's products begin
+      if (!ok) break;
+      go = w.next();
+    }
+    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+// Adds up the parts of a unit that several CTAs share, in their order: CTA (cut i + 1, 32 of 128 rows). Kind ByQueries: dq and
+// delta; ByKeys: dv and dk.
+template <int HD, typename Kind>
+__global__ void __launch_bounds__(256) k_packed_back_join(const PackedParams a, int most) {
+  constexpr bool KEYS = Kind::KEYS;
+  constexpr int STATE = KEYS ? BackLayout<HD>::DKV_STATE : BackLayout<HD>::DQ_STATE, WIDTH = KEYS ? 2 * HD : HD;
+  extern __shared__ int s_pre[];
+  __shared__ int s_bad;
+  __shared__ Cut s_cut[2];
+  const int tid = threadIdx.x, warp = tid >> 5, G = a.Hq / a.Hkv, tok = 128 / G;
+  pdl_launch_dependents();
+  pdl_wait();
+  Line<Kind> line = {{tok}, a.t, a.Hkv, 0, nullptr};
+  if (!line.build(s_pre, &s_bad, a.err)) return;
+  const int workers = line.workers(most), i = blockIdx.x + 1;
+  if (i >= workers || line.total == 0) return;
+  if (warp < 2) {
+    const Cut c = line.cut(i - 1 + warp, workers);
+    if ((tid & 31) == 0) s_cut[warp] = c;
+  }
+  __syncthreads();
+  const Cut before = s_cut[0], c = s_cut[1];
+  if (c.b >= a.t.n_seqs || c.step == 0 || (same_unit(before, c) && before.step > 0)) return;
+  int last = i;  // the part of CTA `last` ends the unit
+  while (last + 1 < workers) {
+    const Cut d = line.cut(last + 1, workers);
+    if (!same_unit(d, c)) break;
+    ++last;
+  }
+  const int r = blockIdx.y * 32 + (tid & 31), r_tok = r / G;
+  const int index = KEYS ? c.u * PT_KEYS + r : c.u * tok + r_tok;
+  if (index >= c.n || (!KEYS && r_tok >= tok)) return;
+  const long long row = c.row0 + index;
+  auto part = [&](int k) { return a.states + (long long)(2 * k + (k == i - 1 ? 1 : 0)) * STATE; };
+#pragma unroll 1
+  for (int x = warp; x < WIDTH / 4; x += 8) {
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = i - 1; k <= last; ++k) {
+      const float4 v = reinterpret_cast<const float4*>(part(k))[x * 128 + r];
+      o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+    }
+    bf16* dst;
+    float f = a.scale;
+    if (!KEYS) {
+      dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (c.kvh * G + r - r_tok * G) * HD + 4 * x;
+    } else if (x < HD / 4) {
+      dst = reinterpret_cast<bf16*>(a.dv) + row * a.ld_dv + c.kvh * HD + 4 * x;
+      f = 1.f;
+    } else {
+      dst = reinterpret_cast<bf16*>(a.dk) + row * a.ld_dk + c.kvh * HD + 4 * x - HD;
+    }
+    dst[0] = __float2bfloat16_rn(o.x * f), dst[1] = __float2bfloat16_rn(o.y * f);
+    dst[2] = __float2bfloat16_rn(o.z * f), dst[3] = __float2bfloat16_rn(o.w * f);
+  }
+  if (!KEYS && warp == 0) {
+    float eps = 0.f;
+    for (int k = i - 1; k <= last; ++k) eps += part(k)[128 * HD + r];
+    a.delta[row * a.Hq + c.kvh * G + r - r_tok * G] = part(i - 1)[128 * (HD + 1) + r] + eps;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------
 struct PackedDevice {
@@ -636,7 +1314,10 @@ PerDeviceOnce g_tc_once;
 PackedDevice g_tc[PerDeviceOnce::kMaxDevices];
 template <int HD>
 cudaError_t tc_prepare() {
-  return cudaFuncSetAttribute(k_packed_attn_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdLayout<HD>::TOTAL);
+  cudaError_t e = cudaFuncSetAttribute(k_packed_attn_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdLayout<HD>::TOTAL);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BackLayout<HD>::TOTAL);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dkv_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BackLayout<HD>::TOTAL);
+  return e;
 }
 const PackedDevice* tc_device() {
   int dev = 0;
@@ -658,8 +1339,8 @@ bool tc_map(CUtensorMap* m, const void* p, long long ld, int heads, int hd, int 
   return encode_tmap_bf16_3d(m, p, dims, strides, box);
 }
 
-// Whether units can be cut: a text of one key tile has units of one step.
-bool tc_cuts(const jf_packed& t) { return t.max_rows > PT_KEYS; }
+// Whether units can be cut: a cut has more than PT_SNAP steps on either side. tile: rows of a step.
+bool tc_cuts(const jf_packed& t, int tile) { return t.max_rows > (2 * PT_SNAP + 1) * tile; }
 
 template <int HD>
 jf_status tc_forward(const PackedParams& a, int sms, cudaStream_t st) {
@@ -669,7 +1350,23 @@ jf_status tc_forward(const PackedParams& a, int sms, cudaStream_t st) {
       !tc_map(&maps.v, a.v, a.ld_v, a.Hkv, HD, a.t.n_rows, 1, 128))
     return JF_ECUDA;
   cudaError_t e = packed_launch(k_packed_attn_tc<HD>, dim3(sms), dim3(PA_THREADS), FwdLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t)) e = packed_launch(k_packed_attn_join<HD>, dim3(sms - 1, 8), dim3(256), (a.t.n_seqs + 1) * 4, st, a, sms);
+  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_attn_join<HD>, dim3(sms - 1, 8), dim3(256), (a.t.n_seqs + 1) * 4, st, a, sms);
+  return e == cudaSuccess ? JF_OK : JF_ECUDA;
+}
+
+template <int HD>
+jf_status tc_backward(const PackedParams& a, int sms, cudaStream_t st) {
+  BackMaps maps;
+  const int G = a.Hq / a.Hkv, tok = 128 / G;
+  if (!tc_map(&maps.q, a.q, a.ld_q, a.Hq, HD, a.t.n_rows, G, tok) || !tc_map(&maps.d_out, a.d_out, a.ld_do, a.Hq, HD, a.t.n_rows, G, tok) ||
+      !tc_map(&maps.k, a.k, a.ld_k, a.Hkv, HD, a.t.n_rows, 1, 128) || !tc_map(&maps.v, a.v, a.ld_v, a.Hkv, HD, a.t.n_rows, 1, 128))
+    return JF_ECUDA;
+  const dim3 join(sms - 1, 4);
+  const size_t pre = (a.t.n_seqs + 1) * 4;
+  cudaError_t e = packed_launch(k_packed_dq_tc<HD>, dim3(sms), dim3(PB_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
+  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByQueries>, join, dim3(256), pre, st, a, sms);
+  if (e == cudaSuccess) e = packed_launch(k_packed_dkv_tc<HD>, dim3(sms), dim3(PB_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
+  if (e == cudaSuccess && tc_cuts(a.t, tok)) e = packed_launch(k_packed_back_join<HD, ByKeys>, join, dim3(256), pre, st, a, sms);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 
@@ -677,10 +1374,19 @@ jf_status tc_forward(const PackedParams& a, int sms, cudaStream_t st) {
 
 bool packed_tc_rows(const void* p, long long ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
-jf_status packed_tc_workspace(const jf_packed& t, int, int, int hd, bool, size_t* out_bytes) {
+// Backward: delta (read by the copies' form and by the other one), then the parts.
+static size_t delta_bytes(const jf_packed& t, int Hq) { return ((size_t)t.n_rows * Hq * 4 + 15) / 16 * 16; }
+
+jf_status packed_tc_workspace(const jf_packed& t, int Hq, int Hkv, int hd, bool backward, size_t* out_bytes) {
   const PackedDevice* d = tc_device();
   if (!d) return JF_ECUDA;
-  *out_bytes = tc_cuts(t) ? (size_t)2 * d->sms * (hd == 128 ? FwdLayout<128>::STATE : FwdLayout<64>::STATE) * 4 : 0;
+  const size_t parts = (size_t)2 * d->sms * 4;
+  if (!backward) {
+    *out_bytes = tc_cuts(t, PT_KEYS) ? parts * (hd == 128 ? FwdLayout<128>::STATE : FwdLayout<64>::STATE) : 0;
+  } else {
+    *out_bytes = delta_bytes(t, Hq);
+    if (tc_cuts(t, 128 / (Hq / Hkv))) *out_bytes += parts * (hd == 128 ? BackLayout<128>::DKV_STATE : BackLayout<64>::DKV_STATE);
+  }
   return JF_OK;
 }
 
@@ -690,6 +1396,15 @@ jf_status packed_tc_forward(const PackedParams& p, int hd, void* workspace, cuda
   PackedParams a = p;
   a.states = reinterpret_cast<float*>(workspace);
   return hd == 128 ? tc_forward<128>(a, d->sms, st) : tc_forward<64>(a, d->sms, st);
+}
+
+jf_status packed_tc_backward(const PackedParams& p, int hd, void* workspace, cudaStream_t st) {
+  const PackedDevice* d = tc_device();
+  if (!d) return JF_ECUDA;
+  PackedParams a = p;
+  a.delta = reinterpret_cast<float*>(workspace);
+  a.states = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + delta_bytes(a.t, a.Hq));
+  return hd == 128 ? tc_backward<128>(a, d->sms, st) : tc_backward<64>(a, d->sms, st);
 }
 
 }  // namespace jf
