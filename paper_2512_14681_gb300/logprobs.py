@@ -168,10 +168,11 @@ def policy_loss(logits, targets, old_logprob, advantage, weight=None, ref_logpro
     of = lambda t, name: None if t is None else _vector(t, rows, torch.float32, dev, name)
     r = torch.empty(5, rows, dtype=torch.float32, device=dev).unbind()
     need = _policy_need(dtype, rows, vocab)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev)  # the call's own, as in Kv8Cache.attention
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # the call's own, as in Kv8Cache.attention
     _checked(lib.jf_op_policy_loss(C.byref(J.PolicyTerms(below, above, kl, entropy)), dtype, logits.data_ptr(), ld, rows, vocab, scale,
                                    _vector(targets, rows, torch.int32, dev, "targets"), of(old_logprob, "old_logprob"),
                                    of(ref_logprob, "ref_logprob"), _vector(advantage, rows, torch.float32, dev, "advantage"),
                                    of(weight, "weight"), *(t.data_ptr() for t in r), out.data_ptr() if want_grad else None, ld_out,
-                                   ws.data_ptr(), need, _error_word(dev).data_ptr(), _raw_stream(dev)), "jf_op_policy_loss")
+                                   ws.data_ptr() if need else None, need, _error_word(dev).data_ptr(), _raw_stream(dev)),
+             "jf_op_policy_loss")
     return PolicyLoss(*r, out)
