@@ -4,10 +4,11 @@
 //   loss = w (-min(ratio A, clip(ratio) A) + beta (e^d - 1 - d) - eta H)
 //   dloss/dlp = w (-ratio A [ratio A <= clip(ratio) A] + beta (1 - e^d)) = g
 //   dloss/dlogit_i = scale (g (1{i = target} - p_i) + w eta p_i (ln p_i + H))
-// Loss and gradient are one pass: a cluster of CTAs holds a row in registers between its sums and its gradient, so that every
+// Loss and gradient are one pass: a cluster of CTAs holds a row in shared memory between its sums and its gradient, so that every
 // logit is read once and every gradient written once. Rows longer than a cluster of eight holds take the log probabilities'
 // two kernels, with one for the rows between them.
 #include "jf_logprobs.cuh"
+#include "jf_once.h"
 
 namespace jf {
 namespace {
@@ -60,17 +61,38 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 }
 
 // ---------------------------------------------------------------------------------------------
-// One pass: cluster (row), each CTA a run of the row's vectors, U a thread.
+// One pass: cluster (row), each CTA a run of the row's 16-byte vectors, which bulk copies bring to shared memory.
+//
+// In the log2 domain, with c = scale log2 e and a reference b = c m rounded (m the thread's largest logit): y = x c - b comes
+// rounded once from a fused product, S = sum 2^y, T = sum 2^y y; states are joined by their b. Then
+//   lp = ln 2 (y_t - log2 S),  H = ln 2 (log2 S - T / S),  p = 2^y / S,
+//   dloss/dx = -scale / S 2^y (g + gh (H - ln S) + gh ln 2 y), + scale g at the target.
+// Logits below -1e30 (and c above 1e6) would leave fp32's range in y: they count as -1e30, whose 2^y is 0, unless the row's
+// largest is such a one itself; its sums then are taken again from differences x - m.
 // ---------------------------------------------------------------------------------------------
-constexpr int PL_THREADS = 512, PL_WARPS = PL_THREADS / 32, PL_MOST = 10, PL_CLUSTER = 8;
+constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8, PL_CHUNKS = 2;
+constexpr int PL_FIT[3] = {56832, 76288, 115200};  // bytes of a CTA's run with which four, three, two are resident on an SM
+constexpr int PL_MOST = PL_FIT[2];
+constexpr float PL_FAR = 1e30f, PL_LARGE = 1e29f, PL_STEEP = 1e6f, LN2 = 0.69314718055994531f;
 
-// (m, S, T) of a warp's lanes, joined in lane order.
-JF_DEV LpStat join_lanes(LpStat st, int lanes, int lane, float c) {
-  for (int o = 1; o < lanes; o <<= 1) {
-    const LpStat b = {__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o), __shfl_xor_sync(0xffffffffu, st.t, o)};
-    st = lane & o ? lp_join(b, st, c) : lp_join(st, b, c);
+JF_DEV float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+// (b, S, T) of groups of `lanes` lanes, joined: every lane gets its group's. S and T of a lane without a reference (b = -infinity)
+// are 0, or NaN.
+JF_DEV LpStat join_lanes(LpStat st, int lanes) {
+  float b = st.m;
+  for (int o = lanes >> 1; o > 0; o >>= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
+  const float d = st.m == -INFINITY ? 0.f : st.m - b, f = ex2_ftz(d);
+  st.t = f * (st.t + d * st.s);
+  st.s = f * st.s;
+  for (int o = lanes >> 1; o > 0; o >>= 1) {
+    st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
+    st.t += __shfl_xor_sync(0xffffffffu, st.t, o);
   }
-  return st;
+  return {b, st.s, st.t};
 }
 JF_DEV float ld_cluster(uint32_t a) {
   float v;
@@ -78,170 +100,331 @@ JF_DEV float ld_cluster(uint32_t a) {
   return v;
 }
 
+// The largest of a vector's values (NaN ignored) and `most`.
+JF_DEV float largest(const uint4& v, float most, float) {
+  return fmaxf(fmaxf(most, fmaxf(__uint_as_float(v.x), __uint_as_float(v.y))), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+}
+JF_DEV float largest(const uint4& v, float most, bf16) {
+  const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&v);
+  const __nv_bfloat162 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+  return fmaxf(most, fmaxf(__low2float(m), __high2float(m)));
+}
+JF_DEV float max_nan(float x, float y) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+// Two fp32 values as one register pair: constants are packed once, and vectors from shared memory are pairs already.
+typedef unsigned long long Pair;
+JF_DEV Pair pair(float x, float y) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+  return r;
+}
+JF_DEV F2 halves(Pair p) {
+  F2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
+}
+JF_DEV Pair fma_pair(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+JF_DEV Pair add_pair(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+JF_DEV Pair mul_pair(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+JF_DEV Pair ex2_pair(Pair y) {
+  const F2 v = halves(y);
+  return pair(ex2_ftz(v.x), ex2_ftz(v.y));
+}
+// A vector's values, none below -PL_FAR (NaN kept).
+JF_DEV void raised(const uint4& v, Pair (&x)[2], float) {
+  x[0] = pair(max_nan(__uint_as_float(v.x), -PL_FAR), max_nan(__uint_as_float(v.y), -PL_FAR));
+  x[1] = pair(max_nan(__uint_as_float(v.z), -PL_FAR), max_nan(__uint_as_float(v.w), -PL_FAR));
+}
+JF_DEV void raised(const uint4& v, Pair (&x)[4], bf16) {
+  const __nv_bfloat162 far = __float2bfloat162_rn(-PL_FAR);
+  const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 m = __hmax2_nan(w[i], far);
+    const uint32_t u = *reinterpret_cast<const uint32_t*>(&m);
+    x[i] = pair(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  }
+}
+
 // 16 bytes from byte `skip` (2 .. 14, even) on of two pieces that lie one behind the other.
 JF_DEV uint4 straddle(const uint4& x, const uint4& y, int skip) {
   const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-  const int sh = (skip & 2) * 8;
-  uint32_t o[4];
+  uint32_t p[6], q[5], o[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint32_t lo = w[k], hi = w[k + 1];
+  for (int k = 0; k < 6; ++k) p[k] = skip & 8 ? w[k + 2] : w[k];
 #pragma unroll
-    for (int i = 1; i < 4; ++i) {
-      lo = skip >> 2 == i ? w[k + i] : lo;
-      if (k + i + 1 < 8) hi = skip >> 2 == i ? w[k + i + 1] : hi;
-    }
-    o[k] = __funnelshift_r(lo, hi, sh);
-  }
+  for (int k = 0; k < 5; ++k) q[k] = skip & 4 ? p[k + 1] : p[k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = __funnelshift_r(q[k], q[k + 1], (skip & 2) * 8);
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
+// A row's inputs beside its logits.
+struct PolicyInputs {
+  int target;
+  float old, ref, A, w;
+};
 
-template <typename T, int U>
-__global__ void __launch_bounds__(PL_THREADS, 2) k_policy(const PolicyParams a) {
+// Clusters walk over rows; while a row's gradient leaves, one thread asks for the next row's logits in the places that have been read.
+template <typename T>
+__global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) {
   constexpr int N = Vec<T>::N;
-  __shared__ LpStat s_warp[PL_WARPS], s_cta;
-  __shared__ float s_row[5];  // m, ln S, H, g, gh
+  extern __shared__ __align__(128) uint4 s_run[];
+  __shared__ __align__(8) uint64_t b_there[PL_CHUNKS];
+  __shared__ LpStat s_warp[PL_WARPS];
+  __shared__ float s_max[PL_WARPS], s_cta[2][4], s_far[2][2];  // by turns (peers read them): the CTA's b, S, T and largest logit; S, T from differences
+  __shared__ float s_row[8];                                    // b, log2 S, S, H, g, gh, m, whether far
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < PL_CHUNKS; ++i) mbar_init(smem_u32(&b_there[i]), 1);
+    fence_mbar_init();
+  }
   pdl_launch_dependents();
   pdl_wait();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  __syncthreads();
   uint32_t parts;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
-  const int rank = (int)cluster_rank(), row = blockIdx.x / parts;
-  const Row<T> r(reinterpret_cast<const T*>(a.logits) + row * a.ld, a.V);
-  const int v_begin = (int)((long long)r.n_vec * rank / (int)parts), v_end = (int)((long long)r.n_vec * (rank + 1) / (int)parts);
+  const int rank = (int)cluster_rank(), lg = 31 - __clz(parts), rows_apart = gridDim.x >> lg;  // (parts: a power of two)
+  const T* logits = reinterpret_cast<const T*>(a.logits);
   const float c = a.scale * LOG2E;
-  uint4 raw[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int v = v_begin + u * PL_THREADS + tid;
-    raw[u] = v < v_end ? Vec<T>::raw(r.vec(v)) : Vec<T>::nothing();
-  }
-  const int e = r.edge(tid);
-  const bool edge = e >= 0 && rank == (tid < N ? 0 : (int)parts - 1);
-  const float at_edge = edge ? act_to_f32(r.p[e]) : -INFINITY;
-  const int target = a.targets[row];
-  const float x_t = target >= 0 && target < a.V ? act_to_f32(r.p[target]) : 0.f;  // (before a gradient in its place)
+  // vectors of a chunk: the same for all rows, whose runs may differ by one (a row's next chunk must not reach into the one behind)
+  const int chunk = ((a.V / N + (int)parts - 1 >> lg) + PL_CHUNKS - 1) / PL_CHUNKS;
+  // chunk i of a row's run
+  auto ask = [&](int row, int i) {
+    const Row<T> r(logits + row * a.ld, a.V);
+    const int v_begin = r.n_vec * rank >> lg, n = (r.n_vec * (rank + 1) >> lg) - v_begin;
+    const int first = min(n, i * chunk), bytes = (min(n, first + chunk) - first) * 16;
+    mbar_arrive_expect_tx(smem_u32(&b_there[i]), (uint32_t)bytes);
+    if (bytes > 0) bulk_load(smem_u32(s_run + first), r.vec(v_begin + first), (uint32_t)bytes, smem_u32(&b_there[i]));
+  };
+  auto inputs = [&](int row) {  // (asked for a row ahead)
+    PolicyInputs q = {-1, 0.f, 0.f, 0.f, 0.f};
+    if (row < a.rows) {
+      q.target = a.targets[row];
+      if (a.old_lp) q.old = a.old_lp[row];
+      if (a.ref_lp) q.ref = a.ref_lp[row];
+      q.A = a.adv[row];
+      q.w = a.weight ? a.weight[row] : 1.f;
+    }
+    return q;
+  };
+  int row = blockIdx.x >> lg, turn = 0;
+  if (tid == 0 && row < a.rows)
+    for (int i = 0; i < PL_CHUNKS; ++i) ask(row, i);
+  PolicyInputs next = inputs(row);
+  for (; row < a.rows; row += rows_apart, turn ^= 1) {
+    const Row<T> r(logits + row * a.ld, a.V);
+    const int v_begin = r.n_vec * rank >> lg, n = (r.n_vec * (rank + 1) >> lg) - v_begin;
+    const PolicyInputs in = next;
+    next = inputs(row + rows_apart);
+    const int e = r.edge(tid), target = in.target;
+    const bool edge = e >= 0 && rank == (tid < N ? 0 : (int)parts - 1);
+    const float at_edge = edge ? act_to_f32(r.p[e]) : -INFINITY;
+    const float x_t = target >= 0 && target < a.V ? act_to_f32(r.p[target]) : 0.f;  // (before a gradient in its place)
 
-  float m = at_edge;
+    float m = at_edge;
+    for (int i = 0; i < PL_CHUNKS; ++i) {
+      if (!mbar_wait_bounded(smem_u32(&b_there[i]), (uint32_t)turn, kWaitLimitDefaultNs)) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
+      const int end = min(n, (i + 1) * chunk);
+#pragma unroll 4
+      for (int v = i * chunk + tid; v < end; v += PL_THREADS) m = largest(s_run[v], m, T{});
+    }
+    LpStat st;
+    {
+      const float b = c <= PL_STEEP && fabsf(m) < PL_LARGE ? c * m : -INFINITY;  // (-inf: the thread's sums do not count, or are taken again)
+      const float minus = b == -INFINITY ? 0.f : -b;
+      const Pair cc = pair(c, c), nb = pair(minus, minus);
+      Pair s = 0, t = 0;
+      auto add = [&](Pair x) {
+        const Pair y = fma_pair(x, cc, nb), p = ex2_pair(y);
+        s = add_pair(s, p);
+        t = fma_pair(p, y, t);
+      };
+      // (the vectors that the thread has looked at)
+#pragma unroll 1
+      for (int i = 0; i < PL_CHUNKS; ++i) {
+        const int end = min(n, (i + 1) * chunk);
+#pragma unroll 2
+        for (int v = i * chunk + tid; v < end; v += PL_THREADS) {
+          Pair x[N / 2];
+          raised(s_run[v], x, T{});
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float x[N];
-    Vec<T>::unpack(raw[u], x);
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
-  }
-  LpStat st;
-  {
-    const float base = m == -INFINITY ? 0.f : -m;
-    F2 s = {0.f, 0.f}, t = {0.f, 0.f};
-    auto add = [&](F2 x) {
-      const F2 d = add2(x, {base, base});
-      F2 p = mul2(d, {c, c});
-      p = {ex2_ftz(p.x), ex2_ftz(p.y)};
-      s = add2(s, p);
-      t = fma2(p, {fmaxf(d.x, -1e30f), fmaxf(d.y, -1e30f)}, t);  // (0 where x = -inf)
+          for (int k = 0; k < N / 2; ++k) add(x[k]);
+        }
+      }
+      if (edge) add(pair(max_nan(at_edge, -PL_FAR), -PL_FAR));
+      st = {b, halves(s).x + halves(s).y, halves(t).x + halves(t).y};
+      if (b == -INFINITY && st.s == st.s) st.s = st.t = 0.f;  // (a NaN among them counts)
+      st = join_lanes(st, 32);
+      m = warp_max(m);
+    }
+    if (lane == 0) s_warp[warp] = st, s_max[warp] = m;
+    __syncthreads();
+    if (warp == 0) {
+      st = join_lanes(s_warp[lane & (PL_WARPS - 1)], PL_WARPS);
+      m = warp_max(s_max[lane & (PL_WARPS - 1)]);
+      if (lane == 0) s_cta[turn][0] = st.m, s_cta[turn][1] = st.s, s_cta[turn][2] = st.t, s_cta[turn][3] = m;
+      __syncwarp();
+    }
+    if (parts > 1) cluster_sync();
+    bool none = false, far = false;
+    if (warp == 0) {
+      if (parts > 1) {
+        const uint32_t from = map_to_rank(smem_u32(s_cta[turn]), (uint32_t)lane & (parts - 1));
+        const float peer_m = ld_cluster(from + 12);
+        st = join_lanes({ld_cluster(from), ld_cluster(from + 4), ld_cluster(from + 8)}, (int)parts);
+        m = warp_max(peer_m);
+      }
+      none = m == -INFINITY, far = !none && (c > PL_STEEP || !(fabsf(m) < PL_LARGE));
+    }
+    auto finish = [&]() {  // by warp 0
+      const bool empty = none && st.s == 0.f;  // no token can occur
+      const float l2 = log2f(st.s), H = empty ? 0.f : LN2 * (l2 - st.t / st.s);
+      float lp = 0.f;
+      if (target >= a.V) {
+        lp = __int_as_float(0x7fffffff);
+      } else if (target >= 0) {
+        const float y = far ? (x_t - m) * c : fmaf(x_t, c, -st.m);
+        lp = empty ? -INFINITY : LN2 * (y - l2);
+      }
+      const PolicyRow p = policy_row(a, target, lp, H, in.old, in.ref, in.A, in.w);
+      if (lane == 0) {
+        s_row[0] = st.m, s_row[1] = l2, s_row[2] = st.s, s_row[3] = H, s_row[4] = empty ? 0.f : p.g, s_row[5] = empty ? 0.f : p.gh;
+        if (rank == 0) {
+          if (target >= a.V) jf_set_error(a.err, JF_DERR_BOUNDS);
+          if (a.loss) a.loss[row] = p.loss;
+          if (a.lp) a.lp[row] = lp;
+          if (a.H) a.H[row] = H;
+          if (a.ratio) a.ratio[row] = p.ratio;
+          if (a.kl) a.kl[row] = p.kl;
+        }
+      }
+      __syncwarp();
     };
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float x[N];
-      Vec<T>::unpack(raw[u], x);
-#pragma unroll
-      for (int i = 0; i < N; i += 2) add({x[i], x[i + 1]});
+    if (warp == 0) {
+      if (lane == 0) s_row[6] = m, s_row[7] = far ? 1.f : 0.f;
+      if (!far) finish();
+      __syncwarp();
     }
-    if (edge) add({at_edge, -INFINITY});
-    st = join_lanes({m, s.x + s.y, t.x + t.y}, 32, lane, c);
-  }
-  if (lane == 0) s_warp[warp] = st;
-  __syncthreads();
-  if (warp == 0) {
-    st = join_lanes(s_warp[lane & (PL_WARPS - 1)], PL_WARPS, lane, c);
-    if (lane == 0) s_cta = st;
-    __syncwarp();
-  }
-  if (parts > 1) cluster_sync();
-  if (warp == 0) {
-    if (parts > 1) {
-      const uint32_t from = map_to_rank(smem_u32(&s_cta), (uint32_t)lane & (parts - 1));
-      st = join_lanes({ld_cluster(from), ld_cluster(from + 4), ld_cluster(from + 8)}, (int)parts, lane, c);
+    __syncthreads();
+    m = s_row[6];
+    far = s_row[7] != 0.f;
+    if (far) {  // (uniform in the cluster)
+      float s = 0.f, t = 0.f;
+      auto add = [&](float x) {
+        const float d = fmaxf(x - m, -PL_FAR) * c, p = x - m != x - m ? x - m : ex2_ftz(d);  // (a NaN stays one)
+        s += p;
+        t += p == 0.f ? 0.f : p * d;
+      };
+      const T* run = reinterpret_cast<const T*>(s_run);
+#pragma unroll 1
+      for (int v = tid; v < n * N; v += PL_THREADS) add(act_to_f32(run[v]));
+      if (edge) add(at_edge);
+      s = warp_sum(s), t = warp_sum(t);
+      if (lane == 0) s_warp[warp] = {0.f, s, t};
+      __syncthreads();
+      if (tid == 0) {
+        s = t = 0.f;
+        for (int w = 0; w < PL_WARPS; ++w) s += s_warp[w].s, t += s_warp[w].t;
+        s_far[turn][0] = s, s_far[turn][1] = t;
+      }
+      __syncthreads();
+      if (parts > 1) cluster_sync();
+      if (warp == 0) {
+        st = {0.f, 0.f, 0.f};
+        for (uint32_t k = 0; k < parts; ++k) {
+          const uint32_t from = map_to_rank(smem_u32(s_far[turn]), k);
+          st.s += ld_cluster(from), st.t += ld_cluster(from + 4);
+        }
+        finish();
+      }
+      __syncthreads();
     }
-    const bool none = st.m == -INFINITY && st.s == 0.f;  // no token can occur
-    const float base = st.m == -INFINITY ? 0.f : st.m, ls = logf(st.s), H = none ? 0.f : ls - a.scale * (st.t / st.s);
-    float lp = 0.f;
-    if (target >= a.V) lp = __int_as_float(0x7fffffff);
-    else if (target >= 0) lp = none ? -INFINITY : fmaf(x_t - base, a.scale, -ls);
-    const PolicyRow p = policy_row(a, target, lp, H, a.old_lp ? a.old_lp[row] : 0.f, a.ref_lp ? a.ref_lp[row] : 0.f, a.adv[row],
-                                   a.weight ? a.weight[row] : 1.f);
-    if (lane == 0) {
-      // a row without a token that can occur has no gradient
-      s_row[0] = st.m, s_row[1] = ls, s_row[2] = H, s_row[3] = p.g, s_row[4] = p.gh;
-      if (rank == 0) {
-        if (target >= a.V) jf_set_error(a.err, JF_DERR_BOUNDS);
-        if (a.loss) a.loss[row] = p.loss;
-        if (a.lp) a.lp[row] = lp;
-        if (a.H) a.H[row] = H;
-        if (a.ratio) a.ratio[row] = p.ratio;
-        if (a.kl) a.kl[row] = p.kl;
+    const bool more = row + rows_apart < a.rows;
+    const float b = s_row[0], l2 = s_row[1], S = s_row[2], H = s_row[3], g = s_row[4], gh = s_row[5], k = a.scale;
+    // -scale / S times (g + gh (H - ln S) + gh ln 2 y)
+    const float f = -k / S, share0 = f * fmaf(gh, H - LN2 * l2, g), share1 = f * (gh * LN2), hot = k * g;
+    const bool still = g == 0.f && gh == 0.f;  // (also a row without a token that can occur)
+    T* out = reinterpret_cast<T*>(a.grad) + (a.grad ? row * a.ld_grad : 0);
+    // the gradient by a logit without the target's own term
+    auto of1 = [&](float x) {
+      const float y = far ? fmaxf(x - m, -PL_FAR) * c : fmaf(max_nan(x, -PL_FAR), c, -b);
+      return still ? 0.f : ex2_ftz(y) * fmaf(fmaxf(y, -PL_FAR), share1, share0);
+    };
+    auto single = [&](int i, float x) { out[i] = to_act<T>(of1(x) + (i == target ? hot : 0.f)); };
+    // Vectors of the output: where it lies otherwise than the logits, each is of two neighbours' elements, and the first and the
+    // last of the run's are stored one by one.
+    const int skip = (int)((16 - ((uintptr_t)(out + r.head) & 15)) & 15), own = skip / (int)sizeof(T), n_out = skip ? n - 1 : n;
+    const int e0 = r.head + v_begin * N;  // the run's first element
+    if (a.grad) {
+      if (edge) single(e, at_edge);
+      if (skip && n > 0 && tid < N) {
+        const int i = tid < own ? tid : (n - 1) * N + tid;
+        single(e0 + i, act_to_f32(reinterpret_cast<const T*>(s_run)[i]));
       }
     }
-  }
-  __syncthreads();
-  // a peer's sums have been read; its memory is there until all have
-  if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  if (a.grad) {
-    const float mx = s_row[0], ls = s_row[1], H = s_row[2], g = s_row[3], gh = s_row[4];
-    const bool none = mx == -INFINITY && ls == -INFINITY, still = none || (g == 0.f && gh == 0.f);
-    const float k = a.scale;
-    // -scale p (g + gh (ln p + H)) of a logit; a probability of 0 without its infinite logarithm
-    auto of = [&](float x, float hot) {
-      const float lp = fmaf(x - mx, k, -ls), p = ex2_ftz(lp * LOG2E);
-      const float share = gh == 0.f ? g : fmaf(gh, fmaxf(lp, -1e4f) + H, g);
-      return still ? 0.f : k * fmaf(-p, share, hot);
-    };
-    T* out = reinterpret_cast<T*>(a.grad) + row * a.ld_grad;
-    if (edge) out[e] = to_act<T>(of(at_edge, e == target ? g : 0.f));
-    const int skip = (int)((16 - ((uintptr_t)(out + r.head) & 15)) & 15);  // bytes of a vector before its output's next 16-byte boundary
+    const Pair cc = pair(c, c), nb = pair(-b, -b), k0 = pair(share0, share0), k1 = pair(share1, share1);
+    auto vector = [&](int v, bool entropy) {
+      const uint4 w = skip ? straddle(s_run[v], s_run[v + 1], skip) : s_run[v];
+      const int i0 = e0 + v * N + own;
+      Pair x[N / 2];
+      float d[N];
+      raised(w, x, T{});
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int v = v_begin + u * PL_THREADS + tid, e0 = r.head + v * N;
-      float x[N], d[N];
-      Vec<T>::unpack(raw[u], x);
-      if (target >= e0 && target < e0 + N) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) d[i] = of(x[i], e0 + i == target ? g : 0.f);
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) d[i] = of(x[i], 0.f);
+      for (int i = 0; i < N / 2; ++i) {
+        const Pair y = fma_pair(x[i], cc, nb);
+        Pair p = ex2_pair(y);
+        p = mul_pair(p, entropy ? fma_pair(y, k1, k0) : k0);
+        d[2 * i] = halves(p).x, d[2 * i + 1] = halves(p).y;
       }
-      if (skip == 0) {
-        if (v < v_end) Vec<T>::store(out + e0, d);
-      } else {
-        // whole 16-byte pieces of the output, each of two neighbours' elements; a warp's ends go one by one
-        uint4 w, n;
-        if constexpr (N == 8) {
-          uint32_t q[4];
+      if (target >= i0 && target < i0 + N) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(d[2 * i], d[2 * i + 1]);
-            q[i] = *reinterpret_cast<const uint32_t*>(&b);
+        for (int i = 0; i < N; ++i) d[i] += i0 + i == target ? hot : 0.f;
+      }
+      Vec<T>::store(out + i0, d);
+    };
+    for (int i = 0; i < PL_CHUNKS; ++i) {
+      const int end = a.grad ? min(n_out, (i + 1) * chunk) : 0;
+      if (still || far) {
+#pragma unroll 1
+        for (int v = i * chunk + tid; v < end; v += PL_THREADS)
+#pragma unroll 1
+          for (int h = 0; h < N; ++h) {
+            const int at = v * N + own + h;
+            single(e0 + at, act_to_f32(reinterpret_cast<const T*>(s_run)[at]));
           }
-          w = make_uint4(q[0], q[1], q[2], q[3]);
-        } else {
-          w = make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
-        }
-        n.x = __shfl_down_sync(0xffffffffu, w.x, 1), n.y = __shfl_down_sync(0xffffffffu, w.y, 1);
-        n.z = __shfl_down_sync(0xffffffffu, w.z, 1), n.w = __shfl_down_sync(0xffffffffu, w.w, 1);
-        const int own = skip / (int)sizeof(T);
-        const bool whole = lane < 31 && v + 1 < v_end;
-        if (whole) __stcs(reinterpret_cast<uint4*>(out + e0 + own), straddle(w, n, skip));
-        if (v < v_end && (lane == 0 || !whole)) {
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (i < own ? lane == 0 : !whole) out[e0 + i] = to_act<T>(d[i]);
+      } else if (gh != 0.f) {
+#pragma unroll 2
+        for (int v = i * chunk + tid; v < end; v += PL_THREADS) vector(v, true);
+      } else {
+#pragma unroll 2
+        for (int v = i * chunk + tid; v < end; v += PL_THREADS) vector(v, false);
+      }
+      if (more) {  // the chunk has been read by all: the next row's takes its place
+        __syncthreads();
+        if (tid == 0) {
+          fence_proxy_async_smem();
+          ask(row + rows_apart, i);
         }
       }
     }
+    __syncthreads();  // (s_row)
   }
-  if (parts > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (parts > 1) cluster_sync();  // peers may still read this CTA's sums
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -261,39 +444,66 @@ __global__ void __launch_bounds__(128) k_policy_rows(const PolicyParams a) {
 
 size_t align16(size_t n) { return (n + 15) / 16 * 16; }
 
-// CTAs of a row's cluster and vectors of a thread; parts 0: a cluster does not hold the row. More CTAs than it takes where
-// rows are few.
-struct PolicyForm {
-  int parts, vecs;
-};
-PolicyForm policy_form(int dtype, int rows, int vocab) {
-  const int n = dtype == JF_BF16 ? Vec<bf16>::N : Vec<float>::N, vecs = vocab / n;
+// CTAs of a row's cluster; 0: a cluster does not hold the row. More CTAs than it takes where rows are few.
+int policy_parts(int dtype, int rows, int vocab) {
+  const int vecs = vocab / (dtype == JF_BF16 ? Vec<bf16>::N : Vec<float>::N);
   int parts = 1;
-  while (parts < PL_CLUSTER && (vecs + parts - 1) / parts > PL_MOST * PL_THREADS) parts *= 2;
-  if ((vecs + parts - 1) / parts > PL_MOST * PL_THREADS) return {0, 0};
+  while (parts < PL_CLUSTER && (vecs + parts - 1) / parts > PL_MOST / 16) parts *= 2;
+  if ((vecs + parts - 1) / parts > PL_MOST / 16) return 0;
   while (parts < PL_CLUSTER && (long long)rows * parts * 2 <= 152 && vecs / parts > 2 * PL_THREADS) parts *= 2;
-  const int each = (vecs + parts - 1) / parts;
-  return {parts, each <= 2 * PL_THREADS ? 2 : (each <= 5 * PL_THREADS ? 5 : 10)};
+  return parts;
 }
 
-template <typename T, int U>
-cudaError_t policy_launch(const PolicyParams& a, int parts, cudaStream_t st) {
+// Clusters that are resident at a time, by type, log2 of their CTAs, and place in PL_FIT.
+struct PolicyDevice {
+  int clusters[2][4][3];
+};
+PerDeviceOnce g_once;
+PolicyDevice g_policy[PerDeviceOnce::kMaxDevices];
+
+struct PolicyLaunch {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.rows * parts);
-  cfg.blockDim = dim3(PL_THREADS);
-  cfg.stream = st;
   cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = (unsigned)parts, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_policy<T, U>, a);
-}
+  PolicyLaunch(int clusters, int parts, size_t smem, cudaStream_t st) {
+    cfg.gridDim = dim3((unsigned)(clusters * parts));
+    cfg.blockDim = dim3(PL_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)parts, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+  }
+};
 template <typename T>
-cudaError_t policy_launch(const PolicyParams& a, PolicyForm f, cudaStream_t st) {
-  return f.vecs == 2 ? policy_launch<T, 2>(a, f.parts, st) : (f.vecs == 5 ? policy_launch<T, 5>(a, f.parts, st) : policy_launch<T, 10>(a, f.parts, st));
+cudaError_t policy_prepare(int (&clusters)[4][3]) {
+  cudaError_t e = cudaFuncSetAttribute(k_policy<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, PL_MOST);
+  for (int i = 0; i < 12 && e == cudaSuccess; ++i) {
+    PolicyLaunch l(1, 1 << i / 3, PL_FIT[i % 3], nullptr);
+    l.cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&clusters[i / 3][i % 3], k_policy<T>, &l.cfg);
+    if (e == cudaSuccess && clusters[i / 3][i % 3] < 1) e = cudaErrorInvalidConfiguration;
+  }
+  return e;
+}
+const PolicyDevice* policy_device() {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return nullptr;
+  const int rc = g_once.run(dev, [&]() -> int {
+    const cudaError_t e = policy_prepare<float>(g_policy[dev].clusters[0]);
+    return (int)(e == cudaSuccess ? policy_prepare<bf16>(g_policy[dev].clusters[1]) : e);
+  });
+  return rc == 0 ? &g_policy[dev] : nullptr;
+}
+
+template <typename T>
+cudaError_t policy_launch(const PolicyParams& a, int parts, const int (&resident)[4][3], cudaStream_t st) {
+  const int smem = (a.V / Vec<T>::N + parts - 1) / parts * 16;
+  const int most = resident[parts == 1 ? 0 : (parts == 2 ? 1 : (parts == 4 ? 2 : 3))][smem <= PL_FIT[0] ? 0 : (smem <= PL_FIT[1] ? 1 : 2)];
+  PolicyLaunch l(a.rows < most ? a.rows : most, parts, (size_t)smem, st);
+  return cudaLaunchKernelEx(&l.cfg, k_policy<T>, a);
 }
 
 }  // namespace
@@ -304,7 +514,7 @@ using namespace jf;
 extern "C" jf_status jf_op_policy_loss_workspace_bytes(int dtype, int rows, int vocab, size_t* out_bytes) {
   if ((dtype != JF_F32 && dtype != JF_BF16) || rows < 0 || vocab < 1 || !out_bytes) return JF_EINVAL;
   *out_bytes = 0;
-  if (rows == 0 || policy_form(dtype, rows, vocab).parts > 0) return JF_OK;
+  if (rows == 0 || policy_parts(dtype, rows, vocab) > 0) return JF_OK;
   size_t n = 0;
   const jf_status s = jf_op_token_logprobs_workspace_bytes(rows, vocab, 0, &n);
   if (s != JF_OK) return s;
@@ -335,10 +545,11 @@ extern "C" jf_status jf_op_policy_loss(const jf_policy_terms* terms, int dtype, 
   PolicyParams a = {*terms, logits, ld, ld_grad, rows, vocab, scale, targets, old_logprob, ref_logprob, advantage, weight, nullptr, nullptr,
                     loss, logprob, entropy, ratio, kl, grad_logits, nullptr, nullptr, err_word};
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const PolicyForm f = policy_form(dtype, rows, vocab);
-  if (f.parts > 0) {
-    if ((long long)rows * f.parts > 0x7fffffffll) return JF_EUNSUPPORTED;
-    const cudaError_t e = dtype == JF_BF16 ? policy_launch<bf16>(a, f, st) : policy_launch<float>(a, f, st);
+  const int parts = policy_parts(dtype, rows, vocab);
+  if (parts > 0) {
+    const PolicyDevice* d = policy_device();
+    if (!d) return JF_ECUDA;
+    const cudaError_t e = dtype == JF_BF16 ? policy_launch<bf16>(a, parts, d->clusters[1], st) : policy_launch<float>(a, parts, d->clusters[0], st);
     return e == cudaSuccess ? JF_OK : JF_ECUDA;
   }
   size_t scores = 0;
