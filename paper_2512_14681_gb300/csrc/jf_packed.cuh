@@ -22,6 +22,7 @@ struct PackedParams {
   void *dq, *dk, *dv;
   long long ld_do, ld_dq, ld_dk, ld_dv;
   float* delta;      // [n_rows][Hq]: sum of d_out * out
+  int* cuts;         // where CTAs' runs begin (null: no unit is shared by several)
   float* states;     // partial results of units that several CTAs share
   int* err;
 };

@@ -17,7 +17,7 @@ namespace {
 
 constexpr int PT_KEYS = 128;                     // keys of a step (of a tile, in dk and dv)
 constexpr int PT_MIN_SHARE = 4;                  // shortest run of a CTA
-constexpr int PT_SNAP = 1;                       // a cut moves to a unit's end over this many steps
+constexpr int PT_SNAP = 2, PT_WHOLE = 6;         // a cut moves to a unit's end over so many steps; units of so many are not cut
 
 // ---------------------------------------------------------------------------------------------
 // The line of units. Kind says how a text is cut: units(n), steps(n, u) for a text of n rows.
@@ -117,8 +117,10 @@ struct Line {
     }
     c.n_steps = kind.steps(c.n, c.u);
     c.step = max(0, rest - Kind::UC);
-    if (c.step <= PT_SNAP) c.step = 0;
-    if (c.n_steps - c.step <= PT_SNAP && c.step > 0) {
+    const int over = c.n_steps <= PT_WHOLE ? c.n_steps / 2 : PT_SNAP;
+    if (c.step <= over) {
+      c.step = 0;
+    } else if (c.n_steps <= PT_WHOLE || c.n_steps - c.step <= over) {
       c.step = 0;
       next(c);
     }
@@ -141,23 +143,53 @@ struct Line {
 };
 JF_DEV bool same_unit(const Cut& x, const Cut& y) { return x.b == y.b && x.kvh == y.kvh && x.u == y.u; }
 
-// A CTA's walk along its run: units from `at` to `end`, steps c0 .. c1 - 1 of each. Uniform.
+// A CTA's walk along its run: units from `at` to `end` (in shared memory), steps c0 .. c1 - 1 of each. Uniform.
 template <typename Kind>
 struct Run {
   Line<Kind> line;
-  Cut at, end;
-  JF_DEV bool there() const { return at.b < line.t.n_seqs && !(same_unit(at, end) && at.step >= end.step); }
+  Cut at;
+  const Cut* end;
+  JF_DEV bool there() const { return at.b < line.t.n_seqs && !(same_unit(at, *end) && at.step >= end->step); }
   JF_DEV int c0() const { return at.step; }
-  JF_DEV int c1() const { return same_unit(at, end) ? end.step : at.n_steps; }
+  JF_DEV int c1() const { return same_unit(at, *end) ? end->step : at.n_steps; }
   JF_DEV bool whole() const { return at.step == 0 && c1() == at.n_steps; }
   JF_DEV int slot(int cta) const { return 2 * cta + (at.step > 0 ? 0 : 1); }  // where a part goes
   JF_DEV bool next() {
-    if (same_unit(at, end)) return false;
+    if (same_unit(at, *end)) return false;
     at.step = 0;
     line.next(at);
     return there();
   }
 };
+
+// Where CTAs' runs begin, for the kernel that joins parts: two int4 a CTA.
+constexpr int NO_UNIT = 0x7fffffff;
+JF_DEV void tell_cut(int* cuts, const Cut& c, bool works) {
+  if (!cuts) return;
+  int4* at = reinterpret_cast<int4*>(cuts) + 2 * blockIdx.x;
+  at[0] = make_int4(works ? c.b : NO_UNIT, c.kvh, c.u, c.step);
+  at[1] = make_int4(c.n_steps, c.row0, c.n, 0);
+}
+JF_DEV Cut read_cut(const int* cuts, int cta) {
+  const int4 x = reinterpret_cast<const int4*>(cuts)[2 * cta], y = reinterpret_cast<const int4*>(cuts)[2 * cta + 1];
+  return {x.x, x.y, x.z, x.w, y.x, y.y, y.z};
+}
+// The parts of a unit that is cut by the beginning of CTA i's run and by none before: CTAs i - 1 .. last. False: there is no such unit.
+JF_DEV bool parts_from(const int* cuts, int ctas, int n_seqs, int i, Cut& c, int& last) {
+  c = read_cut(cuts, i);
+  if (c.b >= n_seqs || c.step == 0) return false;
+  const Cut before = read_cut(cuts, i - 1);
+  if (same_unit(before, c) && before.step > 0) return false;
+  for (last = i;; last += 32) {  // (a unit may lie in many runs)
+    const int k = last + 1 + (threadIdx.x & 31);
+    const bool same = k < ctas && same_unit(read_cut(cuts, k), c);
+    const unsigned rest = __ballot_sync(0xffffffffu, !same);
+    if (rest) {
+      last += __ffs(rest) - 1;
+      return true;
+    }
+  }
+}
 
 // ---------------------------------------------------------------------------------------------
 // Pieces of the kernels
@@ -177,6 +209,58 @@ JF_DEV float2 add2(float2 x, float2 y) {
       : "=f"(r.x), "=f"(r.y)
       : "f"(x.x), "f"(x.y), "f"(y.x), "f"(y.y));
   return r;
+}
+// 64 consecutive columns of this warp's 32 lanes, at once.
+JF_DEV void tmem_ld64(uint32_t taddr, float (&v)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+        "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+        "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+        "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
+        "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+      : "r"(taddr)
+      : "memory");
+}
+// 128 consecutive columns of this warp's 32 lanes, at once.
+JF_DEV void tmem_ld128(uint32_t taddr, float (&v)[128]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x128.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,"
+        "%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79,"
+        "%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,"
+        "%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,"
+        "%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,%126,%127}, [%128];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+        "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+        "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+        "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
+        "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63]),
+        "=f"(v[64]), "=f"(v[65]), "=f"(v[66]), "=f"(v[67]), "=f"(v[68]), "=f"(v[69]), "=f"(v[70]), "=f"(v[71]),
+        "=f"(v[72]), "=f"(v[73]), "=f"(v[74]), "=f"(v[75]), "=f"(v[76]), "=f"(v[77]), "=f"(v[78]), "=f"(v[79]),
+        "=f"(v[80]), "=f"(v[81]), "=f"(v[82]), "=f"(v[83]), "=f"(v[84]), "=f"(v[85]), "=f"(v[86]), "=f"(v[87]),
+        "=f"(v[88]), "=f"(v[89]), "=f"(v[90]), "=f"(v[91]), "=f"(v[92]), "=f"(v[93]), "=f"(v[94]), "=f"(v[95]),
+        "=f"(v[96]), "=f"(v[97]), "=f"(v[98]), "=f"(v[99]), "=f"(v[100]), "=f"(v[101]), "=f"(v[102]), "=f"(v[103]),
+        "=f"(v[104]), "=f"(v[105]), "=f"(v[106]), "=f"(v[107]), "=f"(v[108]), "=f"(v[109]), "=f"(v[110]), "=f"(v[111]),
+        "=f"(v[112]), "=f"(v[113]), "=f"(v[114]), "=f"(v[115]), "=f"(v[116]), "=f"(v[117]), "=f"(v[118]), "=f"(v[119]),
+        "=f"(v[120]), "=f"(v[121]), "=f"(v[122]), "=f"(v[123]), "=f"(v[124]), "=f"(v[125]), "=f"(v[126]), "=f"(v[127])
+      : "r"(taddr)
+      : "memory");
 }
 JF_DEV uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -221,11 +305,12 @@ struct Tile {
                 idesc_bf16_f32(128, 128), kk > 0 ? 1u : 0u, on);
   }
   // D[128][HD] (+)= w b over b's rows; w: bf16 in tensor memory, 64 columns, rows 64 .. at w + gap
+  template <int FIRST = 0, int LAST = 8>
   static JF_DEV void rows(uint32_t d, uint32_t w, uint32_t b, bool fresh, uint32_t on, uint32_t gap = 32) {
     uint64_t db = sdesc_mn_sw128(b, HALF, 1024u);
     asm volatile("" : "+l"(db));
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk)
+    for (int kk = FIRST; kk < LAST; ++kk)  // (16 of b's rows each)
       mma_ts_on(d, w + (kk >> 2) * gap + (kk & 3) * 8, db + (uint64_t)(kk * (2048 >> 4)), idesc_bf16_f32(128, HD) | (1u << 16),
                 kk > 0 || !fresh ? 1u : 0u, on);
   }
@@ -303,8 +388,9 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
   extern __shared__ uint8_t sm_raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sQ = smem_u32(sm), sKV = sQ + Lay::OFF_KV;
-  // queries there, read; keys or values there, read; per stream: S ready, P ready, P V done; everything done
-  __shared__ __align__(8) uint64_t b_q[2], b_qfree[2], b_kv[RING], b_kvfree[RING], b_s[2], b_p[2], b_o[2], b_all;
+  // queries there, read; keys or values there (b_raw: with rows to be cleared), read (by both streams); per stream: S ready, P ready (its first 64 keys, all), P V
+  // done; everything done
+  __shared__ __align__(8) uint64_t b_q[2], b_qfree[2], b_kv[RING], b_raw[RING], b_kvfree[RING], b_s[2], b_p[2][2], b_o[2], b_all[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int s_bad;
   __shared__ Cut s_cut[2];
@@ -315,20 +401,25 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
       mbar_init(smem_u32(&b_q[i]), 1);
       mbar_init(smem_u32(&b_qfree[i]), 1);
       mbar_init(smem_u32(&b_s[i]), 1);
-      mbar_init(smem_u32(&b_p[i]), 4);
+      mbar_init(smem_u32(&b_p[i][0]), 4);
+      mbar_init(smem_u32(&b_p[i][1]), 4);
       mbar_init(smem_u32(&b_o[i]), 1);
+      mbar_init(smem_u32(&b_all[i]), 1);
     }
     for (int i = 0; i < RING; ++i) {
       mbar_init(smem_u32(&b_kv[i]), 1);
-      mbar_init(smem_u32(&b_kvfree[i]), 1);
+      mbar_init(smem_u32(&b_raw[i]), 1);
+      mbar_init(smem_u32(&b_kvfree[i]), 2);
     }
-    mbar_init(smem_u32(&b_all), 1);
     fence_mbar_init();
   }
   pdl_launch_dependents();
   pdl_wait();
-  Run<ByQueries> w = {{{2 * tok}, a.t, a.Hkv, 0, nullptr}, {}, {}};
-  if (!w.line.build(reinterpret_cast<int*>(sm), &s_bad, a.err)) return;
+  Run<ByQueries> w = {{{2 * tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
+  if (!w.line.build(reinterpret_cast<int*>(sm), &s_bad, a.err)) {
+    if (tid == 0) tell_cut(a.cuts, {}, false);
+    return;
+  }
   const int workers = w.line.workers(gridDim.x);
   if (warp < 2 && (int)blockIdx.x < workers) {
     const Cut c = w.line.cut(blockIdx.x + warp, workers);
@@ -343,11 +434,11 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0);
-  const bool works = (int)blockIdx.x < workers && w.line.total > 0;
-  w.at = s_cut[0], w.end = s_cut[1];
-  bool ok = true, go = works && w.there();
+  w.at = s_cut[0];
+  bool ok = true, go = (int)blockIdx.x < workers && w.line.total > 0 && w.there();
+  if (tid == 0) tell_cut(a.cuts, w.at, (int)blockIdx.x < workers && w.line.total > 0);
   // steps of stream s of the unit in hand, within the run: from c0 on
-  auto stream_steps = [&](int s) {
+  auto stream_steps = [&](const Run<ByQueries>& w, int s) {
     const int first = (2 * w.at.u + s) * tok;  // its first token
     if (first >= w.at.n) return 0;
     return max(0, min(w.c1(), (min(w.at.n, first + tok) + PT_KEYS - 1) / PT_KEYS) - w.c0());
@@ -355,92 +446,105 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
 
   // Registers: 384 x 168 at launch; 128 x 80 + 256 x 208 are fewer.
   if (warp >= 8) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-  if (warp == 8) {
-    int tiles = 0, units[2] = {0, 0};
-    const uint32_t q_bytes = (uint32_t)(tok * G * HD * 2);
-    while (go) {
-      const int n = max(stream_steps(0), stream_steps(1));
-      for (int s = 0; s < 2 && ok; ++s) {
-        if (stream_steps(s) == 0) continue;
-        ok = units[s] == 0 || warp_wait(b_qfree[s], units[s] - 1);
-        if (ok && elect_one()) {
-          mbar_arrive_expect_tx(smem_u32(&b_q[s]), q_bytes);
-          T::load(sQ + s * Lay::Q, &maps.q, smem_u32(&b_q[s]), w.at.kvh * G, w.at.row0 + (2 * w.at.u + s) * tok);
-        }
-        __syncwarp();
-        if (ok) ++units[s];
-      }
-      for (int i = 0; i < 2 * n && ok; ++i) {  // K, V, K, V, ...
-        const int place = tiles % RING;
-        ok = tiles < RING || warp_wait(b_kvfree[place], tiles / RING - 1);
-        if (!ok) break;
-        if (elect_one()) {
-          mbar_arrive_expect_tx(smem_u32(&b_kv[place]), T::BYTES);
-          T::load(sKV + place * Lay::KV, i & 1 ? &maps.v : &maps.k, smem_u32(&b_kv[place]), w.at.kvh, w.at.row0 + (w.c0() + i / 2) * PT_KEYS);
-        }
-        __syncwarp();
-        ++tiles;
-      }
-      go = ok && w.next();
-    }
-    // every copy has landed before the CTA may leave, also after a wait that gave up
-    for (int i = max(0, tiles - RING); i < tiles; ++i) warp_wait(b_kv[i % RING], i / RING);
-    for (int s = 0; s < 2; ++s)
-      if (units[s]) warp_wait(b_q[s], units[s] - 1);
-    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
-  } else if (warp == 9) {
-    int tiles = 0, units[2] = {0, 0}, ns[2] = {0, 0}, np[2] = {0, 0};  // (S and P V issued)
-    const uint32_t on = elect_one();
-    // S of stream s; its place is P's of the product before, which has been read then
-    auto issue_s = [&](int s, int k_tile) {
-      if (np[s] > 0) ok = ok && warp_wait(b_o[s], np[s] - 1);
-      if (!ok) return;
-      tc_fence_after();
-      T::dots(tmem + s * 128, sQ + s * Lay::Q, sKV + k_tile % RING * Lay::KV, on);
-      commit_on(smem_u32(&b_s[s]), on);
-      ++ns[s];
-    };
-    while (go) {
-      const int n_of[2] = {stream_steps(0), stream_steps(1)}, n = max(n_of[0], n_of[1]);
-      ok = n == 0 || warp_wait(b_kv[tiles % RING], tiles / RING);
-      for (int s = 0; s < 2 && ok; ++s) {
-        if (n_of[s] == 0) continue;
-        ok = warp_wait(b_q[s], units[s]++);
-        if (ok) issue_s(s, tiles);
-        if (n_of[s] == 1) commit_on(smem_u32(&b_qfree[s]), on);
-      }
-      commit_on(smem_u32(&b_kvfree[tiles % RING]), on);
-      for (int j = 0; j < n && ok; ++j) {
-        const int v_tile = tiles + 2 * j + 1, k_next = v_tile + 1;
-        ok = warp_wait(b_kv[v_tile % RING], v_tile / RING);
-        const int held = w.at.n - (w.c0() + j) * PT_KEYS;
-        if (ok && held < PT_KEYS) T::clear_from(sKV + v_tile % RING * Lay::KV, held, lane);
-        if (ok && j + 1 < n) ok = warp_wait(b_kv[k_next % RING], k_next / RING);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 8) {
+      int tiles = 0, units[2] = {0, 0};
+      const uint32_t q_bytes = (uint32_t)(tok * G * HD * 2);
+      while (go) {
+        const int n0 = stream_steps(w, 0), n1 = stream_steps(w, 1), n = max(n0, n1);
         for (int s = 0; s < 2 && ok; ++s) {
-          if (j >= n_of[s]) continue;
-          ok = warp_wait(b_p[s], np[s]);
+          if ((s ? n1 : n0) == 0) continue;
+          ok = units[s] == 0 || warp_wait(b_qfree[s], units[s] - 1);
+          if (ok && elect_one()) {
+            mbar_arrive_expect_tx(smem_u32(&b_q[s]), q_bytes);
+            T::load(sQ + s * Lay::Q, &maps.q, smem_u32(&b_q[s]), w.at.kvh * G, w.at.row0 + (2 * w.at.u + s) * tok);
+          }
+          __syncwarp();
+          if (ok) ++units[s];
+        }
+        for (int i = 0; i < 2 * n && ok; ++i) {  // K, V, K, V, ...
+          const int place = tiles % RING;
+          ok = tiles < RING || warp_wait(b_kvfree[place], tiles / RING - 1);
+          if (!ok) break;
+          const bool raw = i == 2 * n - 1 && w.c1() * PT_KEYS > w.at.n;  // values of a text's last tile
+          if (elect_one()) {
+            const uint32_t bar = smem_u32(raw ? &b_raw[place] : &b_kv[place]);
+            mbar_arrive_expect_tx(bar, T::BYTES);
+            T::load(sKV + place * Lay::KV, i & 1 ? &maps.v : &maps.k, bar, w.at.kvh, w.at.row0 + (w.c0() + i / 2) * PT_KEYS);
+          }
+          __syncwarp();
+          ++tiles;
+        }
+        go = ok && w.next();
+      }
+      // every copy has landed before the CTA may leave, also after a wait that gave up (b_raw's are forwarded)
+      for (int i = max(0, tiles - RING); i < tiles; ++i) warp_wait(b_kv[i % RING], i / RING);
+      for (int s = 0; s < 2; ++s)
+        if (units[s]) warp_wait(b_q[s], units[s] - 1);
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+    } else if (warp < 11) {
+      // A stream's products. (A warp of its own for each: what one waits for does not hold up the other.)
+      const int s = warp - 9;
+      const uint32_t on = elect_one(), t_s = tmem + s * 128, t_o = tmem + 256 + s * 128;
+      int tiles = 0, units = 0, products = 0;  // tiles before the unit, units, P V so far
+      auto place_of = [&](int tile) { return __shfl_sync(0xffffffffu, tile % RING, 0); };
+      while (go) {
+        const int n = stream_steps(w, s), all = max(n, stream_steps(w, 1 - s));
+        if (n > 0) ok = warp_wait(b_q[s], units++);
+        for (int j = 0; j < n && ok; ++j) {
+          const int k_tile = tiles + 2 * j, v_tile = k_tile + 1, kp = place_of(k_tile), vp = place_of(v_tile);
+          ok = warp_wait(b_kv[kp], k_tile / RING);
+          // S: its place is P's of the product before, which has been read then
+          if (products > 0) ok = ok && warp_wait(b_o[s], products - 1);
           if (!ok) break;
           tc_fence_after();
-          T::rows(tmem + 256 + s * 128, tmem + s * 128, sKV + v_tile % RING * Lay::KV, j == 0, on);
+          T::dots(t_s, sQ + s * Lay::Q, sKV + kp * Lay::KV, on);
+          commit_on(smem_u32(&b_s[s]), on);
+          commit_on(smem_u32(&b_kvfree[kp]), on);
+          if (j + 1 == n) commit_on(smem_u32(&b_qfree[s]), on);
+          ok = warp_wait(b_kv[vp], v_tile / RING) && warp_wait(b_p[s][0], products);
+          if (!ok) break;
+          tc_fence_after();
+          T::template rows<0, 4>(t_o, t_s, sKV + vp * Lay::KV, j == 0, on);
+          ok = warp_wait(b_p[s][1], products);
+          if (!ok) break;
+          tc_fence_after();
+          T::template rows<4, 8>(t_o, t_s, sKV + vp * Lay::KV, false, on);
           commit_on(smem_u32(&b_o[s]), on);
-          ++np[s];
-          if (j + 1 < n_of[s]) {
-            issue_s(s, k_next);
-            if (j + 2 == n_of[s]) commit_on(smem_u32(&b_qfree[s]), on);
-          }
+          commit_on(smem_u32(&b_kvfree[vp]), on);
+          ++products;
         }
-        commit_on(smem_u32(&b_kvfree[v_tile % RING]), on);
-        if (j + 1 < n) commit_on(smem_u32(&b_kvfree[k_next % RING]), on);
+        for (int i = 2 * n; i < 2 * all && ok; ++i) {  // tiles of the other stream's alone: read as soon as they are there
+          const int place = place_of(tiles + i);
+          ok = warp_wait(b_kv[place], (tiles + i) / RING);
+          commit_on(smem_u32(&b_kvfree[place]), on);
+        }
+        tiles += 2 * all;
+        go = ok && w.next();
       }
-      tiles += 2 * n;
-      go = ok && w.next();
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
+      commit_on(smem_u32(&b_all[s]), on);
+      __syncwarp();
+      warp_wait(b_all[s], 0);  // every product is complete before the CTA may leave
+    } else {
+      // Values behind the end of a text are cleared before the products see the tile.
+      int tiles = 0;
+      unsigned uses = 0;  // of each place's b_raw, their parities
+      while (go) {
+        const int n = max(stream_steps(w, 0), stream_steps(w, 1));
+        tiles += 2 * n;
+        if (w.c1() * PT_KEYS > w.at.n) {
+          const int place = (tiles - 1) % RING;
+          ok = warp_wait(b_raw[place], (int)(uses >> place & 1u));
+          uses ^= 1u << place;
+          if (!ok) break;
+          T::clear_from(sKV + place * Lay::KV, w.at.n - (w.c1() - 1) * PT_KEYS, lane);
+          if (lane == 0) mbar_arrive(smem_u32(&b_kv[place]));
+        }
+        go = w.next();
+      }
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
     }
-    if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
-    commit_on(smem_u32(&b_all), on);
-    __syncwarp();
-    warp_wait(b_all, 0);  // every product is complete before the CTA may leave
-  }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     clear_rest<HD>(a, 0, 256);
@@ -451,7 +555,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
     const float c = fmaxf(fabsf(a.scale) * kLog2e, 7.888609e-31f /* 2^-100: a hidden key's -inf stays one */);
     int steps = 0;
     while (go) {
-      const int n = stream_steps(s);
+      const int n = stream_steps(w, s);
       const int i = (2 * w.at.u + s) * tok + r_tok;  // the row's token in its text
       const bool live = r_tok < tok && i < w.at.n;
       float m = -INFINITY, l = 0.f;
@@ -460,28 +564,23 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
         if (!ok) break;
         tc_fence_after();
         const int k0 = (w.c0() + j) * PT_KEYS;
-        float v[4][32];
-#pragma unroll
-        for (int h = 0; h < 4; ++h) tmem_ld32(t_s + 32 * h, v[h]);
+        float v[128];
+        tmem_ld128(t_s, v);
         if (flip) {
 #pragma unroll
-          for (int h = 0; h < 4; ++h)
-#pragma unroll
-            for (int x = 0; x < 32; ++x) v[h][x] = -v[h][x];
+          for (int x = 0; x < 128; ++x) v[x] = -v[x];
         }
         if (k0 + PT_KEYS > (2 * w.at.u + s) * tok) {  // (some row does not see all of them)
           const int see = i - k0;  // columns 0 .. see
 #pragma unroll
-          for (int h = 0; h < 4; ++h)
-#pragma unroll
-            for (int x = 0; x < 32; ++x) v[h][x] = 32 * h + x <= see ? v[h][x] : -INFINITY;
+          for (int x = 0; x < 128; ++x) v[x] = x <= see ? v[x] : -INFINITY;
         }
         float mx[4];
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
-          mx[h] = v[h][0];
+          mx[h] = v[h];
 #pragma unroll
-          for (int x = 1; x < 32; ++x) mx[h] = fmaxf(mx[h], v[h][x]);
+          for (int x = 4; x < 128; x += 4) mx[h] = fmaxf(mx[h], v[x + h]);
         }
         const float mc = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
         const bool raise = mc > m + PA_LAG;
@@ -498,19 +597,21 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
           uint32_t u[16];
 #pragma unroll
           for (int x = 0; x < 16; ++x) {
-            float2 p = fma2(make_float2(v[h][2 * x], v[h][2 * x + 1]), cc, base);
+            float2 p = fma2(make_float2(v[32 * h + 2 * x], v[32 * h + 2 * x + 1]), cc, base);
             p.x = packed_ex2(p.x);
             p.y = packed_ex2(p.y);
             sum = add2(sum, p);
             u[x] = pack_bf16(p.x, p.y);
           }
           tmem_st16(t_s + 16 * h, u);
+          if (h & 1) {
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&b_p[s][h >> 1]));
+          }
         }
         l += sum.x + sum.y;
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&b_p[s]));
       }
       if (!ok) break;
       if (n > 0) {
@@ -564,67 +665,38 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of the units that several CTAs share: CTA (cut i + 1, 32 of the unit's 256 rows). The unit that cut i lies
-// in is joined by the first cut in it: CTAs i - 1, i, ... hold its parts in order.
+// Joins the parts of the units that several CTAs share: CTA (run i + 1, 256 pieces of 4 columns of the unit's 256 rows).
 template <int HD>
-__global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a, int most) {
+__global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) {
   using Lay = FwdLayout<HD>;
-  extern __shared__ int s_pre[];
-  __shared__ int s_bad;
-  __shared__ Cut s_cut[2];
-  const int tid = threadIdx.x, warp = tid >> 5, G = a.Hq / a.Hkv, tok = 128 / G;
+  const int G = a.Hq / a.Hkv, tok = 128 / G, i = blockIdx.x + 1;
   pdl_launch_dependents();
   pdl_wait();
-  Line<ByQueries> line = {{2 * tok}, a.t, a.Hkv, 0, nullptr};
-  if (!line.build(s_pre, &s_bad, a.err)) return;
-  const int workers = line.workers(most), i = blockIdx.x + 1;
-  if (i >= workers || line.total == 0) return;
-  if (warp < 2) {
-    const Cut c = line.cut(i - 1 + warp, workers);
-    if ((tid & 31) == 0) s_cut[warp] = c;
-  }
-  __syncthreads();
-  const Cut before = s_cut[0], c = s_cut[1];
-  if (c.b >= a.t.n_seqs || c.step == 0 || (same_unit(before, c) && before.step > 0)) return;
-  int last = i;  // the part of CTA `last` ends the unit
-  while (last + 1 < workers) {
-    const Cut d = line.cut(last + 1, workers);
-    if (!same_unit(d, c)) break;
-    ++last;
-  }
-  const int row = blockIdx.y * 32 + (tid & 31), s = row >> 7, r = row & 127, r_tok = r / G;
+  Cut c;
+  int last;
+  if (!parts_from(a.cuts, gridDim.x + 1, a.t.n_seqs, i, c, last)) return;
+  const int row = threadIdx.x, x = blockIdx.y, s = row >> 7, r = row & 127, r_tok = r / G;
   const int token = (2 * c.u + s) * tok + r_tok;
   if (r_tok >= tok || token >= c.n) return;
   // the first part lies in its CTA's second place, the others begin inside the unit
   auto part = [&](int k) { return a.states + (long long)(2 * k + (k == i - 1 ? 1 : 0)) * Lay::STATE; };
-  float M = -INFINITY;
-  for (int k = i - 1; k <= last; ++k) {
-    const float* st = part(k);
-    if (st[256 * (HD + 1) + row] != 0.f) M = fmaxf(M, st[256 * HD + row]);
-  }
-  float L = 0.f;
-  float4 o[HD / 32];
-#pragma unroll
-  for (int x = 0; x < HD / 32; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float M = -INFINITY, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
   for (int k = i - 1; k <= last; ++k) {
     const float* st = part(k);
     const float l = st[256 * (HD + 1) + row], m = st[256 * HD + row];
-    if (l == 0.f) continue;
-    const float f = m == M ? 1.f : exp2f(m - M);
-    L = fmaf(f, l, L);
-#pragma unroll
-    for (int x = 0; x < HD / 32; ++x) {
-      const float4 v = reinterpret_cast<const float4*>(st)[(warp + 8 * x) * 256 + row];
-      o[x].x = fmaf(f, v.x, o[x].x), o[x].y = fmaf(f, v.y, o[x].y), o[x].z = fmaf(f, v.z, o[x].z), o[x].w = fmaf(f, v.w, o[x].w);
-    }
+    const float4 v = reinterpret_cast<const float4*>(st)[x * 256 + row];
+    if (l == 0.f) continue;  // (it saw nothing)
+    const float top = fmaxf(M, m), f0 = M == top ? 1.f : exp2f(M - top), f1 = m == top ? 1.f : exp2f(m - top);
+    M = top;
+    L = f0 * L + f1 * l;
+    o.x = f0 * o.x + f1 * v.x, o.y = f0 * o.y + f1 * v.y, o.z = f0 * o.z + f1 * v.z, o.w = f0 * o.w + f1 * v.w;
   }
   const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
   const long long at = (long long)(c.row0 + token) * a.Hq + c.kvh * G + (r - r_tok * G);
-#pragma unroll
-  for (int x = 0; x < HD / 32; ++x)
-    reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(a.out) + at * HD)[warp + 8 * x] =
-        make_uint2(pack_bf16(o[x].x * il, o[x].y * il), pack_bf16(o[x].z * il, o[x].w * il));
-  if (warp == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+  reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(a.out) + at * HD)[x] = make_uint2(pack_bf16(o.x * il, o.y * il), pack_bf16(o.z * il, o.w * il));
+  if (x == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -735,7 +807,10 @@ JF_DEV bool back_begin(Run<Kind>& w, const PackedParams& a, uint8_t* sm, int* s_
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_launch_dependents();
   pdl_wait();
-  if (!w.line.build(reinterpret_cast<int*>(sm), s_bad, a.err)) return false;
+  if (!w.line.build(reinterpret_cast<int*>(sm), s_bad, a.err)) {
+    if (tid == 0) tell_cut(a.cuts, {}, false);
+    return false;
+  }
   const int workers = w.line.workers(gridDim.x);
   if (warp < 2 && (int)blockIdx.x < workers) {
     const Cut c = w.line.cut(blockIdx.x + warp, workers);
@@ -749,8 +824,10 @@ JF_DEV bool back_begin(Run<Kind>& w, const PackedParams& a, uint8_t* sm, int* s_
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  w.at = s_cut[0], w.end = s_cut[1];
-  go = (int)blockIdx.x < workers && w.line.total > 0 && w.there();
+  w.at = s_cut[0];
+  go = (int)blockIdx.x < workers && w.line.total > 0;
+  if (tid == 0) tell_cut(a.cuts, w.at, go);
+  go = go && w.there();
   return true;
 }
 
@@ -781,7 +858,7 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dq_tc(const PackedPara
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.Hq / a.Hkv, tok = 128 / G;
   if (tid == 0) back_init(b);
-  Run<ByQueries> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, {}};
+  Run<ByQueries> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
   bool go, ok = true;
   if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 256, tQ = tmem + 384;
@@ -1018,7 +1095,7 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dkv_tc(const PackedPar
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.Hq / a.Hkv, tok = 128 / G;
   if (tid == 0) back_init(b);
-  Run<ByKeys> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, {}};
+  Run<ByKeys> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
   bool go, ok = true;
   if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
@@ -1243,61 +1320,42 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dkv_tc(const PackedPar
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// Adds up the parts of a unit that several CTAs share, in their order: CTA (cut i + 1, 32 of 128 rows). Kind ByQueries: dq and
-// delta; ByKeys: dv and dk.
+// Adds up the parts of a unit that several CTAs share, in their order: CTA (run i + 1, two pieces of 4 columns of the 128 rows). Kind
+// ByQueries: dq and delta; ByKeys: dv and dk.
 template <int HD, typename Kind>
-__global__ void __launch_bounds__(256) k_packed_back_join(const PackedParams a, int most) {
+__global__ void __launch_bounds__(256) k_packed_back_join(const PackedParams a) {
   constexpr bool KEYS = Kind::KEYS;
-  constexpr int STATE = KEYS ? BackLayout<HD>::DKV_STATE : BackLayout<HD>::DQ_STATE, WIDTH = KEYS ? 2 * HD : HD;
-  extern __shared__ int s_pre[];
-  __shared__ int s_bad;
-  __shared__ Cut s_cut[2];
-  const int tid = threadIdx.x, warp = tid >> 5, G = a.Hq / a.Hkv, tok = 128 / G;
+  constexpr int STATE = KEYS ? BackLayout<HD>::DKV_STATE : BackLayout<HD>::DQ_STATE;
+  const int G = a.Hq / a.Hkv, tok = 128 / G, i = blockIdx.x + 1;
   pdl_launch_dependents();
   pdl_wait();
-  Line<Kind> line = {{tok}, a.t, a.Hkv, 0, nullptr};
-  if (!line.build(s_pre, &s_bad, a.err)) return;
-  const int workers = line.workers(most), i = blockIdx.x + 1;
-  if (i >= workers || line.total == 0) return;
-  if (warp < 2) {
-    const Cut c = line.cut(i - 1 + warp, workers);
-    if ((tid & 31) == 0) s_cut[warp] = c;
-  }
-  __syncthreads();
-  const Cut before = s_cut[0], c = s_cut[1];
-  if (c.b >= a.t.n_seqs || c.step == 0 || (same_unit(before, c) && before.step > 0)) return;
-  int last = i;  // the part of CTA `last` ends the unit
-  while (last + 1 < workers) {
-    const Cut d = line.cut(last + 1, workers);
-    if (!same_unit(d, c)) break;
-    ++last;
-  }
-  const int r = blockIdx.y * 32 + (tid & 31), r_tok = r / G;
+  Cut c;
+  int last;
+  if (!parts_from(a.cuts, gridDim.x + 1, a.t.n_seqs, i, c, last)) return;
+  const int r = threadIdx.x & 127, x = 2 * blockIdx.y + (threadIdx.x >> 7), r_tok = r / G;
   const int index = KEYS ? c.u * PT_KEYS + r : c.u * tok + r_tok;
   if (index >= c.n || (!KEYS && r_tok >= tok)) return;
   const long long row = c.row0 + index;
   auto part = [&](int k) { return a.states + (long long)(2 * k + (k == i - 1 ? 1 : 0)) * STATE; };
-#pragma unroll 1
-  for (int x = warp; x < WIDTH / 4; x += 8) {
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = i - 1; k <= last; ++k) {
-      const float4 v = reinterpret_cast<const float4*>(part(k))[x * 128 + r];
-      o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
-    }
-    bf16* dst;
-    float f = a.scale;
-    if (!KEYS) {
-      dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (c.kvh * G + r - r_tok * G) * HD + 4 * x;
-    } else if (x < HD / 4) {
-      dst = reinterpret_cast<bf16*>(a.dv) + row * a.ld_dv + c.kvh * HD + 4 * x;
-      f = 1.f;
-    } else {
-      dst = reinterpret_cast<bf16*>(a.dk) + row * a.ld_dk + c.kvh * HD + 4 * x - HD;
-    }
-    dst[0] = __float2bfloat16_rn(o.x * f), dst[1] = __float2bfloat16_rn(o.y * f);
-    dst[2] = __float2bfloat16_rn(o.z * f), dst[3] = __float2bfloat16_rn(o.w * f);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+  for (int k = i - 1; k <= last; ++k) {
+    const float4 v = reinterpret_cast<const float4*>(part(k))[x * 128 + r];
+    o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
   }
-  if (!KEYS && warp == 0) {
+  bf16* dst;
+  float f = a.scale;
+  if (!KEYS) {
+    dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (c.kvh * G + r - r_tok * G) * HD + 4 * x;
+  } else if (x < HD / 4) {
+    dst = reinterpret_cast<bf16*>(a.dv) + row * a.ld_dv + c.kvh * HD + 4 * x;
+    f = 1.f;
+  } else {
+    dst = reinterpret_cast<bf16*>(a.dk) + row * a.ld_dk + c.kvh * HD + 4 * x - HD;
+  }
+  dst[0] = __float2bfloat16_rn(o.x * f), dst[1] = __float2bfloat16_rn(o.y * f);
+  dst[2] = __float2bfloat16_rn(o.z * f), dst[3] = __float2bfloat16_rn(o.w * f);
+  if (!KEYS && x == 0) {
     float eps = 0.f;
     for (int k = i - 1; k <= last; ++k) eps += part(k)[128 * HD + r];
     a.delta[row * a.Hq + c.kvh * G + r - r_tok * G] = part(i - 1)[128 * (HD + 1) + r] + eps;
@@ -1339,8 +1397,8 @@ bool tc_map(CUtensorMap* m, const void* p, long long ld, int heads, int hd, int 
   return encode_tmap_bf16_3d(m, p, dims, strides, box);
 }
 
-// Whether units can be cut: a cut has more than PT_SNAP steps on either side. tile: rows of a step.
-bool tc_cuts(const jf_packed& t, int tile) { return t.max_rows > (2 * PT_SNAP + 1) * tile; }
+// Whether units can be cut, tile: rows of a step.
+bool tc_cuts(const jf_packed& t, int tile) { return t.max_rows > PT_WHOLE * tile; }
 
 template <int HD>
 jf_status tc_forward(const PackedParams& a, int sms, cudaStream_t st) {
@@ -1350,7 +1408,7 @@ jf_status tc_forward(const PackedParams& a, int sms, cudaStream_t st) {
       !tc_map(&maps.v, a.v, a.ld_v, a.Hkv, HD, a.t.n_rows, 1, 128))
     return JF_ECUDA;
   cudaError_t e = packed_launch(k_packed_attn_tc<HD>, dim3(sms), dim3(PA_THREADS), FwdLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_attn_join<HD>, dim3(sms - 1, 8), dim3(256), (a.t.n_seqs + 1) * 4, st, a, sms);
+  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_attn_join<HD>, dim3(sms - 1, HD / 4), dim3(256), 0, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 
@@ -1361,12 +1419,10 @@ jf_status tc_backward(const PackedParams& a, int sms, cudaStream_t st) {
   if (!tc_map(&maps.q, a.q, a.ld_q, a.Hq, HD, a.t.n_rows, G, tok) || !tc_map(&maps.d_out, a.d_out, a.ld_do, a.Hq, HD, a.t.n_rows, G, tok) ||
       !tc_map(&maps.k, a.k, a.ld_k, a.Hkv, HD, a.t.n_rows, 1, 128) || !tc_map(&maps.v, a.v, a.ld_v, a.Hkv, HD, a.t.n_rows, 1, 128))
     return JF_ECUDA;
-  const dim3 join(sms - 1, 4);
-  const size_t pre = (a.t.n_seqs + 1) * 4;
   cudaError_t e = packed_launch(k_packed_dq_tc<HD>, dim3(sms), dim3(PB_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByQueries>, join, dim3(256), pre, st, a, sms);
+  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByQueries>, dim3(sms - 1, HD / 8), dim3(256), 0, st, a);
   if (e == cudaSuccess) e = packed_launch(k_packed_dkv_tc<HD>, dim3(sms), dim3(PB_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t, tok)) e = packed_launch(k_packed_back_join<HD, ByKeys>, join, dim3(256), pre, st, a, sms);
+  if (e == cudaSuccess && tc_cuts(a.t, tok)) e = packed_launch(k_packed_back_join<HD, ByKeys>, dim3(sms - 1, HD / 4), dim3(256), 0, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 
@@ -1374,18 +1430,24 @@ jf_status tc_backward(const PackedParams& a, int sms, cudaStream_t st) {
 
 bool packed_tc_rows(const void* p, long long ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
+// The workspace of cuts and parts.
+static void tc_parts(PackedParams& a, void* at, int sms) {
+  a.cuts = reinterpret_cast<int*>(at);
+  a.states = reinterpret_cast<float*>(reinterpret_cast<char*>(at) + (size_t)sms * 32);
+}
+
 // Backward: delta (read by the copies' form and by the other one), then the parts.
 static size_t delta_bytes(const jf_packed& t, int Hq) { return ((size_t)t.n_rows * Hq * 4 + 15) / 16 * 16; }
 
 jf_status packed_tc_workspace(const jf_packed& t, int Hq, int Hkv, int hd, bool backward, size_t* out_bytes) {
   const PackedDevice* d = tc_device();
   if (!d) return JF_ECUDA;
-  const size_t parts = (size_t)2 * d->sms * 4;
+  const size_t parts = (size_t)2 * d->sms * 4, cuts = (size_t)d->sms * 32;
   if (!backward) {
-    *out_bytes = tc_cuts(t, PT_KEYS) ? parts * (hd == 128 ? FwdLayout<128>::STATE : FwdLayout<64>::STATE) : 0;
+    *out_bytes = tc_cuts(t, PT_KEYS) ? cuts + parts * (hd == 128 ? FwdLayout<128>::STATE : FwdLayout<64>::STATE) : 0;
   } else {
     *out_bytes = delta_bytes(t, Hq);
-    if (tc_cuts(t, 128 / (Hq / Hkv))) *out_bytes += parts * (hd == 128 ? BackLayout<128>::DKV_STATE : BackLayout<64>::DKV_STATE);
+    if (tc_cuts(t, 128 / (Hq / Hkv))) *out_bytes += cuts + parts * (hd == 128 ? BackLayout<128>::DKV_STATE : BackLayout<64>::DKV_STATE);
   }
   return JF_OK;
 }
@@ -1394,7 +1456,7 @@ jf_status packed_tc_forward(const PackedParams& p, int hd, void* workspace, cuda
   const PackedDevice* d = tc_device();
   if (!d) return JF_ECUDA;
   PackedParams a = p;
-  a.states = reinterpret_cast<float*>(workspace);
+  if (tc_cuts(a.t, PT_KEYS)) tc_parts(a, workspace, d->sms);
   return hd == 128 ? tc_forward<128>(a, d->sms, st) : tc_forward<64>(a, d->sms, st);
 }
 
@@ -1403,7 +1465,7 @@ jf_status packed_tc_backward(const PackedParams& p, int hd, void* workspace, cud
   if (!d) return JF_ECUDA;
   PackedParams a = p;
   a.delta = reinterpret_cast<float*>(workspace);
-  a.states = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + delta_bytes(a.t, a.Hq));
+  if (tc_cuts(a.t, 128 / (a.Hq / a.Hkv))) tc_parts(a, reinterpret_cast<char*>(workspace) + delta_bytes(a.t, a.Hq), d->sms);
   return hd == 128 ? tc_backward<128>(a, d->sms, st) : tc_backward<64>(a, d->sms, st);
 }
 
