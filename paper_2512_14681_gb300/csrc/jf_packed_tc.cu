@@ -266,6 +266,14 @@ JF_DEV uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+JF_DEV float tmem_ld1(uint32_t taddr) {
+  float v;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=f"(v) : "r"(taddr) : "memory");
+  return v;
+}
+JF_DEV void tmem_st1(uint32_t taddr, float v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(v) : "memory");
+}
 // Products and commits by the one lane whose `on` is set, in code that the warp goes through together (descriptors stay in
 // uniform registers).
 JF_DEV void mma_ss_on(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t on) {
@@ -304,15 +312,18 @@ struct Tile {
       mma_ss_on(d, da + (uint64_t)((kk >> 2) * (HALF >> 4) + (kk & 3) * 2), db + (uint64_t)((kk >> 2) * (HALF >> 4) + (kk & 3) * 2),
                 idesc_bf16_f32(128, 128), kk > 0 ? 1u : 0u, on);
   }
-  // D[128][HD] (+)= w b over b's rows; w: bf16 in tensor memory, 64 columns, rows 64 .. at w + gap
-  template <int FIRST = 0, int LAST = 8>
-  static JF_DEV void rows(uint32_t d, uint32_t w, uint32_t b, bool fresh, uint32_t on, uint32_t gap = 32) {
+  // D[128][HD] (+)= w b over b's rows. w: bf16 in tensor memory in the place of the scores that it came from, those of each PER x 16
+  // of b's rows at the beginning of their columns. FIRST, COUNT: which runs of 16 rows.
+  template <int PER, int FIRST = 0, int COUNT = PER>
+  static JF_DEV void rows(uint32_t d, uint32_t w, uint32_t b, bool fresh, uint32_t on) {
     uint64_t db = sdesc_mn_sw128(b, HALF, 1024u);
     asm volatile("" : "+l"(db));
 #pragma unroll
-    for (int kk = FIRST; kk < LAST; ++kk)  // (16 of b's rows each)
-      mma_ts_on(d, w + (kk >> 2) * gap + (kk & 3) * 8, db + (uint64_t)(kk * (2048 >> 4)), idesc_bf16_f32(128, HD) | (1u << 16),
-                kk > 0 || !fresh ? 1u : 0u, on);
+    for (int i = 0; i < 8 / PER * COUNT; ++i) {
+      const int kk = i / COUNT * PER + FIRST + i % COUNT;  // runs FIRST .. FIRST + COUNT - 1 of each PER
+      mma_ts_on(d, w + kk / PER * (PER * 16) + kk % PER * 8, db + (uint64_t)(kk * (2048 >> 4)), idesc_bf16_f32(128, HD) | (1u << 16),
+                FIRST > 0 || i > 0 || !fresh ? 1u : 0u, on);
+    }
   }
   // Rows from `first` on are cleared, by a warp: what lies behind a text may be anything, and 0 times it nothing.
   static JF_DEV void clear_from(uint32_t tile, int first, int lane) {
@@ -336,10 +347,10 @@ JF_DEV bool warp_wait(uint64_t& bar, int uses) {
   return __all_sync(0xffffffffu, ok) != 0;
 }
 
-template <int HD>
+template <int COLUMNS>
 JF_DEV void scale_o(uint32_t t_o, float x) {
 #pragma unroll 1
-  for (int h = 0; h < HD / 16; ++h) {
+  for (int h = 0; h < COLUMNS / 16; ++h) {
     float o[16];
     uint32_t u[16];
     tmem_ld16(t_o + 16 * h, o);
@@ -352,14 +363,15 @@ JF_DEV void scale_o(uint32_t t_o, float x) {
 // ---------------------------------------------------------------------------------------------
 // Forward. A unit is two tiles of query rows (streams 0 and 1) over the key tiles that they see: while one stream's softmax
 // runs, the tensor core works for the other. Tensor memory: S and O of each stream, P in bf16 in the place of the S it came
-// from. Warps 0-3, 4-7: stream 0, 1, a thread per row; warp 8: copies; warp 9: products (10 and
-// 11 give their registers away).
+// from. Warps 0-3, 4-7: stream 0, 1, a thread per row; warp 8: copies; 9, 10: the streams' products; 11: values behind a text's end.
+// (Two threads a row, in 16 warps, took 1.4 times as long: they have to agree on the row's maximum at every step, and 96 registers
+// are too few.)
 // ---------------------------------------------------------------------------------------------
 constexpr int PA_THREADS = 384;
 constexpr float PA_LAG = 8.f;  // a row's reference maximum follows its scores when they exceed it by more
 template <int HD>
 struct FwdLayout {
-  static constexpr int Q = Tile<HD>::BYTES, KV = Tile<HD>::BYTES, RING = HD == 128 ? 4 : 8;  // (one CTA an SM: it has all tensor memory)
+  static constexpr int Q = Tile<HD>::BYTES, KV = Tile<HD>::BYTES, RING = HD == 128 ? 4 : 8;
   static constexpr int OFF_KV = 2 * Q, TOTAL = OFF_KV + RING * KV + 1024;
   static constexpr int STATE = 256 * (HD + 2);  // floats of a part: O by 4 columns [HD / 4][256 rows][4], m, l
 };
@@ -505,11 +517,11 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
           ok = warp_wait(b_kv[vp], v_tile / RING) && warp_wait(b_p[s][0], products);
           if (!ok) break;
           tc_fence_after();
-          T::template rows<0, 4>(t_o, t_s, sKV + vp * Lay::KV, j == 0, on);
+          T::template rows<8, 0, 4>(t_o, t_s, sKV + vp * Lay::KV, j == 0, on);
           ok = warp_wait(b_p[s][1], products);
           if (!ok) break;
           tc_fence_after();
-          T::template rows<4, 8>(t_o, t_s, sKV + vp * Lay::KV, false, on);
+          T::template rows<8, 4, 4>(t_o, t_s, sKV + vp * Lay::KV, false, on);
           commit_on(smem_u32(&b_o[s]), on);
           commit_on(smem_u32(&b_kvfree[vp]), on);
           ++products;
@@ -707,10 +719,10 @@ __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) 
 // delta, the dq kernel adds up its ds (a row lies in one thread, or two) and corrects delta by it for dk; where a row's keys
 // are one step it takes delta = sum_j p_ij dp_ij to begin with.
 //
-// Tiles come through a ring of four places in pairs, X (needed first and last: K, or Q) and Y (V, or d_out). Y's place is free
-// first and takes the X of two steps on, X's place its Y.
-// Warps 0-3 and 4-7: columns 0-63 and 64-127 of all 128 rows; warp 8: copies; 9: products; 10: row statistics (dk and dv).
+// A step's 128 x 128 scores are 16 warps' work, 32 columns of a row a thread; warp 16: copies; 17: products; 18: row statistics
+// (dk and dv).
 // ---------------------------------------------------------------------------------------------
+constexpr int PT_THREADS = 640;  // 96 registers a thread (and so one CTA an SM, which has all of its tensor memory)
 struct BackMaps {
   CUtensorMap q, k, v, d_out;
 };
@@ -719,39 +731,13 @@ JF_DEV int place_y(int j) { return 2 * (j & 1) + (~j >> 1 & 1); }
 // Completion number of a place's barriers that step j's tile waits for: the places of a pair are used by turns.
 JF_DEV int use_of(int j) { return j >> 1; }
 
-constexpr int PB_THREADS = 384;
 template <int HD>
 struct BackLayout {
   static constexpr int T = Tile<HD>::BYTES, OFF_RING = 2 * T;
-  static constexpr int TOTAL = (HD == 128 ? OFF_RING + 4 * T : 7 * 16384) + 1024;  // (one CTA an SM: it has all tensor memory)
+  static constexpr int TOTAL = OFF_RING + 4 * T + 1024;
   static constexpr int DQ_STATE = 128 * (HD + 2);  // floats of a part: dq by 4 columns [HD / 4][128 rows][4], sum of ds, delta
   static constexpr int DKV_STATE = 2 * 128 * HD;   // dv, dk, each by 4 columns
 };
-
-struct BackBarriers {
-  uint64_t fix, fixfree, tile[4], free[4];  // the unit's own two tiles there, read; the ring's places there, read
-  uint64_t s[2], dp, p, ds, o1, o2, all, stat[2], statfree[2];
-};
-JF_DEV void back_init(BackBarriers& b) {
-  mbar_init(smem_u32(&b.fix), 1);
-  mbar_init(smem_u32(&b.fixfree), 1);
-  for (int i = 0; i < 4; ++i) {
-    mbar_init(smem_u32(&b.tile[i]), 1);
-    mbar_init(smem_u32(&b.free[i]), 1);
-  }
-  for (int i = 0; i < 2; ++i) {
-    mbar_init(smem_u32(&b.s[i]), 1);
-    mbar_init(smem_u32(&b.stat[i]), 1);
-    mbar_init(smem_u32(&b.statfree[i]), 8);
-  }
-  mbar_init(smem_u32(&b.dp), 1);
-  mbar_init(smem_u32(&b.p), 8);
-  mbar_init(smem_u32(&b.ds), 8);
-  mbar_init(smem_u32(&b.o1), 1);
-  mbar_init(smem_u32(&b.o2), 1);
-  mbar_init(smem_u32(&b.all), 1);
-  fence_mbar_init();
-}
 
 // Gradients of rows that belong to no text, by `threads` threads.
 template <int HD>
@@ -761,44 +747,6 @@ JF_DEV void clear_rows(const jf_packed& t, void* p, long long ld, int heads, int
     const long long row = r < head ? r : tail + r - head;
     for (int i = tid; i < width; i += threads) reinterpret_cast<bf16*>(p)[row * ld + i] = __float2bfloat16_rn(0.f);
   }
-}
-
-// The copies of a kernel's run, by warp 8: fix = the unit's own tiles, x and y = a step's.
-template <int HD, typename Kind, typename Fix, typename Step>
-JF_DEV void back_copies(Run<Kind>& w, bool go, BackBarriers& b, uint32_t sm, uint32_t fix_bytes, uint32_t tile_bytes, int* err, Fix fix, Step step) {
-  using Lay = BackLayout<HD>;
-  int units = 0, g = 0;
-  bool ok = true;
-  while (go) {
-    ok = units == 0 || warp_wait(b.fixfree, units - 1);
-    if (!ok) break;
-    if (elect_one()) {
-      mbar_arrive_expect_tx(smem_u32(&b.fix), fix_bytes);
-      fix(sm, smem_u32(&b.fix));
-    }
-    __syncwarp();
-    ++units;
-    for (int j = w.c0(); j < w.c1() && ok; ++j, ++g)
-      for (int y = 0; y < 2 && ok; ++y) {
-        const int place = y ? place_y(g) : place_x(g);
-        ok = g < 2 || warp_wait(b.free[place], use_of(g) - 1);
-        if (!ok) break;
-        if (elect_one()) {
-          mbar_arrive_expect_tx(smem_u32(&b.tile[place]), tile_bytes);
-          step(sm + Lay::OFF_RING + place * Lay::T, smem_u32(&b.tile[place]), j, y);
-        }
-        __syncwarp();
-      }
-    if (!ok) break;
-    go = w.next();
-  }
-  // every copy has landed before the CTA may leave, also after a wait that gave up
-  if (units) warp_wait(b.fix, units - 1);
-  for (int j = max(0, g - 2); j < g; ++j) {
-    warp_wait(b.tile[place_x(j)], use_of(j));
-    warp_wait(b.tile[place_y(j)], use_of(j));
-  }
-  if (!ok && (threadIdx.x & 31) == 0) jf_set_error(err, JF_DERR_TIMEOUT_MMA);
 }
 
 // What both kernels begin with: the line's cuts, tensor memory. False: nothing to do for the whole grid.
@@ -816,7 +764,7 @@ JF_DEV bool back_begin(Run<Kind>& w, const PackedParams& a, uint8_t* sm, int* s_
     const Cut c = w.line.cut(blockIdx.x + warp, workers);
     if (lane == 0) s_cut[warp] = c;
   }
-  if (warp == 8) {
+  if (warp == 16) {
     tmem_alloc(smem_u32(tmem_slot), 512);
     tmem_relinquish();
   }
@@ -831,7 +779,7 @@ JF_DEV bool back_begin(Run<Kind>& w, const PackedParams& a, uint8_t* sm, int* s_
   return true;
 }
 
-// 16 bf16 products of two runs of memory
+// 8 bf16 products of two runs of memory
 JF_DEV float dot8(const uint4& x, const uint4& y, float s) {
   const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -842,103 +790,174 @@ JF_DEV float dot8(const uint4& x, const uint4& y, float s) {
   return s;
 }
 
-// dq. Tensor memory: two S, dP (ds in bf16 in its place), dQ.
+// delta = d_out . out of every row and head, HD / 8 lanes each (rows of no text as well: not used).
 template <int HD>
-__global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dq_tc(const PackedParams a, const __grid_constant__ BackMaps maps) {
-  using Lay = BackLayout<HD>;
+__global__ void __launch_bounds__(256) k_packed_delta_tc(const PackedParams a) {
+  constexpr int LPR = HD / 8;
+  pdl_launch_dependents();
+  pdl_wait();
+  const uint32_t i = (blockIdx.x * 256 + threadIdx.x) / LPR, piece = threadIdx.x % LPR;  // (n_rows * Hq is at most 2^30)
+  const uint32_t row = i / a.Hq;
+  float d = 0.f;
+  if ((int)row < a.t.n_rows)
+    d = dot8(reinterpret_cast<const uint4*>(a.out)[(long long)i * LPR + piece],
+             reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.d_out) + row * a.ld_do + (long long)(i - row * a.Hq) * HD)[piece], 0.f);
+#pragma unroll
+  for (int sh = LPR / 2; sh; sh >>= 1) d += __shfl_xor_sync(0xffffffffu, d, sh);
+  if (piece == 0 && (int)row < a.t.n_rows) a.delta[i] = d;
+}
+
+template <int HD>
+struct DqLayout {
+  static constexpr int T = Tile<HD>::BYTES, KEYS = 3, VALUES = 2;  // tiles in shared memory beside Q and d_out: a value tile is read sooner
+  static constexpr int TOTAL = (2 + KEYS + VALUES) * T + 1024;
+};
+
+// dq. Tensor memory: S, two dP (ds in bf16 in their places), dQ. S and dP of the next step are multiplied before dQ of this one, so that the
+// warps and the tensor core both have work ahead.
+template <int HD>
+__global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedParams a, const __grid_constant__ BackMaps maps) {
+  using Lay = DqLayout<HD>;
   using T = Tile<HD>;
   extern __shared__ uint8_t sm_raw[];
   uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
-  const uint32_t sm = smem_u32(smp), sQ = sm, sdO = sm + Lay::T, ring = sm + Lay::OFF_RING;
-  __shared__ __align__(8) BackBarriers b;
+  const uint32_t sQ = smem_u32(smp), sdO = sQ + Lay::T, sK = sdO + Lay::T, sV = sK + Lay::KEYS * Lay::T;
+  // Q and d_out there, read; keys, values there, read; S ready, read; dP ready; ds ready; dQ of a step done, of a unit; everything
+  // done. (Two of those that a fast warp may meet again before a slow one has.)
+  __shared__ __align__(8) uint64_t b_fix, b_fixfree, b_k[Lay::KEYS], b_kfree[Lay::KEYS], b_v[Lay::VALUES], b_vfree[Lay::VALUES], b_s, b_sread, b_dp[2],
+      b_ds[2], b_o, b_unit, b_all;
   __shared__ uint32_t tmem_slot;
   __shared__ int s_bad;
   __shared__ Cut s_cut[2];
-  __shared__ float s_x[2][2][128];  // (of the two halves of a row, by turns)
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.Hq / a.Hkv, tok = 128 / G;
-  if (tid == 0) back_init(b);
+  if (tid == 0) {
+    uint64_t* const ones[] = {&b_fix, &b_fixfree, &b_s, &b_dp[0], &b_dp[1], &b_o, &b_unit, &b_all};
+    for (uint64_t* b : ones) mbar_init(smem_u32(b), 1);
+    for (int i = 0; i < Lay::KEYS; ++i) mbar_init(smem_u32(&b_k[i]), 1), mbar_init(smem_u32(&b_kfree[i]), 1);
+    for (int i = 0; i < Lay::VALUES; ++i) mbar_init(smem_u32(&b_v[i]), 1), mbar_init(smem_u32(&b_vfree[i]), 1);
+    mbar_init(smem_u32(&b_sread), 16);
+    mbar_init(smem_u32(&b_ds[0]), 16);
+    mbar_init(smem_u32(&b_ds[1]), 16);
+    fence_mbar_init();
+  }
   Run<ByQueries> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
   bool go, ok = true;
   if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
-  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 256, tQ = tmem + 384;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 128, tG = tmem + 384;
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 8) {
-      back_copies<HD>(
-          w, go, b, sm, (uint32_t)(2 * tok * G * HD * 2), (uint32_t)T::BYTES, a.err,
-          [&](uint32_t dst, uint32_t bar) {
-            T::load(dst, &maps.q, bar, w.at.kvh * G, w.at.row0 + w.at.u * tok);
-            T::load(dst + Lay::T, &maps.d_out, bar, w.at.kvh * G, w.at.row0 + w.at.u * tok);
-          },
-          [&](uint32_t dst, uint32_t bar, int j, int y) { T::load(dst, y ? &maps.v : &maps.k, bar, w.at.kvh, w.at.row0 + j * PT_KEYS); });
-    } else if (warp == 9) {
+  if (warp >= 16) {
+    if (warp == 16) {
+      int units = 0, nk = 0, nv = 0;  // asked for
+      const uint32_t fix_bytes = (uint32_t)(2 * tok * G * HD * 2);
+      while (go) {
+        ok = units == 0 || warp_wait(b_fixfree, units - 1);
+        if (!ok) break;
+        if (elect_one()) {
+          mbar_arrive_expect_tx(smem_u32(&b_fix), fix_bytes);
+          T::load(sQ, &maps.q, smem_u32(&b_fix), w.at.kvh * G, w.at.row0 + w.at.u * tok);
+          T::load(sdO, &maps.d_out, smem_u32(&b_fix), w.at.kvh * G, w.at.row0 + w.at.u * tok);
+        }
+        __syncwarp();
+        ++units;
+        for (int j = w.c0(); j < w.c1() && ok; ++j) {
+          int place = nk % Lay::KEYS;
+          ok = nk < Lay::KEYS || warp_wait(b_kfree[place], nk / Lay::KEYS - 1);
+          if (!ok) break;
+          if (elect_one()) {
+            mbar_arrive_expect_tx(smem_u32(&b_k[place]), T::BYTES);
+            T::load(sK + place * Lay::T, &maps.k, smem_u32(&b_k[place]), w.at.kvh, w.at.row0 + j * PT_KEYS);
+          }
+          __syncwarp();
+          ++nk;
+          place = nv % Lay::VALUES;
+          ok = nv < Lay::VALUES || warp_wait(b_vfree[place], nv / Lay::VALUES - 1);
+          if (!ok) break;
+          if (elect_one()) {
+            mbar_arrive_expect_tx(smem_u32(&b_v[place]), T::BYTES);
+            T::load(sV + place * Lay::T, &maps.v, smem_u32(&b_v[place]), w.at.kvh, w.at.row0 + j * PT_KEYS);
+          }
+          __syncwarp();
+          ++nv;
+        }
+        if (!ok) break;
+        go = w.next();
+      }
+      // every copy has landed before the CTA may leave, also after a wait that gave up
+      if (units) warp_wait(b_fix, units - 1);
+      for (int i = max(0, nk - Lay::KEYS); i < nk; ++i) warp_wait(b_k[i % Lay::KEYS], i / Lay::KEYS);
+      for (int i = max(0, nv - Lay::VALUES); i < nv; ++i) warp_wait(b_v[i % Lay::VALUES], i / Lay::VALUES);
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+    } else if (warp == 17) {
       const uint32_t on = elect_one();
       int g = 0, units = 0;  // steps, units so far
-      auto x_there = [&](int j) { return warp_wait(b.tile[place_x(j)], use_of(j)); };
-      auto issue_s = [&](int j) {  // (its S was read two steps ago)
-        tc_fence_after();
-        T::dots(tS + (j & 1) * 128, sQ, ring + place_x(j) * Lay::T, on);
-        commit_on(smem_u32(&b.s[j & 1]), on);
-      };
-      auto issue_dp = [&](int j) {  // (ds of the step before has been read)
-        ok = warp_wait(b.tile[place_y(j)], use_of(j));
-        if (j > 0) ok = ok && warp_wait(b.o1, j - 1);
+      auto place_of = [&](int i, int n) { return __shfl_sync(0xffffffffu, i % n, 0); };
+      auto issue_s = [&](int j) {  // (the S before has been read)
+        const int place = place_of(j, Lay::KEYS);
+        ok = warp_wait(b_k[place], j / Lay::KEYS);
         if (!ok) return;
         tc_fence_after();
-        T::dots(tP, sdO, ring + place_y(j) * Lay::T, on);
-        commit_on(smem_u32(&b.dp), on);
-        commit_on(smem_u32(&b.free[place_y(j)]), on);
+        T::dots(tS, sQ, sK + place * Lay::T, on);
+        commit_on(smem_u32(&b_s), on);
+      };
+      // Its place is ds's of two steps before, which has been read when the last dQ that was issued is done. (It is that one that is waited
+      // for: a wait for an earlier one would not see that it has been followed by another.)
+      auto issue_dp = [&](int j, int last_dq) {
+        const int place = place_of(j, Lay::VALUES);
+        ok = warp_wait(b_v[place], j / Lay::VALUES) && (last_dq < 0 || warp_wait(b_o, last_dq));
+        if (!ok) return;
+        tc_fence_after();
+        T::dots(tP + (j & 1) * 128, sdO, sV + place * Lay::T, on);
+        commit_on(smem_u32(&b_dp[j & 1]), on);
+        commit_on(smem_u32(&b_vfree[place]), on);
       };
       while (go) {
         const int n = w.c1() - w.c0();
-        ok = warp_wait(b.fix, units++) && x_there(g);
-        if (!ok) break;
-        issue_s(g);
-        issue_dp(g);
-        if (n == 1) commit_on(smem_u32(&b.fixfree), on);
-        if (n > 1 && ok) {
-          ok = x_there(g + 1);
-          if (ok) issue_s(g + 1);
-        }
+        ok = warp_wait(b_fix, units++);
+        if (ok) issue_s(g);
+        if (ok) issue_dp(g, g - 1);
+        if (n == 1) commit_on(smem_u32(&b_fixfree), on);
         for (int j = 0; j < n && ok; ++j, ++g) {
-          const int held = w.at.n - (w.c0() + j) * PT_KEYS;
-          if (held < PT_KEYS) T::clear_from(ring + place_x(g) * Lay::T, held, lane);
-          ok = warp_wait(b.ds, g);
+          const int place = place_of(g, Lay::KEYS), held = w.at.n - (w.c0() + j) * PT_KEYS;
+          ok = warp_wait(b_sread, g);
+          if (j + 1 < n) {
+            if (ok) issue_s(g + 1);
+            if (ok) issue_dp(g + 1, g - 1);
+            if (j + 2 == n) commit_on(smem_u32(&b_fixfree), on);
+          }
+          if (ok && held < PT_KEYS) T::clear_from(sK + place * Lay::T, held, lane);  // (S has read it)
+          ok = ok && warp_wait(b_ds[g & 1], g >> 1);
           if (!ok) break;
           tc_fence_after();
-          T::rows(tQ, tP, ring + place_x(g) * Lay::T, j == 0, on, 64);
-          commit_on(smem_u32(&b.o1), on);
-          commit_on(smem_u32(&b.free[place_x(g)]), on);
-          if (j + 1 < n) issue_dp(g + 1);
-          if (j + 2 == n) commit_on(smem_u32(&b.fixfree), on);
-          if (j + 2 < n && ok) {
-            ok = x_there(g + 2);
-            if (ok) issue_s(g + 2);
-          }
+          T::template rows<2>(tG, tP + (g & 1) * 128, sK + place * Lay::T, j == 0, on);
+          commit_on(smem_u32(&b_o), on);
+          commit_on(smem_u32(&b_kfree[place]), on);
+          if (j + 1 == n) commit_on(smem_u32(&b_unit), on);
         }
         go = ok && w.next();
       }
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
-      commit_on(smem_u32(&b.all), on);
+      commit_on(smem_u32(&b_all), on);
       __syncwarp();
-      warp_wait(b.all, 0);  // every product is complete before the CTA may leave
+      warp_wait(b_all, 0);  // every product is complete before the CTA may leave
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    clear_rows<HD>(a.t, a.dq, a.ld_dq, a.Hq, tid, 256);
-    const int half = warp >> 2, r = (warp & 3) * 32 + lane, r_tok = r / G, r_head = r - r_tok * G;
+    clear_rows<HD>(a.t, a.dq, a.ld_dq, a.Hq, tid, 512);
+    const int quarter = warp >> 2, r = (warp & 3) * 32 + lane, r_tok = r / G, r_head = r - r_tok * G;
     const uint32_t t_row = (uint32_t)((warp & 3) * 32) << 16;
     const float c = a.scale * kLog2e;
-    int g = 0, turn = 0;
-    // the sum of both halves of a row; all 256 threads meet, and learn whether one's wait gave up: it keeps to the meetings
-    // until then, so that nobody waits at one alone
-    auto join = [&](float x) {
-      s_x[turn][half][r] = x;
-      ok = sync_and<1, 256>(ok);
-      const float sum = s_x[turn][0][r] + s_x[turn][1][r];
-      turn ^= 1;
+    int g = 0, units = 0;
+    // The sum of the four threads of a row, through tensor memory that each has read its part of. All 512 threads meet, and learn
+    // whether one's wait gave up: it keeps to the meetings until then, so that nobody waits at one alone.
+    auto join = [&](uint32_t columns, int apart, float x) {
+      tmem_st1(columns + t_row + quarter * apart, x);
+      tmem_wait_st();
+      tc_fence_before();
+      ok = sync_and<1, 512>(ok);
+      tc_fence_after();
+      float sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum += tmem_ld1(columns + t_row + k * apart);
       return sum;
     };
     while (go) {
@@ -946,119 +965,101 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dq_tc(const PackedPara
       const bool live = r_tok < tok && i < w.at.n, one = w.at.n_steps == 1;
       const long long row = w.at.row0 + i, at = row * a.Hq + w.at.kvh * G + r_head;
       const float nl = live ? -a.lse[at] * kLog2e : -INFINITY;
-      float delta = 0.f, eps = 0.f;
-      if (!one) {
-        if (live) {
-          const uint4* x = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.out) + at * HD + half * (HD / 2));
-          const uint4* y = reinterpret_cast<const uint4*>(reinterpret_cast<const bf16*>(a.d_out) + row * a.ld_do + (w.at.kvh * G + r_head) * HD + half * (HD / 2));
-#pragma unroll
-          for (int d = 0; d < HD / 16; ++d) delta = dot8(x[d], y[d], delta);
-        }
-        delta = join(delta);
-        if (!ok) break;
-      }
+      float delta = live && !one ? a.delta[at] : 0.f, eps = 0.f;
       bool left = false;  // (after a meeting that ends the run, there is no other)
       for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
-        const int see = i - j * PT_KEYS - 64 * half;  // columns 0 .. see of the 64
+        const int see = i - j * PT_KEYS - 32 * quarter;  // columns 0 .. see of the 32
         const bool cut = (j + 1) * PT_KEYS > w.at.u * tok;
-        ok = warp_wait(b.s[g & 1], g >> 1);
+        ok = warp_wait(b_s, g);
         if (!ok) break;
         tc_fence_after();
-        float p[64];
+        float p[32];
+        tmem_ld32(tS + t_row + 32 * quarter, p);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&b_sread));
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[32];
-          tmem_ld32(tS + t_row + (g & 1) * 128 + 64 * half + 32 * h, v);
-#pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            const float2 e = fma2(make_float2(v[2 * x], v[2 * x + 1]), make_float2(c, c), make_float2(nl, nl));
-            p[32 * h + 2 * x] = packed_ex2(e.x), p[32 * h + 2 * x + 1] = packed_ex2(e.y);
-          }
+        for (int x = 0; x < 32; x += 2) {
+          const float2 e = fma2(make_float2(p[x], p[x + 1]), make_float2(c, c), make_float2(nl, nl));
+          p[x] = packed_ex2(e.x), p[x + 1] = packed_ex2(e.y);
         }
         if (cut) {
 #pragma unroll
-          for (int x = 0; x < 64; ++x) p[x] = x <= see ? p[x] : 0.f;
+          for (int x = 0; x < 32; ++x) p[x] = x <= see ? p[x] : 0.f;
         }
-        ok = warp_wait(b.dp, g);
+        ok = warp_wait(b_dp[g & 1], g >> 1);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t t_p = tP + t_row + 64 * half;
+        const uint32_t t_p = tP + t_row + (g & 1) * 128 + 32 * quarter;
+        float v[32];
+        uint32_t u[16];
+        tmem_ld32(t_p, v);
+        if (cut) {  // (what lies behind the text may be anything)
+#pragma unroll
+          for (int x = 0; x < 32; ++x) v[x] = x <= see ? v[x] : 0.f;
+        }
         if (one) {
           float sum = 0.f;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float v[32];
-            tmem_ld32(t_p + 32 * h, v);
-#pragma unroll
-            for (int x = 0; x < 32; ++x) sum += 32 * h + x <= see ? p[32 * h + x] * v[x] : 0.f;
-          }
-          delta = join(sum);
+          for (int x = 0; x < 32; ++x) sum = fmaf(p[x], v[x], sum);
+          delta = join(tS, 32, sum);
           left = !ok;
           if (left) break;
         }
         float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[32];
-          uint32_t u[16];
-          tmem_ld32(t_p + 32 * h, v);
-#pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            float2 d = add2(make_float2(v[2 * x], v[2 * x + 1]), make_float2(-delta, -delta));
-            d.x *= p[32 * h + 2 * x], d.y *= p[32 * h + 2 * x + 1];
-            if (cut) {  // (what lies behind the text may be anything)
-              d.x = 32 * h + 2 * x <= see ? d.x : 0.f;
-              d.y = 32 * h + 2 * x + 1 <= see ? d.y : 0.f;
-            }
-            sum = add2(sum, d);
-            u[x] = pack_bf16(d.x, d.y);
-          }
-          tmem_st16(t_p + 16 * h, u);
+        for (int x = 0; x < 16; ++x) {
+          float2 d = add2(make_float2(v[2 * x], v[2 * x + 1]), make_float2(-delta, -delta));
+          d.x *= p[2 * x], d.y *= p[2 * x + 1];
+          sum = add2(sum, d);
+          u[x] = pack_bf16(d.x, d.y);
         }
+        tmem_st16(t_p, u);
         eps += sum.x + sum.y;
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&b.ds));
+        if (lane == 0) mbar_arrive(smem_u32(&b_ds[g & 1]));
       }
       if (left) break;
-      ok = ok && warp_wait(b.o1, g - 1);
-      if (!one) eps = join(eps);
-      else ok = sync_and<1, 256>(ok);
-      if (!ok) break;
+      ok = ok && warp_wait(b_unit, units++);
       tc_fence_after();
       const bool whole = w.whole();
-      float* st = a.states + (long long)w.slot(blockIdx.x) * Lay::DQ_STATE;
-#pragma unroll 1
-      for (int d = half * (HD / 2); d < (half + 1) * (HD / 2); d += 32) {
-        float o[32];
-        tmem_ld32(tQ + t_row + d, o);
+      float* st = a.states + (long long)w.slot(blockIdx.x) * BackLayout<HD>::DQ_STATE;
+      constexpr int DW = HD / 4;  // dims of a thread
+      const int d0 = quarter * DW;
+      if (ok) {
+        float o[DW];
+        if constexpr (DW == 32) tmem_ld32(tG + t_row + d0, o);
+        else tmem_ld16(tG + t_row + d0, o);
         if (whole) {
           if (live) {
-            bf16* dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (w.at.kvh * G + r_head) * HD + d;
+            bf16* dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (w.at.kvh * G + r_head) * HD + d0;
             if (((uintptr_t)dst & 15) == 0) {
 #pragma unroll
-              for (int h = 0; h < 4; ++h)
+              for (int h = 0; h < DW / 8; ++h)
                 reinterpret_cast<uint4*>(dst)[h] =
                     make_uint4(pack_bf16(o[8 * h] * a.scale, o[8 * h + 1] * a.scale), pack_bf16(o[8 * h + 2] * a.scale, o[8 * h + 3] * a.scale),
                                pack_bf16(o[8 * h + 4] * a.scale, o[8 * h + 5] * a.scale), pack_bf16(o[8 * h + 6] * a.scale, o[8 * h + 7] * a.scale));
             } else {
 #pragma unroll
-              for (int h = 0; h < 32; ++h) dst[h] = __float2bfloat16_rn(o[h] * a.scale);
+              for (int h = 0; h < DW; ++h) dst[h] = __float2bfloat16_rn(o[h] * a.scale);
             }
           }
         } else {
 #pragma unroll
-          for (int h = 0; h < 8; ++h)
-            reinterpret_cast<float4*>(st)[(d / 4 + h) * 128 + r] = make_float4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]);
+          for (int h = 0; h < DW / 4; ++h)
+            reinterpret_cast<float4*>(st)[(d0 / 4 + h) * 128 + r] = make_float4(o[4 * h], o[4 * h + 1], o[4 * h + 2], o[4 * h + 3]);
         }
       }
-      if (half == 0) {
+      eps = join(tG, DW, eps);  // (dQ has been read; all threads have, after this)
+      if (!ok) break;
+      if (quarter == 0) {
         if (!whole) st[128 * HD + r] = eps, st[128 * (HD + 1) + r] = delta;
         else if (live) a.delta[at] = one ? delta : delta + eps;
       }
       tc_fence_before();
-      ok = sync_and<1, 256>(ok);  // both halves have read dQ (and what they exchanged)
+      ok = sync_and<1, 512>(ok);  // ... and what they exchanged
       if (!ok) break;
       go = w.next();
     }
@@ -1067,7 +1068,7 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dq_tc(const PackedPara
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == 16) tmem_dealloc(tmem, 512);
 }
 
 struct ByKeys {  // tiles of keys over the tiles of `tok` tokens that see them
@@ -1080,102 +1081,140 @@ struct ByKeys {  // tiles of keys over the tiles of `tok` tokens that see them
 };
 
 // dk and dv. Rows of the products are keys, columns query rows. Tensor memory: S (P in bf16 in its place), dP (ds), dV, dK.
+//
+// Q and d_out come through a ring of four places in pairs. d_out's place is free first and takes the Q of two steps on, Q's place its
+// d_out.
+JF_DEV int place_q(int j) { return 2 * (j & 1) + (j >> 1 & 1); }
+JF_DEV int place_do(int j) { return 2 * (j & 1) + (~j >> 1 & 1); }
+
 template <int HD>
-__global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dkv_tc(const PackedParams a, const __grid_constant__ BackMaps maps) {
+__global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedParams a, const __grid_constant__ BackMaps maps) {
   using Lay = BackLayout<HD>;
   using T = Tile<HD>;
   extern __shared__ uint8_t sm_raw[];
   uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
-  const uint32_t sm = smem_u32(smp), sK = sm, sV = sm + Lay::T, ring = sm + Lay::OFF_RING;
-  __shared__ __align__(8) BackBarriers b;
+  const uint32_t sK = smem_u32(smp), sV = sK + Lay::T, ring = sK + Lay::OFF_RING;
+  // keys and values there, read; the ring's places there, read; S, dP, P, ds ready; dV, dK of a step done; everything done;
+  // statistics there, read
+  __shared__ __align__(8) uint64_t b_fix, b_fixfree, b_tile[4], b_free[4], b_s, b_dp, b_p, b_ds, b_o1, b_o2, b_all, b_stat[2], b_statfree[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int s_bad;
   __shared__ Cut s_cut[2];
   __shared__ __align__(16) float s_nl[2][128], s_nd[2][128];  // of a step's columns: -lse log2 e, -delta
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.Hq / a.Hkv, tok = 128 / G;
-  if (tid == 0) back_init(b);
+  if (tid == 0) {
+    uint64_t* const ones[] = {&b_fix, &b_fixfree, &b_s, &b_dp, &b_o1, &b_o2, &b_all, &b_stat[0], &b_stat[1]};
+    for (uint64_t* b : ones) mbar_init(smem_u32(b), 1);
+    for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&b_tile[i]), 1), mbar_init(smem_u32(&b_free[i]), 1);
+    uint64_t* const all[] = {&b_p, &b_ds, &b_statfree[0], &b_statfree[1]};
+    for (uint64_t* b : all) mbar_init(smem_u32(b), 16);
+    fence_mbar_init();
+  }
   Run<ByKeys> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
   bool go, ok = true;
   if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 8) {
-      back_copies<HD>(
-          w, go, b, sm, (uint32_t)(2 * T::BYTES), (uint32_t)(tok * G * HD * 2), a.err,
-          [&](uint32_t dst, uint32_t bar) {
-            T::load(dst, &maps.k, bar, w.at.kvh, w.at.row0 + w.at.u * PT_KEYS);
-            T::load(dst + Lay::T, &maps.v, bar, w.at.kvh, w.at.row0 + w.at.u * PT_KEYS);
-          },
-          [&](uint32_t dst, uint32_t bar, int j, int y) {
-            T::load(dst, y ? &maps.d_out : &maps.q, bar, w.at.kvh * G, w.at.row0 + (w.line.kind.first(w.at.u) + j) * tok);
-          });
-    } else if (warp == 9) {
+  if (warp >= 16) {
+    if (warp == 16) {
+      int units = 0, g = 0, asked = 0;  // of the ring's places
+      const uint32_t tile_bytes = (uint32_t)(tok * G * HD * 2);
+      while (go) {
+        ok = units == 0 || warp_wait(b_fixfree, units - 1);
+        if (!ok) break;
+        if (elect_one()) {
+          mbar_arrive_expect_tx(smem_u32(&b_fix), (uint32_t)(2 * T::BYTES));
+          T::load(sK, &maps.k, smem_u32(&b_fix), w.at.kvh, w.at.row0 + w.at.u * PT_KEYS);
+          T::load(sV, &maps.v, smem_u32(&b_fix), w.at.kvh, w.at.row0 + w.at.u * PT_KEYS);
+        }
+        __syncwarp();
+        ++units;
+        for (int j = w.c0(); j < w.c1() && ok; ++j, ++g)
+          for (int y = 0; y < 2 && ok; ++y) {
+            const int place = y ? place_do(g) : place_q(g);
+            ok = g < 2 || warp_wait(b_free[place], (g >> 1) - 1);
+            if (!ok) break;
+            if (elect_one()) {
+              mbar_arrive_expect_tx(smem_u32(&b_tile[place]), tile_bytes);
+              T::load(ring + place * Lay::T, y ? &maps.d_out : &maps.q, smem_u32(&b_tile[place]), w.at.kvh * G,
+                      w.at.row0 + (w.line.kind.first(w.at.u) + j) * tok);
+            }
+            __syncwarp();
+            ++asked;
+          }
+        if (!ok) break;
+        go = w.next();
+      }
+      // every copy has landed before the CTA may leave, also after a wait that gave up
+      if (units) warp_wait(b_fix, units - 1);
+      for (int i = max(0, asked - 4); i < asked; ++i) warp_wait(b_tile[i & 1 ? place_do(i >> 1) : place_q(i >> 1)], i >> 2);
+      if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
+    } else if (warp == 17) {
       const uint32_t on = elect_one();
       for (int i = 0; i < 4; ++i)
         if (tok * G < 128) T::clear_from(ring + i * Lay::T, tok * G, lane);  // rows that no copy writes
       int g = 0, units = 0;
       // a step's tile, its rows behind the text cleared
       auto there = [&](int place, int j, int q) {
-        if (!warp_wait(b.tile[place], use_of(j))) return false;
+        if (!warp_wait(b_tile[place], j >> 1)) return false;
         const int held = (w.at.n - q * tok) * G;
         if (held < tok * G) T::clear_from(ring + place * Lay::T, held, lane);
         return true;
       };
+      auto of = [&](int place) { return __shfl_sync(0xffffffffu, place, 0); };
       auto issue_s = [&](int j) {
         tc_fence_after();
-        T::dots(tS, sK, ring + place_x(j) * Lay::T, on);
-        commit_on(smem_u32(&b.s[0]), on);
+        T::dots(tS, sK, ring + of(place_q(j)) * Lay::T, on);
+        commit_on(smem_u32(&b_s), on);
       };
       auto issue_dp = [&](int j) {
         tc_fence_after();
-        T::dots(tP, sV, ring + place_y(j) * Lay::T, on);
-        commit_on(smem_u32(&b.dp), on);
+        T::dots(tP, sV, ring + of(place_do(j)) * Lay::T, on);
+        commit_on(smem_u32(&b_dp), on);
       };
       while (go) {
         const int n = w.c1() - w.c0(), q0 = w.line.kind.first(w.at.u) + w.c0();
         // (the last unit's P and ds have been read: its last dK was waited for below)
-        ok = warp_wait(b.fix, units++) && there(place_x(g), g, q0);
+        ok = warp_wait(b_fix, units++) && there(place_q(g), g, q0);
         if (!ok) break;
         issue_s(g);
-        ok = there(place_y(g), g, q0);
+        ok = there(place_do(g), g, q0);
         if (!ok) break;
         issue_dp(g);
-        if (n == 1) commit_on(smem_u32(&b.fixfree), on);
+        if (n == 1) commit_on(smem_u32(&b_fixfree), on);
         for (int j = 0; j < n && ok; ++j, ++g) {
-          ok = warp_wait(b.p, g);
+          ok = warp_wait(b_p, g);
           if (!ok) break;
           tc_fence_after();
-          T::rows(tV, tS, ring + place_y(g) * Lay::T, j == 0, on, 64);
-          commit_on(smem_u32(&b.o1), on);
-          commit_on(smem_u32(&b.free[place_y(g)]), on);
-          if (j + 1 < n) {
-            ok = there(place_x(g + 1), g + 1, q0 + j + 1) && warp_wait(b.o1, g);
+          T::template rows<2>(tV, tS, ring + of(place_do(g)) * Lay::T, j == 0, on);
+          commit_on(smem_u32(&b_o1), on);
+          commit_on(smem_u32(&b_free[place_do(g)]), on);
+          if (j + 1 < n) {  // S: its place is P's, which has been read then
+            ok = there(place_q(g + 1), g + 1, q0 + j + 1) && warp_wait(b_o1, g);
             if (!ok) break;
             issue_s(g + 1);
           }
-          ok = warp_wait(b.ds, g);
+          ok = warp_wait(b_ds, g);
           if (!ok) break;
           tc_fence_after();
-          T::rows(tK, tP, ring + place_x(g) * Lay::T, j == 0, on, 64);
-          commit_on(smem_u32(&b.o2), on);
-          commit_on(smem_u32(&b.free[place_x(g)]), on);
-          ok = j + 1 == n || there(place_y(g + 1), g + 1, q0 + j + 1);
-          ok = ok && warp_wait(b.o2, g);
+          T::template rows<2>(tK, tP, ring + of(place_q(g)) * Lay::T, j == 0, on);
+          commit_on(smem_u32(&b_o2), on);
+          commit_on(smem_u32(&b_free[place_q(g)]), on);
+          ok = j + 1 == n || there(place_do(g + 1), g + 1, q0 + j + 1);
+          ok = ok && warp_wait(b_o2, g);
           if (ok && j + 1 < n) {
             issue_dp(g + 1);
-            if (j + 2 == n) commit_on(smem_u32(&b.fixfree), on);
+            if (j + 2 == n) commit_on(smem_u32(&b_fixfree), on);
           }
         }
         go = ok && w.next();
       }
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
-      commit_on(smem_u32(&b.all), on);
+      commit_on(smem_u32(&b_all), on);
       __syncwarp();
-      warp_wait(b.all, 0);  // every product is complete before the CTA may leave
-    } else if (warp == 10) {
+      warp_wait(b_all, 0);  // every product is complete before the CTA may leave
+    } else if (warp == 18) {
       int g = 0;
       while (go) {
         for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
@@ -1189,106 +1228,90 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dkv_tc(const PackedPar
             nl[x] = live ? -a.lse[at] * kLog2e : -INFINITY;  // (p = 0)
             nd[x] = live ? -a.delta[at] : 0.f;
           }
-          ok = g < 2 || warp_wait(b.statfree[g & 1], (g >> 1) - 1);
+          ok = g < 2 || warp_wait(b_statfree[g & 1], (g >> 1) - 1);
           if (!ok) break;
 #pragma unroll
           for (int x = 0; x < 4; ++x) s_nl[g & 1][lane + 32 * x] = nl[x], s_nd[g & 1][lane + 32 * x] = nd[x];
           __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&b.stat[g & 1]));
+          if (lane == 0) mbar_arrive(smem_u32(&b_stat[g & 1]));
         }
         go = ok && w.next();
       }
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    clear_rows<HD>(a.t, a.dk, a.ld_dk, a.Hkv, tid, 256);
-    clear_rows<HD>(a.t, a.dv, a.ld_dv, a.Hkv, tid, 256);
-    const int half = warp >> 2, r = (warp & 3) * 32 + lane;
-    const uint32_t t_row = (uint32_t)((warp & 3) * 32) << 16;
+    clear_rows<HD>(a.t, a.dk, a.ld_dk, a.Hkv, tid, 512);
+    clear_rows<HD>(a.t, a.dv, a.ld_dv, a.Hkv, tid, 512);
+    const int quarter = warp >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t t_row = (uint32_t)((warp & 3) * 32) << 16, t_s = tS + t_row + 32 * quarter, t_p = tP + t_row + 32 * quarter;
     const float c = a.scale * kLog2e;
     int g = 0;
     while (go) {
       const int k = w.at.u * PT_KEYS + r, q0 = w.line.kind.first(w.at.u);
       for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
-        const int first = (k - (q0 + j) * tok) * G - 64 * half;  // columns from here on see the key
+        const int first = (k - (q0 + j) * tok) * G - 32 * quarter;  // columns from here on see the key
         const bool cut = (q0 + j) * tok < w.at.u * PT_KEYS + PT_KEYS - 1;
-        ok = warp_wait(b.stat[g & 1], g >> 1) && warp_wait(b.s[0], g);
+        ok = warp_wait(b_stat[g & 1], g >> 1) && warp_wait(b_s, g);
         if (!ok) break;
         tc_fence_after();
-        float p[64];
-        const uint32_t t_s = tS + t_row + 64 * half, t_p = tP + t_row + 64 * half;
+        float p[32];
+        uint32_t u[16];
+        tmem_ld32(t_s, p);
+        const float4* nl = reinterpret_cast<const float4*>(s_nl[g & 1] + 32 * quarter);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[32];
-          tmem_ld32(t_s + 32 * h, v);
-          const float4* nl = reinterpret_cast<const float4*>(s_nl[g & 1] + 64 * half + 32 * h);
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const float4 l = nl[x];
-            const float2 e = fma2(make_float2(v[4 * x], v[4 * x + 1]), make_float2(c, c), make_float2(l.x, l.y));
-            const float2 f = fma2(make_float2(v[4 * x + 2], v[4 * x + 3]), make_float2(c, c), make_float2(l.z, l.w));
-            float* o = p + 32 * h + 4 * x;
-            o[0] = packed_ex2(e.x), o[1] = packed_ex2(e.y), o[2] = packed_ex2(f.x), o[3] = packed_ex2(f.y);
-          }
+        for (int x = 0; x < 8; ++x) {
+          const float4 l = nl[x];
+          const float2 e = fma2(make_float2(p[4 * x], p[4 * x + 1]), make_float2(c, c), make_float2(l.x, l.y));
+          const float2 f = fma2(make_float2(p[4 * x + 2], p[4 * x + 3]), make_float2(c, c), make_float2(l.z, l.w));
+          p[4 * x] = packed_ex2(e.x), p[4 * x + 1] = packed_ex2(e.y), p[4 * x + 2] = packed_ex2(f.x), p[4 * x + 3] = packed_ex2(f.y);
         }
         if (cut) {
 #pragma unroll
-          for (int x = 0; x < 64; ++x) p[x] = x >= first ? p[x] : 0.f;
+          for (int x = 0; x < 32; ++x) p[x] = x >= first ? p[x] : 0.f;
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t u[16];
-#pragma unroll
-          for (int x = 0; x < 16; ++x) u[x] = pack_bf16(p[32 * h + 2 * x], p[32 * h + 2 * x + 1]);
-          tmem_st16(t_s + 16 * h, u);
-        }
+        for (int x = 0; x < 16; ++x) u[x] = pack_bf16(p[2 * x], p[2 * x + 1]);
+        tmem_st16(t_s, u);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&b.p));
-        ok = warp_wait(b.dp, g);
+        if (lane == 0) mbar_arrive(smem_u32(&b_p));
+        ok = warp_wait(b_dp, g);
         if (!ok) break;
         tc_fence_after();
+        float v[32];
+        tmem_ld32(t_p, v);
+        const float4* nd = reinterpret_cast<const float4*>(s_nd[g & 1] + 32 * quarter);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[32];
-          uint32_t u[16];
-          tmem_ld32(t_p + 32 * h, v);
-          const float4* nd = reinterpret_cast<const float4*>(s_nd[g & 1] + 64 * half + 32 * h);
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const float4 d = nd[x];
-            const float2 e = add2(make_float2(v[4 * x], v[4 * x + 1]), make_float2(d.x, d.y));
-            const float2 f = add2(make_float2(v[4 * x + 2], v[4 * x + 3]), make_float2(d.z, d.w));
-            const float* o = p + 32 * h + 4 * x;
-            u[2 * x] = pack_bf16(o[0] * e.x, o[1] * e.y);
-            u[2 * x + 1] = pack_bf16(o[2] * f.x, o[3] * f.y);
-          }
-          tmem_st16(t_p + 16 * h, u);
+        for (int x = 0; x < 8; ++x) {
+          const float4 d = nd[x];
+          const float2 e = add2(make_float2(v[4 * x], v[4 * x + 1]), make_float2(d.x, d.y));
+          const float2 f = add2(make_float2(v[4 * x + 2], v[4 * x + 3]), make_float2(d.z, d.w));
+          u[2 * x] = pack_bf16(p[4 * x] * e.x, p[4 * x + 1] * e.y);
+          u[2 * x + 1] = pack_bf16(p[4 * x + 2] * f.x, p[4 * x + 3] * f.y);
         }
+        tmem_st16(t_p, u);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(smem_u32(&b.ds));
-          mbar_arrive(smem_u32(&b.statfree[g & 1]));
+          mbar_arrive(smem_u32(&b_ds));
+          mbar_arrive(smem_u32(&b_statfree[g & 1]));
         }
       }
-      ok = ok && warp_wait(b.o1, g - 1) && warp_wait(b.o2, g - 1);
-      ok = sync_and<1, 256>(ok);
-      if (!ok) break;
+      ok = ok && warp_wait(b_o1, g - 1) && warp_wait(b_o2, g - 1);
       tc_fence_after();
-      // the first four warps take dV, the others dK
-      const bool whole = w.whole(), live = k < w.at.n;
-      const float f = half ? a.scale : 1.f;
-      float* st = a.states + (long long)w.slot(blockIdx.x) * Lay::DKV_STATE + half * (128 * HD);
-      bf16* dst = half ? reinterpret_cast<bf16*>(a.dk) + (w.at.row0 + k) * a.ld_dk : reinterpret_cast<bf16*>(a.dv) + (w.at.row0 + k) * a.ld_dv;
+      // the first eight warps take dV, the others dK, half of the dims each
+      const bool whole = w.whole(), live = k < w.at.n, is_k = quarter >= 2;
+      const float f = is_k ? a.scale : 1.f;
+      const int d0 = (quarter & 1) * (HD / 2);
+      float* st = a.states + (long long)w.slot(blockIdx.x) * Lay::DKV_STATE + (is_k ? 128 * HD : 0);
+      bf16* dst = is_k ? reinterpret_cast<bf16*>(a.dk) + (w.at.row0 + k) * a.ld_dk : reinterpret_cast<bf16*>(a.dv) + (w.at.row0 + k) * a.ld_dv;
       dst += w.at.kvh * HD;
 #pragma unroll 1
-      for (int d = 0; d < HD; d += 32) {
+      for (int d = d0; d < d0 + HD / 2 && ok; d += 32) {
         float o[32];
-        tmem_ld32((half ? tK : tV) + t_row + d, o);
+        tmem_ld32((is_k ? tK : tV) + t_row + d, o);
         if (whole) {
           if (live) {
             if (((uintptr_t)dst & 15) == 0) {
@@ -1308,7 +1331,9 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dkv_tc(const PackedPar
         }
       }
       tc_fence_before();
-      ok = sync_and<1, 256>(ok);  // dV and dK have been read before any warp lets the next unit's products begin
+      // dV and dK have been read before any warp lets the next unit's products begin. (All 512 threads meet here, and learn whether
+      // one's wait gave up.)
+      ok = sync_and<1, 512>(ok);
       if (!ok) break;
       go = w.next();
     }
@@ -1317,7 +1342,7 @@ __global__ void __launch_bounds__(PB_THREADS, 1) k_packed_dkv_tc(const PackedPar
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == 16) tmem_dealloc(tmem, 512);
 }
 
 // Adds up the parts of a unit that several CTAs share, in their order: CTA (run i + 1, two pieces of 4 columns of the 128 rows). Kind
@@ -1373,7 +1398,7 @@ PackedDevice g_tc[PerDeviceOnce::kMaxDevices];
 template <int HD>
 cudaError_t tc_prepare() {
   cudaError_t e = cudaFuncSetAttribute(k_packed_attn_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdLayout<HD>::TOTAL);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BackLayout<HD>::TOTAL);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, DqLayout<HD>::TOTAL);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dkv_tc<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, BackLayout<HD>::TOTAL);
   return e;
 }
@@ -1419,9 +1444,12 @@ jf_status tc_backward(const PackedParams& a, int sms, cudaStream_t st) {
   if (!tc_map(&maps.q, a.q, a.ld_q, a.Hq, HD, a.t.n_rows, G, tok) || !tc_map(&maps.d_out, a.d_out, a.ld_do, a.Hq, HD, a.t.n_rows, G, tok) ||
       !tc_map(&maps.k, a.k, a.ld_k, a.Hkv, HD, a.t.n_rows, 1, 128) || !tc_map(&maps.v, a.v, a.ld_v, a.Hkv, HD, a.t.n_rows, 1, 128))
     return JF_ECUDA;
-  cudaError_t e = packed_launch(k_packed_dq_tc<HD>, dim3(sms), dim3(PB_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
+  cudaError_t e = cudaSuccess;
+  if (a.t.max_rows > PT_KEYS)  // (delta is read where a row has several steps)
+    e = packed_launch(k_packed_delta_tc<HD>, dim3((unsigned)(((long long)a.t.n_rows * a.Hq * (HD / 8) + 255) / 256)), dim3(256), 0, st, a);
+  if (e == cudaSuccess) e = packed_launch(k_packed_dq_tc<HD>, dim3(sms), dim3(PT_THREADS), DqLayout<HD>::TOTAL, st, a, maps);
   if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByQueries>, dim3(sms - 1, HD / 8), dim3(256), 0, st, a);
-  if (e == cudaSuccess) e = packed_launch(k_packed_dkv_tc<HD>, dim3(sms), dim3(PB_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
+  if (e == cudaSuccess) e = packed_launch(k_packed_dkv_tc<HD>, dim3(sms), dim3(PT_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
   if (e == cudaSuccess && tc_cuts(a.t, tok)) e = packed_launch(k_packed_back_join<HD, ByKeys>, dim3(sms - 1, HD / 4), dim3(256), 0, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
