@@ -500,6 +500,9 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
       const uint32_t on = elect_one(), t_s = tmem + s * 128, t_o = tmem + 256 + s * 128;
       int tiles = 0, units = 0, products = 0;  // tiles before the unit, units, P V so far
       auto place_of = [&](int tile) { return __shfl_sync(0xffffffffu, tile % RING, 0); };
+      // The streams run best half a step apart, one's softmax beside the other's products, and stay so: the second begins when the
+      // first's first P is there. (Or after 4 us: nothing depends on it.)
+      if (s == 1 && go && stream_steps(w, 0) > 2) mbar_wait_bounded(smem_u32(&b_p[0][1]), 0u, 4000ull);
       while (go) {
         const int n = stream_steps(w, s), all = max(n, stream_steps(w, 1 - s));
         if (n > 0) ok = warp_wait(b_q[s], units++);
@@ -677,38 +680,49 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of the units that several CTAs share: CTA (run i + 1, 256 pieces of 4 columns of the unit's 256 rows).
+// Joins the parts of the units that several CTAs share: CTA (run i + 1, an eighth of the columns of the unit's 256 rows).
 template <int HD>
 __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) {
   using Lay = FwdLayout<HD>;
+  constexpr int X = HD / 32;  // pieces of 4 columns of a thread
   const int G = a.Hq / a.Hkv, tok = 128 / G, i = blockIdx.x + 1;
   pdl_launch_dependents();
   pdl_wait();
   Cut c;
   int last;
   if (!parts_from(a.cuts, gridDim.x + 1, a.t.n_seqs, i, c, last)) return;
-  const int row = threadIdx.x, x = blockIdx.y, s = row >> 7, r = row & 127, r_tok = r / G;
+  const int row = threadIdx.x, x0 = blockIdx.y * X, s = row >> 7, r = row & 127, r_tok = r / G;
   const int token = (2 * c.u + s) * tok + r_tok;
   if (r_tok >= tok || token >= c.n) return;
   // the first part lies in its CTA's second place, the others begin inside the unit
   auto part = [&](int k) { return a.states + (long long)(2 * k + (k == i - 1 ? 1 : 0)) * Lay::STATE; };
   float M = -INFINITY, L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 o[X];
+#pragma unroll
+  for (int x = 0; x < X; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
   for (int k = i - 1; k <= last; ++k) {
     const float* st = part(k);
     const float l = st[256 * (HD + 1) + row], m = st[256 * HD + row];
-    const float4 v = reinterpret_cast<const float4*>(st)[x * 256 + row];
+    float4 v[X];
+#pragma unroll
+    for (int x = 0; x < X; ++x) v[x] = reinterpret_cast<const float4*>(st)[(x0 + x) * 256 + row];
     if (l == 0.f) continue;  // (it saw nothing)
     const float top = fmaxf(M, m), f0 = M == top ? 1.f : exp2f(M - top), f1 = m == top ? 1.f : exp2f(m - top);
     M = top;
     L = f0 * L + f1 * l;
-    o.x = f0 * o.x + f1 * v.x, o.y = f0 * o.y + f1 * v.y, o.z = f0 * o.z + f1 * v.z, o.w = f0 * o.w + f1 * v.w;
+#pragma unroll
+    for (int x = 0; x < X; ++x)
+      o[x].x = f0 * o[x].x + f1 * v[x].x, o[x].y = f0 * o[x].y + f1 * v[x].y, o[x].z = f0 * o[x].z + f1 * v[x].z, o[x].w = f0 * o[x].w + f1 * v[x].w;
   }
   const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
   const long long at = (long long)(c.row0 + token) * a.Hq + c.kvh * G + (r - r_tok * G);
-  reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(a.out) + at * HD)[x] = make_uint2(pack_bf16(o.x * il, o.y * il), pack_bf16(o.z * il, o.w * il));
-  if (x == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+#pragma unroll
+  for (int x = 0; x < X; x += 2)
+    reinterpret_cast<uint4*>(reinterpret_cast<bf16*>(a.out) + at * HD + 4 * x0)[x / 2] =
+        make_uint4(pack_bf16(o[x].x * il, o[x].y * il), pack_bf16(o[x].z * il, o[x].w * il), pack_bf16(o[x + 1].x * il, o[x + 1].y * il),
+                   pack_bf16(o[x + 1].z * il, o[x + 1].w * il));
+  if (x0 == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -719,8 +733,9 @@ __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) 
 // delta, the dq kernel adds up its ds (a row lies in one thread, or two) and corrects delta by it for dk; where a row's keys
 // are one step it takes delta = sum_j p_ij dp_ij to begin with.
 //
-// A step's 128 x 128 scores are 16 warps' work, 32 columns of a row a thread; warp 16: copies; 17: products; 18: row statistics
-// (dk and dv).
+// A step's 128 x 128 scores are 16 warps' work, 32 columns of a row a thread; warp 16: copies; 17: products that give scores; 18:
+// products with what the scores have become (a warp of its own: a wait of one, which stands behind its products in the tensor
+// core's queue, does not hold up the other); 19: row statistics (dk and dv).
 // ---------------------------------------------------------------------------------------------
 constexpr int PT_THREADS = 640;  // 96 registers a thread (and so one CTA an SM, which has all of its tensor memory)
 struct BackMaps {
@@ -823,16 +838,16 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
   uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sQ = smem_u32(smp), sdO = sQ + Lay::T, sK = sdO + Lay::T, sV = sK + Lay::KEYS * Lay::T;
   // Q and d_out there, read; keys, values there, read; S ready, read; dP ready; ds ready; dQ of a step done, of a unit; everything
-  // done. (Two of those that a fast warp may meet again before a slow one has.)
+  // done. (Two, for even and odd steps, of those that may complete again before a slow warp has seen them.)
   __shared__ __align__(8) uint64_t b_fix, b_fixfree, b_k[Lay::KEYS], b_kfree[Lay::KEYS], b_v[Lay::VALUES], b_vfree[Lay::VALUES], b_s, b_sread, b_dp[2],
-      b_ds[2], b_o, b_unit, b_all;
+      b_ds[2], b_o[2], b_unit, b_all[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int s_bad;
   __shared__ Cut s_cut[2];
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.Hq / a.Hkv, tok = 128 / G;
   if (tid == 0) {
-    uint64_t* const ones[] = {&b_fix, &b_fixfree, &b_s, &b_dp[0], &b_dp[1], &b_o, &b_unit, &b_all};
+    uint64_t* const ones[] = {&b_fix, &b_fixfree, &b_s, &b_dp[0], &b_dp[1], &b_o[0], &b_o[1], &b_unit, &b_all[0], &b_all[1]};
     for (uint64_t* b : ones) mbar_init(smem_u32(b), 1);
     for (int i = 0; i < Lay::KEYS; ++i) mbar_init(smem_u32(&b_k[i]), 1), mbar_init(smem_u32(&b_kfree[i]), 1);
     for (int i = 0; i < Lay::VALUES; ++i) mbar_init(smem_u32(&b_v[i]), 1), mbar_init(smem_u32(&b_vfree[i]), 1);
@@ -888,58 +903,49 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
       for (int i = max(0, nk - Lay::KEYS); i < nk; ++i) warp_wait(b_k[i % Lay::KEYS], i / Lay::KEYS);
       for (int i = max(0, nv - Lay::VALUES); i < nv; ++i) warp_wait(b_v[i % Lay::VALUES], i / Lay::VALUES);
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
-    } else if (warp == 17) {
+    } else if (warp < 19) {
       const uint32_t on = elect_one();
       int g = 0, units = 0;  // steps, units so far
       auto place_of = [&](int i, int n) { return __shfl_sync(0xffffffffu, i % n, 0); };
-      auto issue_s = [&](int j) {  // (the S before has been read)
-        const int place = place_of(j, Lay::KEYS);
-        ok = warp_wait(b_k[place], j / Lay::KEYS);
-        if (!ok) return;
-        tc_fence_after();
-        T::dots(tS, sQ, sK + place * Lay::T, on);
-        commit_on(smem_u32(&b_s), on);
-      };
-      // Its place is ds's of two steps before, which has been read when the last dQ that was issued is done. (It is that one that is waited
-      // for: a wait for an earlier one would not see that it has been followed by another.)
-      auto issue_dp = [&](int j, int last_dq) {
-        const int place = place_of(j, Lay::VALUES);
-        ok = warp_wait(b_v[place], j / Lay::VALUES) && (last_dq < 0 || warp_wait(b_o, last_dq));
-        if (!ok) return;
-        tc_fence_after();
-        T::dots(tP + (j & 1) * 128, sdO, sV + place * Lay::T, on);
-        commit_on(smem_u32(&b_dp[j & 1]), on);
-        commit_on(smem_u32(&b_vfree[place]), on);
-      };
-      while (go) {
-        const int n = w.c1() - w.c0();
+      while (go && warp == 17) {  // S and dP
         ok = warp_wait(b_fix, units++);
-        if (ok) issue_s(g);
-        if (ok) issue_dp(g, g - 1);
-        if (n == 1) commit_on(smem_u32(&b_fixfree), on);
-        for (int j = 0; j < n && ok; ++j, ++g) {
-          const int place = place_of(g, Lay::KEYS), held = w.at.n - (w.c0() + j) * PT_KEYS;
-          ok = warp_wait(b_sread, g);
-          if (j + 1 < n) {
-            if (ok) issue_s(g + 1);
-            if (ok) issue_dp(g + 1, g - 1);
-            if (j + 2 == n) commit_on(smem_u32(&b_fixfree), on);
-          }
-          if (ok && held < PT_KEYS) T::clear_from(sK + place * Lay::T, held, lane);  // (S has read it)
-          ok = ok && warp_wait(b_ds[g & 1], g >> 1);
+        for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
+          int place = place_of(g, Lay::KEYS);
+          ok = (g == 0 || warp_wait(b_sread, g - 1)) && warp_wait(b_k[place], g / Lay::KEYS);
           if (!ok) break;
           tc_fence_after();
-          T::template rows<2>(tG, tP + (g & 1) * 128, sK + place * Lay::T, j == 0, on);
-          commit_on(smem_u32(&b_o), on);
-          commit_on(smem_u32(&b_kfree[place]), on);
-          if (j + 1 == n) commit_on(smem_u32(&b_unit), on);
+          T::dots(tS, sQ, sK + place * Lay::T, on);
+          commit_on(smem_u32(&b_s), on);
+          // dP: its place is ds's of two steps before, which has been read then
+          place = place_of(g, Lay::VALUES);
+          ok = warp_wait(b_v[place], g / Lay::VALUES) && (g < 2 || warp_wait(b_o[g & 1], (g >> 1) - 1));
+          if (!ok) break;
+          tc_fence_after();
+          T::dots(tP + (g & 1) * 128, sdO, sV + place * Lay::T, on);
+          commit_on(smem_u32(&b_dp[g & 1]), on);
+          commit_on(smem_u32(&b_vfree[place]), on);
         }
+        commit_on(smem_u32(&b_fixfree), on);
+        go = ok && w.next();
+      }
+      while (go && warp == 18) {  // dQ
+        for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
+          const int place = place_of(g, Lay::KEYS), held = w.at.n - j * PT_KEYS;
+          ok = warp_wait(b_ds[g & 1], g >> 1);
+          if (!ok) break;
+          if (held < PT_KEYS) T::clear_from(sK + place * Lay::T, held, lane);  // (S has read it, and so has the copy)
+          tc_fence_after();
+          T::template rows<2>(tG, tP + (g & 1) * 128, sK + place * Lay::T, j == w.c0(), on);
+          commit_on(smem_u32(&b_o[g & 1]), on);
+          commit_on(smem_u32(&b_kfree[place]), on);
+        }
+        commit_on(smem_u32(&b_unit), on);
         go = ok && w.next();
       }
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
-      commit_on(smem_u32(&b_all), on);
+      commit_on(smem_u32(&b_all[warp - 17]), on);
       __syncwarp();
-      warp_wait(b_all, 0);  // every product is complete before the CTA may leave
+      warp_wait(b_all[warp - 17], 0);  // every product is complete before the CTA may leave
     }
   } else {
     clear_rows<HD>(a.t, a.dq, a.ld_dq, a.Hq, tid, 512);
@@ -1002,7 +1008,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
           float sum = 0.f;
 #pragma unroll
           for (int x = 0; x < 32; ++x) sum = fmaf(p[x], v[x], sum);
-          delta = join(tS, 32, sum);
+          delta = join(tP + (g & 1) * 128 + 31, 32, sum);  // (a column that ds leaves alone)
           left = !ok;
           if (left) break;
         }
@@ -1094,9 +1100,9 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
   extern __shared__ uint8_t sm_raw[];
   uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sK = smem_u32(smp), sV = sK + Lay::T, ring = sK + Lay::OFF_RING;
-  // keys and values there, read; the ring's places there, read; S, dP, P, ds ready; dV, dK of a step done; everything done;
+  // keys and values there, read; the ring's places there (b_raw: with rows to be cleared), read; S, dP, P, ds ready; dV, dK of a step done; everything done;
   // statistics there, read
-  __shared__ __align__(8) uint64_t b_fix, b_fixfree, b_tile[4], b_free[4], b_s, b_dp, b_p, b_ds, b_o1, b_o2, b_all, b_stat[2], b_statfree[2];
+  __shared__ __align__(8) uint64_t b_fix, b_fixfree, b_tile[4], b_raw[4], b_free[4], b_s, b_dp, b_p, b_ds, b_o1, b_o2, b_all[2], b_stat[2], b_statfree[2];
   __shared__ uint32_t tmem_slot;
   __shared__ int s_bad;
   __shared__ Cut s_cut[2];
@@ -1104,13 +1110,15 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const int G = a.Hq / a.Hkv, tok = 128 / G;
   if (tid == 0) {
-    uint64_t* const ones[] = {&b_fix, &b_fixfree, &b_s, &b_dp, &b_o1, &b_o2, &b_all, &b_stat[0], &b_stat[1]};
+    uint64_t* const ones[] = {&b_fix, &b_fixfree, &b_s, &b_dp, &b_o1, &b_o2, &b_all[0], &b_all[1], &b_stat[0], &b_stat[1]};
     for (uint64_t* b : ones) mbar_init(smem_u32(b), 1);
-    for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&b_tile[i]), 1), mbar_init(smem_u32(&b_free[i]), 1);
+    for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&b_tile[i]), 1), mbar_init(smem_u32(&b_raw[i]), 1), mbar_init(smem_u32(&b_free[i]), 1);
     uint64_t* const all[] = {&b_p, &b_ds, &b_statfree[0], &b_statfree[1]};
     for (uint64_t* b : all) mbar_init(smem_u32(b), 16);
     fence_mbar_init();
   }
+  if (warp == 19 && tok * G < 128)
+    for (int i = 0; i < 4; ++i) T::clear_from(ring + i * Lay::T, tok * G, lane);  // rows that no copy writes
   Run<ByKeys> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
   bool go, ok = true;
   if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
@@ -1135,10 +1143,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
             const int place = y ? place_do(g) : place_q(g);
             ok = g < 2 || warp_wait(b_free[place], (g >> 1) - 1);
             if (!ok) break;
+            const int first = (w.line.kind.first(w.at.u) + j) * tok;  // the tile's first token
             if (elect_one()) {
-              mbar_arrive_expect_tx(smem_u32(&b_tile[place]), tile_bytes);
-              T::load(ring + place * Lay::T, y ? &maps.d_out : &maps.q, smem_u32(&b_tile[place]), w.at.kvh * G,
-                      w.at.row0 + (w.line.kind.first(w.at.u) + j) * tok);
+              const uint32_t bar = smem_u32(first + tok > w.at.n ? &b_raw[place] : &b_tile[place]);
+              mbar_arrive_expect_tx(bar, tile_bytes);
+              T::load(ring + place * Lay::T, y ? &maps.d_out : &maps.q, bar, w.at.kvh * G, w.at.row0 + first);
             }
             __syncwarp();
             ++asked;
@@ -1146,76 +1155,57 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
         if (!ok) break;
         go = w.next();
       }
-      // every copy has landed before the CTA may leave, also after a wait that gave up
+      // every copy has landed before the CTA may leave, also after a wait that gave up (b_raw's are forwarded)
       if (units) warp_wait(b_fix, units - 1);
       for (int i = max(0, asked - 4); i < asked; ++i) warp_wait(b_tile[i & 1 ? place_do(i >> 1) : place_q(i >> 1)], i >> 2);
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_MMA);
-    } else if (warp == 17) {
+    } else if (warp < 19) {
       const uint32_t on = elect_one();
-      for (int i = 0; i < 4; ++i)
-        if (tok * G < 128) T::clear_from(ring + i * Lay::T, tok * G, lane);  // rows that no copy writes
       int g = 0, units = 0;
-      // a step's tile, its rows behind the text cleared
-      auto there = [&](int place, int j, int q) {
-        if (!warp_wait(b_tile[place], j >> 1)) return false;
-        const int held = (w.at.n - q * tok) * G;
-        if (held < tok * G) T::clear_from(ring + place * Lay::T, held, lane);
-        return true;
-      };
       auto of = [&](int place) { return __shfl_sync(0xffffffffu, place, 0); };
-      auto issue_s = [&](int j) {
-        tc_fence_after();
-        T::dots(tS, sK, ring + of(place_q(j)) * Lay::T, on);
-        commit_on(smem_u32(&b_s), on);
-      };
-      auto issue_dp = [&](int j) {
-        tc_fence_after();
-        T::dots(tP, sV, ring + of(place_do(j)) * Lay::T, on);
-        commit_on(smem_u32(&b_dp), on);
-      };
-      while (go) {
-        const int n = w.c1() - w.c0(), q0 = w.line.kind.first(w.at.u) + w.c0();
-        // (the last unit's P and ds have been read: its last dK was waited for below)
-        ok = warp_wait(b_fix, units++) && there(place_q(g), g, q0);
-        if (!ok) break;
-        issue_s(g);
-        ok = there(place_do(g), g, q0);
-        if (!ok) break;
-        issue_dp(g);
-        if (n == 1) commit_on(smem_u32(&b_fixfree), on);
-        for (int j = 0; j < n && ok; ++j, ++g) {
-          ok = warp_wait(b_p, g);
+      while (go && warp == 17) {  // S and dP: their places are P's and ds's of the step before, which have been read then
+        ok = warp_wait(b_fix, units++);
+        for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
+          const int pq = of(place_q(g)), po = of(place_do(g));
+          ok = warp_wait(b_tile[pq], g >> 1) && (g == 0 || warp_wait(b_o1, g - 1));
           if (!ok) break;
           tc_fence_after();
-          T::template rows<2>(tV, tS, ring + of(place_do(g)) * Lay::T, j == 0, on);
+          T::dots(tS, sK, ring + pq * Lay::T, on);
+          commit_on(smem_u32(&b_s), on);
+          ok = warp_wait(b_tile[po], g >> 1) && (g == 0 || warp_wait(b_o2, g - 1));
+          if (!ok) break;
+          tc_fence_after();
+          T::dots(tP, sV, ring + po * Lay::T, on);
+          commit_on(smem_u32(&b_dp), on);
+        }
+        commit_on(smem_u32(&b_fixfree), on);
+        go = ok && w.next();
+      }
+      while (go && warp == 18) {  // dV and dK
+        for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
+          const int pq = of(place_q(g)), po = of(place_do(g));
+          ok = warp_wait(b_tile[po], g >> 1) && warp_wait(b_p, g);
+          if (!ok) break;
+          tc_fence_after();
+          T::template rows<2>(tV, tS, ring + po * Lay::T, j == w.c0(), on);
           commit_on(smem_u32(&b_o1), on);
-          commit_on(smem_u32(&b_free[place_do(g)]), on);
-          if (j + 1 < n) {  // S: its place is P's, which has been read then
-            ok = there(place_q(g + 1), g + 1, q0 + j + 1) && warp_wait(b_o1, g);
-            if (!ok) break;
-            issue_s(g + 1);
-          }
           ok = warp_wait(b_ds, g);
           if (!ok) break;
+          commit_on(smem_u32(&b_free[po]), on);  // (dP, which has read it too, is done)
           tc_fence_after();
-          T::template rows<2>(tK, tP, ring + of(place_q(g)) * Lay::T, j == 0, on);
+          T::template rows<2>(tK, tP, ring + pq * Lay::T, j == w.c0(), on);
           commit_on(smem_u32(&b_o2), on);
-          commit_on(smem_u32(&b_free[place_q(g)]), on);
-          ok = j + 1 == n || there(place_do(g + 1), g + 1, q0 + j + 1);
-          ok = ok && warp_wait(b_o2, g);
-          if (ok && j + 1 < n) {
-            issue_dp(g + 1);
-            if (j + 2 == n) commit_on(smem_u32(&b_fixfree), on);
-          }
+          commit_on(smem_u32(&b_free[pq]), on);
         }
         go = ok && w.next();
       }
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
-      commit_on(smem_u32(&b_all), on);
+      commit_on(smem_u32(&b_all[warp - 17]), on);
       __syncwarp();
-      warp_wait(b_all, 0);  // every product is complete before the CTA may leave
-    } else if (warp == 18) {
+      warp_wait(b_all[warp - 17], 0);  // every product is complete before the CTA may leave
+    } else {
       int g = 0;
+      unsigned uses = 0;  // of each place's b_raw, their parities
       while (go) {
         for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
           const int q = w.line.kind.first(w.at.u) + j;
@@ -1234,6 +1224,17 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
           for (int x = 0; x < 4; ++x) s_nl[g & 1][lane + 32 * x] = nl[x], s_nd[g & 1][lane + 32 * x] = nd[x];
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&b_stat[g & 1]));
+          const int held = (w.at.n - q * tok) * G;
+          if (held < tok * G) {  // rows behind the text: cleared before the products see them
+            for (int y = 0; y < 2 && ok; ++y) {
+              const int place = y ? place_do(g) : place_q(g);
+              ok = warp_wait(b_raw[place], (int)(uses >> place & 1u));
+              uses ^= 1u << place;
+              if (!ok) break;
+              T::clear_from(ring + place * Lay::T, held, lane);
+              if (lane == 0) mbar_arrive(smem_u32(&b_tile[place]));
+            }
+          }
         }
         go = ok && w.next();
       }
@@ -1345,42 +1346,56 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
   if (warp == 16) tmem_dealloc(tmem, 512);
 }
 
-// Adds up the parts of a unit that several CTAs share, in their order: CTA (run i + 1, two pieces of 4 columns of the 128 rows). Kind
+// Adds up the parts of a unit that several CTAs share, in their order: CTA (run i + 1, 8 pieces of 4 columns of the 128 rows). Kind
 // ByQueries: dq and delta; ByKeys: dv and dk.
 template <int HD, typename Kind>
 __global__ void __launch_bounds__(256) k_packed_back_join(const PackedParams a) {
   constexpr bool KEYS = Kind::KEYS;
-  constexpr int STATE = KEYS ? BackLayout<HD>::DKV_STATE : BackLayout<HD>::DQ_STATE;
+  constexpr int STATE = KEYS ? BackLayout<HD>::DKV_STATE : BackLayout<HD>::DQ_STATE, X = 4;
   const int G = a.Hq / a.Hkv, tok = 128 / G, i = blockIdx.x + 1;
   pdl_launch_dependents();
   pdl_wait();
   Cut c;
   int last;
   if (!parts_from(a.cuts, gridDim.x + 1, a.t.n_seqs, i, c, last)) return;
-  const int r = threadIdx.x & 127, x = 2 * blockIdx.y + (threadIdx.x >> 7), r_tok = r / G;
+  const int r = threadIdx.x & 127, x0 = X * (2 * blockIdx.y + (threadIdx.x >> 7)), r_tok = r / G;
   const int index = KEYS ? c.u * PT_KEYS + r : c.u * tok + r_tok;
   if (index >= c.n || (!KEYS && r_tok >= tok)) return;
   const long long row = c.row0 + index;
   auto part = [&](int k) { return a.states + (long long)(2 * k + (k == i - 1 ? 1 : 0)) * STATE; };
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 o[X];
+#pragma unroll
+  for (int x = 0; x < X; ++x) o[x] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
-  for (int k = i - 1; k <= last; ++k) {
-    const float4 v = reinterpret_cast<const float4*>(part(k))[x * 128 + r];
-    o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
-  }
+  for (int k = i - 1; k <= last; ++k)
+#pragma unroll
+    for (int x = 0; x < X; ++x) {
+      const float4 v = reinterpret_cast<const float4*>(part(k))[(x0 + x) * 128 + r];
+      o[x].x += v.x, o[x].y += v.y, o[x].z += v.z, o[x].w += v.w;
+    }
   bf16* dst;
   float f = a.scale;
   if (!KEYS) {
-    dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (c.kvh * G + r - r_tok * G) * HD + 4 * x;
-  } else if (x < HD / 4) {
-    dst = reinterpret_cast<bf16*>(a.dv) + row * a.ld_dv + c.kvh * HD + 4 * x;
+    dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (c.kvh * G + r - r_tok * G) * HD + 4 * x0;
+  } else if (x0 < HD / 4) {
+    dst = reinterpret_cast<bf16*>(a.dv) + row * a.ld_dv + c.kvh * HD + 4 * x0;
     f = 1.f;
   } else {
-    dst = reinterpret_cast<bf16*>(a.dk) + row * a.ld_dk + c.kvh * HD + 4 * x - HD;
+    dst = reinterpret_cast<bf16*>(a.dk) + row * a.ld_dk + c.kvh * HD + 4 * x0 - HD;
   }
-  dst[0] = __float2bfloat16_rn(o.x * f), dst[1] = __float2bfloat16_rn(o.y * f);
-  dst[2] = __float2bfloat16_rn(o.z * f), dst[3] = __float2bfloat16_rn(o.w * f);
-  if (!KEYS && x == 0) {
+  if (((uintptr_t)dst & 15) == 0) {
+#pragma unroll
+    for (int x = 0; x < X; x += 2)
+      reinterpret_cast<uint4*>(dst)[x / 2] = make_uint4(pack_bf16(o[x].x * f, o[x].y * f), pack_bf16(o[x].z * f, o[x].w * f),
+                                                        pack_bf16(o[x + 1].x * f, o[x + 1].y * f), pack_bf16(o[x + 1].z * f, o[x + 1].w * f));
+  } else {
+#pragma unroll
+    for (int x = 0; x < X; ++x) {
+      dst[4 * x] = __float2bfloat16_rn(o[x].x * f), dst[4 * x + 1] = __float2bfloat16_rn(o[x].y * f);
+      dst[4 * x + 2] = __float2bfloat16_rn(o[x].z * f), dst[4 * x + 3] = __float2bfloat16_rn(o[x].w * f);
+    }
+  }
+  if (!KEYS && x0 == 0) {
     float eps = 0.f;
     for (int k = i - 1; k <= last; ++k) eps += part(k)[128 * HD + r];
     a.delta[row * a.Hq + c.kvh * G + r - r_tok * G] = part(i - 1)[128 * (HD + 1) + r] + eps;
@@ -1433,7 +1448,7 @@ jf_status tc_forward(const PackedParams& a, int sms, cudaStream_t st) {
       !tc_map(&maps.v, a.v, a.ld_v, a.Hkv, HD, a.t.n_rows, 1, 128))
     return JF_ECUDA;
   cudaError_t e = packed_launch(k_packed_attn_tc<HD>, dim3(sms), dim3(PA_THREADS), FwdLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_attn_join<HD>, dim3(sms - 1, HD / 4), dim3(256), 0, st, a);
+  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_attn_join<HD>, dim3(sms - 1, 8), dim3(256), 0, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 
@@ -1448,9 +1463,9 @@ jf_status tc_backward(const PackedParams& a, int sms, cudaStream_t st) {
   if (a.t.max_rows > PT_KEYS)  // (delta is read where a row has several steps)
     e = packed_launch(k_packed_delta_tc<HD>, dim3((unsigned)(((long long)a.t.n_rows * a.Hq * (HD / 8) + 255) / 256)), dim3(256), 0, st, a);
   if (e == cudaSuccess) e = packed_launch(k_packed_dq_tc<HD>, dim3(sms), dim3(PT_THREADS), DqLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByQueries>, dim3(sms - 1, HD / 8), dim3(256), 0, st, a);
+  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByQueries>, dim3(sms - 1, HD / 32), dim3(256), 0, st, a);
   if (e == cudaSuccess) e = packed_launch(k_packed_dkv_tc<HD>, dim3(sms), dim3(PT_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t, tok)) e = packed_launch(k_packed_back_join<HD, ByKeys>, dim3(sms - 1, HD / 4), dim3(256), 0, st, a);
+  if (e == cudaSuccess && tc_cuts(a.t, tok)) e = packed_launch(k_packed_back_join<HD, ByKeys>, dim3(sms - 1, HD / 16), dim3(256), 0, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 
