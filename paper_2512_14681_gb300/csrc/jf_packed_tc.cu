@@ -367,7 +367,7 @@ JF_DEV void scale_o(uint32_t t_o, float x) {
 // (Two threads a row, in 16 warps, took 1.4 times as long: they have to agree on the row's maximum at every step, and 96 registers
 // are too few.)
 // ---------------------------------------------------------------------------------------------
-constexpr int PA_THREADS = 384;
+constexpr int PA_THREADS = 384;  // 168 registers a thread: a row's 128 scores fit
 constexpr float PA_LAG = 8.f;  // a row's reference maximum follows its scores when they exceed it by more
 template <int HD>
 struct FwdLayout {
@@ -456,9 +456,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
     return max(0, min(w.c1(), (min(w.at.n, first + tok) + PT_KEYS - 1) / PT_KEYS) - w.c0());
   };
 
-  // Registers: 384 x 168 at launch; 128 x 80 + 256 x 208 are fewer.
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 8) {
       int tiles = 0, units[2] = {0, 0};
       const uint32_t q_bytes = (uint32_t)(tok * G * HD * 2);
@@ -561,7 +559,6 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
       if (!ok && lane == 0) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     clear_rest<HD>(a, 0, 256);
     const int s = warp >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_row + s * 128, t_o = t_row + 256 + s * 128;
