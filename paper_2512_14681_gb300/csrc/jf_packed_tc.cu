@@ -16,19 +16,22 @@ namespace jf {
 namespace {
 
 constexpr int PT_KEYS = 128;                     // keys of a step (of a tile, in dk and dv)
-constexpr int PT_MIN_SHARE = 4;                  // shortest run of a CTA
 constexpr int PT_SNAP = 2, PT_WHOLE = 6;         // a cut moves to a unit's end over so many steps; units of so many are not cut
 
 // ---------------------------------------------------------------------------------------------
 // The line of units. Kind says how a text is cut: units(n), steps(n, u) for a text of n rows.
 // ---------------------------------------------------------------------------------------------
-struct ByQueries {  // tiles of `tok` tokens over the key tiles that they see
+template <int COST>
+struct ByQueries {  // tiles of `tok` tokens over the key tiles that they see; COST: of a unit beside its steps
   static constexpr bool KEYS = false;
-  static constexpr int UC = 2;
+  static constexpr int UC = COST;
   int tok;
   JF_DEV int units(int n) const { return (n + tok - 1) / tok; }
   JF_DEV int steps(int n, int u) const { return (min(n, (u + 1) * tok) + PT_KEYS - 1) / PT_KEYS; }
 };
+
+using ByFwd = ByQueries<2>;
+using ByDq = ByQueries<5>;
 
 struct Cut {        // a place between steps: before step `step` of a unit
   int b, kvh, u, step, n_steps, row0, n;
@@ -78,8 +81,8 @@ struct Line {
     total = pre_[t.n_seqs];
     return true;
   }
-  // How many of `most` CTAs have a run.
-  JF_DEV int workers(int most) const { return max(1, min(most, total / PT_MIN_SHARE)); }
+  // How many of `most` CTAs have a run: none is shorter than a unit of one step.
+  JF_DEV int workers(int most) const { return max(1, min(most, total / (Kind::UC + 1))); }
   // The cut before run i of n, by a whole warp; before the first and behind the last: b = -1 where there is no unit.
   JF_DEV Cut cut(int i, int n) const {
     const int x = (int)((long long)total * i / n), lane = threadIdx.x & 31;
@@ -427,7 +430,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
   }
   pdl_launch_dependents();
   pdl_wait();
-  Run<ByQueries> w = {{{2 * tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
+  Run<ByFwd> w = {{{2 * tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
   if (!w.line.build(reinterpret_cast<int*>(sm), &s_bad, a.err)) {
     if (tid == 0) tell_cut(a.cuts, {}, false);
     return;
@@ -450,7 +453,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
   bool ok = true, go = (int)blockIdx.x < workers && w.line.total > 0 && w.there();
   if (tid == 0) tell_cut(a.cuts, w.at, (int)blockIdx.x < workers && w.line.total > 0);
   // steps of stream s of the unit in hand, within the run: from c0 on
-  auto stream_steps = [&](const Run<ByQueries>& w, int s) {
+  auto stream_steps = [&](const Run<ByFwd>& w, int s) {
     const int first = (2 * w.at.u + s) * tok;  // its first token
     if (first >= w.at.n) return 0;
     return max(0, min(w.c1(), (min(w.at.n, first + tok) + PT_KEYS - 1) / PT_KEYS) - w.c0());
@@ -853,7 +856,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
     mbar_init(smem_u32(&b_ds[1]), 16);
     fence_mbar_init();
   }
-  Run<ByQueries> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
+  Run<ByDq> w = {{{tok}, a.t, a.Hkv, 0, nullptr}, {}, &s_cut[1]};
   bool go, ok = true;
   if (!back_begin(w, a, smp, &s_bad, s_cut, &tmem_slot, go)) return;
   const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_slot, 0), tS = tmem, tP = tmem + 128, tG = tmem + 384;
@@ -1076,7 +1079,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
 
 struct ByKeys {  // tiles of keys over the tiles of `tok` tokens that see them
   static constexpr bool KEYS = true;
-  static constexpr int UC = 2;
+  static constexpr int UC = 3;
   int tok;
   JF_DEV int units(int n) const { return (n + PT_KEYS - 1) / PT_KEYS; }
   JF_DEV int first(int u) const { return u * PT_KEYS / tok; }
@@ -1344,7 +1347,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
 }
 
 // Adds up the parts of a unit that several CTAs share, in their order: CTA (run i + 1, 8 pieces of 4 columns of the 128 rows). Kind
-// ByQueries: dq and delta; ByKeys: dv and dk.
+// ByDq: dq and delta; ByKeys: dv and dk.
 template <int HD, typename Kind>
 __global__ void __launch_bounds__(256) k_packed_back_join(const PackedParams a) {
   constexpr bool KEYS = Kind::KEYS;
@@ -1460,7 +1463,7 @@ jf_status tc_backward(const PackedParams& a, int sms, cudaStream_t st) {
   if (a.t.max_rows > PT_KEYS)  // (delta is read where a row has several steps)
     e = packed_launch(k_packed_delta_tc<HD>, dim3((unsigned)(((long long)a.t.n_rows * a.Hq * (HD / 8) + 255) / 256)), dim3(256), 0, st, a);
   if (e == cudaSuccess) e = packed_launch(k_packed_dq_tc<HD>, dim3(sms), dim3(PT_THREADS), DqLayout<HD>::TOTAL, st, a, maps);
-  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByQueries>, dim3(sms - 1, HD / 32), dim3(256), 0, st, a);
+  if (e == cudaSuccess && tc_cuts(a.t, PT_KEYS)) e = packed_launch(k_packed_back_join<HD, ByDq>, dim3(sms - 1, HD / 32), dim3(256), 0, st, a);
   if (e == cudaSuccess) e = packed_launch(k_packed_dkv_tc<HD>, dim3(sms), dim3(PT_THREADS), BackLayout<HD>::TOTAL, st, a, maps);
   if (e == cudaSuccess && tc_cuts(a.t, tok)) e = packed_launch(k_packed_back_join<HD, ByKeys>, dim3(sms - 1, HD / 16), dim3(256), 0, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
