@@ -14,71 +14,89 @@
 namespace jf {
 namespace {
 
-constexpr int PF_T = 64, PF_THREADS = 256;  // rows of a tile (of queries, of keys)
+// Rows that a CTA owns (of queries, or of keys in dk and dv) and rows of the other kind that it takes at a time. 16 x 16 threads. (With 64
+// owned rows the longest text's last tile is twice as long a chain: 777 rows among others, 4 heads of 64, 76 us instead of 70; 63 with the next step's rows asked for ahead.)
+constexpr int PF_OWN = 32, PF_T = 64, PF_THREADS = 256;
 
-// Values of `rows` rows from p on (row `ld` apart, HD long) as fp32 rows of HD + 4 in shared memory; rows up to PF_T are zeros.
-template <typename T, int HD>
-JF_DEV void pf_load(float* dst, const T* p, long long ld, int rows, bool by16) {
-  constexpr int N = 16 / sizeof(T), C = HD / N;
-  for (int i = threadIdx.x; i < PF_T * C; i += PF_THREADS) {
-    const int r = i / C, c = i % C * N;
-    float x[N];
-    const T* src = p + r * ld + c;
-    if (r >= rows) {
+// Values of `rows` rows from p on (row `ld` apart, HD long): asked for, and then as fp32 rows of HD + 4 in shared memory, where rows up
+// to ALL are zeros. (Rows that 16-byte loads cannot read are read when they are put.)
+template <typename T, int HD, int ALL>
+struct PfRows {
+  static constexpr int N = 16 / sizeof(T), C = HD / N, IT = ALL * C / PF_THREADS;
+  const T* p;
+  long long ld;
+  int rows;
+  bool by16;
+  uint4 w[IT];
+  JF_DEV void ask(const T* p_, long long ld_, int rows_, bool by16_) {
+    p = p_, ld = ld_, rows = rows_, by16 = by16_;
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = 0.f;
-    } else if (by16) {
-      const uint4 w = *reinterpret_cast<const uint4*>(src);
-      const T* t = reinterpret_cast<const T*>(&w);
+    for (int k = 0; k < IT; ++k) {
+      const int i = threadIdx.x + k * PF_THREADS, r = i / C, c = i % C * N;
+      w[k] = by16 && r < rows ? *reinterpret_cast<const uint4*>(p + r * ld + c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  JF_DEV void put(float* dst) const {
+#pragma unroll
+    for (int k = 0; k < IT; ++k) {
+      const int i = threadIdx.x + k * PF_THREADS, r = i / C, c = i % C * N;
+      float x[N];
+      const T* t = reinterpret_cast<const T*>(&w[k]);
 #pragma unroll
       for (int j = 0; j < N; ++j) x[j] = act_to_f32(t[j]);
-    } else {
+      if (!by16 && r < rows) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = act_to_f32(src[j]);
+        for (int j = 0; j < N; ++j) x[j] = act_to_f32(p[r * ld + c + j]);
+      }
+#pragma unroll
+      for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(dst + r * (HD + 4) + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
     }
-#pragma unroll
-    for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(dst + r * (HD + 4) + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
   }
+};
+template <typename T, int HD, int ALL>
+JF_DEV void pf_load(float* dst, const T* p, long long ld, int rows, bool by16) {
+  PfRows<T, HD, ALL> x;
+  x.ask(p, ld, rows, by16);
+  x.put(dst);
 }
 
 // s[i][j] = a row (ty + 16 i) . b row (tx + 16 j)
-template <int HD>
-JF_DEV void pf_dots(const float* a, const float* b, int ty, int tx, float (&s)[4][4]) {
+template <int HD, int I, int J>
+JF_DEV void pf_dots(const float* a, const float* b, int ty, int tx, float (&s)[I][J]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < I; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+    for (int j = 0; j < J; ++j) s[i][j] = 0.f;
 #pragma unroll 4
   for (int d = 0; d < HD; d += 4) {
-    float4 x[4], y[4];
+    float4 x[I], y[J];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * (HD + 4) + d);
-      y[i] = *reinterpret_cast<const float4*>(b + (tx + 16 * i) * (HD + 4) + d);
-    }
+    for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * (HD + 4) + d);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int j = 0; j < J; ++j) y[j] = *reinterpret_cast<const float4*>(b + (tx + 16 * j) * (HD + 4) + d);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
         s[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, s[i][j]))));
   }
 }
 
-// o[i][.] += sum_c w[ty + 16 i][c] b[c][dims 4 tx + 64 j ..], w in rows of PF_T + 4
-template <int HD>
-JF_DEV void pf_rows_by(const float* w, const float* b, int ty, int tx, float (&o)[4][HD / 16]) {
+// o[i][.] += sum_c w[ty + 16 i][c] b[c][dims 4 tx + 64 j ..] over PF_T columns c, w in rows of PF_T + 4
+template <int HD, int I>
+JF_DEV void pf_rows_by(const float* w, const float* b, int ty, int tx, float (&o)[I][HD / 16]) {
 #pragma unroll 2
   for (int c = 0; c < PF_T; c += 4) {
-    float4 x[4];
+    float4 x[I];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * (PF_T + 4) + c);
+    for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * (PF_T + 4) + c);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int j = 0; j < HD / 64; ++j) {
         const float4 y = *reinterpret_cast<const float4*>(b + (c + k) * (HD + 4) + 4 * tx + 64 * j);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < I; ++i) {
           const float f = k == 0 ? x[i].x : (k == 1 ? x[i].y : (k == 2 ? x[i].z : x[i].w));
           o[i][4 * j] = fmaf(f, y.x, o[i][4 * j]);
           o[i][4 * j + 1] = fmaf(f, y.y, o[i][4 * j + 1]);
@@ -89,23 +107,19 @@ JF_DEV void pf_rows_by(const float* w, const float* b, int ty, int tx, float (&o
   }
 }
 
-// o[i][.] += sum_r w[r][4 ty + i] b[r][dims 4 tx + 64 j ..]
+// o[i][.] += sum_r w[r][2 ty + i] b[r][dims 4 tx + 64 j ..] over PF_T rows r, w in rows of PF_OWN + 4
 template <int HD>
-JF_DEV void pf_columns_by(const float* w, const float* b, int ty, int tx, float (&o)[4][HD / 16]) {
+JF_DEV void pf_columns_by(const float* w, const float* b, int ty, int tx, float (&o)[2][HD / 16]) {
 #pragma unroll 4
   for (int r = 0; r < PF_T; ++r) {
-    const float4 x = *reinterpret_cast<const float4*>(w + r * (PF_T + 4) + 4 * ty);
-    const float f[4] = {x.x, x.y, x.z, x.w};
+    const float2 f = *reinterpret_cast<const float2*>(w + r * (PF_OWN + 4) + 2 * ty);
 #pragma unroll
     for (int j = 0; j < HD / 64; ++j) {
       const float4 y = *reinterpret_cast<const float4*>(b + r * (HD + 4) + 4 * tx + 64 * j);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        o[i][4 * j] = fmaf(f[i], y.x, o[i][4 * j]);
-        o[i][4 * j + 1] = fmaf(f[i], y.y, o[i][4 * j + 1]);
-        o[i][4 * j + 2] = fmaf(f[i], y.z, o[i][4 * j + 2]);
-        o[i][4 * j + 3] = fmaf(f[i], y.w, o[i][4 * j + 3]);
-      }
+      o[0][4 * j] = fmaf(f.x, y.x, o[0][4 * j]), o[1][4 * j] = fmaf(f.y, y.x, o[1][4 * j]);
+      o[0][4 * j + 1] = fmaf(f.x, y.y, o[0][4 * j + 1]), o[1][4 * j + 1] = fmaf(f.y, y.y, o[1][4 * j + 1]);
+      o[0][4 * j + 2] = fmaf(f.x, y.z, o[0][4 * j + 2]), o[1][4 * j + 2] = fmaf(f.y, y.z, o[1][4 * j + 2]);
+      o[0][4 * j + 3] = fmaf(f.x, y.w, o[0][4 * j + 3]), o[1][4 * j + 3] = fmaf(f.y, y.w, o[1][4 * j + 3]);
     }
   }
 }
@@ -118,7 +132,7 @@ JF_DEV void pf_store4(T* p, float a, float b, float c, float d) {
 struct PfTile {
   int row0, n, first;  // the text's first row and length; the tile's first row in it. n < 0: no tile
 };
-// The tile that CTA x of the grid has: text by text, PF_T rows each. Rows that belong to no text are cleared by `clear(row)`
+// The tile that CTA x of the grid has: text by text, PF_OWN rows each. Rows that belong to no text are cleared by `clear(row)`
 // on the way, each by one CTA of the grid.
 template <typename Clear>
 JF_DEV PfTile pf_tile(const PackedParams& a, Clear clear) {
@@ -127,7 +141,7 @@ JF_DEV PfTile pf_tile(const PackedParams& a, Clear clear) {
   __syncthreads();
   for (int b = threadIdx.x; b < a.t.n_seqs; b += PF_THREADS) {
     if (!packed_text_ok(a.t, b)) s_bad = 1;
-    s_at[b] = (a.t.row_start[b + 1] - a.t.row_start[b] + PF_T - 1) / PF_T;
+    s_at[b] = (a.t.row_start[b + 1] - a.t.row_start[b] + PF_OWN - 1) / PF_OWN;
   }
   __syncthreads();
   if (s_bad) {
@@ -159,7 +173,7 @@ JF_DEV PfTile pf_tile(const PackedParams& a, Clear clear) {
   const int b = s_found;
   if (b < 0) return {0, -1, 0};
   const int s0 = a.t.row_start[b];
-  return {s0, a.t.row_start[b + 1] - s0, s_at[b] * PF_T};
+  return {s0, a.t.row_start[b + 1] - s0, s_at[b] * PF_OWN};
 }
 
 template <typename T>
@@ -169,10 +183,10 @@ JF_DEV bool pf_by16(const void* p, long long ld) {
 
 // Grid (tiles, query heads).
 template <typename T, int HD>
-__global__ void __launch_bounds__(PF_THREADS, 1) k_packed_attn(const PackedParams a) {
+__global__ void __launch_bounds__(PF_THREADS, 2) k_packed_attn(const PackedParams a) {
   extern __shared__ float sm[];
-  constexpr int TILE = PF_T * (HD + 4);
-  float *sq = sm, *sk = sm + TILE, *sv = sm + 2 * TILE, *sp = sm + 3 * TILE;
+  constexpr int TILE = PF_T * (HD + 4), OWN = PF_OWN * (HD + 4);
+  float *sq = sm, *sk = sm + OWN, *sv = sk + TILE, *sp = sv + TILE;
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16, h = blockIdx.y, kvh = h / (a.Hq / a.Hkv);
   pdl_launch_dependents();
   pdl_wait();
@@ -182,22 +196,29 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_attn(const PackedParam
     if (tid == 0 && a.lse) a.lse[(long long)r * a.Hq + h] = -INFINITY;
   });
   if (t.n < 0) return;
-  const int rows = min(PF_T, t.n - t.first);
+  const int rows = min(PF_OWN, t.n - t.first);
   const bool q16 = pf_by16<T>(a.q, a.ld_q), k16 = pf_by16<T>(a.k, a.ld_k), v16 = pf_by16<T>(a.v, a.ld_v);
-  pf_load<T, HD>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + t.first) * a.ld_q + h * HD, a.ld_q, rows, q16);
-  float m[4], l[4], o[4][HD / 16] = {};
+  pf_load<T, HD, PF_OWN>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + t.first) * a.ld_q + h * HD, a.ld_q, rows, q16);
+  float m[2], l[2], o[2][HD / 16] = {};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
+  for (int i = 0; i < 2; ++i) m[i] = -INFINITY, l[i] = 0.f;
   const float c = a.scale * kLog2e;
+  PfRows<T, HD, PF_T> rk, rv;  // the next step's are on their way while one is worked on
+  auto ask = [&](int k0) {
+    rk.ask(reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
+    rv.ask(reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
+  };
+  ask(0);
   for (int k0 = 0; k0 < t.first + rows; k0 += PF_T) {
     __syncthreads();
-    pf_load<T, HD>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
-    pf_load<T, HD>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
+    rk.put(sk);
+    rv.put(sv);
+    if (k0 + PF_T < t.first + rows) ask(k0 + PF_T);
     __syncthreads();
-    float s[4][4];
+    float s[2][4];
     pf_dots<HD>(sq, sk, ty, tx, s);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const int qi = t.first + ty + 16 * i;
       float mx = -INFINITY;
 #pragma unroll
@@ -227,7 +248,7 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_attn(const PackedParam
     pf_rows_by<HD>(sp, sv, ty, tx, o);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     const int r = ty + 16 * i;
     if (r >= rows) continue;
     const long long at = (long long)(t.row0 + t.first + r) * a.Hq + h;
@@ -257,23 +278,24 @@ __global__ void __launch_bounds__(256) k_packed_delta(const PackedParams a) {
   if (lane == 0) a.delta[i] = s;
 }
 
-// p and ds of a 64 x 64 tile (queries from q0 on, keys from k0 on) into sp and sds.
-template <int HD>
+// p and ds of a tile of I x J queries and keys a thread (queries from q0 on, keys from k0 on) into sp and sds, rows 16 J + 4 apart.
+template <int HD, int I, int J>
 JF_DEV void pf_back_tile(const float* sq, const float* sdo, const float* sk, const float* sv, const float* s_lse, const float* s_delta,
                          int q0, int k0, int n, float c, int ty, int tx, float* sp, float* sds) {
-  float s[4][4], dp[4][4];
+  constexpr int LD = 16 * J + 4;
+  float s[I][J], dp[I][J];
   pf_dots<HD>(sq, sk, ty, tx, s);
   pf_dots<HD>(sdo, sv, ty, tx, dp);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < I; ++i) {
     const int r = ty + 16 * i;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < J; ++j) {
       const int kj = k0 + tx + 16 * j;
       const bool sees = kj <= q0 + r && q0 + r < n;
       const float p = sees ? exp2f(fmaf(s[i][j], c, -s_lse[r])) : 0.f;
-      if (sp) sp[r * (PF_T + 4) + tx + 16 * j] = p;
-      sds[r * (PF_T + 4) + tx + 16 * j] = sees ? p * (dp[i][j] - s_delta[r]) : 0.f;
+      if (sp) sp[r * LD + tx + 16 * j] = p;
+      sds[r * LD + tx + 16 * j] = sees ? p * (dp[i][j] - s_delta[r]) : 0.f;
     }
   }
 }
@@ -282,8 +304,8 @@ JF_DEV void pf_back_tile(const float* sq, const float* sdo, const float* sk, con
 template <typename T, int HD>
 __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dkv(const PackedParams a) {
   extern __shared__ float sm[];
-  constexpr int TILE = PF_T * (HD + 4);
-  float *sq = sm, *sdo = sm + TILE, *sk = sm + 2 * TILE, *sv = sm + 3 * TILE, *sp = sm + 4 * TILE, *sds = sp + PF_T * (PF_T + 4);
+  constexpr int TILE = PF_T * (HD + 4), OWN = PF_OWN * (HD + 4);
+  float *sq = sm, *sdo = sm + TILE, *sk = sm + 2 * TILE, *sv = sk + OWN, *sp = sv + OWN, *sds = sp + PF_T * (PF_OWN + 4);
   __shared__ float s_lse[PF_T], s_delta[PF_T];
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16, kvh = blockIdx.y, G = a.Hq / a.Hkv;
   pdl_launch_dependents();
@@ -293,30 +315,40 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dkv(const PackedParams
     for (int d = tid; d < HD; d += PF_THREADS) dk[r * a.ld_dk + kvh * HD + d] = dv[r * a.ld_dv + kvh * HD + d] = to_act<T>(0.f);
   });
   if (t.n < 0) return;
-  const int rows = min(PF_T, t.n - t.first);
-  pf_load<T, HD>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + t.first) * a.ld_k + kvh * HD, a.ld_k, rows, pf_by16<T>(a.k, a.ld_k));
-  pf_load<T, HD>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + t.first) * a.ld_v + kvh * HD, a.ld_v, rows, pf_by16<T>(a.v, a.ld_v));
+  const int rows = min(PF_OWN, t.n - t.first);
+  pf_load<T, HD, PF_OWN>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + t.first) * a.ld_k + kvh * HD, a.ld_k, rows, pf_by16<T>(a.k, a.ld_k));
+  pf_load<T, HD, PF_OWN>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + t.first) * a.ld_v + kvh * HD, a.ld_v, rows, pf_by16<T>(a.v, a.ld_v));
   const bool q16 = pf_by16<T>(a.q, a.ld_q), do16 = pf_by16<T>(a.d_out, a.ld_do);
-  float gk[4][HD / 16] = {}, gv[4][HD / 16] = {};
-  for (int h = kvh * G; h < (kvh + 1) * G; ++h)
-    for (int q0 = t.first; q0 < t.n; q0 += PF_T) {
-      __syncthreads();
-      const int nq = min(PF_T, t.n - q0);
-      pf_load<T, HD>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + q0) * a.ld_q + h * HD, a.ld_q, nq, q16);
-      pf_load<T, HD>(sdo, reinterpret_cast<const T*>(a.d_out) + (t.row0 + q0) * a.ld_do + h * HD, a.ld_do, nq, do16);
-      if (tid < nq) {
-        s_lse[tid] = a.lse[(long long)(t.row0 + q0 + tid) * a.Hq + h] * kLog2e;
-        s_delta[tid] = a.delta[(long long)(t.row0 + q0 + tid) * a.Hq + h];
-      }
-      __syncthreads();
-      pf_back_tile<HD>(sq, sdo, sk, sv, s_lse, s_delta, q0, t.first, t.n, a.scale * kLog2e, ty, tx, sp, sds);
-      __syncthreads();
-      pf_columns_by<HD>(sp, sdo, ty, tx, gv);
-      pf_columns_by<HD>(sds, sq, ty, tx, gk);
+  float gk[2][HD / 16] = {}, gv[2][HD / 16] = {};
+  PfRows<T, HD, PF_T> rq, rd;  // the next step's are on their way while one is worked on
+  float lse = 0.f, delta = 0.f;
+  auto ask = [&](int h, int q0) {
+    const int nq = min(PF_T, t.n - q0);
+    rq.ask(reinterpret_cast<const T*>(a.q) + (t.row0 + q0) * a.ld_q + h * HD, a.ld_q, nq, q16);
+    rd.ask(reinterpret_cast<const T*>(a.d_out) + (t.row0 + q0) * a.ld_do + h * HD, a.ld_do, nq, do16);
+    if (tid < nq) {
+      lse = a.lse[(long long)(t.row0 + q0 + tid) * a.Hq + h] * kLog2e;
+      delta = a.delta[(long long)(t.row0 + q0 + tid) * a.Hq + h];
     }
+  };
+  ask(kvh * G, t.first);
+  for (int h = kvh * G, q0 = t.first; h < (kvh + 1) * G;) {
+    __syncthreads();
+    rq.put(sq);
+    rd.put(sdo);
+    if (tid < PF_T) s_lse[tid] = lse, s_delta[tid] = delta;
+    const int at = q0;
+    if ((q0 += PF_T) >= t.n) q0 = t.first, ++h;
+    if (h < (kvh + 1) * G) ask(h, q0);
+    __syncthreads();
+    pf_back_tile<HD, PF_T / 16, PF_OWN / 16>(sq, sdo, sk, sv, s_lse, s_delta, at, t.first, t.n, a.scale * kLog2e, ty, tx, sp, sds);
+    __syncthreads();
+    pf_columns_by<HD>(sp, sdo, ty, tx, gv);
+    pf_columns_by<HD>(sds, sq, ty, tx, gk);
+  }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 4 * ty + i;
+  for (int i = 0; i < 2; ++i) {
+    const int r = 2 * ty + i;
     if (r >= rows) continue;
     const long long at = t.row0 + t.first + r;
 #pragma unroll
@@ -332,9 +364,9 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dkv(const PackedParams
 template <typename T, int HD>
 __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dq(const PackedParams a) {
   extern __shared__ float sm[];
-  constexpr int TILE = PF_T * (HD + 4);
-  float *sq = sm, *sdo = sm + TILE, *sk = sm + 2 * TILE, *sv = sm + 3 * TILE, *sds = sm + 4 * TILE;
-  __shared__ float s_lse[PF_T], s_delta[PF_T];
+  constexpr int TILE = PF_T * (HD + 4), OWN = PF_OWN * (HD + 4);
+  float *sq = sm, *sdo = sm + OWN, *sk = sm + 2 * OWN, *sv = sk + TILE, *sds = sv + TILE;
+  __shared__ float s_lse[PF_OWN], s_delta[PF_OWN];
   const int tid = threadIdx.x, ty = tid / 16, tx = tid % 16, h = blockIdx.y, kvh = h / (a.Hq / a.Hkv);
   pdl_launch_dependents();
   pdl_wait();
@@ -343,26 +375,33 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dq(const PackedParams 
     for (int d = tid; d < HD; d += PF_THREADS) dq[r * a.ld_dq + h * HD + d] = to_act<T>(0.f);
   });
   if (t.n < 0) return;
-  const int rows = min(PF_T, t.n - t.first);
-  pf_load<T, HD>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + t.first) * a.ld_q + h * HD, a.ld_q, rows, pf_by16<T>(a.q, a.ld_q));
-  pf_load<T, HD>(sdo, reinterpret_cast<const T*>(a.d_out) + (t.row0 + t.first) * a.ld_do + h * HD, a.ld_do, rows, pf_by16<T>(a.d_out, a.ld_do));
+  const int rows = min(PF_OWN, t.n - t.first);
+  pf_load<T, HD, PF_OWN>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + t.first) * a.ld_q + h * HD, a.ld_q, rows, pf_by16<T>(a.q, a.ld_q));
+  pf_load<T, HD, PF_OWN>(sdo, reinterpret_cast<const T*>(a.d_out) + (t.row0 + t.first) * a.ld_do + h * HD, a.ld_do, rows, pf_by16<T>(a.d_out, a.ld_do));
   if (tid < rows) {
     s_lse[tid] = a.lse[(long long)(t.row0 + t.first + tid) * a.Hq + h] * kLog2e;
     s_delta[tid] = a.delta[(long long)(t.row0 + t.first + tid) * a.Hq + h];
   }
   const bool k16 = pf_by16<T>(a.k, a.ld_k), v16 = pf_by16<T>(a.v, a.ld_v);
-  float g[4][HD / 16] = {};
+  float g[2][HD / 16] = {};
+  PfRows<T, HD, PF_T> rk, rv;  // the next step's are on their way while one is worked on
+  auto ask = [&](int k0) {
+    rk.ask(reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
+    rv.ask(reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
+  };
+  ask(0);
   for (int k0 = 0; k0 < t.first + rows; k0 += PF_T) {
     __syncthreads();
-    pf_load<T, HD>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
-    pf_load<T, HD>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
+    rk.put(sk);
+    rv.put(sv);
+    if (k0 + PF_T < t.first + rows) ask(k0 + PF_T);
     __syncthreads();
-    pf_back_tile<HD>(sq, sdo, sk, sv, s_lse, s_delta, t.first, k0, t.n, a.scale * kLog2e, ty, tx, nullptr, sds);
+    pf_back_tile<HD, PF_OWN / 16, PF_T / 16>(sq, sdo, sk, sv, s_lse, s_delta, t.first, k0, t.n, a.scale * kLog2e, ty, tx, nullptr, sds);
     __syncthreads();
     pf_rows_by<HD>(sds, sk, ty, tx, g);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     const int r = ty + 16 * i;
     if (r >= rows) continue;
 #pragma unroll
@@ -372,15 +411,22 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dq(const PackedParams 
   }
 }
 
+// Shared memory of owned tiles, other tiles, and floats beside them.
 template <int HD>
-constexpr int pf_smem(int tiles, int squares) {
-  return (tiles * PF_T * (HD + 4) + squares * PF_T * (PF_T + 4)) * 4;
+constexpr int pf_smem(int own, int tiles, int more) {
+  return ((own * PF_OWN + tiles * PF_T) * (HD + 4) + more) * 4;
 }
+template <int HD>
+constexpr int pf_smem_attn = pf_smem<HD>(1, 2, PF_OWN * (PF_T + 4));
+template <int HD>
+constexpr int pf_smem_dkv = pf_smem<HD>(2, 2, 2 * PF_T * (PF_OWN + 4));
+template <int HD>
+constexpr int pf_smem_dq = pf_smem<HD>(2, 2, PF_OWN * (PF_T + 4));
 template <typename T, int HD>
 cudaError_t pf_prepare() {
-  cudaError_t e = cudaFuncSetAttribute(k_packed_attn<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem<HD>(3, 1));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dkv<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem<HD>(4, 2));
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem<HD>(4, 1));
+  cudaError_t e = cudaFuncSetAttribute(k_packed_attn<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_attn<HD>);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dkv<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_dkv<HD>);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_dq<HD>);
   return e;
 }
 PerDeviceOnce g_pf_once;
@@ -396,18 +442,18 @@ bool pf_ready() {
   }) == 0;
 }
 
-unsigned pf_tiles(const jf_packed& t) { return (unsigned)((t.n_rows + PF_T - 1) / PF_T + t.n_seqs); }
+unsigned pf_tiles(const jf_packed& t) { return (unsigned)((t.n_rows + PF_OWN - 1) / PF_OWN + t.n_seqs); }
 
 template <typename T, int HD>
 cudaError_t pf_forward(const PackedParams& a, cudaStream_t st) {
-  return packed_launch(k_packed_attn<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem<HD>(3, 1), st, a);
+  return packed_launch(k_packed_attn<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem_attn<HD>, st, a);
 }
 template <typename T, int HD>
 cudaError_t pf_backward(const PackedParams& a, cudaStream_t st) {
   const long long warps = (long long)a.t.n_rows * a.Hq;
   cudaError_t e = packed_launch(k_packed_delta<T, HD>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a);
-  if (e == cudaSuccess) e = packed_launch(k_packed_dkv<T, HD>, dim3(pf_tiles(a.t), a.Hkv), dim3(PF_THREADS), pf_smem<HD>(4, 2), st, a);
-  if (e == cudaSuccess) e = packed_launch(k_packed_dq<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem<HD>(4, 1), st, a);
+  if (e == cudaSuccess) e = packed_launch(k_packed_dkv<T, HD>, dim3(pf_tiles(a.t), a.Hkv), dim3(PF_THREADS), pf_smem_dkv<HD>, st, a);
+  if (e == cudaSuccess) e = packed_launch(k_packed_dq<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem_dq<HD>, st, a);
   return e;
 }
 
