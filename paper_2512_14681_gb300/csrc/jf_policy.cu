@@ -65,7 +65,7 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 //
 // In the log2 domain, with c = scale log2 e and a reference b = c m rounded (m the thread's largest logit): y = x c - b comes
 // rounded once from a fused product, S = sum 2^y, T = sum 2^y y; states are joined by their b. Then
-//   lp = ln 2 (y_t - log2 S),  H = ln 2 (log2 S - T / S),  p = 2^y / S,
+//   lp = scale (x_t - m) - ln 2 (log2 S + b - c m),  H = ln 2 (log2 S - T / S),  p = 2^y / S,
 //   dloss/dx = -scale / S 2^y (g + gh (H - ln S) + gh ln 2 y), + scale g at the target.
 // Logits below -1e30 (and c above 1e6) would leave fp32's range in y: they count as -1e30, whose 2^y is 0, unless the row's
 // largest is such a one itself; its sums then are taken again from differences x - m.
@@ -73,7 +73,9 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8, PL_CHUNKS = 2;
 constexpr int PL_FIT[3] = {56832, 76288, 115200};  // bytes of a CTA's run with which four, three, two are resident on an SM
 constexpr int PL_MOST = PL_FIT[2];
+constexpr int PL_ROWS = 1 << 30;  // (a row and the step to the next fit 31 bits)
 constexpr float PL_FAR = 1e30f, PL_LARGE = 1e29f, PL_STEEP = 1e6f, LN2 = 0.69314718055994531f;
+constexpr float LOG2E_LO = 1.9259630e-8f;  // log2 e beyond LOG2E
 
 JF_DEV float warp_max(float v) {
 #pragma unroll
@@ -298,8 +300,11 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
       if (target >= a.V) {
         lp = __int_as_float(0x7fffffff);
       } else if (target >= 0) {
-        const float y = far ? (x_t - m) * c : fmaf(x_t, c, -st.m);
-        lp = empty ? -INFINITY : LN2 * (y - l2);
+        // With c (1 + d) = scale log2 e before c's rounding: log2 of the sum of 2^(c (1 + d) (x - m)) is log2 S + (b - c m) + d T / S
+        // but for d's square. (KL is small where lp is near ref_logprob, and would show the rounding.)
+        const float d = fmaf(a.scale, LOG2E_LO, fmaf(a.scale, LOG2E, -c)) / c;
+        const float apart = far ? 0.f : fmaf(d, st.t / st.s, -fmaf(m, c, -st.m));
+        lp = empty ? -INFINITY : fmaf(x_t - m, a.scale, -LN2 * (l2 + apart));
       }
       const PolicyRow p = policy_row(a, target, lp, H, in.old, in.ref, in.A, in.w);
       if (lane == 0) {
@@ -532,6 +537,7 @@ extern "C" jf_status jf_op_policy_loss(const jf_policy_terms* terms, int dtype, 
   if (!terms || !(terms->below >= 0.f && terms->below <= 1.f) || !(terms->above >= 0.f) || !finite(terms->kl) || !finite(terms->entropy) ||
       (!ref_logprob && terms->kl != 0.f) || (dtype != JF_F32 && dtype != JF_BF16) || rows < 0 || vocab < 1 || vocab > (1 << 30) || !err_word)
     return JF_EINVAL;
+  if (rows > PL_ROWS) return JF_EUNSUPPORTED;
   if (!(scale > 0.f) || scale > 1e30f || ld < vocab) return JF_EINVAL;
   if (rows == 0) return JF_OK;
   const uintptr_t type_mask = dtype == JF_BF16 ? 1 : 3;

@@ -93,6 +93,7 @@ def test_arguments_of_the_policy_loss_that_are_refused(lib):
                 dict(ld=99), dict(n=-1), dict(vocab=0), dict(scale=0.0), dict(scale=nan), dict(targets=None), dict(adv=None), dict(g=514), dict(ld_g=99),
                 dict(g=256, ld=101), dict(ws=264), dict(err=None)):
         assert policy(lib, **bad) == J.JF_EINVAL, bad
+    assert policy(lib, n=(1 << 30) + 1) == J.JF_EUNSUPPORTED
     n = C.c_size_t()
     assert lib.jf_op_policy_loss_workspace_bytes(J.JF_F32, 2, 100, C.byref(n)) == J.JF_OK
     if n.value:
