@@ -811,7 +811,7 @@ __global__ void __launch_bounds__(256) k_packed_delta_tc(const PackedParams a) {
   constexpr int LPR = HD / 8;
   pdl_launch_dependents();
   pdl_wait();
-  const uint32_t i = (blockIdx.x * 256 + threadIdx.x) / LPR, piece = threadIdx.x % LPR;  // (n_rows * Hq is at most 2^30)
+  const uint32_t i = blockIdx.x * (256 / LPR) + threadIdx.x / LPR, piece = threadIdx.x % LPR;  // (n_rows * Hq is at most 2^30)
   const uint32_t row = i / a.Hq;
   float d = 0.f;
   if ((int)row < a.t.n_rows)

@@ -213,6 +213,53 @@ def test_offsets_beyond_32_bits(torch):
         assert not torch.isnan(x).any()
 
 
+def test_more_heads_times_rows_than_32_bits_of_pieces(torch):
+    """Over 2^28 rows times heads; those of no text get 0. (out and d_out of the call are q: two buffers of 69 GB.)"""
+    from paper_2512_14681_gb300 import packed as P
+
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 160 << 30:
+        pytest.skip("takes 145 GB")
+    heads, lens, before = (128, 1, 128, "bf16"), [70, 130], (1 << 21) + 64
+    (q0, k0, v0, _), _ = make(torch, heads, lens, seed=15)
+    rows, R, scale = slice(before, before + 200), before + 200, 128 ** -0.5
+    q, dq = (torch.full((R, 128, 128), math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k, v = (torch.full((R, 1, 128), math.nan, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q[rows], k[rows], v[rows] = q0, k0, v0
+    q0 = q0.contiguous()
+    _, lse0 = P.attention(texts_of(torch, lens), q0, k0, v0, scale, want_lse=True)
+    want = P.attention_grad(texts_of(torch, lens), q0, k0, v0, q0, lse0, q0, scale)
+    lse = torch.full((R, 128), math.nan, device="cuda")
+    lse[rows] = lse0
+    got = P.attention_grad(texts_of(torch, lens, before), q, k, v, q, lse, q, scale, grads=(dq, torch.full_like(k, math.nan), torch.full_like(v, math.nan)))
+    P.check()
+    for x, w in zip(got, want):
+        assert torch.equal(x[rows], w)
+        for part in x[:before].split(1 << 18):
+            assert part.amax() == 0 and part.amin() == 0
+    del q, dq, k, v, got, x, part, lse
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("heads", [HEADS[0], HEADS[2], HEADS[9]], ids=lambda h: "%d-%d-%d-%s" % h)
+@pytest.mark.parametrize("lens,longest", [([0], 0), ([0, 0, 0], 0), ([0, 0], 40), ([0] * 1024, 1000)], ids=["one", "none-longer-than-0", "two", "most"])
+def test_a_batch_without_a_row(torch, heads, lens, longest):
+    """All rows are of no text: 0, -infinity."""
+    from paper_2512_14681_gb300 import packed as P
+
+    Hq, Hkv, hd, _ = heads
+    _, dtype = make(torch, heads, [1])
+    n = max(longest, 37)
+    q, k, v, d = (torch.full((n, H, hd), math.nan, dtype=dtype, device="cuda") for H in (Hq, Hkv, Hkv, Hq))
+    for at in (0, 5, n):
+        texts = P.Packed(torch.full((len(lens) + 1,), at, dtype=torch.int32, device="cuda"), n, longest)
+        out, lse = P.attention(texts, q, k, v, 0.1, want_lse=True)
+        grads = [torch.full_like(x, math.nan) for x in (q, k, v)]
+        P.attention_grad(texts, q, k, v, out, lse, d, 0.1, grads=grads)
+        P.check()
+        assert (lse == -math.inf).all() and all((x == 0).all() for x in (out, *grads))
+
+
 @pytest.mark.parametrize("start", [[0, 50, 40, 100], [-1, 20, 60, 100], [0, 20, 60, 101], [0, 80, 90, 100]], ids=["falls", "negative", "behind", "long"])
 @pytest.mark.parametrize("heads", [HEADS[0], HEADS[9]], ids=lambda h: "%d-%d-%d-%s" % h)
 def test_texts_that_do_not_fit_are_reported(torch, heads, start):
