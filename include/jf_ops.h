@@ -178,13 +178,14 @@ jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld,
  * old_logprob NULL: ratio 1, with the gradient of lp; ref_logprob NULL: kl must be 0; weight NULL: 1. All device fp32 [rows].
  * Outputs, device fp32 [rows], each optional: loss, logprob (lp), entropy (H), ratio, kl (e^d - 1 - d). grad_logits
  * (optional): [rows] of vocab values of the logits' dtype, rows ld_grad elements apart; it may be logits itself (with
- * ld_grad = ld).
+ * ld_grad = ld), but not overlap them otherwise. rows <= 2^30.
  * A negative target leaves its row out: loss, logprob, ratio, kl and gradient 0 (entropy is the row's). A weight of 0 makes
  * loss and gradient 0 whatever the other terms are, and an advantage of 0 the first term. A target that cannot occur
  * (a logit of -infinity) has ratio 0 and, with a ref_logprob, an infinite kl without a gradient. Rows without a token that can occur, NaN
  * among the logits and targets >= vocab: as in jf_op_token_logprobs (the loss of the last is NaN, its gradient 0). A ratio
  * beyond the range of fp32 is infinite, as loss and gradient then are where A is negative.
- * workspace: device, 16-byte aligned, no initialisation needed; calls that may overlap on the GPU need one each. */
+ * workspace: device, 16-byte aligned, no initialisation needed; calls that may overlap on the GPU need one each. (0 bytes but for
+ * rows longer than a cluster's shared memory, 460,800 fp32 or 921,600 bf16 values.) */
 typedef struct {
   float below, above; /* how far the ratio counts on either side of 1: 0 <= below <= 1, 0 <= above */
   float kl, entropy;  /* factors of the two other terms */
@@ -217,7 +218,8 @@ jf_status jf_op_packed_attention_workspace_bytes(const jf_packed* texts, int dty
  * over its rows 0 .. i. dtype (JF_BF16 or JF_F32): type of everything but lse; head_dim 64 or 128. q, k, v: rows of n_heads
  * or n_kv_heads heads, ld_* elements apart, so that the three may be parts of one projection's rows; bf16 rows are read by tensor copies where
  * their addresses and ld_* are multiples of 16 bytes, by slower kernels otherwise. out: [n_rows][n_heads][head_dim], 16-byte aligned; lse (optional
- * here): fp32 [n_rows][n_heads], the natural logarithm of the sum of exponentials.
+ * here): fp32 [n_rows][n_heads], the natural logarithm of the sum of exponentials. Outputs may not overlap inputs or one another. n_rows *
+ * n_heads <= 2^30; more is refused (JF_EUNSUPPORTED), as are texts so long that the tiles of all scores pass 2^30.
  * Softmax statistics and sums are fp32; JF_BF16 rounds the probabilities (relative to a row's running maximum) to bf16
  * before their product with v. A NaN or an infinity in a text reaches rows of that text only. Results do not depend on the
  * order in which CTAs run; they depend in rounding on the batch, whose work is split evenly over the GPU. */
@@ -228,7 +230,7 @@ jf_status jf_op_packed_attention(const jf_packed* texts, int dtype, const void* 
 
 /* Its backward pass: the gradients dq, dk, dv of a loss by q, k, v from that by out, d_out (rows ld_do elements apart), for
  * the same texts, q, k, v and scale and that call's out and lse. dq, dk, dv: rows ld_* elements apart (so that they may be
- * parts of one buffer's rows); they may not overlap the inputs. dk and dv of a KV head are sums over its query heads. No
+ * parts of one buffer's rows); they may not overlap the inputs or one another. dk and dv of a KV head are sums over its query heads. No
  * atomics: the order of every sum is fixed. JF_BF16 rounds probabilities and the scores' gradients to bf16 before their products. */
 jf_status jf_op_packed_attention_grad(const jf_packed* texts, int dtype, const void* q, long long ld_q, const void* k,
                                       long long ld_k, const void* v, long long ld_v, int n_heads, int n_kv_heads, int head_dim,

@@ -165,6 +165,20 @@ cudaError_t tl_set_decode(void* records, void* counter);
 #endif
 int gemm_default_splits(int n_tiles, int kb_total);
 bool encode_tmap_bf16(CUtensorMap* tm, const void* ptr, long long K, long long rows, int box_rows);
+// Rows of `width` bytes, `pitch` bytes apart; whether two such share memory (rows that lie between one another's do not; of those
+// with different pitches only ranges are looked at).
+struct RowSpan {
+  const void* p;
+  long long pitch, width;
+};
+inline bool rows_overlap(const RowSpan& x, const RowSpan& y, int rows) {
+  if (!x.p || !y.p || rows < 1) return false;
+  const uintptr_t a = (uintptr_t)x.p, b = (uintptr_t)y.p;
+  if (a + (uintptr_t)((rows - 1) * x.pitch + x.width) <= b || b + (uintptr_t)((rows - 1) * y.pitch + y.width) <= a) return false;
+  if (rows == 1 || x.pitch != y.pitch) return true;
+  const long long off = (long long)((b >= a ? b - a : a - b) % (uintptr_t)x.pitch), d = b >= a || off == 0 ? off : x.pitch - off;
+  return d < x.width || d + y.width > x.pitch;
+}
 // 16-bit rank-3 tensor (dims and box innermost first, strides of the outer dims in bytes), 128-byte swizzle.
 bool encode_tmap_bf16_3d(CUtensorMap* tm, const void* ptr, const unsigned long long (&dims)[3], const unsigned long long (&strides)[2],
                          const unsigned (&box)[3]);

@@ -470,6 +470,16 @@ jf_status packed_check(const jf_packed* t, int dtype, int Hq, int Hkv, int hd) {
 bool packed_rows_ok(const void* p, long long ld, long long width, int dtype) {
   return p && ((uintptr_t)p & (dtype == JF_BF16 ? 1 : 3)) == 0 && ld >= width;
 }
+// Whether an output shares memory with an input or another output: the kernels read and write in no fixed order.
+bool packed_overlap(const RowSpan* in, int n_in, const RowSpan* out, int n_out, int rows) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j)
+      if (rows_overlap(in[j], out[i], rows)) return true;
+    for (int j = 0; j < i; ++j)
+      if (rows_overlap(out[j], out[i], rows)) return true;
+  }
+  return false;
+}
 
 }  // namespace
 }  // namespace jf
@@ -496,8 +506,12 @@ extern "C" jf_status jf_op_packed_attention(const jf_packed* texts, int dtype, c
   if (texts->n_rows == 0) return JF_OK;
   const long long wq = (long long)n_heads * head_dim, wkv = (long long)n_kv_heads * head_dim;
   if (!packed_rows_ok(q, ld_q, wq, dtype) || !packed_rows_ok(k, ld_k, wkv, dtype) || !packed_rows_ok(v, ld_v, wkv, dtype) || !out ||
-      ((uintptr_t)out & 15) || ((uintptr_t)workspace & 15))
+      ((uintptr_t)out & 15) || ((uintptr_t)lse & 3) || ((uintptr_t)workspace & 15))
     return JF_EINVAL;
+  const int size = dtype == JF_BF16 ? 2 : 4;
+  const RowSpan in[] = {{q, ld_q * size, wq * size}, {k, ld_k * size, wkv * size}, {v, ld_v * size, wkv * size}};
+  const RowSpan to[] = {{out, wq * size, wq * size}, {lse, n_heads * 4, n_heads * 4}};
+  if (packed_overlap(in, 3, to, 2, texts->n_rows)) return JF_EINVAL;
   size_t need = 0;
   s = jf_op_packed_attention_workspace_bytes(texts, dtype, n_heads, n_kv_heads, head_dim, 0, &need);
   if (s != JF_OK) return s;
@@ -527,8 +541,13 @@ extern "C" jf_status jf_op_packed_attention_grad(const jf_packed* texts, int dty
   const long long wq = (long long)n_heads * head_dim, wkv = (long long)n_kv_heads * head_dim;
   if (!packed_rows_ok(q, ld_q, wq, dtype) || !packed_rows_ok(k, ld_k, wkv, dtype) || !packed_rows_ok(v, ld_v, wkv, dtype) ||
       !packed_rows_ok(d_out, ld_do, wq, dtype) || !packed_rows_ok(dq, ld_dq, wq, dtype) || !packed_rows_ok(dk, ld_dk, wkv, dtype) ||
-      !packed_rows_ok(dv, ld_dv, wkv, dtype) || !out || ((uintptr_t)out & 15) || !lse || ((uintptr_t)workspace & 15))
+      !packed_rows_ok(dv, ld_dv, wkv, dtype) || !out || ((uintptr_t)out & 15) || !lse || ((uintptr_t)lse & 3) || ((uintptr_t)workspace & 15))
     return JF_EINVAL;
+  const int size = dtype == JF_BF16 ? 2 : 4;
+  const RowSpan in[] = {{q, ld_q * size, wq * size},    {k, ld_k * size, wkv * size},      {v, ld_v * size, wkv * size},
+                        {out, wq * size, wq * size},    {lse, n_heads * 4, n_heads * 4},   {d_out, ld_do * size, wq * size}};
+  const RowSpan to[] = {{dq, ld_dq * size, wq * size}, {dk, ld_dk * size, wkv * size}, {dv, ld_dv * size, wkv * size}};
+  if (packed_overlap(in, 6, to, 3, texts->n_rows)) return JF_EINVAL;
   size_t need = 0;
   s = jf_op_packed_attention_workspace_bytes(texts, dtype, n_heads, n_kv_heads, head_dim, 1, &need);
   if (s != JF_OK) return s;

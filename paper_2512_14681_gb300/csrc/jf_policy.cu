@@ -542,7 +542,11 @@ extern "C" jf_status jf_op_policy_loss(const jf_policy_terms* terms, int dtype, 
   if (rows == 0) return JF_OK;
   const uintptr_t type_mask = dtype == JF_BF16 ? 1 : 3;
   if (!logits || ((uintptr_t)logits & type_mask) || !targets || !advantage) return JF_EINVAL;
-  if (grad_logits && (ld_grad < vocab || ((uintptr_t)grad_logits & type_mask) || (grad_logits == logits && ld_grad != ld))) return JF_EINVAL;
+  if (grad_logits && (ld_grad < vocab || ((uintptr_t)grad_logits & type_mask))) return JF_EINVAL;
+  const int size = dtype == JF_BF16 ? 2 : 4;  // (a gradient in its logit's place is written after it was read, any other is not)
+  if (grad_logits && (grad_logits != logits || ld_grad != ld) &&
+      rows_overlap({logits, ld * size, (long long)vocab * size}, {grad_logits, ld_grad * size, (long long)vocab * size}, rows))
+    return JF_EINVAL;
   size_t need = 0;
   jf_status s = jf_op_policy_loss_workspace_bytes(dtype, rows, vocab, &need);
   if (s != JF_OK) return s;
