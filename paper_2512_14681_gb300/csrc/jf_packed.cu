@@ -14,32 +14,35 @@
 namespace jf {
 namespace {
 
-// Rows that a CTA owns (of queries, or of keys in dk and dv) and rows of the other kind that it takes at a time. 16 x 16 threads. (With 64
-// owned rows the longest text's last tile is twice as long a chain: 777 rows among others, 4 heads of 64, 76 us instead of 70; 63 with the next step's rows asked for ahead.)
-constexpr int PF_OWN = 32, PF_T = 64, PF_THREADS = 256;
+// Rows that a CTA owns (of queries, or of keys in dk and dv) and rows of the other kind that it takes at a time.
+//
+// What bounds a step is the shared memory that feeds the FMAs: a 16-byte load of a warp takes 2 to 4 wavefronts, so what counts is
+// how many products a loaded value gets. 16 x 8 threads have 4 x 4 scores each, 8 loads to 64 FMAs; with 16 x 16 of 2 x 4, 6 to 32, and
+// the next step's rows in registers instead of more CTAs on an SM, 777 rows among others (4 heads of 64) took 73 us instead of 60.
+//
+// What bounds a small batch is the longest text's last tile, a chain of all its keys. Clusters of up to PF_PARTS CTAs share a tile's
+// steps where the grid has fewer than PF_CTAS CTAs, and add up through their shared memory. fp32, CTAs of a cluster 1, 2, 4, 8:
+//   forward, 777 rows among others, 4 heads of 64: 60, 45, 33, 33 us; 8 texts of 200 rows, 12 heads of 128 (grid of 672): 72, 90, 89, 90
+//   backward, 301 rows among others, 4 heads of 64: 128, 71, 48, 46 us; 1,000 rows, 12 heads of 128: 1,216, 718, 471, 538
+constexpr int PF_OWN = 32, PF_T = 64, PF_THREADS = 128;
+constexpr int PF_Y = PF_THREADS / 16, PF_R = PF_OWN / PF_Y;  // threads along a tile's rows, owned rows of one
+constexpr int PF_PARTS = 4, PF_CTAS = 608;
 
-// Values of `rows` rows from p on (row `ld` apart, HD long): asked for, and then as fp32 rows of HD + 4 in shared memory, where rows up
-// to ALL are zeros. (Rows that 16-byte loads cannot read are read when they are put.)
+// Values of `rows` rows from p on (row `ld` apart, HD long) as fp32 rows of HD + 4 in shared memory, where rows up to ALL are zeros.
 template <typename T, int HD, int ALL>
-struct PfRows {
-  static constexpr int N = 16 / sizeof(T), C = HD / N, IT = ALL * C / PF_THREADS;
-  const T* p;
-  long long ld;
-  int rows;
-  bool by16;
-  uint4 w[IT];
-  JF_DEV void ask(const T* p_, long long ld_, int rows_, bool by16_) {
-    p = p_, ld = ld_, rows = rows_, by16 = by16_;
+JF_DEV void pf_load(float* dst, const T* p, long long ld, int rows, bool by16) {
+  constexpr int N = 16 / sizeof(T), C = HD / N, IT = ALL * C / PF_THREADS, AT = IT < 8 ? IT : 8;  // 8 loads in flight
+#pragma unroll 1
+  for (int k0 = 0; k0 < IT; k0 += AT) {
+    uint4 w[AT];
 #pragma unroll
-    for (int k = 0; k < IT; ++k) {
-      const int i = threadIdx.x + k * PF_THREADS, r = i / C, c = i % C * N;
+    for (int k = 0; k < AT; ++k) {
+      const int i = threadIdx.x + (k0 + k) * PF_THREADS, r = i / C, c = i % C * N;
       w[k] = by16 && r < rows ? *reinterpret_cast<const uint4*>(p + r * ld + c) : make_uint4(0u, 0u, 0u, 0u);
     }
-  }
-  JF_DEV void put(float* dst) const {
 #pragma unroll
-    for (int k = 0; k < IT; ++k) {
-      const int i = threadIdx.x + k * PF_THREADS, r = i / C, c = i % C * N;
+    for (int k = 0; k < AT; ++k) {
+      const int i = threadIdx.x + (k0 + k) * PF_THREADS, r = i / C, c = i % C * N;
       float x[N];
       const T* t = reinterpret_cast<const T*>(&w[k]);
 #pragma unroll
@@ -52,15 +55,9 @@ struct PfRows {
       for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(dst + r * (HD + 4) + c + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
     }
   }
-};
-template <typename T, int HD, int ALL>
-JF_DEV void pf_load(float* dst, const T* p, long long ld, int rows, bool by16) {
-  PfRows<T, HD, ALL> x;
-  x.ask(p, ld, rows, by16);
-  x.put(dst);
 }
 
-// s[i][j] = a row (ty + 16 i) . b row (tx + 16 j)
+// s[i][j] = a row (ty + PF_Y i) . b row (tx + 16 j)
 template <int HD, int I, int J>
 JF_DEV void pf_dots(const float* a, const float* b, int ty, int tx, float (&s)[I][J]) {
 #pragma unroll
@@ -71,7 +68,7 @@ JF_DEV void pf_dots(const float* a, const float* b, int ty, int tx, float (&s)[I
   for (int d = 0; d < HD; d += 4) {
     float4 x[I], y[J];
 #pragma unroll
-    for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * (HD + 4) + d);
+    for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4*>(a + (ty + PF_Y * i) * (HD + 4) + d);
 #pragma unroll
     for (int j = 0; j < J; ++j) y[j] = *reinterpret_cast<const float4*>(b + (tx + 16 * j) * (HD + 4) + d);
 #pragma unroll
@@ -82,14 +79,14 @@ JF_DEV void pf_dots(const float* a, const float* b, int ty, int tx, float (&s)[I
   }
 }
 
-// o[i][.] += sum_c w[ty + 16 i][c] b[c][dims 4 tx + 64 j ..] over PF_T columns c, w in rows of PF_T + 4
+// o[i][.] += sum_c w[ty + PF_Y i][c] b[c][dims 4 tx + 64 j ..] over PF_T columns c, w in rows of PF_T + 4
 template <int HD, int I>
 JF_DEV void pf_rows_by(const float* w, const float* b, int ty, int tx, float (&o)[I][HD / 16]) {
 #pragma unroll 2
   for (int c = 0; c < PF_T; c += 4) {
     float4 x[I];
 #pragma unroll
-    for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4*>(w + (ty + 16 * i) * (PF_T + 4) + c);
+    for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4*>(w + (ty + PF_Y * i) * (PF_T + 4) + c);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -107,19 +104,24 @@ JF_DEV void pf_rows_by(const float* w, const float* b, int ty, int tx, float (&o
   }
 }
 
-// o[i][.] += sum_r w[r][2 ty + i] b[r][dims 4 tx + 64 j ..] over PF_T rows r, w in rows of PF_OWN + 4
+// o[i][.] += sum_r w[r][PF_R ty + i] b[r][dims 4 tx + 64 j ..] over PF_T rows r, w in rows of PF_OWN + 4
 template <int HD>
-JF_DEV void pf_columns_by(const float* w, const float* b, int ty, int tx, float (&o)[2][HD / 16]) {
+JF_DEV void pf_columns_by(const float* w, const float* b, int ty, int tx, float (&o)[PF_R][HD / 16]) {
+  static_assert(PF_R == 4);
 #pragma unroll 4
   for (int r = 0; r < PF_T; ++r) {
-    const float2 f = *reinterpret_cast<const float2*>(w + r * (PF_OWN + 4) + 2 * ty);
+    const float4 f4 = *reinterpret_cast<const float4*>(w + r * (PF_OWN + 4) + 4 * ty);
+    const float f[4] = {f4.x, f4.y, f4.z, f4.w};
 #pragma unroll
     for (int j = 0; j < HD / 64; ++j) {
       const float4 y = *reinterpret_cast<const float4*>(b + r * (HD + 4) + 4 * tx + 64 * j);
-      o[0][4 * j] = fmaf(f.x, y.x, o[0][4 * j]), o[1][4 * j] = fmaf(f.y, y.x, o[1][4 * j]);
-      o[0][4 * j + 1] = fmaf(f.x, y.y, o[0][4 * j + 1]), o[1][4 * j + 1] = fmaf(f.y, y.y, o[1][4 * j + 1]);
-      o[0][4 * j + 2] = fmaf(f.x, y.z, o[0][4 * j + 2]), o[1][4 * j + 2] = fmaf(f.y, y.z, o[1][4 * j + 2]);
-      o[0][4 * j + 3] = fmaf(f.x, y.w, o[0][4 * j + 3]), o[1][4 * j + 3] = fmaf(f.y, y.w, o[1][4 * j + 3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        o[i][4 * j] = fmaf(f[i], y.x, o[i][4 * j]);
+        o[i][4 * j + 1] = fmaf(f[i], y.y, o[i][4 * j + 1]);
+        o[i][4 * j + 2] = fmaf(f[i], y.z, o[i][4 * j + 2]);
+        o[i][4 * j + 3] = fmaf(f[i], y.w, o[i][4 * j + 3]);
+      }
     }
   }
 }
@@ -132,10 +134,10 @@ JF_DEV void pf_store4(T* p, float a, float b, float c, float d) {
 struct PfTile {
   int row0, n, first;  // the text's first row and length; the tile's first row in it. n < 0: no tile
 };
-// The tile that CTA x of the grid has: text by text, PF_OWN rows each. Rows that belong to no text are cleared by `clear(row)`
-// on the way, each by one CTA of the grid.
+// Tile x: text by text, PF_OWN rows each. Rows that belong to no text are cleared by `clear(row)` on the way, each by one CTA of
+// the grid.
 template <typename Clear>
-JF_DEV PfTile pf_tile(const PackedParams& a, Clear clear) {
+JF_DEV PfTile pf_tile(const PackedParams& a, int x, Clear clear) {
   __shared__ int s_at[kPackedMaxSeqs], s_bad, s_found;
   if (threadIdx.x == 0) s_bad = 0, s_found = -1;
   __syncthreads();
@@ -159,9 +161,9 @@ JF_DEV PfTile pf_tile(const PackedParams& a, Clear clear) {
         if ((int)threadIdx.x >= sh) sum += u;
       }
       const int before = base + sum - n;
-      if ((int)blockIdx.x >= before && (int)blockIdx.x < before + n) {
+      if (x >= before && x < before + n) {
         s_found = b;
-        s_at[b] = blockIdx.x - before;
+        s_at[b] = x - before;
       }
       base += __shfl_sync(0xffffffffu, sum, 31);
     }
@@ -181,9 +183,37 @@ JF_DEV bool pf_by16(const void* p, long long ld) {
   return ((uintptr_t)p & 15) == 0 && ld % (16 / (int)sizeof(T)) == 0;
 }
 
-// Grid (tiles, query heads).
+// The CTAs of a cluster share a tile: each takes every parts'th step, and joins some of the owned rows of all from their shared
+// memory, in their order.
+JF_DEV void pf_join_begin(int parts) {
+  if (parts > 1) cluster_sync();
+  else __syncthreads();
+}
+JF_DEV void pf_join_end(int parts) {
+  if (parts > 1) cluster_sync();  // peers may still read this CTA's rows
+}
+// What a thread has of its owned rows, r0 + apart i, to rows of HD in shared memory.
+template <int HD>
+JF_DEV void pf_put(float* s, int r0, int apart, int tx, const float (&o)[PF_R][HD / 16]) {
+#pragma unroll
+  for (int i = 0; i < PF_R; ++i)
+#pragma unroll
+    for (int j = 0; j < HD / 64; ++j)
+      *reinterpret_cast<float4*>(s + (r0 + apart * i) * HD + 4 * tx + 64 * j) = make_float4(o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]);
+}
+// The sum over the cluster of four values at byte `at` of those rows.
+JF_DEV float4 pf_sum4(const float* s, int at, int parts) {
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k = 0; k < parts; ++k) {
+    const float4 v = ld_cluster4(map_to_rank(smem_u32(s), k) + at);
+    o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+  }
+  return o;
+}
+
+// Grid (tiles x parts, query heads).
 template <typename T, int HD>
-__global__ void __launch_bounds__(PF_THREADS, 2) k_packed_attn(const PackedParams a) {
+__global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 4 : 2) k_packed_attn(const PackedParams a) {
   extern __shared__ float sm[];
   constexpr int TILE = PF_T * (HD + 4), OWN = PF_OWN * (HD + 4);
   float *sq = sm, *sk = sm + OWN, *sv = sk + TILE, *sp = sv + TILE;
@@ -191,7 +221,8 @@ __global__ void __launch_bounds__(PF_THREADS, 2) k_packed_attn(const PackedParam
   pdl_launch_dependents();
   pdl_wait();
   T* out = reinterpret_cast<T*>(a.out);
-  const PfTile t = pf_tile(a, [&](int r) {
+  const int parts = (int)cluster_ctas(), part = (int)cluster_rank();
+  const PfTile t = pf_tile(a, blockIdx.x / parts, [&](int r) {
     for (int d = tid; d < HD; d += PF_THREADS) out[((long long)r * a.Hq + h) * HD + d] = to_act<T>(0.f);
     if (tid == 0 && a.lse) a.lse[(long long)r * a.Hq + h] = -INFINITY;
   });
@@ -199,27 +230,20 @@ __global__ void __launch_bounds__(PF_THREADS, 2) k_packed_attn(const PackedParam
   const int rows = min(PF_OWN, t.n - t.first);
   const bool q16 = pf_by16<T>(a.q, a.ld_q), k16 = pf_by16<T>(a.k, a.ld_k), v16 = pf_by16<T>(a.v, a.ld_v);
   pf_load<T, HD, PF_OWN>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + t.first) * a.ld_q + h * HD, a.ld_q, rows, q16);
-  float m[2], l[2], o[2][HD / 16] = {};
+  float m[PF_R], l[PF_R], o[PF_R][HD / 16] = {};
 #pragma unroll
-  for (int i = 0; i < 2; ++i) m[i] = -INFINITY, l[i] = 0.f;
+  for (int i = 0; i < PF_R; ++i) m[i] = -INFINITY, l[i] = 0.f;
   const float c = a.scale * kLog2e;
-  PfRows<T, HD, PF_T> rk, rv;  // the next step's are on their way while one is worked on
-  auto ask = [&](int k0) {
-    rk.ask(reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
-    rv.ask(reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
-  };
-  ask(0);
-  for (int k0 = 0; k0 < t.first + rows; k0 += PF_T) {
+  for (int k0 = part * PF_T; k0 < t.first + rows; k0 += parts * PF_T) {
     __syncthreads();
-    rk.put(sk);
-    rv.put(sv);
-    if (k0 + PF_T < t.first + rows) ask(k0 + PF_T);
+    pf_load<T, HD, PF_T>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
+    pf_load<T, HD, PF_T>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
     __syncthreads();
-    float s[2][4];
+    float s[PF_R][4];
     pf_dots<HD>(sq, sk, ty, tx, s);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int qi = t.first + ty + 16 * i;
+    for (int i = 0; i < PF_R; ++i) {
+      const int qi = t.first + ty + PF_Y * i;
       float mx = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -235,7 +259,7 @@ __global__ void __launch_bounds__(PF_THREADS, 2) k_packed_attn(const PackedParam
       for (int j = 0; j < 4; ++j) {
         s[i][j] = exp2f(s[i][j] - base);
         sum += s[i][j];
-        sp[(ty + 16 * i) * (PF_T + 4) + tx + 16 * j] = s[i][j];
+        sp[(ty + PF_Y * i) * (PF_T + 4) + tx + 16 * j] = s[i][j];
       }
 #pragma unroll
       for (int sh = 8; sh; sh >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
@@ -247,17 +271,36 @@ __global__ void __launch_bounds__(PF_THREADS, 2) k_packed_attn(const PackedParam
     __syncthreads();
     pf_rows_by<HD>(sp, sv, ty, tx, o);
   }
+  __syncthreads();
+  float *so = sk, *s_m = so + PF_OWN * HD, *s_l = s_m + PF_OWN;  // sums, maxima, sums of exponentials
+  pf_put<HD>(so, ty, PF_Y, tx, o);
+  if (tx == 0) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = ty + 16 * i;
-    if (r >= rows) continue;
-    const long long at = (long long)(t.row0 + t.first + r) * a.Hq + h;
-    const float il = l[i] > 0.f ? 1.f / l[i] : (l[i] == 0.f ? 0.f : l[i]);
-#pragma unroll
-    for (int j = 0; j < HD / 64; ++j)
-      pf_store4<T>(out + at * HD + 4 * tx + 64 * j, o[i][4 * j] * il, o[i][4 * j + 1] * il, o[i][4 * j + 2] * il, o[i][4 * j + 3] * il);
-    if (tx == 0 && a.lse) a.lse[at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
+    for (int i = 0; i < PF_R; ++i) s_m[ty + PF_Y * i] = m[i], s_l[ty + PF_Y * i] = l[i];
   }
+  pf_join_begin(parts);
+  const int mine = PF_OWN / parts;
+  for (int i = tid; i < mine * (HD / 4); i += PF_THREADS) {
+    const int r = part * mine + i / (HD / 4), d = i % (HD / 4) * 4;
+    if (r >= rows) continue;
+    float M = -INFINITY, L = 0.f;
+    float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < parts; ++k) {
+      const uint32_t from = map_to_rank(smem_u32(so), k);
+      const float mk = ld_cluster(from + (PF_OWN * HD + r) * 4), lk = ld_cluster(from + (PF_OWN * HD + PF_OWN + r) * 4);
+      const float4 v = ld_cluster4(from + (r * HD + d) * 4);
+      if (lk == 0.f) continue;  // (it saw nothing)
+      const float top = fmaxf(M, mk), f0 = M == top ? 1.f : exp2f(M - top), f1 = mk == top ? 1.f : exp2f(mk - top);
+      M = top;
+      L = f0 * L + f1 * lk;
+      w.x = f0 * w.x + f1 * v.x, w.y = f0 * w.y + f1 * v.y, w.z = f0 * w.z + f1 * v.z, w.w = f0 * w.w + f1 * v.w;
+    }
+    const long long at = (long long)(t.row0 + t.first + r) * a.Hq + h;
+    const float il = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);
+    pf_store4<T>(out + at * HD + d, w.x * il, w.y * il, w.z * il, w.w * il);
+    if (d == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+  }
+  pf_join_end(parts);
 }
 
 // delta[row][head] = d_out . out, a warp per (row, head); rows of no text as well (their d_out may be anything: not used).
@@ -288,7 +331,7 @@ JF_DEV void pf_back_tile(const float* sq, const float* sdo, const float* sk, con
   pf_dots<HD>(sdo, sv, ty, tx, dp);
 #pragma unroll
   for (int i = 0; i < I; ++i) {
-    const int r = ty + 16 * i;
+    const int r = ty + PF_Y * i;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       const int kj = k0 + tx + 16 * j;
@@ -300,9 +343,9 @@ JF_DEV void pf_back_tile(const float* sq, const float* sdo, const float* sk, con
   }
 }
 
-// Grid (tiles of keys, KV heads): dk and dv.
+// Grid (tiles of keys x parts, KV heads): dk and dv.
 template <typename T, int HD>
-__global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dkv(const PackedParams a) {
+__global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 2 : 1) k_packed_dkv(const PackedParams a) {
   extern __shared__ float sm[];
   constexpr int TILE = PF_T * (HD + 4), OWN = PF_OWN * (HD + 4);
   float *sq = sm, *sdo = sm + TILE, *sk = sm + 2 * TILE, *sv = sk + OWN, *sp = sv + OWN, *sds = sp + PF_T * (PF_OWN + 4);
@@ -311,7 +354,8 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dkv(const PackedParams
   pdl_launch_dependents();
   pdl_wait();
   T *dk = reinterpret_cast<T*>(a.dk), *dv = reinterpret_cast<T*>(a.dv);
-  const PfTile t = pf_tile(a, [&](int r) {
+  const int parts = (int)cluster_ctas(), part = (int)cluster_rank();
+  const PfTile t = pf_tile(a, blockIdx.x / parts, [&](int r) {
     for (int d = tid; d < HD; d += PF_THREADS) dk[r * a.ld_dk + kvh * HD + d] = dv[r * a.ld_dv + kvh * HD + d] = to_act<T>(0.f);
   });
   if (t.n < 0) return;
@@ -319,50 +363,42 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dkv(const PackedParams
   pf_load<T, HD, PF_OWN>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + t.first) * a.ld_k + kvh * HD, a.ld_k, rows, pf_by16<T>(a.k, a.ld_k));
   pf_load<T, HD, PF_OWN>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + t.first) * a.ld_v + kvh * HD, a.ld_v, rows, pf_by16<T>(a.v, a.ld_v));
   const bool q16 = pf_by16<T>(a.q, a.ld_q), do16 = pf_by16<T>(a.d_out, a.ld_do);
-  float gk[2][HD / 16] = {}, gv[2][HD / 16] = {};
-  PfRows<T, HD, PF_T> rq, rd;  // the next step's are on their way while one is worked on
-  float lse = 0.f, delta = 0.f;
-  auto ask = [&](int h, int q0) {
-    const int nq = min(PF_T, t.n - q0);
-    rq.ask(reinterpret_cast<const T*>(a.q) + (t.row0 + q0) * a.ld_q + h * HD, a.ld_q, nq, q16);
-    rd.ask(reinterpret_cast<const T*>(a.d_out) + (t.row0 + q0) * a.ld_do + h * HD, a.ld_do, nq, do16);
+  float gk[PF_R][HD / 16] = {}, gv[PF_R][HD / 16] = {};
+  const int tiles = (t.n - t.first + PF_T - 1) / PF_T, steps = G * tiles;  // (head by head)
+  for (int step = part; step < steps; step += parts) {
+    const int h = kvh * G + step / tiles, q0 = t.first + step % tiles * PF_T, nq = min(PF_T, t.n - q0);
+    __syncthreads();
+    pf_load<T, HD, PF_T>(sq, reinterpret_cast<const T*>(a.q) + (t.row0 + q0) * a.ld_q + h * HD, a.ld_q, nq, q16);
+    pf_load<T, HD, PF_T>(sdo, reinterpret_cast<const T*>(a.d_out) + (t.row0 + q0) * a.ld_do + h * HD, a.ld_do, nq, do16);
     if (tid < nq) {
-      lse = a.lse[(long long)(t.row0 + q0 + tid) * a.Hq + h] * kLog2e;
-      delta = a.delta[(long long)(t.row0 + q0 + tid) * a.Hq + h];
+      s_lse[tid] = a.lse[(long long)(t.row0 + q0 + tid) * a.Hq + h] * kLog2e;
+      s_delta[tid] = a.delta[(long long)(t.row0 + q0 + tid) * a.Hq + h];
     }
-  };
-  ask(kvh * G, t.first);
-  for (int h = kvh * G, q0 = t.first; h < (kvh + 1) * G;) {
     __syncthreads();
-    rq.put(sq);
-    rd.put(sdo);
-    if (tid < PF_T) s_lse[tid] = lse, s_delta[tid] = delta;
-    const int at = q0;
-    if ((q0 += PF_T) >= t.n) q0 = t.first, ++h;
-    if (h < (kvh + 1) * G) ask(h, q0);
-    __syncthreads();
-    pf_back_tile<HD, PF_T / 16, PF_OWN / 16>(sq, sdo, sk, sv, s_lse, s_delta, at, t.first, t.n, a.scale * kLog2e, ty, tx, sp, sds);
+    pf_back_tile<HD, PF_T / PF_Y, PF_OWN / 16>(sq, sdo, sk, sv, s_lse, s_delta, q0, t.first, t.n, a.scale * kLog2e, ty, tx, sp, sds);
     __syncthreads();
     pf_columns_by<HD>(sp, sdo, ty, tx, gv);
     pf_columns_by<HD>(sds, sq, ty, tx, gk);
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = 2 * ty + i;
+  __syncthreads();
+  pf_put<HD>(sq, PF_R * ty, 1, tx, gk);
+  pf_put<HD>(sdo, PF_R * ty, 1, tx, gv);
+  pf_join_begin(parts);
+  const int mine = PF_OWN / parts;
+  for (int i = tid; i < mine * (HD / 4); i += PF_THREADS) {
+    const int r = part * mine + i / (HD / 4), d = i % (HD / 4) * 4;
     if (r >= rows) continue;
     const long long at = t.row0 + t.first + r;
-#pragma unroll
-    for (int j = 0; j < HD / 64; ++j) {
-      const int d = kvh * HD + 4 * tx + 64 * j;
-      pf_store4<T>(dk + at * a.ld_dk + d, a.scale * gk[i][4 * j], a.scale * gk[i][4 * j + 1], a.scale * gk[i][4 * j + 2], a.scale * gk[i][4 * j + 3]);
-      pf_store4<T>(dv + at * a.ld_dv + d, gv[i][4 * j], gv[i][4 * j + 1], gv[i][4 * j + 2], gv[i][4 * j + 3]);
-    }
+    const float4 x = pf_sum4(sq, (r * HD + d) * 4, parts), y = pf_sum4(sdo, (r * HD + d) * 4, parts);
+    pf_store4<T>(dk + at * a.ld_dk + kvh * HD + d, a.scale * x.x, a.scale * x.y, a.scale * x.z, a.scale * x.w);
+    pf_store4<T>(dv + at * a.ld_dv + kvh * HD + d, y.x, y.y, y.z, y.w);
   }
+  pf_join_end(parts);
 }
 
-// Grid (tiles of queries, query heads): dq.
+// Grid (tiles of queries x parts, query heads): dq.
 template <typename T, int HD>
-__global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dq(const PackedParams a) {
+__global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 2 : 1) k_packed_dq(const PackedParams a) {
   extern __shared__ float sm[];
   constexpr int TILE = PF_T * (HD + 4), OWN = PF_OWN * (HD + 4);
   float *sq = sm, *sdo = sm + OWN, *sk = sm + 2 * OWN, *sv = sk + TILE, *sds = sv + TILE;
@@ -371,7 +407,8 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dq(const PackedParams 
   pdl_launch_dependents();
   pdl_wait();
   T* dq = reinterpret_cast<T*>(a.dq);
-  const PfTile t = pf_tile(a, [&](int r) {
+  const int parts = (int)cluster_ctas(), part = (int)cluster_rank();
+  const PfTile t = pf_tile(a, blockIdx.x / parts, [&](int r) {
     for (int d = tid; d < HD; d += PF_THREADS) dq[r * a.ld_dq + h * HD + d] = to_act<T>(0.f);
   });
   if (t.n < 0) return;
@@ -383,32 +420,27 @@ __global__ void __launch_bounds__(PF_THREADS, 1) k_packed_dq(const PackedParams 
     s_delta[tid] = a.delta[(long long)(t.row0 + t.first + tid) * a.Hq + h];
   }
   const bool k16 = pf_by16<T>(a.k, a.ld_k), v16 = pf_by16<T>(a.v, a.ld_v);
-  float g[2][HD / 16] = {};
-  PfRows<T, HD, PF_T> rk, rv;  // the next step's are on their way while one is worked on
-  auto ask = [&](int k0) {
-    rk.ask(reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
-    rv.ask(reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
-  };
-  ask(0);
-  for (int k0 = 0; k0 < t.first + rows; k0 += PF_T) {
+  float g[PF_R][HD / 16] = {};
+  for (int k0 = part * PF_T; k0 < t.first + rows; k0 += parts * PF_T) {
     __syncthreads();
-    rk.put(sk);
-    rv.put(sv);
-    if (k0 + PF_T < t.first + rows) ask(k0 + PF_T);
+    pf_load<T, HD, PF_T>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
+    pf_load<T, HD, PF_T>(sv, reinterpret_cast<const T*>(a.v) + (t.row0 + k0) * a.ld_v + kvh * HD, a.ld_v, min(PF_T, t.n - k0), v16);
     __syncthreads();
-    pf_back_tile<HD, PF_OWN / 16, PF_T / 16>(sq, sdo, sk, sv, s_lse, s_delta, t.first, k0, t.n, a.scale * kLog2e, ty, tx, nullptr, sds);
+    pf_back_tile<HD, PF_R, PF_T / 16>(sq, sdo, sk, sv, s_lse, s_delta, t.first, k0, t.n, a.scale * kLog2e, ty, tx, nullptr, sds);
     __syncthreads();
     pf_rows_by<HD>(sds, sk, ty, tx, g);
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = ty + 16 * i;
+  __syncthreads();
+  pf_put<HD>(sk, ty, PF_Y, tx, g);
+  pf_join_begin(parts);
+  const int mine = PF_OWN / parts;
+  for (int i = tid; i < mine * (HD / 4); i += PF_THREADS) {
+    const int r = part * mine + i / (HD / 4), d = i % (HD / 4) * 4;
     if (r >= rows) continue;
-#pragma unroll
-    for (int j = 0; j < HD / 64; ++j)
-      pf_store4<T>(dq + (t.row0 + t.first + r) * a.ld_dq + h * HD + 4 * tx + 64 * j, a.scale * g[i][4 * j], a.scale * g[i][4 * j + 1],
-                   a.scale * g[i][4 * j + 2], a.scale * g[i][4 * j + 3]);
+    const float4 x = pf_sum4(sk, (r * HD + d) * 4, parts);
+    pf_store4<T>(dq + (t.row0 + t.first + r) * a.ld_dq + h * HD + d, a.scale * x.x, a.scale * x.y, a.scale * x.z, a.scale * x.w);
   }
+  pf_join_end(parts);
 }
 
 // Shared memory of owned tiles, other tiles, and floats beside them.
@@ -444,16 +476,26 @@ bool pf_ready() {
 
 unsigned pf_tiles(const jf_packed& t) { return (unsigned)((t.n_rows + PF_OWN - 1) / PF_OWN + t.n_seqs); }
 
+// CTAs of a cluster, for a grid of `rows` rows of tiles whose longest chain is `steps`.
+int pf_parts(const jf_packed& t, int rows, long long steps) {
+  int parts = 1;
+  while (parts < PF_PARTS && steps > parts && (long long)pf_tiles(t) * rows * parts < PF_CTAS) parts *= 2;
+  return parts;
+}
+long long pf_steps(const jf_packed& t) { return (t.max_rows + PF_T - 1) / PF_T; }
+
 template <typename T, int HD>
 cudaError_t pf_forward(const PackedParams& a, cudaStream_t st) {
-  return packed_launch(k_packed_attn<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem_attn<HD>, st, a);
+  const int parts = pf_parts(a.t, a.Hq, pf_steps(a.t));
+  return packed_launch_clusters(k_packed_attn<T, HD>, parts, dim3(pf_tiles(a.t) * parts, a.Hq), dim3(PF_THREADS), pf_smem_attn<HD>, st, a);
 }
 template <typename T, int HD>
 cudaError_t pf_backward(const PackedParams& a, cudaStream_t st) {
   const long long warps = (long long)a.t.n_rows * a.Hq;
+  const int kv = pf_parts(a.t, a.Hkv, pf_steps(a.t) * (a.Hq / a.Hkv)), q = pf_parts(a.t, a.Hq, pf_steps(a.t));
   cudaError_t e = packed_launch(k_packed_delta<T, HD>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a);
-  if (e == cudaSuccess) e = packed_launch(k_packed_dkv<T, HD>, dim3(pf_tiles(a.t), a.Hkv), dim3(PF_THREADS), pf_smem_dkv<HD>, st, a);
-  if (e == cudaSuccess) e = packed_launch(k_packed_dq<T, HD>, dim3(pf_tiles(a.t), a.Hq), dim3(PF_THREADS), pf_smem_dq<HD>, st, a);
+  if (e == cudaSuccess) e = packed_launch_clusters(k_packed_dkv<T, HD>, kv, dim3(pf_tiles(a.t) * kv, a.Hkv), dim3(PF_THREADS), pf_smem_dkv<HD>, st, a);
+  if (e == cudaSuccess) e = packed_launch_clusters(k_packed_dq<T, HD>, q, dim3(pf_tiles(a.t) * q, a.Hq), dim3(PF_THREADS), pf_smem_dq<HD>, st, a);
   return e;
 }
 

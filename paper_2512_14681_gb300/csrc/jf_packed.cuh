@@ -47,19 +47,26 @@ jf_status packed_tc_workspace(const jf_packed& t, int Hq, int Hkv, int hd, bool 
 jf_status packed_tc_forward(const PackedParams& a, int hd, void* workspace, cudaStream_t st);
 jf_status packed_tc_backward(const PackedParams& a, int hd, void* workspace, cudaStream_t st);
 
+// cluster: CTAs of one, along x.
 template <typename K, typename... Args>
-cudaError_t packed_launch(K kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+cudaError_t packed_launch_clusters(K kernel, int cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)cluster, at[1].val.clusterDim.y = 1, at[1].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+template <typename K, typename... Args>
+cudaError_t packed_launch(K kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args... args) {
+  return packed_launch_clusters(kernel, 1, grid, block, smem, st, args...);
 }
 
 }  // namespace jf

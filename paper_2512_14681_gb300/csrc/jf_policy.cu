@@ -96,12 +96,6 @@ JF_DEV LpStat join_lanes(LpStat st, int lanes) {
   }
   return {b, st.s, st.t};
 }
-JF_DEV float ld_cluster(uint32_t a) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-  return v;
-}
-
 // The largest of a vector's values (NaN ignored) and `most`.
 JF_DEV float largest(const uint4& v, float most, float) {
   return fmaxf(fmaxf(most, fmaxf(__uint_as_float(v.x), __uint_as_float(v.y))), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
@@ -198,8 +192,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
   pdl_launch_dependents();
   pdl_wait();
   __syncthreads();
-  uint32_t parts;
-  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+  const uint32_t parts = cluster_ctas();
   const int rank = (int)cluster_rank(), lg = 31 - __clz(parts), rows_apart = gridDim.x >> lg;  // (parts: a power of two)
   const T* logits = reinterpret_cast<const T*>(a.logits);
   const float c = a.scale * LOG2E;
