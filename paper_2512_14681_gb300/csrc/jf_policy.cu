@@ -70,7 +70,7 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 // Logits below -1e30 (and c above 1e6) would leave fp32's range in y: they count as -1e30, whose 2^y is 0, unless the row's
 // largest is such a one itself; its sums then are taken again from differences x - m.
 // ---------------------------------------------------------------------------------------------
-constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8, PL_CHUNKS = 2;
+constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8;
 constexpr int PL_FIT[3] = {56832, 76288, 115200};  // bytes of a CTA's run with which four, three, two are resident on an SM
 constexpr int PL_MOST = PL_FIT[2];
 constexpr int PL_ROWS = 1 << 30;  // (a row and the step to the next fit 31 bits)
@@ -175,18 +175,19 @@ struct PolicyInputs {
   float old, ref, A, w;
 };
 
-// Clusters walk over rows; while a row's gradient leaves, one thread asks for the next row's logits in the places that have been read.
+// Clusters walk over rows. (Asking for the next row's first half while the second half's gradient leaves took 1 to 3% longer: a
+// row is split finely enough that the SM's other CTAs have copies under way.)
 template <typename T>
 __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) {
   constexpr int N = Vec<T>::N;
   extern __shared__ __align__(128) uint4 s_run[];
-  __shared__ __align__(8) uint64_t b_there[PL_CHUNKS];
+  __shared__ __align__(8) uint64_t b_there;
   __shared__ LpStat s_warp[PL_WARPS];
   __shared__ float s_max[PL_WARPS], s_cta[2][4], s_far[2][2];  // by turns (peers read them): the CTA's b, S, T and largest logit; S, T from differences
   __shared__ float s_row[8];                                    // b, log2 S, S, H, g, gh, m, whether far
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < PL_CHUNKS; ++i) mbar_init(smem_u32(&b_there[i]), 1);
+    mbar_init(smem_u32(&b_there), 1);
     fence_mbar_init();
   }
   pdl_launch_dependents();
@@ -196,15 +197,12 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
   const int rank = (int)cluster_rank(), lg = 31 - __clz(parts), rows_apart = gridDim.x >> lg;  // (parts: a power of two)
   const T* logits = reinterpret_cast<const T*>(a.logits);
   const float c = a.scale * LOG2E;
-  // vectors of a chunk: the same for all rows, whose runs may differ by one (a row's next chunk must not reach into the one behind)
-  const int chunk = ((a.V / N + (int)parts - 1 >> lg) + PL_CHUNKS - 1) / PL_CHUNKS;
-  // chunk i of a row's run
-  auto ask = [&](int row, int i) {
+  // a row's run
+  auto ask = [&](int row) {
     const Row<T> r(logits + row * a.ld, a.V);
-    const int v_begin = r.n_vec * rank >> lg, n = (r.n_vec * (rank + 1) >> lg) - v_begin;
-    const int first = min(n, i * chunk), bytes = (min(n, first + chunk) - first) * 16;
-    mbar_arrive_expect_tx(smem_u32(&b_there[i]), (uint32_t)bytes);
-    if (bytes > 0) bulk_load(smem_u32(s_run + first), r.vec(v_begin + first), (uint32_t)bytes, smem_u32(&b_there[i]));
+    const int v_begin = r.n_vec * rank >> lg, bytes = ((r.n_vec * (rank + 1) >> lg) - v_begin) * 16;
+    mbar_arrive_expect_tx(smem_u32(&b_there), (uint32_t)bytes);
+    if (bytes > 0) bulk_load(smem_u32(s_run), r.vec(v_begin), (uint32_t)bytes, smem_u32(&b_there));
   };
   auto inputs = [&](int row) {  // (asked for a row ahead)
     PolicyInputs q = {-1, 0.f, 0.f, 0.f, 0.f};
@@ -218,8 +216,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
     return q;
   };
   int row = blockIdx.x >> lg, turn = 0;
-  if (tid == 0 && row < a.rows)
-    for (int i = 0; i < PL_CHUNKS; ++i) ask(row, i);
+  if (tid == 0 && row < a.rows) ask(row);
   PolicyInputs next = inputs(row);
   for (; row < a.rows; row += rows_apart, turn ^= 1) {
     const Row<T> r(logits + row * a.ld, a.V);
@@ -232,12 +229,9 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
     const float x_t = target >= 0 && target < a.V ? act_to_f32(r.p[target]) : 0.f;  // (before a gradient in its place)
 
     float m = at_edge;
-    for (int i = 0; i < PL_CHUNKS; ++i) {
-      if (!mbar_wait_bounded(smem_u32(&b_there[i]), (uint32_t)turn, kWaitLimitDefaultNs)) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
-      const int end = min(n, (i + 1) * chunk);
+    if (!mbar_wait_bounded(smem_u32(&b_there), (uint32_t)turn, kWaitLimitDefaultNs)) jf_set_error(a.err, JF_DERR_TIMEOUT_TMA);
 #pragma unroll 4
-      for (int v = i * chunk + tid; v < end; v += PL_THREADS) m = largest(s_run[v], m, T{});
-    }
+    for (int v = tid; v < n; v += PL_THREADS) m = largest(s_run[v], m, T{});
     LpStat st;
     {
       const float b = c <= PL_STEEP && fabsf(m) < PL_LARGE ? c * m : -INFINITY;  // (-inf: the thread's sums do not count, or are taken again)
@@ -250,16 +244,12 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
         t = fma_pair(p, y, t);
       };
       // (the vectors that the thread has looked at)
-#pragma unroll 1
-      for (int i = 0; i < PL_CHUNKS; ++i) {
-        const int end = min(n, (i + 1) * chunk);
 #pragma unroll 2
-        for (int v = i * chunk + tid; v < end; v += PL_THREADS) {
-          Pair x[N / 2];
-          raised(s_run[v], x, T{});
+      for (int v = tid; v < n; v += PL_THREADS) {
+        Pair x[N / 2];
+        raised(s_run[v], x, T{});
 #pragma unroll
-          for (int k = 0; k < N / 2; ++k) add(x[k]);
-        }
+        for (int k = 0; k < N / 2; ++k) add(x[k]);
       }
       if (edge) add(pair(max_nan(at_edge, -PL_FAR), -PL_FAR));
       st = {b, halves(s).x + halves(s).y, halves(t).x + halves(t).y};
@@ -352,7 +342,6 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
       }
       __syncthreads();
     }
-    const bool more = row + rows_apart < a.rows;
     const float b = s_row[0], l2 = s_row[1], S = s_row[2], H = s_row[3], g = s_row[4], gh = s_row[5], k = a.scale;
     // -scale / S times (g + gh (H - ln S) + gh ln 2 y)
     const float f = -k / S, share0 = f * fmaf(gh, H - LN2 * l2, g), share1 = f * (gh * LN2), hot = k * g;
@@ -395,32 +384,31 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
       }
       Vec<T>::store(out + i0, d);
     };
-    for (int i = 0; i < PL_CHUNKS; ++i) {
-      const int end = a.grad ? min(n_out, (i + 1) * chunk) : 0;
-      if (still || far) {
-#pragma unroll 1
-        for (int v = i * chunk + tid; v < end; v += PL_THREADS)
-#pragma unroll 1
-          for (int h = 0; h < N; ++h) {
-            const int at = v * N + own + h;
-            single(e0 + at, act_to_f32(reinterpret_cast<const T*>(s_run)[at]));
-          }
-      } else if (gh != 0.f) {
+    const int end = a.grad ? n_out : 0;
+    if (still) {
+      const float zeros[N] = {};
 #pragma unroll 2
-        for (int v = i * chunk + tid; v < end; v += PL_THREADS) vector(v, true);
-      } else {
-#pragma unroll 2
-        for (int v = i * chunk + tid; v < end; v += PL_THREADS) vector(v, false);
-      }
-      if (more) {  // the chunk has been read by all: the next row's takes its place
-        __syncthreads();
-        if (tid == 0) {
-          fence_proxy_async_smem();
-          ask(row + rows_apart, i);
+      for (int v = tid; v < end; v += PL_THREADS) Vec<T>::store(out + e0 + v * N + own, zeros);
+    } else if (far) {
+#pragma unroll 1
+      for (int v = tid; v < end; v += PL_THREADS)
+#pragma unroll 1
+        for (int h = 0; h < N; ++h) {
+          const int at = v * N + own + h;
+          single(e0 + at, act_to_f32(reinterpret_cast<const T*>(s_run)[at]));
         }
-      }
+    } else if (gh != 0.f) {
+#pragma unroll 2
+      for (int v = tid; v < end; v += PL_THREADS) vector(v, true);
+    } else {
+#pragma unroll 2
+      for (int v = tid; v < end; v += PL_THREADS) vector(v, false);
     }
-    __syncthreads();  // (s_row)
+    __syncthreads();  // (s_row; the run has been read by all: the next row's takes its place)
+    if (tid == 0 && row + rows_apart < a.rows) {
+      fence_proxy_async_smem();
+      ask(row + rows_apart);
+    }
   }
   if (parts > 1) cluster_sync();  // peers may still read this CTA's sums
 }
@@ -448,7 +436,7 @@ int policy_parts(int dtype, int rows, int vocab) {
   int parts = 1;
   while (parts < PL_CLUSTER && (vecs + parts - 1) / parts > PL_MOST / 16) parts *= 2;
   if ((vecs + parts - 1) / parts > PL_MOST / 16) return 0;
-  while (parts < PL_CLUSTER && (long long)rows * parts * 2 <= 152 && vecs / parts > 2 * PL_THREADS) parts *= 2;
+  while (parts < PL_CLUSTER && (long long)rows * parts * 2 <= 152 && vecs / parts > 4 * PL_THREADS) parts *= 2;
   return parts;
 }
 
