@@ -5,6 +5,11 @@
 // tokens times G heads (row = token * G + head), loaded as one box of a tensor copy: a short text fills the tensor core's 128
 // rows G times sooner, and K and V are read once for G heads.
 //
+// What bounds a long text is the tensor core, and before it each stream's chain product -> softmax -> product; a short one, latency.
+// Measured with 28 heads of 128 on 4: forward of 16,384 rows 1.315 ms (1.46 PFLOP/s), 4,096 rows 110 us, 16 texts of up to 128 rows
+// (12 heads on 2) 10.6 us; backward of 8,192 rows 1.22 ms (0.985 PFLOP/s of the five products' work; seven are multiplied), 4 x 1,024
+// rows 151 us.
+//
 // Work is a line of units, (text, KV head, tile), each as long as its steps (tiles of keys, or of query rows in dk and dv)
 // plus a constant for what a unit costs beside them; each CTA takes an equal run of that line. A unit that a run's end cuts leaves a
 // partial result a part in the workspace, at most two a CTA, and a kernel behind joins the parts in their order. Short units are
@@ -24,6 +29,8 @@ constexpr int PT_WHOLE = 8;
 // ---------------------------------------------------------------------------------------------
 // The line of units. Kind says how a text is cut: units(n), steps(n, u) for a text of n rows.
 // ---------------------------------------------------------------------------------------------
+// (What a unit costs beside its steps, in steps, times in us: forward of 16,384 rows 1,432, 1,316, 1,342 with 0, 2, 4, a packed batch of 8,246
+// 205, 155, 164; backward of 8,192 rows by dq's 1,287, 1,225, 1,240 with 2, 5, 8, by that of dk and dv 1,251, 1,225, 1,237 with 1, 3, 6.)
 template <int COST>
 struct ByQueries {  // tiles of `tok` tokens over the key tiles that they see; COST: of a unit beside its steps
   static constexpr bool KEYS = false;
@@ -345,11 +352,17 @@ JF_DEV void scale_o(uint32_t t_o, float x) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// Forward. A unit is two tiles of query rows (streams 0 and 1) over the key tiles that they see: while one stream's softmax
+// Forward: one pass over the keys with a row's running maximum m and sum l, out = O / l. p = 2^(s - m) is rounded to bf16 for its product
+// with V (the tensor core takes both operands in one type), l adds the unrounded ones: up to 2^-8 of a key's share, each with a sign of
+// its own, beside out's own rounding of up to 2^-8. m follows its row's scores only where they exceed it by 2^PA_LAG, so that O is
+// seldom scaled; p then is at most 2^8, which costs bf16 nothing (0 instead of 8: 1,593 us for 16,384 rows, 1,328 with).
+//
+// A unit is two tiles of query rows (streams 0 and 1) over the key tiles that they see: while one stream's softmax
 // runs, the tensor core works for the other. Tensor memory: S and O of each stream, P in bf16 in the place of the S it came
 // from. Warps 0-3, 4-7: stream 0, 1, a thread per row; warp 8: copies; 9, 10: the streams' products; 11: values behind a text's end.
 // (Two threads a row, in 16 warps, took 1.4 times as long: they have to agree on the row's maximum at every step, and 96 registers
-// are too few.)
+// are too few.) At 8,192 rows the tensor pipe is active 62% of the time, issue slots 34%: the rest is a stream's own chain, read S,
+// maximum, exponentials, write P, wait for the product, of which two streams hide a half.
 // ---------------------------------------------------------------------------------------------
 constexpr int PA_THREADS = 384;  // 168 registers a thread: a row's 128 scores fit
 constexpr float PA_LAG = 8.f;  // a row's reference maximum follows its scores when they exceed it by more
@@ -483,7 +496,7 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
       int tiles = 0, units = 0, products = 0;  // tiles before the unit, units, P V so far
       auto place_of = [&](int tile) { return __shfl_sync(0xffffffffu, tile % RING, 0); };
       // The streams run best half a step apart, one's softmax beside the other's products, and stay so: the second begins when the
-      // first's first P is there. (Or after 4 us: nothing depends on it.)
+      // first's first P is there. (Or after 4 us: nothing depends on it. Without, 4,096 rows 113 us instead of 110, the packed batch 162 instead of 154.)
       if (s == 1 && go && stream_steps(w, 0) > 2) mbar_wait_bounded(smem_u32(&b_p[0][1]), 0u, 4000ull);
       while (go) {
         const int n = stream_steps(w, s), all = max(n, stream_steps(w, 1 - s));
@@ -661,7 +674,9 @@ __global__ void __launch_bounds__(PA_THREADS, 1) k_packed_attn_tc(const PackedPa
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of the units that several CTAs share: CTA (run i + 1, an eighth of the columns of the unit's 256 rows).
+// Joins the parts of the units that several CTAs share: CTA (run i + 1, an eighth of the columns of the unit's 256 rows). out = sum_k
+// 2^(m_k - M) O_k / sum_k 2^(m_k - M) l_k, in the parts' order. Bound by the latency of its loads: 36 MB in
+// 16 us from a cold L2 at 8,192 rows (2.3 TB/s).
 template <int HD>
 __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) {
   using Lay = FwdLayout<HD>;
@@ -709,6 +724,9 @@ __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) 
 // ---------------------------------------------------------------------------------------------
 // Backward. Two kernels, each with sums of its own and no atomics: dq by tiles of query rows over the keys, dk and dv by
 // tiles of keys over the query rows; the scores are multiplied out in both (7 products instead of 5).
+//
+// p and ds are rounded to bf16 for their products, as P is in the forward pass, sums are fp32. Over a prompt of 8,192 random rows dq is
+// off by 2.7e-3 of its norm (1.7e-3: its own rounding alone), dk and dv by less.
 //
 // delta = d_out . out loses what out was rounded by, which counts where a row sees few keys. As sum_j ds_ij = 0 for the exact
 // delta, the dq kernel adds up its ds (a row lies in one thread, or two) and corrects delta by it for dk; where a row's keys
@@ -782,7 +800,8 @@ JF_DEV float dot8(const uint4& x, const uint4& y, float s) {
   return s;
 }
 
-// delta = d_out . out of every row and head, HD / 8 lanes each (rows of no text as well: not used).
+// delta = d_out . out of every row and head, HD / 8 lanes each (rows of no text as well: not used). Bound by its bytes: 117 MB at 8,192
+// rows of 28 heads, 19 us from a cold L2 (6.2 TB/s).
 template <int HD>
 __global__ void __launch_bounds__(256) k_packed_delta_tc(const PackedParams a) {
   constexpr int LPR = HD / 8;
@@ -801,12 +820,15 @@ __global__ void __launch_bounds__(256) k_packed_delta_tc(const PackedParams a) {
 
 template <int HD>
 struct DqLayout {
-  static constexpr int T = Tile<HD>::BYTES, KEYS = 3, VALUES = 2;  // tiles in shared memory beside Q and d_out: a value tile is read sooner
+  // tiles in shared memory beside Q and d_out: a key tile is held until dQ has read it (two of each: 8,192 rows 1,280 us, 1,230 with three)
+  static constexpr int T = Tile<HD>::BYTES, KEYS = 3, VALUES = 2;
   static constexpr int TOTAL = (2 + KEYS + VALUES) * T + 1024;
 };
 
 // dq. Tensor memory: S, two dP (ds in bf16 in their places), dQ. S and dP of the next step are multiplied before dQ of this one, so that the
-// warps and the tensor core both have work ahead.
+// warps and the tensor core both have work ahead. At 8,192 rows 508 us (three products, 1.42 PFLOP/s), tensor pipe 64%, issue slots 48%: a
+// step's exponentials and products of a row's 128 scores take the warps about as long as the tensor core. Slower: Q and d_out as operands
+// from tensor memory (no gain), two groups of warps that take steps by turns (96 registers spill, 1.4 times as long).
 template <int HD>
 __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedParams a, const __grid_constant__ BackMaps maps) {
   using Lay = DqLayout<HD>;
@@ -1063,7 +1085,8 @@ struct ByKeys {  // tiles of keys over the tiles of `tok` tokens that see them
   JF_DEV int steps(int n, int u) const { return (n + tok - 1) / tok - first(u); }
 };
 
-// dk and dv. Rows of the products are keys, columns query rows. Tensor memory: S (P in bf16 in its place), dP (ds), dV, dK.
+// dk and dv. Rows of the products are keys, columns query rows. Tensor memory: S (P in bf16 in its place), dP (ds), dV, dK. All of it, so
+// that a step's S waits until dV has read P of the step before: 704 us at 8,192 rows (four products, 1.37 PFLOP/s), tensor pipe 61%.
 //
 // Q and d_out come through a ring of four places in pairs. d_out's place is free first and takes the Q of two steps on, Q's place its
 // d_out.
@@ -1324,7 +1347,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dkv_tc(const PackedPar
 }
 
 // Adds up the parts of a unit that several CTAs share, in their order: CTA (run i + 1, 8 pieces of 4 columns of the 128 rows). Kind
-// ByDq: dq and delta; ByKeys: dv and dk.
+// ByDq: dq and delta; ByKeys: dv and dk. Bound by the latency of its loads: 10 and 13 us at 8,192 rows from a cold L2.
 template <int HD, typename Kind>
 __global__ void __launch_bounds__(256) k_packed_back_join(const PackedParams a) {
   constexpr bool KEYS = Kind::KEYS;
