@@ -166,7 +166,7 @@ def policy_loss(logits, targets, old_logprob, advantage, weight=None, ref_logpro
         ld_out = _logits(out, "out")
         _want(out.dtype == logits.dtype and out.device == dev and out.shape == logits.shape, "out: like logits is wanted")
     of = lambda t, name: None if t is None else _vector(t, rows, torch.float32, dev, name)
-    r = torch.empty(5, rows, dtype=torch.float32, device=dev).unbind()
+    r = [torch.empty(rows, dtype=torch.float32, device=dev) for _ in range(5)]
     need = _policy_need(dtype, rows, vocab)
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # the call's own, as in Kv8Cache.attention
     _checked(lib.jf_op_policy_loss(C.byref(J.PolicyTerms(below, above, kl, entropy)), dtype, logits.data_ptr(), ld, rows, vocab, scale,

@@ -18,7 +18,7 @@ from dataclasses import dataclass
 import torch
 
 from . import _lib as J
-from .kv8 import _Fixed, _checked, _device_i32, _dtype, _on_current, _on_stream, _raw_stream, _row_stride, _take_error, _want
+from .kv8 import _Fixed, _checked, _device_i32, _dtype, _on_current, _on_stream, _raw_stream, _take_error, _want
 
 _err = {}  # error word by device
 
@@ -77,25 +77,42 @@ def _need(n_seqs, n_rows, max_rows, dtype, heads, kv_heads, head_dim, backward, 
     return n.value
 
 
-def _rows(t, n, like, name):
-    """Row stride of [n][heads][head_dim] values."""
-    _want(t.dim() == 3 and t.shape[0] == n and t.stride(2) == 1 and t.stride(1) == t.shape[2] and t.dtype == like.dtype and t.device == like.device,
-          "{}: [{}][heads][head_dim] of {} with contiguous heads on {} is wanted", name, n, like.dtype, like.device)
-    return _row_stride(t, t.shape[1] * t.shape[2], name)
+def _row_stride(shape, stride, n, name):
+    """Of [n][heads][head_dim] values."""
+    _want(len(shape) == 3 and shape[0] == n and stride[2] == 1 and stride[1] == shape[2], "{}: [{}][heads][head_dim] with contiguous heads is wanted", name, n)
+    width = shape[1] * shape[2]
+    if n <= 1:
+        return width  # (one row's stride may be anything)
+    _want(stride[0] >= width, "{}: rows {} elements apart that are {} long (contiguous() gives them memory of their own)", name, stride[0], width)
+    return stride[0]
+
+
+@functools.lru_cache(maxsize=4096)
+def _strides(n, q, q_stride, k, k_stride, v, v_stride):
+    """Row strides of q, k, v, from shapes and strides alone."""
+    lds = _row_stride(q, q_stride, n, "q"), _row_stride(k, k_stride, n, "k"), _row_stride(v, v_stride, n, "v")
+    _want(k == v and k[2] == q[2], "q, k and v differ in head size, or k and v in heads")
+    _want(k[1] > 0 and q[1] % k[1] == 0, "{} query heads over {} KV heads", q[1], k[1])
+    return lds
+
+
+def _alike(t, q, name):
+    _want(t.dtype == q.dtype and t.device == q.device, "{}: of {} on {} is wanted", name, q.dtype, q.device)
 
 
 def _arguments(texts, q, k, v):
     _want(q.is_cuda and texts.row_start.device == q.device, "q: a tensor on the texts' device is wanted")
     _on_current(q.device)
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
+    if (q.requires_grad or k.requires_grad or v.requires_grad) and torch.is_grad_enabled():
         raise J.JfError(J.JF_EUNSUPPORTED, "q, k or v requires a gradient, which is not recorded: detach() them, and see attention_grad")
+    _alike(k, q, "k")
+    _alike(v, q, "v")
     n = texts.n_rows
-    lds = [_rows(t, n, q, name) for t, name in ((q, "q"), (k, "k"), (v, "v"))]
-    _want(k.shape == v.shape and k.shape[2] == q.shape[2], "q, k and v differ in head size, or k and v in heads")
-    heads, kv_heads, hd = q.shape[1], k.shape[1], q.shape[2]
-    _want(kv_heads > 0 and heads % kv_heads == 0, "{} query heads over {} KV heads", heads, kv_heads)
-    head = (C.byref(texts.c), _dtype(q.dtype), q.data_ptr(), lds[0], k.data_ptr(), lds[1], v.data_ptr(), lds[2], heads, kv_heads, hd)
-    return head, (texts.c.n_seqs, n, texts.max_rows, head[1], heads, kv_heads, hd)
+    ld_q, ld_k, ld_v = _strides(n, q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride())
+    _, heads, hd = q.shape
+    kv_heads, dtype = k.shape[1], _dtype(q.dtype)
+    return ((C.byref(texts.c), dtype, q.data_ptr(), ld_q, k.data_ptr(), ld_k, v.data_ptr(), ld_v, heads, kv_heads, hd),
+            (texts.c.n_seqs, n, texts.max_rows, dtype, heads, kv_heads, hd))
 
 
 @_on_stream
@@ -118,19 +135,26 @@ def attention_grad(texts: Packed, q, k, v, out, lse, d_out, scale: float, grads=
     """(dq, dk, dv): gradients by q, k and v of a loss whose gradient by attention()'s out is d_out (jf_op_packed_attention_grad).
     grads: three tensors that they are written to (parts of one buffer's rows, for the projection's gradient); None: new ones."""
     head, key = _arguments(texts, q, k, v)
-    dev, n = q.device, texts.n_rows
-    ld_do = _rows(d_out, n, q, "d_out")
-    _want(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.is_contiguous() and d_out.shape == q.shape,
-          "out, d_out: like q (out contiguous) is wanted")
-    _want(lse.shape == q.shape[:2] and lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous(),
-          "lse: contiguous float32 [{}][{}] is wanted", n, q.shape[1])
+    dev, shape, n = q.device, q.shape, texts.n_rows
+    _alike(out, q, "out")
+    _alike(d_out, q, "d_out")
+    ld_do = _row_stride(d_out.shape, d_out.stride(), n, "d_out")
+    _want(out.shape == shape and d_out.shape == shape and out.is_contiguous(), "out, d_out: shaped like q (out contiguous) is wanted")
+    _want(lse.shape == shape[:2] and lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous(),
+          "lse: contiguous float32 [{}][{}] is wanted", n, shape[1])
     if grads is None:
-        grads = tuple(torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
-    lds = [_rows(g, n, q, name) for g, name in zip(grads, ("dq", "dk", "dv"))]
-    _want(len(grads) == 3 and all(g.shape == t.shape for g, t in zip(grads, (q, k, v))), "grads: shaped like q, k and v is wanted")
+        dtype, kv = q.dtype, k.shape
+        dq, dk, dv = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(kv, dtype=dtype, device=dev), torch.empty(kv, dtype=dtype, device=dev))
+        ld_dq, ld_dk, ld_dv = shape[1] * shape[2], kv[1] * kv[2], kv[1] * kv[2]
+    else:
+        _want(len(grads) == 3 and all(g.shape == t.shape for g, t in zip(grads, (q, k, v))), "grads: shaped like q, k and v is wanted")
+        dq, dk, dv = grads
+        for g, name in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+            _alike(g, q, name)
+        ld_dq, ld_dk, ld_dv = _strides(n, shape, dq.stride(), k.shape, dk.stride(), k.shape, dv.stride())
     need = _need(*key, 1, dev.index)
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    _checked(J.load().jf_op_packed_attention_grad(
-        *head, scale, out.data_ptr(), lse.data_ptr(), d_out.data_ptr(), ld_do, grads[0].data_ptr(), lds[0], grads[1].data_ptr(), lds[1],
-        grads[2].data_ptr(), lds[2], ws.data_ptr(), need, _error_word(dev).data_ptr(), _raw_stream(dev)), "jf_op_packed_attention_grad")
-    return tuple(grads)
+    _checked(J.load().jf_op_packed_attention_grad(*head, scale, out.data_ptr(), lse.data_ptr(), d_out.data_ptr(), ld_do, dq.data_ptr(), ld_dq,
+                                                  dk.data_ptr(), ld_dk, dv.data_ptr(), ld_dv, ws.data_ptr(), need,
+                                                  _error_word(dev).data_ptr(), _raw_stream(dev)), "jf_op_packed_attention_grad")
+    return dq, dk, dv
