@@ -725,8 +725,9 @@ __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) 
 // Backward. Two kernels, each with sums of its own and no atomics: dq by tiles of query rows over the keys, dk and dv by
 // tiles of keys over the query rows; the scores are multiplied out in both (7 products instead of 5).
 //
-// p and ds are rounded to bf16 for their products, as P is in the forward pass, sums are fp32. Over a prompt of 8,192 random rows dq is
-// off by 2.7e-3 of its norm (1.7e-3: its own rounding alone), dk and dv by less.
+// p and ds are rounded to bf16 for their products, as P is in the forward pass, sums are fp32. Of dq's norm the rounding of ds takes
+// 1.8e-3, dq's own 1.65e-3, out's (through delta) 0.3e-3: 2.5e-3 for 2,048 random rows, 2.6e-3 measured over 8,192. The remainders of ds as a
+// second operand would take off the first, for a fourth product in dq.
 //
 // delta = d_out . out loses what out was rounded by, which counts where a row sees few keys. As sum_j ds_ij = 0 for the exact
 // delta, the dq kernel adds up its ds (a row lies in one thread, or two) and corrects delta by it for dk; where a row's keys
