@@ -218,7 +218,7 @@ jf_status jf_op_packed_attention_workspace_bytes(const jf_packed* texts, int dty
  * over its rows 0 .. i. dtype (JF_BF16 or JF_F32): type of everything but lse; head_dim 64 or 128. q, k, v: rows of n_heads
  * or n_kv_heads heads, ld_* elements apart, so that the three may be parts of one projection's rows; bf16 rows are read by tensor copies where
  * their addresses and ld_* are multiples of 16 bytes, by slower kernels otherwise. out: [n_rows][n_heads][head_dim], 16-byte aligned; lse (optional
- * here): fp32 [n_rows][n_heads], the natural logarithm of the sum of exponentials. Outputs may not overlap inputs or one another. n_rows *
+ * here): fp32 [n_rows][n_heads], the natural logarithm of the sum of exponentials. Outputs may not overlap inputs or one another. |scale| <= 1e30. n_rows *
  * n_heads <= 2^30; more is refused (JF_EUNSUPPORTED), as are texts so long that the tiles of all scores pass 2^30.
  * Softmax statistics and sums are fp32; JF_BF16 rounds the probabilities (relative to a row's running maximum) to bf16
  * before their product with v. A NaN or an infinity in a text reaches rows of that text only. Results do not depend on the

@@ -544,7 +544,7 @@ extern "C" jf_status jf_op_packed_attention(const jf_packed* texts, int dtype, c
                                             size_t workspace_bytes, int* err_word, void* cuda_stream) {
   jf_status s = packed_check(texts, dtype, n_heads, n_kv_heads, head_dim);
   if (s != JF_OK) return s;
-  if (!err_word || !(scale - scale == 0.f)) return JF_EINVAL;
+  if (!err_word || !(scale >= -1e30f && scale <= 1e30f)) return JF_EINVAL;
   if (texts->n_rows == 0) return JF_OK;
   const long long wq = (long long)n_heads * head_dim, wkv = (long long)n_kv_heads * head_dim;
   if (!packed_rows_ok(q, ld_q, wq, dtype) || !packed_rows_ok(k, ld_k, wkv, dtype) || !packed_rows_ok(v, ld_v, wkv, dtype) || !out ||
@@ -578,7 +578,7 @@ extern "C" jf_status jf_op_packed_attention_grad(const jf_packed* texts, int dty
                                                  size_t workspace_bytes, int* err_word, void* cuda_stream) {
   jf_status s = packed_check(texts, dtype, n_heads, n_kv_heads, head_dim);
   if (s != JF_OK) return s;
-  if (!err_word || !(scale - scale == 0.f)) return JF_EINVAL;
+  if (!err_word || !(scale >= -1e30f && scale <= 1e30f)) return JF_EINVAL;
   if (texts->n_rows == 0) return JF_OK;
   const long long wq = (long long)n_heads * head_dim, wkv = (long long)n_kv_heads * head_dim;
   if (!packed_rows_ok(q, ld_q, wq, dtype) || !packed_rows_ok(k, ld_k, wkv, dtype) || !packed_rows_ok(v, ld_v, wkv, dtype) ||

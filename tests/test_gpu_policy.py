@@ -148,8 +148,58 @@ def test_without_a_gradient_and_in_place(torch):
     assert got.grad is s["logits"] and torch.equal(s["logits"], want.grad) and all(torch.equal(a, b) for a, b in zip(got[:5], want[:5]))
 
 
+@pytest.mark.parametrize("dtype,vocab", [("float32", 500000), ("float32", 460803), ("bfloat16", 930001), ("bfloat16", 300000), ("float32", 11)])
+def test_in_place_at_any_length(torch, dtype, vocab):
+    """... beside rows that a cluster holds as well; 2 rows whose distance passes the vocabulary by an odd number."""
+    s = make(torch, 2, vocab, getattr(torch, dtype), seed=8, pad=3)
+    beside = s["logits"].as_strided((2, 3), (vocab + 3, 1), s["logits"].storage_offset() + vocab)[:1].clone()
+    want = call(torch, s)
+    got = call(torch, s, out=s["logits"])
+    assert torch.equal(s["logits"], want.grad) and all(torch.equal(a, b) for a, b in zip(got[:5], want[:5]))
+    assert torch.equal(s["logits"].as_strided((2, 3), (vocab + 3, 1), s["logits"].storage_offset() + vocab)[:1], beside)
+
+
+@pytest.mark.parametrize("vocab", [1000, 500000])
+def test_rows_further_apart_than_31_bits(torch, vocab):
+    """Within the bounds, which hold for any split of a sum (the same bits only at the same alignment: a row's 16-byte vectors, and so the
+    order of its sums, begin elsewhere)."""
+    s = make(torch, 4, vocab, torch.bfloat16, seed=9)
+    want, bounds = reference(torch, s, 0.2, 0.28, 0.05, 0.01, 1.0)
+    apart = (1 << 30) + 3
+    room = torch.empty(3 * apart + vocab, dtype=torch.bfloat16, device="cuda")
+    far = room.as_strided((4, vocab), (apart, 1))
+    far.copy_(s["logits"])
+    got = call(torch, {**s, "logits": far}, out=far)
+    for x, v, b, name in zip(got, want, bounds, NAMES):
+        inside(torch, x, v, b, name)
+
+
+@pytest.mark.parametrize("dtype,top", [("float32", 1e32), ("float32", 3.4e38), ("float32", -1e32), ("float32", 1e29), ("bfloat16", 1e31), ("bfloat16", -2e30), ("bfloat16", 3.3e38)])
+@pytest.mark.parametrize("vocab", [9, 5000, 300000])
+def test_logits_of_any_size(torch, dtype, top, vocab):
+    """Two equal largest logits, the others lower by a step of the type or more (and so by more than e^-10000): halves and zeros. Also with
+    a scale of 1e7 and logits around 1."""
+    dtype = getattr(torch, dtype)
+    z = torch.full((3, vocab), top, dtype=dtype, device="cuda")
+    for row, scale in ((0, 1.0), (1, 1.0), (2, 1.0)):
+        z[row] = z[row] - (abs(top) / 16 if row else abs(top) / 2)
+        z[row, row], z[row, vocab - 1 - row] = top, top
+    t = torch.arange(3, device="cuda").int()
+    half = torch.full((3,), -math.log(2), device="cuda")
+    for logits, scale in ((z, 1.0), ((z.float() / abs(top)).to(dtype), 1e7)):
+        got = call(torch, dict(logits=logits, targets=t, old=half, ref=half, adv=torch.ones(3, device="cuda"), weight=torch.ones(3, device="cuda")), kl=0.0, eta=0.0,
+                   scale=scale)
+        # old rounds ln 2, log2 and its product with ln 2 round twice
+        assert (got.logprob + math.log(2)).abs().max() <= 4 * U and (got.entropy - math.log(2)).abs().max() <= 4 * U and (got.ratio - 1).abs().max() <= 8 * U
+        want = torch.zeros(3, vocab, dtype=torch.float64, device="cuda")
+        for row in range(3):
+            want[row, row], want[row, vocab - 1 - row] = -0.5 * scale, 0.5 * scale
+        off = (got.grad.double() - want).abs().max()
+        assert off <= scale * (16 * U + half_step(torch, dtype) * 0.5), (scale, off.item())
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("vocab", [50, 6001, 160000])
+@pytest.mark.parametrize("vocab", [50, 6001, 160000, 1000003])
 def test_rows_that_are_left_out_or_are_no_numbers(torch, dtype, vocab):
     from paper_2512_14681_gb300 import _lib as J
     from paper_2512_14681_gb300 import logprobs as L

@@ -70,7 +70,7 @@ def test_texts_and_shapes_that_are_refused(lib):
 
 def test_arguments_that_are_refused(lib):
     both = [dict(q=None), dict(k=None), dict(v=None), dict(q=257), dict(ld_q=255), dict(ld_k=127), dict(ld_v=127), dict(out=None), dict(out=264),
-            dict(scale=float("nan")), dict(scale=float("inf")), dict(err=None), dict(ws=264), dict(dtype=J.JF_F32, k=258)]
+            dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-1.1e30), dict(err=None), dict(ws=264), dict(dtype=J.JF_F32, k=258)]
     for bad in both:
         assert attention(lib, texts(), **bad) == J.JF_EINVAL, bad
     for bad in both + [dict(lse=None), dict(do=None), dict(do=257), dict(ld_do=255), dict(dq=None), dict(dk=None), dict(dv=None), dict(ld_dq=255),
