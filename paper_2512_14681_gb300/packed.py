@@ -36,6 +36,7 @@ class Packed(_Fixed):
     def __post_init__(self):
         _device_i32(self.row_start, 2, "row_start")
         self.c = J.Packed(self.row_start.data_ptr(), self.row_start.numel() - 1, self.n_rows, self.max_rows)
+        _error_word(self.row_start.device)  # (the first call may be a captured one, which cannot wait for it)
 
     @classmethod
     def of(cls, lengths, n_rows=None, max_rows=None, device="cuda"):
@@ -43,8 +44,8 @@ class Packed(_Fixed):
         start = [0]
         for n in lengths:
             start.append(start[-1] + n)
-        return cls(torch.tensor(start, dtype=torch.int32, device=device), start[-1] if n_rows is None else n_rows,
-                   max(lengths, default=0) if max_rows is None else max_rows)
+        n_rows = start[-1] if n_rows is None else n_rows
+        return cls(torch.tensor(start, dtype=torch.int32, device=device), n_rows, min(n_rows, max(lengths, default=0) if max_rows is None else max_rows))
 
 
 def _error_word(device):

@@ -383,6 +383,25 @@ def test_a_captured_call_follows_its_texts(torch, heads):
     P.check()
 
 
+def test_a_first_call_that_is_captured(torch, monkeypatch):
+    from paper_2512_14681_gb300 import packed as P
+
+    heads, lens = HEADS[0], [30, 9]
+    (q, k, v, d), _ = make(torch, heads, lens, seed=16)
+    monkeypatch.setattr(P, "_err", {})
+    texts = P.Packed.of(lens, max_rows=1000)  # (no text is longer than all rows)
+    assert texts.max_rows == 39
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = P.attention(texts, q, k, v, 0.1, want_lse=True)
+        grads = P.attention_grad(texts, q, k, v, out, lse, d, 0.1)
+    graph.replay()
+    P.check()
+    o, l = P.attention(texts, q, k, v, 0.1, want_lse=True)
+    for x, w in zip((out, lse, *grads), (o, l, *P.attention_grad(texts, q, k, v, o, l, d, 0.1))):
+        assert torch.equal(x, w)
+
+
 def test_tensors_of_another_device_than_the_current_one(torch):
     from paper_2512_14681_gb300 import _lib as J
     from paper_2512_14681_gb300 import packed as P
