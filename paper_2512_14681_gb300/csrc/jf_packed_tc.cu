@@ -362,7 +362,9 @@ JF_DEV void scale_o(uint32_t t_o, float x) {
 // from. Warps 0-3, 4-7: stream 0, 1, a thread per row; warp 8: copies; 9, 10: the streams' products; 11: values behind a text's end.
 // (Two threads a row, in 16 warps, took 1.4 times as long: they have to agree on the row's maximum at every step, and 96 registers
 // are too few.) At 8,192 rows the tensor pipe is active 62% of the time, issue slots 34%: the rest is a stream's own chain, read S,
-// maximum, exponentials, write P, wait for the product, of which two streams hide a half.
+// maximum, exponentials, write P, wait for the product, of which two streams hide a half. (Slower at 16,384 rows, 1,315 us: strict turns between
+// the streams' products, 1,329 to 1,366 by what a turn covers; scores read twice from tensor memory instead of kept, 1,448; a quarter of
+// the exponentials by a polynomial on the FMA units beside that, 1,499.)
 // ---------------------------------------------------------------------------------------------
 constexpr int PA_THREADS = 384;  // 168 registers a thread: a row's 128 scores fit
 constexpr float PA_LAG = 8.f;  // a row's reference maximum follows its scores when they exceed it by more
