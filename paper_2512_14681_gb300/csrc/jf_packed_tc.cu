@@ -7,7 +7,7 @@
 //
 // What bounds a long text is the tensor core, and before it each stream's chain product -> softmax -> product; a short one, latency.
 // Measured with 28 heads of 128 on 4: forward of 16,384 rows 1.315 ms (1.46 PFLOP/s), 4,096 rows 110 us, 16 texts of up to 128 rows
-// (12 heads on 2) 10.6 us; backward of 8,192 rows 1.22 ms (0.985 PFLOP/s of the five products' work; seven are multiplied), 4 x 1,024
+// (12 heads on 2) 10.6 us; backward of 8,192 rows 1.255 ms (0.96 PFLOP/s of the five products' work; seven are multiplied), 4 x 1,024
 // rows 151 us.
 //
 // Work is a line of units, (text, KV head, tile), each as long as its steps (tiles of keys, or of query rows in dk and dv)
@@ -728,8 +728,7 @@ __global__ void __launch_bounds__(256) k_packed_attn_join(const PackedParams a) 
 // tiles of keys over the query rows; the scores are multiplied out in both (7 products instead of 5).
 //
 // p and ds are rounded to bf16 for their products, as P is in the forward pass, sums are fp32. Of dq's norm the rounding of ds takes
-// 1.8e-3, dq's own 1.65e-3, out's (through delta) 0.3e-3: 2.5e-3 for 2,048 random rows, 2.6e-3 measured over 8,192. The remainders of ds as a
-// second operand would take off the first, for a fourth product in dq.
+// 1.8e-3, dq's own 1.65e-3, out's (through delta) 0.3e-3, for 2,048 random rows; of a text's first rows dq takes ds as two terms (two_terms).
 //
 // delta = d_out . out loses what out was rounded by, which counts where a row sees few keys. As sum_j ds_ij = 0 for the exact
 // delta, the dq kernel adds up its ds (a row lies in one thread, or two) and corrects delta by it for dk; where a row's keys
@@ -820,6 +819,13 @@ __global__ void __launch_bounds__(256) k_packed_delta_tc(const PackedParams a) {
   for (int sh = LPR / 2; sh; sh >>= 1) d += __shfl_xor_sync(0xffffffffu, d, sh);
   if (piece == 0 && (int)row < a.t.n_rows) a.delta[i] = d;
 }
+
+// Whether a unit's ds goes into dq as two bf16 terms, the second what the first's rounding leaves: in a text's first quarter, and its first
+// 512 rows. Rows that see few keys have the largest gradients, and so the largest part in dq's error: 2.1e-3 of its norm instead of 2.4 to
+// 2.7e-3 (8,192 rows; 5 texts of up to 2,000), for one more product in a sixteenth of a long text's steps: 1,257 us for the pass over
+// 8,192 rows, 1,228 without, others within 1%. (As if those steps were longer by two thirds in the line: 1,275.) (In the
+// first 1,024 rows of all texts: 1.9 to 2.0e-3, 4% of the pass for 4 x 1,024 rows.)
+JF_DEV bool two_terms(const Cut& c) { return c.n_steps <= max(4, c.n >> 9); }
 
 template <int HD>
 struct DqLayout {
@@ -938,6 +944,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
           if (held < PT_KEYS) T::clear_from(sK + place * Lay::T, held, lane);  // (S has read it, and so has the copy)
           tc_fence_after();
           T::template rows<2>(tG, tP + (g & 1) * 128, sK + place * Lay::T, j == w.c0(), on);
+          if (two_terms(w.at)) T::template rows<2>(tG, tP + (g & 1) * 128 + 16, sK + place * Lay::T, false, on);
           commit_on(smem_u32(&b_o[g & 1]), on);
           commit_on(smem_u32(&b_kfree[place]), on);
         }
@@ -969,11 +976,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
       return sum;
     };
     while (go) {
-      const int i = w.at.u * tok + r_tok;
-      const bool live = r_tok < tok && i < w.at.n, one = w.at.n_steps == 1;
-      const long long row = w.at.row0 + i, at = row * a.Hq + w.at.kvh * G + r_head;
-      const float nl = live ? -a.lse[at] * kLog2e : -INFINITY;
-      float delta = live && !one ? a.delta[at] : 0.f, eps = 0.f;
+      int i = w.at.u * tok + r_tok;
+      const bool live = r_tok < tok && i < w.at.n;
+      auto place = [&]() { return (long long)(w.at.row0 + i) * a.Hq + w.at.kvh * G + r_head; };
+      const float nl = live ? -a.lse[place()] * kLog2e : -INFINITY;
+      float delta = live && w.at.n_steps > 1 ? a.delta[place()] : 0.f, eps = 0.f;
       bool left = false;  // (after a meeting that ends the run, there is no other)
       for (int j = w.c0(); j < w.c1() && ok; ++j, ++g) {
         const int see = i - j * PT_KEYS - 32 * quarter;  // columns 0 .. see of the 32
@@ -1006,23 +1013,40 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
 #pragma unroll
           for (int x = 0; x < 32; ++x) v[x] = x <= see ? v[x] : 0.f;
         }
-        if (one) {
+        if (w.at.n_steps == 1) {
           float sum = 0.f;
 #pragma unroll
           for (int x = 0; x < 32; ++x) sum = fmaf(p[x], v[x], sum);
-          delta = join(tP + (g & 1) * 128 + 31, 32, sum);  // (a column that ds leaves alone)
+          delta = join(tP + (g & 1) * 128 + 31, 32, sum);  // (a column that ds takes, once all have read it)
+          if (ok) ok = sync_and<1, 512>(ok);
           left = !ok;
           if (left) break;
         }
         float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
+        auto ds = [&](int x) {
           float2 d = add2(make_float2(v[2 * x], v[2 * x + 1]), make_float2(-delta, -delta));
           d.x *= p[2 * x], d.y *= p[2 * x + 1];
           sum = add2(sum, d);
-          u[x] = pack_bf16(d.x, d.y);
+          return d;
+        };
+        if (two_terms(w.at)) {  // what the first rounding leaves is a second term
+          uint32_t rest[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const float2 d = ds(x);
+            u[x] = pack_bf16(d.x, d.y);
+            rest[x] = pack_bf16(d.x - __uint_as_float(u[x] << 16), d.y - __uint_as_float(u[x] & 0xffff0000u));
+          }
+          tmem_st16(t_p, u);
+          tmem_st16(t_p + 16, rest);
+        } else {
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const float2 d = ds(x);
+            u[x] = pack_bf16(d.x, d.y);
+          }
+          tmem_st16(t_p, u);
         }
-        tmem_st16(t_p, u);
         eps += sum.x + sum.y;
         tmem_wait_st();
         tc_fence_before();
@@ -1030,6 +1054,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
         if (lane == 0) mbar_arrive(smem_u32(&b_ds[g & 1]));
       }
       if (left) break;
+      asm volatile("" : "+r"(i));  // (the row's places are found again: registers)
       ok = ok && warp_wait(b_unit, units++);
       tc_fence_after();
       const bool whole = w.whole();
@@ -1042,7 +1067,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
         else tmem_ld16(tG + t_row + d0, o);
         if (whole) {
           if (live) {
-            bf16* dst = reinterpret_cast<bf16*>(a.dq) + row * a.ld_dq + (w.at.kvh * G + r_head) * HD + d0;
+            bf16* dst = reinterpret_cast<bf16*>(a.dq) + (w.at.row0 + i) * a.ld_dq + (w.at.kvh * G + r_head) * HD + d0;
             if (((uintptr_t)dst & 15) == 0) {
 #pragma unroll
               for (int h = 0; h < DW / 8; ++h)
@@ -1064,7 +1089,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) k_packed_dq_tc(const PackedPara
       if (!ok) break;
       if (quarter == 0) {
         if (!whole) st[128 * HD + r] = eps, st[128 * (HD + 1) + r] = delta;
-        else if (live) a.delta[at] = one ? delta : delta + eps;
+        else if (live) a.delta[place()] = w.at.n_steps == 1 ? delta : delta + eps;
       }
       tc_fence_before();
       ok = sync_and<1, 512>(ok);  // ... and what they exchanged
