@@ -835,7 +835,7 @@ struct DqLayout {
 };
 
 // dq. Tensor memory: S, two dP (ds in bf16 in their places), dQ. S and dP of the next step are multiplied before dQ of this one, so that the
-// warps and the tensor core both have work ahead. At 8,192 rows 508 us (three products, 1.42 PFLOP/s), tensor pipe 64%, issue slots 48%: a
+// warps and the tensor core both have work ahead. At 8,192 rows, ds as one term, 508 us (three products, 1.42 PFLOP/s; some 30 more with two), tensor pipe 64%, issue slots 48%: a
 // step's exponentials and products of a row's 128 scores take the warps about as long as the tensor core. Slower: Q and d_out as operands
 // from tensor memory (no gain), two groups of warps that take steps by turns (96 registers spill, 1.4 times as long).
 template <int HD>
