@@ -67,8 +67,9 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 // rounded once from a fused product, S = sum 2^y, T = sum 2^y y; states are joined by their b. Then
 //   lp = scale (x_t - m) - ln 2 (log2 S + b - c m),  H = ln 2 (log2 S - T / S),  p = 2^y / S,
 //   dloss/dx = -scale / S 2^y (g + gh (H - ln S) + gh ln 2 y), + scale g at the target.
-// Logits below -1e30 (and c above 1e6) would leave fp32's range in y: they count as -1e30, whose 2^y is 0, unless the row's
-// largest is such a one itself; its sums then are taken again from differences x - m.
+// b is off from c m by up to 2^-24 of it, which every 2^y of the thread takes as a factor: within 2 where |c m| is below 2^24 (PL_NEAR; beyond
+// 2^31 S would leave fp32's range). Sums of a row whose largest logit lies further out (or is beyond 1e29, or has a c above 1e6) are taken
+// again from differences x - m. Logits below -1e30 would leave fp32's range in y: they count as -1e30, whose 2^y is 0.
 //
 // Bound by bytes where rows are many: 2,048 fp32 rows of 152,064 in 441 us (5.65 TB/s of logits in and gradients out, 0.84 of a copy);
 // bf16 ones, whose pairs take as many instructions for half the bytes, by issue: 512 rows in 68 us (4.6 TB/s), at an odd distance 70. A
@@ -78,7 +79,7 @@ constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8;
 constexpr int PL_FIT[3] = {56832, 76288, 115200};  // bytes of a CTA's run with which four, three, two are resident on an SM
 constexpr int PL_MOST = PL_FIT[2];
 constexpr int PL_ROWS = 1 << 30;  // (a row and the step to the next fit 31 bits)
-constexpr float PL_FAR = 1e30f, PL_LARGE = 1e29f, PL_STEEP = 1e6f, LN2 = 0.69314718055994531f;
+constexpr float PL_FAR = 1e30f, PL_LARGE = 1e29f, PL_STEEP = 1e6f, PL_NEAR = 16777216.f, LN2 = 0.69314718055994531f;
 constexpr float LOG2E_LO = 1.9259630e-8f;  // log2 e beyond LOG2E
 
 JF_DEV float warp_max(float v) {
@@ -109,6 +110,9 @@ JF_DEV float largest(const uint4& v, float most, bf16) {
   const __nv_bfloat162 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
   return fmaxf(most, fmaxf(__low2float(m), __high2float(m)));
 }
+// Whether sums relative to c m hold where m is the largest logit, of a row (by 1) or of a thread (by 2, so that one whose sums are left
+// out lies at least PL_NEAR below the row's largest, if the row's sums hold).
+JF_DEV bool holds(float c, float m, float by) { return c <= PL_STEEP && fabsf(m) < PL_LARGE * by && fabsf(c * m) < PL_NEAR * by; }
 JF_DEV float max_nan(float x, float y) {
   float r;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
@@ -238,7 +242,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
     for (int v = tid; v < n; v += PL_THREADS) m = largest(s_run[v], m, T{});
     LpStat st;
     {
-      const float b = c <= PL_STEEP && fabsf(m) < PL_LARGE ? c * m : -INFINITY;  // (-inf: the thread's sums do not count, or are taken again)
+      const float b = holds(c, m, 2.f) ? c * m : -INFINITY;  // (-inf: the thread's sums do not count, or are taken again)
       const float minus = b == -INFINITY ? 0.f : -b;
       const Pair cc = pair(c, c), nb = pair(minus, minus);
       Pair s = 0, t = 0;
@@ -278,7 +282,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
         st = join_lanes({ld_cluster(from), ld_cluster(from + 4), ld_cluster(from + 8)}, (int)parts);
         m = warp_max(peer_m);
       }
-      none = m == -INFINITY, far = !none && (c > PL_STEEP || !(fabsf(m) < PL_LARGE));
+      none = m == -INFINITY, far = !none && !holds(c, m, 1.f);
     }
     auto finish = [&]() {  // by warp 0
       const bool empty = none && st.s == 0.f;  // no token can occur

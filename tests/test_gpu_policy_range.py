@@ -1,0 +1,59 @@
+"""The policy loss over the whole range of its arguments, against plain 64-bit arithmetic (bounds: tests/test_gpu_policy.py).
+
+fp32 rows of up to 230,400 logits (bf16 460,800) are one kernel's, longer ones three kernels': every case runs on both."""
+import math
+
+import pytest
+
+from tests.packed_ref import U, half_step, inside
+from tests.parity import need_gpu
+from tests.test_gpu_policy import NAMES, call, reference
+
+pytestmark = pytest.mark.gpu
+DTYPES = ["float32", "bfloat16"]
+
+
+@pytest.fixture(scope="module")
+def torch():
+    return need_gpu()
+
+
+def on(torch, logits, target, old=0.0, ref=0.0, adv=1.0, weight=1.0):
+    """A call's inputs; what is a number is every row's."""
+    rows = logits.shape[0]
+    f = lambda x: x if isinstance(x, torch.Tensor) else torch.full((rows,), float(x), device="cuda")
+    t = target if isinstance(target, torch.Tensor) else torch.full((rows,), target, dtype=torch.int32, device="cuda")
+    return dict(logits=logits, targets=t, old=f(old), ref=f(ref), adv=f(adv), weight=f(weight))
+
+
+def apart(z):
+    """Logits as 64-bit differences from their row's largest (beside which 64 bits may hold no logarithm of a sum)."""
+    return z.double() - z.double().amax(1, keepdim=True)
+
+
+def held(torch, s, what, **kw):
+    got = call(torch, s, **kw)
+    want, bounds = reference(torch, {**s, "logits": apart(s["logits"])}, 0.2, 0.28, kw["kl"], kw["eta"], kw["scale"])
+    bounds[5] = bounds[5] + half_step(torch, s["logits"].dtype) * want[5].abs()
+    for x, v, b, name in zip(got, want, bounds, NAMES):
+        inside(torch, x, v, b, f"{name} {what}")
+    return got
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("top", [1.1e7, 1.2e7, 2.3e7, 2.4e7, 1e9, 4e9, 1.3e10, 7.7e12, 3e20, 9e28, 2e29, 9e37, 2e38])
+@pytest.mark.parametrize("vocab", [9, 5001, 300001, 470001])
+def test_large_logits(torch, dtype, top, vocab):
+    """Logits a few of the type's steps apart, as far as a step still counts beside the largest; of either sign, at scale 1 and at one
+    that brings them to 2^24 or below."""
+    dtype = getattr(torch, dtype)
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    step = torch.finfo(dtype).eps * 2.0 ** math.floor(math.log2(top))
+    for sign in (1, -1):
+        z = (sign * top - step * torch.randint(0, 30, (4, vocab), generator=g, device="cuda").double()).to(dtype)
+        z[1, ::3] = -math.inf
+        target = z.float().argmax(1)
+        lp = lambda scale: torch.log_softmax(apart(z) * scale, 1).gather(1, target[:, None])[:, 0]
+        for scale in (1.0, max(2.0 ** -math.ceil(math.log2(step)), 2.0 ** -92)):
+            s = on(torch, z, target.int(), old=(lp(scale) + 0.05).float(), ref=(lp(scale) - 0.1).float(), adv=torch.tensor([1.0, -1.0, 0.5, 2.0], device="cuda"))
+            held(torch, s, (sign, scale), kl=0.05, eta=0.01, scale=scale)
