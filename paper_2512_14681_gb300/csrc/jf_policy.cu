@@ -528,7 +528,7 @@ extern "C" jf_status jf_op_policy_loss(const jf_policy_terms* terms, int dtype, 
       (!ref_logprob && terms->kl != 0.f) || (dtype != JF_F32 && dtype != JF_BF16) || rows < 0 || vocab < 1 || vocab > (1 << 30) || !err_word)
     return JF_EINVAL;
   if (rows > PL_ROWS) return JF_EUNSUPPORTED;
-  if (!(scale > 0.f) || scale > 1e30f || ld < vocab) return JF_EINVAL;
+  if (!(scale >= 1e-28f) || scale > 1e30f || ld < vocab) return JF_EINVAL;  // (2^(-1e30 scale log2 e) is 0)
   if (rows == 0) return JF_OK;
   const uintptr_t type_mask = dtype == JF_BF16 ? 1 : 3;
   if (!logits || ((uintptr_t)logits & type_mask) || !targets || !advantage) return JF_EINVAL;

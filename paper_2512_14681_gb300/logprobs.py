@@ -150,7 +150,7 @@ def policy_loss(logits, targets, old_logprob, advantage, weight=None, ref_logpro
                 kl: float = 0.0, entropy: float = 0.0, scale: float = 1.0, want_grad=True, out=None) -> PolicyLoss:
     """Clipped policy loss of every row's target, and its gradient by the logits (jf_op_policy_loss): with r the ratio of the
     target's probability to e^old_logprob, weight (-min(r A, min(max(r, 1 - below), 1 + above) A) + kl KL - entropy H). logits,
-    targets, scale: as in token_logprobs; old_logprob (None: r = 1), advantage, weight (None: 1), ref_logprob (None without
+    targets, scale: as in token_logprobs (no scale below 1e-28); old_logprob (None: r = 1), advantage, weight (None: 1), ref_logprob (None without
     kl): float32 [rows]. out: where the gradient goes (it may be `logits`). As there, no graph is recorded."""
     if logits.requires_grad and torch.is_grad_enabled():
         raise J.JfError(J.JF_EUNSUPPORTED, "logits require a gradient, which is not recorded: detach() them, and give .grad to logits.backward()")
