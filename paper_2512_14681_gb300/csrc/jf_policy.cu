@@ -69,7 +69,8 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 //   dloss/dx = -scale / S 2^y (g + gh (H - ln S) + gh ln 2 y), + scale g at the target.
 // b is off from c m by up to 2^-24 of it, which every 2^y of the thread takes as a factor: within 2 where |c m| is below 2^24 (PL_NEAR; beyond
 // 2^31 S would leave fp32's range). Sums of a row whose largest logit lies further out (or is beyond 1e29, or has a c above 1e6) are taken
-// again from differences x - m. Logits below -1e30 would leave fp32's range in y: they count as -1e30, whose 2^y is 0.
+// again from differences x - m. A logit so far below the largest that 2^y is 0 (PL_BELOW) counts as one at that distance, so that y, and its
+// products with what an entropy term gives, stay in fp32's range whatever the mask and the scale are.
 //
 // Bound by bytes where rows are many: 2,048 fp32 rows of 152,064 in 441 us (5.65 TB/s of logits in and gradients out, 0.84 of a copy);
 // bf16 ones, whose pairs take as many instructions for half the bytes, by issue: 512 rows in 68 us (4.6 TB/s), at an odd distance 70. A
@@ -79,7 +80,7 @@ constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8;
 constexpr int PL_FIT[3] = {56832, 76288, 115200};  // bytes of a CTA's run with which four, three, two are resident on an SM
 constexpr int PL_MOST = PL_FIT[2];
 constexpr int PL_ROWS = 1 << 30;  // (a row and the step to the next fit 31 bits)
-constexpr float PL_FAR = 1e30f, PL_LARGE = 1e29f, PL_STEEP = 1e6f, PL_NEAR = 16777216.f, LN2 = 0.69314718055994531f;
+constexpr float PL_FAR = 1e30f, PL_BELOW = 400.f, PL_LARGE = 1e29f, PL_STEEP = 1e6f, PL_NEAR = 16777216.f, LN2 = 0.69314718055994531f;
 constexpr float LOG2E_LO = 1.9259630e-8f;  // log2 e beyond LOG2E
 
 JF_DEV float warp_max(float v) {
@@ -149,13 +150,13 @@ JF_DEV Pair ex2_pair(Pair y) {
   const F2 v = halves(y);
   return pair(ex2_ftz(v.x), ex2_ftz(v.y));
 }
-// A vector's values, none below -PL_FAR (NaN kept).
-JF_DEV void raised(const uint4& v, Pair (&x)[2], float) {
-  x[0] = pair(max_nan(__uint_as_float(v.x), -PL_FAR), max_nan(__uint_as_float(v.y), -PL_FAR));
-  x[1] = pair(max_nan(__uint_as_float(v.z), -PL_FAR), max_nan(__uint_as_float(v.w), -PL_FAR));
+// A vector's values, none below `low` (bf16: rounded down; NaN kept).
+JF_DEV void raised(const uint4& v, Pair (&x)[2], float low) {
+  x[0] = pair(max_nan(__uint_as_float(v.x), low), max_nan(__uint_as_float(v.y), low));
+  x[1] = pair(max_nan(__uint_as_float(v.z), low), max_nan(__uint_as_float(v.w), low));
 }
-JF_DEV void raised(const uint4& v, Pair (&x)[4], bf16) {
-  const __nv_bfloat162 far = __float2bfloat162_rn(-PL_FAR);
+JF_DEV void raised(const uint4& v, Pair (&x)[4], float low) {
+  const __nv_bfloat162 far = __bfloat162bfloat162(__float2bfloat16_rd(low));
   const __nv_bfloat162* w = reinterpret_cast<const __nv_bfloat162*>(&v);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -204,7 +205,8 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
   const uint32_t parts = cluster_ctas();
   const int rank = (int)cluster_rank(), lg = 31 - __clz(parts), rows_apart = gridDim.x >> lg;  // (parts: a power of two)
   const T* logits = reinterpret_cast<const T*>(a.logits);
-  const float c = a.scale * LOG2E;
+  // (y is at least -PL_BELOW less what rounding takes: a step of fp32 at PL_NEAR, of bf16 2^17)
+  const float c = a.scale * LOG2E, below = PL_BELOW / c;
   // a row's run
   auto ask = [&](int row) {
     const Row<T> r(logits + row * a.ld, a.V);
@@ -243,7 +245,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
     LpStat st;
     {
       const float b = holds(c, m, 2.f) ? c * m : -INFINITY;  // (-inf: the thread's sums do not count, or are taken again)
-      const float minus = b == -INFINITY ? 0.f : -b;
+      const float minus = b == -INFINITY ? 0.f : -b, low = b == -INFINITY ? -PL_FAR : m - below;
       const Pair cc = pair(c, c), nb = pair(minus, minus);
       Pair s = 0, t = 0;
       auto add = [&](Pair x) {
@@ -255,11 +257,11 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
 #pragma unroll 2
       for (int v = tid; v < n; v += PL_THREADS) {
         Pair x[N / 2];
-        raised(s_run[v], x, T{});
+        raised(s_run[v], x, low);
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) add(x[k]);
       }
-      if (edge) add(pair(max_nan(at_edge, -PL_FAR), -PL_FAR));
+      if (edge) add(pair(max_nan(at_edge, low), low));
       st = {b, halves(s).x + halves(s).y, halves(t).x + halves(t).y};
       if (b == -INFINITY && st.s == st.s) st.s = st.t = 0.f;  // (a NaN among them counts)
       st = join_lanes(st, 32);
@@ -353,12 +355,13 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
     const float b = s_row[0], l2 = s_row[1], S = s_row[2], H = s_row[3], g = s_row[4], gh = s_row[5], k = a.scale;
     // -scale / S times (g + gh (H - ln S) + gh ln 2 y)
     const float f = -k / S, share0 = f * fmaf(gh, H - LN2 * l2, g), share1 = f * (gh * LN2), hot = k * g;
+    const float low = m - below;
     const bool still = g == 0.f && gh == 0.f;  // (also a row without a token that can occur)
     T* out = reinterpret_cast<T*>(a.grad) + (a.grad ? row * a.ld_grad : 0);
     // the gradient by a logit without the target's own term
     auto of1 = [&](float x) {
-      const float y = far ? fmaxf(x - m, -PL_FAR) * c : fmaf(max_nan(x, -PL_FAR), c, -b);
-      return still ? 0.f : ex2_ftz(y) * fmaf(fmaxf(y, -PL_FAR), share1, share0);
+      const float y = far ? (x - m) * c : fmaf(max_nan(x, low), c, -b);
+      return still ? 0.f : ex2_ftz(y) * fmaf(max_nan(y, -PL_BELOW), share1, share0);
     };
     auto single = [&](int i, float x) { out[i] = to_act<T>(of1(x) + (i == target ? hot : 0.f)); };
     // Vectors of the output: where it lies otherwise than the logits, each is of two neighbours' elements, and the first and the
@@ -378,7 +381,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
       const int i0 = e0 + v * N + own;
       Pair x[N / 2];
       float d[N];
-      raised(w, x, T{});
+      raised(w, x, low);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
         const Pair y = fma_pair(x[i], cc, nb);

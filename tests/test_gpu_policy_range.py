@@ -57,3 +57,22 @@ def test_large_logits(torch, dtype, top, vocab):
         for scale in (1.0, max(2.0 ** -math.ceil(math.log2(step)), 2.0 ** -92)):
             s = on(torch, z, target.int(), old=(lp(scale) + 0.05).float(), ref=(lp(scale) - 0.1).float(), adv=torch.tensor([1.0, -1.0, 0.5, 2.0], device="cuda"))
             held(torch, s, (sign, scale), kl=0.05, eta=0.01, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [1e-28, 1e-10, 1e3, 1e4, 1e5, 6e5, 1e7, 1e12, 1e30])
+@pytest.mark.parametrize("vocab", [11, 5001, 300001, 470001])
+def test_masks_at_any_scale(torch, dtype, scale, vocab):
+    """Scores around 1 whatever the scale, a third of them masked out, with an entropy term of weight 0.1."""
+    dtype = getattr(torch, dtype)
+    scale = torch.tensor(scale, dtype=torch.float32).item()
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    z = (torch.randn(6, vocab, generator=g, device="cuda").double() * 2 / scale).to(dtype)
+    f = torch.rand(6, vocab, generator=g, device="cuda")
+    z[f < 0.3] = -math.inf
+    z[f > 0.95] = torch.finfo(dtype).min
+    target = z.float().argmax(1)
+    lp = torch.log_softmax(apart(z) * scale, 1).gather(1, target[:, None])[:, 0]
+    s = on(torch, z, target.int(), old=(lp + 0.05).float(), ref=(lp - 0.1).float(), adv=torch.tensor([1.0, -1.0, 0.5, 2.0, 0.0, 1.0], device="cuda"))
+    got = held(torch, s, scale, kl=0.05, eta=0.1, scale=scale)
+    assert (got.grad[z == -math.inf] == 0).all()
