@@ -181,9 +181,11 @@ jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld,
  * ld_grad = ld), but not overlap them otherwise. rows <= 2^30.
  * A negative target leaves its row out: loss, logprob, ratio, kl and gradient 0 (entropy is the row's). A weight of 0 makes
  * loss and gradient 0 whatever the other terms are, and an advantage of 0 the first term. A target that cannot occur
- * (a logit of -infinity) has ratio 0 and, with a ref_logprob, an infinite kl without a gradient. Rows without a token that can occur, NaN
+ * (a logit of -infinity) has ratio 0 and, with a ref_logprob, an infinite kl; a kl beyond the range of fp32 (d above 88) is infinite
+ * and has no gradient. Rows without a token that can occur, NaN
  * among the logits and targets >= vocab: as in jf_op_token_logprobs (the loss of the last is NaN, its gradient 0). A ratio
- * beyond the range of fp32 is infinite, as loss and gradient then are where A is negative.
+ * beyond the range of fp32 is infinite, as loss and gradient then are where A is negative; a logit whose token has probability 0 (in
+ * fp32, below 2^-126 of the row's most likely one) has gradient 0 all the same, unless it is the target.
  * workspace: device, 16-byte aligned, no initialisation needed; calls that may overlap on the GPU need one each. (0 bytes but for
  * rows longer than a cluster's shared memory, 460,800 fp32 or 921,600 bf16 values.) */
 typedef struct {

@@ -408,7 +408,8 @@ constexpr int LP_GRAD_VECS = 4;  // vectors per thread
 // CTA (row, run of LP_GRAD_VECS x 256 vectors); the first run's CTA takes the row's edges too. Bound by the bytes, each
 // logit read and each gradient written once with four vectors of a thread in flight: 512 rows of 152,064 fp32 logits
 // (623 MB) take 94 us, 6.6 TB/s.
-template <typename T>
+// ANY_SIZE: g and h may be infinite (the policy loss's).
+template <typename T, bool ANY_SIZE>
 __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams a) {
   constexpr int N = Vec<T>::N;
   pdl_launch_dependents();
@@ -427,6 +428,7 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams
   const bool none = m == -INFINITY && ls == -INFINITY;
   auto of = [&](float x, int i) {
     const float lp = fmaf(x - m, a.scale, -ls), p = ex2_ftz(lp * LOG2E);
+    if (ANY_SIZE) return none ? 0.f : a.scale * policy_grad(p, lp, H, g, gh, i == target);
     // -g p - gh p (lp + H), the logit of probability 0 without its infinite lp
     const float share = g + gh * (fmaxf(lp, -1e4f) + H);
     return none ? 0.f : a.scale * ((i == target ? g : 0.f) - p * share);
@@ -526,11 +528,10 @@ extern "C" jf_status jf_op_token_logprobs(int dtype, const void* logits, long lo
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 
-extern "C" jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld, int rows, int vocab,
-                                               float scale, const int32_t* targets, const float* row_stats,
-                                               const float* entropy, const float* grad_logprob,
-                                               const float* grad_entropy, void* grad_logits, long long ld_grad,
-                                               int* err_word, void* cuda_stream) {
+template <bool ANY_SIZE>
+static jf_status logprobs_grad(int dtype, const void* logits, long long ld, int rows, int vocab, float scale, const int32_t* targets, const float* row_stats,
+                               const float* entropy, const float* grad_logprob, const float* grad_entropy, void* grad_logits, long long ld_grad,
+                               int* err_word, cudaStream_t st) {
   if (!lp_shape_ok(dtype, logits, ld, rows, vocab, scale) || !err_word || ld_grad < vocab) return JF_EINVAL;
   if (rows == 0) return JF_OK;
   if (!targets || !row_stats || !grad_logits || (grad_entropy && !entropy)) return JF_EINVAL;
@@ -541,9 +542,22 @@ extern "C" jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, lo
   const int segs = (vocab + per_cta - 1) / per_cta;
   const LpGradParams a = {logits, ld, ld_grad, rows, vocab, segs, scale, targets, row_stats, entropy, grad_logprob, grad_entropy,
                           grad_logits, err_word};
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   const long long grid = (long long)rows * segs;
   if (grid > 0x7fffffffll) return JF_EUNSUPPORTED;
-  const cudaError_t e = dtype == JF_BF16 ? lp_launch(k_logprobs_grad<bf16>, grid, st, a) : lp_launch(k_logprobs_grad<float>, grid, st, a);
+  const cudaError_t e = dtype == JF_BF16 ? lp_launch(k_logprobs_grad<bf16, ANY_SIZE>, grid, st, a) : lp_launch(k_logprobs_grad<float, ANY_SIZE>, grid, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
+}
+
+extern "C" jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld, int rows, int vocab,
+                                               float scale, const int32_t* targets, const float* row_stats,
+                                               const float* entropy, const float* grad_logprob,
+                                               const float* grad_entropy, void* grad_logits, long long ld_grad,
+                                               int* err_word, void* cuda_stream) {
+  return logprobs_grad<false>(dtype, logits, ld, rows, vocab, scale, targets, row_stats, entropy, grad_logprob, grad_entropy, grad_logits, ld_grad,
+                              err_word, reinterpret_cast<cudaStream_t>(cuda_stream));
+}
+
+jf_status jf::policy_long_grad(int dtype, const void* logits, long long ld, int rows, int vocab, float scale, const int32_t* targets, const float* row_stats,
+                               const float* entropy, const float* g, const float* gh, void* grad_logits, long long ld_grad, int* err_word, cudaStream_t st) {
+  return logprobs_grad<true>(dtype, logits, ld, rows, vocab, scale, targets, row_stats, entropy, g, gh, grad_logits, ld_grad, err_word, st);
 }

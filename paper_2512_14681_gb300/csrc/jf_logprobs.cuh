@@ -14,6 +14,14 @@ JF_DEV float ex2_ftz(float x) {
   return y;
 }
 
+// dloss/dz of a token of probability p, ln p = lp, where dloss/dlogprob = g, dloss/dentropy = gh and the row's entropy is H. What cannot
+// occur has no share, and what is certain is moved by nothing, also where a term is infinite.
+JF_DEV float policy_grad(float p, float lp, float H, float g, float gh, bool is_target) {
+  float d = is_target ? (p == 1.f ? 0.f : g * (1.f - p)) : (p == 0.f ? 0.f : -g * p);
+  if (gh != 0.f && p != 0.f) d -= gh * p * (lp + H);
+  return d;
+}
+
 struct LpStat {
   float m, s, t;  // largest logit; sums relative to it
 };
@@ -114,5 +122,9 @@ JF_DEV F2 fma2(F2 a, F2 b, F2 c) {
       : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return r;
 }
+
+// jf_op_token_logprobs_grad (jf_logprobs.cu) for g and gh of any size.
+jf_status policy_long_grad(int dtype, const void* logits, long long ld, int rows, int vocab, float scale, const int32_t* targets, const float* row_stats,
+                           const float* entropy, const float* g, const float* gh, void* grad_logits, long long ld_grad, int* err_word, cudaStream_t st);
 
 }  // namespace jf

@@ -43,7 +43,7 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
   r.kl = 0.f;
   if (a.ref_lp) {
     const float d = ref - lp, e = expm1f(d);
-    const bool out = d == INFINITY;
+    const bool out = e == INFINITY;  // (beyond fp32's range: no gradient)
     r.kl = out ? INFINITY : e - d;
     if (a.t.kl != 0.f) {
       sum = fmaf(a.t.kl, r.kl, sum);
@@ -358,12 +358,16 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
     const float low = m - below;
     const bool still = g == 0.f && gh == 0.f;  // (also a row without a token that can occur)
     T* out = reinterpret_cast<T*>(a.grad) + (a.grad ? row * a.ld_grad : 0);
-    // the gradient by a logit without the target's own term
-    auto of1 = [&](float x) {
-      const float y = far ? (x - m) * c : fmaf(max_nan(x, low), c, -b);
-      return still ? 0.f : ex2_ftz(y) * fmaf(max_nan(y, -PL_BELOW), share1, share0);
+    // Whether a 2^y of 0 times its share is 0 (-y < 2^18): not where a term is infinite, or nearly so, or no number. Such rows and those of
+    // sums from differences are taken a value at a time.
+    const bool plain = !far && fabsf(share0) < 1e38f && fabsf(share1) < 1e32f;
+    auto of1 = [&](float x, bool is_target) {
+      const float y = far ? (x - m) * c : fmaf(max_nan(x, low), c, -b), p = ex2_ftz(y);
+      if (still) return 0.f;
+      if (plain) return p * fmaf(y, share1, share0) + (is_target ? hot : 0.f);
+      return k * policy_grad(p / S, LN2 * (y - l2), H, g, gh, is_target);
     };
-    auto single = [&](int i, float x) { out[i] = to_act<T>(of1(x) + (i == target ? hot : 0.f)); };
+    auto single = [&](int i, float x) { out[i] = to_act<T>(of1(x, i == target)); };
     // Vectors of the output: where it lies otherwise than the logits, each is of two neighbours' elements, and the first and the
     // last of the run's are stored one by one.
     const int skip = (int)((16 - ((uintptr_t)(out + r.head) & 15)) & 15), own = skip / (int)sizeof(T), n_out = skip ? n - 1 : n;
@@ -400,7 +404,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
       const float zeros[N] = {};
 #pragma unroll 2
       for (int v = tid; v < end; v += PL_THREADS) Vec<T>::store(out + e0 + v * N + own, zeros);
-    } else if (far) {
+    } else if (!plain) {
 #pragma unroll 1
       for (int v = tid; v < end; v += PL_THREADS)
 #pragma unroll 1
@@ -566,6 +570,5 @@ extern "C" jf_status jf_op_policy_loss(const jf_policy_terms* terms, int dtype, 
   k_policy_rows<<<(rows + 127) / 128, 128, 0, st>>>(a);
   if (cudaGetLastError() != cudaSuccess) return JF_ECUDA;
   if (!grad_logits) return JF_OK;
-  return jf_op_token_logprobs_grad(dtype, logits, ld, rows, vocab, scale, targets, stats, H, a.g, a.gh, grad_logits, ld_grad, err_word,
-                                   cuda_stream);
+  return policy_long_grad(dtype, logits, ld, rows, vocab, scale, targets, stats, H, a.g, a.gh, grad_logits, ld_grad, err_word, st);
 }

@@ -7,7 +7,7 @@ import pytest
 
 from tests.packed_ref import U, half_step, inside
 from tests.parity import need_gpu
-from tests.test_gpu_policy import NAMES, call, reference
+from tests.test_gpu_policy import NAMES, call, make, reference
 
 pytestmark = pytest.mark.gpu
 DTYPES = ["float32", "bfloat16"]
@@ -76,3 +76,55 @@ def test_masks_at_any_scale(torch, dtype, scale, vocab):
     s = on(torch, z, target.int(), old=(lp + 0.05).float(), ref=(lp - 0.1).float(), adv=torch.tensor([1.0, -1.0, 0.5, 2.0, 0.0, 1.0], device="cuda"))
     got = held(torch, s, scale, kl=0.05, eta=0.1, scale=scale)
     assert (got.grad[z == -math.inf] == 0).all()
+
+
+def masked(torch, dtype, vocab, first=1):
+    """Rows at an odd address, a third of them masked out by -infinity and by the type's lowest value, on tokens from 8 on."""
+    s = make(torch, 8, vocab, dtype, seed=21, pad=2, first=first, masked=True)
+    z = s["logits"]
+    z[:, :8] = torch.linspace(-1, 1, 8, device="cuda").to(dtype)
+    s["targets"].fill_(3)
+    out = (z == -math.inf) | (z == torch.finfo(dtype).min)
+    assert out[:, vocab - 8:].any() and (vocab < 100 or out[:, -2:].any())
+    return s, out
+
+
+LONG = [60, 5001, 300001, 470001]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", LONG)
+@pytest.mark.parametrize("eta", [0.0, 0.01])
+def test_an_infinite_ratio_moves_no_token_of_probability_0(torch, dtype, vocab, eta):
+    """A < 0: the gradient is infinite, towards the target and away from the others that can occur, and 0 at those that cannot. (Of a row with
+    one token that can occur, what rounding of its entropy leaves: the exponential's 2^-22 and a few steps of fp32.)"""
+    dtype = getattr(torch, dtype)
+    s, out = masked(torch, dtype, vocab)
+    s["old"].fill_(-1e30), s["adv"].fill_(-1.0)
+    got = call(torch, s, kl=0.0, eta=eta)
+    assert (got.ratio == math.inf).all() and (got.loss == math.inf).all()
+    assert (got.grad[out] == 0).all() and (got.grad[:, 3] == math.inf).all()
+    assert (got.grad[:, :3] == -math.inf).all() and not torch.isnan(got.grad).any()
+    s["logits"][:, 4:] = -math.inf  # one token that can occur has probability 1: nothing moves it
+    s["logits"][:, :3] = -math.inf
+    got = call(torch, s, kl=0.0, eta=eta)
+    assert got.grad.abs().max() <= eta * 16 * U and got.logprob.abs().max() <= 8 * U
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", LONG)
+@pytest.mark.parametrize("scale", [1.0, 1.25])
+def test_an_infinite_kl_has_no_gradient(torch, dtype, vocab, scale):
+    """A target that the type's lowest value, -infinity or a distance of more than 88 puts out of fp32's range of e^d."""
+    dtype = getattr(torch, dtype)
+    s, out = masked(torch, dtype, vocab)
+    z = s["logits"]
+    z[0, 3], z[1, 3], z[2, 3], z[3, 3], z[4, 3] = torch.finfo(dtype).min, -math.inf, -95.0, -1000.0, -1e30
+    s["ref"].fill_(0.0)
+    for eta in (0.0, 0.01):
+        got = call(torch, s, kl=0.05, eta=eta, scale=scale)
+        without = call(torch, s, kl=0.0, eta=eta, scale=scale)
+        assert (got.kl[:5] == math.inf).all() and (got.loss[:5] == math.inf).all()
+        assert torch.equal(got.grad[:5], without.grad[:5]) and torch.isfinite(got.grad).all() and (got.grad[out] == 0).all()
+    s["ref"][5:] = got.logprob[5:] + 80.0  # a large one that is not: held to the same bounds as any
+    assert torch.isfinite(held(torch, {k: x[5:] for k, x in s.items()}, "80", kl=0.05, eta=0.01, scale=scale).loss).all()
