@@ -185,7 +185,9 @@ jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld,
  * and has no gradient. Rows without a token that can occur, NaN
  * among the logits and targets >= vocab: as in jf_op_token_logprobs (the loss of the last is NaN, its gradient 0). A ratio
  * beyond the range of fp32 is infinite, as loss and gradient then are where A is negative; a logit whose token has probability 0 (in
- * fp32, below 2^-126 of the row's most likely one) has gradient 0 all the same, unless it is the target.
+ * fp32, below 2^-126 of the row's most likely one) has gradient 0 all the same, unless it is the target. A NaN in what a
+ * row's loss is made of (old_logprob, advantage, weight, ref_logprob with kl, lp) makes loss and gradient NaN, the latter at tokens that can
+ * occur; NaN among the logits makes the gradient NaN also where the loss does not depend on lp (no old_logprob).
  * workspace: device, 16-byte aligned, no initialisation needed; calls that may overlap on the GPU need one each. (0 bytes but for
  * rows longer than a cluster's shared memory, 460,800 fp32 or 921,600 bf16 values.) */
 typedef struct {

@@ -39,7 +39,7 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
   const float free = A == 0.f ? 0.f : r.ratio * A, held = A == 0.f ? 0.f : fminf(fmaxf(r.ratio, 1.f - a.t.below), 1.f + a.t.above) * A;
   float sum = free <= held ? -free : -held;
   r.g = free <= held ? -free : 0.f;
-  if (!(free <= held) && !(held < free)) sum = free - held;  // (not a number)
+  if (!(free <= held) && !(held < free)) sum = r.g = free - held;  // (not a number: neither is the gradient)
   r.kl = 0.f;
   if (a.ref_lp) {
     const float d = ref - lp, e = expm1f(d);

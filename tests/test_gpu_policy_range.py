@@ -128,3 +128,25 @@ def test_an_infinite_kl_has_no_gradient(torch, dtype, vocab, scale):
         assert torch.equal(got.grad[:5], without.grad[:5]) and torch.isfinite(got.grad).all() and (got.grad[out] == 0).all()
     s["ref"][5:] = got.logprob[5:] + 80.0  # a large one that is not: held to the same bounds as any
     assert torch.isfinite(held(torch, {k: x[5:] for k, x in s.items()}, "80", kl=0.05, eta=0.01, scale=scale).loss).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", LONG)
+def test_terms_that_are_no_numbers_reach_the_gradient(torch, dtype, vocab):
+    """A loss of NaN goes with a gradient of NaN (at tokens that can occur), also without KL and entropy terms; a row's neighbours
+    keep theirs."""
+    dtype = getattr(torch, dtype)
+    s, out = masked(torch, dtype, vocab)
+    clean = call(torch, s, kl=0.0, eta=0.0)
+    s["old"][1] = math.nan
+    s["adv"][2] = math.nan
+    s["logits"][3, 5] = math.nan
+    s["logits"][4, vocab - 1] = math.inf
+    s["weight"][5] = math.nan
+    for eta in (0.0, 0.01):
+        got = call(torch, s, kl=0.0, eta=eta)
+        for row in range(1, 6):
+            assert math.isnan(got.loss[row]) and torch.isnan(got.grad[row, :8]).all(), row
+        assert not torch.isnan(got.loss[[0, 6, 7]]).any() and not torch.isnan(got.grad[[0, 6, 7]]).any()
+        if eta == 0:
+            assert torch.equal(got.grad[[0, 6, 7]], clean.grad[[0, 6, 7]])
