@@ -408,8 +408,8 @@ constexpr int LP_GRAD_VECS = 4;  // vectors per thread
 // CTA (row, run of LP_GRAD_VECS x 256 vectors); the first run's CTA takes the row's edges too. Bound by the bytes, each
 // logit read and each gradient written once with four vectors of a thread in flight: 512 rows of 152,064 fp32 logits
 // (623 MB) take 94 us, 6.6 TB/s.
-// ANY_SIZE: g and h may be infinite (the policy loss's).
-template <typename T, bool ANY_SIZE>
+// POLICY: g and h may be infinite, and a row whose g and h are 0 holds anything.
+template <typename T, bool POLICY>
 __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams a) {
   constexpr int N = Vec<T>::N;
   pdl_launch_dependents();
@@ -425,10 +425,10 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_grad(const LpGradParams
     if (threadIdx.x == 0 && seg == 0) jf_set_error(a.err, JF_DERR_BOUNDS);
     g = 0.f;
   }
-  const bool none = m == -INFINITY && ls == -INFINITY;
+  const bool none = (m == -INFINITY && ls == -INFINITY) || (POLICY && g == 0.f && gh == 0.f);
   auto of = [&](float x, int i) {
     const float lp = fmaf(x - m, a.scale, -ls), p = ex2_ftz(lp * LOG2E);
-    if (ANY_SIZE) return none ? 0.f : a.scale * policy_grad(p, lp, H, g, gh, i == target);
+    if (POLICY) return none ? 0.f : a.scale * policy_grad(p, lp, H, g, gh, i == target);
     // -g p - gh p (lp + H), the logit of probability 0 without its infinite lp
     const float share = g + gh * (fmaxf(lp, -1e4f) + H);
     return none ? 0.f : a.scale * ((i == target ? g : 0.f) - p * share);
@@ -528,7 +528,7 @@ extern "C" jf_status jf_op_token_logprobs(int dtype, const void* logits, long lo
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 
-template <bool ANY_SIZE>
+template <bool POLICY>
 static jf_status logprobs_grad(int dtype, const void* logits, long long ld, int rows, int vocab, float scale, const int32_t* targets, const float* row_stats,
                                const float* entropy, const float* grad_logprob, const float* grad_entropy, void* grad_logits, long long ld_grad,
                                int* err_word, cudaStream_t st) {
@@ -544,7 +544,7 @@ static jf_status logprobs_grad(int dtype, const void* logits, long long ld, int 
                           grad_logits, err_word};
   const long long grid = (long long)rows * segs;
   if (grid > 0x7fffffffll) return JF_EUNSUPPORTED;
-  const cudaError_t e = dtype == JF_BF16 ? lp_launch(k_logprobs_grad<bf16, ANY_SIZE>, grid, st, a) : lp_launch(k_logprobs_grad<float, ANY_SIZE>, grid, st, a);
+  const cudaError_t e = dtype == JF_BF16 ? lp_launch(k_logprobs_grad<bf16, POLICY>, grid, st, a) : lp_launch(k_logprobs_grad<float, POLICY>, grid, st, a);
   return e == cudaSuccess ? JF_OK : JF_ECUDA;
 }
 

@@ -123,7 +123,7 @@ JF_DEV F2 fma2(F2 a, F2 b, F2 c) {
   return r;
 }
 
-// jf_op_token_logprobs_grad (jf_logprobs.cu) for g and gh of any size.
+// jf_op_token_logprobs_grad (jf_logprobs.cu) for g and gh of any size; rows where both are 0 get 0 whatever their logits hold.
 jf_status policy_long_grad(int dtype, const void* logits, long long ld, int rows, int vocab, float scale, const int32_t* targets, const float* row_stats,
                            const float* entropy, const float* g, const float* gh, void* grad_logits, long long ld_grad, int* err_word, cudaStream_t st);
 

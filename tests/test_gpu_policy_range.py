@@ -150,3 +150,21 @@ def test_terms_that_are_no_numbers_reach_the_gradient(torch, dtype, vocab):
         assert not torch.isnan(got.loss[[0, 6, 7]]).any() and not torch.isnan(got.grad[[0, 6, 7]]).any()
         if eta == 0:
             assert torch.equal(got.grad[[0, 6, 7]], clean.grad[[0, 6, 7]])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", LONG)
+def test_rows_that_are_left_out_hold_anything(torch, dtype, vocab):
+    """A negative target or a weight of 0 makes a row's gradient 0 where its logits, its advantage or its old and reference log
+    probabilities are NaN or infinite."""
+    dtype = getattr(torch, dtype)
+    s, _ = masked(torch, dtype, vocab)
+    z = s["logits"]
+    s["targets"][:4], s["weight"][4:] = -1, 0.0
+    for row, bad in ((0, math.nan), (1, math.inf), (2, math.nan), (4, math.nan), (5, math.inf), (6, math.nan)):
+        z[row, 2], z[row, vocab - 1], z[row, vocab // 2] = bad, bad, bad
+    z[2], z[6] = math.nan, math.nan
+    for name in ("old", "ref", "adv"):
+        s[name][3], s[name][7] = math.nan, math.nan
+    got = call(torch, s, kl=0.05, eta=0.01)
+    assert (got.grad == 0).all() and (got.loss == 0).all()
