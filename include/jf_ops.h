@@ -189,7 +189,7 @@ jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld,
  * row's loss is made of (old_logprob, advantage, weight, ref_logprob with kl, lp) makes loss and gradient NaN, the latter at tokens that can
  * occur; NaN among the logits makes the gradient NaN also where the loss does not depend on lp (no old_logprob).
  * workspace: device, 16-byte aligned, no initialisation needed; calls that may overlap on the GPU need one each. (0 bytes but for
- * rows longer than a cluster's shared memory, 460,800 fp32 or 921,600 bf16 values.) */
+ * rows longer than a cluster's shared memory, 230,400 fp32 or 460,800 bf16 values.) */
 typedef struct {
   float below, above; /* how far the ratio counts on either side of 1: 0 <= below <= 1, 0 <= above */
   float kl, entropy;  /* factors of the two other terms */

@@ -168,3 +168,14 @@ def test_rows_that_are_left_out_hold_anything(torch, dtype, vocab):
         s[name][3], s[name][7] = math.nan, math.nan
     got = call(torch, s, kl=0.05, eta=0.01)
     assert (got.grad == 0).all() and (got.loss == 0).all()
+
+
+@pytest.mark.parametrize("first", [0, 1, 3])
+@pytest.mark.parametrize("dtype,vocab", [("float32", v) for v in (230400, 230403, 230404)] + [("bfloat16", v) for v in (460800, 460807, 460808)])
+def test_both_sides_of_the_longest_row_of_one_kernel(torch, dtype, vocab, first):
+    """Rows that fill a cluster's shared memory to the last vector, with elements beside it, and the first that do not fit."""
+    s = make(torch, 3, vocab, getattr(torch, dtype), seed=22, pad=1, first=first, masked=True)
+    held(torch, s, vocab, kl=0.05, eta=0.01, scale=1.0)
+    want = call(torch, s)
+    got = call(torch, s, out=s["logits"])
+    assert torch.equal(got.grad, want.grad) and all(torch.equal(a, b) for a, b in zip(got[:5], want[:5]))
