@@ -60,6 +60,25 @@ def _on_stream(call):
     return wrapped
 
 
+def _zero_word(device):
+    """An error word that is 0 for every stream of the device, its current one. In a call that is being captured it is made outside of the
+    graph: on a stream of its own, in a mode of this thread that lets it wait for that stream."""
+    if not torch.cuda.is_current_stream_capturing():
+        word = torch.zeros(1, dtype=torch.int32, device=device)
+        torch.cuda.current_stream(device).synchronize()
+        return word
+    exchange, mode = C.CDLL("libcuda.so.1").cuThreadExchangeStreamCaptureMode, C.c_int(2)  # CU_STREAM_CAPTURE_MODE_RELAXED
+    _want(exchange(C.byref(mode)) == 0, "the first call on a device cannot be captured here")
+    try:
+        stream = torch.cuda.Stream(device)
+        with torch.cuda.stream(stream):
+            word = torch.zeros(1, dtype=torch.int32, device=device)
+        stream.synchronize()
+    finally:
+        exchange(C.byref(mode))  # (what it was)
+    return word
+
+
 def _take_error(word) -> int:
     """The code in an error word, once all of its device's streams are done; the word is clear for each of them after."""
     torch.cuda.synchronize(word.device)

@@ -15,7 +15,7 @@ from typing import NamedTuple
 import torch
 
 from . import _lib as J
-from .kv8 import _checked, _dtype, _on_current, _on_stream, _raw_stream, _row_stride, _take_error, _want
+from .kv8 import _checked, _dtype, _on_current, _on_stream, _raw_stream, _row_stride, _take_error, _want, _zero_word
 
 _err = {}  # error word by device
 
@@ -32,9 +32,7 @@ class TokenLogprobs(NamedTuple):
 def _error_word(device):
     word = _err.get(device)
     if word is None:
-        word = torch.zeros(1, dtype=torch.int32, device=device)
-        torch.cuda.current_stream(device).synchronize()  # zero for every stream
-        word = _err.setdefault(device, word)  # (the first of several threads')
+        word = _err.setdefault(device, _zero_word(device))  # (the first of several threads')
     return word
 
 

@@ -18,7 +18,7 @@ from dataclasses import dataclass
 import torch
 
 from . import _lib as J
-from .kv8 import _Fixed, _checked, _device_i32, _dtype, _on_current, _on_stream, _raw_stream, _take_error, _want
+from .kv8 import _Fixed, _checked, _device_i32, _dtype, _on_current, _on_stream, _raw_stream, _take_error, _want, _zero_word
 
 _err = {}  # error word by device
 
@@ -36,7 +36,7 @@ class Packed(_Fixed):
     def __post_init__(self):
         _device_i32(self.row_start, 2, "row_start")
         self.c = J.Packed(self.row_start.data_ptr(), self.row_start.numel() - 1, self.n_rows, self.max_rows)
-        _error_word(self.row_start.device)  # (the first call may be a captured one, which cannot wait for it)
+        _error_word(self.row_start.device)
 
     @classmethod
     def of(cls, lengths, n_rows=None, max_rows=None, device="cuda"):
@@ -51,9 +51,7 @@ class Packed(_Fixed):
 def _error_word(device):
     word = _err.get(device)
     if word is None:
-        word = torch.zeros(1, dtype=torch.int32, device=device)
-        torch.cuda.current_stream(device).synchronize()  # zero for every stream
-        word = _err.setdefault(device, word)  # (the first of several threads')
+        word = _err.setdefault(device, _zero_word(device))  # (the first of several threads')
     return word
 
 

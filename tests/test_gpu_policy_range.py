@@ -179,3 +179,34 @@ def test_both_sides_of_the_longest_row_of_one_kernel(torch, dtype, vocab, first)
     want = call(torch, s)
     got = call(torch, s, out=s["logits"])
     assert torch.equal(got.grad, want.grad) and all(torch.equal(a, b) for a, b in zip(got[:5], want[:5]))
+
+
+@pytest.mark.parametrize("which", ["token_logprobs", "policy_loss"])
+def test_a_first_call_that_is_captured(torch, monkeypatch, which):
+    """The error word of a device is there before the call that a graph keeps, and reports what a replay met."""
+    from paper_2512_14681_gb300 import _lib as J
+    from paper_2512_14681_gb300 import logprobs as L
+
+    s = make(torch, 4, 300, torch.float32, seed=23)
+    run = (lambda: call(torch, s)) if which == "policy_loss" else (lambda: L.token_logprobs(s["logits"], s["targets"]))
+    want = run()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(L, "_err", {})
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    graph.replay()
+    L.check()
+    for a, b in zip(got, want):
+        assert a is b is None or torch.equal(a, b)
+    s["targets"][1] = 300
+    graph.replay()
+    with pytest.raises(J.JfError, match="vocabulary"):
+        L.check()
+    L.check()
+    del graph, got  # the word outlives the graph
+    torch.cuda.empty_cache()
+    run()
+    with pytest.raises(J.JfError, match="vocabulary"):
+        L.check()
+    L.check()
