@@ -38,15 +38,15 @@ def _error_word(device):
 
 def check(device=None):
     """Raise what the device has reported since the last check (waits for all of its streams), and clear it: a target
-    beyond the vocabulary."""
+    beyond the vocabulary, a wait that ran out."""
     device = torch.device("cuda" if device is None else device)
     if device.index is None:
         device = torch.device(device.type, torch.cuda.current_device())
     word = _err.get(device)
-    if word is None:
-        return
-    if _take_error(word):
-        raise J.JfError(J.JF_EDEVICE, "a target was beyond the vocabulary")
+    code = _take_error(word) if word is not None else 0
+    if code:
+        what = {4: "a target was beyond the vocabulary", 1: "a copy's wait ran out"}
+        raise J.JfError(J.JF_EDEVICE if code == 4 else J.JF_ETIMEOUT, what.get(code, f"device code {code}"))
 
 
 @functools.lru_cache(maxsize=4096)

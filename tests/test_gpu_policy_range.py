@@ -210,3 +210,17 @@ def test_a_first_call_that_is_captured(torch, monkeypatch, which):
     with pytest.raises(J.JfError, match="vocabulary"):
         L.check()
     L.check()
+
+
+def test_check_names_what_was_reported(torch, monkeypatch):
+    """A wait that ran out is not a target beyond the vocabulary. (The codes are written into the word by hand.)"""
+    from paper_2512_14681_gb300 import _lib as J
+    from paper_2512_14681_gb300 import logprobs as L
+
+    dev = torch.device("cuda", torch.cuda.current_device())
+    for code, status, what in ((4, J.JF_EDEVICE, "vocabulary"), (1, J.JF_ETIMEOUT, "wait")):
+        L._error_word(dev).fill_(code)
+        with pytest.raises(J.JfError, match=what) as e:
+            L.check()
+        assert e.value.status == status
+        L.check()
