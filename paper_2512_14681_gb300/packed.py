@@ -78,7 +78,7 @@ def _need(n_seqs, n_rows, max_rows, dtype, heads, kv_heads, head_dim, backward, 
 
 def _row_stride(shape, stride, n, name):
     """Of [n][heads][head_dim] values."""
-    _want(len(shape) == 3 and shape[0] == n and stride[2] == 1 and stride[1] == shape[2], "{}: [{}][heads][head_dim] with contiguous heads is wanted", name, n)
+    _want(len(shape) == 3 and shape[0] == n and stride[2] == 1 and (stride[1] == shape[2] or shape[1] == 1), "{}: [{}][heads][head_dim] with contiguous heads is wanted", name, n)
     width = shape[1] * shape[2]
     if n <= 1:
         return width  # (one row's stride may be anything)
