@@ -236,7 +236,9 @@ jf_status jf_op_packed_attention(const jf_packed* texts, int dtype, const void* 
  * the same texts, q, k, v and scale and that call's out and lse. dq, dk, dv: rows ld_* elements apart (so that they may be
  * parts of one buffer's rows); they may not overlap the inputs or one another. dk and dv of a KV head are sums over its query heads. No
  * atomics: the order of every sum is fixed. JF_BF16 rounds probabilities and the scores' gradients to bf16 before their products
- * (the latter to two terms for dq in a text's first quarter and its first 512 rows, whose gradients are the largest). */
+ * (the latter to two terms for dq in a text's first quarter and its first 512 rows, whose gradients are the largest), and takes the
+ * product of d_out and out, which the scores' gradients contain, from out as given for dq of a text's rows with more than 128 keys, exactly
+ * otherwise. For bf16 rows that tensor copies cannot read none of these is rounded. */
 jf_status jf_op_packed_attention_grad(const jf_packed* texts, int dtype, const void* q, long long ld_q, const void* k,
                                       long long ld_k, const void* v, long long ld_v, int n_heads, int n_kv_heads, int head_dim,
                                       float scale, const void* out, const float* lse, const void* d_out, long long ld_do,

@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 4 : 2) k_packed_attn(co
   pf_join_end(parts);
 }
 
-// delta[row][head] = d_out . out, a warp per (row, head); rows of no text as well (their d_out may be anything: not used).
+// delta[row][head] = d_out . out of fp32 rows, a warp per (row, head); rows of no text as well (their d_out may be anything: not used).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) k_packed_delta(const PackedParams a) {
   pdl_launch_dependents();
@@ -396,8 +396,10 @@ __global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 2 : 1) k_packed_dkv(con
   pf_join_end(parts);
 }
 
-// Grid (tiles of queries x parts, query heads): dq.
-template <typename T, int HD>
+// Grid (tiles of queries x parts, query heads): dq. DELTA: delta instead, as sum_j p_ij (d_out_i . v_j), for bf16 outputs: that of a rounded out
+// is off by 2^-9 of its terms, which counts where a row sees few keys (texts of two rows: dq off by 3.2e-3 of its norm instead of its
+// own rounding's 1.66e-3, dk alike; 300 rows: 1.86e-3). Two more products to the seven of the pass.
+template <typename T, int HD, bool DELTA>
 __global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 2 : 1) k_packed_dq(const PackedParams a) {
   extern __shared__ float sm[];
   constexpr int TILE = PF_T * (HD + 4), OWN = PF_OWN * (HD + 4);
@@ -409,7 +411,8 @@ __global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 2 : 1) k_packed_dq(cons
   T* dq = reinterpret_cast<T*>(a.dq);
   const int parts = (int)cluster_ctas(), part = (int)cluster_rank();
   const PfTile t = pf_tile(a, blockIdx.x / parts, [&](int r) {
-    for (int d = tid; d < HD; d += PF_THREADS) dq[r * a.ld_dq + h * HD + d] = to_act<T>(0.f);
+    if constexpr (!DELTA)
+      for (int d = tid; d < HD; d += PF_THREADS) dq[r * a.ld_dq + h * HD + d] = to_act<T>(0.f);
   });
   if (t.n < 0) return;
   const int rows = min(PF_OWN, t.n - t.first);
@@ -417,10 +420,10 @@ __global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 2 : 1) k_packed_dq(cons
   pf_load<T, HD, PF_OWN>(sdo, reinterpret_cast<const T*>(a.d_out) + (t.row0 + t.first) * a.ld_do + h * HD, a.ld_do, rows, pf_by16<T>(a.d_out, a.ld_do));
   if (tid < rows) {
     s_lse[tid] = a.lse[(long long)(t.row0 + t.first + tid) * a.Hq + h] * kLog2e;
-    s_delta[tid] = a.delta[(long long)(t.row0 + t.first + tid) * a.Hq + h];
+    s_delta[tid] = DELTA ? 0.f : a.delta[(long long)(t.row0 + t.first + tid) * a.Hq + h];
   }
   const bool k16 = pf_by16<T>(a.k, a.ld_k), v16 = pf_by16<T>(a.v, a.ld_v);
-  float g[PF_R][HD / 16] = {};
+  float g[PF_R][HD / 16] = {}, sum = 0.f;  // (sum: of 16 columns of row tid / 4)
   for (int k0 = part * PF_T; k0 < t.first + rows; k0 += parts * PF_T) {
     __syncthreads();
     pf_load<T, HD, PF_T>(sk, reinterpret_cast<const T*>(a.k) + (t.row0 + k0) * a.ld_k + kvh * HD, a.ld_k, min(PF_T, t.n - k0), k16);
@@ -428,9 +431,28 @@ __global__ void __launch_bounds__(PF_THREADS, HD == 64 ? 2 : 1) k_packed_dq(cons
     __syncthreads();
     pf_back_tile<HD, PF_R, PF_T / 16>(sq, sdo, sk, sv, s_lse, s_delta, t.first, k0, t.n, a.scale * kLog2e, ty, tx, nullptr, sds);
     __syncthreads();
-    pf_rows_by<HD>(sds, sk, ty, tx, g);
+    if constexpr (DELTA) {
+      static_assert(PF_THREADS == 4 * PF_OWN && PF_T == 64);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) sum += sds[(tid >> 2) * (PF_T + 4) + 16 * (tid & 3) + x];
+    } else {
+      pf_rows_by<HD>(sds, sk, ty, tx, g);
+    }
   }
   __syncthreads();
+  if constexpr (DELTA) {
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+    if ((tid & 3) == 0) sk[tid >> 2] = sum;
+    pf_join_begin(parts);
+    if (part == 0 && tid < rows) {
+      sum = 0.f;
+      for (int k = 0; k < parts; ++k) sum += ld_cluster(map_to_rank(smem_u32(sk), k) + 4 * tid);
+      a.delta[(long long)(t.row0 + t.first + tid) * a.Hq + h] = sum;
+    }
+    pf_join_end(parts);
+    return;
+  }
   pf_put<HD>(sk, ty, PF_Y, tx, g);
   pf_join_begin(parts);
   const int mine = PF_OWN / parts;
@@ -458,7 +480,10 @@ template <typename T, int HD>
 cudaError_t pf_prepare() {
   cudaError_t e = cudaFuncSetAttribute(k_packed_attn<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_attn<HD>);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dkv<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_dkv<HD>);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_dq<HD>);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq<T, HD, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_dq<HD>);
+  if constexpr (sizeof(T) == 2) {
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_packed_dq<T, HD, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, pf_smem_dq<HD>);
+  }
   return e;
 }
 PerDeviceOnce g_pf_once;
@@ -493,9 +518,11 @@ template <typename T, int HD>
 cudaError_t pf_backward(const PackedParams& a, cudaStream_t st) {
   const long long warps = (long long)a.t.n_rows * a.Hq;
   const int kv = pf_parts(a.t, a.Hkv, pf_steps(a.t) * (a.Hq / a.Hkv)), q = pf_parts(a.t, a.Hq, pf_steps(a.t));
-  cudaError_t e = packed_launch(k_packed_delta<T, HD>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a);
+  cudaError_t e;
+  if constexpr (sizeof(T) == 2) e = packed_launch_clusters(k_packed_dq<T, HD, true>, q, dim3(pf_tiles(a.t) * q, a.Hq), dim3(PF_THREADS), pf_smem_dq<HD>, st, a);
+  else e = packed_launch(k_packed_delta<T, HD>, dim3((unsigned)((warps + 7) / 8)), dim3(256), 0, st, a);
   if (e == cudaSuccess) e = packed_launch_clusters(k_packed_dkv<T, HD>, kv, dim3(pf_tiles(a.t) * kv, a.Hkv), dim3(PF_THREADS), pf_smem_dkv<HD>, st, a);
-  if (e == cudaSuccess) e = packed_launch_clusters(k_packed_dq<T, HD>, q, dim3(pf_tiles(a.t) * q, a.Hq), dim3(PF_THREADS), pf_smem_dq<HD>, st, a);
+  if (e == cudaSuccess) e = packed_launch_clusters(k_packed_dq<T, HD, false>, q, dim3(pf_tiles(a.t) * q, a.Hq), dim3(PF_THREADS), pf_smem_dq<HD>, st, a);
   return e;
 }
 
