@@ -59,6 +59,8 @@ def _need(rows, vocab, top):
 def _logits(t, name="logits"):
     _want(t.is_cuda and t.dim() == 2 and t.shape[1] >= 1 and (t.stride(1) == 1 or t.shape[1] == 1),
           "{}: CUDA [rows][vocab] with contiguous rows is wanted", name)
+    if max(t.shape) > 0x7fffffff:  # (C's int would take what is left of it modulo 2^32)
+        raise J.JfError(J.JF_EUNSUPPORTED, f"{name}: {tuple(t.shape)}: at most 2^31 - 1 rows and values are taken")
     return _row_stride(t, t.shape[1], name)
 
 
