@@ -82,3 +82,24 @@ def test_norms(torch, lens, heads, copies):
     for name, (off, by_rounding) in distances(torch, lens, q, k, v, d, scale, got, copies).items():
         print(f"{name} {off:.3e} {by_rounding:.3e}")
         assert off <= 1.08 * by_rounding, (name, off, by_rounding)
+
+
+@pytest.mark.parametrize("heads", [(12, 2, 128, "f32"), (4, 2, 64, "f32")], ids=lambda h: "%d-%d-%d-%s" % h)
+@pytest.mark.parametrize("lens", BATCHES, ids=lambda v: "-".join(map(str, v[:4])))
+def test_norms_in_32_bits(torch, lens, heads):
+    """A sum of m terms in fp32 is off by sqrt(m) u of its terms' norm where each addition's rounding has a sign of its own (u = 2^-24), and what a
+    score is off by multiplies its probability. Scores, dp and delta are sums of head_dim terms, the outputs of n times the heads of a group
+    at most: sqrt(head_dim) u of scores and sqrt(n G) u of the outputs. Scores of up to 6 times their norm in the rows that count make that six
+    times as much in the exponent; the sum of both, doubled for delta, is allowed."""
+    from paper_2512_14681_gb300 import packed as P
+
+    scale = heads[2] ** -0.5
+    (q, k, v, d), _ = make(torch, heads, lens, seed=32)
+    texts = texts_of(torch, lens)
+    out, lse = P.attention(texts, q, k, v, scale, want_lse=True)
+    got = (out, lse, *P.attention_grad(texts, q, k, v, out, lse, d, scale))
+    P.check()
+    allowed = 2 * (6 * math.sqrt(heads[2]) + math.sqrt(max(lens) * heads[0] // heads[1])) * 2.0 ** -24
+    for name, (off, _) in distances(torch, lens, q, k, v, d, scale, got, False).items():
+        print(f"{name} {off:.3e} {allowed:.3e}")
+        assert off <= allowed, (name, off, allowed)
