@@ -68,7 +68,7 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 //   lp = scale (x_t - m) - ln 2 (log2 S + b - c m),  H = ln 2 (log2 S - T / S),  p = 2^y / S,
 //   dloss/dx = -scale / S 2^y (g + gh (H - ln S) + gh ln 2 y), + scale g at the target.
 // b is off from c m by up to 2^-24 of it, which every 2^y of the thread takes as a factor: within 2 where |c m| is below 2^24 (PL_NEAR; beyond
-// 2^31 S would leave fp32's range). Sums of a row whose largest logit lies further out (or is beyond 1e29, or has a c above 1e6) are taken
+// 2^31 S would leave fp32's range). Sums of a row whose largest logit lies further out (or is beyond 1e38, or has a c above 1e6) are taken
 // again from differences x - m. A logit so far below the largest that 2^y is 0 (PL_BELOW) counts as one at that distance, so that y, and its
 // products with what an entropy term gives, stay in fp32's range whatever the mask and the scale are.
 //
@@ -80,7 +80,7 @@ constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8;
 constexpr int PL_FIT[3] = {56832, 76288, 115200};  // bytes of a CTA's run with which four, three, two are resident on an SM
 constexpr int PL_MOST = PL_FIT[2];
 constexpr int PL_ROWS = 1 << 30;  // (a row and the step to the next fit 31 bits)
-constexpr float PL_FAR = 1e30f, PL_BELOW = 400.f, PL_LARGE = 1e29f, PL_STEEP = 1e6f, PL_NEAR = 16777216.f, LN2 = 0.69314718055994531f;
+constexpr float PL_FAR = 1e30f, PL_BELOW = 400.f, PL_LARGE = 1e38f, PL_STEEP = 1e6f, PL_NEAR = 16777216.f, LN2 = 0.69314718055994531f;
 constexpr float LOG2E_LO = 1.9259630e-8f;  // log2 e beyond LOG2E
 
 JF_DEV float warp_max(float v) {
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(PL_THREADS, 4) k_policy(const PolicyParams a) 
         // but for d's square. (KL is small where lp is near ref_logprob, and would show the rounding.)
         const float d = fmaf(a.scale, LOG2E_LO, fmaf(a.scale, LOG2E, -c)) / c;
         const float apart = far ? 0.f : fmaf(d, st.t / st.s, -fmaf(m, c, -st.m));
-        lp = empty ? -INFINITY : fmaf(x_t - m, a.scale, -LN2 * (l2 + apart));
+        lp = empty ? -INFINITY : fmaf(0.5f * x_t - 0.5f * m, 2.f * a.scale, -LN2 * (l2 + apart));  // (x_t - m may pass fp32's range)
       }
       const PolicyRow p = policy_row(a, target, lp, H, in.old, in.ref, in.A, in.w);
       if (lane == 0) {

@@ -78,6 +78,33 @@ def test_masks_at_any_scale(torch, dtype, scale, vocab):
     assert (got.grad[z == -math.inf] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("scale", [1e-28, 3e-28, 1e-20, 1.0, 1e5])
+@pytest.mark.parametrize("vocab", [11, 5001, 300001, 470001])
+def test_small_logits_beside_large_ones(torch, dtype, scale, vocab):
+    """Rows of scores around -9, 0 and 9 whose every 16-byte vector but one lies 10 to 40 lower: what they add counts, at any scale. Targets
+    that are the type's lowest value are as far as they are."""
+    dtype = getattr(torch, dtype)
+    scale = torch.tensor(scale, dtype=torch.float32).item()
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    z = -10 - 30 * torch.rand(6, vocab, generator=g, device="cuda", dtype=torch.float64)
+    z[:, :4] = torch.rand(6, 4, generator=g, device="cuda", dtype=torch.float64)
+    z += torch.tensor([-9, 0, 9, -9, 0, 9], device="cuda")[:, None]
+    z = (z / scale).to(dtype)
+    target = torch.tensor([0, 1, 2, 3, 0, 5], device="cuda")
+    z[5, 5] = torch.finfo(dtype).min
+    lp = torch.log_softmax(apart(z) * scale, 1).gather(1, target[:, None])[:, 0]
+    s = on(torch, z, target.int(), old=(lp + 0.05).float(), ref=(lp - 0.1).float(), adv=torch.tensor([1.0, -1.0, 0.5, 2.0, 0.0, 1.0], device="cuda"))
+    first = {k: x[:5] for k, x in s.items()}
+    held(torch, first, scale, kl=0.05, eta=0.1, scale=scale)
+    got, want = call(torch, s, kl=0.0, eta=0.0, scale=scale).logprob[5].item(), lp[5].item()
+    assert abs(got - want) <= 8 * U * abs(want) + 2.0 ** -18 or (want < -3.4e38 and got == -math.inf), (got, want)
+    if vocab < 200000 and scale < 1e-20:  # a target as far below as the type goes
+        z[5, 1] = 2e38
+        got, want = call(torch, s, kl=0.0, eta=0.0, scale=scale).logprob[5].item(), (z[5, 5].double() - z[5, 1].double()).item() * scale
+        assert abs(got - want) <= 8 * U * abs(want), (got, want)
+
+
 def masked(torch, dtype, vocab, first=1):
     """Rows at an odd address, a third of them masked out by -infinity and by the type's lowest value, on tokens from 8 on."""
     s = make(torch, 8, vocab, dtype, seed=21, pad=2, first=first, masked=True)
