@@ -171,8 +171,9 @@ jf_status jf_op_token_logprobs_grad(int dtype, const void* logits, long long ld,
                                     const float* grad_logprob, const float* grad_entropy, void* grad_logits,
                                     long long ld_grad, int* err_word, void* cuda_stream);
 
-/* The clipped policy loss of given tokens, and its gradient. Logits, scale (here 1e-28 <= scale <= 1e30: below, a logit far
- * under the others could not be told from one of -infinity) and targets as in jf_op_token_logprobs; with lp the target's log probability, x = lp - old_logprob, ratio = e^x, A = advantage, d = ref_logprob - lp, H the row's entropy,
+/* The clipped policy loss of given tokens, and its gradient. Logits, scale (here 1e-28 <= scale <= 1e30: below, masked
+ * logits could not be told from the others) and targets as in jf_op_token_logprobs; with lp the target's log probability,
+ * x = lp - old_logprob, ratio = e^x, A = advantage, d = ref_logprob - lp, H the row's entropy,
  *   loss = weight * (-min(ratio * A, min(max(ratio, 1 - below), 1 + above) * A) + kl * (e^d - 1 - d) - entropy * H).
  * The gradient is that of the sum of all losses by the logits; where both sides of a min or max are equal, the ratio's own.
  * old_logprob NULL: ratio 1, with the gradient of lp; ref_logprob NULL: kl must be 0; weight NULL: 1. All device fp32 [rows].

@@ -6,9 +6,9 @@
 // rows G times sooner, and K and V are read once for G heads.
 //
 // What bounds a long text is the tensor core, and before it each stream's chain product -> softmax -> product; a short one, latency.
-// Measured with 28 heads of 128 on 4: forward of 16,384 rows 1.315 ms (1.46 PFLOP/s), 4,096 rows 110 us, 16 texts of up to 128 rows
-// (12 heads on 2) 10.6 us; backward of 8,192 rows 1.255 ms (0.96 PFLOP/s of the five products' work; seven are multiplied), 4 x 1,024
-// rows 151 us.
+// Measured with 28 heads of 128 on 4: forward of 16,384 rows 1.33 ms (1.45 PFLOP/s), 4,096 rows 112 us, 16 texts of up to 128 rows
+// (12 heads on 2) 10.8 us; backward of 8,192 rows 1.24 ms (0.97 PFLOP/s of the five products' work; seven are multiplied), 4 x 1,024
+// rows 151 us. (From run to run by up to 2%, 1,315 to 1,340 us: the figures beside a choice below are of one run each.)
 //
 // Work is a line of units, (text, KV head, tile), each as long as its steps (tiles of keys, or of query rows in dk and dv)
 // plus a constant for what a unit costs beside them; each CTA takes an equal run of that line. A unit that a run's end cuts leaves a
@@ -821,8 +821,8 @@ __global__ void __launch_bounds__(256) k_packed_delta_tc(const PackedParams a) {
 }
 
 // Whether a unit's ds goes into dq as two bf16 terms, the second what the first's rounding leaves: in a text's first quarter, and its first
-// 512 rows. Rows that see few keys have the largest gradients, and so the largest part in dq's error: 2.1e-3 of its norm instead of 2.4 to
-// 2.7e-3 (8,192 rows; 5 texts of up to 2,000), for one more product in a sixteenth of a long text's steps: 1,257 us for the pass over
+// 512 rows. Rows that see few keys have the largest gradients, and so the largest part in dq's error: 1.7e-3 (300 rows) to 2.0e-3 (2,000) of its norm
+// instead of 2.4e-3, for one more product in a sixteenth of a long text's steps: 1,257 us for the pass over
 // 8,192 rows, 1,228 without, others within 1%. (As if those steps were longer by two thirds in the line: 1,275.) (In the
 // first 1,024 rows of all texts: 1.9 to 2.0e-3, 4% of the pass for 4 x 1,024 rows.)
 JF_DEV bool two_terms(const Cut& c) { return c.n_steps <= max(4, c.n >> 9); }

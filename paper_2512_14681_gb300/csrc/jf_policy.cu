@@ -73,8 +73,9 @@ JF_DEV PolicyRow policy_row(const PolicyParams& a, int target, float lp, float H
 // products with what an entropy term gives, stay in fp32's range whatever the mask and the scale are.
 //
 // Bound by bytes where rows are many: 2,048 fp32 rows of 152,064 in 441 us (5.65 TB/s of logits in and gradients out, 0.84 of a copy);
-// bf16 ones, whose pairs take as many instructions for half the bytes, by issue: 512 rows in 68 us (4.6 TB/s), at an odd distance 70. A
-// row in registers instead of shared memory: 516 us; more CTAs a row than it takes to hold: 80 for 71.
+// bf16 ones, whose pairs take as many instructions for half the bytes, by waits between the three walks over a row (barriers 2.1, loads 1.9 warps
+// an issue; 55% of issue slots): 512 rows in 68 us (4.6 TB/s), at an odd distance 71. Without a gradient 41 us, 2,048 fp32
+// rows 297. A row in registers instead of shared memory: 516 us; more CTAs a row than it takes to hold: 80 for 71.
 // ---------------------------------------------------------------------------------------------
 constexpr int PL_THREADS = 256, PL_WARPS = PL_THREADS / 32, PL_CLUSTER = 8;
 constexpr int PL_FIT[3] = {56832, 76288, 115200};  // bytes of a CTA's run with which four, three, two are resident on an SM
@@ -535,7 +536,7 @@ extern "C" jf_status jf_op_policy_loss(const jf_policy_terms* terms, int dtype, 
       (!ref_logprob && terms->kl != 0.f) || (dtype != JF_F32 && dtype != JF_BF16) || rows < 0 || vocab < 1 || vocab > (1 << 30) || !err_word)
     return JF_EINVAL;
   if (rows > PL_ROWS) return JF_EUNSUPPORTED;
-  if (!(scale >= 1e-28f) || scale > 1e30f || ld < vocab) return JF_EINVAL;  // (2^(-1e30 scale log2 e) is 0)
+  if (!(scale >= 1e-28f) || scale > 1e30f || ld < vocab) return JF_EINVAL;  // (2^(-1e30 scale log2 e) is 0: differences are cut there)
   if (rows == 0) return JF_OK;
   const uintptr_t type_mask = dtype == JF_BF16 ? 1 : 3;
   if (!logits || ((uintptr_t)logits & type_mask) || !targets || !advantage) return JF_EINVAL;

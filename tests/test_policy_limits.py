@@ -16,7 +16,7 @@ def lib():
 
 
 def test_scales_that_masks_do_not_survive_are_refused(lib):
-    """A logit of -infinity counts as -1e30 where products are taken: 1e30 * scale * log2 e has to pass the 126 below which 2^-x is not 0.
+    """Logits that differ by more than 1e30 may count as that far apart: 1e30 * scale * log2 e has to pass the 126 up to which 2^-x is not 0.
     (No rows: what is not refused returns without a launch.)"""
     for scale in (9.9e-29, 1e-29, 1e-37, 1e-45, 0.0, -1.0, 1.1e30):
         assert policy(lib, n=0, scale=scale) == J.JF_EINVAL, scale
